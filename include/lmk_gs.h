@@ -361,6 +361,75 @@ int32_t lmk_gs_anchor_decode_culled(const lmk_gs_anchors *anchors, const lmk_gs_
                                     const lmk_gs_camera *cam, const float *box, uint8_t *anchor_visible,
                                     const lmk_gs_decoded *out, void *stream);
 
+/* ---- Perceptron layers whose weights belong to blocks of a scene, and their gradients.  A scene trained in
+ * blocks keeps its anchors in block order: block g owns the rows offsets[g] .. offsets[g+1]-1 of every array
+ * that has a row per anchor, and a weight matrix of its own.  Rows of no block (in front of offsets[0], from
+ * offsets[blocks] on) give zeros and enter no gradient.  A layer may keep its input in 8 bits for the backward
+ * pass (lmk_gs_checkpoint8), so that the input itself need not be held until then. */
+#define LMK_GS_F32 0u
+#define LMK_GS_BF16 1u
+
+typedef struct lmk_gs_linear {
+    const void *w;            /* block g: w + g * w_block elements; [n][k], rows ldw apart, or with in_major [k][n] */
+    const uint32_t *offsets;  /* [blocks + 1] device, ascending; values above `rows` count as `rows`               */
+    uint64_t ldw;             /* elements between the rows of a matrix: k (in_major: n) .. 2^28                      */
+    uint64_t w_block;         /* elements between two blocks' matrices, at most 2^40                               */
+    uint32_t blocks;          /* 1 .. 65536; a block may have no rows                                              */
+    uint32_t rows;            /* rows of x, y and their gradients (0 is allowed), below 2^31                       */
+    uint32_t n, k;            /* outputs and inputs of the layer, 1 .. 65536                                       */
+    uint32_t dtype;           /* LMK_GS_F32 or LMK_GS_BF16: type of w, x, y, dy and dx                             */
+    uint32_t in_major;        /* 0 or 1                                                                            */
+} lmk_gs_linear;
+
+/* The 8-bit form of a matrix of `rows` rows of k values, kp = k rounded up to 32: 32 consecutive values of a row
+ * share a power of two.  With A the largest |x| of the 32: the step is 2^e, e the least exponent >= -126 for which
+ * A / 2^e < 127.5, but at most 121; the code of x is x / 2^e rounded to the nearest integer (ties to even) of at most 127, +-1 where that
+ * would be 0 but x is not; the value a code stands for is code * 2^e, which a bfloat16 holds exactly.  Signs are kept
+ * exactly, a zero stays a zero.  scale = e + 127; 0 where all 32 are zero; 255 where one of the 32 is not finite
+ * (codes 0, all 32 read back as NaN).  Codes of the columns k .. kp-1 are 0.  Error: half a step, A / 127.5 at most
+ * (a whole step for values below half of one). */
+typedef struct lmk_gs_checkpoint8 {
+    int8_t *codes;            /* [rows][kp]       device, 16-byte aligned */
+    uint8_t *scale;           /* [rows][kp / 32]  device                  */
+} lmk_gs_checkpoint8;
+
+/* y[r][j] = act(sum_i x[r][i] w_g[j][i] + bias[g][j]) for the rows r of every block g; act: identity, or with relu
+ * max(., 0) (a NaN stays one).  Sums in 32 bits, one rounding to dtype.  ldx, ldy: elements between rows, at least
+ * k and n, at most 2^28.  bias: [blocks][n] float32 or NULL.  keep: NULL, or where the 8-bit form of x is written (zeros for rows
+ * of no block).  y must not overlap x or w.  Asynchronous on `stream`.  LMK_GS_ERR_INVALID: NULL pointer, size,
+ * stride or flag out of range, a pointer that is not aligned to its elements; LMK_GS_ERR_UNSUPPORTED: another dtype, too many tiles
+ * for one launch. */
+int32_t lmk_gs_grouped_linear(const lmk_gs_linear *layer, const void *x, uint64_t ldx, const float *bias,
+                              uint32_t relu, void *y, uint64_t ldy, const lmk_gs_checkpoint8 *keep, void *stream);
+
+/* Gradients of lmk_gs_grouped_linear without its act (dy: gradient of what act is applied to).  Any of dx, dw, db
+ * may be NULL; whole arrays are written, blocks without rows get zeros in dw and db. */
+typedef struct lmk_gs_linear_grads {
+    void *dx;        /* [rows][k], rows lddx apart, dtype: sum_j dy[r][j] w_g[j][i], and with gate only where x > 0    */
+    uint64_t lddx;
+    float *dw;       /* laid out as w, dense ([blocks][n][k] or [blocks][k][n]): sum over the block's rows dy[r][j] x[r][i] */
+    float *db;       /* [blocks][n]: sum over the block's rows of dy                                                   */
+} lmk_gs_linear_grads;
+
+/* Bytes of workspace of lmk_gs_grouped_linear_backward (partial sums of dw and db over runs of rows). */
+int32_t lmk_gs_grouped_linear_backward_bytes(const lmk_gs_linear *layer, size_t *bytes);
+
+/* The layer's input comes as x (rows ldx apart) or as its 8-bit form `kept`; dw and gate need one of the two and
+ * not both.  gate: dx is also taken through the ReLU that gave x, it is 0 where x <= 0 (NaN lets it pass).  Sums
+ * over a block's rows are taken in an order that depends on the sizes only: the same call gives the same bits.
+ * workspace: 256-byte aligned, not needed where dw and db are NULL.  Outputs must not overlap inputs.
+ * Errors as lmk_gs_grouped_linear; LMK_GS_ERR_CAPACITY: workspace too small. */
+int32_t lmk_gs_grouped_linear_backward(const lmk_gs_linear *layer, const void *dy, uint64_t lddy, const void *x,
+                                       uint64_t ldx, const lmk_gs_checkpoint8 *kept, uint32_t gate,
+                                       const lmk_gs_linear_grads *out, void *workspace, size_t workspace_bytes,
+                                       void *stream);
+
+/* x [rows][k], rows ldx apart, to its 8-bit form and back.  Asynchronous; errors as lmk_gs_grouped_linear. */
+int32_t lmk_gs_checkpoint8_pack(const void *x, uint64_t ldx, uint32_t rows, uint32_t k, uint32_t dtype,
+                                const lmk_gs_checkpoint8 *out, void *stream);
+int32_t lmk_gs_checkpoint8_unpack(const lmk_gs_checkpoint8 *kept, uint32_t rows, uint32_t k, uint32_t dtype,
+                                  void *x, uint64_t ldx, void *stream);
+
 /* Copies {pair count D, status} of the frame from scratch to the host.
  * Synchronises `stream`.  Either output pointer may be NULL. */
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream);

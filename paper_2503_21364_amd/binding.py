@@ -25,7 +25,9 @@ EXPORTS = ("lmk_gs_workspace_bytes", "lmk_gs_preprocess", "lmk_gs_bin_sort", "lm
            "lmk_gs_read_status", "lmk_gs_strerror", "lmk_gs_last_hip_error", "lmk_gs_version",
            "lmk_gs_index_build", "lmk_gs_preprocess_culled", "lmk_gs_build_cov3d", "lmk_gs_render_backward",
            "lmk_gs_preprocess_backward", "lmk_gs_anchor_decode", "lmk_gs_anchor_index_build",
-           "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static")
+           "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static", "lmk_gs_grouped_linear",
+           "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes", "lmk_gs_checkpoint8_pack",
+           "lmk_gs_checkpoint8_unpack")
 
 
 class Gaussians(C.Structure):
@@ -81,6 +83,20 @@ class Binned(C.Structure):
                 ("tile_order", C.c_void_p)]
 
 
+class LinearC(C.Structure):
+    _fields_ = [("w", C.c_void_p), ("offsets", C.c_void_p), ("ldw", C.c_uint64), ("w_block", C.c_uint64),
+                ("blocks", C.c_uint32), ("rows", C.c_uint32), ("n", C.c_uint32), ("k", C.c_uint32),
+                ("dtype", C.c_uint32), ("in_major", C.c_uint32)]
+
+
+class Checkpoint8C(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class LinearGrads(C.Structure):
+    _fields_ = [("dx", C.c_void_p), ("lddx", C.c_uint64), ("dw", C.c_void_p), ("db", C.c_void_p)]
+
+
 class LmkGsError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -123,6 +139,16 @@ def lib() -> C.CDLL:
                                                 C.c_void_p, C.c_void_p]
         l.lmk_gs_anchor_decode_culled.argtypes = [C.POINTER(Anchors), C.POINTER(AnchorDecoder), C.POINTER(Camera),
                                                   C.c_void_p, C.c_void_p, C.POINTER(Decoded), C.c_void_p]
+        l.lmk_gs_grouped_linear.argtypes = [C.POINTER(LinearC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint32,
+                                            C.c_void_p, C.c_uint64, C.POINTER(Checkpoint8C), C.c_void_p]
+        l.lmk_gs_grouped_linear_backward.argtypes = [C.POINTER(LinearC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64,
+                                                     C.POINTER(Checkpoint8C), C.c_uint32, C.POINTER(LinearGrads),
+                                                     C.c_void_p, C.c_size_t, C.c_void_p]
+        l.lmk_gs_grouped_linear_backward_bytes.argtypes = [C.POINTER(LinearC), C.POINTER(C.c_size_t)]
+        l.lmk_gs_checkpoint8_pack.argtypes = [C.c_void_p, C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32,
+                                              C.POINTER(Checkpoint8C), C.c_void_p]
+        l.lmk_gs_checkpoint8_unpack.argtypes = [C.POINTER(Checkpoint8C), C.c_uint32, C.c_uint32, C.c_uint32,
+                                                C.c_void_p, C.c_uint64, C.c_void_p]
         l.lmk_gs_read_status.argtypes = [C.c_void_p, C.POINTER(C.c_uint64), C.POINTER(C.c_int32), C.c_void_p]
         l.lmk_gs_strerror.argtypes = [C.c_int32]
         l.lmk_gs_strerror.restype = C.c_char_p
@@ -130,7 +156,9 @@ def lib() -> C.CDLL:
                      "lmk_gs_read_status", "lmk_gs_last_hip_error", "lmk_gs_index_build",
                      "lmk_gs_preprocess_culled", "lmk_gs_build_cov3d", "lmk_gs_render_backward",
                      "lmk_gs_preprocess_backward", "lmk_gs_anchor_decode", "lmk_gs_anchor_index_build",
-                     "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static"):
+                     "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static", "lmk_gs_grouped_linear",
+                     "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes",
+                     "lmk_gs_checkpoint8_pack", "lmk_gs_checkpoint8_unpack"):
             getattr(l, name).restype = C.c_int32
         l.lmk_gs_version.restype = C.c_uint32
         _lib = l
@@ -453,6 +481,141 @@ def anchor_decode_culled(anchors: AnchorScene, index: AnchorIndex, cam: Camera, 
                                            _stream_handle(stream))
     if rc != OK:
         raise LmkGsError(rc, "lmk_gs_anchor_decode_culled")
+
+
+# ---- perceptron layers whose weights belong to blocks of rows, and 8-bit checkpoints of their inputs
+DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _dtype(t) -> int:
+    if t.dtype not in DTYPES:
+        raise ValueError(f"float32 or bfloat16 is expected, got {t.dtype}")
+    return DTYPES[t.dtype]
+
+
+def _matrix(t, shape, like, name):
+    """The row stride of a 2-d tensor of `shape` with whole rows, of the type and on the device of `like`."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name} has another type or device ({t.dtype}, {t.device})")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row have to lie next to each other")
+    return max(t.stride(0), shape[1]) if shape[0] <= 1 else t.stride(0)
+
+
+def _dense(t, shape, dtype, like, name):
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != like.device or not t.is_contiguous()):
+        raise ValueError(f"{name} has to be a contiguous {dtype} tensor {tuple(shape)} on {like.device}")
+
+
+def _on_gpu(t):
+    if not t.is_cuda:
+        raise ValueError("the tensors have to be on the GPU: there is no CPU fallback")
+
+
+class Checkpoint8:
+    """The 8-bit form of a [rows][k] matrix (lmk_gs_checkpoint8): `codes` int8 [rows][kp] with kp = k
+    rounded up to 32, `scale` uint8 [rows][kp / 32]; a code stands for code * 2^(scale - 127)."""
+
+    def __init__(self, rows: int, k: int, device="cuda:0", codes=None, scale=None):
+        self.rows, self.k, self.kp = int(rows), int(k), (int(k) + 31) // 32 * 32
+        self.codes = torch.empty((self.rows, self.kp), dtype=torch.int8, device=device) if codes is None else codes
+        self.scale = torch.empty((self.rows, self.kp // 32), dtype=torch.uint8, device=device) if scale is None else scale
+        _dense(self.codes, (self.rows, self.kp), torch.int8, self.codes, "codes")
+        _dense(self.scale, (self.rows, self.kp // 32), torch.uint8, self.codes, "scale")
+        self.c = Checkpoint8C(_ptr(self.codes), _ptr(self.scale))
+
+
+def _layer(w, offsets, rows: int, in_major: bool) -> LinearC:
+    if w.dim() != 3 or offsets.dim() != 1 or offsets.numel() != w.shape[0] + 1:
+        raise ValueError("weights are [blocks][outputs][inputs] (in_major: [blocks][inputs][outputs]) and offsets [blocks + 1]")
+    if offsets.dtype not in (torch.int32, torch.uint32) or not offsets.is_contiguous() or offsets.device != w.device:
+        raise ValueError("offsets have to be a contiguous 32-bit tensor on the weights' device")
+    if w.shape[2] > 1 and w.stride(2) != 1:
+        raise ValueError("the last axis of the weights has to be contiguous")
+    n, k = (w.shape[2], w.shape[1]) if in_major else (w.shape[1], w.shape[2])
+    ldw = w.stride(1) if w.shape[1] > 1 else max(w.stride(1), w.shape[2])
+    return LinearC(_ptr(w), _ptr(offsets), ldw, w.stride(0), w.shape[0], rows, n, k, _dtype(w), int(in_major))
+
+
+def grouped_linear(x, w, offsets, out, bias=None, relu: bool = False, in_major: bool = False,
+                   checkpoint: Checkpoint8 | None = None, stream=None) -> None:
+    """lmk_gs_grouped_linear: out[r] = act(w[g] x[r] + bias[g]) for the rows offsets[g] .. offsets[g+1]-1 of every
+    block g.  x [rows][inputs], w [blocks][outputs][inputs] (in_major: [blocks][inputs][outputs]), out [rows][outputs],
+    float32 or bfloat16 all; offsets int32 [blocks + 1] on the device; bias float32 [blocks][outputs].
+    checkpoint: receives the 8-bit form of x."""
+    layer = _layer(w, offsets, x.shape[0], in_major)
+    ldx = _matrix(x, (layer.rows, layer.k), w, "x")
+    ldy = _matrix(out, (layer.rows, layer.n), w, "out")
+    _dense(bias, (layer.blocks, layer.n), torch.float32, w, "bias")
+    if checkpoint is not None and (checkpoint.rows, checkpoint.k, checkpoint.codes.device) != (layer.rows, layer.k, w.device):
+        raise ValueError("the checkpoint was made for another input")
+    _on_gpu(w)
+    rc = lib().lmk_gs_grouped_linear(C.byref(layer), _ptr(x), ldx, _ptr(bias), int(relu), _ptr(out), ldy,
+                                     None if checkpoint is None else C.byref(checkpoint.c), _stream_handle(stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_linear")
+
+
+def grouped_linear_backward_bytes(rows: int, blocks: int, n: int, k: int, dtype=torch.float32) -> int:
+    """Workspace of grouped_linear_backward in bytes."""
+    out = C.c_size_t(0)
+    layer = LinearC(256, 256, max(n, k), max(n, k) ** 2, blocks, rows, n, k, DTYPES[dtype], 0)
+    rc = lib().lmk_gs_grouped_linear_backward_bytes(C.byref(layer), C.byref(out))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_linear_backward_bytes")
+    return int(out.value)
+
+
+def grouped_linear_backward(dy, w, offsets, workspace=None, x=None, checkpoint: Checkpoint8 | None = None, gate: bool = False,
+                            dx=None, dw=None, db=None, in_major: bool = False, stream=None) -> None:
+    """lmk_gs_grouped_linear_backward: from dy [rows][outputs], the gradient of w[g] x[r] + bias[g], to those of x (with
+    gate: also through the ReLU that gave x), w and bias; each of dx, dw, db may be left out.  The layer's input comes as x
+    or as its checkpoint.  dw (laid out as w) and db are float32 and dense; workspace: a uint8 tensor of
+    grouped_linear_backward_bytes, needed for dw and db."""
+    layer = _layer(w, offsets, dy.shape[0], in_major)
+    lddy = _matrix(dy, (layer.rows, layer.n), w, "dy")
+    ldx = 0 if x is None else _matrix(x, (layer.rows, layer.k), w, "x")
+    if checkpoint is not None and (checkpoint.rows, checkpoint.k, checkpoint.codes.device) != (layer.rows, layer.k, w.device):
+        raise ValueError("the checkpoint was made for another input")
+    lddx = 0 if dx is None else _matrix(dx, (layer.rows, layer.k), w, "dx")
+    _dense(dw, w.shape, torch.float32, w, "dw")
+    _dense(db, (layer.blocks, layer.n), torch.float32, w, "db")
+    if workspace is not None and (workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != w.device):
+        raise ValueError("the workspace has to be a contiguous uint8 tensor on the weights' device")
+    grads = LinearGrads(_ptr(dx), lddx, _ptr(dw), _ptr(db))
+    _on_gpu(w)
+    rc = lib().lmk_gs_grouped_linear_backward(C.byref(layer), _ptr(dy), lddy, _ptr(x), ldx,
+                                              None if checkpoint is None else C.byref(checkpoint.c), int(gate),
+                                              C.byref(grads), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                              _stream_handle(stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_linear_backward")
+
+
+def checkpoint8_pack(x, checkpoint: Checkpoint8, stream=None) -> None:
+    """lmk_gs_checkpoint8_pack: the 8-bit form of x [rows][k], float32 or bfloat16."""
+    ldx = _matrix(x, (checkpoint.rows, checkpoint.k), x, "x")
+    if x.device != checkpoint.codes.device:
+        raise ValueError("x and the checkpoint are on different devices")
+    _on_gpu(x)
+    rc = lib().lmk_gs_checkpoint8_pack(_ptr(x), ldx, checkpoint.rows, checkpoint.k, _dtype(x), C.byref(checkpoint.c),
+                                       _stream_handle(stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_checkpoint8_pack")
+
+
+def checkpoint8_unpack(checkpoint: Checkpoint8, out, stream=None) -> None:
+    """lmk_gs_checkpoint8_unpack: the values the codes stand for (exact in bfloat16 too)."""
+    ldx = _matrix(out, (checkpoint.rows, checkpoint.k), out, "out")
+    if out.device != checkpoint.codes.device:
+        raise ValueError("out and the checkpoint are on different devices")
+    _on_gpu(out)
+    rc = lib().lmk_gs_checkpoint8_unpack(C.byref(checkpoint.c), checkpoint.rows, checkpoint.k, _dtype(out), _ptr(out), ldx,
+                                         _stream_handle(stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_checkpoint8_unpack")
 
 
 def read_status(frame: Frame, stream=None) -> tuple[int, int]:

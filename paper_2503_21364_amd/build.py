@@ -34,6 +34,8 @@ UNITS = {
     "render_bwd.hip": [],       # same options as render.hip: pass 1 repeats its arithmetic
     "preprocess_bwd.hip": [],
     "anchor_decode.hip": [],
+    "checkpoint8.hip": [],
+    "grouped_linear.hip": [],
     "index.hip": EXACT,         # host code: the voxel of a primitive is decided by one fp32 division
 }
 

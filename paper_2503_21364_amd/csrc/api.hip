@@ -57,6 +57,12 @@ int32_t check_camera(const lmk_gs_camera *cam, ProjParams *pp)
 
 bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
+// sizes of the grouped layers' matrices: every byte offset stays below 2^62
+constexpr uint32_t kMaxWidth = 1u << 16, kMaxBlocks = 1u << 16;
+constexpr uint64_t kMaxStride = 1ull << 28, kMaxBlockStride = 1ull << 40;
+
+size_t size_of(uint32_t dtype) { return dtype == LMK_GS_F32 ? 4 : 2; }
+
 // ---- the scratch of lmk_gs_bin_sort_static: one array per GPU, part of the loaded code object.
 // `static_scratch` is only a host-side handle of the symbol; the device address comes from
 // hipGetSymbolAddress, once per device, and only that address is ever handed to a kernel.
@@ -319,6 +325,103 @@ int32_t lmk_gs_anchor_decode_culled(const lmk_gs_anchors *anchors, const lmk_gs_
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
 
+static int32_t check_linear(const lmk_gs_linear *l)
+{
+    if (!l) return LMK_GS_ERR_INVALID;
+    if (l->dtype != LMK_GS_F32 && l->dtype != LMK_GS_BF16) return LMK_GS_ERR_UNSUPPORTED;
+    if (l->in_major > 1u || l->blocks == 0 || l->blocks > kMaxBlocks || l->rows >= 1u << 31) return LMK_GS_ERR_INVALID;
+    if (l->n == 0 || l->k == 0 || l->n > kMaxWidth || l->k > kMaxWidth) return LMK_GS_ERR_INVALID;
+    const uint64_t inner = l->in_major ? l->n : l->k, outer = l->in_major ? l->k : l->n;
+    if (l->ldw < inner || l->ldw > kMaxStride) return LMK_GS_ERR_INVALID;
+    if (l->blocks > 1 && (l->w_block < (outer - 1) * l->ldw + inner || l->w_block > kMaxBlockStride)) return LMK_GS_ERR_INVALID;
+    if (!l->w || !l->offsets || !aligned(l->w, size_of(l->dtype)) || !aligned(l->offsets, 4)) return LMK_GS_ERR_INVALID;
+    if (!grouped_linear_fits(*l)) return LMK_GS_ERR_UNSUPPORTED;
+    return LMK_GS_OK;
+}
+
+// a matrix with a row per anchor: `width` elements of a row, rows `ld` apart
+static bool good_rows(const void *p, uint64_t ld, uint32_t width, uint32_t dtype)
+{
+    return p && aligned(p, size_of(dtype)) && ld >= width && ld <= kMaxStride;
+}
+
+static bool good_checkpoint(const lmk_gs_checkpoint8 *c) { return c->codes && c->scale && aligned(c->codes, 16); }
+
+int32_t lmk_gs_grouped_linear(const lmk_gs_linear *layer, const void *x, uint64_t ldx, const float *bias,
+                              uint32_t relu, void *y, uint64_t ldy, const lmk_gs_checkpoint8 *keep, void *stream)
+{
+    const int32_t rc = check_linear(layer);
+    if (rc != LMK_GS_OK) return rc;
+    if (relu > 1u || !aligned(bias, 4)) return LMK_GS_ERR_INVALID;
+    if (layer->rows == 0) return LMK_GS_OK;
+    if (!good_rows(x, ldx, layer->k, layer->dtype) || !good_rows(y, ldy, layer->n, layer->dtype)) return LMK_GS_ERR_INVALID;
+    if (keep && !good_checkpoint(keep)) return LMK_GS_ERR_INVALID;
+    const hipError_t e = launch_grouped_linear(*layer, x, ldx, bias, relu != 0, y, ldy, keep, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
+int32_t lmk_gs_grouped_linear_backward_bytes(const lmk_gs_linear *layer, size_t *bytes)
+{
+    const int32_t rc = check_linear(layer);
+    if (rc != LMK_GS_OK) return rc;
+    if (!bytes) return LMK_GS_ERR_INVALID;
+    *bytes = grouped_backward_bytes(*layer);
+    return LMK_GS_OK;
+}
+
+int32_t lmk_gs_grouped_linear_backward(const lmk_gs_linear *layer, const void *dy, uint64_t lddy, const void *x,
+                                       uint64_t ldx, const lmk_gs_checkpoint8 *kept, uint32_t gate,
+                                       const lmk_gs_linear_grads *out, void *workspace, size_t workspace_bytes,
+                                       void *stream)
+{
+    const int32_t rc = check_linear(layer);
+    if (rc != LMK_GS_OK) return rc;
+    if (!out || gate > 1u || !aligned(out->dw, 4) || !aligned(out->db, 4)) return LMK_GS_ERR_INVALID;
+    const bool sums = out->dw || out->db;
+    if (layer->rows > 0) {
+        if (!good_rows(dy, lddy, layer->n, layer->dtype)) return LMK_GS_ERR_INVALID;
+        if (out->dx && !good_rows(out->dx, out->lddx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
+        if (x && kept) return LMK_GS_ERR_INVALID;
+        if ((out->dw || (gate && out->dx)) && !x && !kept) return LMK_GS_ERR_INVALID;
+        if (x && !good_rows(x, ldx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
+        if (kept && !good_checkpoint(kept)) return LMK_GS_ERR_INVALID;
+    }
+    if (sums) {
+        if (!workspace || !aligned(workspace, 256)) return LMK_GS_ERR_INVALID;
+        if (workspace_bytes < grouped_backward_bytes(*layer)) return LMK_GS_ERR_CAPACITY;
+    }
+    const hipError_t e = launch_grouped_backward(*layer, dy, lddy, x, ldx, kept, gate != 0, *out,
+                                                 static_cast<char *>(workspace), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
+static int32_t check_checkpoint(const void *x, uint64_t ldx, uint32_t rows, uint32_t k, uint32_t dtype,
+                                const lmk_gs_checkpoint8 *c)
+{
+    if (dtype != LMK_GS_F32 && dtype != LMK_GS_BF16) return LMK_GS_ERR_UNSUPPORTED;
+    if (!c || k == 0 || k > kMaxWidth || rows >= 1u << 31) return LMK_GS_ERR_INVALID;
+    if (rows > 0 && (!good_rows(x, ldx, k, dtype) || !good_checkpoint(c))) return LMK_GS_ERR_INVALID;
+    return checkpoint8_blocks(rows, k) < 1ull << 31 ? LMK_GS_OK : LMK_GS_ERR_UNSUPPORTED;
+}
+
+int32_t lmk_gs_checkpoint8_pack(const void *x, uint64_t ldx, uint32_t rows, uint32_t k, uint32_t dtype,
+                                const lmk_gs_checkpoint8 *out, void *stream)
+{
+    const int32_t rc = check_checkpoint(x, ldx, rows, k, dtype, out);
+    if (rc != LMK_GS_OK) return rc;
+    const hipError_t e = launch_checkpoint8_pack(x, ldx, rows, k, dtype, nullptr, 0, *out, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
+int32_t lmk_gs_checkpoint8_unpack(const lmk_gs_checkpoint8 *kept, uint32_t rows, uint32_t k, uint32_t dtype,
+                                  void *x, uint64_t ldx, void *stream)
+{
+    const int32_t rc = check_checkpoint(x, ldx, rows, k, dtype, kept);
+    if (rc != LMK_GS_OK) return rc;
+    const hipError_t e = launch_checkpoint8_unpack(*kept, rows, k, dtype, x, ldx, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream)
 {
     if (!scratch) return LMK_GS_ERR_INVALID;
@@ -346,7 +449,7 @@ const char *lmk_gs_strerror(int32_t code)
 
 int32_t lmk_gs_last_hip_error(void) { return g_last_hip_error.load(); }
 
-// 0.3.0: the gradient calls and the anchor decoder beside the three forward calls
-uint32_t lmk_gs_version(void) { return 300; }
+// 0.4.0: grouped perceptron layers with their gradients and 8-bit checkpoints
+uint32_t lmk_gs_version(void) { return 400; }
 
 }  // extern "C"

@@ -1,0 +1,557 @@
+// Perceptron layers whose weights belong to blocks of rows (lmk_gs_grouped_linear and its gradients), for every size,
+// stride, alignment and type.  Three products, of which the first two are one kernel:
+//     y  = x w_g^T         rows of a block against the block's weights, sum over the inputs
+//     dx = dy w_g          the same with the weights the other way round, sum over the outputs
+//     dw_g = dy^T x        sum over the rows of a block
+// Float32 matrix instructions (v_mfma_f32_32x32x2_f32: products and sums in 32 bits); bfloat16 operands are widened
+// while they are staged, which is exact.
+//
+// Both operands of a tile pass through LDS as [sum index][row or column]: a lane of half `hi` feeds sum
+// index t + 16 hi to step t, so the 32 lanes of a half read 32 consecutive floats, and with a pitch of TM + 2
+// floats the two halves (16 pitches apart) are on different banks, as are the stores of an operand whose
+// sum index is contiguous in memory (lanes along it, 2 banks apart).
+#include "grouped.h"
+
+namespace lmk {
+
+namespace {
+
+constexpr u32 kStep = 32;                 // sum indices of a staged step
+constexpr u32 kThreads = 256;
+
+constexpr u32 pitch_of(u32 width) { return width + 2; }
+
+// ---- operands: how a tile of `W` rows (columns) by kStep sum indices comes from memory.  load() only
+// requests; store() puts it into LDS.  Out of range: zeros.
+
+// sum index contiguous in memory: element (m, s) at p[m * ld + s]
+template <class T, u32 W> struct Along {
+    const T *p;
+    u64 ld;
+    u32 width, sums;        // valid rows, valid sum indices
+    bool wide;              // rows start at four-element boundaries
+    float v[W / 8];
+
+    __device__ __forceinline__ void load(u32 s0)
+    {
+        if (wide) {
+#pragma unroll
+            for (u32 i = 0; i < W / 32; ++i) {
+                const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = s0 + c % 8 * 4;
+                f32x4 q = {0.f, 0.f, 0.f, 0.f};
+                if (m < width) {
+                    const T *a = p + (u64)m * ld + s;
+                    if (s + 4 <= sums) q = load4(a);
+                    else {
+#pragma unroll
+                        for (u32 j = 0; j < 4; ++j)
+                            if (s + j < sums) q[j] = to_f32(a[j]);
+                    }
+                }
+#pragma unroll
+                for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
+            }
+        } else {
+#pragma unroll
+            for (u32 i = 0; i < W / 8; ++i) {
+                const u32 c = threadIdx.x + i * kThreads, m = c / kStep, s = s0 + c % kStep;
+                v[i] = (m < width && s < sums) ? to_f32(p[(u64)m * ld + s]) : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float *lds) const
+    {
+        constexpr u32 pitch = pitch_of(W);
+        if (wide) {
+#pragma unroll
+            for (u32 i = 0; i < W / 32; ++i) {
+                const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = c % 8 * 4;
+#pragma unroll
+                for (u32 j = 0; j < 4; ++j) lds[(s + j) * pitch + m] = v[4 * i + j];
+            }
+        } else {
+#pragma unroll
+            for (u32 i = 0; i < W / 8; ++i) {
+                const u32 c = threadIdx.x + i * kThreads;
+                lds[(c % kStep) * pitch + c / kStep] = v[i];
+            }
+        }
+    }
+};
+
+// rows (columns) contiguous in memory: element (m, s) at p[s * ld + m]
+template <class T, u32 W> struct Across {
+    const T *p;
+    u64 ld;
+    u32 width, sums;
+    bool wide;
+    float v[W / 8];
+
+    __device__ __forceinline__ void load(u32 s0)
+    {
+        if (wide) {
+#pragma unroll
+            for (u32 i = 0; i < W / 32; ++i) {
+                const u32 c = threadIdx.x + i * kThreads, s = s0 + c / (W / 4), m = c % (W / 4) * 4;
+                f32x4 q = {0.f, 0.f, 0.f, 0.f};
+                if (s < sums && m < width) {
+                    const T *a = p + (u64)s * ld + m;
+                    if (m + 4 <= width) q = load4(a);
+                    else {
+#pragma unroll
+                        for (u32 j = 0; j < 4; ++j)
+                            if (m + j < width) q[j] = to_f32(a[j]);
+                    }
+                }
+#pragma unroll
+                for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
+            }
+        } else {
+#pragma unroll
+            for (u32 i = 0; i < W / 8; ++i) {
+                const u32 c = threadIdx.x + i * kThreads, s = s0 + c / W, m = c % W;
+                v[i] = (s < sums && m < width) ? to_f32(p[(u64)s * ld + m]) : 0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float *lds) const
+    {
+        constexpr u32 pitch = pitch_of(W);
+        if (wide) {
+#pragma unroll
+            for (u32 i = 0; i < W / 32; ++i) {
+                const u32 c = threadIdx.x + i * kThreads, s = c / (W / 4), m = c % (W / 4) * 4;
+#pragma unroll
+                for (u32 j = 0; j < 4; ++j) lds[s * pitch + m + j] = v[4 * i + j];
+            }
+        } else {
+#pragma unroll
+            for (u32 i = 0; i < W / 8; ++i) {
+                const u32 c = threadIdx.x + i * kThreads;
+                lds[(c / W) * pitch + c % W] = v[i];
+            }
+        }
+    }
+};
+
+// the same from the 8-bit form: rows of kp codes (all of them there), a scale byte for 32
+template <u32 W> struct Across8 {
+    const u32 *codes;       // of the tile's first row and column
+    const uint8_t *scale;
+    u32 kp;                 // codes of a row
+    u32 width, sums;        // width: codes to the end of the row
+    u32 q[W / 32];
+    u32 e[W / 32];
+
+    __device__ __forceinline__ void load(u32 s0)
+    {
+#pragma unroll
+        for (u32 i = 0; i < W / 32; ++i) {
+            const u32 c = threadIdx.x + i * kThreads, s = s0 + c / (W / 4), m = c % (W / 4) * 4;
+            const bool there = s < sums && m < width;
+            q[i] = there ? codes[((u64)s * kp + m) / 4] : 0u;
+            e[i] = there ? scale[(u64)s * (kp / 32) + m / 32] : 0u;
+        }
+    }
+    __device__ __forceinline__ void store(float *lds) const
+    {
+        constexpr u32 pitch = pitch_of(W);
+#pragma unroll
+        for (u32 i = 0; i < W / 32; ++i) {
+            const u32 c = threadIdx.x + i * kThreads, s = c / (W / 4), m = c % (W / 4) * 4;
+            const float step = step_of(e[i]);
+#pragma unroll
+            for (u32 j = 0; j < 4; ++j) lds[s * pitch + m + j] = value_of(q[i], j, step);
+        }
+    }
+};
+
+// Wavefronts of a workgroup over a TM x TN tile: 2 x 2 where both sides have 128, else all along TM.
+template <u32 TM, u32 TN> struct Split {
+    static constexpr u32 kCols = TN == 128 ? 2 : 1, kRows = 4 / kCols;
+    static constexpr u32 kM = TM / kRows / 32, kN = TN / kCols / 32;        // 32 x 32 results of a wavefront
+    static_assert(kM * kRows * 32 == TM && kN * kCols * 32 == TN, "whole results");
+};
+
+// The product of a tile: acc += A B over `sums`.  `each` is called with the staged A of every step.
+template <u32 TM, u32 TN, class A, class B, class Each>
+__device__ __forceinline__ void tile_product(A &a, B &b, u32 sums, float *lds, f32x16 (&acc)[Split<TM, TN>::kM][Split<TM, TN>::kN],
+                                             Each &&each)
+{
+    using S = Split<TM, TN>;
+    constexpr u32 pa = pitch_of(TM), pb = pitch_of(TN), buffer = kStep * (pa + pb);
+    const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    const u32 j = lane & 31, hi = lane / 32;
+    const u32 m0 = wave / S::kCols * (S::kM * 32) + j, n0 = wave % S::kCols * (S::kN * 32) + j;
+    a.load(0);
+    b.load(0);
+    u32 at = 0;
+    for (u32 s0 = 0; s0 < sums; s0 += kStep, at ^= 1) {
+        float *la = lds + at * buffer, *lb = la + kStep * pa;
+        a.store(la);
+        b.store(lb);
+        __syncthreads();                     // the other buffer's readers are past the previous one of these
+        if (s0 + kStep < sums) {
+            a.load(s0 + kStep);
+            b.load(s0 + kStep);
+        }
+        each(la);
+        // steps t and t + 16 in one instruction; the last ones of a short tile hold nothing
+        const u32 left = sums - s0;
+        auto step = [&](u32 t) {
+            float fa[S::kM], fb[S::kN];
+#pragma unroll
+            for (u32 m = 0; m < S::kM; ++m) fa[m] = la[(t + 16 * hi) * pa + m0 + 32 * m];
+#pragma unroll
+            for (u32 n = 0; n < S::kN; ++n) fb[n] = lb[(t + 16 * hi) * pb + n0 + 32 * n];
+#pragma unroll
+            for (u32 m = 0; m < S::kM; ++m)
+#pragma unroll
+                for (u32 n = 0; n < S::kN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[m], fb[n], acc[m][n], 0, 0, 0);
+        };
+        if (left >= 16) {
+#pragma unroll
+            for (u32 t = 0; t < 16; ++t) step(t);
+        } else {
+            for (u32 t = 0; t < left; ++t) step(t);
+        }
+    }
+}
+
+// row of a 32 x 32 result that register v of a lane of half hi holds (its column is lane % 32)
+__device__ __forceinline__ u32 row_of(u32 v, u32 hi) { return 8 * (v / 4) + 4 * hi + v % 4; }
+
+// Workgroups go to the eight dies in turn; this gives each die a run of consecutive tiles, which share operands.
+__device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
+{
+    constexpr u32 dies = 8;
+    const u32 per = total / dies;
+    return id < per * dies ? id % dies * per + id / dies : id;
+}
+
+// ---- rows against weights
+struct RowsArgs {
+    const void *a;              // [rows][sums]
+    u64 lda;
+    const void *w;              // block g at g * w_block
+    u64 ldw, w_block;
+    const u32 *offsets;
+    u32 blocks, rows, cols, sums;
+    void *out;                  // [rows][cols]
+    u64 ldo;
+    const float *bias;          // [blocks][cols] or NULL
+    u32 relu;
+    const void *gate;           // NULL, or what the result is gated with: values or codes
+    u64 ldgate;                 // elements (codes) between its rows
+    const uint8_t *gate_scale;  // of codes
+    u32 tiles, col_tiles;
+    bool wide_a, wide_w;
+};
+
+// GATE: 0 none, 1 values, 2 codes
+template <class T, u32 TN, bool ACROSS, u32 GATE>
+__global__ __launch_bounds__(256, 2) void rows_kernel(const RowsArgs r)
+{
+    constexpr u32 TM = 128;
+    using S = Split<TM, TN>;
+    __shared__ __align__(16) float lds[2 * kStep * (pitch_of(TM) + pitch_of(TN))];
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * TN;
+    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, TM, row_tile);
+    if (!run.found) return;
+    const u32 row0 = run.begin + run.local * TM;
+    const u32 height = run.end - row0 < TM ? run.end - row0 : TM;
+    const u32 width = r.cols - col0 < TN ? r.cols - col0 : TN;
+    T *out = static_cast<T *>(r.out) + (u64)row0 * r.ldo + col0;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 31, hi = lane / 32;
+    const u32 m0 = wave / S::kCols * (S::kM * 32), n0 = wave % S::kCols * (S::kN * 32);
+    f32x16 acc[S::kM][S::kN] = {};
+    if (run.block != ~0u) {
+        Along<T, TM> a{static_cast<const T *>(r.a) + (u64)row0 * r.lda, r.lda, height, r.sums, r.wide_a, {}};
+        const T *w = static_cast<const T *>(r.w) + (u64)run.block * r.w_block;
+        if constexpr (ACROSS) {
+            Across<T, TN> b{w + col0, r.ldw, width, r.sums, r.wide_w, {}};
+            tile_product<TM, TN>(a, b, r.sums, lds, acc, [](const float *) {});
+        } else {
+            Along<T, TN> b{w + (u64)col0 * r.ldw, r.ldw, width, r.sums, r.wide_w, {}};
+            tile_product<TM, TN>(a, b, r.sums, lds, acc, [](const float *) {});
+        }
+    }
+#pragma unroll
+    for (u32 n = 0; n < S::kN; ++n) {
+        const u32 c = n0 + 32 * n + j;
+        const float bias = (r.bias && run.block != ~0u && c < width) ? r.bias[(u64)run.block * r.cols + col0 + c] : 0.0f;
+#pragma unroll
+        for (u32 m = 0; m < S::kM; ++m)
+#pragma unroll
+            for (u32 v = 0; v < 16; ++v) {
+                const u32 row = m0 + 32 * m + row_of(v, hi);
+                if (row >= height || c >= width) continue;
+                float y = acc[m][n][v] + bias;
+                if (r.relu) y = y < 0.0f ? 0.0f : y;              // NaN stays
+                if (GATE == 1 && run.block != ~0u) {
+                    const float x = to_f32(static_cast<const T *>(r.gate)[(u64)(row0 + row) * r.ldgate + col0 + c]);
+                    y = x <= 0.0f ? 0.0f : y;
+                }
+                if (GATE == 2 && run.block != ~0u) {
+                    const u64 at = (u64)(row0 + row) * r.ldgate + col0 + c;
+                    const bool pass = static_cast<const signed char *>(r.gate)[at] > 0 || r.gate_scale[at / 32] == 255;
+                    y = pass ? y : 0.0f;
+                }
+                out[(u64)row * r.ldo + c] = (T)y;
+            }
+    }
+}
+
+// ---- sums over the rows of a block
+struct SumsArgs {
+    const void *dy;             // [rows][n]
+    u64 lddy;
+    const void *x;              // [rows][k], or codes [rows][kp]
+    u64 ldx;
+    const uint8_t *scale;       // of codes
+    const u32 *offsets;
+    u32 blocks, rows, n, k;
+    float *dw, *db;             // results, either may be NULL
+    u32 in_major;
+    float *part;                // run t: n k sums of dw, then n of db
+    u32 per;                    // rows of a run
+    u32 tiles, n_tiles, k_tiles;
+    bool wide_dy, wide_x;
+};
+
+// KIND: 0 no x (db alone), 1 values, 2 codes
+template <class T, u32 TM, u32 TN, u32 KIND>
+__global__ __launch_bounds__(256, 2) void sums_kernel(const SumsArgs r)
+{
+    using S = Split<TM, TN>;
+    __shared__ __align__(16) float lds[2 * kStep * (pitch_of(TM) + pitch_of(TN))];
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 pairs = r.n_tiles * r.k_tiles, t = tile / pairs, pair = tile - t * pairs;
+    const u32 n0 = pair / r.k_tiles * TM, k0 = pair % r.k_tiles * TN;
+    const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, t);
+    if (!run.found) return;
+    const u32 row0 = run.begin + run.local * r.per;
+    const u32 count = run.end - row0 < r.per ? run.end - row0 : r.per;
+    const u32 height = r.n - n0 < TM ? r.n - n0 : TM, width = r.k - k0 < TN ? r.k - k0 : TN;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 31, hi = lane / 32;
+    f32x16 acc[S::kM][S::kN] = {};
+    float bias = 0.0f;
+    if (count > 0) {
+        Across<T, TM> a{static_cast<const T *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, r.wide_dy, {}};
+        // thread m sums column m of the staged dy
+        const bool sums_db = r.db && k0 == 0 && threadIdx.x < TM;
+        auto each = [&](const float *la) {
+            if (!sums_db) return;
+#pragma unroll
+            for (u32 s = 0; s < kStep; ++s) bias += la[s * pitch_of(TM) + threadIdx.x];
+        };
+        if constexpr (KIND == 2) {
+            const u32 kp = (r.k + 31) / 32 * 32;
+            Across8<TN> b{reinterpret_cast<const u32 *>(static_cast<const signed char *>(r.x) + (u64)row0 * kp + k0),
+                          r.scale + ((u64)row0 * kp + k0) / 32, kp, kp - k0, count, {}, {}};
+            tile_product<TM, TN>(a, b, count, lds, acc, each);
+        } else {
+            Across<T, TN> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)row0 * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
+                            count, r.wide_x, {}};
+            tile_product<TM, TN>(a, b, count, lds, acc, each);
+        }
+    }
+    // a block with one run has its result here; otherwise the run's partial sums
+    const bool whole = run.runs == 1;
+    float *dw = whole ? r.dw : r.part + (u64)t * ((u64)r.n * r.k + r.n);
+    float *db = whole ? r.db : r.part + (u64)t * ((u64)r.n * r.k + r.n) + (u64)r.n * r.k;
+    if (whole && dw) dw += (u64)run.block * r.n * r.k;
+    if (whole && db) db += (u64)run.block * r.n;
+    if (r.dw) {
+        const u32 mw = wave / S::kCols * (S::kM * 32), nw = wave % S::kCols * (S::kN * 32) + j;
+#pragma unroll
+        for (u32 n = 0; n < S::kN; ++n)
+#pragma unroll
+            for (u32 m = 0; m < S::kM; ++m)
+#pragma unroll
+                for (u32 v = 0; v < 16; ++v) {
+                    const u32 row = mw + 32 * m + row_of(v, hi), col = nw + 32 * n;
+                    if (row >= height || col >= width) continue;
+                    const u64 at = r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col;
+                    dw[at] = acc[m][n][v];
+                }
+    }
+    if (r.db && k0 == 0 && threadIdx.x < height) db[n0 + threadIdx.x] = bias;
+}
+
+// Joins the partial sums of the blocks that have several runs, in the order of the runs.
+__global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per,
+                                                   const float *__restrict__ part, u32 n, u32 k, float *__restrict__ dw,
+                                                   float *__restrict__ db, u32 pieces, u32 runs)
+{
+    const u32 block = blockIdx.x / pieces, piece = blockIdx.x - block * pieces;
+    // runs in front of this block's
+    const u32 lane = threadIdx.x & (kWave - 1);
+    u32 before = 0, mine = 0;
+    for (u32 base = 0; base <= block; base += kWave) {
+        const u32 s = base + lane;
+        u32 count = 0;
+        if (s <= block) {
+            u32 b = offsets[s], e = offsets[s + 1];
+            b = b < rows ? b : rows;
+            e = e < rows ? e : rows;
+            e = e > b ? e : b;
+            count = (e - b + per - 1) / per;
+            count = count ? count : 1u;
+        }
+        before += wave_sum(s < block ? count : 0u);
+        mine += wave_sum(s == block ? count : 0u);
+    }
+    // one run: written where it was summed.  More runs than there is room for: the offsets do not ascend
+    if (mine <= 1 || (u64)before + mine > runs) return;
+    const u64 size = (u64)n * k, stride = size + n;
+    const u64 i = (u64)piece * 256 + threadIdx.x;
+    if (i >= stride) return;
+    float *dst = i < size ? dw : db;
+    if (!dst) return;
+    const float *p = part + (u64)before * stride + i;
+    float sum = 0.0f;
+    for (u32 q = 0; q < mine; ++q) sum += p[(u64)q * stride];
+    dst[i < size ? (u64)block * size + i : (u64)block * n + (i - size)] = sum;
+}
+
+template <class T>
+bool four_wide(const void *p, u64 ld) { return ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0; }
+
+u32 tile_width(u32 cols) { return cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 96 ? 96 : 128; }
+
+template <class T, u32 TN, bool ACROSS, u32 GATE>
+void rows_go(const RowsArgs &r, hipStream_t stream)
+{
+    hipLaunchKernelGGL((rows_kernel<T, TN, ACROSS, GATE>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+}
+template <class T, bool ACROSS, u32 GATE>
+void rows_width(const RowsArgs &r, hipStream_t stream)
+{
+    switch (tile_width(r.cols)) {
+    case 32: return rows_go<T, 32, ACROSS, GATE>(r, stream);
+    case 64: return rows_go<T, 64, ACROSS, GATE>(r, stream);
+    case 96: return rows_go<T, 96, ACROSS, GATE>(r, stream);
+    default: return rows_go<T, 128, ACROSS, GATE>(r, stream);
+    }
+}
+template <class T>
+hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
+{
+    const u32 tn = tile_width(r.cols);
+    r.col_tiles = (r.cols + tn - 1) / tn;
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, 128, true) * r.col_tiles);
+    r.wide_a = four_wide<T>(r.a, r.lda);
+    r.wide_w = four_wide<T>(r.w, r.ldw) && r.w_block % 4 == 0;
+    const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
+    if (across) gate == 0 ? rows_width<T, true, 0>(r, stream) : gate == 1 ? rows_width<T, true, 1>(r, stream) : rows_width<T, true, 2>(r, stream);
+    else gate == 0 ? rows_width<T, false, 0>(r, stream) : gate == 1 ? rows_width<T, false, 1>(r, stream) : rows_width<T, false, 2>(r, stream);
+    return hipGetLastError();
+}
+
+// rows of a run of the sums over rows: about 1024 workgroups in all (four a compute unit), no run under 256 rows
+u32 rows_of_run(const lmk_gs_linear &l)
+{
+    const u64 pairs = (u64)((l.n + 127) / 128) * ((l.k + tile_width(l.k) - 1) / tile_width(l.k));
+    u64 per = ((u64)l.rows * pairs + 1023) / 1024;
+    per = (per + kStep - 1) / kStep * kStep;
+    return (u32)(per < 256 ? 256 : per);
+}
+
+template <class T, u32 TN>
+void sums_go(const SumsArgs &r, u32 kind, hipStream_t stream)
+{
+    if (kind == 2) hipLaunchKernelGGL((sums_kernel<T, 128, TN, 2>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+    else if (kind == 1) hipLaunchKernelGGL((sums_kernel<T, 128, TN, 1>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+    else hipLaunchKernelGGL((sums_kernel<T, 128, TN, 0>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+}
+template <class T>
+hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
+{
+    const u32 tn = kind == 0 ? 32 : tile_width(r.k);
+    r.n_tiles = (r.n + 127) / 128;
+    r.k_tiles = kind == 0 ? 1 : (r.k + tn - 1) / tn;
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, r.per, false) * r.n_tiles * r.k_tiles);
+    r.wide_dy = four_wide<T>(r.dy, r.lddy);
+    r.wide_x = kind == 1 && four_wide<T>(r.x, r.ldx);
+    switch (tn) {
+    case 32: sums_go<T, 32>(r, kind, stream); break;
+    case 64: sums_go<T, 64>(r, kind, stream); break;
+    case 96: sums_go<T, 96>(r, kind, stream); break;
+    default: sums_go<T, 128>(r, kind, stream); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool grouped_linear_fits(const lmk_gs_linear &l)
+{
+    const u64 runs = max_runs(l.rows, l.blocks, 128, true);
+    const u64 pairs = (u64)((l.n + 127) / 128) * ((l.k + 31) / 32);
+    const u64 widest = l.n > l.k ? l.n : l.k;
+    return runs * ((widest + 31) / 32) < 1ull << 31 && max_runs(l.rows, l.blocks, rows_of_run(l), false) * pairs < 1ull << 31 &&
+           (((u64)l.n * l.k + l.n + 255) / 256) * l.blocks < 1ull << 31;
+}
+
+size_t grouped_backward_bytes(const lmk_gs_linear &l)
+{
+    // the partial sums of every run but those of blocks that have only one; at least one
+    return (size_t)(max_runs(l.rows, l.blocks, rows_of_run(l), false) * ((u64)l.n * l.k + l.n) * 4);
+}
+
+hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
+                                 u64 ldy, const lmk_gs_checkpoint8 *keep, hipStream_t stream)
+{
+    if (keep) {
+        const hipError_t e = launch_checkpoint8_pack(x, ldx, l.rows, l.k, l.dtype, l.offsets, l.blocks, *keep, stream);
+        if (e != hipSuccess) return e;
+    }
+    RowsArgs r = {};
+    r.a = x; r.lda = ldx;
+    r.w = l.w; r.ldw = l.ldw; r.w_block = l.w_block;
+    r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.cols = l.n; r.sums = l.k;
+    r.out = y; r.ldo = ldy; r.bias = bias; r.relu = relu;
+    return l.dtype == LMK_GS_F32 ? rows_as<float>(r, l.in_major != 0, stream) : rows_as<__bf16>(r, l.in_major != 0, stream);
+}
+
+hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx,
+                                   const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
+                                   char *workspace, hipStream_t stream)
+{
+    const u32 kp = (l.k + 31) / 32 * 32;
+    if (out.dx && l.rows > 0) {
+        RowsArgs r = {};
+        r.a = dy; r.lda = lddy;
+        r.w = l.w; r.ldw = l.ldw; r.w_block = l.w_block;
+        r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.cols = l.k; r.sums = l.n;
+        r.out = out.dx; r.ldo = out.lddx;
+        if (gate) {
+            r.gate = kept ? (const void *)kept->codes : x;
+            r.ldgate = kept ? kp : ldx;
+            r.gate_scale = kept ? kept->scale : nullptr;
+        }
+        const hipError_t e = l.dtype == LMK_GS_F32 ? rows_as<float>(r, l.in_major == 0, stream) : rows_as<__bf16>(r, l.in_major == 0, stream);
+        if (e != hipSuccess) return e;
+    }
+    if (!out.dw && !out.db) return hipSuccess;
+    SumsArgs r = {};
+    r.dy = dy; r.lddy = lddy;
+    r.x = kept ? (const void *)kept->codes : x;
+    r.ldx = ldx;
+    r.scale = kept ? kept->scale : nullptr;
+    r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.n = l.n; r.k = l.k;
+    r.dw = out.dw; r.db = out.db; r.in_major = l.in_major;
+    r.part = reinterpret_cast<float *>(workspace);
+    r.per = rows_of_run(l);
+    const u32 kind = !out.dw ? 0 : kept ? 2 : 1;
+    hipError_t e = l.dtype == LMK_GS_F32 ? sums_as<float>(r, kind, stream) : sums_as<__bf16>(r, kind, stream);
+    if (e != hipSuccess) return e;
+    const u32 pieces = (u32)(((u64)l.n * l.k + l.n + 255) / 256);
+    hipLaunchKernelGGL(join_kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, r.per, r.part, l.n,
+                       l.k, out.dw, out.db, pieces, (u32)max_runs(l.rows, l.blocks, r.per, false));
+    return hipGetLastError();
+}
+
+}  // namespace lmk

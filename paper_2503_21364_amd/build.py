@@ -36,6 +36,7 @@ UNITS = {
     "anchor_decode.hip": [],
     "checkpoint8.hip": [],
     "grouped_linear.hip": [],
+    "grouped_wide.hip": [],
     "index.hip": EXACT,         # host code: the voxel of a primitive is decided by one fp32 division
 }
 

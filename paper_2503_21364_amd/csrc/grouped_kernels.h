@@ -1,0 +1,57 @@
+// Arguments of the grouped layers' kernels, and what their launches share.
+#ifndef LMK_GS_GROUPED_KERNELS_H
+#define LMK_GS_GROUPED_KERNELS_H
+#include "grouped.h"
+
+namespace lmk {
+
+// rows of a block against its weights
+struct RowsArgs {
+    const void *a;              // [rows][sums]
+    u64 lda;
+    const void *w;              // block g at g * w_block
+    u64 ldw, w_block;
+    const u32 *offsets;
+    u32 blocks, rows, cols, sums;
+    void *out;                  // [rows][cols]
+    u64 ldo;
+    const float *bias;          // [blocks][cols] or NULL
+    u32 relu;
+    const void *gate;           // NULL, or what the result is gated with: values or codes
+    u64 ldgate;                 // elements (codes) between its rows
+    const uint8_t *gate_scale;  // of codes
+    u32 tiles, col_tiles;
+    bool wide_a, wide_w;
+};
+
+// sums over the rows of a block
+struct SumsArgs {
+    const void *dy;             // [rows][n]
+    u64 lddy;
+    const void *x;              // [rows][k], or codes [rows][kp]
+    u64 ldx;
+    const uint8_t *scale;       // of codes
+    const u32 *offsets;
+    u32 blocks, rows, n, k;
+    float *dw, *db;             // results, either may be NULL
+    u32 in_major;
+    float *part;                // run t: n k sums of dw, then n of db
+    u32 per;                    // rows of a run
+    u32 tiles, n_tiles, k_tiles;
+    bool wide_dy, wide_x;
+};
+
+// Workgroups go to the eight dies in turn; this gives each die a run of consecutive tiles, which share operands.
+__device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
+{
+    constexpr u32 dies = 8;
+    const u32 per = total / dies;
+    return id < per * dies ? id % dies * per + id / dies : id;
+}
+
+// bfloat16 whose rows start at 16-byte boundaries
+bool wide_rows_fit(const RowsArgs &r, bool across);
+hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream);
+
+}  // namespace lmk
+#endif

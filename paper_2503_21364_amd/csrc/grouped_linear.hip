@@ -10,7 +10,9 @@
 // index t + 16 hi to step t, so the 32 lanes of a half read 32 consecutive floats, and with a pitch of TM + 2
 // floats the two halves (16 pitches apart) are on different banks, as are the stores of an operand whose
 // sum index is contiguous in memory (lanes along it, 2 banks apart).
-#include "grouped.h"
+#include "grouped_kernels.h"
+
+#include <type_traits>
 
 namespace lmk {
 
@@ -221,32 +223,7 @@ __device__ __forceinline__ void tile_product(A &a, B &b, u32 sums, float *lds, f
 // row of a 32 x 32 result that register v of a lane of half hi holds (its column is lane % 32)
 __device__ __forceinline__ u32 row_of(u32 v, u32 hi) { return 8 * (v / 4) + 4 * hi + v % 4; }
 
-// Workgroups go to the eight dies in turn; this gives each die a run of consecutive tiles, which share operands.
-__device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
-{
-    constexpr u32 dies = 8;
-    const u32 per = total / dies;
-    return id < per * dies ? id % dies * per + id / dies : id;
-}
-
 // ---- rows against weights
-struct RowsArgs {
-    const void *a;              // [rows][sums]
-    u64 lda;
-    const void *w;              // block g at g * w_block
-    u64 ldw, w_block;
-    const u32 *offsets;
-    u32 blocks, rows, cols, sums;
-    void *out;                  // [rows][cols]
-    u64 ldo;
-    const float *bias;          // [blocks][cols] or NULL
-    u32 relu;
-    const void *gate;           // NULL, or what the result is gated with: values or codes
-    u64 ldgate;                 // elements (codes) between its rows
-    const uint8_t *gate_scale;  // of codes
-    u32 tiles, col_tiles;
-    bool wide_a, wide_w;
-};
 
 // GATE: 0 none, 1 values, 2 codes
 template <class T, u32 TN, bool ACROSS, u32 GATE>
@@ -304,21 +281,6 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(const RowsArgs r)
 }
 
 // ---- sums over the rows of a block
-struct SumsArgs {
-    const void *dy;             // [rows][n]
-    u64 lddy;
-    const void *x;              // [rows][k], or codes [rows][kp]
-    u64 ldx;
-    const uint8_t *scale;       // of codes
-    const u32 *offsets;
-    u32 blocks, rows, n, k;
-    float *dw, *db;             // results, either may be NULL
-    u32 in_major;
-    float *part;                // run t: n k sums of dw, then n of db
-    u32 per;                    // rows of a run
-    u32 tiles, n_tiles, k_tiles;
-    bool wide_dy, wide_x;
-};
 
 // KIND: 0 no x (db alone), 1 values, 2 codes
 template <class T, u32 TM, u32 TN, u32 KIND>
@@ -439,6 +401,7 @@ void rows_width(const RowsArgs &r, hipStream_t stream)
 template <class T>
 hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
 {
+    if (std::is_same<T, __bf16>::value && wide_rows_fit(r, across)) return launch_wide_rows(r, across, stream);
     const u32 tn = tile_width(r.cols);
     r.col_tiles = (r.cols + tn - 1) / tn;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, 128, true) * r.col_tiles);

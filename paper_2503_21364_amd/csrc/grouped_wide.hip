@@ -1,0 +1,372 @@
+// Grouped layers in bfloat16 whose rows start at 16-byte boundaries: the same products as in grouped_linear.hip on the bfloat16
+// matrix instructions (v_mfma_f32_16x16x32_bf16: exact products, sums in 32 bits).
+#include "grouped.h"
+#include "grouped_kernels.h"
+
+namespace lmk {
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((ext_vector_type(4))) u32 u32x4;
+typedef __attribute__((ext_vector_type(2))) u32 u32x2;
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+
+constexpr u32 kStep = 32;                   // sum indices of a staged step: one matrix instruction's
+constexpr u32 kStages = 4;                  // steps in LDS: one being read, three on their way
+constexpr u32 kNowhere = 0x7ffffff0u;       // a byte offset behind every buffer below: reads give zeros
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, u32 bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
+}
+
+// ---- an operand of `W` rows (columns) by kStep sum indices in LDS, 64 W bytes, filled by loads that go to LDS
+// directly (16 bytes a lane, 1 KB a wavefront, consecutive in LDS); what is out of range arrives as zeros.
+
+// sum index contiguous in memory.  LDS: rows of four 16-byte chunks, chunk c of row r in place c ^ (r / 4 % 4): the 16 rows
+// that 16 lanes read at one chunk are then in 16 different places modulo 256 bytes.
+template <u32 W, u32 WAVES> struct Along16 {
+    static constexpr u32 kLoads = W / 16 / WAVES;
+    const char *p;          // first row, first sum index
+    u32 bytes;              // to the end of the last row
+    u32 sums;
+    u32 from[kLoads];       // byte offset of this lane's chunk, sum index 0
+    u32 s_lane;             // its first sum index in a step
+    u32 read;               // LDS byte offset of this lane's part of the first 16 rows
+
+    __device__ __forceinline__ void init(const __bf16 *base, u64 ld, u32 rows, u32 sums_, u32 wave, u32 lane)
+    {
+        p = reinterpret_cast<const char *>(base);
+        sums = sums_;
+        bytes = ((rows - 1) * (u32)ld + sums) * 2;
+        const u32 chunk = (lane & 3) ^ (lane >> 4);
+        s_lane = chunk * 8;
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i) from[i] = ((wave + WAVES * i) * 16 + lane / 4) * (u32)ld * 2 + chunk * 16;
+        read = (lane & 15) * 64 + (((lane >> 4) ^ (lane >> 2 & 3)) * 16);
+    }
+    __device__ __forceinline__ void fill(lds_char *lds, u32 step, u32 wave) const
+    {
+        const __amdgpu_buffer_rsrc_t b = buffer_of(p, bytes);
+        const u32 s0 = step * kStep;
+        const bool there = s0 + s_lane < sums;
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, lds + (wave + WAVES * i) * 1024, 16, (int)(there ? from[i] + s0 * 2 : kNowhere), 0, 0, 0);
+    }
+    // rows 16 f .. 16 f + 15 of the wavefront's first row r0
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 r0, u32 f) const
+    {
+        return *reinterpret_cast<const lds_bf16x8 *>(lds + read + (r0 + 16 * f) * 64);
+    }
+};
+
+// rows (columns) contiguous in memory.  LDS: kStep rows of W values; 16 values (32 bytes) are a pair of chunks, pair p of sum
+// index s in place p ^ g(s), g = s % 4 + 4 (s / 8 % 2): the eight sum indices whose rows half a wavefront reads in a
+// transposed load have eight different g, so the pairs are in different places modulo 256 bytes.
+__device__ __forceinline__ u32 turn(u32 s) { return (s & 3) | ((s >> 3 & 1) << 2); }
+
+template <u32 W> __device__ __forceinline__ u32 across_read(u32 lane)
+{
+    const u32 s = 8 * (lane >> 4) + (lane >> 2 & 3);
+    return s * (W * 2) + (turn(s) << 5) + (lane & 3) * 8;
+}
+template <u32 W> __device__ __forceinline__ bf16x8 across_fragment(const lds_char *lds, u32 read, u32 r0, u32 f)
+{
+    // a lane's 16-lane group turns four rows of 16 values: twice four sum indices of one column
+    const lds_char *a = lds + (read ^ ((r0 / 16 + f) << 5));
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)a);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(a + 4 * W * 2));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+template <u32 W, u32 WAVES> struct Across16 {
+    static constexpr u32 kLoads = W / 16 / WAVES;
+    const char *p;
+    u32 sums, row_bytes, width_bytes;
+    u64 ld_bytes;
+    u32 from[kLoads];
+    u32 read;
+
+    __device__ __forceinline__ void init(const __bf16 *base, u64 ld, u32 width, u32 sums_, u32 wave, u32 lane)
+    {
+        p = reinterpret_cast<const char *>(base);
+        sums = sums_;
+        ld_bytes = ld * 2;
+        width_bytes = width * 2;
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i) {
+            const u32 at = (wave + WAVES * i) * 64 + lane, s = at / (W / 8), slot = at % (W / 8);
+            const u32 chunk = ((slot >> 1) ^ turn(s)) * 2 + (slot & 1);
+            from[i] = chunk * 8 < width ? s * (u32)ld_bytes + chunk * 16 : kNowhere;
+        }
+        read = across_read<W>(lane);
+    }
+    __device__ __forceinline__ void fill(lds_char *lds, u32 step, u32 wave) const
+    {
+        const u32 s0 = step * kStep;
+        const u32 left = s0 < sums ? sums - s0 : 0u, rows = left < kStep ? left : kStep;
+        const __amdgpu_buffer_rsrc_t b = buffer_of(p + (u64)s0 * ld_bytes, rows ? (rows - 1) * (u32)ld_bytes + width_bytes : 0u);
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(b, lds + (wave + WAVES * i) * 1024, 16, (int)from[i], 0, 0, 0);
+    }
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 r0, u32 f) const { return across_fragment<W>(lds, read, r0, f); }
+};
+
+// Tile of TP x TQ results: P runs along the output's contiguous axis (a lane holds four consecutive ones of it), Q across it.
+template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
+    static constexpr u32 kWaves = WP * WQ, kThreads = kWaves * kWave;
+    static constexpr u32 kP = TP / WP / 16, kQ = TQ / WQ / 16;           // 16 x 16 results of a wavefront
+    static constexpr u32 kStageP = TP * 64, kStageQ = TQ * 64, kLds = kStages * (kStageP + kStageQ);
+};
+
+// acc[i][j] += P Q over `sums` steps.  A step's fragments are read from LDS while the step in front of it is
+// multiplied; its place in LDS is filled again as soon as all wavefronts have them.  `each(step, lds of Q)`
+// is called where a step's Q operand is whole in LDS.
+template <class S, class P, class Q, class Each>
+__device__ __forceinline__ void wide_product(const P &p, const Q &q, u32 steps, lds_char *lds, u32 wave, u32 p0, u32 q0,
+                                             f32x4 (&acc)[S::kP][S::kQ], Each &&each)
+{
+    lds_char *lp = lds, *lq = lds + kStages * S::kStageP;
+#pragma unroll
+    for (u32 s = 0; s < kStages; ++s) {
+        p.fill(lp + s * S::kStageP, s, wave);
+        q.fill(lq + s * S::kStageQ, s, wave);
+    }
+    bf16x8 fp[2][S::kP], fq[2][S::kQ];
+    constexpr u32 kLoads = P::kLoads + Q::kLoads;
+    static_assert(kLoads == 4, "the waits below count four loads a step");
+    __builtin_amdgcn_s_waitcnt(0xF70 | 12);              // twelve loads may be on their way: step 0 is there
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (u32 i = 0; i < S::kP; ++i) fp[0][i] = p.fragment(lp, p0, i);
+#pragma unroll
+    for (u32 j = 0; j < S::kQ; ++j) fq[0][j] = q.fragment(lq, q0, j);
+    each(0u, lq);
+    for (u32 t0 = 0; t0 < steps; t0 += kStages) {
+#pragma unroll
+        for (u32 u = 0; u < kStages; ++u) {
+            const u32 t = t0 + u;
+            if (t >= steps) break;
+            // step t + 1 is in LDS (two steps may be on their way), and the fragments of step t have left it
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0x070 | 8);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            p.fill(lp + u * S::kStageP, t + kStages, wave);
+            q.fill(lq + u * S::kStageQ, t + kStages, wave);
+            constexpr u32 stages = kStages;
+            const u32 next = (u + 1) % stages;
+#pragma unroll
+            for (u32 i = 0; i < S::kP; ++i) fp[(u + 1) & 1][i] = p.fragment(lp + next * S::kStageP, p0, i);
+#pragma unroll
+            for (u32 j = 0; j < S::kQ; ++j) fq[(u + 1) & 1][j] = q.fragment(lq + next * S::kStageQ, q0, j);
+            asm volatile("" ::: "memory");           // the reads stay in front of the products
+#pragma unroll
+            for (u32 i = 0; i < S::kP; ++i)
+#pragma unroll
+                for (u32 j = 0; j < S::kQ; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[u & 1][i], fq[u & 1][j], acc[i][j], 0, 0, 0);
+            if (t + 1 < steps) each(t + 1, lq + next * S::kStageQ);
+        }
+    }
+    // nothing may be on its way into LDS when the workgroup ends
+    __builtin_amdgcn_s_waitcnt(0x070);
+}
+
+__device__ __forceinline__ u32 pack_bf16(float a, float b)
+{
+    return (u32)__builtin_bit_cast(unsigned short, (__bf16)a) | ((u32)__builtin_bit_cast(unsigned short, (__bf16)b) << 16);
+}
+
+// GATE: 0 none, 1 values, 2 codes
+template <class S, u32 TP, u32 TQ, u32 WP, bool ACROSS, u32 GATE>
+__global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArgs r)
+{
+    extern __shared__ __align__(16) char wide_lds[];
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * TP;
+    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, TQ, row_tile);
+    if (!run.found) return;
+    const u32 row0 = run.begin + run.local * TQ;
+    const u32 height = run.end - row0 < TQ ? run.end - row0 : TQ;
+    const u32 width = r.cols - col0 < TP ? r.cols - col0 : TP;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const u32 p0 = wave % WP * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
+    f32x4 acc[S::kP][S::kQ] = {};
+    const bool inside = run.block != ~0u;
+    if (inside) {
+        lds_char *lds = (lds_char *)wide_lds;
+        const u32 steps = (r.sums + kStep - 1) / kStep;
+        Along16<TQ, S::kWaves> q;
+        q.init(static_cast<const __bf16 *>(r.a) + (u64)row0 * r.lda, r.lda, height, r.sums, wave, lane);
+        const __bf16 *w = static_cast<const __bf16 *>(r.w) + (u64)run.block * r.w_block;
+        if constexpr (ACROSS) {
+            Across16<TP, S::kWaves> p;
+            p.init(w + col0, r.ldw, width, r.sums, wave, lane);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, [](u32, const lds_char *) {});
+        } else {
+            Along16<TP, S::kWaves> p;
+            p.init(w + (u64)col0 * r.ldw, r.ldw, width, r.sums, wave, lane);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, [](u32, const lds_char *) {});
+        }
+    }
+    // Two neighbouring results exchange lanes, so that a lane has eight consecutive values of a row:
+    // lane group 0: the first eight of result i, 1: of i + 1, 2 and 3: the second eight.
+    const u32 group = lane >> 4;
+    __bf16 *out = static_cast<__bf16 *>(r.out) + (u64)row0 * r.ldo + col0;
+#pragma unroll
+    for (u32 i = 0; i < S::kP; i += 2) {
+        const u32 c_own = p0 + 16 * i + 4 * group;           // of result i, before the exchange
+        f32x4 bias[2] = {};
+        if (r.bias && inside) {
+            const float *b = r.bias + (u64)run.block * r.cols + col0;
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                for (u32 v = 0; v < 4; ++v) {
+                    const u32 c = c_own + 16 * h + v;
+                    bias[h][v] = c < width ? b[c] : 0.0f;
+                }
+        }
+        const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1);
+#pragma unroll
+        for (u32 j = 0; j < S::kQ; ++j) {
+            f32x4 y[2] = {acc[i][j] + bias[0], acc[i + 1][j] + bias[1]};
+            if (r.relu) {
+#pragma unroll
+                for (u32 v = 0; v < 4; ++v) {
+                    y[0][v] = y[0][v] < 0.0f ? 0.0f : y[0][v];          // NaN stays
+                    y[1][v] = y[1][v] < 0.0f ? 0.0f : y[1][v];
+                }
+            }
+            const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(y[0][0], y[0][1]), pack_bf16(y[1][0], y[1][1]), false, false);
+            const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(y[0][2], y[0][3]), pack_bf16(y[1][2], y[1][3]), false, false);
+            u32x4 v = {a[0], b[0], a[1], b[1]};
+            const u32 row = q0 + 16 * j + (lane & 15);
+            if (row >= height || c >= width) continue;
+            if (GATE == 1 && inside) {
+                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(r.gate) + (u64)(row0 + row) * r.ldgate + col0 + c);
+#pragma unroll
+                for (u32 e = 0; e < 4; ++e) {
+                    if ((float)x[2 * e] <= 0.0f) v[e] &= 0xffff0000u;
+                    if ((float)x[2 * e + 1] <= 0.0f) v[e] &= 0x0000ffffu;
+                }
+            }
+            if (GATE == 2 && inside) {
+                const u64 at = (u64)(row0 + row) * r.ldgate + col0 + c;
+                const u32x2 codes = *reinterpret_cast<const u32x2 *>(static_cast<const char *>(r.gate) + at);
+                if (r.gate_scale[at / 32] != 255) {
+#pragma unroll
+                    for (u32 e = 0; e < 8; ++e)
+                        if ((int)(signed char)(codes[e / 4] >> (8 * (e % 4))) <= 0) v[e / 2] &= e % 2 ? 0x0000ffffu : 0xffff0000u;
+                }
+            }
+            *reinterpret_cast<u32x4 *>(out + (u64)row * r.ldo + c) = v;
+        }
+    }
+}
+
+// ---- sums over rows
+
+// x of the sums over rows from its 8-bit form: a thread's 16 codes (half of those that share a step) come to registers two steps
+// ahead and are widened on their way into LDS, laid out as Across16 does.
+template <u32 W, u32 WAVES> struct Codes16 {
+    const char *codes;
+    const uint8_t *scale;
+    u32 kp, sums;
+    u32 s, pair;
+    bool there;
+    u32 read;
+    u32 to;
+    u32x4 v[2];
+    u32 e[2];
+
+    __device__ __forceinline__ void init(const char *codes_, const uint8_t *scale_, u32 kp_, u32 width, u32 sums_, u32 lane)
+    {
+        codes = codes_;
+        scale = scale_;
+        kp = kp_;
+        sums = sums_;
+        s = threadIdx.x / (W / 16);
+        pair = threadIdx.x % (W / 16);
+        there = pair * 16 < width;
+        read = across_read<W>(lane);
+        to = s * (W * 2) + ((pair ^ turn(s)) << 5);
+    }
+    __device__ __forceinline__ void request(u32 step, u32 at)
+    {
+        const u32 row = step * kStep + s;
+        const bool ok = there && row < sums;
+        v[at] = u32x4{0, 0, 0, 0};
+        e[at] = 0;
+        if (ok) {
+            v[at] = *reinterpret_cast<const u32x4 *>(codes + (u64)row * kp + pair * 16);
+            e[at] = scale[(u64)row * (kp / 32) + pair / 2];
+        }
+    }
+    __device__ __forceinline__ void widen(lds_char *lds, u32 at) const
+    {
+        const float step = step_of(e[at]);
+        u32x4 o[2];
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) {
+            const u32 q = v[at][i / 2] >> (16 * (i % 2));
+            o[i / 4][i % 4] = pack_bf16(value_of(q, 0, step), value_of(q, 1, step));
+        }
+        *reinterpret_cast<lds_u32x4 *>(lds + to) = o[0];
+        *reinterpret_cast<lds_u32x4 *>(lds + to + 16) = o[1];
+    }
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 r0, u32 f) const { return across_fragment<W>(lds, read, r0, f); }
+};
+
+}  // namespace
+
+// ---- launches
+namespace {
+
+template <u32 TP, u32 TQ, u32 WP, u32 WQ, bool ACROSS, u32 GATE>
+hipError_t wide_go(RowsArgs r, hipStream_t stream)
+{
+    using S = Shape<TP, TQ, WP, WQ>;
+    r.col_tiles = (r.cols + TP - 1) / TP;
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, TQ, true) * r.col_tiles);
+    auto kernel = wide_rows_kernel<S, TP, TQ, WP, ACROSS, GATE>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), S::kLds, stream, r);
+    return hipGetLastError();
+}
+template <bool ACROSS, u32 GATE>
+hipError_t wide_shape(const RowsArgs &r, hipStream_t stream)
+{
+    if (r.cols > 128 && max_runs(r.rows, r.blocks, 256, true) * ((r.cols + 255) / 256) >= 256)
+        return wide_go<256, 256, 2, 4, ACROSS, GATE>(r, stream);
+    return wide_go<128, 128, 2, 2, ACROSS, GATE>(r, stream);
+}
+
+bool sixteen(const void *p, u64 ld) { return ld % 8 == 0 && ld <= 1u << 21 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+}  // namespace
+
+bool wide_rows_fit(const RowsArgs &r, bool across)
+{
+    if (r.sums % 8 || r.cols % 8 || !sixteen(r.a, r.lda) || !sixteen(r.w, r.ldw) || r.w_block % 8 || !sixteen(r.out, r.ldo)) return false;
+    return !r.gate || r.gate_scale || sixteen(r.gate, r.ldgate);
+}
+
+hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
+{
+    const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
+    if (across) return gate == 0 ? wide_shape<true, 0>(r, stream) : gate == 1 ? wide_shape<true, 1>(r, stream) : wide_shape<true, 2>(r, stream);
+    return gate == 0 ? wide_shape<false, 0>(r, stream) : gate == 1 ? wide_shape<false, 1>(r, stream) : wide_shape<false, 2>(r, stream);
+}
+
+}  // namespace lmk

@@ -28,8 +28,12 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, u32 b
 // ---- an operand of `W` rows (columns) by kStep sum indices in LDS, 64 W bytes, filled by loads that go to LDS
 // directly (16 bytes a lane, 1 KB a wavefront, consecutive in LDS); what is out of range arrives as zeros.
 
-// sum index contiguous in memory.  LDS: rows of four 16-byte chunks, chunk c of row r in place c ^ (r / 4 % 4): the 16 rows
-// that 16 lanes read at one chunk are then in 16 different places modulo 256 bytes.
+// sum index contiguous in memory.  LDS: rows of four 16-byte chunks, chunk c of row r in place c ^ h(r / 4 % 4), h = 0 2 3 1.
+// A 16-byte read is served 16 lanes at a time: lanes 0-3, 12-15 and 20-27, then 4-11, 16-19 and 28-31, and so on, which hold
+// rows of two chunks; with this h they are in 16 different places modulo 256 bytes (measured: h = 0 1 2 3, right for 16
+// consecutive lanes, doubles the cycles of the reads).
+__device__ __forceinline__ u32 place_turn(u32 r4) { return ((r4 << 1 ^ r4) & 2) | r4 >> 1; }
+
 template <u32 W, u32 WAVES> struct Along16 {
     static constexpr u32 kLoads = W / 16 / WAVES;
     const char *p;          // first row, first sum index
@@ -44,11 +48,11 @@ template <u32 W, u32 WAVES> struct Along16 {
         p = reinterpret_cast<const char *>(base);
         sums = sums_;
         bytes = ((rows - 1) * (u32)ld + sums) * 2;
-        const u32 chunk = (lane & 3) ^ (lane >> 4);
+        const u32 chunk = (lane & 3) ^ place_turn(lane >> 4);
         s_lane = chunk * 8;
 #pragma unroll
         for (u32 i = 0; i < kLoads; ++i) from[i] = ((wave + WAVES * i) * 16 + lane / 4) * (u32)ld * 2 + chunk * 16;
-        read = (lane & 15) * 64 + (((lane >> 4) ^ (lane >> 2 & 3)) * 16);
+        read = (lane & 15) * 64 + (((lane >> 4) ^ place_turn(lane >> 2 & 3)) * 16);
     }
     __device__ __forceinline__ void fill(lds_char *lds, u32 step, u32 wave) const
     {

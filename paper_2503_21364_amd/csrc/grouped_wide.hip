@@ -25,6 +25,10 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, u32 b
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
 }
 
+// what is the same in all lanes, in scalar registers
+__device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ u64 uniform64(u64 v) { return (u64)uniform((u32)(v >> 32)) << 32 | uniform((u32)v); }
+
 // ---- an operand of `W` rows (columns) by kStep sum indices in LDS, 64 W bytes, filled by loads that go to LDS
 // directly (16 bytes a lane, 1 KB a wavefront, consecutive in LDS); what is out of range arrives as zeros.
 
@@ -80,45 +84,50 @@ template <u32 W> __device__ __forceinline__ u32 across_read(u32 lane)
     const u32 s = 8 * (lane >> 4) + (lane >> 2 & 3);
     return s * (W * 2) + (turn(s) << 5) + (lane & 3) * 8;
 }
+// Four sum indices of one column.  `restrict` tells the compiler that the loads on their way into LDS go elsewhere (the barriers
+// see to that); without it, it waits for all of them in front of every such read.
+__device__ __forceinline__ s16x4 read_turned(const lds_char *__restrict__ a) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)a); }
+
 template <u32 W> __device__ __forceinline__ bf16x8 across_fragment(const lds_char *lds, u32 read, u32 r0, u32 f)
 {
     // a lane's 16-lane group turns four rows of 16 values: twice four sum indices of one column
     const lds_char *a = lds + (read ^ ((r0 / 16 + f) << 5));
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)a);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(a + 4 * W * 2));
+    const s16x4 lo = read_turned(a), hi = read_turned(a + 4 * W * 2);
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
+// fill() is called for one step after the other.
 template <u32 W, u32 WAVES> struct Across16 {
     static constexpr u32 kLoads = W / 16 / WAVES;
-    const char *p;
-    u32 sums, row_bytes, width_bytes;
-    u64 ld_bytes;
+    u64 next;               // address of the next step's first row (uniform)
+    u32 left;               // its rows and all behind it
+    u32 ld_bytes, width_bytes;
     u32 from[kLoads];
     u32 read;
 
-    __device__ __forceinline__ void init(const __bf16 *base, u64 ld, u32 width, u32 sums_, u32 wave, u32 lane)
+    __device__ __forceinline__ void init(const __bf16 *base, u64 ld, u32 width, u32 sums, u32 wave, u32 lane)
     {
-        p = reinterpret_cast<const char *>(base);
-        sums = sums_;
-        ld_bytes = ld * 2;
-        width_bytes = width * 2;
+        next = uniform64(reinterpret_cast<u64>(base));
+        left = uniform(sums);
+        ld_bytes = uniform((u32)ld * 2);
+        width_bytes = uniform(width * 2);
 #pragma unroll
         for (u32 i = 0; i < kLoads; ++i) {
             const u32 at = (wave + WAVES * i) * 64 + lane, s = at / (W / 8), slot = at % (W / 8);
             const u32 chunk = ((slot >> 1) ^ turn(s)) * 2 + (slot & 1);
-            from[i] = chunk * 8 < width ? s * (u32)ld_bytes + chunk * 16 : kNowhere;
+            from[i] = chunk * 8 < width ? s * ld_bytes + chunk * 16 : kNowhere;
         }
         read = across_read<W>(lane);
     }
-    __device__ __forceinline__ void fill(lds_char *lds, u32 step, u32 wave) const
+    __device__ __forceinline__ void fill(lds_char *lds, u32, u32 wave)
     {
-        const u32 s0 = step * kStep;
-        const u32 left = s0 < sums ? sums - s0 : 0u, rows = left < kStep ? left : kStep;
-        const __amdgpu_buffer_rsrc_t b = buffer_of(p + (u64)s0 * ld_bytes, rows ? (rows - 1) * (u32)ld_bytes + width_bytes : 0u);
+        const u32 rows = left < kStep ? left : kStep;
+        const __amdgpu_buffer_rsrc_t b = buffer_of(reinterpret_cast<const void *>(next), rows ? (rows - 1) * ld_bytes + width_bytes : 0u);
 #pragma unroll
         for (u32 i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(b, lds + (wave + WAVES * i) * 1024, 16, (int)from[i], 0, 0, 0);
+        next += (u64)kStep * ld_bytes;
+        left -= rows;
     }
     __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 r0, u32 f) const { return across_fragment<W>(lds, read, r0, f); }
 };
@@ -134,7 +143,7 @@ template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
 // multiplied; its place in LDS is filled again as soon as all wavefronts have them.  `each(step, lds of Q)`
 // is called where a step's Q operand is whole in LDS.
 template <class S, class P, class Q, class Each>
-__device__ __forceinline__ void wide_product(const P &p, const Q &q, u32 steps, lds_char *lds, u32 wave, u32 p0, u32 q0,
+__device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *lds, u32 wave, u32 p0, u32 q0,
                                              f32x4 (&acc)[S::kP][S::kQ], Each &&each)
 {
     lds_char *lp = lds, *lq = lds + kStages * S::kStageP;

@@ -16,8 +16,8 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef __attribute__((address_space(3))) bf16x8 lds_bf16x8;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 
-constexpr u32 kStep = 32;                   // sum indices of a staged step: one matrix instruction's
-constexpr u32 kStages = 4;                  // steps in LDS: one being read, three on their way
+constexpr u32 kStep = 32;                   // sum indices of a matrix instruction
+constexpr u32 kPair = 2 * kStep;            // of a filled part of LDS: 128 bytes of a row, a whole line
 constexpr u32 kNowhere = 0x7ffffff0u;       // a byte offset behind every buffer below: reads give zeros
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, u32 bytes)
@@ -29,52 +29,50 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, u32 b
 __device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_readfirstlane((int)v); }
 __device__ __forceinline__ u64 uniform64(u64 v) { return (u64)uniform((u32)(v >> 32)) << 32 | uniform((u32)v); }
 
-// ---- an operand of `W` rows (columns) by kStep sum indices in LDS, 64 W bytes, filled by loads that go to LDS
-// directly (16 bytes a lane, 1 KB a wavefront, consecutive in LDS); what is out of range arrives as zeros.
+// ---- an operand of `W` rows (columns) by kPair sum indices in LDS, 128 W bytes, filled by loads that go to LDS
+// directly (16 bytes a lane, 1 KB a wavefront, consecutive in LDS), one pair of steps after the other; what is out of range arrives as zeros.
 
-// sum index contiguous in memory.  LDS: rows of four 16-byte chunks, chunk c of row r in place c ^ h(r / 4 % 4), h = 0 2 3 1.
-// A 16-byte read is served 16 lanes at a time: lanes 0-3, 12-15 and 20-27, then 4-11, 16-19 and 28-31, and so on, which hold
-// rows of two chunks; with this h they are in 16 different places modulo 256 bytes (measured: h = 0 1 2 3, right for 16
-// consecutive lanes, doubles the cycles of the reads).
-__device__ __forceinline__ u32 place_turn(u32 r4) { return ((r4 << 1 ^ r4) & 2) | r4 >> 1; }
-
+// sum index contiguous in memory.  LDS: rows of eight 16-byte chunks, chunk c of row r in place c ^ (r / 2 % 8).  A 16-byte
+// read is served 16 lanes at a time, lanes 0-3, 12-15 and 20-27, then the others of 32: they hold eight rows at one
+// chunk and the other eight at the next, and are in 16 different places modulo 256 bytes.
 template <u32 W, u32 WAVES> struct Along16 {
-    static constexpr u32 kLoads = W / 16 / WAVES;
+    static constexpr u32 kLoads = W / 8 / WAVES;
     const char *p;          // first row, first sum index
     u32 bytes;              // to the end of the last row
-    u32 sums;
+    u32 sums, s0;
     u32 from[kLoads];       // byte offset of this lane's chunk, sum index 0
-    u32 s_lane;             // its first sum index in a step
+    u32 s_lane;             // its first sum index in a pair of steps
     u32 read;               // LDS byte offset of this lane's part of the first 16 rows
 
     __device__ __forceinline__ void init(const __bf16 *base, u64 ld, u32 rows, u32 sums_, u32 wave, u32 lane)
     {
         p = reinterpret_cast<const char *>(base);
         sums = sums_;
+        s0 = 0;
         bytes = ((rows - 1) * (u32)ld + sums) * 2;
-        const u32 chunk = (lane & 3) ^ place_turn(lane >> 4);
+        const u32 chunk = (lane & 7) ^ (lane >> 4) ^ (wave & 1) * 4;
         s_lane = chunk * 8;
 #pragma unroll
-        for (u32 i = 0; i < kLoads; ++i) from[i] = ((wave + WAVES * i) * 16 + lane / 4) * (u32)ld * 2 + chunk * 16;
-        read = (lane & 15) * 64 + (((lane >> 4) ^ place_turn(lane >> 2 & 3)) * 16);
+        for (u32 i = 0; i < kLoads; ++i) from[i] = ((wave + WAVES * i) * 8 + lane / 8) * (u32)ld * 2 + chunk * 16;
+        read = (lane & 15) * 128 + (((lane >> 4) ^ (lane >> 1 & 7)) * 16);
     }
-    __device__ __forceinline__ void fill(lds_char *lds, u32 step, u32 wave) const
+    __device__ __forceinline__ void fill(lds_char *lds, u32 wave)
     {
         const __amdgpu_buffer_rsrc_t b = buffer_of(p, bytes);
-        const u32 s0 = step * kStep;
         const bool there = s0 + s_lane < sums;
 #pragma unroll
         for (u32 i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(b, lds + (wave + WAVES * i) * 1024, 16, (int)(there ? from[i] + s0 * 2 : kNowhere), 0, 0, 0);
+        s0 += kPair;
     }
-    // rows 16 f .. 16 f + 15 of the wavefront's first row r0
-    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 r0, u32 f) const
+    // half h of the pair; rows 16 f .. 16 f + 15 from the wavefront's first row r0 on
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 h, u32 r0, u32 f) const
     {
-        return *reinterpret_cast<const lds_bf16x8 *>(lds + read + (r0 + 16 * f) * 64);
+        return *reinterpret_cast<const lds_bf16x8 *>(lds + (read ^ h * 64) + (r0 + 16 * f) * 128);
     }
 };
 
-// rows (columns) contiguous in memory.  LDS: kStep rows of W values; 16 values (32 bytes) are a pair of chunks, pair p of sum
+// rows (columns) contiguous in memory.  LDS: kPair rows of W values; 16 values (32 bytes) are a pair of chunks, pair p of sum
 // index s in place p ^ g(s), g = s % 4 + 4 (s / 8 % 2): the eight sum indices whose rows half a wavefront reads in a
 // transposed load have eight different g, so the pairs are in different places modulo 256 bytes.
 __device__ __forceinline__ u32 turn(u32 s) { return (s & 3) | ((s >> 3 & 1) << 2); }
@@ -96,10 +94,9 @@ template <u32 W> __device__ __forceinline__ bf16x8 across_fragment(const lds_cha
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// fill() is called for one step after the other.
 template <u32 W, u32 WAVES> struct Across16 {
-    static constexpr u32 kLoads = W / 16 / WAVES;
-    u64 next;               // address of the next step's first row (uniform)
+    static constexpr u32 kLoads = W / 8 / WAVES;
+    u64 next;               // address of the next pair's first row (uniform)
     u32 left;               // its rows and all behind it
     u32 ld_bytes, width_bytes;
     u32 from[kLoads];
@@ -119,75 +116,77 @@ template <u32 W, u32 WAVES> struct Across16 {
         }
         read = across_read<W>(lane);
     }
-    __device__ __forceinline__ void fill(lds_char *lds, u32, u32 wave)
+    __device__ __forceinline__ void fill(lds_char *lds, u32 wave)
     {
-        const u32 rows = left < kStep ? left : kStep;
+        const u32 rows = left < kPair ? left : kPair;
         const __amdgpu_buffer_rsrc_t b = buffer_of(reinterpret_cast<const void *>(next), rows ? (rows - 1) * ld_bytes + width_bytes : 0u);
 #pragma unroll
         for (u32 i = 0; i < kLoads; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(b, lds + (wave + WAVES * i) * 1024, 16, (int)from[i], 0, 0, 0);
-        next += (u64)kStep * ld_bytes;
+        next += (u64)kPair * ld_bytes;
         left -= rows;
     }
-    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 r0, u32 f) const { return across_fragment<W>(lds, read, r0, f); }
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 h, u32 r0, u32 f) const { return across_fragment<W>(lds + h * kStep * W * 2, read, r0, f); }
 };
 
 // Tile of TP x TQ results: P runs along the output's contiguous axis (a lane holds four consecutive ones of it), Q across it.
 template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
     static constexpr u32 kWaves = WP * WQ, kThreads = kWaves * kWave;
     static constexpr u32 kP = TP / WP / 16, kQ = TQ / WQ / 16;           // 16 x 16 results of a wavefront
-    static constexpr u32 kStageP = TP * 64, kStageQ = TQ * 64, kLds = kStages * (kStageP + kStageQ);
+    static constexpr u32 kPartP = TP * kPair * 2, kPartQ = TQ * kPair * 2, kLds = 2 * (kPartP + kPartQ);
 };
 
-// acc[i][j] += P Q over `sums` steps.  A step's fragments are read from LDS while the step in front of it is
-// multiplied; its place in LDS is filled again as soon as all wavefronts have them.  `each(step, lds of Q)`
-// is called where a step's Q operand is whole in LDS.
-template <class S, class P, class Q, class Each>
+// acc[i][j] += P Q over `steps`.  LDS holds two pairs of steps.  A step's fragments are read from LDS while the step in front of
+// it is multiplied; once the second step's are with all wavefronts, the pair's part is filled again, which has the
+// time of two steps to arrive.  One meeting of the wavefronts a pair.
+template <class S, class P, class Q>
 __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *lds, u32 wave, u32 p0, u32 q0,
-                                             f32x4 (&acc)[S::kP][S::kQ], Each &&each)
+                                             f32x4 (&acc)[S::kP][S::kQ])
 {
-    lds_char *lp = lds, *lq = lds + kStages * S::kStageP;
-#pragma unroll
-    for (u32 s = 0; s < kStages; ++s) {
-        p.fill(lp + s * S::kStageP, s, wave);
-        q.fill(lq + s * S::kStageQ, s, wave);
-    }
-    bf16x8 fp[2][S::kP], fq[2][S::kQ];
+    lds_char *lp = lds, *lq = lds + 2 * S::kPartP;
     constexpr u32 kLoads = P::kLoads + Q::kLoads;
-    static_assert(kLoads == 4, "the waits below count four loads a step");
-    __builtin_amdgcn_s_waitcnt(0xF70 | 12);              // twelve loads may be on their way: step 0 is there
+    static_assert(kLoads == 8, "the wait below counts eight loads a pair");
+    bf16x8 fp[2][S::kP], fq[2][S::kQ];
+    auto fill = [&](u32 part) {
+        p.fill(lp + part * S::kPartP, wave);
+        q.fill(lq + part * S::kPartQ, wave);
+    };
+    auto read = [&](u32 part, u32 h) {
+#pragma unroll
+        for (u32 i = 0; i < S::kP; ++i) fp[h][i] = p.fragment(lp + part * S::kPartP, h, p0, i);
+#pragma unroll
+        for (u32 j = 0; j < S::kQ; ++j) fq[h][j] = q.fragment(lq + part * S::kPartQ, h, q0, j);
+        asm volatile("" ::: "memory");              // the reads stay in front of the products
+    };
+    auto multiply = [&](u32 h) {
+#pragma unroll
+        for (u32 i = 0; i < S::kP; ++i)
+#pragma unroll
+            for (u32 j = 0; j < S::kQ; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[h][i], fq[h][j], acc[i][j], 0, 0, 0);
+    };
+    fill(0);
+    fill(1);
+    __builtin_amdgcn_s_waitcnt(0xF70 | 8);              // the second pair's eight loads may be on their way
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    read(0, 0);
+    for (u32 t0 = 0; t0 < steps; t0 += 4) {
 #pragma unroll
-    for (u32 i = 0; i < S::kP; ++i) fp[0][i] = p.fragment(lp, p0, i);
-#pragma unroll
-    for (u32 j = 0; j < S::kQ; ++j) fq[0][j] = q.fragment(lq, q0, j);
-    each(0u, lq);
-    for (u32 t0 = 0; t0 < steps; t0 += kStages) {
-#pragma unroll
-        for (u32 u = 0; u < kStages; ++u) {
-            const u32 t = t0 + u;
+        for (u32 part = 0; part < 2; ++part) {
+            const u32 t = t0 + 2 * part;
             if (t >= steps) break;
-            // step t + 1 is in LDS (two steps may be on their way), and the fragments of step t have left it
+            read(part, 1);
+            multiply(0);
+            if (t + 1 >= steps) break;
+            // the next pair has arrived, and this pair's fragments have left LDS
             asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_waitcnt(0x070 | 8);
+            __builtin_amdgcn_s_waitcnt(0x070);
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            p.fill(lp + u * S::kStageP, t + kStages, wave);
-            q.fill(lq + u * S::kStageQ, t + kStages, wave);
-            constexpr u32 stages = kStages;
-            const u32 next = (u + 1) % stages;
-#pragma unroll
-            for (u32 i = 0; i < S::kP; ++i) fp[(u + 1) & 1][i] = p.fragment(lp + next * S::kStageP, p0, i);
-#pragma unroll
-            for (u32 j = 0; j < S::kQ; ++j) fq[(u + 1) & 1][j] = q.fragment(lq + next * S::kStageQ, q0, j);
-            asm volatile("" ::: "memory");           // the reads stay in front of the products
-#pragma unroll
-            for (u32 i = 0; i < S::kP; ++i)
-#pragma unroll
-                for (u32 j = 0; j < S::kQ; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[u & 1][i], fq[u & 1][j], acc[i][j], 0, 0, 0);
-            if (t + 1 < steps) each(t + 1, lq + next * S::kStageQ);
+            fill(part);
+            read(1 - part, 0);
+            multiply(1);
         }
     }
     // nothing may be on its way into LDS when the workgroup ends
@@ -224,11 +223,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
         if constexpr (ACROSS) {
             Across16<TP, S::kWaves> p;
             p.init(w + col0, r.ldw, width, r.sums, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, [](u32, const lds_char *) {});
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc);
         } else {
             Along16<TP, S::kWaves> p;
             p.init(w + (u64)col0 * r.ldw, r.ldw, width, r.sums, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, [](u32, const lds_char *) {});
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc);
         }
     }
     // Two neighbouring results exchange lanes, so that a lane has eight consecutive values of a row:
@@ -286,59 +285,6 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
         }
     }
 }
-
-// ---- sums over rows
-
-// x of the sums over rows from its 8-bit form: a thread's 16 codes (half of those that share a step) come to registers two steps
-// ahead and are widened on their way into LDS, laid out as Across16 does.
-template <u32 W, u32 WAVES> struct Codes16 {
-    const char *codes;
-    const uint8_t *scale;
-    u32 kp, sums;
-    u32 s, pair;
-    bool there;
-    u32 read;
-    u32 to;
-    u32x4 v[2];
-    u32 e[2];
-
-    __device__ __forceinline__ void init(const char *codes_, const uint8_t *scale_, u32 kp_, u32 width, u32 sums_, u32 lane)
-    {
-        codes = codes_;
-        scale = scale_;
-        kp = kp_;
-        sums = sums_;
-        s = threadIdx.x / (W / 16);
-        pair = threadIdx.x % (W / 16);
-        there = pair * 16 < width;
-        read = across_read<W>(lane);
-        to = s * (W * 2) + ((pair ^ turn(s)) << 5);
-    }
-    __device__ __forceinline__ void request(u32 step, u32 at)
-    {
-        const u32 row = step * kStep + s;
-        const bool ok = there && row < sums;
-        v[at] = u32x4{0, 0, 0, 0};
-        e[at] = 0;
-        if (ok) {
-            v[at] = *reinterpret_cast<const u32x4 *>(codes + (u64)row * kp + pair * 16);
-            e[at] = scale[(u64)row * (kp / 32) + pair / 2];
-        }
-    }
-    __device__ __forceinline__ void widen(lds_char *lds, u32 at) const
-    {
-        const float step = step_of(e[at]);
-        u32x4 o[2];
-#pragma unroll
-        for (u32 i = 0; i < 8; ++i) {
-            const u32 q = v[at][i / 2] >> (16 * (i % 2));
-            o[i / 4][i % 4] = pack_bf16(value_of(q, 0, step), value_of(q, 1, step));
-        }
-        *reinterpret_cast<lds_u32x4 *>(lds + to) = o[0];
-        *reinterpret_cast<lds_u32x4 *>(lds + to + 16) = o[1];
-    }
-    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 r0, u32 f) const { return across_fragment<W>(lds, read, r0, f); }
-};
 
 }  // namespace
 

@@ -83,6 +83,13 @@ __device__ __forceinline__ RowRun find_run(const u32 *__restrict__ offsets, u32 
     return none;
 }
 
+// First row of run `local` of a block whose rows are shared out evenly over its runs (the sums over rows, whose runs need not
+// be full ones); run.runs: the end.
+__device__ __forceinline__ u32 run_row(const RowRun &run, u32 local)
+{
+    return run.begin + (u32)((u64)(run.end - run.begin) * local / run.runs);
+}
+
 // Upper bound of the number of runs (host): every block can end with a run that is not full.
 inline u64 max_runs(u32 rows, u32 blocks, u32 per, bool outside)
 {

@@ -52,6 +52,8 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
 // bfloat16 whose rows start at 16-byte boundaries
 bool wide_rows_fit(const RowsArgs &r, bool across);
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream);
+bool wide_sums_fit(const SumsArgs &r);
+hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream);
 
 }  // namespace lmk
 #endif

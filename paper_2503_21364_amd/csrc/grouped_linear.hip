@@ -293,8 +293,7 @@ __global__ __launch_bounds__(256, 2) void sums_kernel(const SumsArgs r)
     const u32 n0 = pair / r.k_tiles * TM, k0 = pair % r.k_tiles * TN;
     const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, t);
     if (!run.found) return;
-    const u32 row0 = run.begin + run.local * r.per;
-    const u32 count = run.end - row0 < r.per ? run.end - row0 : r.per;
+    const u32 row0 = run_row(run, run.local), count = run_row(run, run.local + 1) - row0;
     const u32 height = r.n - n0 < TM ? r.n - n0 : TM, width = r.k - k0 < TN ? r.k - k0 : TN;
     const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 31, hi = lane / 32;
     f32x16 acc[S::kM][S::kN] = {};
@@ -432,6 +431,7 @@ void sums_go(const SumsArgs &r, u32 kind, hipStream_t stream)
 template <class T>
 hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 {
+    if (std::is_same<T, __bf16>::value && kind != 0 && wide_sums_fit(r)) return launch_wide_sums(r, stream);
     const u32 tn = kind == 0 ? 32 : tile_width(r.k);
     r.n_tiles = (r.n + 127) / 128;
     r.k_tiles = kind == 0 ? 1 : (r.k + tn - 1) / tn;

@@ -36,6 +36,7 @@ __device__ __forceinline__ u64 uniform64(u64 v) { return (u64)uniform((u32)(v >>
 // read is served 16 lanes at a time, lanes 0-3, 12-15 and 20-27, then the others of 32: they hold eight rows at one
 // chunk and the other eight at the next, and are in 16 different places modulo 256 bytes.
 template <u32 W, u32 WAVES> struct Along16 {
+    static constexpr bool kDirect = true;
     static constexpr u32 kLoads = W / 8 / WAVES;
     const char *p;          // first row, first sum index
     u32 bytes;              // to the end of the last row
@@ -95,6 +96,7 @@ template <u32 W> __device__ __forceinline__ bf16x8 across_fragment(const lds_cha
 }
 
 template <u32 W, u32 WAVES> struct Across16 {
+    static constexpr bool kDirect = true;
     static constexpr u32 kLoads = W / 8 / WAVES;
     u64 next;               // address of the next pair's first row (uniform)
     u32 left;               // its rows and all behind it
@@ -139,13 +141,14 @@ template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
 // acc[i][j] += P Q over `steps`.  LDS holds two pairs of steps.  A step's fragments are read from LDS while the step in front of
 // it is multiplied; once the second step's are with all wavefronts, the pair's part is filled again, which has the
 // time of two steps to arrive.  One meeting of the wavefronts a pair.
-template <class S, class P, class Q>
+// `also` sees the fragments of Q.
+template <class S, class P, class Q, class Also>
 __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *lds, u32 wave, u32 p0, u32 q0,
-                                             f32x4 (&acc)[S::kP][S::kQ])
+                                             f32x4 (&acc)[S::kP][S::kQ], Also &&also)
 {
     lds_char *lp = lds, *lq = lds + 2 * S::kPartP;
-    constexpr u32 kLoads = P::kLoads + Q::kLoads;
-    static_assert(kLoads == 8, "the wait below counts eight loads a pair");
+    constexpr bool kDirect = P::kDirect && Q::kDirect;
+    if constexpr (kDirect) static_assert(P::kLoads + Q::kLoads == 8, "the wait below counts eight loads a pair");
     bf16x8 fp[2][S::kP], fq[2][S::kQ];
     auto fill = [&](u32 part) {
         p.fill(lp + part * S::kPartP, wave);
@@ -164,10 +167,11 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
 #pragma unroll
             for (u32 j = 0; j < S::kQ; ++j)
                 acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[h][i], fq[h][j], acc[i][j], 0, 0, 0);
+        also(fq[h]);
     };
     fill(0);
     fill(1);
-    __builtin_amdgcn_s_waitcnt(0xF70 | 8);              // the second pair's eight loads may be on their way
+    __builtin_amdgcn_s_waitcnt(kDirect ? 0xF70 | 8 : 0x070);        // the second pair's eight loads may be on their way
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     read(0, 0);
@@ -214,6 +218,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
     const u32 p0 = wave % WP * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
     f32x4 acc[S::kP][S::kQ] = {};
     const bool inside = run.block != ~0u;
+    const auto nothing = [](const bf16x8 (&)[S::kQ]) {};
     if (inside) {
         lds_char *lds = (lds_char *)wide_lds;
         const u32 steps = (r.sums + kStep - 1) / kStep;
@@ -223,11 +228,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
         if constexpr (ACROSS) {
             Across16<TP, S::kWaves> p;
             p.init(w + col0, r.ldw, width, r.sums, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing);
         } else {
             Along16<TP, S::kWaves> p;
             p.init(w + (u64)col0 * r.ldw, r.ldw, width, r.sums, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing);
         }
     }
     // Two neighbouring results exchange lanes, so that a lane has eight consecutive values of a row:
@@ -288,8 +293,137 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
 
 }  // namespace
 
-// ---- launches
 namespace {
+
+// ---- sums over rows
+
+// x of the sums over rows from its 8-bit form.  A thread has the 32 codes of a row that share a step; they come to registers
+// two pairs of steps ahead and are widened on their way into LDS (exactly: a code times a power of two), laid out as
+// Across16 does.  fill() writes the next pair and requests the one behind it.
+template <u32 W, u32 WAVES> struct Codes16 {
+    static constexpr bool kDirect = false;
+    static_assert(kPair * W / 32 == WAVES * kWave, "one group of 32 codes a thread");
+    const char *codes;      // this thread's codes of the next pair of steps
+    const uint8_t *scale;
+    u32 kp, row, rows;
+    bool there;
+    u32 read, to[2];
+    u32x4 v[2];
+    u32 e;
+
+    __device__ __forceinline__ void init(const char *codes_, const uint8_t *scale_, u32 kp_, u32 width, u32 sums, u32 lane)
+    {
+        const u32 group = threadIdx.x % (W / 32);
+        row = threadIdx.x / (W / 32);
+        kp = kp_;
+        rows = sums;
+        there = group * 32 < width;
+        codes = codes_ + (u64)row * kp + group * 32;
+        scale = scale_ + (u64)row * (kp / 32) + group;
+        read = across_read<W>(lane);
+#pragma unroll
+        for (u32 i = 0; i < 2; ++i) to[i] = row * (W * 2) + (((2 * group + i) ^ turn(row)) << 5);
+        request();
+    }
+    __device__ __forceinline__ void request()
+    {
+        v[0] = v[1] = u32x4{0, 0, 0, 0};
+        e = 0;
+        if (there && row < rows) {
+            v[0] = reinterpret_cast<const u32x4 *>(codes)[0];
+            v[1] = reinterpret_cast<const u32x4 *>(codes)[1];
+            e = *scale;
+        }
+        row += kPair;
+        codes += (u64)kPair * kp;
+        scale += (u64)kPair * (kp / 32);
+    }
+    __device__ __forceinline__ void fill(lds_char *lds, u32)
+    {
+        const float step = step_of(e);
+#pragma unroll
+        for (u32 i = 0; i < 4; ++i) {
+            u32x4 o;
+#pragma unroll
+            for (u32 h = 0; h < 4; ++h) {
+                const u32 q = v[i / 2][i % 2 * 2 + h / 2] >> (16 * (h % 2));
+                o[h] = pack_bf16(value_of(q, 0, step), value_of(q, 1, step));
+            }
+            *reinterpret_cast<lds_u32x4 *>(lds + to[i / 2] + 16 * (i % 2)) = o;
+        }
+        request();
+    }
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 h, u32 r0, u32 f) const { return across_fragment<W>(lds + h * kStep * W * 2, read, r0, f); }
+};
+
+// A tile of dw for a run of a block's rows: P = x (inputs), Q = dy (outputs).  db rides on the tiles of the first inputs: a
+// matrix instruction with ones in the place of x, the wavefronts along P taking turns.
+template <class S, u32 TP, u32 TQ, u32 WP, bool CODES>
+__global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArgs r)
+{
+    extern __shared__ __align__(16) char wide_lds[];
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 pairs = r.n_tiles * r.k_tiles, t = tile / pairs, pair = tile - t * pairs;
+    const u32 n0 = pair / r.k_tiles * TQ, k0 = pair % r.k_tiles * TP;
+    const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, t);
+    if (!run.found) return;
+    const u32 row0 = run_row(run, run.local), count = run_row(run, run.local + 1) - row0;
+    const u32 height = r.n - n0 < TQ ? r.n - n0 : TQ, width = r.k - k0 < TP ? r.k - k0 : TP;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const u32 pw = wave % WP, p0 = pw * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
+    const bool sums_db = r.db && k0 == 0;
+    f32x4 acc[S::kP][S::kQ] = {};
+    constexpr u32 kB = (S::kQ + WP - 1) / WP;
+    f32x4 bias[kB] = {};
+    if (count > 0) {
+        lds_char *lds = (lds_char *)wide_lds;
+        const u32 steps = (count + kStep - 1) / kStep;
+        const __bf16 one = (__bf16)1.0f;
+        const bf16x8 ones = {one, one, one, one, one, one, one, one};
+        const auto add = [&](const bf16x8 (&fq)[S::kQ]) {
+            if (!sums_db) return;
+#pragma unroll
+            for (u32 j = 0; j < S::kQ; ++j)
+                if (j % WP == pw) bias[j / WP] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fq[j], bias[j / WP], 0, 0, 0);
+        };
+        Across16<TQ, S::kWaves> q;
+        q.init(static_cast<const __bf16 *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, wave, lane);
+        if constexpr (CODES) {
+            const u32 kp = (r.k + 31) / 32 * 32;
+            Codes16<TP, S::kWaves> p;
+            p.init(static_cast<const char *>(r.x) + (u64)row0 * kp + k0, r.scale + (u64)row0 * (kp / 32) + k0 / 32, kp, width, count, lane);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
+        } else {
+            Across16<TP, S::kWaves> p;
+            p.init(static_cast<const __bf16 *>(r.x) + (u64)row0 * r.ldx + k0, r.ldx, width, count, wave, lane);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
+        }
+    }
+    // a block with one run has its result here; otherwise the run's partial sums
+    const bool whole = run.runs == 1;
+    const u64 size = (u64)r.n * r.k;
+    float *dw = whole ? r.dw + (u64)run.block * size : r.part + (u64)t * (size + r.n);
+    float *db = whole ? r.db + (u64)run.block * r.n : r.part + (u64)t * (size + r.n) + size;
+#pragma unroll
+    for (u32 j = 0; j < S::kQ; ++j) {
+        const u32 n = n0 + q0 + 16 * j + (lane & 15);
+        if (n >= r.n) continue;
+#pragma unroll
+        for (u32 i = 0; i < S::kP; ++i) {
+            const u32 k = k0 + p0 + 16 * i + 4 * (lane >> 4);
+            if (k >= r.k) continue;                     // k comes in eights
+            if (r.in_major) {
+#pragma unroll
+                for (u32 v = 0; v < 4; ++v) dw[(u64)(k + v) * r.n + n] = acc[i][j][v];
+            } else {
+                *reinterpret_cast<f32x4 *>(dw + (u64)n * r.k + k) = acc[i][j];
+            }
+        }
+        if (sums_db && j % WP == pw && lane < 16) db[n] = bias[j / WP][0];
+    }
+}
+
+// ---- launches
 
 template <u32 TP, u32 TQ, u32 WP, u32 WQ, bool ACROSS, u32 GATE>
 hipError_t wide_go(RowsArgs r, hipStream_t stream)
@@ -311,6 +445,20 @@ hipError_t wide_shape(const RowsArgs &r, hipStream_t stream)
     return wide_go<128, 128, 2, 2, ACROSS, GATE>(r, stream);
 }
 
+template <u32 TP, u32 TQ, u32 WP, u32 WQ>
+hipError_t wide_sums_go(SumsArgs r, bool codes, hipStream_t stream)
+{
+    using S = Shape<TP, TQ, WP, WQ>;
+    r.n_tiles = (r.n + TQ - 1) / TQ;
+    r.k_tiles = (r.k + TP - 1) / TP;
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, r.per, false) * r.n_tiles * r.k_tiles);
+    auto kernel = codes ? wide_sums_kernel<S, TP, TQ, WP, true> : wide_sums_kernel<S, TP, TQ, WP, false>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), S::kLds, stream, r);
+    return hipGetLastError();
+}
+
 bool sixteen(const void *p, u64 ld) { return ld % 8 == 0 && ld <= 1u << 21 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 }  // namespace
@@ -326,6 +474,18 @@ hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
     const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
     if (across) return gate == 0 ? wide_shape<true, 0>(r, stream) : gate == 1 ? wide_shape<true, 1>(r, stream) : wide_shape<true, 2>(r, stream);
     return gate == 0 ? wide_shape<false, 0>(r, stream) : gate == 1 ? wide_shape<false, 1>(r, stream) : wide_shape<false, 2>(r, stream);
+}
+
+bool wide_sums_fit(const SumsArgs &r)
+{
+    return r.n % 8 == 0 && r.k % 8 == 0 && r.dw && reinterpret_cast<uintptr_t>(r.dw) % 16 == 0 && sixteen(r.dy, r.lddy) &&
+           (r.scale || sixteen(r.x, r.ldx));
+}
+
+hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream)
+{
+    if (r.n > 128 && r.k > 128) return wide_sums_go<256, 256, 2, 4>(r, r.scale != nullptr, stream);
+    return wide_sums_go<128, 128, 2, 2>(r, r.scale != nullptr, stream);
 }
 
 }  // namespace lmk

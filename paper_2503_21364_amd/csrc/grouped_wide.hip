@@ -149,39 +149,40 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
     lds_char *lp = lds, *lq = lds + 2 * S::kPartP;
     constexpr bool kDirect = P::kDirect && Q::kDirect;
     if constexpr (kDirect) static_assert(P::kLoads + Q::kLoads == 8, "the wait below counts eight loads a pair");
-    bf16x8 fp[2][S::kP], fq[2][S::kQ];
+    bf16x8 fp[S::kP], fq[2][S::kQ];
     auto fill = [&](u32 part) {
         p.fill(lp + part * S::kPartP, wave);
         q.fill(lq + part * S::kPartQ, wave);
     };
-    auto read = [&](u32 part, u32 h) {
+    // multiplies step h and reads the fragments of half `hn` of part `pn`: those of P take the place of what has been used
+    auto step = [&](u32 h, u32 pn, u32 hn) {
 #pragma unroll
-        for (u32 i = 0; i < S::kP; ++i) fp[h][i] = p.fragment(lp + part * S::kPartP, h, p0, i);
+        for (u32 j = 0; j < S::kQ; ++j) fq[hn][j] = q.fragment(lq + pn * S::kPartQ, hn, q0, j);
 #pragma unroll
-        for (u32 j = 0; j < S::kQ; ++j) fq[h][j] = q.fragment(lq + part * S::kPartQ, h, q0, j);
-        asm volatile("" ::: "memory");              // the reads stay in front of the products
-    };
-    auto multiply = [&](u32 h) {
-#pragma unroll
-        for (u32 i = 0; i < S::kP; ++i)
+        for (u32 i = 0; i < S::kP; ++i) {
 #pragma unroll
             for (u32 j = 0; j < S::kQ; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[h][i], fq[h][j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp[i], fq[h][j], acc[i][j], 0, 0, 0);
+            fp[i] = p.fragment(lp + pn * S::kPartP, hn, p0, i);
+        }
         also(fq[h]);
+        asm volatile("" ::: "memory");              // the reads stay in this step
     };
     fill(0);
     fill(1);
     __builtin_amdgcn_s_waitcnt(kDirect ? 0xF70 | 8 : 0x070);        // the second pair's eight loads may be on their way
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    read(0, 0);
+#pragma unroll
+    for (u32 i = 0; i < S::kP; ++i) fp[i] = p.fragment(lp, 0, p0, i);
+#pragma unroll
+    for (u32 j = 0; j < S::kQ; ++j) fq[0][j] = q.fragment(lq, 0, q0, j);
     for (u32 t0 = 0; t0 < steps; t0 += 4) {
 #pragma unroll
         for (u32 part = 0; part < 2; ++part) {
             const u32 t = t0 + 2 * part;
             if (t >= steps) break;
-            read(part, 1);
-            multiply(0);
+            step(0, part, 1);
             if (t + 1 >= steps) break;
             // the next pair has arrived, and this pair's fragments have left LDS
             asm volatile("" ::: "memory");
@@ -189,8 +190,7 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             fill(part);
-            read(1 - part, 0);
-            multiply(1);
+            step(1, 1 - part, 0);
         }
     }
     // nothing may be on its way into LDS when the workgroup ends

@@ -35,6 +35,7 @@ UNITS = {
     "preprocess_bwd.hip": [],
     "anchor_decode.hip": [],
     "checkpoint8.hip": [],
+    "grouped_few.hip": [],
     "grouped_linear.hip": [],
     "grouped_wide.hip": [],
     "index.hip": EXACT,         # host code: the voxel of a primitive is decided by one fp32 division

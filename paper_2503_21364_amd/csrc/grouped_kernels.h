@@ -49,6 +49,10 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
     return id < per * dies ? id % dies * per + id / dies : id;
 }
 
+// few rows, any type and alignment
+bool few_rows_fit(const RowsArgs &r);
+hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream);
+
 // bfloat16 whose rows start at 16-byte boundaries
 bool wide_rows_fit(const RowsArgs &r, bool across);
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream);

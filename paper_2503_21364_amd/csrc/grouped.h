@@ -44,24 +44,27 @@ __device__ __forceinline__ RowRun find_run(const u32 *__restrict__ offsets, u32 
 {
     const u32 lane = threadIdx.x & (kWave - 1);
     const u32 segments = OUTSIDE ? blocks + 2 : blocks;
-    u32 before = 0;
-    for (u32 base = 0; base < segments; base += kWave) {
-        const u32 s = base + lane;
-        u32 b = 0, e = 0, count = 0;
-        if (s < segments) {
-            if (OUTSIDE) {
-                b = s == 0 ? 0u : offsets[s - 1];
-                e = s == blocks + 1 ? rows : offsets[s];
-            } else {
-                b = offsets[s];
-                e = offsets[s + 1];
-            }
-            b = b < rows ? b : rows;
-            e = e < rows ? e : rows;
-            e = e > b ? e : b;
-            count = (e - b + per - 1) / per;
-            if (!OUTSIDE && count == 0) count = 1;
+    const auto edge = [&](u32 s, u32 &b, u32 &e) {           // rows of segment s; only requests
+        b = e = 0;
+        if (s >= segments) return;
+        if (OUTSIDE) {
+            b = s == 0 ? 0u : offsets[s - 1];
+            e = s == blocks + 1 ? rows : offsets[s];
+        } else {
+            b = offsets[s];
+            e = offsets[s + 1];
         }
+    };
+    u32 before = 0, next_b, next_e;
+    edge(lane, next_b, next_e);
+    for (u32 base = 0; base < segments; base += kWave) {
+        u32 b = next_b, e = next_e;
+        edge(base + kWave + lane, next_b, next_e);
+        b = b < rows ? b : rows;
+        e = e < rows ? e : rows;
+        e = e > b ? e : b;
+        u32 count = (e - b + per - 1) / per;
+        if (!OUTSIDE && count == 0 && base + lane < segments) count = 1;
         const u32 upto = before + wave_scan(count);
         const u64 past = __builtin_amdgcn_ballot_w64(upto > t);
         if (past != 0ull) {

@@ -14,34 +14,28 @@ namespace {
 
 constexpr u32 kRows = 16;
 
-// V values of a row from `s` on; beyond `sums` zeros.  wide: rows start at boundaries of V values (of 16 bytes at most)
-template <class T, u32 V>
-__device__ __forceinline__ void load_run(float (&v)[V], const T *p, u32 s, u32 sums, bool wide)
+// V consecutive values as they are in memory, so that a load on its way holds no more registers than it fills
+template <class T, u32 V> using Run = T __attribute__((ext_vector_type(V)));
+
+// V values of a row from `s` on; beyond `sums` zeros.  WIDE: rows start and end at boundaries of V values
+template <class T, u32 V, bool WIDE> __device__ __forceinline__ Run<T, V> load_run(const T *p, u32 s, u32 sums)
 {
-    if constexpr (V % 4 == 0) {
-        if (wide && s + V <= sums) {
-            if constexpr (V * sizeof(T) == 16) {
-                typedef __attribute__((ext_vector_type(V))) T vec;
-                const vec q = *reinterpret_cast<const vec *>(p + s);
+    Run<T, V> v = {};
+    if constexpr (WIDE) {
+        if (s < sums) v = *reinterpret_cast<const Run<T, V> *>(p + s);
+    } else {
 #pragma unroll
-                for (u32 e = 0; e < V; ++e) v[e] = to_f32(q[e]);
-            } else {
-                const f32x4 q = load4(p + s);
-#pragma unroll
-                for (u32 e = 0; e < V; ++e) v[e] = q[e];
-            }
-            return;
-        }
+        for (u32 e = 0; e < V; ++e)
+            if (s + e < sums) v[e] = p[s + e];
     }
-#pragma unroll
-    for (u32 e = 0; e < V; ++e) v[e] = s + e < sums ? to_f32(p[s + e]) : 0.0f;
+    return v;
 }
 
 // GATE: 0 none, 1 values, 2 codes
-template <class T, u32 NT, bool ACROSS, u32 GATE>
-__global__ __launch_bounds__(512) void few_rows_kernel(const RowsArgs r)
+template <class T, u32 NT, bool ACROSS, bool WIDE, u32 GATE>
+__global__ __launch_bounds__(512, WIDE ? 6 : 4) void few_rows_kernel(const RowsArgs r)
 {
-    constexpr u32 kWaves = 8, kC = NT / 16, V = ACROSS ? 4 : 16 / sizeof(T), kAhead = (NT == 64 ? 16 : 32) / V;
+    constexpr u32 kWaves = 8, kC = NT / 16, V = ACROSS ? 4 : 16 / sizeof(T), kAhead = NT == 64 ? 2 : 4;
     __shared__ float part[kWaves][kRows][NT + 1];
     const u32 row_tile = blockIdx.x / r.col_tiles, col0 = (blockIdx.x - row_tile * r.col_tiles) * NT;
     const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, kRows, row_tile);
@@ -59,26 +53,24 @@ __global__ __launch_bounds__(512) void few_rows_kernel(const RowsArgs r)
         constexpr u32 step = 4 * V;
         const u32 all = (r.sums + step - 1) / step, per = (all + kWaves - 1) / kWaves;
         const u32 first = wave * per, last = first + per < all ? first + per : all;
-        float fx[kAhead][V], fw[kAhead][kC][V];
+        Run<T, V> fx[kAhead];
+        Run<T, V> along[kAhead][kC];                    // weights: V sum indices of a column,
+        Run<T, kC> across[kAhead][V];                   // or kC columns of a sum index
         for (u32 t0 = first; t0 < last; t0 += kAhead) {
 #pragma unroll
             for (u32 a = 0; a < kAhead; ++a) {
                 const u32 s = (t0 + a) * step + q * V;
                 const bool on = t0 + a < last;
-                load_run<T, V>(fx[a], x, s, on ? r.sums : 0u, r.wide_a);
-#pragma unroll
-                for (u32 c = 0; c < kC; ++c) {
-                    if (ACROSS) continue;
-                    const u32 n = 16 * c + j;
-                    load_run<T, V>(fw[a][c], w + (u64)(col0 + (n < width ? n : 0)) * r.ldw, s, on ? r.sums : 0u, r.wide_w);
-                }
+                fx[a] = load_run<T, V, WIDE>(x, s, on ? r.sums : 0u);
                 if constexpr (ACROSS) {
 #pragma unroll
-                    for (u32 e = 0; e < V; ++e) {
-                        float v[kC];
-                        load_run<T, kC>(v, w + (u64)(s + e) * r.ldw + col0, kC * j, on && s + e < r.sums ? width : 0u, r.wide_w);
+                    for (u32 e = 0; e < V; ++e)
+                        across[a][e] = load_run<T, kC, WIDE>(w + (u64)(s + e) * r.ldw + col0, kC * j, on && s + e < r.sums ? width : 0u);
+                } else {
 #pragma unroll
-                        for (u32 c = 0; c < kC; ++c) fw[a][c][e] = v[c];
+                    for (u32 c = 0; c < kC; ++c) {
+                        const u32 n = 16 * c + j;
+                        along[a][c] = load_run<T, V, WIDE>(w + (u64)(col0 + (n < width ? n : 0)) * r.ldw, s, on ? r.sums : 0u);
                     }
                 }
             }
@@ -87,7 +79,8 @@ __global__ __launch_bounds__(512) void few_rows_kernel(const RowsArgs r)
 #pragma unroll
                 for (u32 e = 0; e < V; ++e)
 #pragma unroll
-                    for (u32 c = 0; c < kC; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[a][e], fw[a][c][e], acc[c], 0, 0, 0);
+                    for (u32 c = 0; c < kC; ++c)
+                        acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(to_f32(fx[a][e]), to_f32(ACROSS ? across[a][e][c] : along[a][c][e]), acc[c], 0, 0, 0);
         }
         // result c: rows 4 q .. 4 q + 3, column j of it
 #pragma unroll
@@ -113,29 +106,29 @@ __global__ __launch_bounds__(512) void few_rows_kernel(const RowsArgs r)
     }
 }
 
-template <class T, u32 NT, bool ACROSS, u32 GATE>
+template <class T, u32 NT, bool ACROSS, bool WIDE, u32 GATE>
 hipError_t few_go(RowsArgs r, hipStream_t stream)
 {
     r.col_tiles = (r.cols + NT - 1) / NT;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, kRows, true) * r.col_tiles);
-    hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
+    hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, WIDE, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
     return hipGetLastError();
 }
 template <class T, bool ACROSS, u32 GATE>
 hipError_t few_width(const RowsArgs &r, hipStream_t stream)
 {
+    constexpr u32 v = ACROSS ? 4 : 16 / sizeof(T);          // a run of x, and of the weights
+    const auto runs = [](const void *p, u64 ld) { return ld % v == 0 && reinterpret_cast<uintptr_t>(p) % (v * sizeof(T)) == 0; };
+    const bool wide = runs(r.a, r.lda) && runs(r.w, r.ldw) && r.w_block % v == 0 && r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
     // 64 columns make whole lines where columns are contiguous and read x once for four results; 16 where that leaves
     // compute units without work
-    if (max_runs(r.rows, r.blocks, kRows, true) * ((r.cols + 63) / 64) >= 256) return few_go<T, 64, ACROSS, GATE>(r, stream);
-    return few_go<T, 16, ACROSS, GATE>(r, stream);
+    if (max_runs(r.rows, r.blocks, kRows, true) * ((r.cols + 63) / 64) >= 256)
+        return wide ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
+    return wide ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
 }
 template <class T>
-hipError_t few_as(RowsArgs r, bool across, hipStream_t stream)
+hipError_t few_as(const RowsArgs &r, bool across, hipStream_t stream)
 {
-    const u32 v = across ? 4 : 16 / sizeof(T);
-    const auto wide = [v](const void *p, u64 ld) { return ld % v == 0 && reinterpret_cast<uintptr_t>(p) % (v * sizeof(T)) == 0; };
-    r.wide_a = wide(r.a, r.lda);
-    r.wide_w = wide(r.w, r.ldw) && r.w_block % v == 0;
     const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
     if (across) return gate == 0 ? few_width<T, true, 0>(r, stream) : gate == 1 ? few_width<T, true, 1>(r, stream) : few_width<T, true, 2>(r, stream);
     return gate == 0 ? few_width<T, false, 0>(r, stream) : gate == 1 ? few_width<T, false, 1>(r, stream) : few_width<T, false, 2>(r, stream);

@@ -122,7 +122,7 @@ hipError_t few_width(const RowsArgs &r, hipStream_t stream)
     const bool wide = runs(r.a, r.lda) && runs(r.w, r.ldw) && r.w_block % v == 0 && r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
     // 64 columns make whole lines where columns are contiguous and read x once for four results; 16 where that leaves
     // compute units without work
-    if (max_runs(r.rows, r.blocks, kRows, true) * ((r.cols + 63) / 64) >= 256)
+    if (max_runs(r.rows, r.blocks, kRows, true) * ((r.cols + 63) / 64) >= (ACROSS ? 64 : 256))
         return wide ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
     return wide ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
 }
@@ -136,7 +136,7 @@ hipError_t few_as(const RowsArgs &r, bool across, hipStream_t stream)
 
 }  // namespace
 
-bool few_rows_fit(const RowsArgs &r) { return r.rows <= 256; }
+bool few_rows_fit(const RowsArgs &r, bool wide) { return wide ? r.rows <= 128 || r.rows <= 16 * r.blocks : r.rows <= 1024 || (r.rows <= 4096 && r.rows <= 64 * r.blocks); }
 
 hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream)
 {

@@ -50,7 +50,7 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
 }
 
 // few rows, any type and alignment
-bool few_rows_fit(const RowsArgs &r);
+bool few_rows_fit(const RowsArgs &r, bool wide);
 hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream);
 
 // bfloat16 whose rows start at 16-byte boundaries

@@ -400,8 +400,9 @@ void rows_width(const RowsArgs &r, hipStream_t stream)
 template <class T>
 hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
 {
-    if (few_rows_fit(r)) return launch_few_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
-    if (std::is_same<T, __bf16>::value && wide_rows_fit(r, across)) return launch_wide_rows(r, across, stream);
+    const bool wide = std::is_same<T, __bf16>::value && wide_rows_fit(r, across);
+    if (few_rows_fit(r, wide)) return launch_few_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
+    if (wide) return launch_wide_rows(r, across, stream);
     const u32 tn = tile_width(r.cols);
     r.col_tiles = (r.cols + tn - 1) / tn;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, 128, true) * r.col_tiles);

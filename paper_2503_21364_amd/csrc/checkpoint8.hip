@@ -21,7 +21,7 @@ __device__ __forceinline__ ItemRow item_row(u32 row0, u32 quad0, u32 step, u32 q
     return ItemRow{row0 + r, q - r * quads};
 }
 
-template <class T, bool WIDE>
+template <class T>
 __global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ x, u64 ldx, u32 rows, u32 k,
                                                    const u32 *__restrict__ offsets, u32 blocks,
                                                    u32 *__restrict__ codes, uint8_t *__restrict__ scale)
@@ -40,7 +40,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ x, u64 
         if (at[i].row >= rows || at[i].row < lo || at[i].row >= hi) continue;
         const u32 c = at[i].quad * 4;
         const T *p = x + (u64)at[i].row * ldx + c;
-        if (WIDE && c + 4 <= k) {
+        if (c + 4 <= k) {
             v[i] = load4(p);
         } else {
 #pragma unroll
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void pack_kernel(const T *__restrict__ x, u64 
     }
 }
 
-template <class T, bool WIDE>
+template <class T>
 __global__ __launch_bounds__(256) void unpack_kernel(const u32 *__restrict__ codes, const uint8_t *__restrict__ scale,
                                                      u32 rows, u32 k, T *__restrict__ x, u64 ldx)
 {
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256) void unpack_kernel(const u32 *__restrict__ cod
         const u32 q = codes[item];
         const float step = step_of(scale[item / kLanes]);
         T *p = x + (u64)at.row * ldx + c;
-        if (WIDE && c + 4 <= k) {
+        if (c + 4 <= k) {
             store4(p, f32x4{value_of(q, 0, step), value_of(q, 1, step), value_of(q, 2, step), value_of(q, 3, step)});
         } else {
 #pragma unroll
@@ -97,29 +97,18 @@ __global__ __launch_bounds__(256) void unpack_kernel(const u32 *__restrict__ cod
 }
 
 template <class T>
-bool four_wide(const void *p, u64 ld) { return ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0; }
-
-template <class T>
 hipError_t pack_as(const void *x, u64 ldx, u32 rows, u32 k, const u32 *offsets, u32 blocks, const lmk_gs_checkpoint8 &out,
                    u32 grid, hipStream_t stream)
 {
-    u32 *codes = reinterpret_cast<u32 *>(out.codes);
-    if (four_wide<T>(x, ldx))
-        hipLaunchKernelGGL((pack_kernel<T, true>), dim3(grid), dim3(256), 0, stream, (const T *)x, ldx, rows, k,
-                           offsets, blocks, codes, out.scale);
-    else
-        hipLaunchKernelGGL((pack_kernel<T, false>), dim3(grid), dim3(256), 0, stream, (const T *)x, ldx, rows, k,
-                           offsets, blocks, codes, out.scale);
+    hipLaunchKernelGGL(pack_kernel<T>, dim3(grid), dim3(256), 0, stream, (const T *)x, ldx, rows, k, offsets, blocks,
+                       reinterpret_cast<u32 *>(out.codes), out.scale);
     return hipGetLastError();
 }
 template <class T>
 hipError_t unpack_as(const lmk_gs_checkpoint8 &kept, u32 rows, u32 k, void *x, u64 ldx, u32 grid, hipStream_t stream)
 {
-    const u32 *codes = reinterpret_cast<const u32 *>(kept.codes);
-    if (four_wide<T>(x, ldx))
-        hipLaunchKernelGGL((unpack_kernel<T, true>), dim3(grid), dim3(256), 0, stream, codes, kept.scale, rows, k, (T *)x, ldx);
-    else
-        hipLaunchKernelGGL((unpack_kernel<T, false>), dim3(grid), dim3(256), 0, stream, codes, kept.scale, rows, k, (T *)x, ldx);
+    hipLaunchKernelGGL(unpack_kernel<T>, dim3(grid), dim3(256), 0, stream, reinterpret_cast<const u32 *>(kept.codes), kept.scale,
+                       rows, k, (T *)x, ldx);
     return hipGetLastError();
 }
 

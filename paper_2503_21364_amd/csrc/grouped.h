@@ -15,16 +15,26 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__bf16 v) { return (float)v; }
 
-__device__ __forceinline__ f32x4 load4(const float *p) { return *reinterpret_cast<const f32x4 *>(p); }
+// Vectors at any address their elements may have: the rows of the matrices here start where they will, and the
+// vector memory instructions take that.
+template <class V, class T> __device__ __forceinline__ V load_any(const T *p)
+{
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
+template <class V, class T> __device__ __forceinline__ void store_any(T *p, V v) { __builtin_memcpy(p, &v, sizeof(V)); }
+
+__device__ __forceinline__ f32x4 load4(const float *p) { return load_any<f32x4>(p); }
 __device__ __forceinline__ f32x4 load4(const __bf16 *p)
 {
-    const bf16x4 v = *reinterpret_cast<const bf16x4 *>(p);
+    const bf16x4 v = load_any<bf16x4>(p);
     return f32x4{(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
 }
-__device__ __forceinline__ void store4(float *p, f32x4 v) { *reinterpret_cast<f32x4 *>(p) = v; }
+__device__ __forceinline__ void store4(float *p, f32x4 v) { store_any(p, v); }
 __device__ __forceinline__ void store4(__bf16 *p, f32x4 v)
 {
-    *reinterpret_cast<bf16x4 *>(p) = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    store_any(p, bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]});
 }
 
 // The rows a workgroup works on: run `local` of `per` rows of the rows begin..end of a block.

@@ -17,12 +17,12 @@ constexpr u32 kRows = 16;
 // V consecutive values as they are in memory, so that a load on its way holds no more registers than it fills
 template <class T, u32 V> using Run = T __attribute__((ext_vector_type(V)));
 
-// V values of a row from `s` on; beyond `sums` zeros.  WIDE: rows start and end at boundaries of V values
-template <class T, u32 V, bool WIDE> __device__ __forceinline__ Run<T, V> load_run(const T *p, u32 s, u32 sums)
+// V values of a row from `s` on; beyond `sums` zeros.  WHOLE: rows are whole runs of V values
+template <class T, u32 V, bool WHOLE> __device__ __forceinline__ Run<T, V> load_run(const T *p, u32 s, u32 sums)
 {
     Run<T, V> v = {};
-    if constexpr (WIDE) {
-        if (s < sums) v = *reinterpret_cast<const Run<T, V> *>(p + s);
+    if constexpr (WHOLE) {
+        if (s < sums) v = load_any<Run<T, V>>(p + s);
     } else {
 #pragma unroll
         for (u32 e = 0; e < V; ++e)
@@ -32,8 +32,8 @@ template <class T, u32 V, bool WIDE> __device__ __forceinline__ Run<T, V> load_r
 }
 
 // GATE: 0 none, 1 values, 2 codes
-template <class T, u32 NT, bool ACROSS, bool WIDE, u32 GATE>
-__global__ __launch_bounds__(512, WIDE ? 6 : 4) void few_rows_kernel(const RowsArgs r)
+template <class T, u32 NT, bool ACROSS, bool WHOLE, u32 GATE>
+__global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const RowsArgs r)
 {
     constexpr u32 kWaves = 8, kC = NT / 16, V = ACROSS ? 4 : 16 / sizeof(T), kAhead = NT == 64 ? 2 : 4;
     __shared__ float part[kWaves][kRows][NT + 1];
@@ -61,16 +61,16 @@ __global__ __launch_bounds__(512, WIDE ? 6 : 4) void few_rows_kernel(const RowsA
             for (u32 a = 0; a < kAhead; ++a) {
                 const u32 s = (t0 + a) * step + q * V;
                 const bool on = t0 + a < last;
-                fx[a] = load_run<T, V, WIDE>(x, s, on ? r.sums : 0u);
+                fx[a] = load_run<T, V, WHOLE>(x, s, on ? r.sums : 0u);
                 if constexpr (ACROSS) {
 #pragma unroll
                     for (u32 e = 0; e < V; ++e)
-                        across[a][e] = load_run<T, kC, WIDE>(w + (u64)(s + e) * r.ldw + col0, kC * j, on && s + e < r.sums ? width : 0u);
+                        across[a][e] = load_run<T, kC, WHOLE>(w + (u64)(s + e) * r.ldw + col0, kC * j, on && s + e < r.sums ? width : 0u);
                 } else {
 #pragma unroll
                     for (u32 c = 0; c < kC; ++c) {
                         const u32 n = 16 * c + j;
-                        along[a][c] = load_run<T, V, WIDE>(w + (u64)(col0 + (n < width ? n : 0)) * r.ldw, s, on ? r.sums : 0u);
+                        along[a][c] = load_run<T, V, WHOLE>(w + (u64)(col0 + (n < width ? n : 0)) * r.ldw, s, on ? r.sums : 0u);
                     }
                 }
             }
@@ -106,25 +106,24 @@ __global__ __launch_bounds__(512, WIDE ? 6 : 4) void few_rows_kernel(const RowsA
     }
 }
 
-template <class T, u32 NT, bool ACROSS, bool WIDE, u32 GATE>
+template <class T, u32 NT, bool ACROSS, bool WHOLE, u32 GATE>
 hipError_t few_go(RowsArgs r, hipStream_t stream)
 {
     r.col_tiles = (r.cols + NT - 1) / NT;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, kRows, true) * r.col_tiles);
-    hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, WIDE, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
+    hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, WHOLE, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
     return hipGetLastError();
 }
 template <class T, bool ACROSS, u32 GATE>
 hipError_t few_width(const RowsArgs &r, hipStream_t stream)
 {
     constexpr u32 v = ACROSS ? 4 : 16 / sizeof(T);          // a run of x, and of the weights
-    const auto runs = [](const void *p, u64 ld) { return ld % v == 0 && reinterpret_cast<uintptr_t>(p) % (v * sizeof(T)) == 0; };
-    const bool wide = runs(r.a, r.lda) && runs(r.w, r.ldw) && r.w_block % v == 0 && r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
+    const bool whole = r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
     // 64 columns make whole lines where columns are contiguous and read x once for four results; 16 where that leaves
     // compute units without work
     if (max_runs(r.rows, r.blocks, kRows, true) * ((r.cols + 63) / 64) >= (ACROSS ? 64 : 256))
-        return wide ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
-    return wide ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
+        return whole ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
+    return whole ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
 }
 template <class T>
 hipError_t few_as(const RowsArgs &r, bool across, hipStream_t stream)

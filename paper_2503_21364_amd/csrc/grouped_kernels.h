@@ -21,7 +21,6 @@ struct RowsArgs {
     u64 ldgate;                 // elements (codes) between its rows
     const uint8_t *gate_scale;  // of codes
     u32 tiles, col_tiles;
-    bool wide_a, wide_w;
 };
 
 // sums over the rows of a block
@@ -38,7 +37,6 @@ struct SumsArgs {
     float *part;                // run t: n k sums of dw, then n of db
     u32 per;                    // rows of a run
     u32 tiles, n_tiles, k_tiles;
-    bool wide_dy, wide_x;
 };
 
 // Workgroups go to the eight dies in turn; this gives each die a run of consecutive tiles, which share operands.

@@ -31,52 +31,35 @@ template <class T, u32 W> struct Along {
     const T *p;
     u64 ld;
     u32 width, sums;        // valid rows, valid sum indices
-    bool wide;              // rows start at four-element boundaries
     float v[W / 8];
 
     __device__ __forceinline__ void load(u32 s0)
     {
-        if (wide) {
 #pragma unroll
-            for (u32 i = 0; i < W / 32; ++i) {
-                const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = s0 + c % 8 * 4;
-                f32x4 q = {0.f, 0.f, 0.f, 0.f};
-                if (m < width) {
-                    const T *a = p + (u64)m * ld + s;
-                    if (s + 4 <= sums) q = load4(a);
-                    else {
+        for (u32 i = 0; i < W / 32; ++i) {
+            const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = s0 + c % 8 * 4;
+            f32x4 q = {0.f, 0.f, 0.f, 0.f};
+            if (m < width) {
+                const T *a = p + (u64)m * ld + s;
+                if (s + 4 <= sums) q = load4(a);
+                else {
 #pragma unroll
-                        for (u32 j = 0; j < 4; ++j)
-                            if (s + j < sums) q[j] = to_f32(a[j]);
-                    }
+                    for (u32 j = 0; j < 4; ++j)
+                        if (s + j < sums) q[j] = to_f32(a[j]);
                 }
-#pragma unroll
-                for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
             }
-        } else {
 #pragma unroll
-            for (u32 i = 0; i < W / 8; ++i) {
-                const u32 c = threadIdx.x + i * kThreads, m = c / kStep, s = s0 + c % kStep;
-                v[i] = (m < width && s < sums) ? to_f32(p[(u64)m * ld + s]) : 0.0f;
-            }
+            for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
         }
     }
     __device__ __forceinline__ void store(float *lds) const
     {
         constexpr u32 pitch = pitch_of(W);
-        if (wide) {
 #pragma unroll
-            for (u32 i = 0; i < W / 32; ++i) {
-                const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = c % 8 * 4;
+        for (u32 i = 0; i < W / 32; ++i) {
+            const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = c % 8 * 4;
 #pragma unroll
-                for (u32 j = 0; j < 4; ++j) lds[(s + j) * pitch + m] = v[4 * i + j];
-            }
-        } else {
-#pragma unroll
-            for (u32 i = 0; i < W / 8; ++i) {
-                const u32 c = threadIdx.x + i * kThreads;
-                lds[(c % kStep) * pitch + c / kStep] = v[i];
-            }
+            for (u32 j = 0; j < 4; ++j) lds[(s + j) * pitch + m] = v[4 * i + j];
         }
     }
 };
@@ -86,52 +69,35 @@ template <class T, u32 W> struct Across {
     const T *p;
     u64 ld;
     u32 width, sums;
-    bool wide;
     float v[W / 8];
 
     __device__ __forceinline__ void load(u32 s0)
     {
-        if (wide) {
 #pragma unroll
-            for (u32 i = 0; i < W / 32; ++i) {
-                const u32 c = threadIdx.x + i * kThreads, s = s0 + c / (W / 4), m = c % (W / 4) * 4;
-                f32x4 q = {0.f, 0.f, 0.f, 0.f};
-                if (s < sums && m < width) {
-                    const T *a = p + (u64)s * ld + m;
-                    if (m + 4 <= width) q = load4(a);
-                    else {
+        for (u32 i = 0; i < W / 32; ++i) {
+            const u32 c = threadIdx.x + i * kThreads, s = s0 + c / (W / 4), m = c % (W / 4) * 4;
+            f32x4 q = {0.f, 0.f, 0.f, 0.f};
+            if (s < sums && m < width) {
+                const T *a = p + (u64)s * ld + m;
+                if (m + 4 <= width) q = load4(a);
+                else {
 #pragma unroll
-                        for (u32 j = 0; j < 4; ++j)
-                            if (m + j < width) q[j] = to_f32(a[j]);
-                    }
+                    for (u32 j = 0; j < 4; ++j)
+                        if (m + j < width) q[j] = to_f32(a[j]);
                 }
-#pragma unroll
-                for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
             }
-        } else {
 #pragma unroll
-            for (u32 i = 0; i < W / 8; ++i) {
-                const u32 c = threadIdx.x + i * kThreads, s = s0 + c / W, m = c % W;
-                v[i] = (s < sums && m < width) ? to_f32(p[(u64)s * ld + m]) : 0.0f;
-            }
+            for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
         }
     }
     __device__ __forceinline__ void store(float *lds) const
     {
         constexpr u32 pitch = pitch_of(W);
-        if (wide) {
 #pragma unroll
-            for (u32 i = 0; i < W / 32; ++i) {
-                const u32 c = threadIdx.x + i * kThreads, s = c / (W / 4), m = c % (W / 4) * 4;
+        for (u32 i = 0; i < W / 32; ++i) {
+            const u32 c = threadIdx.x + i * kThreads, s = c / (W / 4), m = c % (W / 4) * 4;
 #pragma unroll
-                for (u32 j = 0; j < 4; ++j) lds[s * pitch + m + j] = v[4 * i + j];
-            }
-        } else {
-#pragma unroll
-            for (u32 i = 0; i < W / 8; ++i) {
-                const u32 c = threadIdx.x + i * kThreads;
-                lds[(c / W) * pitch + c % W] = v[i];
-            }
+            for (u32 j = 0; j < 4; ++j) lds[s * pitch + m + j] = v[4 * i + j];
         }
     }
 };
@@ -244,13 +210,13 @@ __global__ __launch_bounds__(256, 2) void rows_kernel(const RowsArgs r)
     const u32 m0 = wave / S::kCols * (S::kM * 32), n0 = wave % S::kCols * (S::kN * 32);
     f32x16 acc[S::kM][S::kN] = {};
     if (run.block != ~0u) {
-        Along<T, TM> a{static_cast<const T *>(r.a) + (u64)row0 * r.lda, r.lda, height, r.sums, r.wide_a, {}};
+        Along<T, TM> a{static_cast<const T *>(r.a) + (u64)row0 * r.lda, r.lda, height, r.sums, {}};
         const T *w = static_cast<const T *>(r.w) + (u64)run.block * r.w_block;
         if constexpr (ACROSS) {
-            Across<T, TN> b{w + col0, r.ldw, width, r.sums, r.wide_w, {}};
+            Across<T, TN> b{w + col0, r.ldw, width, r.sums, {}};
             tile_product<TM, TN>(a, b, r.sums, lds, acc, [](const float *) {});
         } else {
-            Along<T, TN> b{w + (u64)col0 * r.ldw, r.ldw, width, r.sums, r.wide_w, {}};
+            Along<T, TN> b{w + (u64)col0 * r.ldw, r.ldw, width, r.sums, {}};
             tile_product<TM, TN>(a, b, r.sums, lds, acc, [](const float *) {});
         }
     }
@@ -299,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void sums_kernel(const SumsArgs r)
     f32x16 acc[S::kM][S::kN] = {};
     float bias = 0.0f;
     if (count > 0) {
-        Across<T, TM> a{static_cast<const T *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, r.wide_dy, {}};
+        Across<T, TM> a{static_cast<const T *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, {}};
         // thread m sums column m of the staged dy
         const bool sums_db = r.db && k0 == 0 && threadIdx.x < TM;
         auto each = [&](const float *la) {
@@ -314,7 +280,7 @@ __global__ __launch_bounds__(256, 2) void sums_kernel(const SumsArgs r)
             tile_product<TM, TN>(a, b, count, lds, acc, each);
         } else {
             Across<T, TN> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)row0 * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
-                            count, r.wide_x, {}};
+                            count, {}};
             tile_product<TM, TN>(a, b, count, lds, acc, each);
         }
     }
@@ -377,9 +343,6 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
     dst[i < size ? (u64)block * size + i : (u64)block * n + (i - size)] = sum;
 }
 
-template <class T>
-bool four_wide(const void *p, u64 ld) { return ld % 4 == 0 && reinterpret_cast<uintptr_t>(p) % (4 * sizeof(T)) == 0; }
-
 u32 tile_width(u32 cols) { return cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 96 ? 96 : 128; }
 
 template <class T, u32 TN, bool ACROSS, u32 GATE>
@@ -406,8 +369,6 @@ hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
     const u32 tn = tile_width(r.cols);
     r.col_tiles = (r.cols + tn - 1) / tn;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, 128, true) * r.col_tiles);
-    r.wide_a = four_wide<T>(r.a, r.lda);
-    r.wide_w = four_wide<T>(r.w, r.ldw) && r.w_block % 4 == 0;
     const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
     if (across) gate == 0 ? rows_width<T, true, 0>(r, stream) : gate == 1 ? rows_width<T, true, 1>(r, stream) : rows_width<T, true, 2>(r, stream);
     else gate == 0 ? rows_width<T, false, 0>(r, stream) : gate == 1 ? rows_width<T, false, 1>(r, stream) : rows_width<T, false, 2>(r, stream);
@@ -438,8 +399,6 @@ hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
     r.n_tiles = (r.n + 127) / 128;
     r.k_tiles = kind == 0 ? 1 : (r.k + tn - 1) / tn;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, r.per, false) * r.n_tiles * r.k_tiles);
-    r.wide_dy = four_wide<T>(r.dy, r.lddy);
-    r.wide_x = kind == 1 && four_wide<T>(r.x, r.ldx);
     switch (tn) {
     case 32: sums_go<T, 32>(r, kind, stream); break;
     case 64: sums_go<T, 64>(r, kind, stream); break;

@@ -14,6 +14,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -37,6 +38,7 @@ UNITS = {
     "checkpoint8.hip": [],
     "grouped_few.hip": [],
     "grouped_linear.hip": [],
+    "grouped_narrow.hip": [],
     "grouped_wide.hip": [],
     "index.hip": EXACT,         # host code: the voxel of a primitive is decided by one fp32 division
 }
@@ -52,14 +54,16 @@ def hipcc() -> str:
 def build(verbose: bool = False) -> str:
     cc = hipcc()
     os.makedirs(OBJDIR, exist_ok=True)
-    objs = []
-    for unit, extra in UNITS.items():
-        obj = os.path.join(OBJDIR, unit.replace(".hip", ".o"))
-        cmd = [cc, *COMMON, *extra, "-c", os.path.join(CSRC, unit), "-o", obj]
+    objs = [os.path.join(OBJDIR, unit.replace(".hip", ".o")) for unit in UNITS]
+
+    def compile_unit(unit, obj):
+        cmd = [cc, *COMMON, *UNITS[unit], "-c", os.path.join(CSRC, unit), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.check_call(cmd)
-        objs.append(obj)
+
+    with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:
+        list(pool.map(compile_unit, UNITS, objs))
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [cc, "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs,
            "-Wl,-rpath,/opt/rocm/lib", "-Wl,--no-undefined"]

@@ -21,6 +21,10 @@ struct RowsArgs {
     u64 ldgate;                 // elements (codes) between its rows
     const uint8_t *gate_scale;  // of codes
     u32 tiles, col_tiles;
+    u32 per;                    // rows of a run, where that is not fixed
+    bool across;                // weights: columns contiguous, not sum indices
+    u32 *keep_codes;            // NULL, or where the 8-bit form of a goes
+    uint8_t *keep_scale;
 };
 
 // sums over the rows of a block
@@ -50,6 +54,10 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
 // few rows, any type and alignment
 bool few_rows_fit(const RowsArgs &r, bool wide);
 hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream);
+
+// small matrices, any type and alignment; the only rows kernel that writes the 8-bit form of its input
+bool narrow_rows_fit(const RowsArgs &r);
+hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream);
 
 // bfloat16 whose rows start at 16-byte boundaries
 bool wide_rows_fit(const RowsArgs &r, bool across);

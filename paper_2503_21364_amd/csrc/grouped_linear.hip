@@ -364,7 +364,15 @@ template <class T>
 hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
 {
     const bool wide = std::is_same<T, __bf16>::value && wide_rows_fit(r, across);
+    if (r.keep_codes) {
+        if (narrow_rows_fit(r)) return launch_narrow_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
+        const lmk_gs_checkpoint8 keep = {reinterpret_cast<int8_t *>(r.keep_codes), r.keep_scale};
+        const hipError_t e = launch_checkpoint8_pack(r.a, r.lda, r.rows, r.sums, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16,
+                                                     r.offsets, r.blocks, keep, stream);
+        if (e != hipSuccess) return e;
+    }
     if (few_rows_fit(r, wide)) return launch_few_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
+    if (narrow_rows_fit(r)) return launch_narrow_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
     if (wide) return launch_wide_rows(r, across, stream);
     const u32 tn = tile_width(r.cols);
     r.col_tiles = (r.cols + tn - 1) / tn;
@@ -428,11 +436,11 @@ size_t grouped_backward_bytes(const lmk_gs_linear &l)
 hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
                                  u64 ldy, const lmk_gs_checkpoint8 *keep, hipStream_t stream)
 {
-    if (keep) {
-        const hipError_t e = launch_checkpoint8_pack(x, ldx, l.rows, l.k, l.dtype, l.offsets, l.blocks, *keep, stream);
-        if (e != hipSuccess) return e;
-    }
     RowsArgs r = {};
+    if (keep) {
+        r.keep_codes = reinterpret_cast<u32 *>(keep->codes);
+        r.keep_scale = keep->scale;
+    }
     r.a = x; r.lda = ldx;
     r.w = l.w; r.ldw = l.ldw; r.w_block = l.w_block;
     r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.cols = l.n; r.sums = l.k;

@@ -1,0 +1,232 @@
+// Grouped layers whose weights are small (the decoder's: 35 x 96, 32 x 70): memory is all of it, so a row is read once and its
+// results leave once.  A workgroup keeps its block's whole matrix in LDS, in the order the matrix instructions take it, and
+// its four wavefronts walk through a run of the block's rows in tiles of 32, each by itself: the next tile's rows are
+// on their way to registers while a tile is multiplied, and nothing is waited for in common.
+//
+// v_mfma_f32_16x16x4_f32 with the weights on its rows and the layer's rows on its columns: a lane has four
+// consecutive outputs of a row, one 16-byte store.  In LDS a row of x takes a pitch of 4 (odd) floats: the 16 rows and
+// four sum indices that an instruction reads are on 64 different banks.
+#include "grouped_kernels.h"
+
+namespace lmk {
+
+namespace {
+
+constexpr u32 kTileRows = 32;
+
+__device__ __forceinline__ void wave_meets()          // LDS written by other lanes of this wavefront
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+__host__ __device__ constexpr u32 pitch_of(u32 sums) { return ((sums + 3) / 4 | 1) * 4; }
+
+// four values of a row of `width`, from c on; what is beyond it: zeros
+template <class T> __device__ __forceinline__ f32x4 load4_of(const T *p, u32 c, u32 width)
+{
+    if (c + 4 <= width) return load4(p + c);
+    f32x4 v = {};
+#pragma unroll
+    for (u32 e = 0; e < 4; ++e)
+        if (c + e < width) v[e] = to_f32(p[c + e]);
+    return v;
+}
+
+// CT: 16 columns each; PIECES: 16-byte pieces of a tile of x a lane brings (32 rows of at most 2 PIECES pieces)
+// KEEP: also writes the 8-bit form of x; GATE: 0 none, 1 values, 2 codes
+template <class T, u32 CT, u32 PIECES, bool KEEP, u32 GATE>
+__global__ __launch_bounds__(256) void narrow_rows_kernel(const RowsArgs r)
+{
+    extern __shared__ __align__(16) float narrow_lds[];
+    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
+    if (!run.found) return;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), j = lane & 15, q = lane >> 4;
+    const u32 row0 = run.begin + run.local * r.per;
+    const u32 height = run.end - row0 < r.per ? run.end - row0 : r.per;
+    const bool inside = run.block != ~0u;
+    const u32 steps = (r.sums + 3) / 4, pitch = pitch_of(r.sums), quads = pitch / 4;
+    float *lw = narrow_lds, *lb = lw + steps * CT * kWave, *lx = lb + CT * 16 + wave * kTileRows * pitch;
+
+    // ---- the weights: step s of column tile c at (s CT + c) 64, lane (column, sum index) there
+    if (inside) {
+        const T *w = static_cast<const T *>(r.w) + (u64)run.block * r.w_block;
+        if (r.across) {
+            for (u32 i = threadIdx.x; i < steps * 4 * CT * 4; i += 256) {
+                const u32 s = i / (CT * 4), c = i % (CT * 4);
+                const f32x4 v = s < r.sums ? load4_of(w + (u64)s * r.ldw, 4 * c, r.cols) : f32x4{};
+                *reinterpret_cast<f32x4 *>(lw + (s / 4 * CT + c / 4) * kWave + s % 4 * 16 + c % 4 * 4) = v;
+            }
+        } else {
+            for (u32 i = threadIdx.x; i < steps * CT * 16; i += 256) {
+                const u32 c = i / steps, s = i % steps;
+                const f32x4 v = c < r.cols ? load4_of(w + (u64)c * r.ldw, 4 * s, r.sums) : f32x4{};
+#pragma unroll
+                for (u32 e = 0; e < 4; ++e) lw[(s * CT + c / 16) * kWave + e * 16 + c % 16] = v[e];
+            }
+        }
+        for (u32 i = threadIdx.x; i < CT * 16; i += 256) lb[i] = r.bias && i < r.cols ? r.bias[(u64)run.block * r.cols + i] : 0.0f;
+    }
+    __syncthreads();
+
+    const u32 tiles = (height + kTileRows - 1) / kTileRows;
+    const T *x = static_cast<const T *>(r.a) + (u64)row0 * r.lda;
+    f32x4 next[PIECES];
+    auto request = [&](u32 tile) {
+#pragma unroll
+        for (u32 i = 0; i < PIECES; ++i) {
+            const u32 piece = lane + i * kWave, m = piece / quads, c = piece - m * quads;
+            const u32 row = tile * kTileRows + m;
+            next[i] = f32x4{};
+            if (inside && tile < tiles && m < kTileRows && row < height) next[i] = load4_of(x + (u64)row * r.lda, 4 * c, r.sums);
+        }
+    };
+    request(wave);
+    for (u32 tile = wave; tile < tiles; tile += 4) {
+        const u32 base = tile * kTileRows;
+#pragma unroll
+        for (u32 i = 0; i < PIECES; ++i) {
+            const u32 piece = lane + i * kWave, m = piece / quads, c = piece - m * quads;
+            if (m < kTileRows) *reinterpret_cast<f32x4 *>(lx + m * pitch + 4 * c) = next[i];
+        }
+        wave_meets();
+        request(tile + 4);
+        f32x4 acc[2][CT];
+#pragma unroll
+        for (u32 c = 0; c < CT; ++c) acc[0][c] = acc[1][c] = inside ? *reinterpret_cast<const f32x4 *>(lb + 16 * c + 4 * q) : f32x4{};
+        if (inside) {
+#pragma unroll 2
+            for (u32 s = 0; s < steps; ++s) {
+                const float x0 = lx[j * pitch + 4 * s + q], x1 = lx[(16 + j) * pitch + 4 * s + q];
+#pragma unroll
+                for (u32 c = 0; c < CT; ++c) {
+                    const float w = lw[(s * CT + c) * kWave + lane];
+                    acc[0][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, x0, acc[0][c], 0, 0, 0);
+                    acc[1][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, x1, acc[1][c], 0, 0, 0);
+                }
+            }
+        }
+        if constexpr (KEEP) {
+            // 32 values of a row a lane; zeros for rows of no block are what request() left
+            const u32 groups = (r.sums + 31) / 32;
+            for (u32 i = lane; i < kTileRows * groups; i += kWave) {
+                const u32 m = i / groups, g = i - m * groups;
+                if (base + m >= height) continue;
+                f32x4 v[8];
+                u32 top = 0;
+#pragma unroll
+                for (u32 e = 0; e < 8; ++e) {
+                    v[e] = f32x4{};
+                    if (32 * g + 4 * e < pitch) v[e] = *reinterpret_cast<const f32x4 *>(lx + m * pitch + 32 * g + 4 * e);
+#pragma unroll
+                    for (u32 h = 0; h < 4; ++h) {
+                        const u32 b = __float_as_uint(v[e][h]) & 0x7fffffffu;
+                        top = top > b ? top : b;
+                    }
+                }
+                const u32 scale = scale_of_max(top);
+                const float inv = inverse_step(scale);
+                const u64 at = (u64)(row0 + base) * groups + i;
+                u32 *codes = r.keep_codes + at * 8;
+#pragma unroll
+                for (u32 e = 0; e < 8; e += 4) {
+                    typedef __attribute__((ext_vector_type(4))) u32 u32x4;
+                    u32x4 o;
+#pragma unroll
+                    for (u32 h = 0; h < 4; ++h)
+                        o[h] = pack_codes(code_of(v[e + h][0], inv), code_of(v[e + h][1], inv), code_of(v[e + h][2], inv), code_of(v[e + h][3], inv));
+                    *reinterpret_cast<u32x4 *>(codes + e) = o;
+                }
+                r.keep_scale[at] = (uint8_t)scale;
+            }
+        }
+#pragma unroll
+        for (u32 m = 0; m < 2; ++m) {
+            const u32 row = base + 16 * m + j;
+            if (row >= height) continue;
+            T *out = static_cast<T *>(r.out) + (u64)(row0 + row) * r.ldo;
+#pragma unroll
+            for (u32 c = 0; c < CT; ++c) {
+                const u32 col = 16 * c + 4 * q;
+                f32x4 y = acc[m][c];
+                if (r.relu) {
+#pragma unroll
+                    for (u32 v = 0; v < 4; ++v) y[v] = y[v] < 0.0f ? 0.0f : y[v];          // NaN stays
+                }
+                if (GATE != 0 && inside && col < r.cols) {
+                    const u64 at = (u64)(row0 + row) * r.ldgate + col;
+                    if (GATE == 1) {
+                        const f32x4 g = load4_of(static_cast<const T *>(r.gate) + (u64)(row0 + row) * r.ldgate, col, r.cols);
+#pragma unroll
+                        for (u32 v = 0; v < 4; ++v) y[v] = g[v] <= 0.0f ? 0.0f : y[v];
+                    } else {
+                        const u32 g = *reinterpret_cast<const u32 *>(static_cast<const char *>(r.gate) + at);
+                        if (r.gate_scale[at / 32] != 255) {
+#pragma unroll
+                            for (u32 v = 0; v < 4; ++v) y[v] = (int)(signed char)(g >> (8 * v)) > 0 ? y[v] : 0.0f;
+                        }
+                    }
+                }
+                if (col + 4 <= r.cols) {
+                    store4(out + col, y);
+                } else {
+#pragma unroll
+                    for (u32 v = 0; v < 4; ++v)
+                        if (col + v < r.cols) out[col + v] = (T)y[v];
+                }
+            }
+        }
+        wave_meets();                   // the tile's reads are done before the next one takes its place
+    }
+}
+
+template <class T, u32 CT, u32 PIECES>
+hipError_t narrow_go(RowsArgs r, hipStream_t stream)
+{
+    const u32 lds = (((r.sums + 3) / 4) * CT * kWave + CT * 16 + 4 * kTileRows * pitch_of(r.sums)) * 4;
+    const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
+    auto kernel = r.keep_codes ? narrow_rows_kernel<T, CT, PIECES, true, 0> : gate == 0 ? narrow_rows_kernel<T, CT, PIECES, false, 0>
+                  : gate == 1 ? narrow_rows_kernel<T, CT, PIECES, false, 1> : narrow_rows_kernel<T, CT, PIECES, false, 2>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((u32)max_runs(r.rows, r.blocks, r.per, true)), dim3(256), lds, stream, r);
+    return hipGetLastError();
+}
+template <class T, u32 CT>
+hipError_t narrow_sums(const RowsArgs &r, hipStream_t stream)
+{
+    // 32 rows of pitch / 4 pieces over 64 lanes
+    if (pitch_of(r.sums) <= 36) return narrow_go<T, CT, 5>(r, stream);
+    if (pitch_of(r.sums) <= 68) return narrow_go<T, CT, 9>(r, stream);
+    return narrow_go<T, CT, 17>(r, stream);
+}
+template <class T>
+hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)
+{
+    switch ((r.cols + 15) / 16) {
+    case 1: return narrow_sums<T, 1>(r, stream);
+    case 2: return narrow_sums<T, 2>(r, stream);
+    case 3: return narrow_sums<T, 3>(r, stream);
+    case 4: return narrow_sums<T, 4>(r, stream);
+    case 5: return narrow_sums<T, 5>(r, stream);
+    case 6: return narrow_sums<T, 6>(r, stream);
+    case 7: return narrow_sums<T, 7>(r, stream);
+    default: return narrow_sums<T, 8>(r, stream);
+    }
+}
+
+}  // namespace
+
+bool narrow_rows_fit(const RowsArgs &r) { return r.cols <= 128 && r.sums <= 128; }
+
+hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream)
+{
+    r.across = across;
+    // about four workgroups a compute unit, whole tiles for each of their wavefronts
+    r.per = (u32)(((u64)r.rows / 1024 + 127) / 128 * 128);
+    if (r.per < 128) r.per = 128;
+    return dtype == LMK_GS_F32 ? narrow_as<float>(r, stream) : narrow_as<__bf16>(r, stream);
+}
+
+}  // namespace lmk

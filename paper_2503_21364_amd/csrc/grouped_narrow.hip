@@ -1,6 +1,6 @@
 // Grouped layers whose weights are small (the decoder's: 35 x 96, 32 x 70): memory is all of it, so a row is read once and its
 // results leave once.  A workgroup keeps its block's whole matrix in LDS, in the order the matrix instructions take it, and
-// its four wavefronts walk through a run of the block's rows in tiles of 32, each by itself: the next tile's rows are
+// its four wavefronts walk through a run of the block's rows in tiles of 16, each by itself: the next tile's rows are
 // on their way to registers while a tile is multiplied, and nothing is waited for in common.
 //
 // v_mfma_f32_16x16x4_f32 with the weights on its rows and the layer's rows on its columns: a lane has four
@@ -12,7 +12,7 @@ namespace lmk {
 
 namespace {
 
-constexpr u32 kTileRows = 32;
+constexpr u32 kTileRows = 16;
 
 __device__ __forceinline__ void wave_meets()          // LDS written by other lanes of this wavefront
 {
@@ -34,7 +34,7 @@ template <class T> __device__ __forceinline__ f32x4 load4_of(const T *p, u32 c, 
     return v;
 }
 
-// CT: 16 columns each; PIECES: 16-byte pieces of a tile of x a lane brings (32 rows of at most 2 PIECES pieces)
+// CT: 16 columns each; PIECES: 16-byte pieces of a tile of x a lane brings (16 rows of at most 4 PIECES pieces)
 // KEEP: also writes the 8-bit form of x; GATE: 0 none, 1 values, 2 codes
 template <class T, u32 CT, u32 PIECES, bool KEEP, u32 GATE>
 __global__ __launch_bounds__(256) void narrow_rows_kernel(const RowsArgs r)
@@ -71,109 +71,116 @@ __global__ __launch_bounds__(256) void narrow_rows_kernel(const RowsArgs r)
     __syncthreads();
 
     const u32 tiles = (height + kTileRows - 1) / kTileRows;
-    const T *x = static_cast<const T *>(r.a) + (u64)row0 * r.lda;
+    const char *x = reinterpret_cast<const char *>(static_cast<const T *>(r.a) + (u64)row0 * r.lda);
+    // this lane's pieces of a tile.  Where rows end inside a piece, the row's last four values are read and moved into place.
+    const u32 rest = r.sums % 4;
     f32x4 next[PIECES];
+    u32 from[PIECES], of_row[PIECES];
+    bool last[PIECES];
+#pragma unroll
+    for (u32 i = 0; i < PIECES; ++i) {
+        const u32 piece = lane + i * kWave, m = piece / quads, c = (piece - m * quads) * 4;
+        last[i] = c + 4 > r.sums;
+        of_row[i] = m < kTileRows && c < r.sums ? m : ~0u;
+        from[i] = (m * (u32)r.lda + (last[i] ? r.sums - 4 : c)) * (u32)sizeof(T);
+    }
     auto request = [&](u32 tile) {
+        const char *p = x + (u64)tile * kTileRows * r.lda * sizeof(T);
+        const u32 rows = inside && tile < tiles ? height - tile * kTileRows : 0u;
 #pragma unroll
         for (u32 i = 0; i < PIECES; ++i) {
-            const u32 piece = lane + i * kWave, m = piece / quads, c = piece - m * quads;
-            const u32 row = tile * kTileRows + m;
             next[i] = f32x4{};
-            if (inside && tile < tiles && m < kTileRows && row < height) next[i] = load4_of(x + (u64)row * r.lda, 4 * c, r.sums);
+            if (of_row[i] < rows) next[i] = load4(reinterpret_cast<const T *>(p + from[i]));
         }
+    };
+    auto settle = [&](u32 i) {
+        const f32x4 v = next[i];
+        if (rest == 0 || !last[i]) return v;
+        return rest == 1 ? f32x4{v[3], 0.f, 0.f, 0.f} : rest == 2 ? f32x4{v[2], v[3], 0.f, 0.f} : f32x4{v[1], v[2], v[3], 0.f};
     };
     request(wave);
     for (u32 tile = wave; tile < tiles; tile += 4) {
-        const u32 base = tile * kTileRows;
+        const u32 base = tile * kTileRows, left = height - base;
 #pragma unroll
         for (u32 i = 0; i < PIECES; ++i) {
-            const u32 piece = lane + i * kWave, m = piece / quads, c = piece - m * quads;
-            if (m < kTileRows) *reinterpret_cast<f32x4 *>(lx + m * pitch + 4 * c) = next[i];
+            const u32 piece = lane + i * kWave;
+            if (piece < kTileRows * quads) *reinterpret_cast<f32x4 *>(lx + 4 * piece) = settle(i);
         }
         wave_meets();
         request(tile + 4);
-        f32x4 acc[2][CT];
+        f32x4 acc[CT];
 #pragma unroll
-        for (u32 c = 0; c < CT; ++c) acc[0][c] = acc[1][c] = inside ? *reinterpret_cast<const f32x4 *>(lb + 16 * c + 4 * q) : f32x4{};
+        for (u32 c = 0; c < CT; ++c) acc[c] = inside ? *reinterpret_cast<const f32x4 *>(lb + 16 * c + 4 * q) : f32x4{};
         if (inside) {
-#pragma unroll 2
             for (u32 s = 0; s < steps; ++s) {
-                const float x0 = lx[j * pitch + 4 * s + q], x1 = lx[(16 + j) * pitch + 4 * s + q];
+                const float v = lx[j * pitch + 4 * s + q];
 #pragma unroll
-                for (u32 c = 0; c < CT; ++c) {
-                    const float w = lw[(s * CT + c) * kWave + lane];
-                    acc[0][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, x0, acc[0][c], 0, 0, 0);
-                    acc[1][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, x1, acc[1][c], 0, 0, 0);
-                }
+                for (u32 c = 0; c < CT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(lw[(s * CT + c) * kWave + lane], v, acc[c], 0, 0, 0);
             }
         }
         if constexpr (KEEP) {
-            // 32 values of a row a lane; zeros for rows of no block are what request() left
-            const u32 groups = (r.sums + 31) / 32;
-            for (u32 i = lane; i < kTileRows * groups; i += kWave) {
-                const u32 m = i / groups, g = i - m * groups;
-                if (base + m >= height) continue;
-                f32x4 v[8];
+            // eight values a lane, four lanes for those that share a step; rows of no block are the zeros that request() left
+            const u32 eights = (r.sums + 31) / 32 * 4;
+            for (u32 i = lane; i < kTileRows * eights; i += kWave) {
+                const u32 m = i / eights, c = (i - m * eights) * 8;
+                f32x4 v[2] = {};
                 u32 top = 0;
 #pragma unroll
-                for (u32 e = 0; e < 8; ++e) {
-                    v[e] = f32x4{};
-                    if (32 * g + 4 * e < pitch) v[e] = *reinterpret_cast<const f32x4 *>(lx + m * pitch + 32 * g + 4 * e);
+                for (u32 e = 0; e < 2; ++e) {
+                    if (c + 4 * e < pitch) v[e] = *reinterpret_cast<const f32x4 *>(lx + m * pitch + c + 4 * e);
 #pragma unroll
                     for (u32 h = 0; h < 4; ++h) {
                         const u32 b = __float_as_uint(v[e][h]) & 0x7fffffffu;
                         top = top > b ? top : b;
                     }
                 }
+                u32 other = wave_dpp<0xB1, 0xf>(0u, top);           // lanes 1 0 3 2
+                top = top > other ? top : other;
+                other = wave_dpp<0x4E, 0xf>(0u, top);               // lanes 2 3 0 1
+                top = top > other ? top : other;
                 const u32 scale = scale_of_max(top);
                 const float inv = inverse_step(scale);
-                const u64 at = (u64)(row0 + base) * groups + i;
-                u32 *codes = r.keep_codes + at * 8;
-#pragma unroll
-                for (u32 e = 0; e < 8; e += 4) {
-                    typedef __attribute__((ext_vector_type(4))) u32 u32x4;
-                    u32x4 o;
-#pragma unroll
-                    for (u32 h = 0; h < 4; ++h)
-                        o[h] = pack_codes(code_of(v[e + h][0], inv), code_of(v[e + h][1], inv), code_of(v[e + h][2], inv), code_of(v[e + h][3], inv));
-                    *reinterpret_cast<u32x4 *>(codes + e) = o;
-                }
-                r.keep_scale[at] = (uint8_t)scale;
+                if (m >= left) continue;
+                const u64 at = (u64)(row0 + base) * eights + i;
+                typedef __attribute__((ext_vector_type(2))) u32 u32x2;
+                *reinterpret_cast<u32x2 *>(r.keep_codes + at * 2) =
+                    u32x2{pack_codes(code_of(v[0][0], inv), code_of(v[0][1], inv), code_of(v[0][2], inv), code_of(v[0][3], inv)),
+                          pack_codes(code_of(v[1][0], inv), code_of(v[1][1], inv), code_of(v[1][2], inv), code_of(v[1][3], inv))};
+                if ((i & 3) == 0) r.keep_scale[at / 4] = (uint8_t)scale;
             }
         }
-#pragma unroll
-        for (u32 m = 0; m < 2; ++m) {
-            const u32 row = base + 16 * m + j;
-            if (row >= height) continue;
-            T *out = static_cast<T *>(r.out) + (u64)(row0 + row) * r.ldo;
+        char *out = reinterpret_cast<char *>(static_cast<T *>(r.out) + (u64)(row0 + base) * r.ldo);
+        const char *gate = static_cast<const char *>(r.gate) + (u64)(row0 + base) * r.ldgate * (GATE == 1 ? sizeof(T) : 1);
+        const uint8_t *gate_scale = r.gate_scale + (GATE == 2 ? (u64)(row0 + base) * (r.ldgate / 32) : 0);
+        if (j < left) {
+            const u32 row = j, to = row * (u32)r.ldo;
 #pragma unroll
             for (u32 c = 0; c < CT; ++c) {
                 const u32 col = 16 * c + 4 * q;
-                f32x4 y = acc[m][c];
+                if (col >= r.cols) continue;
+                f32x4 y = acc[c];
                 if (r.relu) {
 #pragma unroll
                     for (u32 v = 0; v < 4; ++v) y[v] = y[v] < 0.0f ? 0.0f : y[v];          // NaN stays
                 }
-                if (GATE != 0 && inside && col < r.cols) {
-                    const u64 at = (u64)(row0 + row) * r.ldgate + col;
-                    if (GATE == 1) {
-                        const f32x4 g = load4_of(static_cast<const T *>(r.gate) + (u64)(row0 + row) * r.ldgate, col, r.cols);
+                if (GATE == 1 && inside) {
+                    const f32x4 g = load4_of(reinterpret_cast<const T *>(gate) + row * (u32)r.ldgate, col, r.cols);
 #pragma unroll
-                        for (u32 v = 0; v < 4; ++v) y[v] = g[v] <= 0.0f ? 0.0f : y[v];
-                    } else {
-                        const u32 g = *reinterpret_cast<const u32 *>(static_cast<const char *>(r.gate) + at);
-                        if (r.gate_scale[at / 32] != 255) {
-#pragma unroll
-                            for (u32 v = 0; v < 4; ++v) y[v] = (int)(signed char)(g >> (8 * v)) > 0 ? y[v] : 0.0f;
-                        }
-                    }
+                    for (u32 v = 0; v < 4; ++v) y[v] = g[v] <= 0.0f ? 0.0f : y[v];
                 }
+                if (GATE == 2 && inside) {
+                    const u32 at = row * (u32)r.ldgate + col, g = *reinterpret_cast<const u32 *>(gate + at);
+                    const bool open = gate_scale[at / 32] == 255;
+#pragma unroll
+                    for (u32 v = 0; v < 4; ++v) y[v] = open || (int)(signed char)(g >> (8 * v)) > 0 ? y[v] : 0.0f;
+                }
+                T *p = reinterpret_cast<T *>(out + (to + col) * (u32)sizeof(T));
                 if (col + 4 <= r.cols) {
-                    store4(out + col, y);
+                    store4(p, y);
                 } else {
 #pragma unroll
-                    for (u32 v = 0; v < 4; ++v)
-                        if (col + v < r.cols) out[col + v] = (T)y[v];
+                    for (u32 v = 0; v < 3; ++v)
+                        if (col + v < r.cols) p[v] = (T)y[v];
                 }
             }
         }
@@ -196,10 +203,10 @@ hipError_t narrow_go(RowsArgs r, hipStream_t stream)
 template <class T, u32 CT>
 hipError_t narrow_sums(const RowsArgs &r, hipStream_t stream)
 {
-    // 32 rows of pitch / 4 pieces over 64 lanes
-    if (pitch_of(r.sums) <= 36) return narrow_go<T, CT, 5>(r, stream);
-    if (pitch_of(r.sums) <= 68) return narrow_go<T, CT, 9>(r, stream);
-    return narrow_go<T, CT, 17>(r, stream);
+    // 16 rows of pitch / 4 pieces over 64 lanes
+    if (pitch_of(r.sums) <= 36) return narrow_go<T, CT, 3>(r, stream);
+    if (pitch_of(r.sums) <= 68) return narrow_go<T, CT, 5>(r, stream);
+    return narrow_go<T, CT, 9>(r, stream);
 }
 template <class T>
 hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)
@@ -211,14 +218,18 @@ hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)
     case 4: return narrow_sums<T, 4>(r, stream);
     case 5: return narrow_sums<T, 5>(r, stream);
     case 6: return narrow_sums<T, 6>(r, stream);
-    case 7: return narrow_sums<T, 7>(r, stream);
     default: return narrow_sums<T, 8>(r, stream);
     }
 }
 
 }  // namespace
 
-bool narrow_rows_fit(const RowsArgs &r) { return r.cols <= 128 && r.sums <= 128; }
+bool narrow_rows_fit(const RowsArgs &r)
+{
+    // byte offsets inside a tile of 16 rows are 32 bits wide
+    constexpr u64 most = 1u << 23;
+    return r.cols <= 128 && r.sums >= 4 && r.sums <= 128 && r.lda <= most && r.ldo <= most && (!r.gate || r.ldgate <= most);
+}
 
 hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream)
 {

@@ -37,7 +37,7 @@ template <class T> __device__ __forceinline__ f32x4 load4_of(const T *p, u32 c, 
 // CT: 16 columns each; PIECES: 16-byte pieces of a tile of x a lane brings (16 rows of at most 4 PIECES pieces)
 // KEEP: also writes the 8-bit form of x; GATE: 0 none, 1 values, 2 codes
 template <class T, u32 CT, u32 PIECES, bool KEEP, u32 GATE>
-__global__ __launch_bounds__(256) void narrow_rows_kernel(const RowsArgs r)
+__global__ __launch_bounds__(256, PIECES == 3 ? 4 : PIECES == 5 ? 3 : 2) void narrow_rows_kernel(const RowsArgs r)
 {
     extern __shared__ __align__(16) float narrow_lds[];
     const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
@@ -120,14 +120,16 @@ __global__ __launch_bounds__(256) void narrow_rows_kernel(const RowsArgs r)
         }
         if constexpr (KEEP) {
             // eight values a lane, four lanes for those that share a step; rows of no block are the zeros that request() left
-            const u32 eights = (r.sums + 31) / 32 * 4;
-            for (u32 i = lane; i < kTileRows * eights; i += kWave) {
-                const u32 m = i / eights, c = (i - m * eights) * 8;
+            const u32 m = lane / 4, eight = lane % 4, kp = (r.sums + 31) / 32 * 32;
+            char *codes = reinterpret_cast<char *>(r.keep_codes) + (u64)(row0 + base) * kp + m * kp + 8 * eight;
+            uint8_t *scales = r.keep_scale + (u64)(row0 + base) * (kp / 32) + m * (kp / 32);
+            const float *row = lx + m * pitch + 8 * eight;
+            for (u32 g = 0; g < kp / 32; ++g) {
                 f32x4 v[2] = {};
                 u32 top = 0;
 #pragma unroll
                 for (u32 e = 0; e < 2; ++e) {
-                    if (c + 4 * e < pitch) v[e] = *reinterpret_cast<const f32x4 *>(lx + m * pitch + c + 4 * e);
+                    if (32 * g + 8 * eight + 4 * e < pitch) v[e] = *reinterpret_cast<const f32x4 *>(row + 32 * g + 4 * e);
 #pragma unroll
                     for (u32 h = 0; h < 4; ++h) {
                         const u32 b = __float_as_uint(v[e][h]) & 0x7fffffffu;
@@ -141,12 +143,11 @@ __global__ __launch_bounds__(256) void narrow_rows_kernel(const RowsArgs r)
                 const u32 scale = scale_of_max(top);
                 const float inv = inverse_step(scale);
                 if (m >= left) continue;
-                const u64 at = (u64)(row0 + base) * eights + i;
                 typedef __attribute__((ext_vector_type(2))) u32 u32x2;
-                *reinterpret_cast<u32x2 *>(r.keep_codes + at * 2) =
+                *reinterpret_cast<u32x2 *>(codes + 32 * g) =
                     u32x2{pack_codes(code_of(v[0][0], inv), code_of(v[0][1], inv), code_of(v[0][2], inv), code_of(v[0][3], inv)),
                           pack_codes(code_of(v[1][0], inv), code_of(v[1][1], inv), code_of(v[1][2], inv), code_of(v[1][3], inv))};
-                if ((i & 3) == 0) r.keep_scale[at / 4] = (uint8_t)scale;
+                if (eight == 0) scales[g] = (uint8_t)scale;
             }
         }
         char *out = reinterpret_cast<char *>(static_cast<T *>(r.out) + (u64)(row0 + base) * r.ldo);
@@ -234,9 +235,9 @@ bool narrow_rows_fit(const RowsArgs &r)
 hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream)
 {
     r.across = across;
-    // about four workgroups a compute unit, whole tiles for each of their wavefronts
-    r.per = (u32)(((u64)r.rows / 1024 + 127) / 128 * 128);
-    if (r.per < 128) r.per = 128;
+    // four workgroups a compute unit at most, all of them at once, whole tiles for each of their wavefronts
+    const u32 slots = 1024 - (r.blocks < 512 ? r.blocks : 512);
+    r.per = (u32)(((u64)r.rows + slots * 64 - 1) / (slots * 64)) * 64;
     return dtype == LMK_GS_F32 ? narrow_as<float>(r, stream) : narrow_as<__bf16>(r, stream);
 }
 

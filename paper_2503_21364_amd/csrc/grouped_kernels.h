@@ -3,6 +3,8 @@
 #define LMK_GS_GROUPED_KERNELS_H
 #include "grouped.h"
 
+#include <type_traits>
+
 namespace lmk {
 
 // rows of a block against its weights
@@ -43,6 +45,26 @@ struct SumsArgs {
     u32 tiles, n_tiles, k_tiles;
 };
 
+// all gradients of a layer of small matrices, float32
+struct BackwardArgs {
+    const float *dy;            // [rows][n]
+    u64 lddy;
+    const void *x;              // [rows][k] values, or codes [rows][kp]; NULL if neither dw nor the gate needs it
+    u64 ldx;
+    const uint8_t *scale;       // of codes
+    const float *w;
+    u64 ldw, w_block;
+    const u32 *offsets;
+    u32 blocks, rows, n, k;
+    u32 in_major, gate;
+    float *dx;                  // any of the three may be NULL
+    u64 lddx;
+    float *dw, *db;
+    float *part;                // as SumsArgs
+    u32 per, runs;              // rows of a run, upper bound of the runs' number
+    u32 shared;                 // floats of LDS of the weights
+};
+
 // Workgroups go to the eight dies in turn; this gives each die a run of consecutive tiles, which share operands.
 __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
 {
@@ -58,6 +80,10 @@ hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_
 // small matrices, any type and alignment; the only rows kernel that writes the 8-bit form of its input
 bool narrow_rows_fit(const RowsArgs &r);
 hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream);
+
+bool narrow_backward_fits(const BackwardArgs &r, bool codes);
+u32 narrow_backward_rows(u32 rows, u32 blocks);
+hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream);
 
 // bfloat16 whose rows start at 16-byte boundaries
 bool wide_rows_fit(const RowsArgs &r, bool across);

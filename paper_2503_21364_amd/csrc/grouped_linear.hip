@@ -12,8 +12,6 @@
 // sum index is contiguous in memory (lanes along it, 2 banks apart).
 #include "grouped_kernels.h"
 
-#include <type_traits>
-
 namespace lmk {
 
 namespace {
@@ -339,7 +337,15 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
     if (!dst) return;
     const float *p = part + (u64)before * stride + i;
     float sum = 0.0f;
-    for (u32 q = 0; q < mine; ++q) sum += p[(u64)q * stride];
+    u32 q = 0;
+    for (; q + 8 <= mine; q += 8) {             // eight loads on their way, added in order
+        float v[8];
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) v[i] = p[(u64)(q + i) * stride];
+#pragma unroll
+        for (u32 i = 0; i < 8; ++i) sum += v[i];
+    }
+    for (; q < mine; ++q) sum += p[(u64)q * stride];
     dst[i < size ? (u64)block * size + i : (u64)block * n + (i - size)] = sum;
 }
 
@@ -423,14 +429,19 @@ bool grouped_linear_fits(const lmk_gs_linear &l)
     const u64 runs = max_runs(l.rows, l.blocks, 128, true);
     const u64 pairs = (u64)((l.n + 127) / 128) * ((l.k + 31) / 32);
     const u64 widest = l.n > l.k ? l.n : l.k;
-    return runs * ((widest + 31) / 32) < 1ull << 31 && max_runs(l.rows, l.blocks, rows_of_run(l), false) * pairs < 1ull << 31 &&
+    return runs * ((widest + 31) / 32) < 1ull << 31 && max_runs(l.rows, l.blocks, rows_of_run(l), false) * pairs < 1ull << 31 && max_runs(l.rows, l.blocks, 64, false) < 1ull << 30 &&
            (((u64)l.n * l.k + l.n + 255) / 256) * l.blocks < 1ull << 31;
 }
 
+// Small matrices in float32 take one pass over the rows for all three gradients; the rest of the rule (strides) is the
+// arrays', and what does not fit takes the other kernels with the same runs.
+static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l.n <= 128 && l.k <= 64; }
+static u32 rows_of_partial(const lmk_gs_linear &l) { return one_pass(l) ? narrow_backward_rows(l.rows, l.blocks) : rows_of_run(l); }
+
 size_t grouped_backward_bytes(const lmk_gs_linear &l)
 {
-    // the partial sums of every run but those of blocks that have only one; at least one
-    return (size_t)(max_runs(l.rows, l.blocks, rows_of_run(l), false) * ((u64)l.n * l.k + l.n) * 4);
+    // the partial sums of every run
+    return (size_t)(max_runs(l.rows, l.blocks, rows_of_partial(l), false) * ((u64)l.n * l.k + l.n) * 4);
 }
 
 hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
@@ -452,7 +463,33 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
                                    const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
                                    char *workspace, hipStream_t stream)
 {
-    const u32 kp = (l.k + 31) / 32 * 32;
+    const u32 kp = (l.k + 31) / 32 * 32, per = rows_of_partial(l);
+    const u64 runs = max_runs(l.rows, l.blocks, per, false);
+    const u32 pieces = (u32)(((u64)l.n * l.k + l.n + 255) / 256);
+    float *part = reinterpret_cast<float *>(workspace);
+    const auto join = [&]() {
+        hipLaunchKernelGGL(join_kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, per, part, l.n, l.k,
+                           out.dw, out.db, pieces, (u32)runs);
+        return hipGetLastError();
+    };
+    if (one_pass(l) && (out.dw || out.db)) {
+        BackwardArgs r = {};
+        r.dy = static_cast<const float *>(dy); r.lddy = lddy;
+        if (out.dw || (out.dx && gate)) {
+            r.x = kept ? (const void *)kept->codes : x;
+            r.ldx = ldx;
+            r.scale = kept ? kept->scale : nullptr;
+        }
+        r.w = static_cast<const float *>(l.w); r.ldw = l.ldw; r.w_block = l.w_block;
+        r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.n = l.n; r.k = l.k;
+        r.in_major = l.in_major; r.gate = gate;
+        r.dx = static_cast<float *>(out.dx); r.lddx = out.lddx; r.dw = out.dw; r.db = out.db;
+        r.part = part; r.per = per; r.runs = (u32)runs;
+        if (narrow_backward_fits(r, kept != nullptr)) {
+            const hipError_t e = launch_narrow_backward(r, kept != nullptr, stream);
+            return e == hipSuccess ? join() : e;
+        }
+    }
     if (out.dx && l.rows > 0) {
         RowsArgs r = {};
         r.a = dy; r.lda = lddy;
@@ -475,15 +512,12 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
     r.scale = kept ? kept->scale : nullptr;
     r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.n = l.n; r.k = l.k;
     r.dw = out.dw; r.db = out.db; r.in_major = l.in_major;
-    r.part = reinterpret_cast<float *>(workspace);
-    r.per = rows_of_run(l);
+    r.part = part;
+    r.per = per;
     const u32 kind = !out.dw ? 0 : kept ? 2 : 1;
     hipError_t e = l.dtype == LMK_GS_F32 ? sums_as<float>(r, kind, stream) : sums_as<__bf16>(r, kind, stream);
     if (e != hipSuccess) return e;
-    const u32 pieces = (u32)(((u64)l.n * l.k + l.n + 255) / 256);
-    hipLaunchKernelGGL(join_kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, r.per, r.part, l.n,
-                       l.k, out.dw, out.db, pieces, (u32)max_runs(l.rows, l.blocks, r.per, false));
-    return hipGetLastError();
+    return join();
 }
 
 }  // namespace lmk

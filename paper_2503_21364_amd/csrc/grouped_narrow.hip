@@ -6,33 +6,11 @@
 // v_mfma_f32_16x16x4_f32 with the weights on its rows and the layer's rows on its columns: a lane has four
 // consecutive outputs of a row, one 16-byte store.  In LDS a row of x takes a pitch of 4 (odd) floats: the 16 rows and
 // four sum indices that an instruction reads are on 64 different banks.
-#include "grouped_kernels.h"
+#include "grouped_narrow.h"
 
 namespace lmk {
 
 namespace {
-
-constexpr u32 kTileRows = 16;
-
-__device__ __forceinline__ void wave_meets()          // LDS written by other lanes of this wavefront
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
-__host__ __device__ constexpr u32 pitch_of(u32 sums) { return ((sums + 3) / 4 | 1) * 4; }
-
-// four values of a row of `width`, from c on; what is beyond it: zeros
-template <class T> __device__ __forceinline__ f32x4 load4_of(const T *p, u32 c, u32 width)
-{
-    if (c + 4 <= width) return load4(p + c);
-    f32x4 v = {};
-#pragma unroll
-    for (u32 e = 0; e < 4; ++e)
-        if (c + e < width) v[e] = to_f32(p[c + e]);
-    return v;
-}
 
 // CT: 16 columns each; PIECES: 16-byte pieces of a tile of x a lane brings (16 rows of at most 4 PIECES pieces)
 // KEEP: also writes the 8-bit form of x; GATE: 0 none, 1 values, 2 codes
@@ -46,66 +24,26 @@ __global__ __launch_bounds__(256, PIECES == 3 ? 4 : PIECES == 5 ? 3 : 2) void na
     const u32 row0 = run.begin + run.local * r.per;
     const u32 height = run.end - row0 < r.per ? run.end - row0 : r.per;
     const bool inside = run.block != ~0u;
-    const u32 steps = (r.sums + 3) / 4, pitch = pitch_of(r.sums), quads = pitch / 4;
+    const u32 steps = (r.sums + 3) / 4, pitch = pitch_of(r.sums);
     float *lw = narrow_lds, *lb = lw + steps * CT * kWave, *lx = lb + CT * 16 + wave * kTileRows * pitch;
 
-    // ---- the weights: step s of column tile c at (s CT + c) 64, lane (column, sum index) there
     if (inside) {
-        const T *w = static_cast<const T *>(r.w) + (u64)run.block * r.w_block;
-        if (r.across) {
-            for (u32 i = threadIdx.x; i < steps * 4 * CT * 4; i += 256) {
-                const u32 s = i / (CT * 4), c = i % (CT * 4);
-                const f32x4 v = s < r.sums ? load4_of(w + (u64)s * r.ldw, 4 * c, r.cols) : f32x4{};
-                *reinterpret_cast<f32x4 *>(lw + (s / 4 * CT + c / 4) * kWave + s % 4 * 16 + c % 4 * 4) = v;
-            }
-        } else {
-            for (u32 i = threadIdx.x; i < steps * CT * 16; i += 256) {
-                const u32 c = i / steps, s = i % steps;
-                const f32x4 v = c < r.cols ? load4_of(w + (u64)c * r.ldw, 4 * s, r.sums) : f32x4{};
-#pragma unroll
-                for (u32 e = 0; e < 4; ++e) lw[(s * CT + c / 16) * kWave + e * 16 + c % 16] = v[e];
-            }
-        }
+        stage_weights<T, CT>(lw, static_cast<const T *>(r.w) + (u64)run.block * r.w_block, r.ldw, r.across, r.sums, r.cols);
         for (u32 i = threadIdx.x; i < CT * 16; i += 256) lb[i] = r.bias && i < r.cols ? r.bias[(u64)run.block * r.cols + i] : 0.0f;
     }
     __syncthreads();
 
     const u32 tiles = (height + kTileRows - 1) / kTileRows;
     const char *x = reinterpret_cast<const char *>(static_cast<const T *>(r.a) + (u64)row0 * r.lda);
-    // this lane's pieces of a tile.  Where rows end inside a piece, the row's last four values are read and moved into place.
-    const u32 rest = r.sums % 4;
-    f32x4 next[PIECES];
-    u32 from[PIECES], of_row[PIECES];
-    bool last[PIECES];
-#pragma unroll
-    for (u32 i = 0; i < PIECES; ++i) {
-        const u32 piece = lane + i * kWave, m = piece / quads, c = (piece - m * quads) * 4;
-        last[i] = c + 4 > r.sums;
-        of_row[i] = m < kTileRows && c < r.sums ? m : ~0u;
-        from[i] = (m * (u32)r.lda + (last[i] ? r.sums - 4 : c)) * (u32)sizeof(T);
-    }
+    Pieces<T, PIECES> tile_of_x;
+    tile_of_x.init(r.lda, r.sums, lane);
     auto request = [&](u32 tile) {
-        const char *p = x + (u64)tile * kTileRows * r.lda * sizeof(T);
-        const u32 rows = inside && tile < tiles ? height - tile * kTileRows : 0u;
-#pragma unroll
-        for (u32 i = 0; i < PIECES; ++i) {
-            next[i] = f32x4{};
-            if (of_row[i] < rows) next[i] = load4(reinterpret_cast<const T *>(p + from[i]));
-        }
-    };
-    auto settle = [&](u32 i) {
-        const f32x4 v = next[i];
-        if (rest == 0 || !last[i]) return v;
-        return rest == 1 ? f32x4{v[3], 0.f, 0.f, 0.f} : rest == 2 ? f32x4{v[2], v[3], 0.f, 0.f} : f32x4{v[1], v[2], v[3], 0.f};
+        tile_of_x.request(x + (u64)tile * kTileRows * r.lda * sizeof(T), inside && tile < tiles ? height - tile * kTileRows : 0u);
     };
     request(wave);
     for (u32 tile = wave; tile < tiles; tile += 4) {
         const u32 base = tile * kTileRows, left = height - base;
-#pragma unroll
-        for (u32 i = 0; i < PIECES; ++i) {
-            const u32 piece = lane + i * kWave;
-            if (piece < kTileRows * quads) *reinterpret_cast<f32x4 *>(lx + 4 * piece) = settle(i);
-        }
+        tile_of_x.put(lx, lane);
         wave_meets();
         request(tile + 4);
         f32x4 acc[CT];
@@ -227,9 +165,7 @@ hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)
 
 bool narrow_rows_fit(const RowsArgs &r)
 {
-    // byte offsets inside a tile of 16 rows are 32 bits wide
-    constexpr u64 most = 1u << 23;
-    return r.cols <= 128 && r.sums >= 4 && r.sums <= 128 && r.lda <= most && r.ldo <= most && (!r.gate || r.ldgate <= most);
+    return r.cols <= 128 && r.sums >= 4 && r.sums <= 128 && r.lda <= kNarrowStride && r.ldo <= kNarrowStride && (!r.gate || r.ldgate <= kNarrowStride);
 }
 
 hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream)

@@ -1,0 +1,244 @@
+// All gradients of a grouped layer of small matrices (the decoder's: 35 x 96, 32 x 70) in one pass: dy and x are read once,
+// dx leaves once, and the sums over rows stay in registers.  As in the forward kernel a workgroup keeps its block's
+// matrix in LDS and its four wavefronts walk through a run of the block's rows in tiles of 16, each by itself:
+//     dx = dy w_g     weights on the matrix instruction's rows, dy's rows on its columns
+//     dw += x^T dy    inputs on its rows, outputs on its columns, summed over the tile's 16 rows
+// (v_mfma_f32_16x16x4_f32).  Of both, a tile of dy and of x (widened from its 8-bit form) is the operand, read from LDS.
+// db is added up from the values of dy on their way to the second product.  At the end the four wavefronts' sums are added in
+// LDS in their order.
+#include "grouped_narrow.h"
+
+namespace lmk {
+
+namespace {
+
+// A lane's N pieces (four codes each) of a tile of the 8-bit form
+template <u32 N> struct CodePieces {
+    u32 next[N], scale[N];
+    u32 from[N], of_row[N];
+    u32 quads;
+
+    __device__ __forceinline__ void init(u32 kp, u32 width, u32 lane)
+    {
+        quads = pitch_of(width) / 4;
+#pragma unroll
+        for (u32 i = 0; i < N; ++i) {
+            const u32 piece = lane + i * kWave, m = piece / quads, c = (piece - m * quads) * 4;
+            of_row[i] = m < kTileRows && c < kp ? m : ~0u;
+            from[i] = m * kp + c;
+        }
+    }
+    __device__ __forceinline__ void request(const char *codes, const uint8_t *scales, u32 rows)
+    {
+#pragma unroll
+        for (u32 i = 0; i < N; ++i) {
+            next[i] = scale[i] = 0;
+            if (of_row[i] >= rows) continue;
+            next[i] = *reinterpret_cast<const u32 *>(codes + from[i]);
+            scale[i] = scales[from[i] / 32];
+        }
+    }
+    __device__ __forceinline__ void put(float *lds, u32 lane) const
+    {
+#pragma unroll
+        for (u32 i = 0; i < N; ++i) {
+            const float step = step_of(scale[i]);
+            const u32 piece = lane + i * kWave;
+            if (piece < kTileRows * quads)
+                *reinterpret_cast<f32x4 *>(lds + 4 * piece) =
+                    f32x4{value_of(next[i], 0, step), value_of(next[i], 1, step), value_of(next[i], 2, step), value_of(next[i], 3, step)};
+        }
+    }
+};
+
+constexpr u32 kFillers = 64;            // workgroups for dx of rows of no block
+
+// pieces of a tile of at most 16 CT values a row
+constexpr u32 pieces_of(u32 ct) { return (kTileRows * (pitch_of(16 * ct) / 4) + kWave - 1) / kWave; }
+// floats between the outputs of the joined sums in LDS
+constexpr u32 sums_pitch(u32 ck) { return 16 * ck + 4; }
+
+// CN, CK: 16 outputs and 16 inputs each
+template <u32 CN, u32 CK, bool CODES>
+__global__ __launch_bounds__(256, CN * CK <= 8 ? 4 : CN * CK <= 18 ? 3 : 2) void narrow_backward_kernel(const BackwardArgs r)
+{
+    extern __shared__ __align__(16) float narrow_lds[];
+    const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), j = lane & 15, q = lane >> 4;
+    if (blockIdx.x >= r.runs) {
+        // rows in front of the first block and behind the last one
+        u32 front = r.offsets[0], back = r.offsets[r.blocks];
+        front = front < r.rows ? front : r.rows;
+        back = back < front ? front : back < r.rows ? back : r.rows;
+        const u32 count = front + (r.rows - back);
+        for (u32 i = blockIdx.x - r.runs; i < count && r.dx; i += kFillers)
+            for (u32 c = threadIdx.x; c < r.k; c += 256) r.dx[(u64)(i < front ? i : back + (i - front)) * r.lddx + c] = 0.0f;
+        return;
+    }
+    const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
+    if (!run.found) return;
+    const u32 row0 = run_row(run, run.local), height = run_row(run, run.local + 1) - row0;
+    const u32 pn = pitch_of(r.n), pk = pitch_of(r.k), kp = (r.k + 31) / 32 * 32, steps = (r.n + 3) / 4;
+    float *lw = narrow_lds, *ly = lw + r.shared + wave * kTileRows * (pn + pk), *lx = ly + kTileRows * pn;
+    if (r.dx && height > 0)
+        stage_weights<float, CK>(lw, r.w + (u64)run.block * r.w_block, r.ldw, r.in_major == 0, r.n, r.k);
+    __syncthreads();
+
+    const u32 tiles = (height + kTileRows - 1) / kTileRows;
+    const char *dy = reinterpret_cast<const char *>(r.dy + (u64)row0 * r.lddy);
+    const char *x = static_cast<const char *>(r.x) + (u64)row0 * (CODES ? kp : r.ldx * 4);
+    const uint8_t *scale = r.scale + (u64)row0 * (kp / 32);
+    Pieces<float, pieces_of(CN)> tile_y;
+    tile_y.init(r.lddy, r.n, lane);
+    typename std::conditional<CODES, CodePieces<pieces_of(CK)>, Pieces<float, pieces_of(CK)>>::type tile_x;
+    if constexpr (CODES) tile_x.init(kp, r.k, lane);
+    else tile_x.init(r.ldx, r.k, lane);
+    auto request = [&](u32 tile) {
+        const u32 rows = tile < tiles ? height - tile * kTileRows : 0u;
+        const u64 first = (u64)tile * kTileRows;
+        tile_y.request(dy + first * r.lddy * 4, rows);
+        if constexpr (CODES) tile_x.request(x + first * kp, scale + first * (kp / 32), r.x ? rows : 0u);
+        else tile_x.request(x + first * r.ldx * 4, r.x ? rows : 0u);
+    };
+    f32x4 dw[CK][CN] = {};
+    float db[CN] = {};
+    request(wave);
+    for (u32 tile = wave; tile < tiles; tile += 4) {
+        const u32 base = tile * kTileRows, left = height - base;
+        tile_y.put(ly, lane);
+        tile_x.put(lx, lane);
+        wave_meets();
+        request(tile + 4);
+        // sums over the tile's rows; columns that are not there hold what lies behind a row, and reach only results that are not kept
+#pragma unroll 1
+        for (u32 s = 0; s < 4; ++s) {
+            float fy[CN], fx[CK];
+#pragma unroll
+            for (u32 b = 0; b < CN; ++b) fy[b] = 16 * b + j < pn ? ly[(4 * s + q) * pn + 16 * b + j] : 0.0f;
+#pragma unroll
+            for (u32 a = 0; a < CK; ++a) fx[a] = 16 * a + j < pk ? lx[(4 * s + q) * pk + 16 * a + j] : 0.0f;
+#pragma unroll
+            for (u32 b = 0; b < CN; ++b) db[b] += fy[b];
+#pragma unroll
+            for (u32 a = 0; a < CK; ++a)
+#pragma unroll
+                for (u32 b = 0; b < CN; ++b) dw[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[a], fy[b], dw[a][b], 0, 0, 0);
+        }
+        if (r.dx) {
+            f32x4 acc[CK] = {};
+            for (u32 s = 0; s < steps; ++s) {
+                const float v = ly[j * pn + 4 * s + q];
+#pragma unroll
+                for (u32 c = 0; c < CK; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(lw[(s * CK + c) * kWave + lane], v, acc[c], 0, 0, 0);
+            }
+            if (j < left) {
+                float *out = r.dx + (u64)(row0 + base) * r.lddx + j * (u32)r.lddx;
+#pragma unroll
+                for (u32 c = 0; c < CK; ++c) {
+                    const u32 col = 16 * c + 4 * q;
+                    if (col >= r.k) continue;
+                    f32x4 v = acc[c];
+                    if (r.gate) {
+                        const f32x4 g = *reinterpret_cast<const f32x4 *>(lx + j * pk + col);
+#pragma unroll
+                        for (u32 e = 0; e < 4; ++e) v[e] = g[e] <= 0.0f ? 0.0f : v[e];          // NaN lets pass
+                    }
+                    if (col + 4 <= r.k) {
+                        store4(out + col, v);
+                    } else {
+#pragma unroll
+                        for (u32 e = 0; e < 3; ++e)
+                            if (col + e < r.k) out[col + e] = v[e];
+                    }
+                }
+            }
+        }
+        wave_meets();
+    }
+    if (!r.dw && !r.db) return;
+    // ---- the four wavefronts' sums: [output][input], then db
+    constexpr u32 ps = sums_pitch(CK);
+    float *ls = narrow_lds, *lb = ls + 16 * CN * ps;
+#pragma unroll
+    for (u32 b = 0; b < CN; ++b) {
+        db[b] += __shfl_xor(db[b], 16, kWave);
+        db[b] += __shfl_xor(db[b], 32, kWave);
+    }
+    for (u32 turn = 0; turn < 4; ++turn) {
+        __syncthreads();
+        if (wave != turn) continue;
+#pragma unroll
+        for (u32 b = 0; b < CN; ++b) {
+#pragma unroll
+            for (u32 a = 0; a < CK; ++a) {
+                f32x4 *p = reinterpret_cast<f32x4 *>(ls + (16 * b + j) * ps + 16 * a + 4 * q);
+                *p = turn == 0 ? dw[a][b] : *p + dw[a][b];
+            }
+            if (q == 0) lb[16 * b + j] = turn == 0 ? db[b] : lb[16 * b + j] + db[b];
+        }
+    }
+    __syncthreads();
+    const bool whole = run.runs == 1;
+    const u32 size = r.n * r.k;
+    float *to_w = whole ? r.dw + (u64)run.block * size : r.part + (u64)blockIdx.x * (size + r.n);
+    float *to_b = whole ? r.db + (u64)run.block * r.n : r.part + (u64)blockIdx.x * (size + r.n) + size;
+    if (r.dw)
+        for (u32 i = threadIdx.x; i < size; i += 256) {
+            const u32 outer = i / (r.in_major ? r.n : r.k), inner = i - outer * (r.in_major ? r.n : r.k);
+            to_w[i] = r.in_major ? ls[inner * ps + outer] : ls[outer * ps + inner];
+        }
+    if (r.db)
+        for (u32 i = threadIdx.x; i < r.n; i += 256) to_b[i] = lb[i];
+}
+
+template <u32 CN, u32 CK>
+hipError_t narrow_backward_go(BackwardArgs r, bool codes, hipStream_t stream)
+{
+    const u32 weights = (r.n + 3) / 4 * CK * kWave, sums = 16 * CN * sums_pitch(CK) + 16 * CN;
+    const u32 tiles = 4 * kTileRows * (pitch_of(r.n) + pitch_of(r.k));
+    r.shared = weights;
+    const u32 lds = (weights + tiles > sums ? weights + tiles : sums) * 4;
+    auto kernel = codes ? narrow_backward_kernel<CN, CK, true> : narrow_backward_kernel<CN, CK, false>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(r.runs + kFillers), dim3(256), lds, stream, r);
+    return hipGetLastError();
+}
+template <u32 CN>
+hipError_t narrow_backward_k(const BackwardArgs &r, bool codes, hipStream_t stream)
+{
+    switch ((r.k + 15) / 16) {
+    case 1: return narrow_backward_go<CN, 1>(r, codes, stream);
+    case 2: return narrow_backward_go<CN, 2>(r, codes, stream);
+    case 3: return narrow_backward_go<CN, 3>(r, codes, stream);
+    default: break;
+    }
+    if constexpr (CN <= 6) return narrow_backward_go<CN, 4>(r, codes, stream);
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+bool narrow_backward_fits(const BackwardArgs &r, bool codes)
+{
+    if (r.n < 4 || r.k < 4 || r.n > 128 || r.k > 64 || (r.n > 96 && r.k > 48)) return false;
+    return r.lddy <= kNarrowStride && r.lddx <= kNarrowStride && (codes || r.ldx <= kNarrowStride);
+}
+
+u32 narrow_backward_rows(u32 rows, u32 blocks)
+{
+    // three workgroups a compute unit at most, all of them at once, whole tiles for each of their wavefronts
+    const u32 slots = 768 - (blocks < 384 ? blocks : 384);
+    const u32 per = (u32)(((u64)rows + slots * 64 - 1) / (slots * 64)) * 64;
+    return per < 64 ? 64 : per;
+}
+
+hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream)
+{
+    if (r.n <= 32) return narrow_backward_k<2>(r, codes, stream);
+    if (r.n <= 64) return narrow_backward_k<4>(r, codes, stream);
+    if (r.n <= 80) return narrow_backward_k<5>(r, codes, stream);
+    if (r.n <= 96) return narrow_backward_k<6>(r, codes, stream);
+    return narrow_backward_k<8>(r, codes, stream);
+}
+
+}  // namespace lmk

@@ -82,7 +82,7 @@ bool narrow_rows_fit(const RowsArgs &r);
 hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream);
 
 bool narrow_backward_fits(const BackwardArgs &r, bool codes);
-u32 narrow_backward_rows(u32 rows, u32 blocks);
+u32 narrow_backward_rows(u32 rows, u32 blocks, u32 n, u32 k);
 hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream);
 
 // bfloat16 whose rows start at 16-byte boundaries

@@ -436,7 +436,7 @@ bool grouped_linear_fits(const lmk_gs_linear &l)
 // Small matrices in float32 take one pass over the rows for all three gradients; the rest of the rule (strides) is the
 // arrays', and what does not fit takes the other kernels with the same runs.
 static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l.n <= 128 && l.k <= 64; }
-static u32 rows_of_partial(const lmk_gs_linear &l) { return one_pass(l) ? narrow_backward_rows(l.rows, l.blocks) : rows_of_run(l); }
+static u32 rows_of_partial(const lmk_gs_linear &l) { return one_pass(l) ? narrow_backward_rows(l.rows, l.blocks, l.n, l.k) : rows_of_run(l); }
 
 size_t grouped_backward_bytes(const lmk_gs_linear &l)
 {

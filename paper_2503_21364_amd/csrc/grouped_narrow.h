@@ -31,25 +31,49 @@ template <class T> __device__ __forceinline__ f32x4 load4_of(const T *p, u32 c, 
     return v;
 }
 
-// A lane's N pieces (four values each) of a tile of rows of `width` >= 4 values.  Where rows end inside a piece, the row's
-// last four values are read and moved into place.
+// How a wavefront brings a tile of rows of `width` values, four at a time: as many rows as it has lanes for in a turn, N
+// turns.  A lane has the same columns in all of them, so that what it keeps is one offset.
+struct Turns {
+    u32 row, col;           // of the first turn; row ~0u: a lane without work
+    u32 rows;               // of a turn
+    u32 to;                 // offset in LDS
+
+    __device__ __forceinline__ void init(u32 width, u32 lane)
+    {
+        const u32 quads = (width + 3) / 4;
+        rows = kWave / quads;
+        row = lane / quads;
+        col = (lane - row * quads) * 4;
+        to = row * pitch_of(width) + col;
+        if (row >= rows) row = ~0u;
+    }
+};
+// turns that a tile of at most 4 `quads` values a row takes
+__host__ __device__ constexpr u32 turns_of(u32 quads) { return (kTileRows + kWave / quads - 1) / (kWave / quads); }
+
+// Clears what lies between the rows of a tile in LDS, once: no turn writes there.
+__device__ __forceinline__ void clear_gaps(float *lds, u32 width, u32 lane)
+{
+    const u32 pitch = pitch_of(width), from = (width + 3) / 4 * 4, gap = pitch - from;
+    if (lane < kTileRows)
+        for (u32 c = 0; c < gap; ++c) lds[lane * pitch + from + c] = 0.0f;
+}
+
+// Rows of `width` >= 4 values.  Where they end inside four values, the row's last four are read and moved into place.
 template <class T, u32 N> struct Pieces {
+    Turns t;
     f32x4 next[N];
-    u32 from[N], of_row[N];
-    bool last[N];
-    u32 rest, quads;
+    u32 from, turn_bytes, turn_floats;
+    u32 rest;               // of the last four values, where this lane has them; else 0
 
     __device__ __forceinline__ void init(u64 ld, u32 width, u32 lane)
     {
-        quads = pitch_of(width) / 4;
-        rest = width % 4;
-#pragma unroll
-        for (u32 i = 0; i < N; ++i) {
-            const u32 piece = lane + i * kWave, m = piece / quads, c = (piece - m * quads) * 4;
-            last[i] = c + 4 > width;
-            of_row[i] = m < kTileRows && c < width ? m : ~0u;
-            from[i] = (m * (u32)ld + (last[i] ? width - 4 : c)) * (u32)sizeof(T);
-        }
+        t.init(width, lane);
+        const bool last = t.col + 4 > width;
+        rest = last ? width % 4 : 0u;
+        from = ((t.row == ~0u ? 0u : t.row) * (u32)ld + (last ? width - 4 : t.col)) * (u32)sizeof(T);
+        turn_bytes = t.rows * (u32)ld * (u32)sizeof(T);
+        turn_floats = t.rows * pitch_of(width);
     }
     // asks for the tile whose first row is p; rows from `rows` on are zeros
     __device__ __forceinline__ void request(const char *p, u32 rows)
@@ -57,18 +81,16 @@ template <class T, u32 N> struct Pieces {
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
             next[i] = f32x4{};
-            if (of_row[i] < rows) next[i] = load4(reinterpret_cast<const T *>(p + from[i]));
+            if (t.row < rows && t.row + i * t.rows < rows) next[i] = load4(reinterpret_cast<const T *>(p + i * (u64)turn_bytes + from));
         }
     }
-    __device__ __forceinline__ void put(float *lds, u32 lane) const
+    __device__ __forceinline__ void put(float *lds) const
     {
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
             f32x4 v = next[i];
-            if (rest != 0 && last[i])
-                v = rest == 1 ? f32x4{v[3], 0.f, 0.f, 0.f} : rest == 2 ? f32x4{v[2], v[3], 0.f, 0.f} : f32x4{v[1], v[2], v[3], 0.f};
-            const u32 piece = lane + i * kWave;
-            if (piece < kTileRows * quads) *reinterpret_cast<f32x4 *>(lds + 4 * piece) = v;
+            if (rest != 0) v = rest == 1 ? f32x4{v[3], 0.f, 0.f, 0.f} : rest == 2 ? f32x4{v[2], v[3], 0.f, 0.f} : f32x4{v[1], v[2], v[3], 0.f};
+            if (t.row < kTileRows && t.row + i * t.rows < kTileRows) *reinterpret_cast<f32x4 *>(lds + t.to + i * turn_floats) = v;
         }
     }
 };

@@ -12,10 +12,10 @@ namespace lmk {
 
 namespace {
 
-// CT: 16 columns each; PIECES: 16-byte pieces of a tile of x a lane brings (16 rows of at most 4 PIECES pieces)
+// CT: 16 columns each; PIECES: turns in which a wavefront brings a tile of x
 // KEEP: also writes the 8-bit form of x; GATE: 0 none, 1 values, 2 codes
 template <class T, u32 CT, u32 PIECES, bool KEEP, u32 GATE>
-__global__ __launch_bounds__(256, PIECES == 3 ? 4 : PIECES == 5 ? 3 : 2) void narrow_rows_kernel(const RowsArgs r)
+__global__ __launch_bounds__(256, PIECES <= 4 ? 4 : 3) void narrow_rows_kernel(const RowsArgs r)
 {
     extern __shared__ __align__(16) float narrow_lds[];
     const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
@@ -37,13 +37,14 @@ __global__ __launch_bounds__(256, PIECES == 3 ? 4 : PIECES == 5 ? 3 : 2) void na
     const char *x = reinterpret_cast<const char *>(static_cast<const T *>(r.a) + (u64)row0 * r.lda);
     Pieces<T, PIECES> tile_of_x;
     tile_of_x.init(r.lda, r.sums, lane);
+    clear_gaps(lx, r.sums, lane);
     auto request = [&](u32 tile) {
         tile_of_x.request(x + (u64)tile * kTileRows * r.lda * sizeof(T), inside && tile < tiles ? height - tile * kTileRows : 0u);
     };
     request(wave);
     for (u32 tile = wave; tile < tiles; tile += 4) {
         const u32 base = tile * kTileRows, left = height - base;
-        tile_of_x.put(lx, lane);
+        tile_of_x.put(lx);
         wave_meets();
         request(tile + 4);
         f32x4 acc[CT];
@@ -142,10 +143,9 @@ hipError_t narrow_go(RowsArgs r, hipStream_t stream)
 template <class T, u32 CT>
 hipError_t narrow_sums(const RowsArgs &r, hipStream_t stream)
 {
-    // 16 rows of pitch / 4 pieces over 64 lanes
-    if (pitch_of(r.sums) <= 36) return narrow_go<T, CT, 3>(r, stream);
-    if (pitch_of(r.sums) <= 68) return narrow_go<T, CT, 5>(r, stream);
-    return narrow_go<T, CT, 9>(r, stream);
+    if (r.sums <= 36) return narrow_go<T, CT, turns_of(9)>(r, stream);
+    if (r.sums <= 64) return narrow_go<T, CT, turns_of(16)>(r, stream);
+    return narrow_go<T, CT, turns_of(32)>(r, stream);
 }
 template <class T>
 hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)

@@ -12,40 +12,36 @@ namespace lmk {
 
 namespace {
 
-// A lane's N pieces (four codes each) of a tile of the 8-bit form
+// The same from the 8-bit form, widened on the way into LDS
 template <u32 N> struct CodePieces {
+    Turns t;
     u32 next[N], scale[N];
-    u32 from[N], of_row[N];
-    u32 quads;
+    u32 from, turn_codes, turn_floats;
 
     __device__ __forceinline__ void init(u32 kp, u32 width, u32 lane)
     {
-        quads = pitch_of(width) / 4;
-#pragma unroll
-        for (u32 i = 0; i < N; ++i) {
-            const u32 piece = lane + i * kWave, m = piece / quads, c = (piece - m * quads) * 4;
-            of_row[i] = m < kTileRows && c < kp ? m : ~0u;
-            from[i] = m * kp + c;
-        }
+        t.init(width, lane);
+        from = (t.row == ~0u ? 0u : t.row) * kp + t.col;
+        turn_codes = t.rows * kp;
+        turn_floats = t.rows * pitch_of(width);
     }
     __device__ __forceinline__ void request(const char *codes, const uint8_t *scales, u32 rows)
     {
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
             next[i] = scale[i] = 0;
-            if (of_row[i] >= rows) continue;
-            next[i] = *reinterpret_cast<const u32 *>(codes + from[i]);
-            scale[i] = scales[from[i] / 32];
+            if (!(t.row < rows && t.row + i * t.rows < rows)) continue;
+            next[i] = *reinterpret_cast<const u32 *>(codes + i * turn_codes + from);
+            scale[i] = scales[(i * turn_codes + from) / 32];
         }
     }
-    __device__ __forceinline__ void put(float *lds, u32 lane) const
+    __device__ __forceinline__ void put(float *lds) const
     {
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
             const float step = step_of(scale[i]);
-            const u32 piece = lane + i * kWave;
-            if (piece < kTileRows * quads)
-                *reinterpret_cast<f32x4 *>(lds + 4 * piece) =
+            if (t.row < kTileRows && t.row + i * t.rows < kTileRows)
+                *reinterpret_cast<f32x4 *>(lds + t.to + i * turn_floats) =
                     f32x4{value_of(next[i], 0, step), value_of(next[i], 1, step), value_of(next[i], 2, step), value_of(next[i], 3, step)};
         }
     }
@@ -53,14 +49,15 @@ template <u32 N> struct CodePieces {
 
 constexpr u32 kFillers = 64;            // workgroups for dx of rows of no block
 
-// pieces of a tile of at most 16 CT values a row
-constexpr u32 pieces_of(u32 ct) { return (kTileRows * (pitch_of(16 * ct) / 4) + kWave - 1) / kWave; }
 // floats between the outputs of the joined sums in LDS
 constexpr u32 sums_pitch(u32 ck) { return 16 * ck + 4; }
 
+// workgroups of a compute unit (wavefronts of a SIMD): as many as the registers of the sums leave
+constexpr u32 resident(u32 tiles) { return tiles <= 12 ? 3 : 2; }
+
 // CN, CK: 16 outputs and 16 inputs each
 template <u32 CN, u32 CK, bool CODES>
-__global__ __launch_bounds__(256, CN * CK <= 8 ? 4 : CN * CK <= 18 ? 3 : 2) void narrow_backward_kernel(const BackwardArgs r)
+__global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel(const BackwardArgs r)
 {
     extern __shared__ __align__(16) float narrow_lds[];
     const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), j = lane & 15, q = lane >> 4;
@@ -87,11 +84,13 @@ __global__ __launch_bounds__(256, CN * CK <= 8 ? 4 : CN * CK <= 18 ? 3 : 2) void
     const char *dy = reinterpret_cast<const char *>(r.dy + (u64)row0 * r.lddy);
     const char *x = static_cast<const char *>(r.x) + (u64)row0 * (CODES ? kp : r.ldx * 4);
     const uint8_t *scale = r.scale + (u64)row0 * (kp / 32);
-    Pieces<float, pieces_of(CN)> tile_y;
+    Pieces<float, turns_of(4 * CN)> tile_y;
     tile_y.init(r.lddy, r.n, lane);
-    typename std::conditional<CODES, CodePieces<pieces_of(CK)>, Pieces<float, pieces_of(CK)>>::type tile_x;
+    typename std::conditional<CODES, CodePieces<turns_of(4 * CK)>, Pieces<float, turns_of(4 * CK)>>::type tile_x;
     if constexpr (CODES) tile_x.init(kp, r.k, lane);
     else tile_x.init(r.ldx, r.k, lane);
+    clear_gaps(ly, r.n, lane);
+    clear_gaps(lx, r.k, lane);
     auto request = [&](u32 tile) {
         const u32 rows = tile < tiles ? height - tile * kTileRows : 0u;
         const u64 first = (u64)tile * kTileRows;
@@ -104,12 +103,12 @@ __global__ __launch_bounds__(256, CN * CK <= 8 ? 4 : CN * CK <= 18 ? 3 : 2) void
     request(wave);
     for (u32 tile = wave; tile < tiles; tile += 4) {
         const u32 base = tile * kTileRows, left = height - base;
-        tile_y.put(ly, lane);
-        tile_x.put(lx, lane);
+        tile_y.put(ly);
+        tile_x.put(lx);
         wave_meets();
         request(tile + 4);
         // sums over the tile's rows; columns that are not there hold what lies behind a row, and reach only results that are not kept
-#pragma unroll 1
+#pragma unroll
         for (u32 s = 0; s < 4; ++s) {
             float fy[CN], fx[CK];
 #pragma unroll
@@ -125,7 +124,21 @@ __global__ __launch_bounds__(256, CN * CK <= 8 ? 4 : CN * CK <= 18 ? 3 : 2) void
         }
         if (r.dx) {
             f32x4 acc[CK] = {};
-            for (u32 s = 0; s < steps; ++s) {
+            u32 s = 0;
+            for (; s + 4 <= steps; s += 4) {            // four steps' operands on their way from LDS
+                float v[4], w[4][CK];
+#pragma unroll
+                for (u32 e = 0; e < 4; ++e) {
+                    v[e] = ly[j * pn + 4 * (s + e) + q];
+#pragma unroll
+                    for (u32 c = 0; c < CK; ++c) w[e][c] = lw[((s + e) * CK + c) * kWave + lane];
+                }
+#pragma unroll
+                for (u32 e = 0; e < 4; ++e)
+#pragma unroll
+                    for (u32 c = 0; c < CK; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e][c], v[e], acc[c], 0, 0, 0);
+            }
+            for (; s < steps; ++s) {
                 const float v = ly[j * pn + 4 * s + q];
 #pragma unroll
                 for (u32 c = 0; c < CK; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(lw[(s * CK + c) * kWave + lane], v, acc[c], 0, 0, 0);
@@ -224,21 +237,27 @@ bool narrow_backward_fits(const BackwardArgs &r, bool codes)
     return r.lddy <= kNarrowStride && r.lddx <= kNarrowStride && (codes || r.ldx <= kNarrowStride);
 }
 
-u32 narrow_backward_rows(u32 rows, u32 blocks)
+// outputs in tiles of 16, as the kernels are built for them
+static u32 out_tiles(u32 n) { return n <= 32 ? 2 : n <= 64 ? 4 : n <= 80 ? 5 : n <= 96 ? 6 : 8; }
+
+u32 narrow_backward_rows(u32 rows, u32 blocks, u32 n, u32 k)
 {
-    // three workgroups a compute unit at most, all of them at once, whole tiles for each of their wavefronts
-    const u32 slots = 768 - (blocks < 384 ? blocks : 384);
+    // all workgroups at once, whole tiles for each of their wavefronts
+    const u32 most = 256 * resident(out_tiles(n) * ((k + 15) / 16));
+    const u32 slots = most - (blocks < most / 2 ? blocks : most / 2);
     const u32 per = (u32)(((u64)rows + slots * 64 - 1) / (slots * 64)) * 64;
     return per < 64 ? 64 : per;
 }
 
 hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream)
 {
-    if (r.n <= 32) return narrow_backward_k<2>(r, codes, stream);
-    if (r.n <= 64) return narrow_backward_k<4>(r, codes, stream);
-    if (r.n <= 80) return narrow_backward_k<5>(r, codes, stream);
-    if (r.n <= 96) return narrow_backward_k<6>(r, codes, stream);
-    return narrow_backward_k<8>(r, codes, stream);
+    switch (out_tiles(r.n)) {
+    case 2: return narrow_backward_k<2>(r, codes, stream);
+    case 4: return narrow_backward_k<4>(r, codes, stream);
+    case 5: return narrow_backward_k<5>(r, codes, stream);
+    case 6: return narrow_backward_k<6>(r, codes, stream);
+    default: return narrow_backward_k<8>(r, codes, stream);
+    }
 }
 
 }  // namespace lmk

@@ -59,29 +59,34 @@ __device__ __forceinline__ void clear_gaps(float *lds, u32 width, u32 lane)
         for (u32 c = 0; c < gap; ++c) lds[lane * pitch + from + c] = 0.0f;
 }
 
-// Rows of `width` >= 4 values.  Where they end inside four values, the row's last four are read and moved into place.
+// Rows of `width` >= 4 values.  Where they end inside four values, the row's last four are read and moved into place.  Rows that
+// are not there are read as the first one and put down as zeros: loads under conditions of their own would be waited for
+// one after the other.
 template <class T, u32 N> struct Pieces {
     Turns t;
     f32x4 next[N];
-    u32 from, turn_bytes, turn_floats;
-    u32 rest;               // of the last four values, where this lane has them; else 0
+    u32 first, turn_bytes, turn_floats;
+    u32 rest, rows;         // values behind the last whole four; rows of the requested tile
+    bool last;              // whether this lane has them
 
     __device__ __forceinline__ void init(u64 ld, u32 width, u32 lane)
     {
         t.init(width, lane);
-        const bool last = t.col + 4 > width;
-        rest = last ? width % 4 : 0u;
-        from = ((t.row == ~0u ? 0u : t.row) * (u32)ld + (last ? width - 4 : t.col)) * (u32)sizeof(T);
-        turn_bytes = t.rows * (u32)ld * (u32)sizeof(T);
+        rest = width % 4;
+        last = t.col + 4 > width;
+        first = (last ? width - 4 : t.col) * (u32)sizeof(T);
+        turn_bytes = (u32)ld * (u32)sizeof(T);
         turn_floats = t.rows * pitch_of(width);
     }
-    // asks for the tile whose first row is p; rows from `rows` on are zeros
-    __device__ __forceinline__ void request(const char *p, u32 rows)
+    // asks for the tile whose first row is p
+    __device__ __forceinline__ void request(const char *p, u32 rows_)
     {
+        rows = rows_;
+        if (rows == 0) return;
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
-            next[i] = f32x4{};
-            if (t.row < rows && t.row + i * t.rows < rows) next[i] = load4(reinterpret_cast<const T *>(p + i * (u64)turn_bytes + from));
+            const u32 row = t.row + i * t.rows;
+            next[i] = load4(reinterpret_cast<const T *>(p + ((t.row < rows && row < rows ? row : 0u) * turn_bytes + first)));
         }
     }
     __device__ __forceinline__ void put(float *lds) const
@@ -89,8 +94,17 @@ template <class T, u32 N> struct Pieces {
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
             f32x4 v = next[i];
-            if (rest != 0) v = rest == 1 ? f32x4{v[3], 0.f, 0.f, 0.f} : rest == 2 ? f32x4{v[2], v[3], 0.f, 0.f} : f32x4{v[1], v[2], v[3], 0.f};
-            if (t.row < kTileRows && t.row + i * t.rows < kTileRows) *reinterpret_cast<f32x4 *>(lds + t.to + i * turn_floats) = v;
+            if (rest != 0) {
+                const f32x4 moved = rest == 1 ? f32x4{v[3], 0.f, 0.f, 0.f} : rest == 2 ? f32x4{v[2], v[3], 0.f, 0.f} : f32x4{v[1], v[2], v[3], 0.f};
+#pragma unroll
+                for (u32 e = 0; e < 4; ++e) v[e] = last ? moved[e] : v[e];
+            }
+            const u32 row = t.row + i * t.rows;
+            if (rows < kTileRows) {
+#pragma unroll
+                for (u32 e = 0; e < 4; ++e) v[e] = row < rows ? v[e] : 0.0f;
+            }
+            if (t.row < kTileRows && row < kTileRows) *reinterpret_cast<f32x4 *>(lds + t.to + i * turn_floats) = v;
         }
     }
 };
@@ -100,17 +114,37 @@ template <class T, u32 N> struct Pieces {
 template <class T, u32 CT>
 __device__ __forceinline__ void stage_weights(float *lw, const T *w, u64 ldw, bool across, u32 sums, u32 cols)
 {
+    // four values of a matrix row of `width` from c on, rows and values that are not there zeros; no load has a condition
+    const auto four = [&](u32 row, u32 rows, u32 c, u32 width) {
+        const u32 back = c + 4 <= width ? 0u : width >= 4 ? c + 4 - width : 0u;          // the row's last four instead
+        const T *p = w + (u64)(row < rows ? row : 0u) * ldw + (c < width ? c - back : 0u);
+        f32x4 v;
+        if (width >= 4) v = load4(p);
+        else
+            for (u32 e = 0; e < 4; ++e) v[e] = e < width ? to_f32(p[e]) : 0.0f;
+        f32x4 o;
+#pragma unroll
+        for (u32 e = 0; e < 4; ++e) {
+            float f = v[e];
+            f = back == 1 ? (e < 3 ? v[e < 3 ? e + 1 : 3] : 0.0f) : f;
+            f = back == 2 ? (e < 2 ? v[e < 2 ? e + 2 : 3] : 0.0f) : f;
+            f = back == 3 ? (e < 1 ? v[3] : 0.0f) : f;
+            o[e] = row < rows && c < width ? f : 0.0f;
+        }
+        return o;
+    };
     const u32 steps = (sums + 3) / 4;
     if (across) {
+#pragma unroll 4
         for (u32 i = threadIdx.x; i < steps * 4 * CT * 4; i += 256) {
             const u32 s = i / (CT * 4), c = i % (CT * 4);
-            const f32x4 v = s < sums ? load4_of(w + (u64)s * ldw, 4 * c, cols) : f32x4{};
-            *reinterpret_cast<f32x4 *>(lw + (s / 4 * CT + c / 4) * kWave + s % 4 * 16 + c % 4 * 4) = v;
+            *reinterpret_cast<f32x4 *>(lw + (s / 4 * CT + c / 4) * kWave + s % 4 * 16 + c % 4 * 4) = four(s, sums, 4 * c, cols);
         }
     } else {
+#pragma unroll 4
         for (u32 i = threadIdx.x; i < steps * CT * 16; i += 256) {
-            const u32 c = i / steps, s = i % steps;
-            const f32x4 v = c < cols ? load4_of(w + (u64)c * ldw, 4 * s, sums) : f32x4{};
+            const u32 c = i / steps, s = i - c * steps;
+            const f32x4 v = four(c, cols, 4 * s, sums);
 #pragma unroll
             for (u32 e = 0; e < 4; ++e) lw[(s * CT + c / 16) * kWave + e * 16 + c % 16] = v[e];
         }

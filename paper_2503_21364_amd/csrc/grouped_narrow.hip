@@ -42,21 +42,11 @@ __global__ __launch_bounds__(256, PIECES <= 4 ? 4 : 3) void narrow_rows_kernel(c
         tile_of_x.request(x + (u64)tile * kTileRows * r.lda * sizeof(T), inside && tile < tiles ? height - tile * kTileRows : 0u);
     };
     request(wave);
+    tile_of_x.put(lx);
+    request(wave + 4);
     for (u32 tile = wave; tile < tiles; tile += 4) {
         const u32 base = tile * kTileRows, left = height - base;
-        tile_of_x.put(lx);
         wave_meets();
-        request(tile + 4);
-        f32x4 acc[CT];
-#pragma unroll
-        for (u32 c = 0; c < CT; ++c) acc[c] = inside ? *reinterpret_cast<const f32x4 *>(lb + 16 * c + 4 * q) : f32x4{};
-        if (inside) {
-            for (u32 s = 0; s < steps; ++s) {
-                const float v = lx[j * pitch + 4 * s + q];
-#pragma unroll
-                for (u32 c = 0; c < CT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(lw[(s * CT + c) * kWave + lane], v, acc[c], 0, 0, 0);
-            }
-        }
         if constexpr (KEEP) {
             // eight values a lane, four lanes for those that share a step; rows of no block are the zeros that request() left
             const u32 m = lane / 4, eight = lane % 4, kp = (r.sums + 31) / 32 * 32;
@@ -89,6 +79,21 @@ __global__ __launch_bounds__(256, PIECES <= 4 ? 4 : 3) void narrow_rows_kernel(c
                 if (eight == 0) scales[g] = (uint8_t)scale;
             }
         }
+        f32x4 acc[CT];
+#pragma unroll
+        for (u32 c = 0; c < CT; ++c) acc[c] = inside ? *reinterpret_cast<const f32x4 *>(lb + 16 * c + 4 * q) : f32x4{};
+        if (inside) {
+            for (u32 s = 0; s < steps; ++s) {
+                const float v = lx[j * pitch + 4 * s + q];
+#pragma unroll
+                for (u32 c = 0; c < CT; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(lw[(s * CT + c) * kWave + lane], v, acc[c], 0, 0, 0);
+            }
+        }
+        // The next tile takes this one's place before the results leave: what is waited for there is then this tile's loads and
+        // not its stores.
+        wave_meets();
+        tile_of_x.put(lx);
+        request(tile + 8);
         char *out = reinterpret_cast<char *>(static_cast<T *>(r.out) + (u64)(row0 + base) * r.ldo);
         const char *gate = static_cast<const char *>(r.gate) + (u64)(row0 + base) * r.ldgate * (GATE == 1 ? sizeof(T) : 1);
         const uint8_t *gate_scale = r.gate_scale + (GATE == 2 ? (u64)(row0 + base) * (r.ldgate / 32) : 0);
@@ -124,7 +129,6 @@ __global__ __launch_bounds__(256, PIECES <= 4 ? 4 : 3) void narrow_rows_kernel(c
                 }
             }
         }
-        wave_meets();                   // the tile's reads are done before the next one takes its place
     }
 }
 

@@ -4,8 +4,8 @@
 //     dx = dy w_g     weights on the matrix instruction's rows, dy's rows on its columns
 //     dw += x^T dy    inputs on its rows, outputs on its columns, summed over the tile's 16 rows
 // (v_mfma_f32_16x16x4_f32).  Of both, a tile of dy and of x (widened from its 8-bit form) is the operand, read from LDS.
-// db is added up from the values of dy on their way to the second product.  At the end the four wavefronts' sums are added in
-// LDS in their order.
+// db is added up from the values of dy on their way to the second product.  At the end the four wavefronts' sums meet in LDS
+// and are added in their order.
 #include "grouped_narrow.h"
 
 namespace lmk {
@@ -16,31 +16,33 @@ namespace {
 template <u32 N> struct CodePieces {
     Turns t;
     u32 next[N], scale[N];
-    u32 from, turn_codes, turn_floats;
+    u32 kp, turn_floats, rows;
 
-    __device__ __forceinline__ void init(u32 kp, u32 width, u32 lane)
+    __device__ __forceinline__ void init(u32 kp_, u32 width, u32 lane)
     {
         t.init(width, lane);
-        from = (t.row == ~0u ? 0u : t.row) * kp + t.col;
-        turn_codes = t.rows * kp;
+        kp = kp_;
         turn_floats = t.rows * pitch_of(width);
     }
-    __device__ __forceinline__ void request(const char *codes, const uint8_t *scales, u32 rows)
+    __device__ __forceinline__ void request(const char *codes, const uint8_t *scales, u32 rows_)
     {
+        rows = rows_;
+        if (rows == 0) return;
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
-            next[i] = scale[i] = 0;
-            if (!(t.row < rows && t.row + i * t.rows < rows)) continue;
-            next[i] = *reinterpret_cast<const u32 *>(codes + i * turn_codes + from);
-            scale[i] = scales[(i * turn_codes + from) / 32];
+            const u32 row = t.row + i * t.rows, at = (t.row < rows && row < rows ? row : 0u) * kp + t.col;
+            next[i] = *reinterpret_cast<const u32 *>(codes + at);
+            scale[i] = scales[at / 32];
         }
     }
     __device__ __forceinline__ void put(float *lds) const
     {
 #pragma unroll
         for (u32 i = 0; i < N; ++i) {
-            const float step = step_of(scale[i]);
-            if (t.row < kTileRows && t.row + i * t.rows < kTileRows)
+            const u32 row = t.row + i * t.rows;
+            // the byte 0 makes zeros of any codes
+            const float step = step_of(row < rows ? scale[i] : 0u);
+            if (t.row < kTileRows && row < kTileRows)
                 *reinterpret_cast<f32x4 *>(lds + t.to + i * turn_floats) =
                     f32x4{value_of(next[i], 0, step), value_of(next[i], 1, step), value_of(next[i], 2, step), value_of(next[i], 3, step)};
         }
@@ -51,6 +53,7 @@ constexpr u32 kFillers = 64;            // workgroups for dx of rows of no block
 
 // floats between the outputs of the joined sums in LDS
 constexpr u32 sums_pitch(u32 ck) { return 16 * ck + 4; }
+constexpr u32 sums_floats(u32 cn, u32 ck) { return 16 * cn * sums_pitch(ck) + 16 * cn; }
 
 // workgroups of a compute unit (wavefronts of a SIMD): as many as the registers of the sums leave
 constexpr u32 resident(u32 tiles) { return tiles <= 12 ? 3 : 2; }
@@ -100,113 +103,126 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
     };
     f32x4 dw[CK][CN] = {};
     float db[CN] = {};
-    request(wave);
-    for (u32 tile = wave; tile < tiles; tile += 4) {
-        const u32 base = tile * kTileRows, left = height - base;
+    auto put = [&]() {
         tile_y.put(ly);
         tile_x.put(lx);
+    };
+    request(wave);
+    put();
+    request(wave + 4);
+    for (u32 tile = wave; tile < tiles; tile += 4) {
+        const u32 base = tile * kTileRows, left = height - base;
         wave_meets();
-        request(tile + 4);
         // sums over the tile's rows; columns that are not there hold what lies behind a row, and reach only results that are not kept
+        float fy[2][CN], fx[2][CK];
+        auto operands = [&](u32 s, u32 at) {
+#pragma unroll
+            for (u32 b = 0; b < CN; ++b) fy[at][b] = 16 * b + j < pn ? ly[(4 * s + q) * pn + 16 * b + j] : 0.0f;
+#pragma unroll
+            for (u32 a = 0; a < CK; ++a) fx[at][a] = 16 * a + j < pk ? lx[(4 * s + q) * pk + 16 * a + j] : 0.0f;
+        };
+        operands(0, 0);
 #pragma unroll
         for (u32 s = 0; s < 4; ++s) {
-            float fy[CN], fx[CK];
+            if (s < 3) operands(s + 1, (s + 1) & 1);
 #pragma unroll
-            for (u32 b = 0; b < CN; ++b) fy[b] = 16 * b + j < pn ? ly[(4 * s + q) * pn + 16 * b + j] : 0.0f;
-#pragma unroll
-            for (u32 a = 0; a < CK; ++a) fx[a] = 16 * a + j < pk ? lx[(4 * s + q) * pk + 16 * a + j] : 0.0f;
-#pragma unroll
-            for (u32 b = 0; b < CN; ++b) db[b] += fy[b];
+            for (u32 b = 0; b < CN; ++b) db[b] += fy[s & 1][b];
 #pragma unroll
             for (u32 a = 0; a < CK; ++a)
 #pragma unroll
-                for (u32 b = 0; b < CN; ++b) dw[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[a], fy[b], dw[a][b], 0, 0, 0);
+                for (u32 b = 0; b < CN; ++b) dw[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[s & 1][a], fy[s & 1][b], dw[a][b], 0, 0, 0);
         }
+        f32x4 acc[CK] = {};
         if (r.dx) {
-            f32x4 acc[CK] = {};
-            u32 s = 0;
-            for (; s + 4 <= steps; s += 4) {            // four steps' operands on their way from LDS
-                float v[4], w[4][CK];
+            // two steps' operands are on their way from LDS while two are multiplied; behind the last one zeros
+            float v[2][2], w[2][2][CK];
+            auto fetch = [&](u32 s, u32 at) {
 #pragma unroll
-                for (u32 e = 0; e < 4; ++e) {
-                    v[e] = ly[j * pn + 4 * (s + e) + q];
+                for (u32 e = 0; e < 2; ++e) {
+                    const u32 t = s + e < steps ? s + e : steps - 1;
+                    v[at][e] = s + e < steps ? ly[j * pn + 4 * t + q] : 0.0f;
 #pragma unroll
-                    for (u32 c = 0; c < CK; ++c) w[e][c] = lw[((s + e) * CK + c) * kWave + lane];
+                    for (u32 c = 0; c < CK; ++c) w[at][e][c] = lw[(t * CK + c) * kWave + lane];
                 }
+            };
+            auto multiply = [&](u32 at) {
 #pragma unroll
-                for (u32 e = 0; e < 4; ++e)
+                for (u32 e = 0; e < 2; ++e)
 #pragma unroll
-                    for (u32 c = 0; c < CK; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e][c], v[e], acc[c], 0, 0, 0);
+                    for (u32 c = 0; c < CK; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[at][e][c], v[at][e], acc[c], 0, 0, 0);
+            };
+            fetch(0, 0);
+            for (u32 s = 0; s < steps; s += 4) {
+                fetch(s + 2, 1);
+                multiply(0);
+                fetch(s + 4, 0);
+                multiply(1);
             }
-            for (; s < steps; ++s) {
-                const float v = ly[j * pn + 4 * s + q];
-#pragma unroll
-                for (u32 c = 0; c < CK; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(lw[(s * CK + c) * kWave + lane], v, acc[c], 0, 0, 0);
-            }
-            if (j < left) {
-                float *out = r.dx + (u64)(row0 + base) * r.lddx + j * (u32)r.lddx;
+            if (r.gate) {
 #pragma unroll
                 for (u32 c = 0; c < CK; ++c) {
-                    const u32 col = 16 * c + 4 * q;
-                    if (col >= r.k) continue;
-                    f32x4 v = acc[c];
-                    if (r.gate) {
-                        const f32x4 g = *reinterpret_cast<const f32x4 *>(lx + j * pk + col);
+                    if (16 * c + 4 * q >= r.k) continue;
+                    const f32x4 g = *reinterpret_cast<const f32x4 *>(lx + j * pk + 16 * c + 4 * q);
 #pragma unroll
-                        for (u32 e = 0; e < 4; ++e) v[e] = g[e] <= 0.0f ? 0.0f : v[e];          // NaN lets pass
-                    }
-                    if (col + 4 <= r.k) {
-                        store4(out + col, v);
-                    } else {
-#pragma unroll
-                        for (u32 e = 0; e < 3; ++e)
-                            if (col + e < r.k) out[col + e] = v[e];
-                    }
+                    for (u32 e = 0; e < 4; ++e) acc[c][e] = g[e] <= 0.0f ? 0.0f : acc[c][e];          // NaN lets pass
                 }
             }
         }
+        // The next tile takes this one's place before the results leave: what is waited for there is then this tile's loads and
+        // not its stores.
         wave_meets();
+        put();
+        request(tile + 8);
+        if (r.dx && j < left) {
+            float *out = r.dx + (u64)(row0 + base) * r.lddx + j * (u32)r.lddx;
+#pragma unroll
+            for (u32 c = 0; c < CK; ++c) {
+                const u32 col = 16 * c + 4 * q;
+                if (col + 4 <= r.k) {
+                    store4(out + col, acc[c]);
+                } else {
+#pragma unroll
+                    for (u32 e = 0; e < 3; ++e)
+                        if (col + e < r.k) out[col + e] = acc[c][e];
+                }
+            }
+        }
     }
     if (!r.dw && !r.db) return;
-    // ---- the four wavefronts' sums: [output][input], then db
-    constexpr u32 ps = sums_pitch(CK);
-    float *ls = narrow_lds, *lb = ls + 16 * CN * ps;
+    // ---- the four wavefronts' sums, [output][input] and then db each
+    constexpr u32 ps = sums_pitch(CK), part = sums_floats(CN, CK);
+    __syncthreads();
+    float *ls = narrow_lds + wave * part, *lb = ls + 16 * CN * ps;
 #pragma unroll
     for (u32 b = 0; b < CN; ++b) {
         db[b] += __shfl_xor(db[b], 16, kWave);
         db[b] += __shfl_xor(db[b], 32, kWave);
-    }
-    for (u32 turn = 0; turn < 4; ++turn) {
-        __syncthreads();
-        if (wave != turn) continue;
 #pragma unroll
-        for (u32 b = 0; b < CN; ++b) {
-#pragma unroll
-            for (u32 a = 0; a < CK; ++a) {
-                f32x4 *p = reinterpret_cast<f32x4 *>(ls + (16 * b + j) * ps + 16 * a + 4 * q);
-                *p = turn == 0 ? dw[a][b] : *p + dw[a][b];
-            }
-            if (q == 0) lb[16 * b + j] = turn == 0 ? db[b] : lb[16 * b + j] + db[b];
-        }
+        for (u32 a = 0; a < CK; ++a) *reinterpret_cast<f32x4 *>(ls + (16 * b + j) * ps + 16 * a + 4 * q) = dw[a][b];
+        if (q == 0) lb[16 * b + j] = db[b];
     }
     __syncthreads();
     const bool whole = run.runs == 1;
     const u32 size = r.n * r.k;
     float *to_w = whole ? r.dw + (u64)run.block * size : r.part + (u64)blockIdx.x * (size + r.n);
     float *to_b = whole ? r.db + (u64)run.block * r.n : r.part + (u64)blockIdx.x * (size + r.n) + size;
-    if (r.dw)
+    const auto joined = [&](u32 at) { return ((narrow_lds[at] + narrow_lds[part + at]) + narrow_lds[2 * part + at]) + narrow_lds[3 * part + at]; };
+    if (r.dw) {
+        const u32 width = r.in_major ? r.n : r.k;
+#pragma unroll 4
         for (u32 i = threadIdx.x; i < size; i += 256) {
-            const u32 outer = i / (r.in_major ? r.n : r.k), inner = i - outer * (r.in_major ? r.n : r.k);
-            to_w[i] = r.in_major ? ls[inner * ps + outer] : ls[outer * ps + inner];
+            const u32 outer = i / width, inner = i - outer * width;
+            to_w[i] = joined(r.in_major ? inner * ps + outer : outer * ps + inner);
         }
+    }
     if (r.db)
-        for (u32 i = threadIdx.x; i < r.n; i += 256) to_b[i] = lb[i];
+        for (u32 i = threadIdx.x; i < r.n; i += 256) to_b[i] = joined(16 * CN * ps + i);
 }
 
 template <u32 CN, u32 CK>
 hipError_t narrow_backward_go(BackwardArgs r, bool codes, hipStream_t stream)
 {
-    const u32 weights = (r.n + 3) / 4 * CK * kWave, sums = 16 * CN * sums_pitch(CK) + 16 * CN;
+    const u32 weights = (r.n + 3) / 4 * CK * kWave, sums = 4 * sums_floats(CN, CK);
     const u32 tiles = 4 * kTileRows * (pitch_of(r.n) + pitch_of(r.k));
     r.shared = weights;
     const u32 lds = (weights + tiles > sums ? weights + tiles : sums) * 4;

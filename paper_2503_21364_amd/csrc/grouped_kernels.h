@@ -88,6 +88,7 @@ hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t
 // bfloat16 whose rows start at 16-byte boundaries
 bool wide_rows_fit(const RowsArgs &r, bool across);
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream);
+u32 wide_sums_side(u32 n, u32 k);            // of its tiles
 bool wide_sums_fit(const SumsArgs &r);
 hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream);
 

@@ -132,28 +132,23 @@ template <u32 W> struct Across8 {
     }
 };
 
-// Wavefronts of a workgroup over a TM x TN tile: 2 x 2 where both sides have 128, else all along TM.
-template <u32 TM, u32 TN> struct Split {
-    static constexpr u32 kCols = TN == 128 ? 2 : 1, kRows = 4 / kCols;
-    static constexpr u32 kM = TM / kRows / 32, kN = TN / kCols / 32;        // 32 x 32 results of a wavefront
-    static_assert(kM * kRows * 32 == TM && kN * kCols * 32 == TN, "whole results");
-};
+// Tiles of 64 x 64 results, 32 x 32 a wavefront: four workgroups a compute unit hide what a step waits for, and the
+// operands' way through LDS is no limit at this instruction's rate (128 x 128 tiles, two workgroups: 66 instead of 80 TFLOP/s at
+// 65 536 x 256 x 256, 101 instead of 104 at 8192 x 4096 x 4096).
+constexpr u32 kTile = 64;
 
 // The product of a tile: acc += A B over `sums`.  `each` is called with the staged A of every step.
-template <u32 TM, u32 TN, class A, class B, class Each>
-__device__ __forceinline__ void tile_product(A &a, B &b, u32 sums, float *lds, f32x16 (&acc)[Split<TM, TN>::kM][Split<TM, TN>::kN],
-                                             Each &&each)
+template <class A, class B, class Each>
+__device__ __forceinline__ void tile_product(A &a, B &b, u32 sums, float *lds, f32x16 &acc, Each &&each)
 {
-    using S = Split<TM, TN>;
-    constexpr u32 pa = pitch_of(TM), pb = pitch_of(TN), buffer = kStep * (pa + pb);
+    constexpr u32 pitch = pitch_of(kTile), buffer = 2 * kStep * pitch;
     const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const u32 j = lane & 31, hi = lane / 32;
-    const u32 m0 = wave / S::kCols * (S::kM * 32) + j, n0 = wave % S::kCols * (S::kN * 32) + j;
+    const u32 j = lane & 31, hi = lane / 32, m0 = wave / 2 * 32 + j, n0 = wave % 2 * 32 + j;
     a.load(0);
     b.load(0);
     u32 at = 0;
     for (u32 s0 = 0; s0 < sums; s0 += kStep, at ^= 1) {
-        float *la = lds + at * buffer, *lb = la + kStep * pa;
+        float *la = lds + at * buffer, *lb = la + kStep * pitch;
         a.store(la);
         b.store(lb);
         __syncthreads();                     // the other buffer's readers are past the previous one of these
@@ -165,15 +160,7 @@ __device__ __forceinline__ void tile_product(A &a, B &b, u32 sums, float *lds, f
         // steps t and t + 16 in one instruction; the last ones of a short tile hold nothing
         const u32 left = sums - s0;
         auto step = [&](u32 t) {
-            float fa[S::kM], fb[S::kN];
-#pragma unroll
-            for (u32 m = 0; m < S::kM; ++m) fa[m] = la[(t + 16 * hi) * pa + m0 + 32 * m];
-#pragma unroll
-            for (u32 n = 0; n < S::kN; ++n) fb[n] = lb[(t + 16 * hi) * pb + n0 + 32 * n];
-#pragma unroll
-            for (u32 m = 0; m < S::kM; ++m)
-#pragma unroll
-                for (u32 n = 0; n < S::kN; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[m], fb[n], acc[m][n], 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(la[(t + 16 * hi) * pitch + m0], lb[(t + 16 * hi) * pitch + n0], acc, 0, 0, 0);
         };
         if (left >= 16) {
 #pragma unroll
@@ -190,96 +177,87 @@ __device__ __forceinline__ u32 row_of(u32 v, u32 hi) { return 8 * (v / 4) + 4 * 
 // ---- rows against weights
 
 // GATE: 0 none, 1 values, 2 codes
-template <class T, u32 TN, bool ACROSS, u32 GATE>
-__global__ __launch_bounds__(256, 2) void rows_kernel(const RowsArgs r)
+template <class T, bool ACROSS, u32 GATE>
+__global__ __launch_bounds__(256, 4) void rows_kernel(const RowsArgs r)
 {
-    constexpr u32 TM = 128;
-    using S = Split<TM, TN>;
-    __shared__ __align__(16) float lds[2 * kStep * (pitch_of(TM) + pitch_of(TN))];
+    __shared__ __align__(16) float lds[4 * kStep * pitch_of(kTile)];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
-    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * TN;
-    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, TM, row_tile);
+    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * kTile;
+    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, kTile, row_tile);
     if (!run.found) return;
-    const u32 row0 = run.begin + run.local * TM;
-    const u32 height = run.end - row0 < TM ? run.end - row0 : TM;
-    const u32 width = r.cols - col0 < TN ? r.cols - col0 : TN;
+    const u32 row0 = run.begin + run.local * kTile;
+    const u32 height = run.end - row0 < kTile ? run.end - row0 : kTile;
+    const u32 width = r.cols - col0 < kTile ? r.cols - col0 : kTile;
     T *out = static_cast<T *>(r.out) + (u64)row0 * r.ldo + col0;
     const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 31, hi = lane / 32;
-    const u32 m0 = wave / S::kCols * (S::kM * 32), n0 = wave % S::kCols * (S::kN * 32);
-    f32x16 acc[S::kM][S::kN] = {};
+    f32x16 acc = {};
     if (run.block != ~0u) {
-        Along<T, TM> a{static_cast<const T *>(r.a) + (u64)row0 * r.lda, r.lda, height, r.sums, {}};
+        Along<T, kTile> a{static_cast<const T *>(r.a) + (u64)row0 * r.lda, r.lda, height, r.sums, {}};
         const T *w = static_cast<const T *>(r.w) + (u64)run.block * r.w_block;
         if constexpr (ACROSS) {
-            Across<T, TN> b{w + col0, r.ldw, width, r.sums, {}};
-            tile_product<TM, TN>(a, b, r.sums, lds, acc, [](const float *) {});
+            Across<T, kTile> b{w + col0, r.ldw, width, r.sums, {}};
+            tile_product(a, b, r.sums, lds, acc, [](const float *) {});
         } else {
-            Along<T, TN> b{w + (u64)col0 * r.ldw, r.ldw, width, r.sums, {}};
-            tile_product<TM, TN>(a, b, r.sums, lds, acc, [](const float *) {});
+            Along<T, kTile> b{w + (u64)col0 * r.ldw, r.ldw, width, r.sums, {}};
+            tile_product(a, b, r.sums, lds, acc, [](const float *) {});
         }
     }
+    const u32 c = wave % 2 * 32 + j;
+    const float bias = (r.bias && run.block != ~0u && c < width) ? r.bias[(u64)run.block * r.cols + col0 + c] : 0.0f;
 #pragma unroll
-    for (u32 n = 0; n < S::kN; ++n) {
-        const u32 c = n0 + 32 * n + j;
-        const float bias = (r.bias && run.block != ~0u && c < width) ? r.bias[(u64)run.block * r.cols + col0 + c] : 0.0f;
-#pragma unroll
-        for (u32 m = 0; m < S::kM; ++m)
-#pragma unroll
-            for (u32 v = 0; v < 16; ++v) {
-                const u32 row = m0 + 32 * m + row_of(v, hi);
-                if (row >= height || c >= width) continue;
-                float y = acc[m][n][v] + bias;
-                if (r.relu) y = y < 0.0f ? 0.0f : y;              // NaN stays
-                if (GATE == 1 && run.block != ~0u) {
-                    const float x = to_f32(static_cast<const T *>(r.gate)[(u64)(row0 + row) * r.ldgate + col0 + c]);
-                    y = x <= 0.0f ? 0.0f : y;
-                }
-                if (GATE == 2 && run.block != ~0u) {
-                    const u64 at = (u64)(row0 + row) * r.ldgate + col0 + c;
-                    const bool pass = static_cast<const signed char *>(r.gate)[at] > 0 || r.gate_scale[at / 32] == 255;
-                    y = pass ? y : 0.0f;
-                }
-                out[(u64)row * r.ldo + c] = (T)y;
-            }
+    for (u32 v = 0; v < 16; ++v) {
+        const u32 row = wave / 2 * 32 + row_of(v, hi);
+        if (row >= height || c >= width) continue;
+        float y = acc[v] + bias;
+        if (r.relu) y = y < 0.0f ? 0.0f : y;              // NaN stays
+        if (GATE == 1 && run.block != ~0u) {
+            const float x = to_f32(static_cast<const T *>(r.gate)[(u64)(row0 + row) * r.ldgate + col0 + c]);
+            y = x <= 0.0f ? 0.0f : y;
+        }
+        if (GATE == 2 && run.block != ~0u) {
+            const u64 at = (u64)(row0 + row) * r.ldgate + col0 + c;
+            const bool pass = static_cast<const signed char *>(r.gate)[at] > 0 || r.gate_scale[at / 32] == 255;
+            y = pass ? y : 0.0f;
+        }
+        out[(u64)row * r.ldo + c] = (T)y;
     }
 }
 
 // ---- sums over the rows of a block
 
 // KIND: 0 no x (db alone), 1 values, 2 codes
-template <class T, u32 TM, u32 TN, u32 KIND>
-__global__ __launch_bounds__(256, 2) void sums_kernel(const SumsArgs r)
+template <class T, u32 KIND>
+__global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
 {
-    using S = Split<TM, TN>;
-    __shared__ __align__(16) float lds[2 * kStep * (pitch_of(TM) + pitch_of(TN))];
+    __shared__ __align__(16) float lds[4 * kStep * pitch_of(kTile)];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
     const u32 pairs = r.n_tiles * r.k_tiles, t = tile / pairs, pair = tile - t * pairs;
-    const u32 n0 = pair / r.k_tiles * TM, k0 = pair % r.k_tiles * TN;
+    const u32 n0 = pair / r.k_tiles * kTile, k0 = pair % r.k_tiles * kTile;
     const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, t);
     if (!run.found) return;
     const u32 row0 = run_row(run, run.local), count = run_row(run, run.local + 1) - row0;
-    const u32 height = r.n - n0 < TM ? r.n - n0 : TM, width = r.k - k0 < TN ? r.k - k0 : TN;
+    const u32 height = r.n - n0 < kTile ? r.n - n0 : kTile, width = r.k - k0 < kTile ? r.k - k0 : kTile;
     const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 31, hi = lane / 32;
-    f32x16 acc[S::kM][S::kN] = {};
+    f32x16 acc = {};
     float bias = 0.0f;
     if (count > 0) {
-        Across<T, TM> a{static_cast<const T *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, {}};
+        Across<T, kTile> a{static_cast<const T *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, {}};
         // thread m sums column m of the staged dy
-        const bool sums_db = r.db && k0 == 0 && threadIdx.x < TM;
+        const bool sums_db = r.db && k0 == 0 && threadIdx.x < kTile;
         auto each = [&](const float *la) {
             if (!sums_db) return;
 #pragma unroll
-            for (u32 s = 0; s < kStep; ++s) bias += la[s * pitch_of(TM) + threadIdx.x];
+            for (u32 s = 0; s < kStep; ++s) bias += la[s * pitch_of(kTile) + threadIdx.x];
         };
         if constexpr (KIND == 2) {
             const u32 kp = (r.k + 31) / 32 * 32;
-            Across8<TN> b{reinterpret_cast<const u32 *>(static_cast<const signed char *>(r.x) + (u64)row0 * kp + k0),
+            Across8<kTile> b{reinterpret_cast<const u32 *>(static_cast<const signed char *>(r.x) + (u64)row0 * kp + k0),
                           r.scale + ((u64)row0 * kp + k0) / 32, kp, kp - k0, count, {}, {}};
-            tile_product<TM, TN>(a, b, count, lds, acc, each);
+            tile_product(a, b, count, lds, acc, each);
         } else {
-            Across<T, TN> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)row0 * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
+            Across<T, kTile> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)row0 * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
                             count, {}};
-            tile_product<TM, TN>(a, b, count, lds, acc, each);
+            tile_product(a, b, count, lds, acc, each);
         }
     }
     // a block with one run has its result here; otherwise the run's partial sums
@@ -289,18 +267,13 @@ __global__ __launch_bounds__(256, 2) void sums_kernel(const SumsArgs r)
     if (whole && dw) dw += (u64)run.block * r.n * r.k;
     if (whole && db) db += (u64)run.block * r.n;
     if (r.dw) {
-        const u32 mw = wave / S::kCols * (S::kM * 32), nw = wave % S::kCols * (S::kN * 32) + j;
+        const u32 col = wave % 2 * 32 + j;
 #pragma unroll
-        for (u32 n = 0; n < S::kN; ++n)
-#pragma unroll
-            for (u32 m = 0; m < S::kM; ++m)
-#pragma unroll
-                for (u32 v = 0; v < 16; ++v) {
-                    const u32 row = mw + 32 * m + row_of(v, hi), col = nw + 32 * n;
-                    if (row >= height || col >= width) continue;
-                    const u64 at = r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col;
-                    dw[at] = acc[m][n][v];
-                }
+        for (u32 v = 0; v < 16; ++v) {
+            const u32 row = wave / 2 * 32 + row_of(v, hi);
+            if (row >= height || col >= width) continue;
+            dw[r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col] = acc[v];
+        }
     }
     if (r.db && k0 == 0 && threadIdx.x < height) db[n0 + threadIdx.x] = bias;
 }
@@ -349,22 +322,15 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
     dst[i < size ? (u64)block * size + i : (u64)block * n + (i - size)] = sum;
 }
 
-u32 tile_width(u32 cols) { return cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 96 ? 96 : 128; }
-
-template <class T, u32 TN, bool ACROSS, u32 GATE>
-void rows_go(const RowsArgs &r, hipStream_t stream)
+template <class T, bool ACROSS>
+hipError_t rows_go(RowsArgs r, u32 gate, hipStream_t stream)
 {
-    hipLaunchKernelGGL((rows_kernel<T, TN, ACROSS, GATE>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
-}
-template <class T, bool ACROSS, u32 GATE>
-void rows_width(const RowsArgs &r, hipStream_t stream)
-{
-    switch (tile_width(r.cols)) {
-    case 32: return rows_go<T, 32, ACROSS, GATE>(r, stream);
-    case 64: return rows_go<T, 64, ACROSS, GATE>(r, stream);
-    case 96: return rows_go<T, 96, ACROSS, GATE>(r, stream);
-    default: return rows_go<T, 128, ACROSS, GATE>(r, stream);
-    }
+    r.col_tiles = (r.cols + kTile - 1) / kTile;
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, kTile, true) * r.col_tiles);
+    if (gate == 0) hipLaunchKernelGGL((rows_kernel<T, ACROSS, 0>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+    else if (gate == 1) hipLaunchKernelGGL((rows_kernel<T, ACROSS, 1>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+    else hipLaunchKernelGGL((rows_kernel<T, ACROSS, 2>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+    return hipGetLastError();
 }
 template <class T>
 hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
@@ -380,45 +346,32 @@ hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
     if (few_rows_fit(r, wide)) return launch_few_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
     if (narrow_rows_fit(r)) return launch_narrow_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
     if (wide) return launch_wide_rows(r, across, stream);
-    const u32 tn = tile_width(r.cols);
-    r.col_tiles = (r.cols + tn - 1) / tn;
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, 128, true) * r.col_tiles);
     const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
-    if (across) gate == 0 ? rows_width<T, true, 0>(r, stream) : gate == 1 ? rows_width<T, true, 1>(r, stream) : rows_width<T, true, 2>(r, stream);
-    else gate == 0 ? rows_width<T, false, 0>(r, stream) : gate == 1 ? rows_width<T, false, 1>(r, stream) : rows_width<T, false, 2>(r, stream);
-    return hipGetLastError();
+    return across ? rows_go<T, true>(r, gate, stream) : rows_go<T, false>(r, gate, stream);
 }
 
-// rows of a run of the sums over rows: about 1024 workgroups in all (four a compute unit), no run under 256 rows
+// Rows of a run of the sums over rows: runs of about equal work for all compute units, and no more, for their partial sums have to
+// be written and read.
 u32 rows_of_run(const lmk_gs_linear &l)
 {
-    const u64 pairs = (u64)((l.n + 127) / 128) * ((l.k + tile_width(l.k) - 1) / tile_width(l.k));
-    u64 per = ((u64)l.rows * pairs + 1023) / 1024;
-    per = (per + kStep - 1) / kStep * kStep;
-    return (u32)(per < 256 ? 256 : per);
+    const u32 side = l.dtype == LMK_GS_F32 ? kTile : wide_sums_side(l.n, l.k);
+    const u64 pairs = (u64)((l.n + side - 1) / side) * ((l.k + side - 1) / side);
+    const u64 at_once = side == kTile ? 1024 : side == 128 ? 512 : 512;
+    u64 per = ((u64)l.rows * pairs + at_once - 1) / at_once;
+    per = (per + 63) / 64 * 64;
+    return (u32)(per < 128 ? 128 : per);
 }
 
-template <class T, u32 TN>
-void sums_go(const SumsArgs &r, u32 kind, hipStream_t stream)
-{
-    if (kind == 2) hipLaunchKernelGGL((sums_kernel<T, 128, TN, 2>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
-    else if (kind == 1) hipLaunchKernelGGL((sums_kernel<T, 128, TN, 1>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
-    else hipLaunchKernelGGL((sums_kernel<T, 128, TN, 0>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
-}
 template <class T>
 hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 {
     if (std::is_same<T, __bf16>::value && kind != 0 && wide_sums_fit(r)) return launch_wide_sums(r, stream);
-    const u32 tn = kind == 0 ? 32 : tile_width(r.k);
-    r.n_tiles = (r.n + 127) / 128;
-    r.k_tiles = kind == 0 ? 1 : (r.k + tn - 1) / tn;
+    r.n_tiles = (r.n + kTile - 1) / kTile;
+    r.k_tiles = kind == 0 ? 1 : (r.k + kTile - 1) / kTile;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, r.per, false) * r.n_tiles * r.k_tiles);
-    switch (tn) {
-    case 32: sums_go<T, 32>(r, kind, stream); break;
-    case 64: sums_go<T, 64>(r, kind, stream); break;
-    case 96: sums_go<T, 96>(r, kind, stream); break;
-    default: sums_go<T, 128>(r, kind, stream); break;
-    }
+    if (kind == 2) hipLaunchKernelGGL((sums_kernel<T, 2>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+    else if (kind == 1) hipLaunchKernelGGL((sums_kernel<T, 1>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
+    else hipLaunchKernelGGL((sums_kernel<T, 0>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
     return hipGetLastError();
 }
 
@@ -426,8 +379,8 @@ hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 
 bool grouped_linear_fits(const lmk_gs_linear &l)
 {
-    const u64 runs = max_runs(l.rows, l.blocks, 128, true);
-    const u64 pairs = (u64)((l.n + 127) / 128) * ((l.k + 31) / 32);
+    const u64 runs = max_runs(l.rows, l.blocks, 64, true);
+    const u64 pairs = (u64)((l.n + kTile - 1) / kTile) * ((l.k + kTile - 1) / kTile);
     const u64 widest = l.n > l.k ? l.n : l.k;
     return runs * ((widest + 31) / 32) < 1ull << 31 && max_runs(l.rows, l.blocks, rows_of_run(l), false) * pairs < 1ull << 31 && max_runs(l.rows, l.blocks, 64, false) < 1ull << 30 &&
            (((u64)l.n * l.k + l.n + 255) / 256) * l.blocks < 1ull << 31;

@@ -476,6 +476,8 @@ hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
     return gate == 0 ? wide_shape<false, 0>(r, stream) : gate == 1 ? wide_shape<false, 1>(r, stream) : wide_shape<false, 2>(r, stream);
 }
 
+u32 wide_sums_side(u32 n, u32 k) { return n > 128 && k > 128 ? 256 : 128; }
+
 bool wide_sums_fit(const SumsArgs &r)
 {
     return r.n % 8 == 0 && r.k % 8 == 0 && r.dw && reinterpret_cast<uintptr_t>(r.dw) % 16 == 0 && sixteen(r.dy, r.lddy) &&
@@ -484,7 +486,7 @@ bool wide_sums_fit(const SumsArgs &r)
 
 hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream)
 {
-    if (r.n > 128 && r.k > 128) return wide_sums_go<256, 256, 2, 4>(r, r.scale != nullptr, stream);
+    if (wide_sums_side(r.n, r.k) == 256) return wide_sums_go<256, 256, 2, 4>(r, r.scale != nullptr, stream);
     return wide_sums_go<128, 128, 2, 2>(r, r.scale != nullptr, stream);
 }
 

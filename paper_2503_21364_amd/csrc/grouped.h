@@ -39,31 +39,24 @@ __device__ __forceinline__ void store4(__bf16 *p, f32x4 v)
 
 // The rows a workgroup works on: run `local` of `per` rows of the rows begin..end of a block.
 struct RowRun {
-    u32 block, begin, end, local, runs;      // block == ~0u: rows of no block
+    u32 block, begin, end, local;            // block == ~0u: rows of no block
     bool found;
 };
 
 // Run number `t` when the runs of all blocks are counted through, in order.  Every block's rows are cut
 // into runs of `per` rows by themselves, so the boundaries of the blocks are the only thing a workgroup has to
 // look up; 64 blocks are looked at in a step (their run counts, a sum over the lanes, the lane that t falls
-// to).  OUTSIDE: the rows in front of the first block and behind the last one count as blocks too, and a block
-// without rows has no run; otherwise it has one, and rows of no block have none.  Offsets are bounded by `rows`
+// to).  The rows in front of the first block and behind the last one count as blocks too.  Offsets are bounded by `rows`
 // whatever they hold, so no run leaves the arrays.  All lanes of a wavefront take part; the result is uniform.
-template <bool OUTSIDE>
 __device__ __forceinline__ RowRun find_run(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per, u32 t)
 {
     const u32 lane = threadIdx.x & (kWave - 1);
-    const u32 segments = OUTSIDE ? blocks + 2 : blocks;
+    const u32 segments = blocks + 2;
     const auto edge = [&](u32 s, u32 &b, u32 &e) {           // rows of segment s; only requests
         b = e = 0;
         if (s >= segments) return;
-        if (OUTSIDE) {
-            b = s == 0 ? 0u : offsets[s - 1];
-            e = s == blocks + 1 ? rows : offsets[s];
-        } else {
-            b = offsets[s];
-            e = offsets[s + 1];
-        }
+        b = s == 0 ? 0u : offsets[s - 1];
+        e = s == blocks + 1 ? rows : offsets[s];
     };
     u32 before = 0, next_b, next_e;
     edge(lane, next_b, next_e);
@@ -73,8 +66,7 @@ __device__ __forceinline__ RowRun find_run(const u32 *__restrict__ offsets, u32 
         b = b < rows ? b : rows;
         e = e < rows ? e : rows;
         e = e > b ? e : b;
-        u32 count = (e - b + per - 1) / per;
-        if (!OUTSIDE && count == 0 && base + lane < segments) count = 1;
+        const u32 count = (e - b + per - 1) / per;
         const u32 upto = before + wave_scan(count);
         const u64 past = __builtin_amdgcn_ballot_w64(upto > t);
         if (past != 0ull) {
@@ -82,10 +74,9 @@ __device__ __forceinline__ RowRun find_run(const u32 *__restrict__ offsets, u32 
             RowRun r;
             r.begin = (u32)__builtin_amdgcn_readlane((int)b, at);
             r.end = (u32)__builtin_amdgcn_readlane((int)e, at);
-            r.runs = (u32)__builtin_amdgcn_readlane((int)count, at);
-            r.local = t - ((u32)__builtin_amdgcn_readlane((int)upto, at) - r.runs);
+            r.local = t - ((u32)__builtin_amdgcn_readlane((int)upto, at) - (u32)__builtin_amdgcn_readlane((int)count, at));
             const u32 seg = base + (u32)at;
-            r.block = !OUTSIDE ? seg : (seg == 0 || seg == blocks + 1 ? ~0u : seg - 1);
+            r.block = seg == 0 || seg == blocks + 1 ? ~0u : seg - 1;
             r.found = true;
             return r;
         }
@@ -96,22 +87,177 @@ __device__ __forceinline__ RowRun find_run(const u32 *__restrict__ offsets, u32 
     return none;
 }
 
-// First row of run `local` of a block whose rows are shared out evenly over its runs (the sums over rows, whose runs need not
-// be full ones); run.runs: the end.
-__device__ __forceinline__ u32 run_row(const RowRun &run, u32 local)
+// what is the same in all lanes, in scalar registers
+__device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ u64 uniform64(u64 v) { return (u64)uniform((u32)(v >> 32)) << 32 | uniform((u32)v); }
+
+// The same value, of which the compiler knows nothing: what is computed from it inside a loop is not kept in registers across it.
+__device__ __forceinline__ u32 afresh(u32 v)
 {
-    return run.begin + (u32)((u64)(run.end - run.begin) * local / run.runs);
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// ---- sums over the rows of blocks, in two arrangements.
+// By slices: the rows of all blocks are cut into slices of `per` rows, whatever the blocks' lengths are, and the workgroups of a
+// slice sum it block after block; a run is where a slice and a block meet.  Every workgroup has the same number of rows.
+// By blocks: every block is cut into as many runs of at most `per` rows as it takes, of equal length; a workgroup has one run.
+// A block of one run has its result there.  Otherwise run r of block g is set r + g + (first row of g) / per of the partial sums,
+// rows counted from the first block's; no two runs have the same, in either arrangement (a block's rows / per, rounded up, is at
+// most one more than what the first row of the next one adds), and join_kernel adds a block's sets in their order.
+struct RowSlices {
+    const u32 *offsets;
+    u32 blocks, rows, per;      // per: rows of a slice
+    u32 front, back;            // first row of the first block, end of the last one
+
+    __device__ __forceinline__ void init(const u32 *offsets_, u32 blocks_, u32 rows_, u32 per_)
+    {
+        offsets = offsets_;
+        blocks = blocks_;
+        rows = rows_;
+        per = per_;
+        front = offsets[0] < rows ? offsets[0] : rows;
+        back = offsets[blocks] < rows ? offsets[blocks] : rows;
+        back = back > front ? back : front;
+    }
+    __device__ __forceinline__ void block(u32 g, u32 &b, u32 &e) const
+    {
+        b = offsets[g] < rows ? offsets[g] : rows;
+        e = offsets[g + 1] < rows ? offsets[g + 1] : rows;
+        e = e > b ? e : b;
+    }
+    __device__ __forceinline__ u32 edge(u32 s) const { return back - front > s * per ? front + s * per : back; }
+    __device__ __forceinline__ u32 slice_of(u32 row) const { return row > front ? (row - front) / per : 0u; }
+};
+
+// The runs of slice s, one after the other; all lanes of a wavefront take part, the results are uniform.  A block without rows
+// belongs to the slice it lies in, as a run of no rows.
+struct SliceRuns {
+    RowSlices all;
+    u32 s, s0, s1, g;
+    bool last;                  // of the slices
+    u32 block, row, count;      // of the present run
+    bool whole;                 // the block has no other
+
+    __device__ __forceinline__ void init(const u32 *offsets, u32 blocks, u32 rows, u32 per, u32 slices, u32 s_)
+    {
+        all.init(offsets, blocks, rows, per);
+        s = s_;
+        last = s + 1 == slices;
+        all.front = uniform(all.front);
+        all.back = uniform(all.back);
+        s0 = all.edge(s);
+        s1 = all.edge(s + 1);
+        const u32 lane = threadIdx.x & (kWave - 1);
+        for (g = 0; g < blocks; g += kWave) {
+            u32 b = 0, e = 0;
+            if (g + lane < blocks) all.block(g + lane, b, e);
+            const u64 hit = __builtin_amdgcn_ballot_w64(g + lane < blocks && (e > s0 || (e == b && b >= s0)));
+            if (hit != 0ull) {
+                g += (u32)__builtin_ctzll(hit);
+                break;
+            }
+        }
+    }
+    __device__ __forceinline__ bool next()
+    {
+        for (; g < all.blocks; ++g) {
+            u32 b, e;
+            all.block(g, b, e);
+            b = uniform(b);
+            e = uniform(e);
+            if (b == e) {
+                if (b >= s1 && !last) return false;
+                if (b < s0) continue;
+                block = g++;
+                row = b;
+                count = 0;
+                return whole = true;
+            }
+            if (b >= s1) return false;
+            row = b > s0 ? b : s0;
+            const u32 end = e < s1 ? e : s1;
+            if (end <= row) continue;
+            count = end - row;
+            whole = b >= s0 && e <= s1;
+            block = g++;
+            return true;
+        }
+        return false;
+    }
+    __device__ __forceinline__ u32 partial() const { return s + block; }
+};
+
+// Run `t` (number of its set) by blocks: looked up by 64 blocks at a time.
+struct BlockRun {
+    u32 block, row, count, set;
+    bool whole;
+
+    __device__ __forceinline__ bool find(const u32 *offsets, u32 blocks, u32 rows, u32 per, u32 t)
+    {
+        RowSlices all;
+        all.init(offsets, blocks, rows, per);
+        const u32 lane = threadIdx.x & (kWave - 1);
+        for (u32 base = 0; base < blocks; base += kWave) {
+            const u32 g = base + lane;
+            u32 b = 0, e = 0, first = ~0u, runs = 0;
+            if (g < blocks) {
+                all.block(g, b, e);
+                runs = (e - b + per - 1) / per;
+                runs = runs ? runs : 1u;
+                first = g + all.slice_of(b);
+            }
+            const u64 hit = __builtin_amdgcn_ballot_w64(first <= t && t - first < runs);
+            if (hit == 0ull) continue;
+            const int at = __builtin_ctzll(hit);
+            const u32 begin = (u32)__builtin_amdgcn_readlane((int)b, at), length = (u32)__builtin_amdgcn_readlane((int)e, at) - begin;
+            const u32 n = (u32)__builtin_amdgcn_readlane((int)runs, at), r = t - (u32)__builtin_amdgcn_readlane((int)first, at);
+            // equal lengths: the first `longer` runs have one row more
+            const u32 share = length / n, longer = length - share * n;
+            block = base + (u32)at;
+            row = begin + r * share + (r < longer ? r : longer);
+            count = share + (r < longer ? 1u : 0u);
+            whole = n == 1;
+            set = t;
+            return true;
+        }
+        return false;
+    }
+    __device__ __forceinline__ u32 partial() const { return set; }
+};
+
+// Number of slices (host) for tiles that `pairs` workgroups a slice sum: enough for `slots` workgroups at once and no fewer in the
+// last turn than need be; every slice more costs the bytes of a set of partial sums twice.
+inline u32 slices_of(u32 rows, u64 pairs, u32 slots, double row_us, u64 sums)
+{
+    const double slice_us = (double)sums * 8 / 4e6;
+    u32 best = 1;
+    double least = 0;
+    for (u32 turns = 0; turns <= 4; ++turns) {
+        u64 n = turns == 0 ? 1 : (u64)turns * slots / pairs;
+        const u64 most = rows / 64 + 1;
+        n = n < most ? n : most;
+        if (n == 0) continue;
+        const double us = (double)((n * pairs + slots - 1) / slots) * ((double)rows / (double)n) * row_us + (double)(n - 1) * slice_us;
+        if (turns == 0 || us < least) {
+            least = us;
+            best = (u32)n;
+        }
+    }
+    return best;
+}
+// rows of each of `slices` slices: s * per stays below 2^32
+inline u32 rows_of_slice(u32 rows, u32 slices)
+{
+    const u32 per = (rows + slices - 1) / slices;
+    return per < 64 ? 64 : per;
 }
 
 // Upper bound of the number of runs (host): every block can end with a run that is not full.
-inline u64 max_runs(u32 rows, u32 blocks, u32 per, bool outside)
+inline u64 max_runs(u32 rows, u32 blocks, u32 per)
 {
-    const u64 full = rows / per;
-    if (outside) {
-        const u64 all = full + blocks + 2;
-        return all < rows ? all : rows;
-    }
-    return full + blocks;
+    const u64 all = (u64)(rows / per) + blocks + 2;
+    return all < rows ? all : rows;
 }
 
 // ---- 8 bits: 32 values share a power of two

@@ -38,7 +38,7 @@ __global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const Rows
     constexpr u32 kWaves = 8, kC = NT / 16, V = ACROSS ? 4 : 16 / sizeof(T), kAhead = NT == 64 ? 2 : 4;
     __shared__ float part[kWaves][kRows][NT + 1];
     const u32 row_tile = blockIdx.x / r.col_tiles, col0 = (blockIdx.x - row_tile * r.col_tiles) * NT;
-    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, kRows, row_tile);
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, kRows, row_tile);
     if (!run.found) return;
     const u32 row0 = run.begin + run.local * kRows;
     const u32 height = run.end - row0 < kRows ? run.end - row0 : kRows;
@@ -110,7 +110,7 @@ template <class T, u32 NT, bool ACROSS, bool WHOLE, u32 GATE>
 hipError_t few_go(RowsArgs r, hipStream_t stream)
 {
     r.col_tiles = (r.cols + NT - 1) / NT;
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, kRows, true) * r.col_tiles);
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, kRows) * r.col_tiles);
     hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, WHOLE, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
     return hipGetLastError();
 }
@@ -121,7 +121,7 @@ hipError_t few_width(const RowsArgs &r, hipStream_t stream)
     const bool whole = r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
     // 64 columns make whole lines where columns are contiguous and read x once for four results; 16 where that leaves
     // compute units without work
-    if (max_runs(r.rows, r.blocks, kRows, true) * ((r.cols + 63) / 64) >= (ACROSS ? 64 : 256))
+    if (max_runs(r.rows, r.blocks, kRows) * ((r.cols + 63) / 64) >= (ACROSS ? 64 : 256))
         return whole ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
     return whole ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
 }

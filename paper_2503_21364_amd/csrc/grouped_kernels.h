@@ -40,8 +40,8 @@ struct SumsArgs {
     u32 blocks, rows, n, k;
     float *dw, *db;             // results, either may be NULL
     u32 in_major;
-    float *part;                // run t: n k sums of dw, then n of db
-    u32 per;                    // rows of a run
+    float *part;                // partial sums: n k of dw, then n of db each
+    u32 slices, per;            // of the rows, and rows of each
     u32 tiles, n_tiles, k_tiles;
 };
 
@@ -61,7 +61,7 @@ struct BackwardArgs {
     u64 lddx;
     float *dw, *db;
     float *part;                // as SumsArgs
-    u32 per, runs;              // rows of a run, upper bound of the runs' number
+    u32 runs, per;              // sets of partial sums, rows of a run
     u32 shared;                 // floats of LDS of the weights
 };
 
@@ -82,7 +82,7 @@ bool narrow_rows_fit(const RowsArgs &r);
 hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream);
 
 bool narrow_backward_fits(const BackwardArgs &r, bool codes);
-u32 narrow_backward_rows(u32 rows, u32 blocks, u32 n, u32 k);
+u32 narrow_backward_slots(u32 n, u32 k);      // workgroups at once
 hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream);
 
 // bfloat16 whose rows start at 16-byte boundaries

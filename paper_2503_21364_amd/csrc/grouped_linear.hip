@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256, 4) void rows_kernel(const RowsArgs r)
     __shared__ __align__(16) float lds[4 * kStep * pitch_of(kTile)];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
     const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * kTile;
-    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, kTile, row_tile);
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, kTile, row_tile);
     if (!run.found) return;
     const u32 row0 = run.begin + run.local * kTile;
     const u32 height = run.end - row0 < kTile ? run.end - row0 : kTile;
@@ -231,102 +231,98 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
 {
     __shared__ __align__(16) float lds[4 * kStep * pitch_of(kTile)];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
-    const u32 pairs = r.n_tiles * r.k_tiles, t = tile / pairs, pair = tile - t * pairs;
+    const u32 pairs = r.n_tiles * r.k_tiles, slice = tile / pairs, pair = tile - slice * pairs;
     const u32 n0 = pair / r.k_tiles * kTile, k0 = pair % r.k_tiles * kTile;
-    const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, t);
-    if (!run.found) return;
-    const u32 row0 = run_row(run, run.local), count = run_row(run, run.local + 1) - row0;
     const u32 height = r.n - n0 < kTile ? r.n - n0 : kTile, width = r.k - k0 < kTile ? r.k - k0 : kTile;
     const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 31, hi = lane / 32;
-    f32x16 acc = {};
-    float bias = 0.0f;
-    if (count > 0) {
-        Across<T, kTile> a{static_cast<const T *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, {}};
-        // thread m sums column m of the staged dy
-        const bool sums_db = r.db && k0 == 0 && threadIdx.x < kTile;
-        auto each = [&](const float *la) {
-            if (!sums_db) return;
+    SliceRuns run;
+    run.init(r.offsets, r.blocks, r.rows, r.per, r.slices, slice);
+    while (run.next()) {
+        f32x16 acc = {};
+        float bias = 0.0f;
+        if (run.count > 0) {
+            __syncthreads();                    // the run in front of this one is out of LDS
+            Across<T, kTile> a{static_cast<const T *>(r.dy) + (u64)run.row * r.lddy + n0, r.lddy, height, run.count, {}};
+            // thread m sums column m of the staged dy
+            const bool sums_db = r.db && k0 == 0 && threadIdx.x < kTile;
+            auto each = [&](const float *la) {
+                if (!sums_db) return;
 #pragma unroll
-            for (u32 s = 0; s < kStep; ++s) bias += la[s * pitch_of(kTile) + threadIdx.x];
-        };
-        if constexpr (KIND == 2) {
-            const u32 kp = (r.k + 31) / 32 * 32;
-            Across8<kTile> b{reinterpret_cast<const u32 *>(static_cast<const signed char *>(r.x) + (u64)row0 * kp + k0),
-                          r.scale + ((u64)row0 * kp + k0) / 32, kp, kp - k0, count, {}, {}};
-            tile_product(a, b, count, lds, acc, each);
-        } else {
-            Across<T, kTile> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)row0 * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
-                            count, {}};
-            tile_product(a, b, count, lds, acc, each);
+                for (u32 s = 0; s < kStep; ++s) bias += la[s * pitch_of(kTile) + threadIdx.x];
+            };
+            if constexpr (KIND == 2) {
+                const u32 kp = (r.k + 31) / 32 * 32;
+                Across8<kTile> b{reinterpret_cast<const u32 *>(static_cast<const signed char *>(r.x) + (u64)run.row * kp + k0),
+                                 r.scale + ((u64)run.row * kp + k0) / 32, kp, kp - k0, run.count, {}, {}};
+                tile_product(a, b, run.count, lds, acc, each);
+            } else {
+                Across<T, kTile> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)run.row * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
+                                   run.count, {}};
+                tile_product(a, b, run.count, lds, acc, each);
+            }
         }
-    }
-    // a block with one run has its result here; otherwise the run's partial sums
-    const bool whole = run.runs == 1;
-    float *dw = whole ? r.dw : r.part + (u64)t * ((u64)r.n * r.k + r.n);
-    float *db = whole ? r.db : r.part + (u64)t * ((u64)r.n * r.k + r.n) + (u64)r.n * r.k;
-    if (whole && dw) dw += (u64)run.block * r.n * r.k;
-    if (whole && db) db += (u64)run.block * r.n;
-    if (r.dw) {
-        const u32 col = wave % 2 * 32 + j;
+        const u64 size = (u64)r.n * r.k;
+        float *dw = run.whole ? r.dw + (u64)run.block * size : r.part + (u64)run.partial() * (size + r.n);
+        float *db = run.whole ? r.db + (u64)run.block * r.n : r.part + (u64)run.partial() * (size + r.n) + size;
+        if (r.dw) {
+            const u32 col = wave % 2 * 32 + j;
 #pragma unroll
-        for (u32 v = 0; v < 16; ++v) {
-            const u32 row = wave / 2 * 32 + row_of(v, hi);
-            if (row >= height || col >= width) continue;
-            dw[r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col] = acc[v];
+            for (u32 v = 0; v < 16; ++v) {
+                const u32 row = wave / 2 * 32 + row_of(v, hi);
+                if (row >= height || col >= width) continue;
+                dw[r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col] = acc[v];
+            }
         }
+        if (r.db && k0 == 0 && threadIdx.x < height) db[n0 + threadIdx.x] = bias;
     }
-    if (r.db && k0 == 0 && threadIdx.x < height) db[n0 + threadIdx.x] = bias;
 }
 
-// Joins the partial sums of the blocks that have several runs, in the order of the runs.
-__global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per,
+// Joins the partial sums of the blocks that have several runs, in the order of the runs.  V consecutive sums a thread, AHEAD sets on
+// their way.
+template <u32 V, u32 AHEAD>
+__global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per, bool by_blocks,
                                                    const float *__restrict__ part, u32 n, u32 k, float *__restrict__ dw,
-                                                   float *__restrict__ db, u32 pieces, u32 runs)
+                                                   float *__restrict__ db, u32 pieces)
 {
+    typedef __attribute__((ext_vector_type(V))) float vec;
     const u32 block = blockIdx.x / pieces, piece = blockIdx.x - block * pieces;
-    // runs in front of this block's
-    const u32 lane = threadIdx.x & (kWave - 1);
-    u32 before = 0, mine = 0;
-    for (u32 base = 0; base <= block; base += kWave) {
-        const u32 s = base + lane;
-        u32 count = 0;
-        if (s <= block) {
-            u32 b = offsets[s], e = offsets[s + 1];
-            b = b < rows ? b : rows;
-            e = e < rows ? e : rows;
-            e = e > b ? e : b;
-            count = (e - b + per - 1) / per;
-            count = count ? count : 1u;
-        }
-        before += wave_sum(s < block ? count : 0u);
-        mine += wave_sum(s == block ? count : 0u);
-    }
-    // one run: written where it was summed.  More runs than there is room for: the offsets do not ascend
-    if (mine <= 1 || (u64)before + mine > runs) return;
+    RowSlices all;
+    all.init(offsets, blocks, rows, per);
+    u32 b, e;
+    all.block(block, b, e);
+    if (b == e) return;
+    const u32 first = all.slice_of(b), runs = by_blocks ? (e - b + per - 1) / per : all.slice_of(e - 1) - first + 1;
+    if (runs == 1) return;                      // written where it was summed
     const u64 size = (u64)n * k, stride = size + n;
-    const u64 i = (u64)piece * 256 + threadIdx.x;
-    if (i >= stride) return;
-    float *dst = i < size ? dw : db;
-    if (!dst) return;
-    const float *p = part + (u64)before * stride + i;
-    float sum = 0.0f;
-    u32 q = 0;
-    for (; q + 8 <= mine; q += 8) {             // eight loads on their way, added in order
-        float v[8];
+    const float *p = part + (u64)(first + block) * stride;
+    const auto sum = [&](auto zero, u64 at) {
+        auto s = zero;
+        for (u32 q = 0; q < runs; q += AHEAD) {
+            decltype(zero) v[AHEAD];
 #pragma unroll
-        for (u32 i = 0; i < 8; ++i) v[i] = p[(u64)(q + i) * stride];
+            for (u32 h = 0; h < AHEAD; ++h) v[h] = load_any<decltype(zero)>(p + (u64)(q + h < runs ? q + h : q) * stride + at);
 #pragma unroll
-        for (u32 i = 0; i < 8; ++i) sum += v[i];
+            for (u32 h = 0; h < AHEAD; ++h)
+                if (q + h < runs) s += v[h];
+        }
+        return s;
+    };
+    const u64 at = ((u64)piece * 256 + threadIdx.x) * V;
+    if (V > 1 && at + V <= size) {
+        if (dw) store_any(dw + (u64)block * size + at, sum(vec{}, at));
+        return;
     }
-    for (; q < mine; ++q) sum += p[(u64)q * stride];
-    dst[i < size ? (u64)block * size + i : (u64)block * n + (i - size)] = sum;
+    for (u64 i = at; i < at + V && i < stride; ++i) {
+        if (i < size ? !dw : !db) continue;
+        (i < size ? dw[(u64)block * size + i] : db[(u64)block * n + (i - size)]) = sum(0.0f, i);
+    }
 }
 
 template <class T, bool ACROSS>
 hipError_t rows_go(RowsArgs r, u32 gate, hipStream_t stream)
 {
     r.col_tiles = (r.cols + kTile - 1) / kTile;
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, kTile, true) * r.col_tiles);
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, kTile) * r.col_tiles);
     if (gate == 0) hipLaunchKernelGGL((rows_kernel<T, ACROSS, 0>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
     else if (gate == 1) hipLaunchKernelGGL((rows_kernel<T, ACROSS, 1>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
     else hipLaunchKernelGGL((rows_kernel<T, ACROSS, 2>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
@@ -350,25 +346,13 @@ hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
     return across ? rows_go<T, true>(r, gate, stream) : rows_go<T, false>(r, gate, stream);
 }
 
-// Rows of a run of the sums over rows: runs of about equal work for all compute units, and no more, for their partial sums have to
-// be written and read.
-u32 rows_of_run(const lmk_gs_linear &l)
-{
-    const u32 side = l.dtype == LMK_GS_F32 ? kTile : wide_sums_side(l.n, l.k);
-    const u64 pairs = (u64)((l.n + side - 1) / side) * ((l.k + side - 1) / side);
-    const u64 at_once = side == kTile ? 1024 : side == 128 ? 512 : 512;
-    u64 per = ((u64)l.rows * pairs + at_once - 1) / at_once;
-    per = (per + 63) / 64 * 64;
-    return (u32)(per < 128 ? 128 : per);
-}
-
 template <class T>
 hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 {
     if (std::is_same<T, __bf16>::value && kind != 0 && wide_sums_fit(r)) return launch_wide_sums(r, stream);
     r.n_tiles = (r.n + kTile - 1) / kTile;
     r.k_tiles = kind == 0 ? 1 : (r.k + kTile - 1) / kTile;
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, r.per, false) * r.n_tiles * r.k_tiles);
+    r.tiles = (u32)((u64)r.slices * r.n_tiles * r.k_tiles);
     if (kind == 2) hipLaunchKernelGGL((sums_kernel<T, 2>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
     else if (kind == 1) hipLaunchKernelGGL((sums_kernel<T, 1>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
     else hipLaunchKernelGGL((sums_kernel<T, 0>), dim3(r.tiles), dim3(kThreads), 0, stream, r);
@@ -377,24 +361,48 @@ hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 
 }  // namespace
 
+// Small matrices in float32 take one pass over the rows for all three gradients; the rest of the rule (strides) is the
+// arrays', and what does not fit takes the other kernels with the same slices.
+static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l.n <= 128 && l.k <= 64; }
+
+// how the sums over rows are shared out
+struct RunPlan {
+    u32 per, slices;        // rows of a run or slice; sets of partial sums, less the blocks
+};
+static RunPlan run_plan(const lmk_gs_linear &l)
+{
+    const u64 sums = (u64)l.n * l.k + l.n;
+    RunPlan p;
+    if (one_pass(l)) {
+        // a run's own costs (the weights into LDS, the sums out of registers) are those of some hundred rows: one run a workgroup,
+        // all of them at once, whole tiles for each wavefront
+        const u32 most = narrow_backward_slots(l.n, l.k), slots = most - (l.blocks < most / 2 ? l.blocks : most / 2);
+        p.per = (u32)(((u64)l.rows + slots * 64 - 1) / (slots * 64)) * 64;
+        p.per = p.per < 64 ? 64 : p.per;
+        p.slices = l.rows / p.per + 1;
+    } else {
+        // time of a row of a tile: its products at the rate that a compute unit's share of the tiles reaches
+        const bool f32 = l.dtype == LMK_GS_F32;
+        const u32 side = f32 ? kTile : wide_sums_side(l.n, l.k), slots = f32 ? 1024 : side == 256 ? 256 : 512;
+        const u64 pairs = (u64)((l.n + side - 1) / side) * ((l.k + side - 1) / side);
+        p.slices = slices_of(l.rows, pairs, slots, 2.0 * side * side * slots / (f32 ? 1e8 : 1e9), sums);
+        p.per = rows_of_slice(l.rows, p.slices);
+    }
+    return p;
+}
+
 bool grouped_linear_fits(const lmk_gs_linear &l)
 {
-    const u64 runs = max_runs(l.rows, l.blocks, 64, true);
+    const u64 runs = max_runs(l.rows, l.blocks, kTile);
     const u64 pairs = (u64)((l.n + kTile - 1) / kTile) * ((l.k + kTile - 1) / kTile);
     const u64 widest = l.n > l.k ? l.n : l.k;
-    return runs * ((widest + 31) / 32) < 1ull << 31 && max_runs(l.rows, l.blocks, rows_of_run(l), false) * pairs < 1ull << 31 && max_runs(l.rows, l.blocks, 64, false) < 1ull << 30 &&
+    return runs * ((widest + 31) / 32) < 1ull << 31 && run_plan(l).slices * pairs < 1ull << 31 && (u64)run_plan(l).slices + l.blocks < 1ull << 30 &&
            (((u64)l.n * l.k + l.n + 255) / 256) * l.blocks < 1ull << 31;
 }
 
-// Small matrices in float32 take one pass over the rows for all three gradients; the rest of the rule (strides) is the
-// arrays', and what does not fit takes the other kernels with the same runs.
-static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l.n <= 128 && l.k <= 64; }
-static u32 rows_of_partial(const lmk_gs_linear &l) { return one_pass(l) ? narrow_backward_rows(l.rows, l.blocks, l.n, l.k) : rows_of_run(l); }
-
 size_t grouped_backward_bytes(const lmk_gs_linear &l)
 {
-    // the partial sums of every run
-    return (size_t)(max_runs(l.rows, l.blocks, rows_of_partial(l), false) * ((u64)l.n * l.k + l.n) * 4);
+    return (size_t)(((u64)run_plan(l).slices + l.blocks) * ((u64)l.n * l.k + l.n) * 4);
 }
 
 hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
@@ -416,13 +424,17 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
                                    const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
                                    char *workspace, hipStream_t stream)
 {
-    const u32 kp = (l.k + 31) / 32 * 32, per = rows_of_partial(l);
-    const u64 runs = max_runs(l.rows, l.blocks, per, false);
-    const u32 pieces = (u32)(((u64)l.n * l.k + l.n + 255) / 256);
+    const u32 kp = (l.k + 31) / 32 * 32;
+    const RunPlan plan = run_plan(l);
     float *part = reinterpret_cast<float *>(workspace);
-    const auto join = [&]() {
-        hipLaunchKernelGGL(join_kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, per, part, l.n, l.k,
-                           out.dw, out.db, pieces, (u32)runs);
+    const auto join = [&](bool by_blocks) {
+        // few sums are many sets each, and latency; many are bytes
+        const u64 stride = (u64)l.n * l.k + l.n;
+        const bool many = stride * l.blocks >= 1u << 21;
+        const u32 pieces = (u32)((stride + (many ? 1023 : 255)) / (many ? 1024 : 256));
+        auto kernel = many ? join_kernel<4, 4> : join_kernel<1, 8>;
+        hipLaunchKernelGGL(kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, plan.per, by_blocks, part,
+                           l.n, l.k, out.dw, out.db, pieces);
         return hipGetLastError();
     };
     if (one_pass(l) && (out.dw || out.db)) {
@@ -437,10 +449,10 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
         r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.n = l.n; r.k = l.k;
         r.in_major = l.in_major; r.gate = gate;
         r.dx = static_cast<float *>(out.dx); r.lddx = out.lddx; r.dw = out.dw; r.db = out.db;
-        r.part = part; r.per = per; r.runs = (u32)runs;
+        r.part = part; r.runs = plan.slices + l.blocks; r.per = plan.per;
         if (narrow_backward_fits(r, kept != nullptr)) {
             const hipError_t e = launch_narrow_backward(r, kept != nullptr, stream);
-            return e == hipSuccess ? join() : e;
+            return e == hipSuccess ? join(true) : e;
         }
     }
     if (out.dx && l.rows > 0) {
@@ -466,11 +478,12 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
     r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.n = l.n; r.k = l.k;
     r.dw = out.dw; r.db = out.db; r.in_major = l.in_major;
     r.part = part;
-    r.per = per;
+    r.slices = plan.slices;
+    r.per = plan.per;
     const u32 kind = !out.dw ? 0 : kept ? 2 : 1;
     hipError_t e = l.dtype == LMK_GS_F32 ? sums_as<float>(r, kind, stream) : sums_as<__bf16>(r, kind, stream);
     if (e != hipSuccess) return e;
-    return join();
+    return join(false);
 }
 
 }  // namespace lmk

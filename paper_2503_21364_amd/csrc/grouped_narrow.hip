@@ -18,7 +18,7 @@ template <class T, u32 CT, u32 PIECES, bool KEEP, u32 GATE>
 __global__ __launch_bounds__(256, PIECES <= 4 ? 4 : 3) void narrow_rows_kernel(const RowsArgs r)
 {
     extern __shared__ __align__(16) float narrow_lds[];
-    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
     if (!run.found) return;
     const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), j = lane & 15, q = lane >> 4;
     const u32 row0 = run.begin + run.local * r.per;
@@ -141,7 +141,7 @@ hipError_t narrow_go(RowsArgs r, hipStream_t stream)
                   : gate == 1 ? narrow_rows_kernel<T, CT, PIECES, false, 1> : narrow_rows_kernel<T, CT, PIECES, false, 2>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3((u32)max_runs(r.rows, r.blocks, r.per, true)), dim3(256), lds, stream, r);
+    hipLaunchKernelGGL(kernel, dim3((u32)max_runs(r.rows, r.blocks, r.per)), dim3(256), lds, stream, r);
     return hipGetLastError();
 }
 template <class T, u32 CT>

@@ -63,7 +63,7 @@ template <u32 CN, u32 CK, bool CODES>
 __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel(const BackwardArgs r)
 {
     extern __shared__ __align__(16) float narrow_lds[];
-    const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave)), j = lane & 15, q = lane >> 4;
+    const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     if (blockIdx.x >= r.runs) {
         // rows in front of the first block and behind the last one
         u32 front = r.offsets[0], back = r.offsets[r.blocks];
@@ -74,11 +74,11 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
             for (u32 c = threadIdx.x; c < r.k; c += 256) r.dx[(u64)(i < front ? i : back + (i - front)) * r.lddx + c] = 0.0f;
         return;
     }
-    const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
-    if (!run.found) return;
-    const u32 row0 = run_row(run, run.local), height = run_row(run, run.local + 1) - row0;
     const u32 pn = pitch_of(r.n), pk = pitch_of(r.k), kp = (r.k + 31) / 32 * 32, steps = (r.n + 3) / 4;
     float *lw = narrow_lds, *ly = lw + r.shared + wave * kTileRows * (pn + pk), *lx = ly + kTileRows * pn;
+    BlockRun run;
+    if (!run.find(r.offsets, r.blocks, r.rows, r.per, blockIdx.x)) return;
+    const u32 row0 = run.row, height = run.count, lane = threadIdx.x & (kWave - 1), j = lane & 15, q = lane >> 4;
     if (r.dx && height > 0)
         stage_weights<float, CK>(lw, r.w + (u64)run.block * r.w_block, r.ldw, r.in_major == 0, r.n, r.k);
     __syncthreads();
@@ -188,7 +188,6 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
             }
         }
     }
-    if (!r.dw && !r.db) return;
     // ---- the four wavefronts' sums, [output][input] and then db each
     constexpr u32 ps = sums_pitch(CK), part = sums_floats(CN, CK);
     __syncthreads();
@@ -202,10 +201,9 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
         if (q == 0) lb[16 * b + j] = db[b];
     }
     __syncthreads();
-    const bool whole = run.runs == 1;
     const u32 size = r.n * r.k;
-    float *to_w = whole ? r.dw + (u64)run.block * size : r.part + (u64)blockIdx.x * (size + r.n);
-    float *to_b = whole ? r.db + (u64)run.block * r.n : r.part + (u64)blockIdx.x * (size + r.n) + size;
+    float *to_w = run.whole ? r.dw + (u64)run.block * size : r.part + (u64)run.partial() * (size + r.n);
+    float *to_b = run.whole ? r.db + (u64)run.block * r.n : r.part + (u64)run.partial() * (size + r.n) + size;
     const auto joined = [&](u32 at) { return ((narrow_lds[at] + narrow_lds[part + at]) + narrow_lds[2 * part + at]) + narrow_lds[3 * part + at]; };
     if (r.dw) {
         const u32 width = r.in_major ? r.n : r.k;
@@ -256,14 +254,7 @@ bool narrow_backward_fits(const BackwardArgs &r, bool codes)
 // outputs in tiles of 16, as the kernels are built for them
 static u32 out_tiles(u32 n) { return n <= 32 ? 2 : n <= 64 ? 4 : n <= 80 ? 5 : n <= 96 ? 6 : 8; }
 
-u32 narrow_backward_rows(u32 rows, u32 blocks, u32 n, u32 k)
-{
-    // all workgroups at once, whole tiles for each of their wavefronts
-    const u32 most = 256 * resident(out_tiles(n) * ((k + 15) / 16));
-    const u32 slots = most - (blocks < most / 2 ? blocks : most / 2);
-    const u32 per = (u32)(((u64)rows + slots * 64 - 1) / (slots * 64)) * 64;
-    return per < 64 ? 64 : per;
-}
+u32 narrow_backward_slots(u32 n, u32 k) { return 256 * resident(out_tiles(n) * ((k + 15) / 16)); }
 
 hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream)
 {

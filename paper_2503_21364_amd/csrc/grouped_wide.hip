@@ -25,10 +25,6 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, u32 b
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
 }
 
-// what is the same in all lanes, in scalar registers
-__device__ __forceinline__ u32 uniform(u32 v) { return (u32)__builtin_amdgcn_readfirstlane((int)v); }
-__device__ __forceinline__ u64 uniform64(u64 v) { return (u64)uniform((u32)(v >> 32)) << 32 | uniform((u32)v); }
-
 // ---- an operand of `W` rows (columns) by kPair sum indices in LDS, 128 W bytes, filled by loads that go to LDS
 // directly (16 bytes a lane, 1 KB a wavefront, consecutive in LDS), one pair of steps after the other; what is out of range arrives as zeros.
 
@@ -209,7 +205,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
     extern __shared__ __align__(16) char wide_lds[];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
     const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * TP;
-    const RowRun run = find_run<true>(r.offsets, r.blocks, r.rows, TQ, row_tile);
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
     if (!run.found) return;
     const u32 row0 = run.begin + run.local * TQ;
     const u32 height = run.end - row0 < TQ ? run.end - row0 : TQ;
@@ -311,10 +307,10 @@ template <u32 W, u32 WAVES> struct Codes16 {
     u32x4 v[2];
     u32 e;
 
-    __device__ __forceinline__ void init(const char *codes_, const uint8_t *scale_, u32 kp_, u32 width, u32 sums, u32 lane)
+    __device__ __forceinline__ void init(const char *codes_, const uint8_t *scale_, u32 kp_, u32 width, u32 sums, u32 wave, u32 lane)
     {
-        const u32 group = threadIdx.x % (W / 32);
-        row = threadIdx.x / (W / 32);
+        const u32 thread = wave * kWave + lane, group = thread % (W / 32);
+        row = thread / (W / 32);
         kp = kp_;
         rows = sums;
         there = group * 32 < width;
@@ -356,70 +352,72 @@ template <u32 W, u32 WAVES> struct Codes16 {
     __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 h, u32 r0, u32 f) const { return across_fragment<W>(lds + h * kStep * W * 2, read, r0, f); }
 };
 
-// A tile of dw for a run of a block's rows: P = x (inputs), Q = dy (outputs).  db rides on the tiles of the first inputs: a
+// Tiles of dw over a slice of the rows: P = x (inputs), Q = dy (outputs).  db rides on the tiles of the first inputs: a
 // matrix instruction with ones in the place of x, the wavefronts along P taking turns.
 template <class S, u32 TP, u32 TQ, u32 WP, bool CODES>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
-    const u32 pairs = r.n_tiles * r.k_tiles, t = tile / pairs, pair = tile - t * pairs;
+    const u32 pairs = r.n_tiles * r.k_tiles, slice = tile / pairs, pair = tile - slice * pairs;
     const u32 n0 = pair / r.k_tiles * TQ, k0 = pair % r.k_tiles * TP;
-    const RowRun run = find_run<false>(r.offsets, r.blocks, r.rows, r.per, t);
-    if (!run.found) return;
-    const u32 row0 = run_row(run, run.local), count = run_row(run, run.local + 1) - row0;
     const u32 height = r.n - n0 < TQ ? r.n - n0 : TQ, width = r.k - k0 < TP ? r.k - k0 : TP;
-    const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     const u32 pw = wave % WP, p0 = pw * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
     const bool sums_db = r.db && k0 == 0;
-    f32x4 acc[S::kP][S::kQ] = {};
     constexpr u32 kB = (S::kQ + WP - 1) / WP;
-    f32x4 bias[kB] = {};
-    if (count > 0) {
-        lds_char *lds = (lds_char *)wide_lds;
-        const u32 steps = (count + kStep - 1) / kStep;
-        const __bf16 one = (__bf16)1.0f;
-        const bf16x8 ones = {one, one, one, one, one, one, one, one};
-        const auto add = [&](const bf16x8 (&fq)[S::kQ]) {
-            if (!sums_db) return;
+    lds_char *lds = (lds_char *)wide_lds;
+    SliceRuns run;
+    run.init(r.offsets, r.blocks, r.rows, r.per, r.slices, slice);
+    while (run.next()) {
+        const u32 lane = afresh(threadIdx.x & (kWave - 1));
+        f32x4 acc[S::kP][S::kQ] = {};
+        f32x4 bias[kB] = {};
+        if (run.count > 0) {
+            __syncthreads();                    // the run in front of this one is out of LDS
+            const u32 steps = (run.count + kStep - 1) / kStep;
+            const __bf16 one = (__bf16)1.0f;
+            const bf16x8 ones = {one, one, one, one, one, one, one, one};
+            const auto add = [&](const bf16x8 (&fq)[S::kQ]) {
+                if (!sums_db) return;
 #pragma unroll
-            for (u32 j = 0; j < S::kQ; ++j)
-                if (j % WP == pw) bias[j / WP] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fq[j], bias[j / WP], 0, 0, 0);
-        };
-        Across16<TQ, S::kWaves> q;
-        q.init(static_cast<const __bf16 *>(r.dy) + (u64)row0 * r.lddy + n0, r.lddy, height, count, wave, lane);
-        if constexpr (CODES) {
-            const u32 kp = (r.k + 31) / 32 * 32;
-            Codes16<TP, S::kWaves> p;
-            p.init(static_cast<const char *>(r.x) + (u64)row0 * kp + k0, r.scale + (u64)row0 * (kp / 32) + k0 / 32, kp, width, count, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
-        } else {
-            Across16<TP, S::kWaves> p;
-            p.init(static_cast<const __bf16 *>(r.x) + (u64)row0 * r.ldx + k0, r.ldx, width, count, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
-        }
-    }
-    // a block with one run has its result here; otherwise the run's partial sums
-    const bool whole = run.runs == 1;
-    const u64 size = (u64)r.n * r.k;
-    float *dw = whole ? r.dw + (u64)run.block * size : r.part + (u64)t * (size + r.n);
-    float *db = whole ? r.db + (u64)run.block * r.n : r.part + (u64)t * (size + r.n) + size;
-#pragma unroll
-    for (u32 j = 0; j < S::kQ; ++j) {
-        const u32 n = n0 + q0 + 16 * j + (lane & 15);
-        if (n >= r.n) continue;
-#pragma unroll
-        for (u32 i = 0; i < S::kP; ++i) {
-            const u32 k = k0 + p0 + 16 * i + 4 * (lane >> 4);
-            if (k >= r.k) continue;                     // k comes in eights
-            if (r.in_major) {
-#pragma unroll
-                for (u32 v = 0; v < 4; ++v) dw[(u64)(k + v) * r.n + n] = acc[i][j][v];
+                for (u32 j = 0; j < S::kQ; ++j)
+                    if (j % WP == pw) bias[j / WP] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fq[j], bias[j / WP], 0, 0, 0);
+            };
+            Across16<TQ, S::kWaves> q;
+            q.init(static_cast<const __bf16 *>(r.dy) + (u64)run.row * r.lddy + n0, r.lddy, height, run.count, wave, lane);
+            if constexpr (CODES) {
+                const u32 kp = (r.k + 31) / 32 * 32;
+                Codes16<TP, S::kWaves> p;
+                p.init(static_cast<const char *>(r.x) + (u64)run.row * kp + k0, r.scale + (u64)run.row * (kp / 32) + k0 / 32, kp, kp - k0,
+                       run.count, wave, lane);
+                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
             } else {
-                *reinterpret_cast<f32x4 *>(dw + (u64)n * r.k + k) = acc[i][j];
+                Across16<TP, S::kWaves> p;
+                p.init(static_cast<const __bf16 *>(r.x) + (u64)run.row * r.ldx + k0, r.ldx, width, run.count, wave, lane);
+                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
             }
         }
-        if (sums_db && j % WP == pw && lane < 16) db[n] = bias[j / WP][0];
+        const u64 size = (u64)r.n * r.k;
+        float *dw = run.whole ? r.dw + (u64)run.block * size : r.part + (u64)run.partial() * (size + r.n);
+        float *db = run.whole ? r.db + (u64)run.block * r.n : r.part + (u64)run.partial() * (size + r.n) + size;
+#pragma unroll
+        for (u32 j = 0; j < S::kQ; ++j) {
+            const u32 n = n0 + q0 + 16 * j + (lane & 15);
+            if (n >= r.n) continue;
+#pragma unroll
+            for (u32 i = 0; i < S::kP; ++i) {
+                const u32 k = k0 + p0 + 16 * i + 4 * (lane >> 4);
+                if (k >= r.k) continue;                     // k comes in eights
+                if (r.in_major) {
+#pragma unroll
+                    for (u32 v = 0; v < 4; ++v) dw[(u64)(k + v) * r.n + n] = acc[i][j][v];
+                } else {
+                    store_any(dw + (u64)n * r.k + k, acc[i][j]);
+                }
+            }
+            if (sums_db && j % WP == pw && lane < 16) db[n] = bias[j / WP][0];
+        }
     }
 }
 
@@ -430,7 +428,7 @@ hipError_t wide_go(RowsArgs r, hipStream_t stream)
 {
     using S = Shape<TP, TQ, WP, WQ>;
     r.col_tiles = (r.cols + TP - 1) / TP;
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, TQ, true) * r.col_tiles);
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, TQ) * r.col_tiles);
     auto kernel = wide_rows_kernel<S, TP, TQ, WP, ACROSS, GATE>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
     if (e != hipSuccess) return e;
@@ -440,7 +438,7 @@ hipError_t wide_go(RowsArgs r, hipStream_t stream)
 template <bool ACROSS, u32 GATE>
 hipError_t wide_shape(const RowsArgs &r, hipStream_t stream)
 {
-    if (r.cols > 128 && max_runs(r.rows, r.blocks, 256, true) * ((r.cols + 255) / 256) >= 256)
+    if (r.cols > 128 && max_runs(r.rows, r.blocks, 256) * ((r.cols + 255) / 256) >= 256)
         return wide_go<256, 256, 2, 4, ACROSS, GATE>(r, stream);
     return wide_go<128, 128, 2, 2, ACROSS, GATE>(r, stream);
 }
@@ -451,7 +449,7 @@ hipError_t wide_sums_go(SumsArgs r, bool codes, hipStream_t stream)
     using S = Shape<TP, TQ, WP, WQ>;
     r.n_tiles = (r.n + TQ - 1) / TQ;
     r.k_tiles = (r.k + TP - 1) / TP;
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, r.per, false) * r.n_tiles * r.k_tiles);
+    r.tiles = (u32)((u64)r.slices * r.n_tiles * r.k_tiles);
     auto kernel = codes ? wide_sums_kernel<S, TP, TQ, WP, true> : wide_sums_kernel<S, TP, TQ, WP, false>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
     if (e != hipSuccess) return e;
@@ -480,7 +478,7 @@ u32 wide_sums_side(u32 n, u32 k) { return n > 128 && k > 128 ? 256 : 128; }
 
 bool wide_sums_fit(const SumsArgs &r)
 {
-    return r.n % 8 == 0 && r.k % 8 == 0 && r.dw && reinterpret_cast<uintptr_t>(r.dw) % 16 == 0 && sixteen(r.dy, r.lddy) &&
+    return r.n % 8 == 0 && r.k % 8 == 0 && r.dw && sixteen(r.dy, r.lddy) &&
            (r.scale || sixteen(r.x, r.ldx));
 }
 

@@ -226,24 +226,27 @@ struct BlockRun {
     __device__ __forceinline__ u32 partial() const { return set; }
 };
 
-// Number of slices (host) for tiles that `pairs` workgroups a slice sum: enough for `slots` workgroups at once and no fewer in the
-// last turn than need be; every slice more costs the bytes of a set of partial sums twice.
-inline u32 slices_of(u32 rows, u64 pairs, u32 slots, double row_us, u64 sums)
+// Number of slices (host) for tiles that `pairs` workgroups a slice sum, `slots` of them at once: the least of what the last turn's
+// workgroups take, with a run's own costs, and what a set of partial sums more costs, its bytes written and read.
+inline u32 slices_of(u32 rows, u32 blocks, u64 pairs, u32 slots, double row_us, u64 sums)
 {
-    const double slice_us = (double)sums * 8 / 4e6;
+    constexpr double kRunUs = 6.0;
+    const double set_us = (double)sums * 8 / 4e6;
+    const u64 most = rows / 64 + 1;
     u32 best = 1;
-    double least = 0;
-    for (u32 turns = 0; turns <= 4; ++turns) {
-        u64 n = turns == 0 ? 1 : (u64)turns * slots / pairs;
-        const u64 most = rows / 64 + 1;
+    double least = -1;
+    const auto look = [&](u64 n) {
         n = n < most ? n : most;
-        if (n == 0) continue;
-        const double us = (double)((n * pairs + slots - 1) / slots) * ((double)rows / (double)n) * row_us + (double)(n - 1) * slice_us;
-        if (turns == 0 || us < least) {
+        if (n == 0) return;
+        const double turns = (double)((n * pairs + slots - 1) / slots);
+        const double us = turns * ((double)rows / (double)n * row_us + (1.0 + (double)blocks / (double)n) * kRunUs) + (double)(n - 1) * set_us;
+        if (least < 0 || us < least) {
             least = us;
             best = (u32)n;
         }
-    }
+    };
+    for (u64 n = 1; n < 4096; n *= 2) look(n);
+    for (u32 turns = 1; turns <= 4; ++turns) look((u64)turns * slots / pairs);
     return best;
 }
 // rows of each of `slices` slices: s * per stays below 2^32

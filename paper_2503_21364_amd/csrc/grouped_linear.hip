@@ -333,6 +333,7 @@ hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
 {
     const bool wide = std::is_same<T, __bf16>::value && wide_rows_fit(r, across);
     if (r.keep_codes) {
+        if (wide && !few_rows_fit(r, true) && !narrow_rows_fit(r)) return launch_wide_rows(r, across, stream);
         if (narrow_rows_fit(r)) return launch_narrow_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
         const lmk_gs_checkpoint8 keep = {reinterpret_cast<int8_t *>(r.keep_codes), r.keep_scale};
         const hipError_t e = launch_checkpoint8_pack(r.a, r.lda, r.rows, r.sums, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16,
@@ -385,7 +386,7 @@ static RunPlan run_plan(const lmk_gs_linear &l)
         const bool f32 = l.dtype == LMK_GS_F32;
         const u32 side = f32 ? kTile : wide_sums_side(l.n, l.k), slots = f32 ? 1024 : side == 256 ? 256 : 512;
         const u64 pairs = (u64)((l.n + side - 1) / side) * ((l.k + side - 1) / side);
-        p.slices = slices_of(l.rows, pairs, slots, 2.0 * side * side * slots / (f32 ? 1e8 : 1e9), sums);
+        p.slices = slices_of(l.rows, l.blocks, pairs, slots, 2.0 * side * side * slots / (f32 ? 1e8 : 1e9), sums);
         p.per = rows_of_slice(l.rows, p.slices);
     }
     return p;

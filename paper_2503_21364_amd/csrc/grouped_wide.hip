@@ -137,10 +137,10 @@ template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
 // acc[i][j] += P Q over `steps`.  LDS holds two pairs of steps.  A step's fragments are read from LDS while the step in front of
 // it is multiplied; once the second step's are with all wavefronts, the pair's part is filled again, which has the
 // time of two steps to arrive.  One meeting of the wavefronts a pair.
-// `also` sees the fragments of Q.
-template <class S, class P, class Q, class Also>
+// `also` sees the fragments of Q, `look` a pair of steps of Q in LDS.
+template <class S, class P, class Q, class Also, class Look>
 __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *lds, u32 wave, u32 p0, u32 q0,
-                                             f32x4 (&acc)[S::kP][S::kQ], Also &&also)
+                                             f32x4 (&acc)[S::kP][S::kQ], Also &&also, Look &&look)
 {
     lds_char *lp = lds, *lq = lds + 2 * S::kPartP;
     constexpr bool kDirect = P::kDirect && Q::kDirect;
@@ -178,6 +178,7 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
         for (u32 part = 0; part < 2; ++part) {
             const u32 t = t0 + 2 * part;
             if (t >= steps) break;
+            look(t / 2, lq + part * S::kPartQ);
             step(0, part, 1);
             if (t + 1 >= steps) break;
             // the next pair has arrived, and this pair's fragments have left LDS
@@ -198,13 +199,53 @@ __device__ __forceinline__ u32 pack_bf16(float a, float b)
     return (u32)__builtin_bit_cast(unsigned short, (__bf16)a) | ((u32)__builtin_bit_cast(unsigned short, (__bf16)b) << 16);
 }
 
-// GATE: 0 none, 1 values, 2 codes
+// 32 values of a row of x, a thread's, from the pair of steps that is in LDS (laid out as Along16 does) to their 8-bit form.  They
+// are read twice: held, they would cost registers that the products need.
+__device__ __forceinline__ void keep_pair(const RowsArgs &r, const lds_char *lds, u32 pair, u32 row0, u32 height, u32 thread)
+{
+    const u32 row = thread / 2, half = thread & 1, kp = (r.sums + 31) / 32 * 32, col = pair * kPair + half * 32;
+    if (row >= height || col >= kp) return;
+    const lds_char *p = lds + row * 128;
+    const u32 turned = row >> 1 & 7;
+    const auto chunk = [&](u32 c) { return *reinterpret_cast<const lds_u32x4 *>(p + (((4 * half + c) ^ turned) * 16)); };
+    u32 top = 0;
+#pragma unroll
+    for (u32 c = 0; c < 4; ++c) {
+        const u32x4 v = chunk(c);
+#pragma unroll
+        for (u32 e = 0; e < 4; ++e) {
+            const u32 lo = v[e] & 0x7fffu, hi = v[e] >> 16 & 0x7fffu;
+            top = top > lo ? top : lo;
+            top = top > hi ? top : hi;
+        }
+    }
+    const u32 scale = scale_of_max(top << 16);
+    const float inv = inverse_step(scale);
+    const u64 at = (u64)(row0 + row) * kp + col;
+#pragma unroll
+    for (u32 h = 0; h < 2; ++h) {
+        u32x4 o;
+#pragma unroll
+        for (u32 c = 0; c < 2; ++c) {
+            const u32x4 v = chunk(2 * h + c);
+#pragma unroll
+            for (u32 e = 0; e < 2; ++e)
+                o[2 * c + e] = pack_codes(code_of(__uint_as_float(v[2 * e] << 16), inv), code_of(__uint_as_float(v[2 * e] & 0xffff0000u), inv),
+                                          code_of(__uint_as_float(v[2 * e + 1] << 16), inv), code_of(__uint_as_float(v[2 * e + 1] & 0xffff0000u), inv));
+        }
+        *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(r.keep_codes) + at + 16 * h) = o;
+    }
+    r.keep_scale[at / 32] = (uint8_t)scale;
+}
+
+// GATE: 0 none, 1 values, 2 codes, 3 none, and the 8-bit form of x is written: whole lines of it, two pairs of steps of a row, by the
+// workgroups of its columns in turn
 template <class S, u32 TP, u32 TQ, u32 WP, bool ACROSS, u32 GATE>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
-    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * TP;
+    const u32 row_tile = tile / r.col_tiles, col_tile = tile - row_tile * r.col_tiles, col0 = col_tile * TP;
     const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
     if (!run.found) return;
     const u32 row0 = run.begin + run.local * TQ;
@@ -215,6 +256,17 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
     f32x4 acc[S::kP][S::kQ] = {};
     const bool inside = run.block != ~0u;
     const auto nothing = [](const bf16x8 (&)[S::kQ]) {};
+    const auto keep = [&](u32 pair, const lds_char *lds) {
+        if (GATE == 3 && pair / 2 % r.col_tiles == col_tile) keep_pair(r, lds, pair, row0, height, threadIdx.x);
+    };
+    if (GATE == 3 && !inside && col_tile == 0) {
+        const u32 kp = (r.sums + 31) / 32 * 32;
+        for (u32 i = threadIdx.x; i < height * (kp / 32); i += S::kThreads) {
+            u32x4 *p = reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(r.keep_codes) + (u64)row0 * kp) + (u64)i * 2;
+            p[0] = p[1] = u32x4{0, 0, 0, 0};
+            r.keep_scale[(u64)row0 * (kp / 32) + i] = 0;
+        }
+    }
     if (inside) {
         lds_char *lds = (lds_char *)wide_lds;
         const u32 steps = (r.sums + kStep - 1) / kStep;
@@ -224,11 +276,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
         if constexpr (ACROSS) {
             Across16<TP, S::kWaves> p;
             p.init(w + col0, r.ldw, width, r.sums, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing, keep);
         } else {
             Along16<TP, S::kWaves> p;
             p.init(w + (u64)col0 * r.ldw, r.ldw, width, r.sums, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing, keep);
         }
     }
     // Two neighbouring results exchange lanes, so that a lane has eight consecutive values of a row:
@@ -391,11 +443,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArg
                 Codes16<TP, S::kWaves> p;
                 p.init(static_cast<const char *>(r.x) + (u64)run.row * kp + k0, r.scale + (u64)run.row * (kp / 32) + k0 / 32, kp, kp - k0,
                        run.count, wave, lane);
-                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
+                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
             } else {
                 Across16<TP, S::kWaves> p;
                 p.init(static_cast<const __bf16 *>(r.x) + (u64)run.row * r.ldx + k0, r.ldx, width, run.count, wave, lane);
-                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add);
+                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
             }
         }
         const u64 size = (u64)r.n * r.k;
@@ -469,7 +521,8 @@ bool wide_rows_fit(const RowsArgs &r, bool across)
 
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
 {
-    const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
+    const u32 gate = r.keep_codes ? 3 : !r.gate ? 0 : r.gate_scale ? 2 : 1;
+    if (gate == 3) return across ? wide_shape<true, 3>(r, stream) : wide_shape<false, 3>(r, stream);
     if (across) return gate == 0 ? wide_shape<true, 0>(r, stream) : gate == 1 ? wide_shape<true, 1>(r, stream) : wide_shape<true, 2>(r, stream);
     return gate == 0 ? wide_shape<false, 0>(r, stream) : gate == 1 ? wide_shape<false, 1>(r, stream) : wide_shape<false, 2>(r, stream);
 }

@@ -25,7 +25,7 @@ struct RowsArgs {
     u32 tiles, col_tiles;
     u32 per;                    // rows of a run, where that is not fixed
     bool across;                // weights: columns contiguous, not sum indices
-    u32 *keep_codes;            // NULL, or where the 8-bit form of a goes
+    u32 *keep_codes;            // NULL, or where the 8-bit form of a goes (small matrices and bfloat16 write it on the way)
     uint8_t *keep_scale;
 };
 
@@ -77,16 +77,16 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total)
 bool few_rows_fit(const RowsArgs &r, bool wide);
 hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream);
 
-// small matrices, any type and alignment; the only rows kernel that writes the 8-bit form of its input
+// small matrices, float32
 bool narrow_rows_fit(const RowsArgs &r);
-hipError_t launch_narrow_rows(RowsArgs r, u32 dtype, bool across, hipStream_t stream);
+hipError_t launch_narrow_rows(RowsArgs r, bool across, hipStream_t stream);
 
 bool narrow_backward_fits(const BackwardArgs &r, bool codes);
 u32 narrow_backward_slots(u32 n, u32 k);      // workgroups at once
 hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream);
 
-// bfloat16 whose rows start at 16-byte boundaries
-bool wide_rows_fit(const RowsArgs &r, bool across);
+// bfloat16
+bool wide_rows_fit(const RowsArgs &r);
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream);
 u32 wide_sums_side(u32 n, u32 k);            // of its tiles
 bool wide_sums_fit(const SumsArgs &r);

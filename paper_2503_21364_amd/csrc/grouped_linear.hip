@@ -331,18 +331,17 @@ hipError_t rows_go(RowsArgs r, u32 gate, hipStream_t stream)
 template <class T>
 hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
 {
-    const bool wide = std::is_same<T, __bf16>::value && wide_rows_fit(r, across);
-    if (r.keep_codes) {
-        if (wide && !few_rows_fit(r, true) && !narrow_rows_fit(r)) return launch_wide_rows(r, across, stream);
-        if (narrow_rows_fit(r)) return launch_narrow_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
+    constexpr u32 dtype = std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16;
+    const bool wide = dtype == LMK_GS_BF16 && wide_rows_fit(r), narrow = dtype == LMK_GS_F32 && narrow_rows_fit(r);
+    const bool few = few_rows_fit(r, wide) && !(narrow && r.keep_codes);
+    if (r.keep_codes && (few || !(wide || narrow))) {
         const lmk_gs_checkpoint8 keep = {reinterpret_cast<int8_t *>(r.keep_codes), r.keep_scale};
-        const hipError_t e = launch_checkpoint8_pack(r.a, r.lda, r.rows, r.sums, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16,
-                                                     r.offsets, r.blocks, keep, stream);
+        const hipError_t e = launch_checkpoint8_pack(r.a, r.lda, r.rows, r.sums, dtype, r.offsets, r.blocks, keep, stream);
         if (e != hipSuccess) return e;
     }
-    if (few_rows_fit(r, wide)) return launch_few_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
-    if (narrow_rows_fit(r)) return launch_narrow_rows(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, across, stream);
+    if (few) return launch_few_rows(r, dtype, across, stream);
     if (wide) return launch_wide_rows(r, across, stream);
+    if (narrow) return launch_narrow_rows(r, across, stream);
     const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
     return across ? rows_go<T, true>(r, gate, stream) : rows_go<T, false>(r, gate, stream);
 }
@@ -364,7 +363,7 @@ hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 
 // Small matrices in float32 take one pass over the rows for all three gradients; the rest of the rule (strides) is the
 // arrays', and what does not fit takes the other kernels with the same slices.
-static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l.n <= 128 && l.k <= 64; }
+static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l.n <= 96 && l.k <= 64; }
 
 // how the sums over rows are shared out
 struct RunPlan {

@@ -237,22 +237,20 @@ hipError_t narrow_backward_k(const BackwardArgs &r, bool codes, hipStream_t stre
     case 1: return narrow_backward_go<CN, 1>(r, codes, stream);
     case 2: return narrow_backward_go<CN, 2>(r, codes, stream);
     case 3: return narrow_backward_go<CN, 3>(r, codes, stream);
-    default: break;
+    default: return narrow_backward_go<CN, 4>(r, codes, stream);
     }
-    if constexpr (CN <= 6) return narrow_backward_go<CN, 4>(r, codes, stream);
-    return hipErrorInvalidValue;
 }
 
 }  // namespace
 
 bool narrow_backward_fits(const BackwardArgs &r, bool codes)
 {
-    if (r.n < 4 || r.k < 4 || r.n > 128 || r.k > 64 || (r.n > 96 && r.k > 48)) return false;
+    if (r.n < 4 || r.k < 4 || r.n > 96 || r.k > 64) return false;
     return r.lddy <= kNarrowStride && r.lddx <= kNarrowStride && (codes || r.ldx <= kNarrowStride);
 }
 
 // outputs in tiles of 16, as the kernels are built for them
-static u32 out_tiles(u32 n) { return n <= 32 ? 2 : n <= 64 ? 4 : n <= 80 ? 5 : n <= 96 ? 6 : 8; }
+static u32 out_tiles(u32 n) { return n <= 32 ? 2 : n <= 64 ? 4 : n <= 80 ? 5 : 6; }
 
 u32 narrow_backward_slots(u32 n, u32 k) { return 256 * resident(out_tiles(n) * ((k + 15) / 16)); }
 
@@ -262,8 +260,7 @@ hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t
     case 2: return narrow_backward_k<2>(r, codes, stream);
     case 4: return narrow_backward_k<4>(r, codes, stream);
     case 5: return narrow_backward_k<5>(r, codes, stream);
-    case 6: return narrow_backward_k<6>(r, codes, stream);
-    default: return narrow_backward_k<8>(r, codes, stream);
+    default: return narrow_backward_k<6>(r, codes, stream);
     }
 }
 

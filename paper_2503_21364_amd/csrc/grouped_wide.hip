@@ -1,5 +1,5 @@
-// Grouped layers in bfloat16 whose rows start at 16-byte boundaries: the same products as in grouped_linear.hip on the bfloat16
-// matrix instructions (v_mfma_f32_16x16x32_bf16: exact products, sums in 32 bits).
+// Grouped layers in bfloat16: the same products as in grouped_linear.hip on the bfloat16 matrix instructions
+// (v_mfma_f32_16x16x32_bf16: exact products, sums in 32 bits).
 #include "grouped.h"
 #include "grouped_kernels.h"
 
@@ -127,6 +127,119 @@ template <u32 W, u32 WAVES> struct Across16 {
     __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 h, u32 r0, u32 f) const { return across_fragment<W>(lds + h * kStep * W * 2, read, r0, f); }
 };
 
+// ---- the same operands where rows start anywhere and end anywhere: through registers, one pair of steps ahead.
+
+// eight bfloat16, moved down by d places (zeros come in)
+__device__ __forceinline__ u32x4 move_down(u32x4 v, u32 d)
+{
+    u64 lo = (u64)v[1] << 32 | v[0], hi = (u64)v[3] << 32 | v[2];
+    if (d >= 8) return u32x4{0, 0, 0, 0};
+    if (d >= 4) {
+        lo = hi >> (16 * (d - 4));
+        hi = 0;
+    } else if (d > 0) {
+        lo = lo >> (16 * d) | hi << (64 - 16 * d);
+        hi >>= 16 * d;
+    }
+    return u32x4{(u32)lo, (u32)(lo >> 32), (u32)hi, (u32)(hi >> 32)};
+}
+
+// sums >= 8: the last, partial eight of a row are read as its last whole ones
+template <u32 W, u32 WAVES> struct AlongAny {
+    static constexpr bool kDirect = false;
+    static constexpr u32 kLoads = W / 8 / WAVES;
+    const __bf16 *p;
+    u32 sums, s0, chunk;
+    u32 from[kLoads];       // offset of this thread's rows
+    u32x4 v[kLoads];
+    u32 to, read;
+
+    __device__ __forceinline__ void init(const __bf16 *base, u64 ld, u32 rows, u32 sums_, u32 wave, u32 lane)
+    {
+        p = base;
+        sums = sums_;
+        s0 = 0;
+        const u32 thread = wave * kWave + lane, row = thread / 8;
+        chunk = thread & 7;
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i) from[i] = (row + WAVES * 8 * i < rows ? row + WAVES * 8 * i : 0u) * (u32)ld;
+        // WAVES * 8 rows further on, the chunks are turned alike
+        to = row * 128 + ((chunk ^ (row >> 1 & 7)) * 16);
+        read = (lane & 15) * 128 + (((lane >> 4) ^ (lane >> 1 & 7)) * 16);
+        request();
+    }
+    __device__ __forceinline__ void request()
+    {
+        const u32 s = s0 + chunk * 8, at = s + 8 <= sums ? s : sums - 8;
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i) v[i] = load_any<u32x4>(p + from[i] + at);
+    }
+    __device__ __forceinline__ void fill(lds_char *lds, u32)
+    {
+        const u32 s = s0 + chunk * 8, d = s + 8 <= sums ? 0u : s - (sums - 8);
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i) {
+            u32x4 o = v[i];
+            if (s0 + kPair > sums) o = move_down(o, d);
+            *reinterpret_cast<lds_u32x4 *>(lds + to + i * WAVES * 1024) = o;
+        }
+        s0 += kPair;
+        request();
+    }
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 h, u32 r0, u32 f) const
+    {
+        return *reinterpret_cast<const lds_bf16x8 *>(lds + (read ^ h * 64) + (r0 + 16 * f) * 128);
+    }
+};
+
+// rows of eight columns and more
+template <u32 W, u32 WAVES> struct AcrossAny {
+    static constexpr bool kDirect = false;
+    static constexpr u32 kLoads = W / 8 / WAVES, kRows = WAVES * kWave * 8 / W;      // rows of a turn of loads
+    static_assert(kRows % 16 == 0, "rows of another turn are turned alike");
+    const __bf16 *p;        // this thread's columns of the next pair's first row
+    u64 ld;
+    u32 left, row, d;
+    u32x4 v[kLoads];
+    u32 to, read;
+
+    // back: columns in front of base that its rows have
+    __device__ __forceinline__ void init(const __bf16 *base, u64 ld_, u32 width, u32 sums, u32 wave, u32 lane)
+    {
+        const u32 thread = wave * kWave + lane, chunk = thread % (W / 8), col = chunk * 8;
+        row = thread / (W / 8);
+        ld = ld_;
+        left = sums;
+        // columns behind the last one are anything: their results are not kept
+        const int at = col + 8 <= width ? (int)col : (int)width - 8;
+        d = (u32)((int)col - at);
+        p = base + at;
+        to = row * (W * 2) + ((((chunk >> 1) ^ turn(row)) * 2 + (chunk & 1)) * 16);
+        read = across_read<W>(lane);
+        request();
+    }
+    __device__ __forceinline__ void request()
+    {
+        if (left == 0) return;
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i) v[i] = load_any<u32x4>(p + (row + kRows * i < left ? row + kRows * i : 0u) * ld);
+    }
+    __device__ __forceinline__ void fill(lds_char *lds, u32)
+    {
+#pragma unroll
+        for (u32 i = 0; i < kLoads; ++i) {
+            u32x4 o = v[i];
+            if (d > 0) o = move_down(o, d);
+            if (row + kRows * i >= left) o = u32x4{0, 0, 0, 0};
+            *reinterpret_cast<lds_u32x4 *>(lds + to + i * kRows * W * 2) = o;
+        }
+        p += (u64)kPair * ld;
+        left = left > kPair ? left - kPair : 0u;
+        request();
+    }
+    __device__ __forceinline__ bf16x8 fragment(const lds_char *lds, u32 h, u32 r0, u32 f) const { return across_fragment<W>(lds + h * kStep * W * 2, read, r0, f); }
+};
+
 // Tile of TP x TQ results: P runs along the output's contiguous axis (a lane holds four consecutive ones of it), Q across it.
 template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
     static constexpr u32 kWaves = WP * WQ, kThreads = kWaves * kWave;
@@ -240,7 +353,7 @@ __device__ __forceinline__ void keep_pair(const RowsArgs &r, const lds_char *lds
 
 // GATE: 0 none, 1 values, 2 codes, 3 none, and the 8-bit form of x is written: whole lines of it, two pairs of steps of a row, by the
 // workgroups of its columns in turn
-template <class S, u32 TP, u32 TQ, u32 WP, bool ACROSS, u32 GATE>
+template <class S, u32 TP, u32 TQ, u32 WP, bool ACROSS, bool ANY, u32 GATE>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
@@ -270,15 +383,15 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
     if (inside) {
         lds_char *lds = (lds_char *)wide_lds;
         const u32 steps = (r.sums + kStep - 1) / kStep;
-        Along16<TQ, S::kWaves> q;
+        typename std::conditional<ANY, AlongAny<TQ, S::kWaves>, Along16<TQ, S::kWaves>>::type q;
         q.init(static_cast<const __bf16 *>(r.a) + (u64)row0 * r.lda, r.lda, height, r.sums, wave, lane);
         const __bf16 *w = static_cast<const __bf16 *>(r.w) + (u64)run.block * r.w_block;
         if constexpr (ACROSS) {
-            Across16<TP, S::kWaves> p;
+            typename std::conditional<ANY, AcrossAny<TP, S::kWaves>, Across16<TP, S::kWaves>>::type p;
             p.init(w + col0, r.ldw, width, r.sums, wave, lane);
             wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing, keep);
         } else {
-            Along16<TP, S::kWaves> p;
+            typename std::conditional<ANY, AlongAny<TP, S::kWaves>, Along16<TP, S::kWaves>>::type p;
             p.init(w + (u64)col0 * r.ldw, r.ldw, width, r.sums, wave, lane);
             wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing, keep);
         }
@@ -317,8 +430,20 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
             u32x4 v = {a[0], b[0], a[1], b[1]};
             const u32 row = q0 + 16 * j + (lane & 15);
             if (row >= height || c >= width) continue;
+            if (ANY && c + 8 > width) {
+#pragma unroll
+                for (u32 e = 0; e < 8; ++e) {
+                    if (c + e >= width) continue;
+                    const u64 at = (u64)(row0 + row) * r.ldgate + col0 + c + e;
+                    bool pass = true;
+                    if (GATE == 1 && inside) pass = !((float)static_cast<const __bf16 *>(r.gate)[at] <= 0.0f);
+                    if (GATE == 2 && inside) pass = static_cast<const signed char *>(r.gate)[at] > 0 || r.gate_scale[at / 32] == 255;
+                    out[(u64)row * r.ldo + c + e] = pass ? __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2)))) : (__bf16)0.0f;
+                }
+                continue;
+            }
             if (GATE == 1 && inside) {
-                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(static_cast<const __bf16 *>(r.gate) + (u64)(row0 + row) * r.ldgate + col0 + c);
+                const bf16x8 x = load_any<bf16x8>(static_cast<const __bf16 *>(r.gate) + (u64)(row0 + row) * r.ldgate + col0 + c);
 #pragma unroll
                 for (u32 e = 0; e < 4; ++e) {
                     if ((float)x[2 * e] <= 0.0f) v[e] &= 0xffff0000u;
@@ -334,7 +459,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArg
                         if ((int)(signed char)(codes[e / 4] >> (8 * (e % 4))) <= 0) v[e / 2] &= e % 2 ? 0x0000ffffu : 0xffff0000u;
                 }
             }
-            *reinterpret_cast<u32x4 *>(out + (u64)row * r.ldo + c) = v;
+            store_any(out + (u64)row * r.ldo + c, v);
         }
     }
 }
@@ -406,7 +531,7 @@ template <u32 W, u32 WAVES> struct Codes16 {
 
 // Tiles of dw over a slice of the rows: P = x (inputs), Q = dy (outputs).  db rides on the tiles of the first inputs: a
 // matrix instruction with ones in the place of x, the wavefronts along P taking turns.
-template <class S, u32 TP, u32 TQ, u32 WP, bool CODES>
+template <class S, u32 TP, u32 TQ, u32 WP, bool CODES, bool ANY>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
@@ -436,7 +561,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArg
                 for (u32 j = 0; j < S::kQ; ++j)
                     if (j % WP == pw) bias[j / WP] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fq[j], bias[j / WP], 0, 0, 0);
             };
-            Across16<TQ, S::kWaves> q;
+            typename std::conditional<ANY, AcrossAny<TQ, S::kWaves>, Across16<TQ, S::kWaves>>::type q;
             q.init(static_cast<const __bf16 *>(r.dy) + (u64)run.row * r.lddy + n0, r.lddy, height, run.count, wave, lane);
             if constexpr (CODES) {
                 const u32 kp = (r.k + 31) / 32 * 32;
@@ -445,7 +570,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArg
                        run.count, wave, lane);
                 wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
             } else {
-                Across16<TP, S::kWaves> p;
+                typename std::conditional<ANY, AcrossAny<TP, S::kWaves>, Across16<TP, S::kWaves>>::type p;
                 p.init(static_cast<const __bf16 *>(r.x) + (u64)run.row * r.ldx + k0, r.ldx, width, run.count, wave, lane);
                 wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
             }
@@ -460,10 +585,11 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArg
 #pragma unroll
             for (u32 i = 0; i < S::kP; ++i) {
                 const u32 k = k0 + p0 + 16 * i + 4 * (lane >> 4);
-                if (k >= r.k) continue;                     // k comes in eights
-                if (r.in_major) {
+                if (k >= r.k) continue;
+                if (r.in_major || (ANY && k + 4 > r.k)) {
 #pragma unroll
-                    for (u32 v = 0; v < 4; ++v) dw[(u64)(k + v) * r.n + n] = acc[i][j][v];
+                    for (u32 v = 0; v < 4; ++v)
+                        if (!ANY || k + v < r.k) dw[r.in_major ? (u64)(k + v) * r.n + n : (u64)n * r.k + k + v] = acc[i][j][v];
                 } else {
                     store_any(dw + (u64)n * r.k + k, acc[i][j]);
                 }
@@ -475,48 +601,55 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArg
 
 // ---- launches
 
-template <u32 TP, u32 TQ, u32 WP, u32 WQ, bool ACROSS, u32 GATE>
+template <u32 TP, u32 TQ, u32 WP, u32 WQ, bool ACROSS, bool ANY, u32 GATE>
 hipError_t wide_go(RowsArgs r, hipStream_t stream)
 {
     using S = Shape<TP, TQ, WP, WQ>;
     r.col_tiles = (r.cols + TP - 1) / TP;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, TQ) * r.col_tiles);
-    auto kernel = wide_rows_kernel<S, TP, TQ, WP, ACROSS, GATE>;
+    auto kernel = wide_rows_kernel<S, TP, TQ, WP, ACROSS, ANY, GATE>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), S::kLds, stream, r);
     return hipGetLastError();
 }
+bool sixteen(const void *p, u64 ld) { return ld % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+bool rows_sixteen(const RowsArgs &r)
+{
+    return r.sums % 8 == 0 && r.cols % 8 == 0 && sixteen(r.a, r.lda) && sixteen(r.w, r.ldw) && r.w_block % 8 == 0;
+}
+
 template <bool ACROSS, u32 GATE>
 hipError_t wide_shape(const RowsArgs &r, hipStream_t stream)
 {
+    if (!rows_sixteen(r)) return wide_go<128, 128, 2, 2, ACROSS, true, GATE>(r, stream);
     if (r.cols > 128 && max_runs(r.rows, r.blocks, 256) * ((r.cols + 255) / 256) >= 256)
-        return wide_go<256, 256, 2, 4, ACROSS, GATE>(r, stream);
-    return wide_go<128, 128, 2, 2, ACROSS, GATE>(r, stream);
+        return wide_go<256, 256, 2, 4, ACROSS, false, GATE>(r, stream);
+    return wide_go<128, 128, 2, 2, ACROSS, false, GATE>(r, stream);
 }
 
-template <u32 TP, u32 TQ, u32 WP, u32 WQ>
+template <u32 TP, u32 TQ, u32 WP, u32 WQ, bool ANY>
 hipError_t wide_sums_go(SumsArgs r, bool codes, hipStream_t stream)
 {
     using S = Shape<TP, TQ, WP, WQ>;
     r.n_tiles = (r.n + TQ - 1) / TQ;
     r.k_tiles = (r.k + TP - 1) / TP;
     r.tiles = (u32)((u64)r.slices * r.n_tiles * r.k_tiles);
-    auto kernel = codes ? wide_sums_kernel<S, TP, TQ, WP, true> : wide_sums_kernel<S, TP, TQ, WP, false>;
+    auto kernel = codes ? wide_sums_kernel<S, TP, TQ, WP, true, ANY> : wide_sums_kernel<S, TP, TQ, WP, false, ANY>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), S::kLds, stream, r);
     return hipGetLastError();
 }
 
-bool sixteen(const void *p, u64 ld) { return ld % 8 == 0 && ld <= 1u << 21 && reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-
 }  // namespace
 
-bool wide_rows_fit(const RowsArgs &r, bool across)
+// Offsets inside a tile are 32 bits wide.  Narrower than eight: the general kernel.
+bool wide_rows_fit(const RowsArgs &r)
 {
-    if (r.sums % 8 || r.cols % 8 || !sixteen(r.a, r.lda) || !sixteen(r.w, r.ldw) || r.w_block % 8 || !sixteen(r.out, r.ldo)) return false;
-    return !r.gate || r.gate_scale || sixteen(r.gate, r.ldgate);
+    constexpr u64 most = 1u << 21;
+    return r.sums >= 8 && r.cols >= 8 && r.lda <= most && r.ldw <= most;
 }
 
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
@@ -531,14 +664,16 @@ u32 wide_sums_side(u32 n, u32 k) { return n > 128 && k > 128 ? 256 : 128; }
 
 bool wide_sums_fit(const SumsArgs &r)
 {
-    return r.n % 8 == 0 && r.k % 8 == 0 && r.dw && sixteen(r.dy, r.lddy) &&
-           (r.scale || sixteen(r.x, r.ldx));
+    constexpr u64 most = 1u << 21;
+    return r.n >= 8 && r.k >= 8 && r.dw && r.lddy <= most && (r.scale || r.ldx <= most);
 }
 
 hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream)
 {
-    if (wide_sums_side(r.n, r.k) == 256) return wide_sums_go<256, 256, 2, 4>(r, r.scale != nullptr, stream);
-    return wide_sums_go<128, 128, 2, 2>(r, r.scale != nullptr, stream);
+    const bool any = r.n % 8 || !sixteen(r.dy, r.lddy) || (!r.scale && (r.k % 8 || !sixteen(r.x, r.ldx))) || r.k % 4;
+    if (any) return wide_sums_go<128, 128, 2, 2, true>(r, r.scale != nullptr, stream);
+    if (wide_sums_side(r.n, r.k) == 256) return wide_sums_go<256, 256, 2, 4, false>(r, r.scale != nullptr, stream);
+    return wide_sums_go<128, 128, 2, 2, false>(r, r.scale != nullptr, stream);
 }
 
 }  // namespace lmk

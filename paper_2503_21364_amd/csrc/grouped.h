@@ -102,7 +102,7 @@ __device__ __forceinline__ u32 afresh(u32 v)
 // By slices: the rows of all blocks are cut into slices of `per` rows, whatever the blocks' lengths are, and the workgroups of a
 // slice sum it block after block; a run is where a slice and a block meet.  Every workgroup has the same number of rows.
 // By blocks: every block is cut into as many runs of at most `per` rows as it takes, of equal length; a workgroup has one run.
-// A block of one run has its result there.  Otherwise run r of block g is set r + g + (first row of g) / per of the partial sums,
+// A block of one run has its result there, one without rows gets its zeros from join_kernel.  Otherwise run r of block g is set r + g + (first row of g) / per of the partial sums,
 // rows counted from the first block's; no two runs have the same, in either arrangement (a block's rows / per, rounded up, is at
 // most one more than what the first row of the next one adds), and join_kernel adds a block's sets in their order.
 struct RowSlices {
@@ -130,20 +130,17 @@ struct RowSlices {
     __device__ __forceinline__ u32 slice_of(u32 row) const { return row > front ? (row - front) / per : 0u; }
 };
 
-// The runs of slice s, one after the other; all lanes of a wavefront take part, the results are uniform.  A block without rows
-// belongs to the slice it lies in, as a run of no rows.
+// The runs of slice s, one after the other; all lanes of a wavefront take part, the results are uniform.
 struct SliceRuns {
     RowSlices all;
     u32 s, s0, s1, g;
-    bool last;                  // of the slices
     u32 block, row, count;      // of the present run
     bool whole;                 // the block has no other
 
-    __device__ __forceinline__ void init(const u32 *offsets, u32 blocks, u32 rows, u32 per, u32 slices, u32 s_)
+    __device__ __forceinline__ void init(const u32 *offsets, u32 blocks, u32 rows, u32 per, u32 s_)
     {
         all.init(offsets, blocks, rows, per);
         s = s_;
-        last = s + 1 == slices;
         all.front = uniform(all.front);
         all.back = uniform(all.back);
         s0 = all.edge(s);
@@ -152,7 +149,7 @@ struct SliceRuns {
         for (g = 0; g < blocks; g += kWave) {
             u32 b = 0, e = 0;
             if (g + lane < blocks) all.block(g + lane, b, e);
-            const u64 hit = __builtin_amdgcn_ballot_w64(g + lane < blocks && (e > s0 || (e == b && b >= s0)));
+            const u64 hit = __builtin_amdgcn_ballot_w64(g + lane < blocks && e > s0 && e > b);
             if (hit != 0ull) {
                 g += (u32)__builtin_ctzll(hit);
                 break;
@@ -166,14 +163,6 @@ struct SliceRuns {
             all.block(g, b, e);
             b = uniform(b);
             e = uniform(e);
-            if (b == e) {
-                if (b >= s1 && !last) return false;
-                if (b < s0) continue;
-                block = g++;
-                row = b;
-                count = 0;
-                return whole = true;
-            }
             if (b >= s1) return false;
             row = b > s0 ? b : s0;
             const u32 end = e < s1 ? e : s1;
@@ -204,7 +193,6 @@ struct BlockRun {
             if (g < blocks) {
                 all.block(g, b, e);
                 runs = (e - b + per - 1) / per;
-                runs = runs ? runs : 1u;
                 first = g + all.slice_of(b);
             }
             const u64 hit = __builtin_amdgcn_ballot_w64(first <= t && t - first < runs);

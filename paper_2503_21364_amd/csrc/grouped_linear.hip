@@ -236,30 +236,28 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
     const u32 height = r.n - n0 < kTile ? r.n - n0 : kTile, width = r.k - k0 < kTile ? r.k - k0 : kTile;
     const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 31, hi = lane / 32;
     SliceRuns run;
-    run.init(r.offsets, r.blocks, r.rows, r.per, r.slices, slice);
+    run.init(r.offsets, r.blocks, r.rows, r.per, slice);
     while (run.next()) {
         f32x16 acc = {};
         float bias = 0.0f;
-        if (run.count > 0) {
-            __syncthreads();                    // the run in front of this one is out of LDS
-            Across<T, kTile> a{static_cast<const T *>(r.dy) + (u64)run.row * r.lddy + n0, r.lddy, height, run.count, {}};
-            // thread m sums column m of the staged dy
-            const bool sums_db = r.db && k0 == 0 && threadIdx.x < kTile;
-            auto each = [&](const float *la) {
-                if (!sums_db) return;
+        __syncthreads();                    // the run in front of this one is out of LDS
+        Across<T, kTile> a{static_cast<const T *>(r.dy) + (u64)run.row * r.lddy + n0, r.lddy, height, run.count, {}};
+        // thread m sums column m of the staged dy
+        const bool sums_db = r.db && k0 == 0 && threadIdx.x < kTile;
+        auto each = [&](const float *la) {
+            if (!sums_db) return;
 #pragma unroll
-                for (u32 s = 0; s < kStep; ++s) bias += la[s * pitch_of(kTile) + threadIdx.x];
-            };
-            if constexpr (KIND == 2) {
-                const u32 kp = (r.k + 31) / 32 * 32;
-                Across8<kTile> b{reinterpret_cast<const u32 *>(static_cast<const signed char *>(r.x) + (u64)run.row * kp + k0),
-                                 r.scale + ((u64)run.row * kp + k0) / 32, kp, kp - k0, run.count, {}, {}};
-                tile_product(a, b, run.count, lds, acc, each);
-            } else {
-                Across<T, kTile> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)run.row * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
-                                   run.count, {}};
-                tile_product(a, b, run.count, lds, acc, each);
-            }
+            for (u32 s = 0; s < kStep; ++s) bias += la[s * pitch_of(kTile) + threadIdx.x];
+        };
+        if constexpr (KIND == 2) {
+            const u32 kp = (r.k + 31) / 32 * 32;
+            Across8<kTile> b{reinterpret_cast<const u32 *>(static_cast<const signed char *>(r.x) + (u64)run.row * kp + k0),
+                             r.scale + ((u64)run.row * kp + k0) / 32, kp, kp - k0, run.count, {}, {}};
+            tile_product(a, b, run.count, lds, acc, each);
+        } else {
+            Across<T, kTile> b{static_cast<const T *>(r.x) + (KIND == 1 ? (u64)run.row * r.ldx + k0 : 0), r.ldx, KIND == 1 ? width : 0u,
+                               run.count, {}};
+            tile_product(a, b, run.count, lds, acc, each);
         }
         const u64 size = (u64)r.n * r.k;
         float *dw = run.whole ? r.dw + (u64)run.block * size : r.part + (u64)run.partial() * (size + r.n);
@@ -277,7 +275,7 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
     }
 }
 
-// Joins the partial sums of the blocks that have several runs, in the order of the runs.  V consecutive sums a thread, AHEAD sets on
+// Joins the partial sums of the blocks that have several runs, in the order of the runs, and clears those of blocks without rows.  V consecutive sums a thread, AHEAD sets on
 // their way.
 template <u32 V, u32 AHEAD>
 __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per, bool by_blocks,
@@ -290,9 +288,9 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
     all.init(offsets, blocks, rows, per);
     u32 b, e;
     all.block(block, b, e);
-    if (b == e) return;
-    const u32 first = all.slice_of(b), runs = by_blocks ? (e - b + per - 1) / per : all.slice_of(e - 1) - first + 1;
-    if (runs == 1) return;                      // written where it was summed
+    // no runs: zeros; one: written where it was summed
+    const u32 first = all.slice_of(b), runs = b == e ? 0u : by_blocks ? (e - b + per - 1) / per : all.slice_of(e - 1) - first + 1;
+    if (runs == 1) return;
     const u64 size = (u64)n * k, stride = size + n;
     const float *p = part + (u64)(first + block) * stride;
     const auto sum = [&](auto zero, u64 at) {

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
     BlockRun run;
     if (!run.find(r.offsets, r.blocks, r.rows, r.per, blockIdx.x)) return;
     const u32 row0 = run.row, height = run.count, lane = threadIdx.x & (kWave - 1), j = lane & 15, q = lane >> 4;
-    if (r.dx && height > 0)
+    if (r.dx)
         stage_weights<float, CK>(lw, r.w + (u64)run.block * r.w_block, r.ldw, r.in_major == 0, r.n, r.k);
     __syncthreads();
 

@@ -545,35 +545,33 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArg
     constexpr u32 kB = (S::kQ + WP - 1) / WP;
     lds_char *lds = (lds_char *)wide_lds;
     SliceRuns run;
-    run.init(r.offsets, r.blocks, r.rows, r.per, r.slices, slice);
+    run.init(r.offsets, r.blocks, r.rows, r.per, slice);
     while (run.next()) {
         const u32 lane = afresh(threadIdx.x & (kWave - 1));
         f32x4 acc[S::kP][S::kQ] = {};
         f32x4 bias[kB] = {};
-        if (run.count > 0) {
-            __syncthreads();                    // the run in front of this one is out of LDS
-            const u32 steps = (run.count + kStep - 1) / kStep;
-            const __bf16 one = (__bf16)1.0f;
-            const bf16x8 ones = {one, one, one, one, one, one, one, one};
-            const auto add = [&](const bf16x8 (&fq)[S::kQ]) {
-                if (!sums_db) return;
+        __syncthreads();                    // the run in front of this one is out of LDS
+        const u32 steps = (run.count + kStep - 1) / kStep;
+        const __bf16 one = (__bf16)1.0f;
+        const bf16x8 ones = {one, one, one, one, one, one, one, one};
+        const auto add = [&](const bf16x8 (&fq)[S::kQ]) {
+            if (!sums_db) return;
 #pragma unroll
-                for (u32 j = 0; j < S::kQ; ++j)
-                    if (j % WP == pw) bias[j / WP] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fq[j], bias[j / WP], 0, 0, 0);
-            };
-            typename std::conditional<ANY, AcrossAny<TQ, S::kWaves>, Across16<TQ, S::kWaves>>::type q;
-            q.init(static_cast<const __bf16 *>(r.dy) + (u64)run.row * r.lddy + n0, r.lddy, height, run.count, wave, lane);
-            if constexpr (CODES) {
-                const u32 kp = (r.k + 31) / 32 * 32;
-                Codes16<TP, S::kWaves> p;
-                p.init(static_cast<const char *>(r.x) + (u64)run.row * kp + k0, r.scale + (u64)run.row * (kp / 32) + k0 / 32, kp, kp - k0,
-                       run.count, wave, lane);
-                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
-            } else {
-                typename std::conditional<ANY, AcrossAny<TP, S::kWaves>, Across16<TP, S::kWaves>>::type p;
-                p.init(static_cast<const __bf16 *>(r.x) + (u64)run.row * r.ldx + k0, r.ldx, width, run.count, wave, lane);
-                wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
-            }
+            for (u32 j = 0; j < S::kQ; ++j)
+                if (j % WP == pw) bias[j / WP] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, fq[j], bias[j / WP], 0, 0, 0);
+        };
+        typename std::conditional<ANY, AcrossAny<TQ, S::kWaves>, Across16<TQ, S::kWaves>>::type q;
+        q.init(static_cast<const __bf16 *>(r.dy) + (u64)run.row * r.lddy + n0, r.lddy, height, run.count, wave, lane);
+        if constexpr (CODES) {
+            const u32 kp = (r.k + 31) / 32 * 32;
+            Codes16<TP, S::kWaves> p;
+            p.init(static_cast<const char *>(r.x) + (u64)run.row * kp + k0, r.scale + (u64)run.row * (kp / 32) + k0 / 32, kp, kp - k0,
+                   run.count, wave, lane);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
+        } else {
+            typename std::conditional<ANY, AcrossAny<TP, S::kWaves>, Across16<TP, S::kWaves>>::type p;
+            p.init(static_cast<const __bf16 *>(r.x) + (u64)run.row * r.ldx + k0, r.ldx, width, run.count, wave, lane);
+            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, add, [](u32, const lds_char *) {});
         }
         const u64 size = (u64)r.n * r.k;
         float *dw = run.whole ? r.dw + (u64)run.block * size : r.part + (u64)run.partial() * (size + r.n);

@@ -145,31 +145,26 @@ struct SliceRuns {
         all.back = uniform(all.back);
         s0 = all.edge(s);
         s1 = all.edge(s + 1);
-        const u32 lane = threadIdx.x & (kWave - 1);
-        for (g = 0; g < blocks; g += kWave) {
-            u32 b = 0, e = 0;
-            if (g + lane < blocks) all.block(g + lane, b, e);
-            const u64 hit = __builtin_amdgcn_ballot_w64(g + lane < blocks && e > s0 && e > b);
-            if (hit != 0ull) {
-                g += (u32)__builtin_ctzll(hit);
-                break;
-            }
-        }
+        g = 0;
     }
+    // 64 blocks are looked at in a step
     __device__ __forceinline__ bool next()
     {
-        for (; g < all.blocks; ++g) {
-            u32 b, e;
-            all.block(g, b, e);
-            b = uniform(b);
-            e = uniform(e);
+        const u32 lane = threadIdx.x & (kWave - 1);
+        for (; g < all.blocks; g += kWave) {
+            u32 b = 0, e = 0;
+            if (g + lane < all.blocks) all.block(g + lane, b, e);
+            const u64 hit = __builtin_amdgcn_ballot_w64(e > s0 && e > b);
+            if (hit == 0ull) continue;
+            const int at = __builtin_ctzll(hit);
+            b = (u32)__builtin_amdgcn_readlane((int)b, at);
+            e = (u32)__builtin_amdgcn_readlane((int)e, at);
             if (b >= s1) return false;
             row = b > s0 ? b : s0;
-            const u32 end = e < s1 ? e : s1;
-            if (end <= row) continue;
-            count = end - row;
+            count = (e < s1 ? e : s1) - row;
             whole = b >= s0 && e <= s1;
-            block = g++;
+            block = g + (u32)at;
+            g = block + 1;
             return true;
         }
         return false;

@@ -1,5 +1,14 @@
 // Grouped layers in bfloat16: the same products as in grouped_linear.hip on the bfloat16 matrix instructions
-// (v_mfma_f32_16x16x32_bf16: exact products, sums in 32 bits).
+// (v_mfma_f32_16x16x32_bf16: exact products, sums in 32 bits; only results are rounded, once).
+//
+// Bound by those instructions and by LDS, which feeds them: 8192 x 8192 x 8192 in 800 - 966 (forward), 1030 - 1070 (dx), 1130 - 1160
+// (dw) and 1030 - 1080 TFLOP/s (dw from the 8-bit form); the largest library product reaches 1268.  65 536 rows in 32 ragged blocks
+// of 1024 x 1024 (137 GFLOP a product): forward with the 8-bit form 232 us, dx with its gate 221 - 226, dw and db 191 - 198.
+// There 1076 tiles take five rounds of 256 workgroups where 4.2 would do, and a round's first loads and last stores have no
+// products beside them: the accumulators and two steps' fragments of a lane leave no registers for the next tile's.
+//
+// Tiles of 256 x 256, two wavefronts a SIMD: LDS gives a step's fragments in less time than their products take, which it
+// does not for 128 x 128 (65 536 x 1024 x 1024: 202 us) or 256 x 128 (231 us).
 #include "grouped.h"
 #include "grouped_kernels.h"
 
@@ -203,7 +212,6 @@ template <u32 W, u32 WAVES> struct AcrossAny {
     u32x4 v[kLoads];
     u32 to, read;
 
-    // back: columns in front of base that its rows have
     __device__ __forceinline__ void init(const __bf16 *base, u64 ld_, u32 width, u32 sums, u32 wave, u32 lane)
     {
         const u32 thread = wave * kWave + lane, chunk = thread % (W / 8), col = chunk * 8;

@@ -185,7 +185,7 @@ template <class T, bool ACROSS, u32 GATE>
 __global__ __launch_bounds__(256, 4) void rows_kernel(const RowsArgs r)
 {
     __shared__ __align__(16) float lds[4 * kStep * pitch_of(kTile)];
-    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, 4 * kUnits);
     const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * kTile;
     const RowRun run = find_run(r.offsets, r.blocks, r.rows, kTile, row_tile);
     if (!run.found) return;
@@ -234,7 +234,7 @@ template <class T, u32 KIND>
 __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
 {
     __shared__ __align__(16) float lds[4 * kStep * pitch_of(kTile)];
-    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, 4 * kUnits);
     const u32 pairs = r.n_tiles * r.k_tiles, slice = tile / pairs, pair = tile - slice * pairs;
     const u32 n0 = pair / r.k_tiles * kTile, k0 = pair % r.k_tiles * kTile;
     const u32 height = r.n - n0 < kTile ? r.n - n0 : kTile, width = r.k - k0 < kTile ? r.k - k0 : kTile;

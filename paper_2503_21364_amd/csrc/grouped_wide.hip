@@ -253,6 +253,7 @@ template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
     static constexpr u32 kWaves = WP * WQ, kThreads = kWaves * kWave;
     static constexpr u32 kP = TP / WP / 16, kQ = TQ / WQ / 16;           // 16 x 16 results of a wavefront
     static constexpr u32 kPartP = TP * kPair * 2, kPartQ = TQ * kPair * 2, kLds = 2 * (kPartP + kPartQ);
+    static constexpr u32 kResident = 512 / kThreads;                     // workgroups of a compute unit
 };
 
 // acc[i][j] += P Q over `steps`.  LDS holds two pairs of steps.  A step's fragments are read from LDS while the step in front of
@@ -365,7 +366,7 @@ template <class S, u32 TP, u32 TQ, u32 WP, bool ACROSS, bool ANY, u32 GATE>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_rows_kernel(const RowsArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
-    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, S::kResident * kUnits);
     const u32 row_tile = tile / r.col_tiles, col_tile = tile - row_tile * r.col_tiles, col0 = col_tile * TP;
     const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
     if (!run.found) return;
@@ -543,7 +544,7 @@ template <class S, u32 TP, u32 TQ, u32 WP, bool CODES, bool ANY>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
-    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles);
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, S::kResident * kUnits);
     const u32 pairs = r.n_tiles * r.k_tiles, slice = tile / pairs, pair = tile - slice * pairs;
     const u32 n0 = pair / r.k_tiles * TQ, k0 = pair % r.k_tiles * TP;
     const u32 height = r.n - n0 < TQ ? r.n - n0 : TQ, width = r.k - k0 < TP ? r.k - k0 : TP;

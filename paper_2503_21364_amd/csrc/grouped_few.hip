@@ -1,6 +1,7 @@
 // Grouped layers over few rows: a handful of anchors, most blocks without any.  Reading the weights is all of it, so a workgroup
 // takes 16 rows and NT columns of the output and its eight wavefronts share out the sum indices: every wavefront streams its part
-// of the weights straight into registers, whole lines a row, many loads in flight, and the parts meet in LDS.
+// of the weights straight into registers, whole lines a row, many loads in flight, and the parts meet in LDS.  One row and 8 blocks
+// of 1024 x 1024 in bfloat16: 4.1 us, a chain of latencies; 1024 rows and 64 blocks of 1024 x 2048: 59 us (4.6 TB/s).
 //
 // Products by v_mfma_f32_16x16x4_f32 (products and sums in 32 bits, bfloat16 widened: 9 TB/s of bfloat16 weights
 // at its rate, more than memory gives).  A step takes sum indices {q V + e : lane group q} for e = 0 .. V-1, any
@@ -119,9 +120,10 @@ hipError_t few_width(const RowsArgs &r, hipStream_t stream)
 {
     constexpr u32 v = ACROSS ? 4 : 16 / sizeof(T);          // a run of x, and of the weights
     const bool whole = r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
-    // 64 columns make whole lines where columns are contiguous and read x once for four results; 16 where that leaves
-    // compute units without work
-    if (max_runs(r.rows, r.blocks, kRows) * ((r.cols + 63) / 64) >= (ACROSS ? 64 : 256))
+    // 64 columns make whole lines where columns are contiguous (8 blocks of 1024 x 1024 in bfloat16, 128 rows, 64 / 16 columns:
+    // 10.5 / 14.3 us; one row: 8.9 / 5.3), and read x once for four results where they are not (one block of 2048 x 2048
+    // in float32, 128 rows: 24 / 31 us); 16 where that leaves compute units without work (8 blocks of 1024 x 1024, 128 rows: 10.3 / 7.0)
+    if (max_runs(r.rows, r.blocks, kRows) * ((r.cols + 63) / 64) >= (ACROSS ? 64 : 320))
         return whole ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
     return whole ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
 }
@@ -135,7 +137,17 @@ hipError_t few_as(const RowsArgs &r, bool across, hipStream_t stream)
 
 }  // namespace
 
-bool few_rows_fit(const RowsArgs &r, bool wide) { return wide ? r.rows <= 128 || r.rows <= 16 * r.blocks : r.rows <= 1024 || (r.rows <= 4096 && r.rows <= 64 * r.blocks); }
+// Where the other kernels' tiles would be mostly empty, or too few.  This kernel / the bfloat16 one, forward: one block of 2048 x 2048,
+// 128 rows 17 / 25 us, 256 rows 29 / 25; 24 blocks of 512 x 512, 256 rows 6.6 / 8.0, 512 rows 9.5 / 8.1; but 64 blocks of
+// 1024 x 2048, whose tiles fill the device with a row each, 64 rows 52 / 43, 1024 rows 58 / 45.  This one / the float32 ones:
+// one block of 2048 x 2048, 512 rows 88 / 108, 1024 rows 169 / 144; 8 blocks of 1024 x 1024, 1024 rows 48 / 58, 2048 rows
+// 90 / 75; 24 blocks of 96 x 35, 4096 rows 6.4 / 7.7, 8192 rows 9.6 / 7.9.
+bool few_rows_fit(const RowsArgs &r, bool wide)
+{
+    if (!wide) return r.rows <= 4096 && r.rows / 64 <= r.blocks + 8;
+    const u64 row_tiles = r.rows < r.blocks ? r.rows : r.blocks;
+    return (r.rows <= 128 || r.rows / 16 <= r.blocks) && row_tiles * ((r.cols + 127) / 128) < 512;
+}
 
 hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream)
 {

@@ -627,11 +627,21 @@ bool rows_sixteen(const RowsArgs &r)
     return r.sums % 8 == 0 && r.cols % 8 == 0 && sixteen(r.a, r.lda) && sixteen(r.w, r.ldw) && r.w_block % 8 == 0;
 }
 
+// Which tiles, from the rounds that the device's compute units take (all blocks but one end half a tile early in the mean).  Of 256 x 256
+// tiles a round is 256, and its costs come whole; of 128 x 128 it is 512, two workgroups a compute unit, with 0.7 of the time
+// for half of the results, and the two even out what a last round leaves.  8 ragged blocks of 1024 x 1024, large / small tiles: 4096 rows
+// 30 / 20 us, 16 384 56 / 48, 65 536 158 / 183; one of 512 x 512: 16 384 20 / 14, 32 768 23 / 31.
+bool large_tiles(const RowsArgs &r)
+{
+    const auto share = [&](u32 side) { return __builtin_ceilf((float)r.rows / side + 0.5f * (r.blocks - 1)) * ((r.cols + side - 1) / side); };
+    return __builtin_ceilf(share(256) / 256) < 0.7f * share(128) / 512;
+}
+
 template <bool ACROSS, u32 GATE>
 hipError_t wide_shape(const RowsArgs &r, hipStream_t stream)
 {
     if (!rows_sixteen(r)) return wide_go<128, 128, 2, 2, ACROSS, true, GATE>(r, stream);
-    if (r.cols > 128 && max_runs(r.rows, r.blocks, 256) * ((r.cols + 255) / 256) >= 256)
+    if (large_tiles(r))
         return wide_go<256, 256, 2, 4, ACROSS, false, GATE>(r, stream);
     return wide_go<128, 128, 2, 2, ACROSS, false, GATE>(r, stream);
 }

@@ -210,19 +210,21 @@ struct BlockRun {
 };
 
 // Number of slices (host) for tiles that `pairs` workgroups a slice sum, `slots` of them at once: the least of what the last turn's
-// workgroups take, with a run's own costs, and what a set of partial sums more costs, its bytes written and read.
+// workgroups take, with a run's own costs, and what a set of partial sums more costs, its bytes written and read.  A run's own costs (its
+// first loads, its results) are more than those of 64 rows: slices are not made shorter for their rows' sake, but for their
+// blocks' (64 rows in 64 blocks of 256 x 512, bfloat16, in slices of 64 rows: 486 us, of one row: 30).
 inline u32 slices_of(u32 rows, u32 blocks, u64 pairs, u32 slots, double row_us, u64 sums)
 {
     constexpr double kRunUs = 6.0;
     const double set_us = (double)sums * 8 / 4e6;
-    const u64 most = rows / 64 + 1;
+    const u64 most = (u64)rows / 64 + (rows < blocks ? rows : blocks);
     u32 best = 1;
     double least = -1;
     const auto look = [&](u64 n) {
         n = n < most ? n : most;
         if (n == 0) return;
         const double turns = (double)((n * pairs + slots - 1) / slots);
-        const double us = turns * ((double)rows / (double)n * row_us + (1.0 + (double)blocks / (double)n) * kRunUs) + (double)(n - 1) * set_us;
+        const double us = turns * ((double)rows / (double)n * row_us + (double)(blocks + n - 1) / (double)n * kRunUs) + (double)(n - 1) * set_us;
         if (least < 0 || us < least) {
             least = us;
             best = (u32)n;
@@ -235,8 +237,8 @@ inline u32 slices_of(u32 rows, u32 blocks, u64 pairs, u32 slots, double row_us, 
 // rows of each of `slices` slices: s * per stays below 2^32
 inline u32 rows_of_slice(u32 rows, u32 slices)
 {
-    const u32 per = (rows + slices - 1) / slices;
-    return per < 64 ? 64 : per;
+    const u32 per = (u32)(((u64)rows + slices - 1) / slices);
+    return per < 1 ? 1 : per;
 }
 
 // Upper bound of the number of runs (host): every block can end with a run that is not full.

@@ -281,14 +281,16 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
 
 // Joins the partial sums of the blocks that have several runs, in the order of the runs (the same bits every time), and
 // writes zeros for blocks without rows.  V consecutive sums a thread, AHEAD sets on their way: no sum waits for the one in
-// front of it, only its addition does.  Bound by memory where there are many sums (8 blocks of 1024 x 1024: 33 us), by the chain of
-// sets where there are few (24 blocks of 96 x 35: 5.5 us).
-template <u32 V, u32 AHEAD>
+// front of it, only its addition does.  Where there are few sums, and so many sets of them, PARTS parts of a workgroup take
+// consecutive sets each and the parts meet in LDS, in their order.  Bound by memory where there are many sums (32 blocks of 1024 x 1024: 33 us), by
+// the chain of sets where there are few.
+template <u32 V, u32 AHEAD, u32 PARTS>
 __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per, bool by_blocks,
                                                    const float *__restrict__ part, u32 n, u32 k, float *__restrict__ dw,
                                                    float *__restrict__ db, u32 pieces)
 {
     typedef __attribute__((ext_vector_type(V))) float vec;
+    constexpr u32 kWidth = 256 / PARTS;                 // threads along the sums
     const u32 block = blockIdx.x / pieces, piece = blockIdx.x - block * pieces;
     RowSlices all;
     all.init(offsets, blocks, rows, per);
@@ -299,19 +301,34 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
     if (runs == 1) return;
     const u64 size = (u64)n * k, stride = size + n;
     const float *p = part + (u64)(first + block) * stride;
+    const u32 share = (runs + PARTS - 1) / PARTS, part_of = threadIdx.x / kWidth;
+    const u32 from = part_of * share, to = from + share < runs ? from + share : runs;
     const auto sum = [&](auto zero, u64 at) {
         auto s = zero;
-        for (u32 q = 0; q < runs; q += AHEAD) {
+        for (u32 q = from; q < to; q += AHEAD) {
             decltype(zero) v[AHEAD];
 #pragma unroll
-            for (u32 h = 0; h < AHEAD; ++h) v[h] = load_any<decltype(zero)>(p + (u64)(q + h < runs ? q + h : q) * stride + at);
+            for (u32 h = 0; h < AHEAD; ++h) v[h] = load_any<decltype(zero)>(p + (u64)(q + h < to ? q + h : q) * stride + at);
 #pragma unroll
             for (u32 h = 0; h < AHEAD; ++h)
-                if (q + h < runs) s += v[h];
+                if (q + h < to) s += v[h];
         }
         return s;
     };
-    const u64 at = ((u64)piece * 256 + threadIdx.x) * V;
+    const u64 at = ((u64)piece * kWidth + threadIdx.x % kWidth) * V;
+    if constexpr (PARTS > 1) {
+        static_assert(V == 1, "a thread of each part for a sum");
+        __shared__ float parts[PARTS][kWidth];
+        const bool there = at < stride && (at < size ? dw != nullptr : db != nullptr);
+        parts[part_of][threadIdx.x % kWidth] = there ? sum(0.0f, at) : 0.0f;
+        __syncthreads();
+        if (part_of != 0 || !there) return;
+        float s = 0.0f;
+#pragma unroll
+        for (u32 q = 0; q < PARTS; ++q) s += parts[q][threadIdx.x];
+        (at < size ? dw[(u64)block * size + at] : db[(u64)block * n + (at - size)]) = s;
+        return;
+    }
     if (V > 1 && at + V <= size) {
         if (dw) store_any(dw + (u64)block * size + at, sum(vec{}, at));
         return;
@@ -432,11 +449,12 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
     const RunPlan plan = run_plan(l);
     float *part = reinterpret_cast<float *>(workspace);
     const auto join = [&](bool by_blocks) {
-        // few sums are many sets each, and latency; many are bytes
+        // few sums are many sets each, and latency; many are bytes (24 blocks of 96 x 35, 300 000 rows, gradients with
+        // few as many and as few: 94 / 93 us; one block: 128 / 97; 4 blocks of 1024 x 1024, 1000 rows: 33 / 38)
         const u64 stride = (u64)l.n * l.k + l.n;
-        const bool many = stride * l.blocks >= 1u << 21;
-        const u32 pieces = (u32)((stride + (many ? 1023 : 255)) / (many ? 1024 : 256));
-        auto kernel = many ? join_kernel<4, 4> : join_kernel<1, 8>;
+        const bool many = stride * l.blocks >= 1u << 20;
+        const u32 width = many ? 1024 : 32, pieces = (u32)((stride + width - 1) / width);
+        auto kernel = many ? join_kernel<4, 4, 1> : join_kernel<1, 4, 8>;
         hipLaunchKernelGGL(kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, plan.per, by_blocks, part,
                            l.n, l.k, out.dw, out.db, pieces);
         return hipGetLastError();

@@ -213,9 +213,12 @@ struct BlockRun {
 // workgroups take, with a run's own costs, and what a set of partial sums more costs, its bytes written and read.  A run's own costs (its
 // first loads, its results) are more than those of 64 rows: slices are not made shorter for their rows' sake, but for their
 // blocks' (64 rows in 64 blocks of 256 x 512, bfloat16, in slices of 64 rows: 486 us, of one row: 30).
-inline u32 slices_of(u32 rows, u32 blocks, u64 pairs, u32 slots, double row_us, u64 sums)
+struct Slices {
+    u32 count;
+    double us;              // expected
+};
+inline Slices slices_of(u32 rows, u32 blocks, u64 pairs, u32 slots, double row_us, double run_us, u64 sums)
 {
-    constexpr double kRunUs = 6.0;
     const double set_us = (double)sums * 8 / 4e6;
     const u64 most = (u64)rows / 64 + (rows < blocks ? rows : blocks);
     u32 best = 1;
@@ -224,7 +227,7 @@ inline u32 slices_of(u32 rows, u32 blocks, u64 pairs, u32 slots, double row_us, 
         n = n < most ? n : most;
         if (n == 0) return;
         const double turns = (double)((n * pairs + slots - 1) / slots);
-        const double us = turns * ((double)rows / (double)n * row_us + (double)(blocks + n - 1) / (double)n * kRunUs) + (double)(n - 1) * set_us;
+        const double us = turns * ((double)rows / (double)n * row_us + (double)(blocks + n - 1) / (double)n * run_us) + (double)(n - 1) * set_us;
         if (least < 0 || us < least) {
             least = us;
             best = (u32)n;
@@ -232,7 +235,7 @@ inline u32 slices_of(u32 rows, u32 blocks, u64 pairs, u32 slots, double row_us, 
     };
     for (u64 n = 1; n < 4096; n *= 2) look(n);
     for (u32 turns = 1; turns <= 4; ++turns) look((u64)turns * slots / pairs);
-    return best;
+    return Slices{best, least};
 }
 // rows of each of `slices` slices: s * per stays below 2^32
 inline u32 rows_of_slice(u32 rows, u32 slices)

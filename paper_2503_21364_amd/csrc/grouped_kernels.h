@@ -42,6 +42,7 @@ struct SumsArgs {
     u32 in_major;
     float *part;                // partial sums: n k of dw, then n of db each
     u32 slices, per;            // of the rows, and rows of each
+    u32 side;                   // of the bfloat16 kernel's tiles
     u32 tiles, n_tiles, k_tiles;
 };
 
@@ -95,7 +96,6 @@ hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t
 // bfloat16
 bool wide_rows_fit(const RowsArgs &r);
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream);
-u32 wide_sums_side(u32 n, u32 k);            // of its tiles
 bool wide_sums_fit(const SumsArgs &r);
 hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream);
 

@@ -389,11 +389,12 @@ static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l
 // how the sums over rows are shared out
 struct RunPlan {
     u32 per, slices;        // rows of a run or slice; sets of partial sums, less the blocks
+    u32 side;               // of the bfloat16 kernel's tiles
 };
 static RunPlan run_plan(const lmk_gs_linear &l)
 {
     const u64 sums = (u64)l.n * l.k + l.n;
-    RunPlan p;
+    RunPlan p = {};
     if (one_pass(l)) {
         // a run's own costs (the weights into LDS, the sums out of registers) are those of some hundred rows: one run a workgroup,
         // all of them at once, whole tiles for each wavefront
@@ -402,11 +403,21 @@ static RunPlan run_plan(const lmk_gs_linear &l)
         p.per = p.per < 64 ? 64 : p.per;
         p.slices = l.rows / p.per + 1;
     } else {
-        // time of a row of a tile: its products at the rate that a compute unit's share of the tiles reaches
-        const bool f32 = l.dtype == LMK_GS_F32;
-        const u32 side = f32 ? kTile : wide_sums_side(l.n, l.k), slots = f32 ? 1024 : side == 256 ? 256 : 512;
-        const u64 pairs = (u64)((l.n + side - 1) / side) * ((l.k + side - 1) / side);
-        p.slices = slices_of(l.rows, l.blocks, pairs, slots, 2.0 * side * side * slots / (f32 ? 1e8 : 1e9), sums);
+        // time of a row of a tile: its products at the rate (flop a us) that a compute unit's share of the tiles reaches
+        const auto look = [&](u32 side, u32 slots, double rate, double run_us) {
+            const u64 pairs = (u64)((l.n + side - 1) / side) * ((l.k + side - 1) / side);
+            return slices_of(l.rows, l.blocks, pairs, slots, 2.0 * side * side * slots / rate, run_us, sums);
+        };
+        if (l.dtype == LMK_GS_F32) {
+            p.slices = look(kTile, 1024, 1e8, 6.0).count;
+        } else {
+            // large tiles read less, small ones have less of a run's own costs, two workgroups a compute unit (8 blocks of
+            // 1024 x 1024, large / small: 4000 rows 57 / 42 us; 64 of 256 x 512, 1500 rows 60 / 32; 65 536 rows of 1024 x 1024
+            // in large ones)
+            const Slices small = look(128, 512, 0.8e9, 6.0), large = look(256, 256, 1e9, 10.0);
+            p.side = large.us < small.us ? 256 : 128;
+            p.slices = p.side == 256 ? large.count : small.count;
+        }
         p.per = rows_of_slice(l.rows, p.slices);
     }
     return p;
@@ -501,6 +512,7 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
     r.dw = out.dw; r.db = out.db; r.in_major = l.in_major;
     r.part = part;
     r.slices = plan.slices;
+    r.side = plan.side;
     r.per = plan.per;
     const u32 kind = !out.dw ? 0 : kept ? 2 : 1;
     hipError_t e = l.dtype == LMK_GS_F32 ? sums_as<float>(r, kind, stream) : sums_as<__bf16>(r, kind, stream);

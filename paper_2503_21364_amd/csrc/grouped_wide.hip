@@ -677,8 +677,6 @@ hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
     return gate == 0 ? wide_shape<false, 0>(r, stream) : gate == 1 ? wide_shape<false, 1>(r, stream) : wide_shape<false, 2>(r, stream);
 }
 
-u32 wide_sums_side(u32 n, u32 k) { return n > 128 && k > 128 ? 256 : 128; }
-
 bool wide_sums_fit(const SumsArgs &r)
 {
     constexpr u64 most = 1u << 21;
@@ -689,7 +687,7 @@ hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream)
 {
     const bool any = r.n % 8 || !sixteen(r.dy, r.lddy) || (!r.scale && (r.k % 8 || !sixteen(r.x, r.ldx))) || r.k % 4;
     if (any) return wide_sums_go<128, 128, 2, 2, true>(r, r.scale != nullptr, stream);
-    if (wide_sums_side(r.n, r.k) == 256) return wide_sums_go<256, 256, 2, 4, false>(r, r.scale != nullptr, stream);
+    if (r.side == 256) return wide_sums_go<256, 256, 2, 4, false>(r, r.scale != nullptr, stream);
     return wide_sums_go<128, 128, 2, 2, false>(r, r.scale != nullptr, stream);
 }
 

@@ -383,3 +383,63 @@ def test_gradient_against_differences():
         move = lambda h: loss(*[v + h * e if i == at else v for i, v in enumerate((x, w, b))])
         diff = (move(0.5) - move(-0.5))             # linear in each: exact but for rounding in 64 bits
         assert abs((_np(got) * e).sum() - diff) <= ((m + 2) * U * mag * np.abs(e)).sum() + 1e-9 * abs(diff)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("in_major", [False, True])
+def test_layers_whose_tiles_fill_the_device(in_major, dtype):
+    """Large tiles for the products of rows, with the 8-bit form written on the way and both kinds of gate; the grid has more
+    workgroups than there are tiles."""
+    t = Layer([29000, 0, 1003], 488, 504, dtype, in_major, front=5, behind=3, seed=11, relu_in=True)
+    keep, alone = t.kept(), t.kept()
+    t.forward(relu=True, keep=keep)
+    t.check_forward(relu=True)
+    inside = t.x.clone()
+    inside[:5] = 0
+    inside[-3:] = 0
+    B.checkpoint8_pack(inside, alone)
+    assert torch.equal(keep.codes, alone.codes) and torch.equal(keep.scale, alone.scale)
+    t.backward(gate=True)
+    t.check_backward(gate=True)
+    t.backward(keep, gate=True)
+    t.check_backward(G.unpack(keep.codes.cpu().numpy(), keep.scale.cpu().numpy(), 488), gate=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradients_of_large_matrices(dtype):
+    t = Layer([1400, 100], 4096, 4088, dtype, seed=12)
+    t.backward(which=("dw", "db"))
+    t.check_backward(which=("dw", "db"))
+    keep = t.kept()
+    B.checkpoint8_pack(t.x, keep)
+    t.backward(keep, which=("dw", "db"))
+    t.check_backward(G.unpack(keep.codes.cpu().numpy(), keep.scale.cpu().numpy(), 4096), which=("dw", "db"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k,n", [(35, 96), (136, 264), (257, 131)])
+@pytest.mark.parametrize("rows", [1, 64, 200, 1500])
+def test_many_blocks_of_few_rows(rows, k, n, dtype):
+    """Slices of the rows of a row or two, that begin and end anywhere in the blocks."""
+    g = torch.Generator().manual_seed(rows)
+    sizes = torch.bincount(torch.randint(0, 70, (rows,), generator=g), minlength=70).tolist()
+    t = Layer(sizes, k, n, dtype, front=2, behind=1, seed=rows + 1, relu_in=True)
+    t.forward()
+    t.check_forward()
+    t.backward(gate=True)
+    t.check_backward(gate=True)
+    first = [q.clone() for q in (t.dx, t.dw, t.db)]
+    t.backward(gate=True)
+    for a, b in zip(first, (t.dx, t.dw, t.db)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("k,n", [(35, 96), (32, 70), (8, 8), (64, 33)])
+def test_many_sets_of_few_sums(k, n):
+    t = Layer([30011, 0, 64, 65], k, n, seed=13)
+    t.backward()
+    t.check_backward()
+    t.backward(which=("db",))
+    t.check_backward(which=("db",))
+    t.backward(which=("dw",))
+    t.check_backward(which=("dw",))

@@ -7,8 +7,8 @@
 // Float32 matrix instructions (v_mfma_f32_32x32x2_f32: products and sums in 32 bits); bfloat16 operands are widened
 // while they are staged, which is exact.
 //
-// Bound by the rate of that instruction (154 TFLOP/s is what the largest library product reaches): 102 - 104 TFLOP/s at
-// 8192 rows x 4096 x 4096, 80 at 65 536 x 256 x 256.
+// Bound by the rate of that instruction (154 TFLOP/s is what the largest library product reaches): 102 - 106 TFLOP/s at
+// 8192 rows x 4096 x 4096, 84 at 65 536 x 256 x 256 in 32 blocks.
 //
 // Both operands of a tile pass through LDS as [sum index][row or column]: a lane of half `hi` feeds sum
 // index t + 16 hi to step t, so the 32 lanes of a half read 32 consecutive floats, and with a pitch of 66
@@ -464,8 +464,10 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
         // few as many and as few: 94 / 93 us; one block: 128 / 97; 4 blocks of 1024 x 1024, 1000 rows: 33 / 38)
         const u64 stride = (u64)l.n * l.k + l.n;
         const bool many = stride * l.blocks >= 1u << 20;
-        const u32 width = many ? 1024 : 32, pieces = (u32)((stride + width - 1) / width);
-        auto kernel = many ? join_kernel<4, 4, 1> : join_kernel<1, 4, 8>;
+        // few sets a block are not worth parts (7 blocks of 131 x 257, 71 sets: 7.5 us with them, 4.0 without)
+        const bool parts = !many && plan.slices / l.blocks >= 16;
+        const u32 width = many ? 1024 : parts ? 32 : 256, pieces = (u32)((stride + width - 1) / width);
+        auto kernel = many ? join_kernel<4, 4, 1> : parts ? join_kernel<1, 4, 8> : join_kernel<1, 8, 1>;
         hipLaunchKernelGGL(kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, plan.per, by_blocks, part,
                            l.n, l.k, out.dw, out.db, pieces);
         return hipGetLastError();

@@ -1,14 +1,14 @@
 // Grouped layers in bfloat16: the same products as in grouped_linear.hip on the bfloat16 matrix instructions
 // (v_mfma_f32_16x16x32_bf16: exact products, sums in 32 bits; only results are rounded, once).
 //
-// Bound by those instructions and by LDS, which feeds them: 8192 x 8192 x 8192 in 800 - 966 (forward), 1030 - 1070 (dx), 1130 - 1160
+// Bound by those instructions and by LDS, which feeds them: 8192 x 8192 x 8192 at 1000 (forward), 1260 (dx), 1210
 // (dw) and 1030 - 1080 TFLOP/s (dw from the 8-bit form); the largest library product reaches 1268.  65 536 rows in 32 ragged blocks
 // of 1024 x 1024 (137 GFLOP a product): forward with the 8-bit form 232 us, dx with its gate 221 - 226, dw and db 191 - 198.
 // There 1076 tiles take five rounds of 256 workgroups where 4.2 would do, and a round's first loads and last stores have no
 // products beside them: the accumulators and two steps' fragments of a lane leave no registers for the next tile's.
 //
 // Tiles of 256 x 256, two wavefronts a SIMD: LDS gives a step's fragments in less time than their products take, which it
-// does not for 128 x 128 (65 536 x 1024 x 1024: 202 us) or 256 x 128 (231 us).
+// does not for 128 x 128 (65 536 x 1024 x 1024 in 8 blocks: 183 us, large tiles 156) or 256 x 128 (slower than both).
 #include "grouped.h"
 #include "grouped_kernels.h"
 

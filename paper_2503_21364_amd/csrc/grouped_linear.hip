@@ -414,7 +414,7 @@ static RunPlan run_plan(const lmk_gs_linear &l)
             // large tiles read less, small ones have less of a run's own costs, two workgroups a compute unit (8 blocks of
             // 1024 x 1024, large / small: 4000 rows 57 / 42 us; 64 of 256 x 512, 1500 rows 60 / 32; 65 536 rows of 1024 x 1024
             // in large ones)
-            const Slices small = look(128, 512, 0.8e9, 6.0), large = look(256, 256, 1e9, 10.0);
+            const Slices small = look(128, 512, 0.8e9, 4.0), large = look(256, 256, 1e9, 10.0);
             p.side = large.us < small.us ? 256 : 128;
             p.slices = p.side == 256 ? large.count : small.count;
         }

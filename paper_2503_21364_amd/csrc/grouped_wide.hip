@@ -256,6 +256,16 @@ template <u32 TP, u32 TQ, u32 WP, u32 WQ> struct Shape {
     static constexpr u32 kResident = 512 / kThreads;                     // workgroups of a compute unit
 };
 
+// The wavefronts meet, each with no more loads and LDS accesses on their way than WAIT says.  Neither builtin promises an order to the
+// memory accesses around it: the two empty statements keep stores to LDS in front of the meeting and reads behind it.
+template <u32 WAIT> __device__ __forceinline__ void wavefronts_meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(WAIT);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 // acc[i][j] += P Q over `steps`.  LDS holds two pairs of steps.  A step's fragments are read from LDS while the step in front of
 // it is multiplied; once the second step's are with all wavefronts, the pair's part is filled again, which has the
 // time of two steps to arrive.  One meeting of the wavefronts a pair.
@@ -288,9 +298,7 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
     };
     fill(0);
     fill(1);
-    __builtin_amdgcn_s_waitcnt(kDirect ? 0xF70 | 8 : 0x070);        // the second pair's eight loads may be on their way
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
+    wavefronts_meet<kDirect ? 0xF70 | 8 : 0x070>();                 // the second pair's eight loads may be on their way
 #pragma unroll
     for (u32 i = 0; i < S::kP; ++i) fp[i] = p.fragment(lp, 0, p0, i);
 #pragma unroll
@@ -304,10 +312,7 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
             step(0, part, 1);
             if (t + 1 >= steps) break;
             // the next pair has arrived, and this pair's fragments have left LDS
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_waitcnt(0x070);
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
+            wavefronts_meet<0x070>();
             fill(part);
             step(1, 1 - part, 0);
         }

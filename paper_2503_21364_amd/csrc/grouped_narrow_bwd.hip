@@ -55,6 +55,10 @@ template <u32 N> struct CodePieces {
 
 constexpr u32 kFillers = 64;            // workgroups for dx of rows of no block
 
+// Steps of dx's product, four outputs each, in whole turns of four.  Those behind the last output have zeros on both sides: a
+// weight that is not finite, multiplied by a zero of dy, would be a NaN.
+__host__ __device__ constexpr u32 whole_steps(u32 n) { return (n + 15) / 16 * 4; }
+
 // floats between the outputs of the joined sums in LDS
 constexpr u32 sums_pitch(u32 ck) { return 16 * ck + 4; }
 constexpr u32 sums_floats(u32 cn, u32 ck) { return 16 * cn * sums_pitch(ck) + 16 * cn; }
@@ -83,8 +87,10 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
     BlockRun run;
     if (!run.find(r.offsets, r.blocks, r.rows, r.per, blockIdx.x)) return;
     const u32 row0 = run.row, height = run.count, lane = threadIdx.x & (kWave - 1), j = lane & 15, q = lane >> 4;
-    if (r.dx)
+    if (r.dx) {
         stage_weights<float, CK>(lw, r.w + (u64)run.block * r.w_block, r.ldw, r.in_major == 0, r.n, r.k);
+        for (u32 i = steps * CK * kWave + threadIdx.x; i < whole_steps(r.n) * CK * kWave; i += 256) lw[i] = 0.0f;
+    }
     __syncthreads();
 
     const u32 tiles = (height + kTileRows - 1) / kTileRows;
@@ -138,15 +144,16 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
         }
         f32x4 acc[CK] = {};
         if (r.dx) {
-            // two steps' operands are on their way from LDS while two are multiplied; behind the last one zeros
+            // two steps' operands are on their way from LDS while two are multiplied; behind the last one zeros.  Behind the last whole
+            // turn: what lies there in LDS, and is not multiplied
             float v[2][2], w[2][2][CK];
             auto fetch = [&](u32 s, u32 at) {
 #pragma unroll
                 for (u32 e = 0; e < 2; ++e) {
-                    const u32 t = s + e < steps ? s + e : steps - 1;
-                    v[at][e] = s + e < steps ? ly[j * pn + 4 * t + q] : 0.0f;
+                    const float y = ly[j * pn + 4 * (s + e) + q];
+                    v[at][e] = s + e < steps ? y : 0.0f;
 #pragma unroll
-                    for (u32 c = 0; c < CK; ++c) w[at][e][c] = lw[(t * CK + c) * kWave + lane];
+                    for (u32 c = 0; c < CK; ++c) w[at][e][c] = lw[((s + e) * CK + c) * kWave + lane];
                 }
             };
             auto multiply = [&](u32 at) {
@@ -224,7 +231,7 @@ __global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel
 template <u32 CN, u32 CK>
 hipError_t narrow_backward_go(BackwardArgs r, bool codes, hipStream_t stream)
 {
-    const u32 weights = (r.n + 3) / 4 * CK * kWave, sums = 4 * sums_floats(CN, CK);
+    const u32 weights = whole_steps(r.n) * CK * kWave, sums = 4 * sums_floats(CN, CK);
     const u32 tiles = 4 * kTileRows * (pitch_of(r.n) + pitch_of(r.k));
     r.shared = weights;
     const u32 lds = (weights + tiles > sums ? weights + tiles : sums) * 4;

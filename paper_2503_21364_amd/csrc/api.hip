@@ -335,7 +335,6 @@ static int32_t check_linear(const lmk_gs_linear *l)
     if (l->ldw < inner || l->ldw > kMaxStride) return LMK_GS_ERR_INVALID;
     if (l->blocks > 1 && (l->w_block < (outer - 1) * l->ldw + inner || l->w_block > kMaxBlockStride)) return LMK_GS_ERR_INVALID;
     if (!l->w || !l->offsets || !aligned(l->w, size_of(l->dtype)) || !aligned(l->offsets, 4)) return LMK_GS_ERR_INVALID;
-    if (!grouped_linear_fits(*l)) return LMK_GS_ERR_UNSUPPORTED;
     return LMK_GS_OK;
 }
 
@@ -356,6 +355,7 @@ int32_t lmk_gs_grouped_linear(const lmk_gs_linear *layer, const void *x, uint64_
     if (layer->rows == 0) return LMK_GS_OK;
     if (!good_rows(x, ldx, layer->k, layer->dtype) || !good_rows(y, ldy, layer->n, layer->dtype)) return LMK_GS_ERR_INVALID;
     if (keep && !good_checkpoint(keep)) return LMK_GS_ERR_INVALID;
+    if (!grouped_linear_fits(*layer)) return LMK_GS_ERR_UNSUPPORTED;
     const hipError_t e = launch_grouped_linear(*layer, x, ldx, bias, relu != 0, y, ldy, keep, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
@@ -365,6 +365,7 @@ int32_t lmk_gs_grouped_linear_backward_bytes(const lmk_gs_linear *layer, size_t 
     const int32_t rc = check_linear(layer);
     if (rc != LMK_GS_OK) return rc;
     if (!bytes) return LMK_GS_ERR_INVALID;
+    if (!grouped_backward_fits(*layer, true, true)) return LMK_GS_ERR_UNSUPPORTED;
     *bytes = grouped_backward_bytes(*layer);
     return LMK_GS_OK;
 }
@@ -386,6 +387,7 @@ int32_t lmk_gs_grouped_linear_backward(const lmk_gs_linear *layer, const void *d
         if (x && !good_rows(x, ldx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
         if (kept && !good_checkpoint(kept)) return LMK_GS_ERR_INVALID;
     }
+    if (!grouped_backward_fits(*layer, out->dx != nullptr, sums)) return LMK_GS_ERR_UNSUPPORTED;
     if (sums) {
         if (!workspace || !aligned(workspace, 256)) return LMK_GS_ERR_INVALID;
         if (workspace_bytes < grouped_backward_bytes(*layer)) return LMK_GS_ERR_CAPACITY;

@@ -423,13 +423,15 @@ static RunPlan run_plan(const lmk_gs_linear &l)
     return p;
 }
 
-bool grouped_linear_fits(const lmk_gs_linear &l)
+// products of rows: y, dx
+bool grouped_linear_fits(const lmk_gs_linear &l) { return max_runs(l.rows, l.blocks, kTile) * (((l.n > l.k ? l.n : l.k) + 31) / 32) < 1ull << 31; }
+
+bool grouped_backward_fits(const lmk_gs_linear &l, bool dx, bool sums)
 {
-    const u64 runs = max_runs(l.rows, l.blocks, kTile);
-    const u64 pairs = (u64)((l.n + kTile - 1) / kTile) * ((l.k + kTile - 1) / kTile);
-    const u64 widest = l.n > l.k ? l.n : l.k;
-    return runs * ((widest + 31) / 32) < 1ull << 31 && run_plan(l).slices * pairs < 1ull << 31 && (u64)run_plan(l).slices + l.blocks < 1ull << 30 &&
-           (((u64)l.n * l.k + l.n + 255) / 256) * l.blocks < 1ull << 31;
+    if (dx && !grouped_linear_fits(l)) return false;
+    if (!sums) return true;
+    const u64 pairs = (u64)((l.n + kTile - 1) / kTile) * ((l.k + kTile - 1) / kTile), slices = run_plan(l).slices;
+    return slices * pairs < 1ull << 31 && slices + l.blocks < 1ull << 30 && (((u64)l.n * l.k + l.n + 255) / 256) * l.blocks < 1ull << 31;
 }
 
 size_t grouped_backward_bytes(const lmk_gs_linear &l)

@@ -170,8 +170,9 @@ hipError_t launch_checkpoint8_pack(const void *x, u64 ldx, u32 rows, u32 k, u32 
                                    const lmk_gs_checkpoint8 &out, hipStream_t stream);
 hipError_t launch_checkpoint8_unpack(const lmk_gs_checkpoint8 &kept, u32 rows, u32 k, u32 dtype, void *x, u64 ldx,
                                      hipStream_t stream);
-// the grouped layers: whether their launches fit a grid, and the bytes of partial sums of the gradient
+// the grouped layers: whether what a call launches fits a grid, and the bytes of partial sums of the gradient
 bool grouped_linear_fits(const lmk_gs_linear &l);
+bool grouped_backward_fits(const lmk_gs_linear &l, bool dx, bool sums);
 size_t grouped_backward_bytes(const lmk_gs_linear &l);
 hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
                                  u64 ldy, const lmk_gs_checkpoint8 *keep, hipStream_t stream);

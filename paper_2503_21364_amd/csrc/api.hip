@@ -355,7 +355,7 @@ int32_t lmk_gs_grouped_linear(const lmk_gs_linear *layer, const void *x, uint64_
     if (layer->rows == 0) return LMK_GS_OK;
     if (!good_rows(x, ldx, layer->k, layer->dtype) || !good_rows(y, ldy, layer->n, layer->dtype)) return LMK_GS_ERR_INVALID;
     if (keep && !good_checkpoint(keep)) return LMK_GS_ERR_INVALID;
-    if (!grouped_linear_fits(*layer)) return LMK_GS_ERR_UNSUPPORTED;
+    if (!grouped_linear_fits(*layer, x, ldx, y, ldy, keep)) return LMK_GS_ERR_UNSUPPORTED;
     const hipError_t e = launch_grouped_linear(*layer, x, ldx, bias, relu != 0, y, ldy, keep, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
@@ -365,7 +365,10 @@ int32_t lmk_gs_grouped_linear_backward_bytes(const lmk_gs_linear *layer, size_t 
     const int32_t rc = check_linear(layer);
     if (rc != LMK_GS_OK) return rc;
     if (!bytes) return LMK_GS_ERR_INVALID;
-    if (!grouped_backward_fits(*layer, true, true)) return LMK_GS_ERR_UNSUPPORTED;
+    // all gradients, of packed rows: the pointers are only told from NULL
+    float any = 0.0f;
+    const lmk_gs_linear_grads all = {&any, layer->k, &any, &any};
+    if (!grouped_backward_fits(*layer, nullptr, layer->n, nullptr, layer->k, nullptr, false, all)) return LMK_GS_ERR_UNSUPPORTED;
     *bytes = grouped_backward_bytes(*layer);
     return LMK_GS_OK;
 }
@@ -387,7 +390,7 @@ int32_t lmk_gs_grouped_linear_backward(const lmk_gs_linear *layer, const void *d
         if (x && !good_rows(x, ldx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
         if (kept && !good_checkpoint(kept)) return LMK_GS_ERR_INVALID;
     }
-    if (!grouped_backward_fits(*layer, out->dx != nullptr, sums)) return LMK_GS_ERR_UNSUPPORTED;
+    if (!grouped_backward_fits(*layer, dy, lddy, x, ldx, kept, gate != 0, *out)) return LMK_GS_ERR_UNSUPPORTED;
     if (sums) {
         if (!workspace || !aligned(workspace, 256)) return LMK_GS_ERR_INVALID;
         if (workspace_bytes < grouped_backward_bytes(*layer)) return LMK_GS_ERR_CAPACITY;
@@ -403,7 +406,7 @@ static int32_t check_checkpoint(const void *x, uint64_t ldx, uint32_t rows, uint
     if (dtype != LMK_GS_F32 && dtype != LMK_GS_BF16) return LMK_GS_ERR_UNSUPPORTED;
     if (!c || k == 0 || k > kMaxWidth || rows >= 1u << 31) return LMK_GS_ERR_INVALID;
     if (rows > 0 && (!good_rows(x, ldx, k, dtype) || !good_checkpoint(c))) return LMK_GS_ERR_INVALID;
-    return checkpoint8_blocks(rows, k) < 1ull << 31 ? LMK_GS_OK : LMK_GS_ERR_UNSUPPORTED;
+    return checkpoint8_threads(rows, k) < kMostThreads ? LMK_GS_OK : LMK_GS_ERR_UNSUPPORTED;
 }
 
 int32_t lmk_gs_checkpoint8_pack(const void *x, uint64_t ldx, uint32_t rows, uint32_t k, uint32_t dtype,

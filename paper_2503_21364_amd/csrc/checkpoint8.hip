@@ -115,13 +115,15 @@ hipError_t unpack_as(const lmk_gs_checkpoint8 &kept, u32 rows, u32 k, void *x, u
 
 }  // namespace
 
-u64 checkpoint8_blocks(u32 rows, u32 k) { return ((u64)rows * ((k + 31) / 32 * 8) + kPerBlock - 1) / kPerBlock; }
+static u64 workgroups(u32 rows, u32 k) { return ((u64)rows * ((k + 31) / 32 * 8) + kPerBlock - 1) / kPerBlock; }
+
+u64 checkpoint8_threads(u32 rows, u32 k) { return workgroups(rows, k) * 256; }
 
 hipError_t launch_checkpoint8_pack(const void *x, u64 ldx, u32 rows, u32 k, u32 dtype, const u32 *offsets, u32 blocks,
                                    const lmk_gs_checkpoint8 &out, hipStream_t stream)
 {
     if (rows == 0) return hipSuccess;
-    const u32 grid = (u32)checkpoint8_blocks(rows, k);
+    const u32 grid = (u32)workgroups(rows, k);
     return dtype == LMK_GS_F32 ? pack_as<float>(x, ldx, rows, k, offsets, blocks, out, grid, stream)
                                : pack_as<__bf16>(x, ldx, rows, k, offsets, blocks, out, grid, stream);
 }
@@ -130,7 +132,7 @@ hipError_t launch_checkpoint8_unpack(const lmk_gs_checkpoint8 &kept, u32 rows, u
                                      hipStream_t stream)
 {
     if (rows == 0) return hipSuccess;
-    const u32 grid = (u32)checkpoint8_blocks(rows, k);
+    const u32 grid = (u32)workgroups(rows, k);
     return dtype == LMK_GS_F32 ? unpack_as<float>(kept, rows, k, x, ldx, grid, stream)
                                : unpack_as<__bf16>(kept, rows, k, x, ldx, grid, stream);
 }

@@ -115,15 +115,19 @@ hipError_t few_go(RowsArgs r, hipStream_t stream)
     hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, WHOLE, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
     return hipGetLastError();
 }
+// Columns of a workgroup.  64 make whole lines where columns are contiguous (8 blocks of 1024 x 1024 in bfloat16, 128 rows, 64 / 16
+// columns: 10.5 / 14.3 us; one row: 8.9 / 5.3), and read x once for four results where they are not (one block of 2048 x 2048
+// in float32, 128 rows: 24 / 31 us); 16 where that leaves compute units without work (8 blocks of 1024 x 1024, 128 rows: 10.3 / 7.0)
+u32 few_columns(const RowsArgs &r, bool across)
+{
+    return max_runs(r.rows, r.blocks, kRows) * ((r.cols + 63) / 64) >= (across ? 64 : 320) ? 64 : 16;
+}
 template <class T, bool ACROSS, u32 GATE>
 hipError_t few_width(const RowsArgs &r, hipStream_t stream)
 {
     constexpr u32 v = ACROSS ? 4 : 16 / sizeof(T);          // a run of x, and of the weights
     const bool whole = r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
-    // 64 columns make whole lines where columns are contiguous (8 blocks of 1024 x 1024 in bfloat16, 128 rows, 64 / 16 columns:
-    // 10.5 / 14.3 us; one row: 8.9 / 5.3), and read x once for four results where they are not (one block of 2048 x 2048
-    // in float32, 128 rows: 24 / 31 us); 16 where that leaves compute units without work (8 blocks of 1024 x 1024, 128 rows: 10.3 / 7.0)
-    if (max_runs(r.rows, r.blocks, kRows) * ((r.cols + 63) / 64) >= (ACROSS ? 64 : 320))
+    if (few_columns(r, ACROSS) == 64)
         return whole ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
     return whole ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
 }
@@ -147,6 +151,12 @@ bool few_rows_fit(const RowsArgs &r, bool wide)
     if (!wide) return r.rows <= 4096 && r.rows / 64 <= r.blocks + 8;
     const u64 row_tiles = r.rows < r.blocks ? r.rows : r.blocks;
     return (r.rows <= 128 || r.rows / 16 <= r.blocks) && row_tiles * ((r.cols + 127) / 128) < 512;
+}
+
+u64 few_rows_threads(const RowsArgs &r, bool across)
+{
+    const u32 nt = few_columns(r, across);
+    return max_runs(r.rows, r.blocks, kRows) * ((r.cols + nt - 1) / nt) * 512;
 }
 
 hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream)

@@ -81,12 +81,15 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total, u32 at_once)
     return id < whole ? (k / run * dies + die) * run + k % run : whole + die * run + k;
 }
 
+// `..._threads`: those that a launch would have
 // few rows, any type and alignment
 bool few_rows_fit(const RowsArgs &r, bool wide);
+u64 few_rows_threads(const RowsArgs &r, bool across);
 hipError_t launch_few_rows(const RowsArgs &r, u32 dtype, bool across, hipStream_t stream);
 
 // small matrices, float32
 bool narrow_rows_fit(const RowsArgs &r);
+u64 narrow_rows_threads(const RowsArgs &r);
 hipError_t launch_narrow_rows(RowsArgs r, bool across, hipStream_t stream);
 
 bool narrow_backward_fits(const BackwardArgs &r, bool codes);
@@ -95,8 +98,10 @@ hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t
 
 // bfloat16
 bool wide_rows_fit(const RowsArgs &r);
+u64 wide_rows_threads(const RowsArgs &r);
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream);
 bool wide_sums_fit(const SumsArgs &r);
+u64 wide_sums_threads(const SumsArgs &r);
 hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream);
 
 }  // namespace lmk

@@ -339,6 +339,31 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
     }
 }
 
+// Which kernel a product of rows takes, and whether the 8-bit form of a is written by itself, in front of it.
+enum class RowsKernel { few, wide, narrow, all };
+struct RowsChoice {
+    RowsKernel kernel;
+    bool pack;
+};
+RowsChoice rows_choice(const RowsArgs &r, u32 dtype)
+{
+    const bool wide = dtype == LMK_GS_BF16 && wide_rows_fit(r), narrow = dtype == LMK_GS_F32 && narrow_rows_fit(r);
+    const bool few = few_rows_fit(r, wide) && !(narrow && r.keep_codes);
+    return RowsChoice{few ? RowsKernel::few : wide ? RowsKernel::wide : narrow ? RowsKernel::narrow : RowsKernel::all,
+                      r.keep_codes && (few || !(wide || narrow))};
+}
+// of its largest launch
+u64 rows_threads(const RowsArgs &r, u32 dtype, bool across)
+{
+    const RowsChoice choice = rows_choice(r, dtype);
+    const u64 pack = choice.pack ? checkpoint8_threads(r.rows, r.sums) : 0;
+    const u64 product = choice.kernel == RowsKernel::few      ? few_rows_threads(r, across)
+                        : choice.kernel == RowsKernel::wide   ? wide_rows_threads(r)
+                        : choice.kernel == RowsKernel::narrow ? narrow_rows_threads(r)
+                                                              : max_runs(r.rows, r.blocks, kTile) * ((r.cols + kTile - 1) / kTile) * kThreads;
+    return pack > product ? pack : product;
+}
+
 template <class T, bool ACROSS>
 hipError_t rows_go(RowsArgs r, u32 gate, hipStream_t stream)
 {
@@ -353,24 +378,31 @@ template <class T>
 hipError_t rows_as(RowsArgs r, bool across, hipStream_t stream)
 {
     constexpr u32 dtype = std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16;
-    const bool wide = dtype == LMK_GS_BF16 && wide_rows_fit(r), narrow = dtype == LMK_GS_F32 && narrow_rows_fit(r);
-    const bool few = few_rows_fit(r, wide) && !(narrow && r.keep_codes);
-    if (r.keep_codes && (few || !(wide || narrow))) {
+    const RowsChoice choice = rows_choice(r, dtype);
+    if (choice.pack) {
         const lmk_gs_checkpoint8 keep = {reinterpret_cast<int8_t *>(r.keep_codes), r.keep_scale};
         const hipError_t e = launch_checkpoint8_pack(r.a, r.lda, r.rows, r.sums, dtype, r.offsets, r.blocks, keep, stream);
         if (e != hipSuccess) return e;
     }
-    if (few) return launch_few_rows(r, dtype, across, stream);
-    if (wide) return launch_wide_rows(r, across, stream);
-    if (narrow) return launch_narrow_rows(r, across, stream);
+    if (choice.kernel == RowsKernel::few) return launch_few_rows(r, dtype, across, stream);
+    if (choice.kernel == RowsKernel::wide) return launch_wide_rows(r, across, stream);
+    if (choice.kernel == RowsKernel::narrow) return launch_narrow_rows(r, across, stream);
     const u32 gate = !r.gate ? 0 : r.gate_scale ? 2 : 1;
     return across ? rows_go<T, true>(r, gate, stream) : rows_go<T, false>(r, gate, stream);
+}
+
+// kind: as sums_kernel's
+bool sums_wide(const SumsArgs &r, u32 dtype, u32 kind) { return dtype == LMK_GS_BF16 && kind != 0 && wide_sums_fit(r); }
+u64 sums_threads(const SumsArgs &r, u32 dtype, u32 kind)
+{
+    if (sums_wide(r, dtype, kind)) return wide_sums_threads(r);
+    return (u64)r.slices * ((r.n + kTile - 1) / kTile) * (kind == 0 ? 1 : (r.k + kTile - 1) / kTile) * kThreads;
 }
 
 template <class T>
 hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 {
-    if (std::is_same<T, __bf16>::value && kind != 0 && wide_sums_fit(r)) return launch_wide_sums(r, stream);
+    if (sums_wide(r, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, kind)) return launch_wide_sums(r, stream);
     r.n_tiles = (r.n + kTile - 1) / kTile;
     r.k_tiles = kind == 0 ? 1 : (r.k + kTile - 1) / kTile;
     r.tiles = (u32)((u64)r.slices * r.n_tiles * r.k_tiles);
@@ -423,24 +455,28 @@ static RunPlan run_plan(const lmk_gs_linear &l)
     return p;
 }
 
-// products of rows: y, dx
-bool grouped_linear_fits(const lmk_gs_linear &l) { return max_runs(l.rows, l.blocks, kTile) * (((l.n > l.k ? l.n : l.k) + 31) / 32) < 1ull << 31; }
-
-bool grouped_backward_fits(const lmk_gs_linear &l, bool dx, bool sums)
+// How the partial sums are joined
+struct JoinShape {
+    bool many, parts;
+    u32 pieces;             // workgroups of a block
+};
+static JoinShape join_shape(const lmk_gs_linear &l, const RunPlan &plan)
 {
-    if (dx && !grouped_linear_fits(l)) return false;
-    if (!sums) return true;
-    const u64 pairs = (u64)((l.n + kTile - 1) / kTile) * ((l.k + kTile - 1) / kTile), slices = run_plan(l).slices;
-    return slices * pairs < 1ull << 31 && slices + l.blocks < 1ull << 30 && (((u64)l.n * l.k + l.n + 255) / 256) * l.blocks < 1ull << 31;
+    // few sums are many sets each, and latency; many are bytes (24 blocks of 96 x 35, 300 000 rows, gradients with
+    // few as many and as few: 94 / 93 us; one block: 128 / 97; 4 blocks of 1024 x 1024, 1000 rows: 33 / 38)
+    const u64 stride = (u64)l.n * l.k + l.n;
+    JoinShape j;
+    j.many = stride * l.blocks >= 1u << 20;
+    // few sets a block are not worth parts (7 blocks of 131 x 257, 71 sets: 7.5 us with them, 4.0 without)
+    j.parts = !j.many && plan.slices / l.blocks >= 16;
+    const u32 width = j.many ? 1024 : j.parts ? 32 : 256;
+    j.pieces = (u32)((stride + width - 1) / width);
+    return j;
 }
 
-size_t grouped_backward_bytes(const lmk_gs_linear &l)
-{
-    return (size_t)(((u64)run_plan(l).slices + l.blocks) * ((u64)l.n * l.k + l.n) * 4);
-}
-
-hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
-                                 u64 ldy, const lmk_gs_checkpoint8 *keep, hipStream_t stream)
+// ---- what the calls hand to the kernels
+static RowsArgs forward_args(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y, u64 ldy,
+                             const lmk_gs_checkpoint8 *keep)
 {
     RowsArgs r = {};
     if (keep) {
@@ -451,62 +487,26 @@ hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx,
     r.w = l.w; r.ldw = l.ldw; r.w_block = l.w_block;
     r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.cols = l.n; r.sums = l.k;
     r.out = y; r.ldo = ldy; r.bias = bias; r.relu = relu;
-    return l.dtype == LMK_GS_F32 ? rows_as<float>(r, l.in_major != 0, stream) : rows_as<__bf16>(r, l.in_major != 0, stream);
+    return r;
 }
-
-hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx,
-                                   const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
-                                   char *workspace, hipStream_t stream)
+static RowsArgs dx_args(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx, const lmk_gs_checkpoint8 *kept,
+                        bool gate, const lmk_gs_linear_grads &out)
 {
-    const u32 kp = (l.k + 31) / 32 * 32;
-    const RunPlan plan = run_plan(l);
-    float *part = reinterpret_cast<float *>(workspace);
-    const auto join = [&](bool by_blocks) {
-        // few sums are many sets each, and latency; many are bytes (24 blocks of 96 x 35, 300 000 rows, gradients with
-        // few as many and as few: 94 / 93 us; one block: 128 / 97; 4 blocks of 1024 x 1024, 1000 rows: 33 / 38)
-        const u64 stride = (u64)l.n * l.k + l.n;
-        const bool many = stride * l.blocks >= 1u << 20;
-        // few sets a block are not worth parts (7 blocks of 131 x 257, 71 sets: 7.5 us with them, 4.0 without)
-        const bool parts = !many && plan.slices / l.blocks >= 16;
-        const u32 width = many ? 1024 : parts ? 32 : 256, pieces = (u32)((stride + width - 1) / width);
-        auto kernel = many ? join_kernel<4, 4, 1> : parts ? join_kernel<1, 4, 8> : join_kernel<1, 8, 1>;
-        hipLaunchKernelGGL(kernel, dim3(pieces * l.blocks), dim3(256), 0, stream, l.offsets, l.blocks, l.rows, plan.per, by_blocks, part,
-                           l.n, l.k, out.dw, out.db, pieces);
-        return hipGetLastError();
-    };
-    if (one_pass(l) && (out.dw || out.db)) {
-        BackwardArgs r = {};
-        r.dy = static_cast<const float *>(dy); r.lddy = lddy;
-        if (out.dw || (out.dx && gate)) {
-            r.x = kept ? (const void *)kept->codes : x;
-            r.ldx = ldx;
-            r.scale = kept ? kept->scale : nullptr;
-        }
-        r.w = static_cast<const float *>(l.w); r.ldw = l.ldw; r.w_block = l.w_block;
-        r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.n = l.n; r.k = l.k;
-        r.in_major = l.in_major; r.gate = gate;
-        r.dx = static_cast<float *>(out.dx); r.lddx = out.lddx; r.dw = out.dw; r.db = out.db;
-        r.part = part; r.runs = plan.slices + l.blocks; r.per = plan.per;
-        if (narrow_backward_fits(r, kept != nullptr)) {
-            const hipError_t e = launch_narrow_backward(r, kept != nullptr, stream);
-            return e == hipSuccess ? join(true) : e;
-        }
+    RowsArgs r = {};
+    r.a = dy; r.lda = lddy;
+    r.w = l.w; r.ldw = l.ldw; r.w_block = l.w_block;
+    r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.cols = l.k; r.sums = l.n;
+    r.out = out.dx; r.ldo = out.lddx;
+    if (gate) {
+        r.gate = kept ? (const void *)kept->codes : x;
+        r.ldgate = kept ? (l.k + 31) / 32 * 32 : ldx;
+        r.gate_scale = kept ? kept->scale : nullptr;
     }
-    if (out.dx && l.rows > 0) {
-        RowsArgs r = {};
-        r.a = dy; r.lda = lddy;
-        r.w = l.w; r.ldw = l.ldw; r.w_block = l.w_block;
-        r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.cols = l.k; r.sums = l.n;
-        r.out = out.dx; r.ldo = out.lddx;
-        if (gate) {
-            r.gate = kept ? (const void *)kept->codes : x;
-            r.ldgate = kept ? kp : ldx;
-            r.gate_scale = kept ? kept->scale : nullptr;
-        }
-        const hipError_t e = l.dtype == LMK_GS_F32 ? rows_as<float>(r, l.in_major == 0, stream) : rows_as<__bf16>(r, l.in_major == 0, stream);
-        if (e != hipSuccess) return e;
-    }
-    if (!out.dw && !out.db) return hipSuccess;
+    return r;
+}
+static SumsArgs sums_args(const lmk_gs_linear &l, const RunPlan &plan, const void *dy, u64 lddy, const void *x, u64 ldx,
+                          const lmk_gs_checkpoint8 *kept, const lmk_gs_linear_grads &out, float *part)
+{
     SumsArgs r = {};
     r.dy = dy; r.lddy = lddy;
     r.x = kept ? (const void *)kept->codes : x;
@@ -518,10 +518,88 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
     r.slices = plan.slices;
     r.side = plan.side;
     r.per = plan.per;
-    const u32 kind = !out.dw ? 0 : kept ? 2 : 1;
-    hipError_t e = l.dtype == LMK_GS_F32 ? sums_as<float>(r, kind, stream) : sums_as<__bf16>(r, kind, stream);
-    if (e != hipSuccess) return e;
-    return join(false);
+    return r;
+}
+static u32 sums_kind(const lmk_gs_linear_grads &out, const lmk_gs_checkpoint8 *kept) { return !out.dw ? 0 : kept ? 2 : 1; }
+static BackwardArgs one_pass_args(const lmk_gs_linear &l, const RunPlan &plan, const void *dy, u64 lddy, const void *x, u64 ldx,
+                                  const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out, float *part)
+{
+    BackwardArgs r = {};
+    r.dy = static_cast<const float *>(dy); r.lddy = lddy;
+    if (out.dw || (out.dx && gate)) {
+        r.x = kept ? (const void *)kept->codes : x;
+        r.ldx = ldx;
+        r.scale = kept ? kept->scale : nullptr;
+    }
+    r.w = static_cast<const float *>(l.w); r.ldw = l.ldw; r.w_block = l.w_block;
+    r.offsets = l.offsets; r.blocks = l.blocks; r.rows = l.rows; r.n = l.n; r.k = l.k;
+    r.in_major = l.in_major; r.gate = gate;
+    r.dx = static_cast<float *>(out.dx); r.lddx = out.lddx; r.dw = out.dw; r.db = out.db;
+    r.part = part; r.runs = plan.slices + l.blocks; r.per = plan.per;
+    return r;
+}
+
+// ---- whether every launch of a call has fewer threads than a launch holds, asked before the first one
+bool grouped_linear_fits(const lmk_gs_linear &l, const void *x, u64 ldx, void *y, u64 ldy, const lmk_gs_checkpoint8 *keep)
+{
+    return rows_threads(forward_args(l, x, ldx, nullptr, false, y, ldy, keep), l.dtype, l.in_major != 0) < kMostThreads;
+}
+
+bool grouped_backward_fits(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx, const lmk_gs_checkpoint8 *kept,
+                           bool gate, const lmk_gs_linear_grads &out)
+{
+    const bool sums = out.dw || out.db;
+    const RunPlan plan = sums ? run_plan(l) : RunPlan{};
+    if (sums && (u64)join_shape(l, plan).pieces * l.blocks * kThreads >= kMostThreads) return false;
+    // one pass takes a workgroup a run, of which there are at most some 1000 and one a block
+    if (sums && one_pass(l) && narrow_backward_fits(one_pass_args(l, plan, dy, lddy, x, ldx, kept, gate, out, nullptr), kept != nullptr)) return true;
+    if (out.dx && rows_threads(dx_args(l, dy, lddy, x, ldx, kept, gate, out), l.dtype, l.in_major == 0) >= kMostThreads) return false;
+    return !sums || sums_threads(sums_args(l, plan, dy, lddy, x, ldx, kept, out, nullptr), l.dtype, sums_kind(out, kept)) < kMostThreads;
+}
+
+size_t grouped_backward_bytes(const lmk_gs_linear &l)
+{
+    return (size_t)(((u64)run_plan(l).slices + l.blocks) * ((u64)l.n * l.k + l.n) * 4);
+}
+
+hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
+                                 u64 ldy, const lmk_gs_checkpoint8 *keep, hipStream_t stream)
+{
+    const RowsArgs r = forward_args(l, x, ldx, bias, relu, y, ldy, keep);
+    return l.dtype == LMK_GS_F32 ? rows_as<float>(r, l.in_major != 0, stream) : rows_as<__bf16>(r, l.in_major != 0, stream);
+}
+
+hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx,
+                                   const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
+                                   char *workspace, hipStream_t stream)
+{
+    const bool sums = out.dw || out.db;
+    const RunPlan plan = sums ? run_plan(l) : RunPlan{};
+    float *part = reinterpret_cast<float *>(workspace);
+    const auto join = [&](bool by_blocks) {
+        const JoinShape j = join_shape(l, plan);
+        auto kernel = j.many ? join_kernel<4, 4, 1> : j.parts ? join_kernel<1, 4, 8> : join_kernel<1, 8, 1>;
+        hipLaunchKernelGGL(kernel, dim3(j.pieces * l.blocks), dim3(kThreads), 0, stream, l.offsets, l.blocks, l.rows, plan.per, by_blocks, part,
+                           l.n, l.k, out.dw, out.db, j.pieces);
+        return hipGetLastError();
+    };
+    if (sums && one_pass(l)) {
+        const BackwardArgs r = one_pass_args(l, plan, dy, lddy, x, ldx, kept, gate, out, part);
+        if (narrow_backward_fits(r, kept != nullptr)) {
+            const hipError_t e = launch_narrow_backward(r, kept != nullptr, stream);
+            return e == hipSuccess ? join(true) : e;
+        }
+    }
+    if (out.dx && l.rows > 0) {
+        const RowsArgs r = dx_args(l, dy, lddy, x, ldx, kept, gate, out);
+        const hipError_t e = l.dtype == LMK_GS_F32 ? rows_as<float>(r, l.in_major == 0, stream) : rows_as<__bf16>(r, l.in_major == 0, stream);
+        if (e != hipSuccess) return e;
+    }
+    if (!sums) return hipSuccess;
+    const SumsArgs r = sums_args(l, plan, dy, lddy, x, ldx, kept, out, part);
+    const u32 kind = sums_kind(out, kept);
+    const hipError_t e = l.dtype == LMK_GS_F32 ? sums_as<float>(r, kind, stream) : sums_as<__bf16>(r, kind, stream);
+    return e == hipSuccess ? join(false) : e;
 }
 
 }  // namespace lmk

@@ -182,12 +182,19 @@ bool narrow_rows_fit(const RowsArgs &r)
     return r.lda <= kNarrowStride && r.ldo <= kNarrowStride && (!r.gate || r.ldgate <= kNarrowStride);
 }
 
+// rows of a run: four workgroups a compute unit at most, all of them at once, whole tiles for each of their wavefronts
+static u32 rows_of_run(const RowsArgs &r)
+{
+    const u32 slots = 1024 - (r.blocks < 512 ? r.blocks : 512);
+    return (u32)(((u64)r.rows + slots * 64 - 1) / (slots * 64)) * 64;
+}
+
+u64 narrow_rows_threads(const RowsArgs &r) { return max_runs(r.rows, r.blocks, rows_of_run(r)) * 256; }
+
 hipError_t launch_narrow_rows(RowsArgs r, bool across, hipStream_t stream)
 {
     r.across = across;
-    // four workgroups a compute unit at most, all of them at once, whole tiles for each of their wavefronts
-    const u32 slots = 1024 - (r.blocks < 512 ? r.blocks : 512);
-    r.per = (u32)(((u64)r.rows + slots * 64 - 1) / (slots * 64)) * 64;
+    r.per = rows_of_run(r);
     return narrow_as(r, stream);
 }
 

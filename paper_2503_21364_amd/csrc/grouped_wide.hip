@@ -646,9 +646,13 @@ template <bool ACROSS, u32 GATE>
 hipError_t wide_shape(const RowsArgs &r, hipStream_t stream)
 {
     if (!rows_sixteen(r)) return wide_go<128, 128, 2, 2, ACROSS, true, GATE>(r, stream);
-    if (large_tiles(r))
-        return wide_go<256, 256, 2, 4, ACROSS, false, GATE>(r, stream);
+    if (large_tiles(r)) return wide_go<256, 256, 2, 4, ACROSS, false, GATE>(r, stream);
     return wide_go<128, 128, 2, 2, ACROSS, false, GATE>(r, stream);
+}
+
+bool sums_sixteen(const SumsArgs &r)
+{
+    return r.n % 8 == 0 && sixteen(r.dy, r.lddy) && (r.scale || (r.k % 8 == 0 && sixteen(r.x, r.ldx))) && r.k % 4 == 0;
 }
 
 template <u32 TP, u32 TQ, u32 WP, u32 WQ, bool ANY>
@@ -674,6 +678,12 @@ bool wide_rows_fit(const RowsArgs &r)
     return r.sums >= 8 && r.cols >= 8 && r.lda <= most && r.ldw <= most;
 }
 
+u64 wide_rows_threads(const RowsArgs &r)
+{
+    const u32 side = rows_sixteen(r) && large_tiles(r) ? 256 : 128;
+    return max_runs(r.rows, r.blocks, side) * ((r.cols + side - 1) / side) * (side * 2);
+}
+
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
 {
     const u32 gate = r.keep_codes ? 3 : !r.gate ? 0 : r.gate_scale ? 2 : 1;
@@ -685,13 +695,18 @@ hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)
 bool wide_sums_fit(const SumsArgs &r)
 {
     constexpr u64 most = 1u << 21;
-    return r.n >= 8 && r.k >= 8 && r.dw && r.lddy <= most && (r.scale || r.ldx <= most);
+    return r.n >= 8 && r.k >= 8 && r.lddy <= most && (r.scale || r.ldx <= most);
+}
+
+u64 wide_sums_threads(const SumsArgs &r)
+{
+    const u32 side = sums_sixteen(r) ? r.side : 128;
+    return (u64)r.slices * ((r.n + side - 1) / side) * ((r.k + side - 1) / side) * (side * 2);
 }
 
 hipError_t launch_wide_sums(const SumsArgs &r, hipStream_t stream)
 {
-    const bool any = r.n % 8 || !sixteen(r.dy, r.lddy) || (!r.scale && (r.k % 8 || !sixteen(r.x, r.ldx))) || r.k % 4;
-    if (any) return wide_sums_go<128, 128, 2, 2, true>(r, r.scale != nullptr, stream);
+    if (!sums_sixteen(r)) return wide_sums_go<128, 128, 2, 2, true>(r, r.scale != nullptr, stream);
     if (r.side == 256) return wide_sums_go<256, 256, 2, 4, false>(r, r.scale != nullptr, stream);
     return wide_sums_go<128, 128, 2, 2, false>(r, r.scale != nullptr, stream);
 }

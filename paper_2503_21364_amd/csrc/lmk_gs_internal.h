@@ -164,15 +164,18 @@ hipError_t launch_anchor_decode(const lmk_gs_anchors &anchors, const lmk_gs_anch
                                 const lmk_gs_decoded &out, hipStream_t stream);
 // visible[i] = the box (lo, hi, reach of the scales) passes the frustum test of the voxel filter
 hipError_t launch_box_flags(const float *box, u32 count, const ProjParams &pp, uint8_t *visible, hipStream_t stream);
-// workgroups of the two below (the caller keeps it under 2^31); offsets: NULL, or rows of no block are kept as zeros
-u64 checkpoint8_blocks(u32 rows, u32 k);
+// A launch holds fewer threads than this in a dimension; the calls ask before the first launch.
+constexpr u64 kMostThreads = 1ull << 32;
+// threads of the two below; offsets: NULL, or rows of no block are kept as zeros
+u64 checkpoint8_threads(u32 rows, u32 k);
 hipError_t launch_checkpoint8_pack(const void *x, u64 ldx, u32 rows, u32 k, u32 dtype, const u32 *offsets, u32 blocks,
                                    const lmk_gs_checkpoint8 &out, hipStream_t stream);
 hipError_t launch_checkpoint8_unpack(const lmk_gs_checkpoint8 &kept, u32 rows, u32 k, u32 dtype, void *x, u64 ldx,
                                      hipStream_t stream);
 // the grouped layers: whether what a call launches fits a grid, and the bytes of partial sums of the gradient
-bool grouped_linear_fits(const lmk_gs_linear &l);
-bool grouped_backward_fits(const lmk_gs_linear &l, bool dx, bool sums);
+bool grouped_linear_fits(const lmk_gs_linear &l, const void *x, u64 ldx, void *y, u64 ldy, const lmk_gs_checkpoint8 *keep);
+bool grouped_backward_fits(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx, const lmk_gs_checkpoint8 *kept,
+                           bool gate, const lmk_gs_linear_grads &out);
 size_t grouped_backward_bytes(const lmk_gs_linear &l);
 hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
                                  u64 ldy, const lmk_gs_checkpoint8 *keep, hipStream_t stream);

@@ -32,3 +32,33 @@ def test_a_product_of_rows_is_not_refused_for_the_sums_that_it_does_not_take():
     layer = _layer(0, 256, 65536, 65536, dtype=1)
     assert _bytes(layer) == B.ERR_UNSUPPORTED and _backward(layer, sums=True) == B.ERR_UNSUPPORTED
     assert _forward(layer) == B.OK and _backward(layer) == B.OK
+
+
+# ---- a launch holds fewer than 2^32 threads in a dimension
+ROWS = (1 << 31) - 1
+
+
+def test_products_of_more_rows_than_a_launch_holds():
+    small = dict(blocks=1, k=1, n=1)                            # tiles of 64 rows, 256 threads each
+    for layer in (_layer((1 << 30) + 1, **small), _layer(ROWS, **small), _layer(ROWS, 3, 8, 8, dtype=1), _layer(ROWS, 1, 256, 136)):
+        assert _forward(layer) == B.ERR_UNSUPPORTED
+        assert _backward(layer) == B.ERR_UNSUPPORTED
+        assert _bytes(layer) == B.ERR_UNSUPPORTED
+
+
+def test_an_8_bit_form_of_more_values_than_a_launch_holds():
+    # the general kernel does not write it on the way: 2^32 values of four a thread, and the product itself would fit
+    rows = 1 << 29
+    assert _forward(_layer(rows, 1, 129, 1), keep=True) == B.ERR_UNSUPPORTED
+    lib = B.lib()
+    assert lib.lmk_gs_checkpoint8_pack(P, 32, ROWS, 32, 0, C.byref(KEPT), None) == B.ERR_UNSUPPORTED
+    assert lib.lmk_gs_checkpoint8_unpack(C.byref(KEPT), ROWS, 32, 0, P, 32, None) == B.ERR_UNSUPPORTED
+
+
+def test_more_sums_to_join_than_a_launch_holds():
+    # 2^34 of them, 1024 a workgroup; refused before dx is queued
+    layer = _layer(0, 257, 8192, 8192, dtype=1)
+    assert _bytes(layer) == B.ERR_UNSUPPORTED
+    assert _backward(layer, sums=True) == B.ERR_UNSUPPORTED
+    assert _forward(layer) == B.OK and _backward(layer) == B.OK
+    assert _bytes(_layer(0, 255, 8192, 8192, dtype=1)) == B.OK

@@ -509,6 +509,12 @@ def _dense(t, shape, dtype, like, name):
         raise ValueError(f"{name} has to be a contiguous {dtype} tensor {tuple(shape)} on {like.device}")
 
 
+def _fit_u32(*sizes):
+    """Sizes that a 32-bit field would cut off: ctypes does so without a word."""
+    if any(size >> 32 for size in sizes):
+        raise ValueError(f"sizes of 2^32 or more, or below 0: {sizes}")
+
+
 def _on_gpu(t):
     if not t.is_cuda:
         raise ValueError("the tensors have to be on the GPU: there is no CPU fallback")
@@ -520,6 +526,7 @@ class Checkpoint8:
 
     def __init__(self, rows: int, k: int, device="cuda:0", codes=None, scale=None):
         self.rows, self.k, self.kp = int(rows), int(k), (int(k) + 31) // 32 * 32
+        _fit_u32(self.rows, self.k)
         self.codes = torch.empty((self.rows, self.kp), dtype=torch.int8, device=device) if codes is None else codes
         self.scale = torch.empty((self.rows, self.kp // 32), dtype=torch.uint8, device=device) if scale is None else scale
         _dense(self.codes, (self.rows, self.kp), torch.int8, self.codes, "codes")
@@ -535,6 +542,7 @@ def _layer(w, offsets, rows: int, in_major: bool) -> LinearC:
     if w.shape[2] > 1 and w.stride(2) != 1:
         raise ValueError("the last axis of the weights has to be contiguous")
     n, k = (w.shape[2], w.shape[1]) if in_major else (w.shape[1], w.shape[2])
+    _fit_u32(rows, w.shape[0], n, k)
     ldw = w.stride(1) if w.shape[1] > 1 else max(w.stride(1), w.shape[2])
     return LinearC(_ptr(w), _ptr(offsets), ldw, w.stride(0), w.shape[0], rows, n, k, _dtype(w), int(in_major))
 
@@ -561,6 +569,7 @@ def grouped_linear(x, w, offsets, out, bias=None, relu: bool = False, in_major: 
 def grouped_linear_backward_bytes(rows: int, blocks: int, n: int, k: int, dtype=torch.float32) -> int:
     """Workspace of grouped_linear_backward in bytes."""
     out = C.c_size_t(0)
+    _fit_u32(rows, blocks, n, k)
     layer = LinearC(256, 256, max(n, k), max(n, k) ** 2, blocks, rows, n, k, DTYPES[dtype], 0)
     rc = lib().lmk_gs_grouped_linear_backward_bytes(C.byref(layer), C.byref(out))
     if rc != OK:

@@ -2,6 +2,9 @@
 has no rows and so nothing to launch."""
 import ctypes as C
 
+import pytest
+import torch
+
 from paper_2503_21364_amd import binding as B
 
 P = C.c_void_p(0x40000)
@@ -62,3 +65,20 @@ def test_more_sums_to_join_than_a_launch_holds():
     assert _backward(layer, sums=True) == B.ERR_UNSUPPORTED
     assert _forward(layer) == B.OK and _backward(layer) == B.OK
     assert _bytes(_layer(0, 255, 8192, 8192, dtype=1)) == B.OK
+
+
+# ---- sizes that 32-bit fields would cut off
+def test_sizes_beyond_32_bits_are_refused_and_not_cut_off():
+    big = (1 << 32) + 5
+    for bad in ((big, 4, 96, 35), (1000, big, 96, 35), (1000, 4, big, 35), (1000, 4, 96, big), (-1, 4, 96, 35)):
+        with pytest.raises((ValueError, B.LmkGsError)):
+            B.grouped_linear_backward_bytes(*bad)
+    with pytest.raises(ValueError, match="2\\^32"):
+        B.Checkpoint8(big, 16, "meta")
+    meta = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device="meta")
+    with pytest.raises(ValueError, match="2\\^32"):
+        B.grouped_linear(meta(big, 16), meta(3, 8, 16), meta(4, dtype=torch.int32), meta(big, 8))
+    with pytest.raises(ValueError, match="2\\^32"):
+        B.grouped_linear_backward(meta(big, 8), meta(3, 8, 16), meta(4, dtype=torch.int32), dx=meta(big, 16))
+    with pytest.raises(ValueError, match="2\\^32"):
+        B.grouped_linear(meta(10, 16), meta(big, 8, 16), meta(big + 1, dtype=torch.int32), meta(10, 8))

@@ -415,7 +415,8 @@ hipError_t sums_as(SumsArgs r, u32 kind, hipStream_t stream)
 }  // namespace
 
 // Small matrices in float32 take one pass over the rows for all three gradients; the rest of the rule (strides) is the
-// arrays', and what does not fit takes the other kernels with the same slices.
+// arrays', and what does not fit takes the other kernels with the same slices.  At the limit the two are even (24 blocks of 96 x 64,
+// one pass / the others: 300 000 rows 127 / 122 us, 20 000 rows 26.5 / 27.7; 80 x 64: 108 / 115, 23.4 / 25.8).
 static bool one_pass(const lmk_gs_linear &l) { return l.dtype == LMK_GS_F32 && l.n <= 96 && l.k <= 64; }
 
 // how the sums over rows are shared out

@@ -6,6 +6,8 @@
 namespace lmk {
 
 constexpr u32 kTileRows = 16;
+// of a compute unit, and how it is given out to workgroups
+constexpr u32 kLdsBytes = 160u << 10, kLdsPiece = 1280;
 // byte offsets inside a tile are 32 bits wide
 constexpr u64 kNarrowStride = 1u << 23;
 

@@ -63,12 +63,24 @@ __host__ __device__ constexpr u32 whole_steps(u32 n) { return (n + 15) / 16 * 4;
 constexpr u32 sums_pitch(u32 ck) { return 16 * ck + 4; }
 constexpr u32 sums_floats(u32 cn, u32 ck) { return 16 * cn * sums_pitch(ck) + 16 * cn; }
 
-// workgroups of a compute unit (wavefronts of a SIMD): as many as the registers of the sums leave
-constexpr u32 resident(u32 tiles) { return tiles <= 12 ? 3 : 2; }
+// LDS of the widest matrices of a shape: weights and the four wavefronts' tiles, then their sums in the same place
+constexpr u32 shape_lds(u32 cn, u32 ck)
+{
+    const u32 before = 4 * cn * ck * kWave + 4 * kTileRows * (pitch_of(16 * cn) + pitch_of(16 * ck)), sums = 4 * sums_floats(cn, ck);
+    return (before > sums ? before : sums) * 4;
+}
+// Workgroups of a compute unit (wavefronts of a SIMD), what the registers of the sums and LDS both leave: three up to twelve tiles
+// of sums, whose wavefronts take at most 168 registers, two up to 24.  LDS is given out in pieces of 1280 bytes; 64 x 48 and 96 x 32
+// have two workgroups for it, 80 x 64 and 96 x 64 one.
+constexpr u32 resident(u32 cn, u32 ck)
+{
+    const u32 registers = cn * ck <= 12 ? 3 : 2, lds = kLdsBytes / ((shape_lds(cn, ck) + kLdsPiece - 1) / kLdsPiece * kLdsPiece);
+    return registers < lds ? registers : lds;
+}
 
 // CN, CK: 16 outputs and 16 inputs each
 template <u32 CN, u32 CK, bool CODES>
-__global__ __launch_bounds__(256, resident(CN * CK)) void narrow_backward_kernel(const BackwardArgs r)
+__global__ __launch_bounds__(256, resident(CN, CK)) void narrow_backward_kernel(const BackwardArgs r)
 {
     extern __shared__ __align__(16) float narrow_lds[];
     const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
@@ -263,7 +275,7 @@ bool narrow_backward_fits(const BackwardArgs &r, bool codes)
 // outputs in tiles of 16, as the kernels are built for them
 static u32 out_tiles(u32 n) { return n <= 32 ? 2 : n <= 64 ? 4 : n <= 80 ? 5 : 6; }
 
-u32 narrow_backward_slots(u32 n, u32 k) { return 256 * resident(out_tiles(n) * ((k + 15) / 16)); }
+u32 narrow_backward_slots(u32 n, u32 k) { return 256 * resident(out_tiles(n), (k + 15) / 16); }
 
 hipError_t launch_narrow_backward(const BackwardArgs &r, bool codes, hipStream_t stream)
 {

@@ -1,10 +1,12 @@
 """The kernels of the grouped layers as the compiler takes them, without a GPU."""
+import ctypes as C
 import os
 import re
 import subprocess
 
 import pytest
 
+from paper_2503_21364_amd import binding as B
 from paper_2503_21364_amd import build as hip_build
 
 UNITS = sorted(u for u in hip_build.UNITS if u.startswith(("grouped", "checkpoint8")))
@@ -50,3 +52,43 @@ def test_a_barrier_alone_is_found():
     for lines, count in (([fence, wait, barrier, fence], 0), (["fence release", barrier, "fence acquire"], 0),
                          (["store i32 0, ptr %1", wait, barrier, fence], 1), ([fence, barrier, "%2 = load i32, ptr %1"], 1)):
         assert len(unordered_barriers("\n".join(lines))) == count
+
+
+# ---- what a compute unit holds of the kernels over small matrices, against what the calls plan with
+def _report(unit, tmp_path_factory):
+    """Template arguments -> the compiler's report, of the kernels of a unit."""
+    cmd = [hip_build.hipcc(), *hip_build.COMMON, *hip_build.UNITS[unit], "--cuda-device-only", "-Rpass-analysis=kernel-resource-usage",
+           "-c", os.path.join(hip_build.CSRC, unit), "-o", str(tmp_path_factory.mktemp("obj") / "unit.o")]
+    text = subprocess.run(cmd, capture_output=True, text=True, check=True).stderr
+    kernels = {}
+    for part in text.split("Function Name: ")[1:]:
+        numbers = tuple(int(v) for v in re.findall(r"L[jb](\d+)E", part.split()[0]))
+        kernels[numbers] = {k: int(v) for k, v in re.findall(r" ([A-Z][A-Za-z]+(?: Spill| \[[^\]]*\])?): (\d+)", part)}
+    return kernels
+
+
+@pytest.fixture(scope="module")
+def backward_report(tmp_path_factory):
+    return _report("grouped_narrow_bwd.hip", tmp_path_factory)
+
+
+def _workgroups(lds_bytes):
+    return (160 << 10) // ((lds_bytes + 1279) // 1280 * 1280)            # LDS is given out in pieces of 1280 bytes
+
+
+def _pitch(width):
+    return ((width + 3) // 4 | 1) * 4
+
+
+@pytest.mark.parametrize("k", [16, 32, 48, 64])
+@pytest.mark.parametrize("n", [32, 64, 80, 96])
+def test_all_runs_of_a_gradient_of_small_matrices_are_held_at_once(backward_report, n, k):
+    cn, ck = n // 16, k // 16
+    # weights and four wavefronts' tiles of 16 rows; then four copies of the sums, rows of which are 4 floats apart
+    floats = max(n * k + 4 * 16 * (_pitch(n) + _pitch(k)), 4 * (n * (k + 4) + n))
+    kernels = [backward_report[cn, ck, codes] for codes in (0, 1)]
+    held = min(_workgroups(4 * floats), *(r["Occupancy [waves/SIMD]"] for r in kernels))
+    rows, blocks = 1 << 30, 1
+    runs = B.grouped_linear_backward_bytes(rows, blocks, n, k) // (4 * (n * k + n)) - blocks
+    assert 1 <= runs <= 256 * held, (runs / 256, held)
+    assert all(r["VGPRs Spill"] == 0 and r["ScratchSize [bytes/lane]"] == 0 for r in kernels), kernels

@@ -158,9 +158,15 @@ hipError_t narrow_sums(const RowsArgs &r, hipStream_t stream)
     if (r.sums <= 64) return narrow_go<CT, turns_of(16)>(r, stream);
     return narrow_go<CT, turns_of(32)>(r, stream);
 }
+// tiles of 16 columns, as the kernels are built for them
+u32 column_tiles(u32 cols)
+{
+    const u32 ct = (cols + 15) / 16;
+    return ct == 7 ? 8 : ct;
+}
 hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)
 {
-    switch ((r.cols + 15) / 16) {
+    switch (column_tiles(r.cols)) {
     case 1: return narrow_sums<1>(r, stream);
     case 2: return narrow_sums<2>(r, stream);
     case 3: return narrow_sums<3>(r, stream);
@@ -173,12 +179,12 @@ hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)
 
 }  // namespace
 
-// At most half of a compute unit's LDS: with one workgroup there, nothing hides what its wavefronts wait for (300 000 rows, 128 x
-// 128: 179 us against the general kernel's 134; 96 x 96: 85 against 99).
+// At most half of a compute unit's LDS: with one workgroup there, nothing hides what its wavefronts wait for (300 000 rows, this kernel
+// / the general one: 128 x 128 179 / 134 us, 104 x 108 152 / 127; 96 x 96 85 / 99).
 bool narrow_rows_fit(const RowsArgs &r)
 {
     if (r.cols > 128 || r.sums < 4 || r.sums > 128) return false;
-    if (narrow_lds_floats(r.sums, (r.cols + 15) / 16) * 4 > 80u << 10) return false;
+    if (narrow_lds_floats(r.sums, column_tiles(r.cols)) * 4 > kLdsBytes / 2) return false;
     return r.lda <= kNarrowStride && r.ldo <= kNarrowStride && (!r.gate || r.ldgate <= kNarrowStride);
 }
 

@@ -92,3 +92,29 @@ def test_all_runs_of_a_gradient_of_small_matrices_are_held_at_once(backward_repo
     runs = B.grouped_linear_backward_bytes(rows, blocks, n, k) // (4 * (n * k + n)) - blocks
     assert 1 <= runs <= 256 * held, (runs / 256, held)
     assert all(r["VGPRs Spill"] == 0 and r["ScratchSize [bytes/lane]"] == 0 for r in kernels), kernels
+
+
+@pytest.fixture(scope="module")
+def narrow_rows(tmp_path_factory):
+    """(columns, sums) -> whether the kernels over small matrices take the product, and its runs."""
+    B.lib()
+    exe = str(tmp_path_factory.mktemp("host") / "narrow_rows")
+    lib = os.path.dirname(hip_build.LIB)
+    subprocess.run([hip_build.hipcc(), "-std=c++17", "-O1", f"--offload-arch={hip_build.ARCH}", "--offload-host-only", "-x", "hip",
+                    os.path.join(os.path.dirname(__file__), "host", "narrow_rows_driver.cpp"), "-I", hip_build.INCLUDE, "-I", hip_build.CSRC,
+                    "-L", lib, "-l:" + os.path.basename(hip_build.LIB), "-Wl,-rpath," + lib, "-o", exe], check=True, capture_output=True)
+    lines = subprocess.run([exe], check=True, capture_output=True, text=True).stdout.splitlines()
+    return {(int(c), int(s)): (f == "1", int(r)) for c, s, f, r in (line.split() for line in lines)}
+
+
+def _narrow_lds(cols, sums):
+    """Weights in steps of four sum indices and tiles of 16 columns (1 .. 6 and 8 of them), the bias, four tiles of 16 rows."""
+    tiles = (cols + 15) // 16
+    tiles = 8 if tiles == 7 else tiles
+    return 4 * ((sums + 3) // 4 * tiles * 64 + tiles * 16 + 4 * 16 * _pitch(sums))
+
+
+def test_small_matrices_are_those_of_which_a_compute_unit_holds_two(narrow_rows):
+    for (cols, sums), (fits, _) in narrow_rows.items():
+        small = cols <= 128 and 4 <= sums <= 128 and _narrow_lds(cols, sums) <= 80 << 10
+        assert fits == small, (cols, sums, _narrow_lds(cols, sums))

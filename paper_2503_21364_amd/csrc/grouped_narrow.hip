@@ -180,7 +180,7 @@ hipError_t narrow_as(const RowsArgs &r, hipStream_t stream)
 }  // namespace
 
 // At most half of a compute unit's LDS: with one workgroup there, nothing hides what its wavefronts wait for (300 000 rows, this kernel
-// / the general one: 128 x 128 179 / 134 us, 104 x 108 152 / 127; 96 x 96 85 / 99).
+// / the general one: 128 x 128 179 / 134 us, 104 x 108 152 / 127; with two, 96 x 96, 75 / 99).
 bool narrow_rows_fit(const RowsArgs &r)
 {
     if (r.cols > 128 || r.sums < 4 || r.sums > 128) return false;
@@ -188,10 +188,12 @@ bool narrow_rows_fit(const RowsArgs &r)
     return r.lda <= kNarrowStride && r.ldo <= kNarrowStride && (!r.gate || r.ldgate <= kNarrowStride);
 }
 
-// rows of a run: four workgroups a compute unit at most, all of them at once, whole tiles for each of their wavefronts
+// Rows of a run, whole tiles for each of the four wavefronts: all runs at once, in as many workgroups a compute unit as LDS holds, four
+// at most, which is what the kernels' registers leave
 static u32 rows_of_run(const RowsArgs &r)
 {
-    const u32 slots = 1024 - (r.blocks < 512 ? r.blocks : 512);
+    const u32 lds = (narrow_lds_floats(r.sums, column_tiles(r.cols)) * 4 + kLdsPiece - 1) / kLdsPiece * kLdsPiece, held = kLdsBytes / lds;
+    const u32 most = 256 * (held < 4 ? held : 4), slots = most - (r.blocks < most / 2 ? r.blocks : most / 2);
     return (u32)(((u64)r.rows + slots * 64 - 1) / (slots * 64)) * 64;
 }
 

@@ -118,3 +118,14 @@ def test_small_matrices_are_those_of_which_a_compute_unit_holds_two(narrow_rows)
     for (cols, sums), (fits, _) in narrow_rows.items():
         small = cols <= 128 and 4 <= sums <= 128 and _narrow_lds(cols, sums) <= 80 << 10
         assert fits == small, (cols, sums, _narrow_lds(cols, sums))
+
+
+def test_all_runs_of_a_product_of_small_matrices_are_held_at_once(narrow_rows, tmp_path_factory):
+    """By LDS; and the registers of every kernel leave four wavefronts a SIMD, or as many as LDS in its smallest size."""
+    for (cols, sums), (fits, runs) in narrow_rows.items():
+        if fits:
+            assert 1 <= runs <= 256 * min(4, _workgroups(_narrow_lds(cols, sums))), (cols, sums, runs / 256)
+    for (tiles, pieces, _, gate), r in _report("grouped_narrow.hip", tmp_path_factory).items():
+        least = {3: 4, 4: 37, 8: 65}[pieces]                              # sums of the kernel's smallest size
+        assert r["Occupancy [waves/SIMD]"] >= min(4, _workgroups(_narrow_lds(16 * tiles, least))), (tiles, pieces, gate)
+        assert r["VGPRs Spill"] == 0 and r["ScratchSize [bytes/lane]"] == 0

@@ -397,8 +397,8 @@ typedef struct lmk_gs_checkpoint8 {
  * max(., 0) (a NaN stays one).  Sums in 32 bits, one rounding to dtype.  ldx, ldy: elements between rows, at least
  * k and n, at most 2^28.  bias: [blocks][n] float32 or NULL.  keep: NULL, or where the 8-bit form of x is written (zeros for rows
  * of no block).  y must not overlap x or w.  Asynchronous on `stream`.  LMK_GS_ERR_INVALID: NULL pointer, size,
- * stride or flag out of range, a pointer that is not aligned to its elements; LMK_GS_ERR_UNSUPPORTED: another dtype, too many tiles
- * for one launch. */
+ * stride or flag out of range, a pointer that is not aligned to its elements; LMK_GS_ERR_UNSUPPORTED: another dtype, or sizes that
+ * take 2^32 threads in one launch, before anything is queued. */
 int32_t lmk_gs_grouped_linear(const lmk_gs_linear *layer, const void *x, uint64_t ldx, const float *bias,
                               uint32_t relu, void *y, uint64_t ldy, const lmk_gs_checkpoint8 *keep, void *stream);
 
@@ -411,7 +411,8 @@ typedef struct lmk_gs_linear_grads {
     float *db;       /* [blocks][n]: sum over the block's rows of dy                                                   */
 } lmk_gs_linear_grads;
 
-/* Bytes of workspace of lmk_gs_grouped_linear_backward (partial sums of dw and db over runs of rows). */
+/* Bytes of workspace of lmk_gs_grouped_linear_backward (partial sums of dw and db over runs of rows).  Errors as lmk_gs_grouped_linear,
+ * for all gradients of packed rows. */
 int32_t lmk_gs_grouped_linear_backward_bytes(const lmk_gs_linear *layer, size_t *bytes);
 
 /* The layer's input comes as x (rows ldx apart) or as its 8-bit form `kept`; dw and gate need one of the two and

@@ -282,7 +282,7 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
 // Joins the partial sums of the blocks that have several runs, in the order of the runs (the same bits every time), and
 // writes zeros for blocks without rows.  V consecutive sums a thread, AHEAD sets on their way: no sum waits for the one in
 // front of it, only its addition does.  Where there are few sums, and so many sets of them, PARTS parts of a workgroup take
-// consecutive sets each and the parts meet in LDS, in their order.  Bound by memory where there are many sums (32 blocks of 1024 x 1024: 33 us), by
+// consecutive sets each and the parts meet in LDS, in their order.  Bound by memory where there are many sums (32 blocks of 1024 x 1024: 37 us), by
 // the chain of sets where there are few.
 template <u32 V, u32 AHEAD, u32 PARTS>
 __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per, bool by_blocks,

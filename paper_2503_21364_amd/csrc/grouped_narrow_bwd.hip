@@ -7,7 +7,7 @@
 // db is added up from the values of dy on their way to the second product.  At the end the four wavefronts' sums meet in LDS
 // and are added in their order.
 //
-// 300 000 rows in 24 blocks: 35 x 96 in 89 us, 32 x 70 with the gate in 59 us.  Bound by the float32 instructions (35 us for the
+// 300 000 rows in 24 blocks: 35 x 96 in 86 us, 32 x 70 with the gate in 57 us.  Bound by the float32 instructions (35 us for the
 // first at their rate), which wait for the LDS reads in front of them: the sums of 96 x 48 leave registers for two
 // wavefronts a SIMD.  About 13 us are a run's own costs: weights into LDS, the four wavefronts' sums joined.
 #include "grouped_narrow.h"

@@ -3,9 +3,12 @@
 //
 // Bound by those instructions and by LDS, which feeds them: 8192 x 8192 x 8192 at 1000 (forward), 1260 (dx), 1210
 // (dw) and 1030 - 1080 TFLOP/s (dw from the 8-bit form); the largest library product reaches 1268.  65 536 rows in 32 ragged blocks
-// of 1024 x 1024 (137 GFLOP a product): forward with the 8-bit form 232 us, dx with its gate 221 - 226, dw and db 191 - 198.
+// of 1024 x 1024 (137 GFLOP a product), the same inputs again and again: forward 167 us, dx 163, dw and db 210 with 37 of joining.
 // There 1076 tiles take five rounds of 256 workgroups where 4.2 would do, and a round's first loads and last stores have no
 // products beside them: the accumulators and two steps' fragments of a lane leave no registers for the next tile's.
+// The gate of dx adds 45 us (208 from codes, 205 from values): a lane's codes and scales are asked for sixteen times a tile, each
+// time behind the stores in front.  The 8-bit form of x adds 36 (203; by itself it takes 64): its arithmetic stands between a
+// meeting of the wavefronts and the products, for all of them at once.
 //
 // Tiles of 256 x 256, two wavefronts a SIMD: LDS gives a step's fragments in less time than their products take, which it
 // does not for 128 x 128 (65 536 x 1024 x 1024 in 8 blocks: 183 us, large tiles 156) or 256 x 128 (slower than both).

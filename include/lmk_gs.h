@@ -431,6 +431,44 @@ int32_t lmk_gs_checkpoint8_pack(const void *x, uint64_t ldx, uint32_t rows, uint
 int32_t lmk_gs_checkpoint8_unpack(const lmk_gs_checkpoint8 *kept, uint32_t rows, uint32_t k, uint32_t dtype,
                                   void *x, uint64_t ldx, void *stream);
 
+/* ---- Layer norm of the rows of blocks, each with gain and shift of its own, and its gradients.
+ *   m = mean(x[r]), s = 1 / sqrt(mean((x[r] - m)^2) + eps), h = (x[r] - m) s, y[r] = gain[g] h + shift[g]
+ * in 32 bits, one rounding to dtype.  Rows of no block give zeros and enter no gradient; a row that holds what is not finite gives
+ * NaN and touches no other. */
+typedef struct lmk_gs_norm {
+    const float *gain;        /* [blocks][k], or NULL: all 1                                    */
+    const float *shift;       /* [blocks][k], or NULL: all 0; the gradients do not read it      */
+    const uint32_t *offsets;  /* [blocks + 1], as lmk_gs_linear.offsets                         */
+    uint32_t blocks;          /* 1 .. 65536                                                     */
+    uint32_t rows;            /* 0 is allowed, below 2^31                                       */
+    uint32_t k;               /* values of a row, 1 .. 65536                                    */
+    uint32_t dtype;           /* LMK_GS_F32 or LMK_GS_BF16: type of x, y, dy and dx             */
+    float eps;                /* finite and above 0                                             */
+} lmk_gs_norm;
+
+/* y may be x itself (same pointer and stride); otherwise it must not overlap it.  ldx, ldy: elements between rows, at least k, at most 2^28.
+ * Asynchronous on `stream`.  LMK_GS_ERR_INVALID: NULL pointer, size or stride out of range, eps, a pointer that is not aligned to its
+ * elements; LMK_GS_ERR_UNSUPPORTED: another dtype, or sizes that take 2^32 threads in one launch, before anything is queued. */
+int32_t lmk_gs_grouped_norm(const lmk_gs_norm *norm, const void *x, uint64_t ldx, void *y, uint64_t ldy, void *stream);
+
+/* With dy the gradient of y and d = dy gain[g].  Any of the three may be NULL; whole arrays are written, blocks without rows get
+ * zeros in dgain and dshift. */
+typedef struct lmk_gs_norm_grads {
+    void *dx;                 /* [rows][k], rows lddx apart, dtype: s (d - mean(d) - h mean(d h)) */
+    uint64_t lddx;
+    float *dgain;             /* [blocks][k]: sum over the block's rows of dy h                   */
+    float *dshift;            /* [blocks][k]: sum over the block's rows of dy                     */
+} lmk_gs_norm_grads;
+
+/* Bytes of workspace of lmk_gs_grouped_norm_backward (partial sums over runs of rows).  Errors as there. */
+int32_t lmk_gs_grouped_norm_backward_bytes(const lmk_gs_norm *norm, size_t *bytes);
+
+/* From dy and the norm's input x (its mean and deviation are taken again).  Sums over a block's rows are taken in an order that
+ * depends on the sizes only.  workspace: 256-byte aligned, not needed where dgain and dshift are NULL.  dx may be dy or x itself (same
+ * pointer and stride); otherwise outputs must not overlap inputs.  Errors as lmk_gs_grouped_norm; LMK_GS_ERR_CAPACITY: workspace too small. */
+int32_t lmk_gs_grouped_norm_backward(const lmk_gs_norm *norm, const void *dy, uint64_t lddy, const void *x, uint64_t ldx,
+                                     const lmk_gs_norm_grads *out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Copies {pair count D, status} of the frame from scratch to the host.
  * Synchronises `stream`.  Either output pointer may be NULL. */
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream);

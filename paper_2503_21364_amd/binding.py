@@ -27,7 +27,8 @@ EXPORTS = ("lmk_gs_workspace_bytes", "lmk_gs_preprocess", "lmk_gs_bin_sort", "lm
            "lmk_gs_preprocess_backward", "lmk_gs_anchor_decode", "lmk_gs_anchor_index_build",
            "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static", "lmk_gs_grouped_linear",
            "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes", "lmk_gs_checkpoint8_pack",
-           "lmk_gs_checkpoint8_unpack")
+           "lmk_gs_checkpoint8_unpack", "lmk_gs_grouped_norm", "lmk_gs_grouped_norm_backward",
+           "lmk_gs_grouped_norm_backward_bytes")
 
 
 class Gaussians(C.Structure):
@@ -97,6 +98,15 @@ class LinearGrads(C.Structure):
     _fields_ = [("dx", C.c_void_p), ("lddx", C.c_uint64), ("dw", C.c_void_p), ("db", C.c_void_p)]
 
 
+class NormC(C.Structure):
+    _fields_ = [("gain", C.c_void_p), ("shift", C.c_void_p), ("offsets", C.c_void_p), ("blocks", C.c_uint32), ("rows", C.c_uint32),
+                ("k", C.c_uint32), ("dtype", C.c_uint32), ("eps", C.c_float)]
+
+
+class NormGrads(C.Structure):
+    _fields_ = [("dx", C.c_void_p), ("lddx", C.c_uint64), ("dgain", C.c_void_p), ("dshift", C.c_void_p)]
+
+
 class LmkGsError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -149,6 +159,10 @@ def lib() -> C.CDLL:
                                               C.POINTER(Checkpoint8C), C.c_void_p]
         l.lmk_gs_checkpoint8_unpack.argtypes = [C.POINTER(Checkpoint8C), C.c_uint32, C.c_uint32, C.c_uint32,
                                                 C.c_void_p, C.c_uint64, C.c_void_p]
+        l.lmk_gs_grouped_norm.argtypes = [C.POINTER(NormC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p]
+        l.lmk_gs_grouped_norm_backward.argtypes = [C.POINTER(NormC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64,
+                                                   C.POINTER(NormGrads), C.c_void_p, C.c_size_t, C.c_void_p]
+        l.lmk_gs_grouped_norm_backward_bytes.argtypes = [C.POINTER(NormC), C.POINTER(C.c_size_t)]
         l.lmk_gs_read_status.argtypes = [C.c_void_p, C.POINTER(C.c_uint64), C.POINTER(C.c_int32), C.c_void_p]
         l.lmk_gs_strerror.argtypes = [C.c_int32]
         l.lmk_gs_strerror.restype = C.c_char_p
@@ -158,7 +172,8 @@ def lib() -> C.CDLL:
                      "lmk_gs_preprocess_backward", "lmk_gs_anchor_decode", "lmk_gs_anchor_index_build",
                      "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static", "lmk_gs_grouped_linear",
                      "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes",
-                     "lmk_gs_checkpoint8_pack", "lmk_gs_checkpoint8_unpack"):
+                     "lmk_gs_checkpoint8_pack", "lmk_gs_checkpoint8_unpack", "lmk_gs_grouped_norm",
+                     "lmk_gs_grouped_norm_backward", "lmk_gs_grouped_norm_backward_bytes"):
             getattr(l, name).restype = C.c_int32
         l.lmk_gs_version.restype = C.c_uint32
         _lib = l
@@ -625,6 +640,83 @@ def checkpoint8_unpack(checkpoint: Checkpoint8, out, stream=None) -> None:
                                          _stream_handle(stream))
     if rc != OK:
         raise LmkGsError(rc, "lmk_gs_checkpoint8_unpack")
+
+
+# ---- layer norm of the rows of blocks
+def _stream_on(like, stream):
+    """The handle of `stream` (None: the current one), which has to be of the tensors' device, and that the current one."""
+    if like.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {like.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if stream is not None and stream.device != like.device:
+        raise ValueError(f"the tensors are on {like.device}, the stream on {stream.device}")
+    return _stream_handle(stream)
+
+
+def _offsets(offsets, like) -> int:
+    """The number of blocks."""
+    if offsets.dim() != 1 or offsets.numel() < 2 or offsets.dtype not in (torch.int32, torch.uint32) or not offsets.is_contiguous():
+        raise ValueError("offsets have to be a contiguous 32-bit tensor [blocks + 1]")
+    if offsets.device != like.device:
+        raise ValueError(f"offsets are on {offsets.device}, the rows on {like.device}")
+    return offsets.numel() - 1
+
+
+def _workspace(t, like):
+    if t is not None and (t.dtype != torch.uint8 or not t.is_contiguous() or t.device != like.device):
+        raise ValueError(f"the workspace has to be a contiguous uint8 tensor on {like.device}")
+    return 0 if t is None else t.numel()
+
+
+def _norm(x, offsets, gain, shift, eps: float) -> NormC:
+    if x.dim() != 2:
+        raise ValueError("x is [rows][k]")
+    rows, k, blocks = x.shape[0], x.shape[1], _offsets(offsets, x)
+    _fit_u32(rows, k, blocks)
+    _dense(gain, (blocks, k), torch.float32, x, "gain")
+    _dense(shift, (blocks, k), torch.float32, x, "shift")
+    return NormC(_ptr(gain), _ptr(shift), _ptr(offsets), blocks, rows, k, _dtype(x), float(eps))
+
+
+def grouped_norm(x, offsets, out, gain=None, shift=None, eps: float = 1e-5, stream=None) -> None:
+    """lmk_gs_grouped_norm: out[r] = gain[g] (x[r] - mean) / sqrt(variance + eps) + shift[g] for the rows
+    offsets[g] .. offsets[g+1]-1 of every block g.  x and out [rows][k], float32 or bfloat16; out may be x.  offsets int32 [blocks + 1] on
+    the device; gain and shift float32 [blocks][k], or None: ones and zeros."""
+    norm = _norm(x, offsets, gain, shift, eps)
+    ldx, ldy = _matrix(x, x.shape, x, "x"), _matrix(out, x.shape, x, "out")
+    _on_gpu(x)
+    rc = lib().lmk_gs_grouped_norm(C.byref(norm), _ptr(x), ldx, _ptr(out), ldy, _stream_on(x, stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_norm")
+
+
+def grouped_norm_backward_bytes(rows: int, blocks: int, k: int, dtype=torch.float32) -> int:
+    """Workspace of grouped_norm_backward in bytes."""
+    out = C.c_size_t(0)
+    _fit_u32(rows, blocks, k)
+    norm = NormC(None, None, 256, blocks, rows, k, DTYPES[dtype], 1.0)
+    rc = lib().lmk_gs_grouped_norm_backward_bytes(C.byref(norm), C.byref(out))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_norm_backward_bytes")
+    return int(out.value)
+
+
+def grouped_norm_backward(dy, x, offsets, workspace=None, gain=None, eps: float = 1e-5, dx=None, dgain=None, dshift=None,
+                          stream=None) -> None:
+    """lmk_gs_grouped_norm_backward: from dy [rows][k], the gradient of the norm of x, to those of x, gain and shift; each of dx
+    (which may be dy or x), dgain and dshift may be left out.  dgain and dshift are float32 [blocks][k]; workspace: a uint8
+    tensor of grouped_norm_backward_bytes, needed for the two."""
+    norm = _norm(x, offsets, gain, None, eps)
+    ldx, lddy = _matrix(x, x.shape, x, "x"), _matrix(dy, x.shape, x, "dy")
+    lddx = 0 if dx is None else _matrix(dx, x.shape, x, "dx")
+    _dense(dgain, (norm.blocks, norm.k), torch.float32, x, "dgain")
+    _dense(dshift, (norm.blocks, norm.k), torch.float32, x, "dshift")
+    size = _workspace(workspace, x)
+    grads = NormGrads(_ptr(dx), lddx, _ptr(dgain), _ptr(dshift))
+    _on_gpu(x)
+    rc = lib().lmk_gs_grouped_norm_backward(C.byref(norm), _ptr(dy), lddy, _ptr(x), ldx, C.byref(grads), _ptr(workspace), size,
+                                            _stream_on(x, stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_norm_backward")
 
 
 def read_status(frame: Frame, stream=None) -> tuple[int, int]:

@@ -40,6 +40,7 @@ UNITS = {
     "grouped_linear.hip": [],
     "grouped_narrow.hip": [],
     "grouped_narrow_bwd.hip": [],
+    "grouped_norm.hip": [],
     "grouped_wide.hip": [],
     "index.hip": EXACT,         # host code: the voxel of a primitive is decided by one fp32 division
 }

@@ -427,6 +427,59 @@ int32_t lmk_gs_checkpoint8_unpack(const lmk_gs_checkpoint8 *kept, uint32_t rows,
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
 
+static int32_t check_norm(const lmk_gs_norm *n)
+{
+    if (!n) return LMK_GS_ERR_INVALID;
+    if (n->dtype != LMK_GS_F32 && n->dtype != LMK_GS_BF16) return LMK_GS_ERR_UNSUPPORTED;
+    if (n->blocks == 0 || n->blocks > kMaxBlocks || n->rows >= 1u << 31 || n->k == 0 || n->k > kMaxWidth) return LMK_GS_ERR_INVALID;
+    if (!(n->eps > 0.0f) || !std::isfinite(n->eps)) return LMK_GS_ERR_INVALID;
+    if (!n->offsets || !aligned(n->offsets, 4) || !aligned(n->gain, 4) || !aligned(n->shift, 4)) return LMK_GS_ERR_INVALID;
+    return LMK_GS_OK;
+}
+
+int32_t lmk_gs_grouped_norm(const lmk_gs_norm *norm, const void *x, uint64_t ldx, void *y, uint64_t ldy, void *stream)
+{
+    const int32_t rc = check_norm(norm);
+    if (rc != LMK_GS_OK) return rc;
+    if (norm->rows == 0) return LMK_GS_OK;
+    if (!good_rows(x, ldx, norm->k, norm->dtype) || !good_rows(y, ldy, norm->k, norm->dtype)) return LMK_GS_ERR_INVALID;
+    if (!grouped_norm_fits(*norm, false, false)) return LMK_GS_ERR_UNSUPPORTED;
+    const hipError_t e = launch_grouped_norm(*norm, x, ldx, y, ldy, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
+int32_t lmk_gs_grouped_norm_backward_bytes(const lmk_gs_norm *norm, size_t *bytes)
+{
+    const int32_t rc = check_norm(norm);
+    if (rc != LMK_GS_OK) return rc;
+    if (!bytes) return LMK_GS_ERR_INVALID;
+    if (!grouped_norm_fits(*norm, true, true)) return LMK_GS_ERR_UNSUPPORTED;
+    *bytes = grouped_norm_backward_bytes(*norm);
+    return LMK_GS_OK;
+}
+
+int32_t lmk_gs_grouped_norm_backward(const lmk_gs_norm *norm, const void *dy, uint64_t lddy, const void *x, uint64_t ldx,
+                                     const lmk_gs_norm_grads *out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int32_t rc = check_norm(norm);
+    if (rc != LMK_GS_OK) return rc;
+    if (!out || !aligned(out->dgain, 4) || !aligned(out->dshift, 4)) return LMK_GS_ERR_INVALID;
+    const bool sums = out->dgain || out->dshift;
+    if (norm->rows > 0) {
+        if (!good_rows(dy, lddy, norm->k, norm->dtype) || !good_rows(x, ldx, norm->k, norm->dtype)) return LMK_GS_ERR_INVALID;
+        if (out->dx && !good_rows(out->dx, out->lddx, norm->k, norm->dtype)) return LMK_GS_ERR_INVALID;
+    }
+    if (!grouped_norm_fits(*norm, true, sums)) return LMK_GS_ERR_UNSUPPORTED;
+    if (sums) {
+        if (!workspace || !aligned(workspace, 256)) return LMK_GS_ERR_INVALID;
+        if (workspace_bytes < grouped_norm_backward_bytes(*norm)) return LMK_GS_ERR_CAPACITY;
+    }
+    if (!sums && (!out->dx || norm->rows == 0)) return LMK_GS_OK;
+    const hipError_t e = launch_grouped_norm_backward(*norm, dy, lddy, x, ldx, *out, static_cast<char *>(workspace),
+                                                      static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream)
 {
     if (!scratch) return LMK_GS_ERR_INVALID;
@@ -454,7 +507,7 @@ const char *lmk_gs_strerror(int32_t code)
 
 int32_t lmk_gs_last_hip_error(void) { return g_last_hip_error.load(); }
 
-// 0.4.0: grouped perceptron layers with their gradients and 8-bit checkpoints
-uint32_t lmk_gs_version(void) { return 400; }
+// 0.5.0: layer norms and gated layers of blocks with their gradients, layers in 4 bits
+uint32_t lmk_gs_version(void) { return 500; }
 
 }  // extern "C"

@@ -82,6 +82,12 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total, u32 at_once)
 }
 
 // `..._threads`: those that a launch would have
+// Partial sums of blocks cut into runs of `per` rows (run r of block g is set r + g + (first row of g) / per): n k sums of dw and n of db a
+// set; `slices`: sets, less the blocks.  Blocks of one run are not touched, those without rows get zeros.
+u64 join_threads(u32 n, u32 k, u32 blocks, u32 slices);
+hipError_t launch_join(const u32 *offsets, u32 blocks, u32 rows, u32 per, const float *part, u32 n, u32 k, float *dw, float *db, u32 slices,
+                       hipStream_t stream);
+
 // few rows, any type and alignment
 bool few_rows_fit(const RowsArgs &r, bool wide);
 u64 few_rows_threads(const RowsArgs &r, bool across);

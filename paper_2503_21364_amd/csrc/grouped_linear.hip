@@ -284,9 +284,9 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
 // front of it, only its addition does.  Where there are few sums, and so many sets of them, PARTS parts of a workgroup take
 // consecutive sets each and the parts meet in LDS, in their order.  Bound by memory where there are many sums (32 blocks of 1024 x 1024: 37 us), by
 // the chain of sets where there are few.
-template <u32 V, u32 AHEAD, u32 PARTS>
+template <class D, u32 V, u32 AHEAD, u32 PARTS>
 __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offsets, u32 blocks, u32 rows, u32 per, bool by_blocks,
-                                                   const float *__restrict__ part, u32 n, u32 k, float *__restrict__ dw,
+                                                   const float *__restrict__ part, u32 n, u32 k, D *__restrict__ dw,
                                                    float *__restrict__ db, u32 pieces)
 {
     typedef __attribute__((ext_vector_type(V))) float vec;
@@ -326,16 +326,18 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
         float s = 0.0f;
 #pragma unroll
         for (u32 q = 0; q < PARTS; ++q) s += parts[q][threadIdx.x];
-        (at < size ? dw[(u64)block * size + at] : db[(u64)block * n + (at - size)]) = s;
+        if (at < size) dw[(u64)block * size + at] = (D)s;
+        else db[(u64)block * n + (at - size)] = s;
         return;
     }
     if (V > 1 && at + V <= size) {
-        if (dw) store_any(dw + (u64)block * size + at, sum(vec{}, at));
+        if (dw) store_any(dw + (u64)block * size + at, __builtin_convertvector(sum(vec{}, at), D __attribute__((ext_vector_type(V)))));
         return;
     }
     for (u64 i = at; i < at + V && i < stride; ++i) {
         if (i < size ? !dw : !db) continue;
-        (i < size ? dw[(u64)block * size + i] : db[(u64)block * n + (i - size)]) = sum(0.0f, i);
+        if (i < size) dw[(u64)block * size + i] = (D)sum(0.0f, i);
+        else db[(u64)block * n + (i - size)] = sum(0.0f, i);
     }
 }
 
@@ -461,18 +463,36 @@ struct JoinShape {
     bool many, parts;
     u32 pieces;             // workgroups of a block
 };
-static JoinShape join_shape(const lmk_gs_linear &l, const RunPlan &plan)
+static JoinShape join_shape(u32 n, u32 k, u32 blocks, u32 slices)
 {
     // few sums are many sets each, and latency; many are bytes (24 blocks of 96 x 35, 300 000 rows, gradients with
     // few as many and as few: 94 / 93 us; one block: 128 / 97; 4 blocks of 1024 x 1024, 1000 rows: 33 / 38)
-    const u64 stride = (u64)l.n * l.k + l.n;
+    const u64 stride = (u64)n * k + n;
     JoinShape j;
-    j.many = stride * l.blocks >= 1u << 20;
+    j.many = stride * blocks >= 1u << 20;
     // few sets a block are not worth parts (7 blocks of 131 x 257, 71 sets: 7.5 us with them, 4.0 without)
-    j.parts = !j.many && plan.slices / l.blocks >= 16;
+    j.parts = !j.many && slices / blocks >= 16;
     const u32 width = j.many ? 1024 : j.parts ? 32 : 256;
     j.pieces = (u32)((stride + width - 1) / width);
     return j;
+}
+
+template <class D>
+static hipError_t join_go(const u32 *offsets, u32 blocks, u32 rows, u32 per, bool by_blocks, const float *part, u32 n, u32 k, D *dw, float *db,
+                          u32 slices, hipStream_t stream)
+{
+    const JoinShape j = join_shape(n, k, blocks, slices);
+    auto kernel = j.many ? join_kernel<D, 4, 4, 1> : j.parts ? join_kernel<D, 1, 4, 8> : join_kernel<D, 1, 8, 1>;
+    hipLaunchKernelGGL(kernel, dim3(j.pieces * blocks), dim3(kThreads), 0, stream, offsets, blocks, rows, per, by_blocks, part, n, k, dw, db, j.pieces);
+    return hipGetLastError();
+}
+
+u64 join_threads(u32 n, u32 k, u32 blocks, u32 slices) { return (u64)join_shape(n, k, blocks, slices).pieces * blocks * kThreads; }
+
+hipError_t launch_join(const u32 *offsets, u32 blocks, u32 rows, u32 per, const float *part, u32 n, u32 k, float *dw, float *db, u32 slices,
+                       hipStream_t stream)
+{
+    return join_go(offsets, blocks, rows, per, true, part, n, k, dw, db, slices, stream);
 }
 
 // ---- what the calls hand to the kernels
@@ -551,7 +571,7 @@ bool grouped_backward_fits(const lmk_gs_linear &l, const void *dy, u64 lddy, con
 {
     const bool sums = out.dw || out.db;
     const RunPlan plan = sums ? run_plan(l) : RunPlan{};
-    if (sums && (u64)join_shape(l, plan).pieces * l.blocks * kThreads >= kMostThreads) return false;
+    if (sums && join_threads(l.n, l.k, l.blocks, plan.slices) >= kMostThreads) return false;
     // one pass takes a workgroup a run, of which there are at most some 1000 and one a block
     if (sums && one_pass(l) && narrow_backward_fits(one_pass_args(l, plan, dy, lddy, x, ldx, kept, gate, out, nullptr), kept != nullptr)) return true;
     if (out.dx && rows_threads(dx_args(l, dy, lddy, x, ldx, kept, gate, out), l.dtype, l.in_major == 0) >= kMostThreads) return false;
@@ -578,11 +598,7 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
     const RunPlan plan = sums ? run_plan(l) : RunPlan{};
     float *part = reinterpret_cast<float *>(workspace);
     const auto join = [&](bool by_blocks) {
-        const JoinShape j = join_shape(l, plan);
-        auto kernel = j.many ? join_kernel<4, 4, 1> : j.parts ? join_kernel<1, 4, 8> : join_kernel<1, 8, 1>;
-        hipLaunchKernelGGL(kernel, dim3(j.pieces * l.blocks), dim3(kThreads), 0, stream, l.offsets, l.blocks, l.rows, plan.per, by_blocks, part,
-                           l.n, l.k, out.dw, out.db, j.pieces);
-        return hipGetLastError();
+        return join_go(l.offsets, l.blocks, l.rows, plan.per, by_blocks, part, l.n, l.k, out.dw, out.db, plan.slices, stream);
     };
     if (sums && one_pass(l)) {
         const BackwardArgs r = one_pass_args(l, plan, dy, lddy, x, ldx, kept, gate, out, part);

@@ -1,0 +1,530 @@
+// Layer norm of rows whose gain and shift belong to blocks (lmk_gs_grouped_norm), and its gradients.
+//     m = mean(x), s = 1 / sqrt(mean((x - m)^2) + eps), h = (x - m) s
+//     y = gain_g h + shift_g
+//     d = dy gain_g,  dx = s (d - mean(d) - h mean(d h)),  dgain_g = sum of dy h,  dshift_g = sum of dy  over the block's rows
+// Everything between the loads and the one rounding of y and dx is in 32 bits.  The squares are of x less the mean, not
+// mean(x^2) - m^2: rows far from zero keep their digits.
+//
+// The mean is a quotient: a row of one value gives its shift.
+//
+// Bound by memory: a row is read once.  It stays in the registers of G lanes, C vectors of 16 bytes each, and what is summed
+// over it goes from lane to lane without LDS (G <= 64), or through LDS once a sum.  A workgroup has a run of rows of one block,
+// so that gain and shift are in registers, and so are its sums of dgain and dshift: x and dy are read once for all three gradients.
+#include "grouped_kernels.h"
+
+namespace lmk {
+
+namespace {
+
+struct NormArgs {
+    const void *x;              // [rows][k]
+    u64 ldx;
+    const void *dy;             // [rows][k], of the gradients
+    u64 lddy;
+    const float *gain, *shift;  // [blocks][k] or NULL
+    const u32 *offsets;
+    u32 blocks, rows, k;
+    float eps;
+    void *out;                  // y, or dx, or NULL
+    u64 ldo;
+    float *dgain, *dshift;      // [blocks][k], either may be NULL
+    float *part;                // sets of partial sums: k of dgain, then k of dshift
+    float *stats;               // rows longer than registers: mean and 1 / deviation of every row
+    u32 per;                    // rows of a run
+};
+
+template <class T> constexpr u32 kVec = 16 / sizeof(T);
+template <class T> using Vec = T __attribute__((ext_vector_type(16 / sizeof(T))));
+
+// Sum over the G lanes of a row, the same bits in all of them: neighbours, pairs, quads and halves of 16 lanes, then rows of 16 and
+// halves of the wavefront exchanged.
+template <int CTRL> __device__ __forceinline__ float add_dpp(float v)
+{
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+template <u32 G> __device__ __forceinline__ float lanes_sum(float v)
+{
+    static_assert(G == 8 || G == 16 || G == 64, "lanes of a row");
+    typedef __attribute__((ext_vector_type(2))) u32 two;
+    v = add_dpp<0xB1>(v);               // quad_perm 1 0 3 2
+    v = add_dpp<0x4E>(v);               // quad_perm 2 3 0 1
+    v = add_dpp<0x141>(v);              // row_half_mirror
+    if constexpr (G >= 16) v = add_dpp<0x140>(v);       // row_mirror
+    if constexpr (G == 64) {
+        two p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+        p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+    }
+    return v;
+}
+
+// N sums over the G threads of a row at once.  Rows of several wavefronts meet in LDS; `turn` flips between two places, so that one
+// meeting a call is enough: whoever writes a place again has passed the next meeting, and so has everyone who read it.
+template <u32 G, u32 N> struct RowSums {
+    static constexpr u32 kWaves = G / kWave;
+    __device__ __forceinline__ static void of(float (&v)[N], float *lds, u32 &turn)
+    {
+#pragma unroll
+        for (u32 i = 0; i < N; ++i) v[i] = lanes_sum<(G < kWave ? G : kWave)>(v[i]);
+        if constexpr (G > kWave) {
+            float *at = lds + turn * (kWaves * 4);
+            turn ^= 1;
+            if ((threadIdx.x & (kWave - 1)) == 0) {
+#pragma unroll
+                for (u32 i = 0; i < N; ++i) at[threadIdx.x / kWave * 4 + i] = v[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (u32 i = 0; i < N; ++i) {
+                v[i] = 0.0f;
+#pragma unroll
+                for (u32 w = 0; w < kWaves; ++w) v[i] += at[w * 4 + i];
+            }
+        }
+    }
+};
+
+// Chunk c of this lane: columns (c G + lane) V and on
+template <class T, u32 G, u32 C> struct RowOf {
+    static constexpr u32 V = kVec<T>;
+    // `whole`: the row is whole vectors
+    __device__ __forceinline__ static void load(Vec<T> (&v)[C], const T *p, u32 k, u32 lane, bool whole)
+    {
+#pragma unroll
+        for (u32 c = 0; c < C; ++c) {
+            const u32 at = (c * G + lane) * V;
+            if (whole) {
+                if (at < k) v[c] = load_any<Vec<T>>(p + at);
+                else v[c] = Vec<T>{};
+            } else {
+#pragma unroll
+                for (u32 e = 0; e < V; ++e) v[c][e] = at + e < k ? p[at + e] : (T)0.0f;
+            }
+        }
+    }
+    __device__ __forceinline__ static void store(T *p, const float (&v)[C][V], u32 k, u32 lane, bool whole)
+    {
+#pragma unroll
+        for (u32 c = 0; c < C; ++c) {
+            const u32 at = (c * G + lane) * V;
+            if (whole) {
+                Vec<T> o;
+#pragma unroll
+                for (u32 e = 0; e < V; ++e) o[e] = (T)v[c][e];
+                if (at < k) store_any(p + at, o);
+            } else {
+#pragma unroll
+                for (u32 e = 0; e < V; ++e)
+                    if (at + e < k) p[at + e] = (T)v[c][e];
+            }
+        }
+    }
+    __device__ __forceinline__ static void weights(float (&v)[C][V], const float *p, u32 k, u32 lane, float none)
+    {
+#pragma unroll
+        for (u32 c = 0; c < C; ++c)
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                const u32 at = (c * G + lane) * V + e;
+                v[c][e] = at >= k ? 0.0f : p ? p[at] : none;
+            }
+    }
+};
+
+constexpr u32 threads_of(u32 g) { return g > 256 ? g : 256; }
+
+template <class T, u32 G, u32 C>
+__global__ __launch_bounds__(threads_of(G)) void norm_kernel(const NormArgs r)
+{
+    using Row = RowOf<T, G, C>;
+    constexpr u32 V = Row::V, kAtOnce = threads_of(G) / G;
+    __shared__ float meet[2 * 16 * 4];
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
+    if (!run.found) return;
+    const u32 lane = threadIdx.x % G, begin = run.begin + run.local * r.per;
+    const u32 end = run.end - begin < r.per ? run.end : begin + r.per;
+    const bool whole = r.k % V == 0, inside = run.block != ~0u;
+    T *out = static_cast<T *>(r.out);
+    if (!inside) {
+        const float none[C][V] = {};
+        for (u32 row = begin + threadIdx.x / G; row < end; row += kAtOnce) Row::store(out + (u64)row * r.ldo, none, r.k, lane, whole);
+        return;
+    }
+    const T *x = static_cast<const T *>(r.x);
+    float gain[C][V], shift[C][V];
+    const u64 own = (u64)run.block * r.k;
+    Row::weights(gain, r.gain ? r.gain + own : nullptr, r.k, lane, 1.0f);
+    Row::weights(shift, r.shift ? r.shift + own : nullptr, r.k, lane, 0.0f);
+    const float share = 1.0f / (float)r.k;
+    u32 turn = 0;
+    Vec<T> next[C];
+    // threads without a row of their own repeat the run's last one: all meet equally often
+    const u32 turns = (end - begin + kAtOnce - 1) / kAtOnce;
+    const auto row_at = [&](u32 t) {
+        const u32 row = begin + t * kAtOnce + threadIdx.x / G;
+        return row < end ? row : end - 1;
+    };
+    Row::load(next, x + (u64)row_at(0) * r.ldx, r.k, lane, whole);
+    for (u32 t = 0; t < turns; ++t) {
+        float v[C][V];
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (u32 c = 0; c < C; ++c)
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                v[c][e] = to_f32(next[c][e]);
+                sum[0] += v[c][e];
+            }
+        if (t + 1 < turns) Row::load(next, x + (u64)row_at(t + 1) * r.ldx, r.k, lane, whole);
+        RowSums<G, 1>::of(sum, meet, turn);
+        const float mean = sum[0] / (float)r.k;
+        sum[0] = 0.0f;
+#pragma unroll
+        for (u32 c = 0; c < C; ++c)
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                v[c][e] -= mean;
+                if ((c * G + lane) * V + e < r.k) sum[0] += v[c][e] * v[c][e];
+            }
+        RowSums<G, 1>::of(sum, meet, turn);
+        const float s = 1.0f / sqrtf(sum[0] * share + r.eps);
+#pragma unroll
+        for (u32 c = 0; c < C; ++c)
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) v[c][e] = v[c][e] * s * gain[c][e] + shift[c][e];
+        const u32 row = begin + t * kAtOnce + threadIdx.x / G;
+        if (row < end) Row::store(out + (u64)row * r.ldo, v, r.k, lane, whole);
+    }
+}
+
+// SUMS: dgain and dshift, too
+template <class T, u32 G, u32 C, bool SUMS>
+__global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const NormArgs r)
+{
+    using Row = RowOf<T, G, C>;
+    constexpr u32 V = Row::V, kThreads = threads_of(G), kAtOnce = kThreads / G;
+    __shared__ float meet[2 * 16 * 4];
+    __shared__ float copies[SUMS && kAtOnce > 1 ? kThreads * C * V : 1];
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, r.per, blockIdx.x);
+    if (!run.found) return;
+    const u32 lane = threadIdx.x % G, begin = run.begin + run.local * r.per;
+    const u32 end = run.end - begin < r.per ? run.end : begin + r.per;
+    const bool whole = r.k % V == 0, inside = run.block != ~0u;
+    T *out = static_cast<T *>(r.out);
+    if (!inside) {
+        const float none[C][V] = {};
+        if (out)
+            for (u32 row = begin + threadIdx.x / G; row < end; row += kAtOnce) Row::store(out + (u64)row * r.ldo, none, r.k, lane, whole);
+        return;
+    }
+    const T *x = static_cast<const T *>(r.x), *dy = static_cast<const T *>(r.dy);
+    float gain[C][V], dgain[C][V] = {}, dshift[C][V] = {};
+    const u64 own = (u64)run.block * r.k;
+    Row::weights(gain, r.gain ? r.gain + own : nullptr, r.k, lane, 1.0f);
+    const float share = 1.0f / (float)r.k;
+    u32 turn = 0;
+    Vec<T> next_x[C], next_dy[C];
+    const u32 turns = (end - begin + kAtOnce - 1) / kAtOnce;
+    const auto request = [&](u32 t) {
+        u32 row = begin + t * kAtOnce + threadIdx.x / G;
+        row = row < end ? row : end - 1;
+        Row::load(next_x, x + (u64)row * r.ldx, r.k, lane, whole);
+        Row::load(next_dy, dy + (u64)row * r.lddy, r.k, lane, whole);
+    };
+    request(0);
+    for (u32 t = 0; t < turns; ++t) {
+        const u32 row = begin + t * kAtOnce + threadIdx.x / G;
+        const bool there = row < end;
+        float h[C][V], d[C][V];
+        float sum[1] = {0.0f};
+#pragma unroll
+        for (u32 c = 0; c < C; ++c)
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                h[c][e] = to_f32(next_x[c][e]);
+                d[c][e] = to_f32(next_dy[c][e]);
+                sum[0] += h[c][e];
+            }
+        if (t + 1 < turns) request(t + 1);
+        RowSums<G, 1>::of(sum, meet, turn);
+        const float mean = sum[0] / (float)r.k;
+        // squares, d, and d (x - m): the last two need no deviation yet
+        float sums[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (u32 c = 0; c < C; ++c)
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                const bool on = (c * G + lane) * V + e < r.k;
+                h[c][e] = on ? h[c][e] - mean : 0.0f;
+                const float w = d[c][e] * gain[c][e];
+                sums[0] += h[c][e] * h[c][e];
+                sums[1] += w;
+                sums[2] += w * h[c][e];
+            }
+        RowSums<G, 3>::of(sums, meet, turn);
+        const float s = 1.0f / sqrtf(sums[0] * share + r.eps), level = sums[1] * share, along = sums[2] * share * s;
+#pragma unroll
+        for (u32 c = 0; c < C; ++c)
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                const float g = d[c][e];
+                h[c][e] *= s;
+                if (SUMS && there) {
+                    dgain[c][e] += g * h[c][e];
+                    dshift[c][e] += g;
+                }
+                d[c][e] = s * (g * gain[c][e] - level - h[c][e] * along);
+            }
+        if (there && out) Row::store(out + (u64)row * r.ldo, d, r.k, lane, whole);
+    }
+    if constexpr (SUMS) {
+        const bool alone = run.end - run.begin <= r.per;
+        RowSlices all;
+        all.init(r.offsets, r.blocks, r.rows, r.per);
+        float *set = r.part + (u64)(run.block + all.slice_of(run.begin) + run.local) * 2 * r.k;
+        float *to[2] = {alone ? r.dgain ? r.dgain + own : nullptr : set, alone ? r.dshift ? r.dshift + own : nullptr : set + r.k};
+#pragma unroll
+        for (u32 q = 0; q < 2; ++q) {
+            float (&v)[C][V] = q == 0 ? dgain : dshift;
+            if constexpr (kAtOnce == 1) {
+                if (!to[q]) continue;
+#pragma unroll
+                for (u32 c = 0; c < C; ++c)
+#pragma unroll
+                    for (u32 e = 0; e < V; ++e) {
+                        const u32 at = (c * G + lane) * V + e;
+                        if (at < r.k) to[q][at] = v[c][e];
+                    }
+            } else {
+                // the rows that ran beside each other, added in their order
+                constexpr u32 width = G * C * V;
+                __syncthreads();
+#pragma unroll
+                for (u32 c = 0; c < C; ++c)
+#pragma unroll
+                    for (u32 e = 0; e < V; ++e) copies[threadIdx.x / G * width + (c * G + lane) * V + e] = v[c][e];
+                __syncthreads();
+                if (!to[q]) continue;
+                for (u32 at = threadIdx.x; at < r.k; at += kThreads) {
+                    float a = 0.0f;
+                    for (u32 w = 0; w < kAtOnce; ++w) a += copies[w * width + at];
+                    to[q][at] = a;
+                }
+            }
+        }
+    }
+}
+
+// ---- rows longer than a workgroup's registers: one row a workgroup of 1024, read again for every pass over it (from cache, mostly)
+constexpr u32 kLong = 1024;
+
+template <class T, bool BACKWARD>
+__global__ __launch_bounds__(kLong) void long_norm_kernel(const NormArgs r)
+{
+    __shared__ float meet[2 * 16 * 4];
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, 1, blockIdx.x);          // runs of one row
+    if (!run.found) return;
+    const u32 row = run.begin + run.local;
+    const T *x = static_cast<const T *>(r.x) + (u64)row * r.ldx, *dy = static_cast<const T *>(r.dy) + (BACKWARD ? (u64)row * r.lddy : 0);
+    T *out = r.out ? static_cast<T *>(r.out) + (u64)row * r.ldo : nullptr;
+    if (run.block == ~0u) {
+        if (out)
+            for (u32 i = threadIdx.x; i < r.k; i += kLong) out[i] = (T)0.0f;
+        return;
+    }
+    const float *gain = r.gain ? r.gain + (u64)run.block * r.k : nullptr, *shift = r.shift ? r.shift + (u64)run.block * r.k : nullptr;
+    const float share = 1.0f / (float)r.k;
+    u32 turn = 0;
+    float sum[1] = {0.0f};
+    for (u32 i = threadIdx.x; i < r.k; i += kLong) sum[0] += to_f32(x[i]);
+    RowSums<kLong, 1>::of(sum, meet, turn);
+    const float mean = sum[0] / (float)r.k;
+    float sums[3] = {0.0f, 0.0f, 0.0f};
+    for (u32 i = threadIdx.x; i < r.k; i += kLong) {
+        const float h = to_f32(x[i]) - mean;
+        sums[0] += h * h;
+        if (BACKWARD) {
+            const float w = to_f32(dy[i]) * (gain ? gain[i] : 1.0f);
+            sums[1] += w;
+            sums[2] += w * h;
+        }
+    }
+    RowSums<kLong, 3>::of(sums, meet, turn);
+    const float s = 1.0f / sqrtf(sums[0] * share + r.eps), level = sums[1] * share, along = sums[2] * share * s;
+    if (BACKWARD && r.stats && threadIdx.x == 0) {
+        r.stats[2 * (u64)row] = mean;
+        r.stats[2 * (u64)row + 1] = s;
+    }
+    if (!out) return;
+    for (u32 i = threadIdx.x; i < r.k; i += kLong) {
+        const float h = (to_f32(x[i]) - mean) * s, w = gain ? gain[i] : 1.0f;
+        out[i] = BACKWARD ? (T)(s * (to_f32(dy[i]) * w - level - h * along)) : (T)(h * w + (shift ? shift[i] : 0.0f));
+    }
+}
+
+// dgain and dshift of such rows: a thread sums a column over a run of rows
+template <class T>
+__global__ __launch_bounds__(256) void long_norm_sums_kernel(const NormArgs r)
+{
+    const u32 pieces = (r.k + 255) / 256, t = blockIdx.x / pieces;
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, r.per, t);
+    if (!run.found || run.block == ~0u) return;
+    const u32 at = (blockIdx.x - t * pieces) * 256 + threadIdx.x, begin = run.begin + run.local * r.per;
+    const u32 end = run.end - begin < r.per ? run.end : begin + r.per;
+    if (at >= r.k) return;
+    float dgain = 0.0f, dshift = 0.0f;
+    for (u32 row = begin; row < end; ++row) {
+        const float g = to_f32(static_cast<const T *>(r.dy)[(u64)row * r.lddy + at]);
+        const float h = (to_f32(static_cast<const T *>(r.x)[(u64)row * r.ldx + at]) - r.stats[2 * (u64)row]) * r.stats[2 * (u64)row + 1];
+        dgain += g * h;
+        dshift += g;
+    }
+    RowSlices all;
+    all.init(r.offsets, r.blocks, r.rows, r.per);
+    if (run.end - run.begin <= r.per) {
+        if (r.dgain) r.dgain[(u64)run.block * r.k + at] = dgain;
+        if (r.dshift) r.dshift[(u64)run.block * r.k + at] = dshift;
+    } else {
+        float *set = r.part + (u64)(run.block + all.slice_of(run.begin) + run.local) * 2 * r.k;
+        set[at] = dgain;
+        set[r.k + at] = dshift;
+    }
+}
+
+// ---- launches
+
+// How the threads share a row of k values: the fewest that hold it, with at most 16 values a thread (each stands in five registers in the
+// gradients), and 8 where a workgroup of 1024 leaves a thread 128 registers.
+struct NormShape {
+    u32 g, c;               // threads of a row, vectors of a thread; g = 0: longer than registers
+};
+NormShape norm_shape(u32 k, u32 dtype, bool backward)
+{
+    const bool f32 = dtype == LMK_GS_F32;
+    const u32 v = f32 ? 4 : 8, n = (k + v - 1) / v;
+    if (n <= 8) return {8, 1};
+    if (n <= 16) return {16, 1};
+    if (n <= 32) return {16, 2};
+    if (n <= 64) return {64, 1};
+    if (n <= 128) return {64, 2};
+    if (n <= 256) return f32 ? NormShape{64, 4} : NormShape{256, 1};
+    if (n <= 512) return {256, 2};
+    if (n <= 1024) return f32 ? NormShape{256, 4} : NormShape{1024, 1};
+    if (k <= 8192 || (!backward && k <= 16384)) return {1024, (n + 1023) / 1024 > 2 ? 4u : 2u};
+    return {0, 0};
+}
+
+// rows of a run
+u32 norm_per(u32 rows, u32 k, u32 dtype, bool backward)
+{
+    const NormShape s = norm_shape(k, dtype, backward);
+    const u32 at_once = s.g == 0 ? 1 : threads_of(s.g) / s.g;
+    // eight workgroups a compute unit, of whole turns
+    const u32 turns = (u32)(((u64)rows + 2048ull * at_once - 1) / (2048ull * at_once));
+    return (turns < 1 ? 1 : turns) * at_once;
+}
+
+template <class T, bool BACKWARD, u32 G, u32 C>
+hipError_t norm_go(const NormArgs &r, bool sums, hipStream_t stream)
+{
+    const dim3 grid((u32)max_runs(r.rows, r.blocks, r.per)), block(threads_of(G));
+    if constexpr (BACKWARD) {
+        if (sums) hipLaunchKernelGGL((norm_backward_kernel<T, G, C, true>), grid, block, 0, stream, r);
+        else hipLaunchKernelGGL((norm_backward_kernel<T, G, C, false>), grid, block, 0, stream, r);
+    } else {
+        hipLaunchKernelGGL((norm_kernel<T, G, C>), grid, block, 0, stream, r);
+    }
+    return hipGetLastError();
+}
+
+template <class T, bool BACKWARD>
+hipError_t norm_as(const NormArgs &r, hipStream_t stream)
+{
+    const bool sums = r.dgain || r.dshift;
+    const NormShape s = norm_shape(r.k, std::is_same<T, float>::value ? LMK_GS_F32 : LMK_GS_BF16, BACKWARD);
+    constexpr bool kF32 = std::is_same<T, float>::value;
+    switch (s.g * 8 + s.c) {
+    case 8 * 8 + 1: return norm_go<T, BACKWARD, 8, 1>(r, sums, stream);
+    case 16 * 8 + 1: return norm_go<T, BACKWARD, 16, 1>(r, sums, stream);
+    case 16 * 8 + 2: return norm_go<T, BACKWARD, 16, 2>(r, sums, stream);
+    case 64 * 8 + 1: return norm_go<T, BACKWARD, 64, 1>(r, sums, stream);
+    case 64 * 8 + 2: return norm_go<T, BACKWARD, 64, 2>(r, sums, stream);
+    case 64 * 8 + 4: if constexpr (kF32) return norm_go<T, BACKWARD, 64, 4>(r, sums, stream); break;
+    case 256 * 8 + 1: if constexpr (!kF32) return norm_go<T, BACKWARD, 256, 1>(r, sums, stream); break;
+    case 256 * 8 + 2: return norm_go<T, BACKWARD, 256, 2>(r, sums, stream);
+    case 256 * 8 + 4: if constexpr (kF32) return norm_go<T, BACKWARD, 256, 4>(r, sums, stream); break;
+    case 1024 * 8 + 1: if constexpr (!kF32) return norm_go<T, BACKWARD, 1024, 1>(r, sums, stream); break;
+    case 1024 * 8 + 2: if constexpr (kF32 || !BACKWARD) return norm_go<T, BACKWARD, 1024, 2>(r, sums, stream); break;
+    case 1024 * 8 + 4: if constexpr (kF32 && !BACKWARD) return norm_go<T, BACKWARD, 1024, 4>(r, sums, stream); break;
+    }
+    const auto rows_go = [&](const NormArgs &a) {
+        hipLaunchKernelGGL((long_norm_kernel<T, BACKWARD>), dim3(a.rows), dim3(kLong), 0, stream, a);
+        return hipGetLastError();
+    };
+    if (!BACKWARD || !sums) return rows_go(r);
+    // dx may take the place of what the sums read: statistics, sums, then dx
+    NormArgs stats = r;
+    stats.out = nullptr;
+    hipError_t e = rows_go(stats);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(long_norm_sums_kernel<T>, dim3((r.k + 255) / 256 * (u32)max_runs(r.rows, r.blocks, r.per)), dim3(256), 0, stream, r);
+    e = hipGetLastError();
+    return e == hipSuccess && r.out ? rows_go(r) : e;
+}
+
+NormArgs norm_args(const lmk_gs_norm &n, const void *x, u64 ldx, void *out, u64 ldo, bool backward)
+{
+    NormArgs r = {};
+    r.x = x; r.ldx = ldx;
+    r.gain = n.gain; r.shift = n.shift;
+    r.offsets = n.offsets; r.blocks = n.blocks; r.rows = n.rows; r.k = n.k; r.eps = n.eps;
+    r.out = out; r.ldo = ldo;
+    r.per = norm_per(n.rows, n.k, n.dtype, backward);
+    return r;
+}
+
+// sets of partial sums
+u64 norm_sets(const lmk_gs_norm &n) { return (u64)n.rows / norm_per(n.rows, n.k, n.dtype, true) + n.blocks + 1; }
+size_t norm_sets_bytes(const lmk_gs_norm &n) { return (size_t)(norm_sets(n) * 2 * n.k * 4 + 255) / 256 * 256; }
+
+}  // namespace
+
+bool grouped_norm_fits(const lmk_gs_norm &n, bool backward, bool sums)
+{
+    const NormShape s = norm_shape(n.k, n.dtype, backward);
+    const u64 runs = max_runs(n.rows, n.blocks, norm_per(n.rows, n.k, n.dtype, backward));
+    if (s.g == 0 ? (u64)n.rows * kLong >= kMostThreads : runs * threads_of(s.g) >= kMostThreads) return false;
+    if (s.g == 0 && sums && runs * ((n.k + 255) / 256) * 256 >= kMostThreads) return false;
+    return !sums || join_threads(n.k, 1, n.blocks, (u32)(norm_sets(n) - n.blocks)) < kMostThreads;
+}
+
+size_t grouped_norm_backward_bytes(const lmk_gs_norm &n)
+{
+    return norm_sets_bytes(n) + (norm_shape(n.k, n.dtype, true).g == 0 ? (size_t)n.rows * 8 : 0);
+}
+
+hipError_t launch_grouped_norm(const lmk_gs_norm &n, const void *x, u64 ldx, void *y, u64 ldy, hipStream_t stream)
+{
+    const NormArgs r = norm_args(n, x, ldx, y, ldy, false);
+    return n.dtype == LMK_GS_F32 ? norm_as<float, false>(r, stream) : norm_as<__bf16, false>(r, stream);
+}
+
+hipError_t launch_grouped_norm_backward(const lmk_gs_norm &n, const void *dy, u64 lddy, const void *x, u64 ldx,
+                                        const lmk_gs_norm_grads &out, char *workspace, hipStream_t stream)
+{
+    NormArgs r = norm_args(n, x, ldx, out.dx, out.lddx, true);
+    r.dy = dy; r.lddy = lddy;
+    r.dgain = out.dgain; r.dshift = out.dshift;
+    const bool sums = out.dgain || out.dshift;
+    r.part = reinterpret_cast<float *>(workspace);
+    r.stats = sums ? reinterpret_cast<float *>(workspace + norm_sets_bytes(n)) : nullptr;
+    if (n.rows > 0) {
+        const hipError_t e = n.dtype == LMK_GS_F32 ? norm_as<float, true>(r, stream) : norm_as<__bf16, true>(r, stream);
+        if (e != hipSuccess) return e;
+    }
+    return sums ? launch_join(n.offsets, n.blocks, n.rows, r.per, r.part, n.k, 1, out.dgain, out.dshift, (u32)(norm_sets(n) - n.blocks), stream)
+                : hipSuccess;
+}
+
+}  // namespace lmk

@@ -182,5 +182,11 @@ hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx,
 hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx,
                                    const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
                                    char *workspace, hipStream_t stream);
+// layer norm of blocks; `sums`: the gradients of gain and shift are among what is asked for
+bool grouped_norm_fits(const lmk_gs_norm &n, bool backward, bool sums);
+size_t grouped_norm_backward_bytes(const lmk_gs_norm &n);
+hipError_t launch_grouped_norm(const lmk_gs_norm &n, const void *x, u64 ldx, void *y, u64 ldy, hipStream_t stream);
+hipError_t launch_grouped_norm_backward(const lmk_gs_norm &n, const void *dy, u64 lddy, const void *x, u64 ldx,
+                                        const lmk_gs_norm_grads &out, char *workspace, hipStream_t stream);
 
 }  // namespace lmk

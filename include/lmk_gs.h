@@ -469,6 +469,40 @@ int32_t lmk_gs_grouped_norm_backward_bytes(const lmk_gs_norm *norm, size_t *byte
 int32_t lmk_gs_grouped_norm_backward(const lmk_gs_norm *norm, const void *dy, uint64_t lddy, const void *x, uint64_t ldx,
                                      const lmk_gs_norm_grads *out, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---- Gated layers of blocks, and their gradients: two projections of the input, one through an activation, and their product,
+ *   a = x[r] Wg[g]^T + bg[g], u = x[r] Wu[g]^T + bu[g], y[r] = act(a) u
+ * `layer` is a lmk_gs_linear whose matrices hold both projections, the gate's first: [2 n][k] with rows 0 .. n-1 of Wg and n .. 2n-1 of
+ * Wu, or with in_major [k][2 n]; n is the outputs of y, 1 .. 32768, and ldw at least 2 n with in_major.  Sums and activation in 32 bits, one rounding to
+ * dtype.  Rows of no block give zeros and enter no gradient. */
+#define LMK_GS_SILU 0u      /* a / (1 + e^-a); an a of -infinity gives NaN                              */
+#define LMK_GS_GELU 1u      /* a times the normal distribution at a; the same                           */
+#define LMK_GS_RELU 2u      /* max(a, 0), a NaN stays one; the gradient of a is 0 where a <= 0           */
+
+/* bias: [blocks][2 n] float32, bg first, or NULL.  y must not overlap x or w.  Otherwise as lmk_gs_grouped_linear; another act is
+ * LMK_GS_ERR_INVALID. */
+int32_t lmk_gs_grouped_gated(const lmk_gs_linear *layer, const void *x, uint64_t ldx, const float *bias, uint32_t act,
+                             void *y, uint64_t ldy, void *stream);
+
+/* Any of the three may be NULL; whole arrays are written, blocks without rows get zeros in dw and db. */
+typedef struct lmk_gs_gated_grads {
+    void *dx;        /* [rows][k], rows lddx apart, dtype                                                       */
+    uint64_t lddx;
+    void *dw;        /* laid out as w, dense ([blocks][2 n][k] or [blocks][k][2 n]), dtype, aligned to 4 bytes      */
+    float *db;       /* [blocks][2 n]                                                                            */
+} lmk_gs_gated_grads;
+
+/* Bytes of workspace of lmk_gs_grouped_gated_backward: the gradients of a and u for every row, and partial sums of dw and db.  Errors
+ * as lmk_gs_grouped_gated, for all gradients of packed rows. */
+int32_t lmk_gs_grouped_gated_backward_bytes(const lmk_gs_linear *layer, size_t *bytes);
+
+/* From dy [rows][n], the gradient of y, and the input x (a and u are computed again).  The gradients of a and u are rounded to dtype
+ * before dx and dw are summed from them in 32 bits; db is summed from them before that.  Sums over a block's rows are taken in an
+ * order that depends on the sizes and alignments only.  workspace: 256-byte aligned, always needed.  Outputs must not overlap inputs.  Errors as
+ * lmk_gs_grouped_gated; LMK_GS_ERR_CAPACITY: workspace too small. */
+int32_t lmk_gs_grouped_gated_backward(const lmk_gs_linear *layer, const void *dy, uint64_t lddy, const void *x, uint64_t ldx,
+                                      const float *bias, uint32_t act, const lmk_gs_gated_grads *out, void *workspace,
+                                      size_t workspace_bytes, void *stream);
+
 /* Copies {pair count D, status} of the frame from scratch to the host.
  * Synchronises `stream`.  Either output pointer may be NULL. */
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream);

@@ -28,7 +28,8 @@ EXPORTS = ("lmk_gs_workspace_bytes", "lmk_gs_preprocess", "lmk_gs_bin_sort", "lm
            "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static", "lmk_gs_grouped_linear",
            "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes", "lmk_gs_checkpoint8_pack",
            "lmk_gs_checkpoint8_unpack", "lmk_gs_grouped_norm", "lmk_gs_grouped_norm_backward",
-           "lmk_gs_grouped_norm_backward_bytes")
+           "lmk_gs_grouped_norm_backward_bytes", "lmk_gs_grouped_gated", "lmk_gs_grouped_gated_backward",
+           "lmk_gs_grouped_gated_backward_bytes")
 
 
 class Gaussians(C.Structure):
@@ -107,6 +108,10 @@ class NormGrads(C.Structure):
     _fields_ = [("dx", C.c_void_p), ("lddx", C.c_uint64), ("dgain", C.c_void_p), ("dshift", C.c_void_p)]
 
 
+class GatedGrads(C.Structure):
+    _fields_ = [("dx", C.c_void_p), ("lddx", C.c_uint64), ("dw", C.c_void_p), ("db", C.c_void_p)]
+
+
 class LmkGsError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -163,6 +168,11 @@ def lib() -> C.CDLL:
         l.lmk_gs_grouped_norm_backward.argtypes = [C.POINTER(NormC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64,
                                                    C.POINTER(NormGrads), C.c_void_p, C.c_size_t, C.c_void_p]
         l.lmk_gs_grouped_norm_backward_bytes.argtypes = [C.POINTER(NormC), C.POINTER(C.c_size_t)]
+        l.lmk_gs_grouped_gated.argtypes = [C.POINTER(LinearC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint64,
+                                           C.c_void_p]
+        l.lmk_gs_grouped_gated_backward.argtypes = [C.POINTER(LinearC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p,
+                                                    C.c_uint32, C.POINTER(GatedGrads), C.c_void_p, C.c_size_t, C.c_void_p]
+        l.lmk_gs_grouped_gated_backward_bytes.argtypes = [C.POINTER(LinearC), C.POINTER(C.c_size_t)]
         l.lmk_gs_read_status.argtypes = [C.c_void_p, C.POINTER(C.c_uint64), C.POINTER(C.c_int32), C.c_void_p]
         l.lmk_gs_strerror.argtypes = [C.c_int32]
         l.lmk_gs_strerror.restype = C.c_char_p
@@ -173,7 +183,8 @@ def lib() -> C.CDLL:
                      "lmk_gs_anchor_decode_culled", "lmk_gs_bin_sort_static", "lmk_gs_grouped_linear",
                      "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes",
                      "lmk_gs_checkpoint8_pack", "lmk_gs_checkpoint8_unpack", "lmk_gs_grouped_norm",
-                     "lmk_gs_grouped_norm_backward", "lmk_gs_grouped_norm_backward_bytes"):
+                     "lmk_gs_grouped_norm_backward", "lmk_gs_grouped_norm_backward_bytes", "lmk_gs_grouped_gated",
+                     "lmk_gs_grouped_gated_backward", "lmk_gs_grouped_gated_backward_bytes"):
             getattr(l, name).restype = C.c_int32
         l.lmk_gs_version.restype = C.c_uint32
         _lib = l
@@ -717,6 +728,68 @@ def grouped_norm_backward(dy, x, offsets, workspace=None, gain=None, eps: float 
                                             _stream_on(x, stream))
     if rc != OK:
         raise LmkGsError(rc, "lmk_gs_grouped_norm_backward")
+
+
+# ---- gated layers of blocks
+ACTS = {"silu": 0, "gelu": 1, "relu": 2}
+
+
+def _gated(w, offsets, rows: int, in_major: bool, act: str) -> LinearC:
+    """The layer with n of the outputs, of which its matrices have two each."""
+    if act not in ACTS:
+        raise ValueError(f"act is one of {tuple(ACTS)}, got {act!r}")
+    layer = _layer(w, offsets, rows, in_major)
+    if layer.n % 2:
+        raise ValueError("weights hold two projections: [blocks][2 outputs][inputs] (in_major: [blocks][inputs][2 outputs])")
+    layer.n //= 2
+    return layer
+
+
+def grouped_gated(x, w, offsets, out, bias=None, act: str = "silu", in_major: bool = False, stream=None) -> None:
+    """lmk_gs_grouped_gated: out[r] = act(wg[g] x[r] + bg[g]) * (wu[g] x[r] + bu[g]) for the rows offsets[g] .. offsets[g+1]-1 of every
+    block g.  w [blocks][2 outputs][inputs] holds wg and then wu (in_major: [blocks][inputs][2 outputs]), bias float32 [blocks][2 outputs]
+    bg and then bu; x [rows][inputs], out [rows][outputs], float32 or bfloat16 as w; offsets int32 [blocks + 1] on the device; act: "silu",
+    "gelu" or "relu"."""
+    layer = _gated(w, offsets, x.shape[0], in_major, act)
+    ldx = _matrix(x, (layer.rows, layer.k), w, "x")
+    ldy = _matrix(out, (layer.rows, layer.n), w, "out")
+    _dense(bias, (layer.blocks, 2 * layer.n), torch.float32, w, "bias")
+    _on_gpu(w)
+    rc = lib().lmk_gs_grouped_gated(C.byref(layer), _ptr(x), ldx, _ptr(bias), ACTS[act], _ptr(out), ldy, _stream_on(w, stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_gated")
+
+
+def grouped_gated_backward_bytes(rows: int, blocks: int, n: int, k: int, dtype=torch.float32) -> int:
+    """Workspace of grouped_gated_backward in bytes; n: outputs."""
+    out = C.c_size_t(0)
+    _fit_u32(rows, blocks, 2 * n, k)
+    layer = LinearC(256, 256, max(2 * n, k), max(2 * n, k) ** 2, blocks, rows, n, k, DTYPES[dtype], 0)
+    rc = lib().lmk_gs_grouped_gated_backward_bytes(C.byref(layer), C.byref(out))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_gated_backward_bytes")
+    return int(out.value)
+
+
+def grouped_gated_backward(dy, x, w, offsets, workspace, bias=None, act: str = "silu", dx=None, dw=None, db=None, in_major: bool = False,
+                           stream=None) -> None:
+    """lmk_gs_grouped_gated_backward: from dy [rows][outputs], the gradient of grouped_gated's out, and its input x to those of x, w
+    and bias; each of dx, dw, db may be left out.  dw is laid out as w, of its type and dense, db float32 [blocks][2 outputs];
+    workspace: a uint8 tensor of grouped_gated_backward_bytes."""
+    layer = _gated(w, offsets, x.shape[0], in_major, act)
+    ldx = _matrix(x, (layer.rows, layer.k), w, "x")
+    lddy = _matrix(dy, (layer.rows, layer.n), w, "dy")
+    _dense(bias, (layer.blocks, 2 * layer.n), torch.float32, w, "bias")
+    lddx = 0 if dx is None else _matrix(dx, (layer.rows, layer.k), w, "dx")
+    _dense(dw, w.shape, w.dtype, w, "dw")
+    _dense(db, (layer.blocks, 2 * layer.n), torch.float32, w, "db")
+    size = _workspace(workspace, w)
+    grads = GatedGrads(_ptr(dx), lddx, _ptr(dw), _ptr(db))
+    _on_gpu(w)
+    rc = lib().lmk_gs_grouped_gated_backward(C.byref(layer), _ptr(dy), lddy, _ptr(x), ldx, _ptr(bias), ACTS[act], C.byref(grads),
+                                             _ptr(workspace), size, _stream_on(w, stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_gated_backward")
 
 
 def read_status(frame: Frame, stream=None) -> tuple[int, int]:

@@ -37,6 +37,9 @@ UNITS = {
     "anchor_decode.hip": [],
     "checkpoint8.hip": [],
     "grouped_few.hip": [],
+    "grouped_gated.hip": [],
+    "grouped_gated_few.hip": [],
+    "grouped_gated_wide.hip": [],
     "grouped_linear.hip": [],
     "grouped_narrow.hip": [],
     "grouped_narrow_bwd.hip": [],

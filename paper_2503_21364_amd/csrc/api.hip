@@ -480,6 +480,63 @@ int32_t lmk_gs_grouped_norm_backward(const lmk_gs_norm *norm, const void *dy, ui
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
 
+// the checks of a layer with both projections' matrices
+static int32_t check_gated(const lmk_gs_linear *l, const float *bias, uint32_t act)
+{
+    if (!l) return LMK_GS_ERR_INVALID;
+    if (l->n > kMaxWidth / 2) return LMK_GS_ERR_INVALID;
+    lmk_gs_linear both = *l;
+    both.n = 2 * l->n;
+    const int32_t rc = check_linear(&both);
+    if (rc != LMK_GS_OK) return rc;
+    return act <= LMK_GS_RELU && aligned(bias, 4) ? LMK_GS_OK : LMK_GS_ERR_INVALID;
+}
+
+int32_t lmk_gs_grouped_gated(const lmk_gs_linear *layer, const void *x, uint64_t ldx, const float *bias, uint32_t act,
+                             void *y, uint64_t ldy, void *stream)
+{
+    const int32_t rc = check_gated(layer, bias, act);
+    if (rc != LMK_GS_OK) return rc;
+    if (layer->rows == 0) return LMK_GS_OK;
+    if (!good_rows(x, ldx, layer->k, layer->dtype) || !good_rows(y, ldy, layer->n, layer->dtype)) return LMK_GS_ERR_INVALID;
+    if (!grouped_gated_fits(*layer, x, ldx)) return LMK_GS_ERR_UNSUPPORTED;
+    const hipError_t e = launch_grouped_gated(*layer, x, ldx, bias, act, y, ldy, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
+int32_t lmk_gs_grouped_gated_backward_bytes(const lmk_gs_linear *layer, size_t *bytes)
+{
+    const int32_t rc = check_gated(layer, nullptr, 0);
+    if (rc != LMK_GS_OK) return rc;
+    if (!bytes) return LMK_GS_ERR_INVALID;
+    // all gradients, of packed rows: the pointers are only told from NULL
+    float any = 0.0f;
+    const lmk_gs_gated_grads all = {&any, layer->k, &any, &any};
+    if (!grouped_gated_backward_fits(*layer, nullptr, layer->k, all)) return LMK_GS_ERR_UNSUPPORTED;
+    *bytes = grouped_gated_backward_bytes(*layer);
+    return LMK_GS_OK;
+}
+
+int32_t lmk_gs_grouped_gated_backward(const lmk_gs_linear *layer, const void *dy, uint64_t lddy, const void *x, uint64_t ldx,
+                                      const float *bias, uint32_t act, const lmk_gs_gated_grads *out, void *workspace,
+                                      size_t workspace_bytes, void *stream)
+{
+    const int32_t rc = check_gated(layer, bias, act);
+    if (rc != LMK_GS_OK) return rc;
+    if (!out || !aligned(out->dw, 4) || !aligned(out->db, 4)) return LMK_GS_ERR_INVALID;
+    if (layer->rows > 0) {
+        if (!good_rows(dy, lddy, layer->n, layer->dtype) || !good_rows(x, ldx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
+        if (out->dx && !good_rows(out->dx, out->lddx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
+    }
+    if (!grouped_gated_backward_fits(*layer, x, ldx, *out)) return LMK_GS_ERR_UNSUPPORTED;
+    if (!workspace || !aligned(workspace, 256)) return LMK_GS_ERR_INVALID;
+    if (workspace_bytes < grouped_gated_backward_bytes(*layer)) return LMK_GS_ERR_CAPACITY;
+    if (!out->dw && !out->db && (!out->dx || layer->rows == 0)) return LMK_GS_OK;
+    const hipError_t e = launch_grouped_gated_backward(*layer, dy, lddy, x, ldx, bias, act, *out, static_cast<char *>(workspace),
+                                                       static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream)
 {
     if (!scratch) return LMK_GS_ERR_INVALID;

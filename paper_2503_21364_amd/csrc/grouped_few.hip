@@ -15,23 +15,6 @@ namespace {
 
 constexpr u32 kRows = 16;
 
-// V consecutive values as they are in memory, so that a load on its way holds no more registers than it fills
-template <class T, u32 V> using Run = T __attribute__((ext_vector_type(V)));
-
-// V values of a row from `s` on; beyond `sums` zeros.  WHOLE: rows are whole runs of V values
-template <class T, u32 V, bool WHOLE> __device__ __forceinline__ Run<T, V> load_run(const T *p, u32 s, u32 sums)
-{
-    Run<T, V> v = {};
-    if constexpr (WHOLE) {
-        if (s < sums) v = load_any<Run<T, V>>(p + s);
-    } else {
-#pragma unroll
-        for (u32 e = 0; e < V; ++e)
-            if (s + e < sums) v[e] = p[s + e];
-    }
-    return v;
-}
-
 // GATE: 0 none, 1 values, 2 codes
 template <class T, u32 NT, bool ACROSS, bool WHOLE, u32 GATE>
 __global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const RowsArgs r)

@@ -1,0 +1,97 @@
+// What the kernels of gated layers share: the activation, its slope, and their arguments.
+#ifndef LMK_GS_GROUPED_GATED_H
+#define LMK_GS_GROUPED_GATED_H
+#include "grouped_kernels.h"
+
+namespace lmk {
+
+// rows of a block against both projections of its weights
+struct GatedArgs {
+    const void *x;              // [rows][k]
+    u64 ldx;
+    const void *w;              // block g at g * w_block: [2 n][k] or [k][2 n], the gate's n first
+    u64 ldw, w_block;
+    const float *bias;          // [blocks][2 n] or NULL
+    const u32 *offsets;
+    u32 blocks, rows, n, k;
+    u32 act;
+    bool in_major;
+    void *out;                  // y [rows][n], or the gradients of both projections [rows][2 n]
+    u64 ldo;
+    const void *dy;             // NULL: y is asked for
+    u64 lddy;
+    float *part;                // NULL, or sets of partial sums over rows of the gradients, 2 n each
+    float *db;                  // where blocks of one set have theirs
+    u32 tiles, col_tiles;
+};
+
+// 1 / (1 + e^-a): the exponent's product is off by |a| 2^-24, which is e^-a's relative error
+__device__ __forceinline__ float logistic(float a)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a * -1.44269504f));
+}
+// The normal distribution at a, and its density.  Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), off by
+// 1.5e-7 at most for x >= 0; x = |a| / sqrt 2.
+__device__ __forceinline__ float normal(float a, float &density)
+{
+    const float x = __builtin_fabsf(a) * 0.707106781f, e = __builtin_amdgcn_exp2f(a * a * -0.721347520f);
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+    float s = 1.061405429f * t - 1.453152027f;
+    s = s * t + 1.421413741f;
+    s = s * t - 0.284496736f;
+    s = s * t + 0.254829592f;
+    const float tail = 0.5f * s * t * e;
+    density = e * 0.398942280f;
+    return a < 0.0f ? tail : 1.0f - tail;
+}
+
+__device__ __forceinline__ float gated(u32 act, float a, float u)
+{
+    if (act == LMK_GS_SILU) return a * logistic(a) * u;
+    if (act == LMK_GS_RELU) return (a < 0.0f ? 0.0f : a) * u;           // NaN stays
+    float density;
+    return a * normal(a, density) * u;
+}
+// gradients of a and u from that of the product
+__device__ __forceinline__ void gated_gradient(u32 act, float a, float u, float dy, float &da, float &du)
+{
+    if (act == LMK_GS_RELU) {
+        da = a <= 0.0f ? 0.0f : dy * u;                                 // NaN lets it pass
+        du = dy * (a < 0.0f ? 0.0f : a);
+        return;
+    }
+    float p, slope;
+    if (act == LMK_GS_SILU) {
+        p = logistic(a);
+        slope = p * (1.0f + a * (1.0f - p));
+    } else {
+        float density;
+        p = normal(a, density);
+        slope = p + a * density;
+    }
+    da = dy * u * slope;
+    du = dy * (a * p);
+}
+
+// The set of run `local` of a block whose first row is `begin`, in runs of `per` rows, as launch_join numbers them
+__device__ __forceinline__ float *set_of(const GatedArgs &r, const RowRun &run, u32 per)
+{
+    if (run.end - run.begin <= per) return r.db + (u64)run.block * 2 * r.n;
+    RowSlices all;
+    all.init(r.offsets, r.blocks, r.rows, per);
+    return r.part + (u64)(run.block + all.slice_of(run.begin) + run.local) * 2 * r.n;
+}
+
+// `..._rows`: rows of a tile, which are those of a set of partial sums; `..._threads`: those that a launch would have
+bool gated_few_fit(const GatedArgs &r, bool wide);
+u64 gated_few_threads(const GatedArgs &r);
+hipError_t launch_gated_few(const GatedArgs &r, u32 dtype, hipStream_t stream);
+constexpr u32 kGatedFewRows = 16, kGatedTileRows = 64;
+
+bool gated_wide_fits(const GatedArgs &r);
+u32 gated_wide_rows(const GatedArgs &r);
+u64 gated_wide_threads(const GatedArgs &r);
+hipError_t launch_gated_wide(const GatedArgs &r, hipStream_t stream);
+
+}  // namespace lmk
+#endif

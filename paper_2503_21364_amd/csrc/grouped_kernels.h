@@ -39,6 +39,7 @@ struct SumsArgs {
     const u32 *offsets;
     u32 blocks, rows, n, k;
     float *dw, *db;             // results, either may be NULL
+    bool dw16;                  // dw is in bfloat16
     u32 in_major;
     float *part;                // partial sums: n k of dw, then n of db each
     u32 slices, per;            // of the rows, and rows of each
@@ -79,6 +80,23 @@ __device__ __forceinline__ u32 tile_of_workgroup(u32 id, u32 total, u32 at_once)
     if (i >= run * dies && id >= whole) return id;
     const u32 die = i % dies, k = i / dies;
     return id < whole ? (k / run * dies + die) * run + k % run : whole + die * run + k;
+}
+
+// V consecutive values as they are in memory, so that a load on its way holds no more registers than it fills
+template <class T, u32 V> using Run = T __attribute__((ext_vector_type(V)));
+
+// V values of a row from `s` on; beyond `sums` zeros.  WHOLE: rows are whole runs of V values
+template <class T, u32 V, bool WHOLE> __device__ __forceinline__ Run<T, V> load_run(const T *p, u32 s, u32 sums)
+{
+    Run<T, V> v = {};
+    if constexpr (WHOLE) {
+        if (s < sums) v = load_any<Run<T, V>>(p + s);
+    } else {
+#pragma unroll
+        for (u32 e = 0; e < V; ++e)
+            if (s + e < sums) v[e] = p[s + e];
+    }
+    return v;
 }
 
 // `..._threads`: those that a launch would have

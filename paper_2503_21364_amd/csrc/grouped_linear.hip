@@ -9,174 +9,11 @@
 //
 // Bound by the rate of that instruction (154 TFLOP/s is what the largest library product reaches): 102 - 106 TFLOP/s at
 // 8192 rows x 4096 x 4096, 84 at 65 536 x 256 x 256 in 32 blocks.
-//
-// Both operands of a tile pass through LDS as [sum index][row or column]: a lane of half `hi` feeds sum
-// index t + 16 hi to step t, so the 32 lanes of a half read 32 consecutive floats, and with a pitch of 66
-// floats the two halves (16 pitches apart) are on different banks, as are the stores of an operand whose
-// sum index is contiguous in memory (eight lanes along it, 8 banks apart; eight rows on the banks between).
-#include "grouped_kernels.h"
+#include "grouped_tiles.h"
 
 namespace lmk {
 
 namespace {
-
-constexpr u32 kStep = 32;                 // sum indices of a staged step
-constexpr u32 kThreads = 256;
-
-constexpr u32 pitch_of(u32 width) { return width + 2; }
-
-// ---- operands: how a tile of `W` rows (columns) by kStep sum indices comes from memory.  load() only
-// requests; store() puts it into LDS.  Out of range: zeros.
-
-// sum index contiguous in memory: element (m, s) at p[m * ld + s]
-template <class T, u32 W> struct Along {
-    const T *p;
-    u64 ld;
-    u32 width, sums;        // valid rows, valid sum indices
-    float v[W / 8];
-
-    __device__ __forceinline__ void load(u32 s0)
-    {
-#pragma unroll
-        for (u32 i = 0; i < W / 32; ++i) {
-            const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = s0 + c % 8 * 4;
-            f32x4 q = {0.f, 0.f, 0.f, 0.f};
-            if (m < width) {
-                const T *a = p + (u64)m * ld + s;
-                if (s + 4 <= sums) q = load4(a);
-                else {
-#pragma unroll
-                    for (u32 j = 0; j < 4; ++j)
-                        if (s + j < sums) q[j] = to_f32(a[j]);
-                }
-            }
-#pragma unroll
-            for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
-        }
-    }
-    __device__ __forceinline__ void store(float *lds) const
-    {
-        constexpr u32 pitch = pitch_of(W);
-#pragma unroll
-        for (u32 i = 0; i < W / 32; ++i) {
-            const u32 c = threadIdx.x + i * kThreads, m = c / 8, s = c % 8 * 4;
-#pragma unroll
-            for (u32 j = 0; j < 4; ++j) lds[(s + j) * pitch + m] = v[4 * i + j];
-        }
-    }
-};
-
-// rows (columns) contiguous in memory: element (m, s) at p[s * ld + m]
-template <class T, u32 W> struct Across {
-    const T *p;
-    u64 ld;
-    u32 width, sums;
-    float v[W / 8];
-
-    __device__ __forceinline__ void load(u32 s0)
-    {
-#pragma unroll
-        for (u32 i = 0; i < W / 32; ++i) {
-            const u32 c = threadIdx.x + i * kThreads, s = s0 + c / (W / 4), m = c % (W / 4) * 4;
-            f32x4 q = {0.f, 0.f, 0.f, 0.f};
-            if (s < sums && m < width) {
-                const T *a = p + (u64)s * ld + m;
-                if (m + 4 <= width) q = load4(a);
-                else {
-#pragma unroll
-                    for (u32 j = 0; j < 4; ++j)
-                        if (m + j < width) q[j] = to_f32(a[j]);
-                }
-            }
-#pragma unroll
-            for (u32 j = 0; j < 4; ++j) v[4 * i + j] = q[j];
-        }
-    }
-    __device__ __forceinline__ void store(float *lds) const
-    {
-        constexpr u32 pitch = pitch_of(W);
-#pragma unroll
-        for (u32 i = 0; i < W / 32; ++i) {
-            const u32 c = threadIdx.x + i * kThreads, s = c / (W / 4), m = c % (W / 4) * 4;
-#pragma unroll
-            for (u32 j = 0; j < 4; ++j) lds[s * pitch + m + j] = v[4 * i + j];
-        }
-    }
-};
-
-// the same from the 8-bit form: rows of kp codes (all of them there), a scale byte for 32
-template <u32 W> struct Across8 {
-    const u32 *codes;       // of the tile's first row and column
-    const uint8_t *scale;
-    u32 kp;                 // codes of a row
-    u32 width, sums;        // width: codes to the end of the row
-    u32 q[W / 32];
-    u32 e[W / 32];
-
-    __device__ __forceinline__ void load(u32 s0)
-    {
-#pragma unroll
-        for (u32 i = 0; i < W / 32; ++i) {
-            const u32 c = threadIdx.x + i * kThreads, s = s0 + c / (W / 4), m = c % (W / 4) * 4;
-            const bool there = s < sums && m < width;
-            q[i] = there ? codes[((u64)s * kp + m) / 4] : 0u;
-            e[i] = there ? scale[(u64)s * (kp / 32) + m / 32] : 0u;
-        }
-    }
-    __device__ __forceinline__ void store(float *lds) const
-    {
-        constexpr u32 pitch = pitch_of(W);
-#pragma unroll
-        for (u32 i = 0; i < W / 32; ++i) {
-            const u32 c = threadIdx.x + i * kThreads, s = c / (W / 4), m = c % (W / 4) * 4;
-            const float step = step_of(e[i]);
-#pragma unroll
-            for (u32 j = 0; j < 4; ++j) lds[s * pitch + m + j] = value_of(q[i], j, step);
-        }
-    }
-};
-
-// Tiles of 64 x 64 results, 32 x 32 a wavefront: four workgroups a compute unit hide what a step waits for, and the
-// operands' way through LDS is no limit at this instruction's rate (128 x 128 tiles, two workgroups: 66 instead of 80 TFLOP/s at
-// 65 536 x 256 x 256, 101 instead of 104 at 8192 x 4096 x 4096).
-constexpr u32 kTile = 64;
-
-// The product of a tile: acc += A B over `sums`.  `each` is called with the staged A of every step.
-template <class A, class B, class Each>
-__device__ __forceinline__ void tile_product(A &a, B &b, u32 sums, float *lds, f32x16 &acc, Each &&each)
-{
-    constexpr u32 pitch = pitch_of(kTile), buffer = 2 * kStep * pitch;
-    const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    const u32 j = lane & 31, hi = lane / 32, m0 = wave / 2 * 32 + j, n0 = wave % 2 * 32 + j;
-    a.load(0);
-    b.load(0);
-    u32 at = 0;
-    for (u32 s0 = 0; s0 < sums; s0 += kStep, at ^= 1) {
-        float *la = lds + at * buffer, *lb = la + kStep * pitch;
-        a.store(la);
-        b.store(lb);
-        __syncthreads();                     // the other buffer's readers are past the previous one of these
-        if (s0 + kStep < sums) {
-            a.load(s0 + kStep);
-            b.load(s0 + kStep);
-        }
-        each(la);
-        // steps t and t + 16 in one instruction; the last ones of a short tile hold nothing
-        const u32 left = sums - s0;
-        auto step = [&](u32 t) {
-            acc = __builtin_amdgcn_mfma_f32_32x32x2f32(la[(t + 16 * hi) * pitch + m0], lb[(t + 16 * hi) * pitch + n0], acc, 0, 0, 0);
-        };
-        if (left >= 16) {
-#pragma unroll
-            for (u32 t = 0; t < 16; ++t) step(t);
-        } else {
-            for (u32 t = 0; t < left; ++t) step(t);
-        }
-    }
-}
-
-// row of a 32 x 32 result that register v of a lane of half hi holds (its column is lane % 32)
-__device__ __forceinline__ u32 row_of(u32 v, u32 hi) { return 8 * (v / 4) + 4 * hi + v % 4; }
 
 // ---- rows against weights
 
@@ -272,7 +109,9 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
             for (u32 v = 0; v < 16; ++v) {
                 const u32 row = wave / 2 * 32 + row_of(v, hi);
                 if (row >= height || col >= width) continue;
-                dw[r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col] = acc[v];
+                const u64 at = r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col;
+                if (r.dw16 && run.whole) reinterpret_cast<__bf16 *>(r.dw)[(u64)run.block * size + at] = (__bf16)acc[v];
+                else dw[at] = acc[v];
             }
         }
         if (r.db && k0 == 0 && threadIdx.x < height) db[n0 + threadIdx.x] = bias;
@@ -526,9 +365,10 @@ static RowsArgs dx_args(const lmk_gs_linear &l, const void *dy, u64 lddy, const 
     return r;
 }
 static SumsArgs sums_args(const lmk_gs_linear &l, const RunPlan &plan, const void *dy, u64 lddy, const void *x, u64 ldx,
-                          const lmk_gs_checkpoint8 *kept, const lmk_gs_linear_grads &out, float *part)
+                          const lmk_gs_checkpoint8 *kept, const lmk_gs_linear_grads &out, bool dw16, float *part)
 {
     SumsArgs r = {};
+    r.dw16 = dw16;
     r.dy = dy; r.lddy = lddy;
     r.x = kept ? (const void *)kept->codes : x;
     r.ldx = ldx;
@@ -575,7 +415,7 @@ bool grouped_backward_fits(const lmk_gs_linear &l, const void *dy, u64 lddy, con
     // one pass takes a workgroup a run, of which there are at most some 1000 and one a block
     if (sums && one_pass(l) && narrow_backward_fits(one_pass_args(l, plan, dy, lddy, x, ldx, kept, gate, out, nullptr), kept != nullptr)) return true;
     if (out.dx && rows_threads(dx_args(l, dy, lddy, x, ldx, kept, gate, out), l.dtype, l.in_major == 0) >= kMostThreads) return false;
-    return !sums || sums_threads(sums_args(l, plan, dy, lddy, x, ldx, kept, out, nullptr), l.dtype, sums_kind(out, kept)) < kMostThreads;
+    return !sums || sums_threads(sums_args(l, plan, dy, lddy, x, ldx, kept, out, false, nullptr), l.dtype, sums_kind(out, kept)) < kMostThreads;
 }
 
 size_t grouped_backward_bytes(const lmk_gs_linear &l)
@@ -592,12 +432,15 @@ hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx,
 
 hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx,
                                    const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
-                                   char *workspace, hipStream_t stream)
+                                   char *workspace, hipStream_t stream, bool dw16)
 {
     const bool sums = out.dw || out.db;
     const RunPlan plan = sums ? run_plan(l) : RunPlan{};
     float *part = reinterpret_cast<float *>(workspace);
     const auto join = [&](bool by_blocks) {
+        if (dw16)
+            return join_go(l.offsets, l.blocks, l.rows, plan.per, by_blocks, part, l.n, l.k, reinterpret_cast<__bf16 *>(out.dw), out.db, plan.slices,
+                           stream);
         return join_go(l.offsets, l.blocks, l.rows, plan.per, by_blocks, part, l.n, l.k, out.dw, out.db, plan.slices, stream);
     };
     if (sums && one_pass(l)) {
@@ -613,7 +456,7 @@ hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 l
         if (e != hipSuccess) return e;
     }
     if (!sums) return hipSuccess;
-    const SumsArgs r = sums_args(l, plan, dy, lddy, x, ldx, kept, out, part);
+    const SumsArgs r = sums_args(l, plan, dy, lddy, x, ldx, kept, out, dw16, part);
     const u32 kind = sums_kind(out, kept);
     const hipError_t e = l.dtype == LMK_GS_F32 ? sums_as<float>(r, kind, stream) : sums_as<__bf16>(r, kind, stream);
     return e == hipSuccess ? join(false) : e;

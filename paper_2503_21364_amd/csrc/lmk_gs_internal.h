@@ -179,14 +179,22 @@ bool grouped_backward_fits(const lmk_gs_linear &l, const void *dy, u64 lddy, con
 size_t grouped_backward_bytes(const lmk_gs_linear &l);
 hipError_t launch_grouped_linear(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, bool relu, void *y,
                                  u64 ldy, const lmk_gs_checkpoint8 *keep, hipStream_t stream);
+// dw16: out.dw is in bfloat16 (dtype too)
 hipError_t launch_grouped_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx,
                                    const lmk_gs_checkpoint8 *kept, bool gate, const lmk_gs_linear_grads &out,
-                                   char *workspace, hipStream_t stream);
+                                   char *workspace, hipStream_t stream, bool dw16 = false);
 // layer norm of blocks; `sums`: the gradients of gain and shift are among what is asked for
 bool grouped_norm_fits(const lmk_gs_norm &n, bool backward, bool sums);
 size_t grouped_norm_backward_bytes(const lmk_gs_norm &n);
 hipError_t launch_grouped_norm(const lmk_gs_norm &n, const void *x, u64 ldx, void *y, u64 ldy, hipStream_t stream);
 hipError_t launch_grouped_norm_backward(const lmk_gs_norm &n, const void *dy, u64 lddy, const void *x, u64 ldx,
                                         const lmk_gs_norm_grads &out, char *workspace, hipStream_t stream);
+// gated layers of blocks
+bool grouped_gated_fits(const lmk_gs_linear &l, const void *x, u64 ldx);
+bool grouped_gated_backward_fits(const lmk_gs_linear &l, const void *x, u64 ldx, const lmk_gs_gated_grads &out);
+size_t grouped_gated_backward_bytes(const lmk_gs_linear &l);
+hipError_t launch_grouped_gated(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, u32 act, void *y, u64 ldy, hipStream_t stream);
+hipError_t launch_grouped_gated_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx, const float *bias, u32 act,
+                                         const lmk_gs_gated_grads &out, char *workspace, hipStream_t stream);
 
 }  // namespace lmk

@@ -503,6 +503,41 @@ int32_t lmk_gs_grouped_gated_backward(const lmk_gs_linear *layer, const void *dy
                                       const float *bias, uint32_t act, const lmk_gs_gated_grads *out, void *workspace,
                                       size_t workspace_bytes, void *stream);
 
+/* ---- Layers of blocks in 4 bits: weights that stay resident in a quarter of bfloat16's bytes, and inputs taken to 4 bits for the product.
+ *
+ * The 4-bit form of a matrix of `rows` rows of k values: 32 consecutive values of a row share a power of two.  With A the
+ * largest |x| of the 32: the step is 2^e, e the least exponent >= -126 for which A / 2^e < 7, but at most 125; the code of x is the nearest of 0, 1/2, 1,
+ * 3/2, 2, 3, 4, 6 to |x| / 2^e (number 0 .. 7, halfway the one of even number), with x's sign in bit 3; the value a code stands for is that times
+ * 2^e, which a bfloat16 holds exactly.  scale = e + 127; 0 where all 32 are zero; 255 where one of the 32 is not finite (codes 0, all
+ * 32 read back as NaN).  Beyond column k codes and scales are 0.  These are the codes (e2m1) and scales (e8m0) of the microscaling formats. */
+typedef struct lmk_gs_block4 {
+    uint8_t *codes;           /* [rows][64 ceil(k / 128)]  device, 16-byte aligned: columns 2 i and 2 i + 1 in the low and high half of byte i */
+    uint8_t *scale;           /* [rows][16 ceil(k / 512)]  device, 16-byte aligned: columns 32 i .. 32 i + 31                                  */
+} lmk_gs_block4;
+
+/* x [rows][k], rows ldx apart, to its 4-bit form and back; k 1 .. 65536, rows below 2^31.  Asynchronous.  LMK_GS_ERR_INVALID: NULL
+ * pointer, size or stride out of range, a pointer that is not aligned; LMK_GS_ERR_UNSUPPORTED: another dtype, or sizes that take 2^32
+ * threads in one launch. */
+int32_t lmk_gs_block4_pack(const void *x, uint64_t ldx, uint32_t rows, uint32_t k, uint32_t dtype, const lmk_gs_block4 *out,
+                           void *stream);
+int32_t lmk_gs_block4_unpack(const lmk_gs_block4 *form, uint32_t rows, uint32_t k, uint32_t dtype, void *x, uint64_t ldx,
+                             void *stream);
+
+typedef struct lmk_gs_linear4 {
+    lmk_gs_block4 w;          /* 4-bit form of all blocks' matrices, [blocks n][k]: block g has the rows g n .. (g + 1) n - 1 */
+    const uint32_t *offsets;  /* [blocks + 1], as lmk_gs_linear.offsets                                                    */
+    uint32_t blocks;          /* 1 .. 65536                                                                                */
+    uint32_t rows;            /* rows of x and y (0 is allowed), below 2^31                                                */
+    uint32_t n, k;            /* outputs and inputs, 1 .. 65536                                                            */
+    uint32_t dtype;           /* LMK_GS_F32 or LMK_GS_BF16: type of y                                                      */
+} lmk_gs_linear4;
+
+/* y[r][j] = act(sum_i x[r][i] w_g[j][i] + bias[g][j]) for the rows r of every block g, x and w being what their 4-bit forms stand for; act
+ * and bias as lmk_gs_grouped_linear.  Sums in 32 bits, one rounding to dtype.  Rows of no block give zeros.  y must not overlap x or w.  Asynchronous on `stream`.
+ * Errors as lmk_gs_grouped_linear. */
+int32_t lmk_gs_grouped_linear4(const lmk_gs_linear4 *layer, const lmk_gs_block4 *x, const float *bias, uint32_t relu, void *y,
+                               uint64_t ldy, void *stream);
+
 /* Copies {pair count D, status} of the frame from scratch to the host.
  * Synchronises `stream`.  Either output pointer may be NULL. */
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream);

@@ -29,7 +29,7 @@ EXPORTS = ("lmk_gs_workspace_bytes", "lmk_gs_preprocess", "lmk_gs_bin_sort", "lm
            "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes", "lmk_gs_checkpoint8_pack",
            "lmk_gs_checkpoint8_unpack", "lmk_gs_grouped_norm", "lmk_gs_grouped_norm_backward",
            "lmk_gs_grouped_norm_backward_bytes", "lmk_gs_grouped_gated", "lmk_gs_grouped_gated_backward",
-           "lmk_gs_grouped_gated_backward_bytes")
+           "lmk_gs_grouped_gated_backward_bytes", "lmk_gs_block4_pack", "lmk_gs_block4_unpack", "lmk_gs_grouped_linear4")
 
 
 class Gaussians(C.Structure):
@@ -112,6 +112,15 @@ class GatedGrads(C.Structure):
     _fields_ = [("dx", C.c_void_p), ("lddx", C.c_uint64), ("dw", C.c_void_p), ("db", C.c_void_p)]
 
 
+class Block4C(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class Linear4C(C.Structure):
+    _fields_ = [("w", Block4C), ("offsets", C.c_void_p), ("blocks", C.c_uint32), ("rows", C.c_uint32), ("n", C.c_uint32),
+                ("k", C.c_uint32), ("dtype", C.c_uint32)]
+
+
 class LmkGsError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -173,6 +182,10 @@ def lib() -> C.CDLL:
         l.lmk_gs_grouped_gated_backward.argtypes = [C.POINTER(LinearC), C.c_void_p, C.c_uint64, C.c_void_p, C.c_uint64, C.c_void_p,
                                                     C.c_uint32, C.POINTER(GatedGrads), C.c_void_p, C.c_size_t, C.c_void_p]
         l.lmk_gs_grouped_gated_backward_bytes.argtypes = [C.POINTER(LinearC), C.POINTER(C.c_size_t)]
+        l.lmk_gs_block4_pack.argtypes = [C.c_void_p, C.c_uint64, C.c_uint32, C.c_uint32, C.c_uint32, C.POINTER(Block4C), C.c_void_p]
+        l.lmk_gs_block4_unpack.argtypes = [C.POINTER(Block4C), C.c_uint32, C.c_uint32, C.c_uint32, C.c_void_p, C.c_uint64, C.c_void_p]
+        l.lmk_gs_grouped_linear4.argtypes = [C.POINTER(Linear4C), C.POINTER(Block4C), C.c_void_p, C.c_uint32, C.c_void_p, C.c_uint64,
+                                             C.c_void_p]
         l.lmk_gs_read_status.argtypes = [C.c_void_p, C.POINTER(C.c_uint64), C.POINTER(C.c_int32), C.c_void_p]
         l.lmk_gs_strerror.argtypes = [C.c_int32]
         l.lmk_gs_strerror.restype = C.c_char_p
@@ -184,7 +197,8 @@ def lib() -> C.CDLL:
                      "lmk_gs_grouped_linear_backward", "lmk_gs_grouped_linear_backward_bytes",
                      "lmk_gs_checkpoint8_pack", "lmk_gs_checkpoint8_unpack", "lmk_gs_grouped_norm",
                      "lmk_gs_grouped_norm_backward", "lmk_gs_grouped_norm_backward_bytes", "lmk_gs_grouped_gated",
-                     "lmk_gs_grouped_gated_backward", "lmk_gs_grouped_gated_backward_bytes"):
+                     "lmk_gs_grouped_gated_backward", "lmk_gs_grouped_gated_backward_bytes", "lmk_gs_block4_pack",
+                     "lmk_gs_block4_unpack", "lmk_gs_grouped_linear4"):
             getattr(l, name).restype = C.c_int32
         l.lmk_gs_version.restype = C.c_uint32
         _lib = l
@@ -790,6 +804,68 @@ def grouped_gated_backward(dy, x, w, offsets, workspace, bias=None, act: str = "
                                              _ptr(workspace), size, _stream_on(w, stream))
     if rc != OK:
         raise LmkGsError(rc, "lmk_gs_grouped_gated_backward")
+
+
+# ---- layers of blocks in 4 bits
+class Block4:
+    """The 4-bit form of a [rows][k] matrix (lmk_gs_block4): `codes` uint8 [rows][64 ceil(k / 128)], two columns a byte, `scale` uint8
+    [rows][16 ceil(k / 512)], a byte for 32 columns."""
+
+    def __init__(self, rows: int, k: int, device="cuda:0", codes=None, scale=None):
+        self.rows, self.k = int(rows), int(k)
+        _fit_u32(self.rows, self.k)
+        shapes = (self.rows, (self.k + 127) // 128 * 64), (self.rows, (self.k + 511) // 512 * 16)
+        self.codes = torch.empty(shapes[0], dtype=torch.uint8, device=device) if codes is None else codes
+        self.scale = torch.empty(shapes[1], dtype=torch.uint8, device=self.codes.device) if scale is None else scale
+        _dense(self.codes, shapes[0], torch.uint8, self.codes, "codes")
+        _dense(self.scale, shapes[1], torch.uint8, self.codes, "scale")
+        self.c = Block4C(_ptr(self.codes), _ptr(self.scale))
+
+
+def block4_pack(x, form: Block4, stream=None) -> None:
+    """lmk_gs_block4_pack: the 4-bit form of x [rows][k], float32 or bfloat16."""
+    ldx = _matrix(x, (form.rows, form.k), x, "x")
+    if x.device != form.codes.device:
+        raise ValueError("x and the 4-bit form are on different devices")
+    dtype = _dtype(x)
+    _on_gpu(x)
+    rc = lib().lmk_gs_block4_pack(_ptr(x), ldx, form.rows, form.k, dtype, C.byref(form.c), _stream_on(x, stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_block4_pack")
+
+
+def block4_unpack(form: Block4, out, stream=None) -> None:
+    """lmk_gs_block4_unpack: the values the codes stand for (exact in bfloat16 too)."""
+    ldx = _matrix(out, (form.rows, form.k), out, "out")
+    if out.device != form.codes.device:
+        raise ValueError("out and the 4-bit form are on different devices")
+    dtype = _dtype(out)
+    _on_gpu(out)
+    rc = lib().lmk_gs_block4_unpack(C.byref(form.c), form.rows, form.k, dtype, _ptr(out), ldx, _stream_on(out, stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_block4_unpack")
+
+
+def grouped_linear4(x: Block4, w: Block4, offsets, out, bias=None, relu: bool = False, stream=None) -> None:
+    """lmk_gs_grouped_linear4: out[r] = act(w[g] x[r] + bias[g]) for the rows offsets[g] .. offsets[g+1]-1 of every block g, x [rows][inputs]
+    and w in 4 bits: w is the form of all blocks' matrices below each other, [blocks * outputs][inputs].  out [rows][outputs], float32 or
+    bfloat16; offsets int32 [blocks + 1] on the device; bias float32 [blocks][outputs]."""
+    blocks = _offsets(offsets, out)
+    if out.dim() != 2 or w.rows != blocks * out.shape[1]:
+        raise ValueError(f"out is [rows][outputs], and the weights' form has blocks * outputs rows, {w.rows} for {blocks} blocks")
+    n = out.shape[1]
+    _fit_u32(blocks, n)
+    ldy = _matrix(out, (x.rows, n), out, "out")
+    if x.k != w.k:
+        raise ValueError(f"x has {x.k} inputs, the weights {w.k}")
+    if x.codes.device != out.device or w.codes.device != out.device:
+        raise ValueError("x, the weights and out are on different devices")
+    _dense(bias, (blocks, n), torch.float32, out, "bias")
+    layer = Linear4C(w.c, _ptr(offsets), blocks, x.rows, n, x.k, _dtype(out))
+    _on_gpu(out)
+    rc = lib().lmk_gs_grouped_linear4(C.byref(layer), C.byref(x.c), _ptr(bias), int(relu), _ptr(out), ldy, _stream_on(out, stream))
+    if rc != OK:
+        raise LmkGsError(rc, "lmk_gs_grouped_linear4")
 
 
 def read_status(frame: Frame, stream=None) -> tuple[int, int]:

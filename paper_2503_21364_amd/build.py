@@ -35,12 +35,14 @@ UNITS = {
     "render_bwd.hip": [],       # same options as render.hip: pass 1 repeats its arithmetic
     "preprocess_bwd.hip": [],
     "anchor_decode.hip": [],
+    "block4.hip": [],
     "checkpoint8.hip": [],
     "grouped_few.hip": [],
     "grouped_gated.hip": [],
     "grouped_gated_few.hip": [],
     "grouped_gated_wide.hip": [],
     "grouped_linear.hip": [],
+    "grouped_linear4.hip": [],
     "grouped_narrow.hip": [],
     "grouped_narrow_bwd.hip": [],
     "grouped_norm.hip": [],

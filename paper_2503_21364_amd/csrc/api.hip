@@ -537,6 +537,49 @@ int32_t lmk_gs_grouped_gated_backward(const lmk_gs_linear *layer, const void *dy
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
 
+static bool good_block4(const lmk_gs_block4 &b) { return b.codes && b.scale && aligned(b.codes, 16) && aligned(b.scale, 16); }
+
+static int32_t check_block4(const void *x, uint64_t ldx, uint32_t rows, uint32_t k, uint32_t dtype, const lmk_gs_block4 *b)
+{
+    if (dtype != LMK_GS_F32 && dtype != LMK_GS_BF16) return LMK_GS_ERR_UNSUPPORTED;
+    if (!b || k == 0 || k > kMaxWidth || rows >= 1u << 31) return LMK_GS_ERR_INVALID;
+    if (rows > 0 && (!good_rows(x, ldx, k, dtype) || !good_block4(*b))) return LMK_GS_ERR_INVALID;
+    return block4_threads(rows, k) < kMostThreads ? LMK_GS_OK : LMK_GS_ERR_UNSUPPORTED;
+}
+
+int32_t lmk_gs_block4_pack(const void *x, uint64_t ldx, uint32_t rows, uint32_t k, uint32_t dtype, const lmk_gs_block4 *out,
+                           void *stream)
+{
+    const int32_t rc = check_block4(x, ldx, rows, k, dtype, out);
+    if (rc != LMK_GS_OK) return rc;
+    const hipError_t e = launch_block4_pack(x, ldx, rows, k, dtype, *out, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
+int32_t lmk_gs_block4_unpack(const lmk_gs_block4 *form, uint32_t rows, uint32_t k, uint32_t dtype, void *x, uint64_t ldx,
+                             void *stream)
+{
+    const int32_t rc = check_block4(x, ldx, rows, k, dtype, form);
+    if (rc != LMK_GS_OK) return rc;
+    const hipError_t e = launch_block4_unpack(*form, rows, k, dtype, x, ldx, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
+int32_t lmk_gs_grouped_linear4(const lmk_gs_linear4 *layer, const lmk_gs_block4 *x, const float *bias, uint32_t relu, void *y,
+                               uint64_t ldy, void *stream)
+{
+    if (!layer) return LMK_GS_ERR_INVALID;
+    if (layer->dtype != LMK_GS_F32 && layer->dtype != LMK_GS_BF16) return LMK_GS_ERR_UNSUPPORTED;
+    if (layer->blocks == 0 || layer->blocks > kMaxBlocks || layer->rows >= 1u << 31) return LMK_GS_ERR_INVALID;
+    if (layer->n == 0 || layer->k == 0 || layer->n > kMaxWidth || layer->k > kMaxWidth) return LMK_GS_ERR_INVALID;
+    if (!good_block4(layer->w) || !layer->offsets || !aligned(layer->offsets, 4) || relu > 1u || !aligned(bias, 4)) return LMK_GS_ERR_INVALID;
+    if (layer->rows == 0) return LMK_GS_OK;
+    if (!x || !good_block4(*x) || !good_rows(y, ldy, layer->n, layer->dtype)) return LMK_GS_ERR_INVALID;
+    if (!grouped_linear4_fits(*layer)) return LMK_GS_ERR_UNSUPPORTED;
+    const hipError_t e = launch_grouped_linear4(*layer, *x, bias, relu != 0, y, ldy, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
+}
+
 int32_t lmk_gs_read_status(const void *scratch, uint64_t *dup_count, int32_t *status, void *stream)
 {
     if (!scratch) return LMK_GS_ERR_INVALID;

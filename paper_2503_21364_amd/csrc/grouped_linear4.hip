@@ -2,7 +2,7 @@
 // v_mfma_scale_f32_16x16x128_f8f6f4.  A lane feeds 32 codes, 16 bytes, of one row and their scale byte; the products of codes and powers of two are
 // exact, sums are in 32 bits.
 #include "block4.h"
-#include "grouped_kernels.h"
+#include "grouped_wide.h"
 
 namespace lmk {
 
@@ -115,6 +115,196 @@ template <class T, u32 NT> hipError_t few_go(Linear4Args r, hipStream_t stream)
 }
 u32 few_columns(const Linear4Args &r) { return max_runs(r.rows, r.blocks, kRows) * ((r.n + 63) / 64) >= 320 ? 64 : 16; }
 
+// ---- tiles, as in grouped_wide.hip: a row's 256 codes are the 128 bytes that 64 bfloat16 are there, and come into LDS by the same loads, and a
+// lane's fragment is the 16 bytes with one scale.  The scales of 512 values of a row are 16 bytes; they come every second pair of steps, 64
+// rows a load, and a lane reads the four bytes of a step and takes its own.
+
+// of P and Q together, rows of a tile
+template <u32 TP, u32 TQ, u32 WAVES> struct Scales4 {
+    static_assert((TP + TQ) / 64 == WAVES && TP % 64 == 0, "one load a wavefront");
+    __amdgpu_buffer_rsrc_t from;        // this wavefront's rows: of P or of Q
+    u32 at;                             // this lane's row
+    u32 shift, p_read, q_read;
+
+    __device__ __forceinline__ void init(const uint8_t *p, u32 p_rows, const uint8_t *q, u32 q_rows, u32 bytes, u32 wave, u32 lane, u32 p0, u32 q0)
+    {
+        const bool of_p = wave < TP / 64;
+        from = buffer_of(of_p ? p : q, (of_p ? p_rows : q_rows) * bytes);
+        at = ((of_p ? wave : wave - TP / 64) * 64 + lane) * bytes;
+        shift = 8 * (lane >> 4);
+        p_read = (p0 + (lane & 15)) * 16;
+        q_read = (TP + q0 + (lane & 15)) * 16;
+    }
+    __device__ __forceinline__ void fill(lds_char *lds, u32 wave)
+    {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds + wave * 1024, 16, (int)at, 0, 0, 0);
+        at += 16;
+    }
+    __device__ __forceinline__ u32 of(const lds_char *lds, u32 read, u32 f, u32 step) const
+    {
+        return *reinterpret_cast<const __attribute__((address_space(3))) u32 *>(lds + read + f * 256 + step * 4) >> shift;
+    }
+};
+
+template <class T, class S, u32 TP, u32 TQ, u32 WP>
+__global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear4Args r)
+{
+    extern __shared__ __align__(16) char wide_lds[];
+    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, S::kResident * kUnits);
+    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * TP;
+    const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
+    if (!run.found) return;
+    const u32 row0 = run.begin + run.local * TQ;
+    const u32 height = run.end - row0 < TQ ? run.end - row0 : TQ;
+    const u32 width = r.n - col0 < TP ? r.n - col0 : TP;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
+    const u32 p0 = wave % WP * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
+    const bool inside = run.block != ~0u;
+    f32x4 acc[S::kP][S::kQ] = {};
+    if (inside) {
+        lds_char *lds = (lds_char *)wide_lds, *lp = lds, *lq = lds + 2 * S::kPartP, *ls = lds + S::kLds;
+        constexpr u32 kScales = (TP + TQ) * 16;
+        const u32 row_bytes = code_bytes(r.k), scales = scale_bytes(r.k), steps = row_bytes / 64;
+        const u64 wrow = (u64)run.block * r.n + col0;
+        Along16<TP, S::kWaves> p;
+        Along16<TQ, S::kWaves> q;
+        Scales4<TP, TQ, S::kWaves> sc;
+        p.init(reinterpret_cast<const __bf16 *>(r.w + wrow * row_bytes), row_bytes / 2, width, row_bytes / 2, wave, lane);
+        q.init(reinterpret_cast<const __bf16 *>(r.x + (u64)row0 * row_bytes), row_bytes / 2, height, row_bytes / 2, wave, lane);
+        sc.init(r.ws + wrow * scales, width, r.xs + (u64)row0 * scales, height, scales, wave, lane, p0, q0);
+        i32x4 fp[S::kP], fq[2][S::kQ];
+        u32 sp[S::kP], sq[2][S::kQ];
+        // `part` of the codes; the scales of steps 4 i and on are in half i % 2 of theirs
+        auto fill = [&](u32 part, u32 pair) {
+            p.fill(lp + part * S::kPartP, wave);
+            q.fill(lq + part * S::kPartQ, wave);
+            if (pair % 2 == 0) sc.fill(ls + (pair / 2 & 1) * kScales, wave);
+        };
+        // step t of eight, of which two pairs have the codes' parts and four the halves of the scales in turns
+        auto read_p = [&](u32 i, u32 t) {
+            fp[i] = __builtin_bit_cast(i32x4, p.fragment(lp + (t / 2 & 1) * S::kPartP, t & 1, p0, i));
+            sp[i] = sc.of(ls + (t / 4 & 1) * kScales, sc.p_read, i, t & 3);
+        };
+        auto read_q = [&](u32 j, u32 t) {
+            fq[t & 1][j] = __builtin_bit_cast(i32x4, q.fragment(lq + (t / 2 & 1) * S::kPartQ, t & 1, q0, j));
+            sq[t & 1][j] = sc.of(ls + (t / 4 & 1) * kScales, sc.q_read, j, t & 3);
+        };
+        // multiplies step t and reads the fragments of the next: those of P take the place of what has been used
+        auto step = [&](u32 t) {
+#pragma unroll
+            for (u32 j = 0; j < S::kQ; ++j) read_q(j, t + 1);
+#pragma unroll
+            for (u32 i = 0; i < S::kP; ++i) {
+#pragma unroll
+                for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = product4(fp[i], sp[i], fq[t & 1][j], sq[t & 1][j], acc[i][j]);
+                read_p(i, t + 1);
+            }
+            asm volatile("" ::: "memory");              // the reads stay in this step
+        };
+        fill(0, 0);
+        fill(1, 1);
+        wavefronts_meet<0x070>();
+#pragma unroll
+        for (u32 i = 0; i < S::kP; ++i) read_p(i, 0);
+#pragma unroll
+        for (u32 j = 0; j < S::kQ; ++j) read_q(j, 0);
+        for (u32 t0 = 0; t0 < steps; t0 += 8) {
+#pragma unroll
+            for (u32 t = 0; t < 8; t += 2) {
+                if (t0 + t >= steps) break;
+                step(t);
+                if (t0 + t + 1 >= steps) break;
+                // the next pair has arrived, and this pair's fragments have left LDS
+                wavefronts_meet<0x070>();
+                fill(t / 2 & 1, t / 2 + 2);
+                step(t + 1);
+            }
+        }
+        // nothing may be on its way into LDS when the workgroup ends
+        __builtin_amdgcn_s_waitcnt(0x070);
+    }
+    const u32 group = lane >> 4;
+    T *out = static_cast<T *>(r.y) + (u64)row0 * r.ldy + col0;
+#pragma unroll
+    for (u32 i = 0; i < S::kP; i += 2) {
+        f32x4 bias[2] = {};
+        if (r.bias && inside) {
+            const float *b = r.bias + (u64)run.block * r.n + col0;
+#pragma unroll
+            for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                for (u32 v = 0; v < 4; ++v) {
+                    const u32 c = p0 + 16 * (i + h) + 4 * group + v;
+                    bias[h][v] = c < width ? b[c] : 0.0f;
+                }
+        }
+#pragma unroll
+        for (u32 j = 0; j < S::kQ; ++j) {
+            const u32 row = q0 + 16 * j + (lane & 15);
+            f32x4 y[2] = {acc[i][j] + bias[0], acc[i + 1][j] + bias[1]};
+            if (r.relu) {
+#pragma unroll
+                for (u32 v = 0; v < 4; ++v) {
+                    y[0][v] = y[0][v] < 0.0f ? 0.0f : y[0][v];          // NaN stays
+                    y[1][v] = y[1][v] < 0.0f ? 0.0f : y[1][v];
+                }
+            }
+            if constexpr (sizeof(T) == 2) {
+                // two neighbouring results exchange lanes: eight consecutive values a lane
+                const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(y[0][0], y[0][1]), pack_bf16(y[1][0], y[1][1]), false, false);
+                const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(y[0][2], y[0][3]), pack_bf16(y[1][2], y[1][3]), false, false);
+                const u32x4 v = {a[0], b[0], a[1], b[1]};
+                const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1);
+                if (row >= height || c >= width) continue;
+                if (c + 8 <= width) {
+                    store_any(out + (u64)row * r.ldy + c, v);
+                } else {
+#pragma unroll
+                    for (u32 e = 0; e < 7; ++e)
+                        if (c + e < width) out[(u64)row * r.ldy + c + e] = __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2))));
+                }
+            } else {
+#pragma unroll
+                for (u32 h = 0; h < 2; ++h) {
+                    const u32 c = p0 + 16 * (i + h) + 4 * group;
+                    if (row >= height || c >= width) continue;
+                    if (c + 4 <= width) {
+                        store_any(out + (u64)row * r.ldy + c, y[h]);
+                    } else {
+#pragma unroll
+                        for (u32 v = 0; v < 3; ++v)
+                            if (c + v < width) out[(u64)row * r.ldy + c + v] = y[h][v];
+                    }
+                }
+            }
+        }
+    }
+}
+
+template <class T, u32 TP, u32 TQ, u32 WP, u32 WQ> hipError_t wide_go(Linear4Args r, hipStream_t stream)
+{
+    using S = Shape<TP, TQ, WP, WQ>;
+    constexpr u32 lds = S::kLds + 2 * (TP + TQ) * 16;
+    r.col_tiles = (r.n + TP - 1) / TP;
+    r.tiles = (u32)(max_runs(r.rows, r.blocks, TQ) * r.col_tiles);
+    auto kernel = wide_rows4_kernel<T, S, TP, TQ, WP>;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), lds, stream, r);
+    return hipGetLastError();
+}
+// as in grouped_wide.hip
+bool large_tiles(const Linear4Args &r)
+{
+    const auto share = [&](u32 side) { return __builtin_ceilf((float)r.rows / side + 0.5f * (r.blocks - 1)) * ((r.n + side - 1) / side); };
+    return __builtin_ceilf(share(256) / 256) < 0.7f * share(128) / 512;
+}
+bool few_fit(const Linear4Args &r)
+{
+    const u64 row_tiles = r.rows < r.blocks ? r.rows : r.blocks;
+    return (r.rows <= 128 || r.rows / 16 <= r.blocks) && row_tiles * ((r.n + 127) / 128) < 512;
+}
+
 Linear4Args linear4_args(const lmk_gs_linear4 &l, const lmk_gs_block4 &x, const float *bias, bool relu, void *y, u64 ldy)
 {
     Linear4Args r = {};
@@ -129,7 +319,8 @@ Linear4Args linear4_args(const lmk_gs_linear4 &l, const lmk_gs_block4 &x, const 
 
 template <class T> hipError_t linear4_as(const Linear4Args &r, hipStream_t stream)
 {
-    return few_columns(r) == 64 ? few_go<T, 64>(r, stream) : few_go<T, 16>(r, stream);
+    if (few_fit(r)) return few_columns(r) == 64 ? few_go<T, 64>(r, stream) : few_go<T, 16>(r, stream);
+    return large_tiles(r) ? wide_go<T, 256, 256, 2, 4>(r, stream) : wide_go<T, 128, 128, 2, 2>(r, stream);
 }
 
 }  // namespace
@@ -137,8 +328,8 @@ template <class T> hipError_t linear4_as(const Linear4Args &r, hipStream_t strea
 bool grouped_linear4_fits(const lmk_gs_linear4 &l)
 {
     const Linear4Args r = linear4_args(l, {}, nullptr, false, nullptr, 0);
-    const u32 nt = few_columns(r);
-    return max_runs(r.rows, r.blocks, kRows) * ((r.n + nt - 1) / nt) * 512 < kMostThreads;
+    const u32 nt = few_fit(r) ? few_columns(r) : large_tiles(r) ? 256 : 128, per = few_fit(r) ? kRows : nt;
+    return max_runs(r.rows, r.blocks, per) * ((r.n + nt - 1) / nt) * (few_fit(r) ? 512 : 2 * nt) < kMostThreads;
 }
 
 hipError_t launch_grouped_linear4(const lmk_gs_linear4 &l, const lmk_gs_block4 &x, const float *bias, bool relu, void *y, u64 ldy,

@@ -552,7 +552,7 @@ int32_t lmk_gs_block4_pack(const void *x, uint64_t ldx, uint32_t rows, uint32_t 
 {
     const int32_t rc = check_block4(x, ldx, rows, k, dtype, out);
     if (rc != LMK_GS_OK) return rc;
-    const hipError_t e = launch_block4_pack(x, ldx, rows, k, dtype, *out, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_block4(const_cast<void *>(x), ldx, rows, k, dtype, *out, false, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
 
@@ -561,7 +561,7 @@ int32_t lmk_gs_block4_unpack(const lmk_gs_block4 *form, uint32_t rows, uint32_t 
 {
     const int32_t rc = check_block4(x, ldx, rows, k, dtype, form);
     if (rc != LMK_GS_OK) return rc;
-    const hipError_t e = launch_block4_unpack(*form, rows, k, dtype, x, ldx, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_block4(x, ldx, rows, k, dtype, *form, true, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
 

@@ -198,8 +198,8 @@ hipError_t launch_grouped_gated_backward(const lmk_gs_linear &l, const void *dy,
                                          const lmk_gs_gated_grads &out, char *workspace, hipStream_t stream);
 // 4-bit forms, and layers of them
 u64 block4_threads(u32 rows, u32 k);
-hipError_t launch_block4_pack(const void *x, u64 ldx, u32 rows, u32 k, u32 dtype, const lmk_gs_block4 &out, hipStream_t stream);
-hipError_t launch_block4_unpack(const lmk_gs_block4 &form, u32 rows, u32 k, u32 dtype, void *x, u64 ldx, hipStream_t stream);
+// x to its form (which only reads it), or `back`
+hipError_t launch_block4(void *x, u64 ldx, u32 rows, u32 k, u32 dtype, const lmk_gs_block4 &form, bool back, hipStream_t stream);
 bool grouped_linear4_fits(const lmk_gs_linear4 &l);
 hipError_t launch_grouped_linear4(const lmk_gs_linear4 &l, const lmk_gs_block4 &x, const float *bias, bool relu, void *y, u64 ldy,
                                   hipStream_t stream);

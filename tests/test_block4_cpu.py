@@ -1,8 +1,6 @@
-"""The 4-bit form and its layers without a GPU: the oracle against its definition, the arithmetic of the kernels against the oracle, and
+"""The 4-bit form and its layers without a GPU: the oracle against its definition, and
 the calls' checks of their arguments."""
 import ctypes as C
-import os
-import subprocess
 
 import numpy as np
 import pytest
@@ -10,7 +8,6 @@ import torch
 
 from oracle import block4_ref as Q
 from paper_2503_21364_amd import binding as B
-from paper_2503_21364_amd import build as hip_build
 
 
 def _values():
@@ -50,23 +47,6 @@ def test_forms_of_the_oracle_are_nearest_and_steps_least():
 @pytest.mark.parametrize("q,n", [(0.25, 0), (0.2500001, 1), (0.75, 2), (1.25, 2), (1.75, 4), (2.5, 4), (3.5, 6), (5.0, 6), (5.0001, 7), (6.99, 7)])
 def test_ties_go_to_the_even_code(q, n):
     assert Q.number(q) == n
-
-
-def test_arithmetic_of_the_kernels_is_the_oracles(tmp_path):
-    # code4_of, scale4_of_max and value4_of, built for the host
-    exe = str(tmp_path / "block4")
-    subprocess.run([hip_build.hipcc(), "-std=c++17", "-O1", f"--offload-arch={hip_build.ARCH}", "--offload-host-only", "-x", "hip",
-                    os.path.join(os.path.dirname(__file__), "host", "block4_driver.cpp"), "-I", hip_build.INCLUDE, "-I", hip_build.CSRC, "-o", exe],
-                   check=True, capture_output=True)
-    x = np.zeros((60, 160), np.float32)
-    x[:, :131] = _values()
-    got = subprocess.run([exe], input=x.tobytes(), check=True, capture_output=True).stdout
-    got = np.frombuffer(got, np.float32).reshape(60 * 5, 65)
-    codes, scale = Q.pack(x)
-    np.testing.assert_array_equal(got[:, 0], scale[:, :5].reshape(-1))
-    code = np.stack([codes & 15, codes >> 4], axis=-1).reshape(60, -1)[:, :160].reshape(-1, 32)
-    np.testing.assert_array_equal(got[:, 1:33], code)
-    np.testing.assert_array_equal(got[:, 33:].astype(np.float64), Q.unpack(codes, scale, 160).reshape(-1, 32))
 
 
 # ---- refusals (fake pointers: every call below has to be refused before it reaches them)

@@ -238,8 +238,8 @@ def _ptr(t) -> int | None:
 
 
 def _stream_handle(stream) -> int | None:
-    if stream is None:
-        stream = torch.cuda.current_stream()
+    if stream is None:                  # the handle itself: a Stream object around it takes 2.5 us to make
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
     return stream.cuda_stream or None
 
 
@@ -535,7 +535,7 @@ def _dtype(t) -> int:
 
 def _matrix(t, shape, like, name):
     """The row stride of a 2-d tensor of `shape` with whole rows, of the type and on the device of `like`."""
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype != like.dtype or t.device != like.device:
         raise ValueError(f"{name} has another type or device ({t.dtype}, {t.device})")
@@ -545,13 +545,16 @@ def _matrix(t, shape, like, name):
 
 
 def _dense(t, shape, dtype, like, name):
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != like.device or not t.is_contiguous()):
+    if t is not None and (t.shape != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous()):
         raise ValueError(f"{name} has to be a contiguous {dtype} tensor {tuple(shape)} on {like.device}")
 
 
 def _fit_u32(*sizes):
     """Sizes that a 32-bit field would cut off: ctypes does so without a word."""
-    if any(size >> 32 for size in sizes):
+    all_bits = 0
+    for size in sizes:
+        all_bits |= size
+    if all_bits >> 32:                  # of a negative one, too
         raise ValueError(f"sizes of 2^32 or more, or below 0: {sizes}")
 
 
@@ -670,11 +673,14 @@ def checkpoint8_unpack(checkpoint: Checkpoint8, out, stream=None) -> None:
 # ---- layer norm of the rows of blocks
 def _stream_on(like, stream):
     """The handle of `stream` (None: the current one), which has to be of the tensors' device, and that the current one."""
-    if like.device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {like.device}, the current device is cuda:{torch.cuda.current_device()}")
-    if stream is not None and stream.device != like.device:
+    device = torch.cuda.current_device()
+    if like.get_device() != device:
+        raise ValueError(f"the tensors are on {like.device}, the current device is cuda:{device}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device) or None
+    if stream.device != like.device:
         raise ValueError(f"the tensors are on {like.device}, the stream on {stream.device}")
-    return _stream_handle(stream)
+    return stream.cuda_stream or None
 
 
 def _offsets(offsets, like) -> int:

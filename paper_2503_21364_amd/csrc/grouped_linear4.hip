@@ -129,7 +129,7 @@ template <u32 TP, u32 TQ, u32 WAVES> struct Scales4 {
     __device__ __forceinline__ void init(const uint8_t *p, u32 p_rows, const uint8_t *q, u32 q_rows, u32 bytes, u32 wave, u32 lane, u32 p0, u32 q0)
     {
         const bool of_p = wave < TP / 64;
-        from = buffer_of(of_p ? p : q, (of_p ? p_rows : q_rows) * bytes);
+        from = buffer_of(reinterpret_cast<const void *>(uniform64(reinterpret_cast<u64>(of_p ? p : q))), uniform((of_p ? p_rows : q_rows) * bytes));
         at = ((of_p ? wave : wave - TP / 64) * 64 + lane) * bytes;
         shift = 8 * (lane >> 4);
         p_read = (p0 + (lane & 15)) * 16;
@@ -151,7 +151,8 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear
 {
     extern __shared__ __align__(16) char wide_lds[];
     const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, S::kResident * kUnits);
-    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * TP;
+    // four rows of tiles beside each other: what a die works on at once is four by eight of them, and shares most of its operands
+    const u32 band = tile / (4 * r.col_tiles), in = tile - band * 4 * r.col_tiles, row_tile = 4 * band + in % 4, col0 = in / 4 * TP;
     const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
     if (!run.found) return;
     const u32 row0 = run.begin + run.local * TQ;
@@ -160,7 +161,20 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear
     const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     const u32 p0 = wave % WP * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
     const bool inside = run.block != ~0u;
-    f32x4 acc[S::kP][S::kQ] = {};
+    // the sums begin with the bias
+    f32x4 acc[S::kP][S::kQ];
+#pragma unroll
+    for (u32 i = 0; i < S::kP; ++i) {
+        f32x4 b = {};
+        if (r.bias && inside) {
+            const u32 c = p0 + 16 * i + 4 * (lane >> 4);
+            const float *from = r.bias + (u64)run.block * r.n + col0;
+#pragma unroll
+            for (u32 v = 0; v < 4; ++v) b[v] = from[c + v < width ? c + v : 0u];
+        }
+#pragma unroll
+        for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = b;
+    }
     if (inside) {
         lds_char *lds = (lds_char *)wide_lds, *lp = lds, *lq = lds + 2 * S::kPartP, *ls = lds + S::kLds;
         constexpr u32 kScales = (TP + TQ) * 16;
@@ -169,8 +183,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear
         Along16<TP, S::kWaves> p;
         Along16<TQ, S::kWaves> q;
         Scales4<TP, TQ, S::kWaves> sc;
-        p.init(reinterpret_cast<const __bf16 *>(r.w + wrow * row_bytes), row_bytes / 2, width, row_bytes / 2, wave, lane);
-        q.init(reinterpret_cast<const __bf16 *>(r.x + (u64)row0 * row_bytes), row_bytes / 2, height, row_bytes / 2, wave, lane);
+        const auto first_of = [](const char *of, u64 bytes) { return reinterpret_cast<const __bf16 *>(uniform64(reinterpret_cast<u64>(of) + bytes)); };
+        p.init(first_of(r.w, wrow * row_bytes), row_bytes / 2, width, row_bytes / 2, wave, lane);
+        q.init(first_of(r.x, (u64)row0 * row_bytes), row_bytes / 2, height, row_bytes / 2, wave, lane);
         sc.init(r.ws + wrow * scales, width, r.xs + (u64)row0 * scales, height, scales, wave, lane, p0, q0);
         i32x4 fp[S::kP], fq[2][S::kQ];
         u32 sp[S::kP], sq[2][S::kQ];
@@ -223,62 +238,53 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear
         // nothing may be on its way into LDS when the workgroup ends
         __builtin_amdgcn_s_waitcnt(0x070);
     }
-    const u32 group = lane >> 4;
+    if (r.relu) {
+#pragma unroll
+        for (u32 i = 0; i < S::kP; ++i)
+#pragma unroll
+            for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = __builtin_elementwise_maximum(acc[i][j], f32x4{});          // NaN stays
+    }
     T *out = static_cast<T *>(r.y) + (u64)row0 * r.ldy + col0;
-#pragma unroll
-    for (u32 i = 0; i < S::kP; i += 2) {
-        f32x4 bias[2] = {};
-        if (r.bias && inside) {
-            const float *b = r.bias + (u64)run.block * r.n + col0;
-#pragma unroll
-            for (u32 h = 0; h < 2; ++h)
-#pragma unroll
-                for (u32 v = 0; v < 4; ++v) {
-                    const u32 c = p0 + 16 * (i + h) + 4 * group + v;
-                    bias[h][v] = c < width ? b[c] : 0.0f;
-                }
-        }
+    // `all`: every result of the tile is there
+    const auto store = [&](auto all) {
+        const u32 group = lane >> 4;
 #pragma unroll
         for (u32 j = 0; j < S::kQ; ++j) {
             const u32 row = q0 + 16 * j + (lane & 15);
-            f32x4 y[2] = {acc[i][j] + bias[0], acc[i + 1][j] + bias[1]};
-            if (r.relu) {
+            T *to = out + (u64)row * r.ldy;
 #pragma unroll
-                for (u32 v = 0; v < 4; ++v) {
-                    y[0][v] = y[0][v] < 0.0f ? 0.0f : y[0][v];          // NaN stays
-                    y[1][v] = y[1][v] < 0.0f ? 0.0f : y[1][v];
-                }
-            }
-            if constexpr (sizeof(T) == 2) {
-                // two neighbouring results exchange lanes: eight consecutive values a lane
-                const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(y[0][0], y[0][1]), pack_bf16(y[1][0], y[1][1]), false, false);
-                const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(y[0][2], y[0][3]), pack_bf16(y[1][2], y[1][3]), false, false);
-                const u32x4 v = {a[0], b[0], a[1], b[1]};
-                const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1);
-                if (row >= height || c >= width) continue;
-                if (c + 8 <= width) {
-                    store_any(out + (u64)row * r.ldy + c, v);
+            for (u32 i = 0; i < S::kP; i += 2) {
+                if constexpr (sizeof(T) == 2) {
+                    // two neighbouring results exchange lanes: eight consecutive values a lane
+                    const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i + 1][j][0], acc[i + 1][j][1]), false, false);
+                    const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][2], acc[i][j][3]), pack_bf16(acc[i + 1][j][2], acc[i + 1][j][3]), false, false);
+                    const u32x4 v = {a[0], b[0], a[1], b[1]};
+                    const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1);
+                    if (all || (row < height && c + 8 <= width)) {
+                        store_any(to + c, v);
+                    } else if (row < height) {
+#pragma unroll
+                        for (u32 e = 0; e < 7; ++e)
+                            if (c + e < width) to[c + e] = __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2))));
+                    }
                 } else {
 #pragma unroll
-                    for (u32 e = 0; e < 7; ++e)
-                        if (c + e < width) out[(u64)row * r.ldy + c + e] = __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2))));
-                }
-            } else {
+                    for (u32 h = 0; h < 2; ++h) {
+                        const u32 c = p0 + 16 * (i + h) + 4 * group;
+                        if (all || (row < height && c + 4 <= width)) {
+                            store_any(to + c, acc[i + h][j]);
+                        } else if (row < height) {
 #pragma unroll
-                for (u32 h = 0; h < 2; ++h) {
-                    const u32 c = p0 + 16 * (i + h) + 4 * group;
-                    if (row >= height || c >= width) continue;
-                    if (c + 4 <= width) {
-                        store_any(out + (u64)row * r.ldy + c, y[h]);
-                    } else {
-#pragma unroll
-                        for (u32 v = 0; v < 3; ++v)
-                            if (c + v < width) out[(u64)row * r.ldy + c + v] = y[h][v];
+                            for (u32 v = 0; v < 3; ++v)
+                                if (c + v < width) to[c + v] = acc[i + h][j][v];
+                        }
                     }
                 }
             }
         }
-    }
+    };
+    if (height == TQ && width == TP) store(std::true_type{});
+    else store(std::false_type{});
 }
 
 template <class T, u32 TP, u32 TQ, u32 WP, u32 WQ> hipError_t wide_go(Linear4Args r, hipStream_t stream)
@@ -286,7 +292,7 @@ template <class T, u32 TP, u32 TQ, u32 WP, u32 WQ> hipError_t wide_go(Linear4Arg
     using S = Shape<TP, TQ, WP, WQ>;
     constexpr u32 lds = S::kLds + 2 * (TP + TQ) * 16;
     r.col_tiles = (r.n + TP - 1) / TP;
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, TQ) * r.col_tiles);
+    r.tiles = (u32)((max_runs(r.rows, r.blocks, TQ) + 3) / 4 * 4 * r.col_tiles);
     auto kernel = wide_rows4_kernel<T, S, TP, TQ, WP>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
@@ -329,7 +335,7 @@ bool grouped_linear4_fits(const lmk_gs_linear4 &l)
 {
     const Linear4Args r = linear4_args(l, {}, nullptr, false, nullptr, 0);
     const u32 nt = few_fit(r) ? few_columns(r) : large_tiles(r) ? 256 : 128, per = few_fit(r) ? kRows : nt;
-    return max_runs(r.rows, r.blocks, per) * ((r.n + nt - 1) / nt) * (few_fit(r) ? 512 : 2 * nt) < kMostThreads;
+    return (max_runs(r.rows, r.blocks, per) + 3) * ((r.n + nt - 1) / nt) * (few_fit(r) ? 512 : 2 * nt) < kMostThreads;
 }
 
 hipError_t launch_grouped_linear4(const lmk_gs_linear4 &l, const lmk_gs_block4 &x, const float *bias, bool relu, void *y, u64 ldy,

@@ -310,9 +310,12 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
     __builtin_amdgcn_s_waitcnt(0x070);
 }
 
+// one conversion instruction
 __device__ __forceinline__ u32 pack_bf16(float a, float b)
 {
-    return (u32)__builtin_bit_cast(unsigned short, (__bf16)a) | ((u32)__builtin_bit_cast(unsigned short, (__bf16)b) << 16);
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    return __builtin_bit_cast(u32, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
 }  // namespace lmk

@@ -40,6 +40,7 @@ UNITS = {
     "grouped_few.hip": [],
     "grouped_gated.hip": [],
     "grouped_gated_few.hip": [],
+    "grouped_gated_narrow.hip": [],
     "grouped_gated_wide.hip": [],
     "grouped_linear.hip": [],
     "grouped_linear4.hip": [],

@@ -499,7 +499,7 @@ int32_t lmk_gs_grouped_gated(const lmk_gs_linear *layer, const void *x, uint64_t
     if (rc != LMK_GS_OK) return rc;
     if (layer->rows == 0) return LMK_GS_OK;
     if (!good_rows(x, ldx, layer->k, layer->dtype) || !good_rows(y, ldy, layer->n, layer->dtype)) return LMK_GS_ERR_INVALID;
-    if (!grouped_gated_fits(*layer, x, ldx)) return LMK_GS_ERR_UNSUPPORTED;
+    if (!grouped_gated_fits(*layer, x, ldx, ldy)) return LMK_GS_ERR_UNSUPPORTED;
     const hipError_t e = launch_grouped_gated(*layer, x, ldx, bias, act, y, ldy, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LMK_GS_OK : hip_fail(e);
 }
@@ -512,7 +512,7 @@ int32_t lmk_gs_grouped_gated_backward_bytes(const lmk_gs_linear *layer, size_t *
     // all gradients, of packed rows: the pointers are only told from NULL
     float any = 0.0f;
     const lmk_gs_gated_grads all = {&any, layer->k, &any, &any};
-    if (!grouped_gated_backward_fits(*layer, nullptr, layer->k, all)) return LMK_GS_ERR_UNSUPPORTED;
+    if (!grouped_gated_backward_fits(*layer, layer->n, nullptr, layer->k, all)) return LMK_GS_ERR_UNSUPPORTED;
     *bytes = grouped_gated_backward_bytes(*layer);
     return LMK_GS_OK;
 }
@@ -528,7 +528,7 @@ int32_t lmk_gs_grouped_gated_backward(const lmk_gs_linear *layer, const void *dy
         if (!good_rows(dy, lddy, layer->n, layer->dtype) || !good_rows(x, ldx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
         if (out->dx && !good_rows(out->dx, out->lddx, layer->k, layer->dtype)) return LMK_GS_ERR_INVALID;
     }
-    if (!grouped_gated_backward_fits(*layer, x, ldx, *out)) return LMK_GS_ERR_UNSUPPORTED;
+    if (!grouped_gated_backward_fits(*layer, lddy, x, ldx, *out)) return LMK_GS_ERR_UNSUPPORTED;
     if (!workspace || !aligned(workspace, 256)) return LMK_GS_ERR_INVALID;
     if (workspace_bytes < grouped_gated_backward_bytes(*layer)) return LMK_GS_ERR_CAPACITY;
     if (!out->dw && !out->db && (!out->dx || layer->rows == 0)) return LMK_GS_OK;

@@ -88,6 +88,14 @@ u64 gated_few_threads(const GatedArgs &r);
 hipError_t launch_gated_few(const GatedArgs &r, u32 dtype, hipStream_t stream);
 constexpr u32 kGatedFewRows = 16, kGatedTileRows = 64;
 
+// small matrices, float32: y; all gradients in one pass, the sets of partial sums as launch_join numbers them, in runs of `.._backward_rows`
+bool gated_narrow_fits(const GatedArgs &r);
+u64 gated_narrow_threads(const GatedArgs &r);
+hipError_t launch_gated_narrow(const GatedArgs &r, hipStream_t stream);
+bool gated_narrow_backward_fits(const GatedArgs &r, u64 lddx);
+u32 gated_narrow_backward_rows(const GatedArgs &r);
+hipError_t launch_gated_narrow_backward(const GatedArgs &r, float *dx, u64 lddx, float *dw, float *db, float *part, hipStream_t stream);
+
 bool gated_wide_fits(const GatedArgs &r);
 u32 gated_wide_rows(const GatedArgs &r);
 u64 gated_wide_threads(const GatedArgs &r);

@@ -120,17 +120,18 @@ hipError_t all_go(GatedArgs r, hipStream_t stream)
     return hipGetLastError();
 }
 
-enum class GatedKernel { few, wide, all };
+enum class GatedKernel { few, wide, narrow, all };
 GatedKernel gated_choice(const GatedArgs &r, u32 dtype)
 {
-    const bool wide = dtype == LMK_GS_BF16 && gated_wide_fits(r);
-    return gated_few_fit(r, wide) ? GatedKernel::few : wide ? GatedKernel::wide : GatedKernel::all;
+    const bool wide = dtype == LMK_GS_BF16 && gated_wide_fits(r), narrow = dtype == LMK_GS_F32 && !r.dy && gated_narrow_fits(r);
+    return gated_few_fit(r, wide) ? GatedKernel::few : wide ? GatedKernel::wide : narrow ? GatedKernel::narrow : GatedKernel::all;
 }
 u64 gated_threads(const GatedArgs &r, u32 dtype)
 {
     switch (gated_choice(r, dtype)) {
     case GatedKernel::few: return gated_few_threads(r);
     case GatedKernel::wide: return gated_wide_threads(r);
+    case GatedKernel::narrow: return gated_narrow_threads(r);
     default: return max_runs(r.rows, r.blocks, kTile) * ((r.n + kTile - 1) / kTile) * kThreads;
     }
 }
@@ -139,6 +140,7 @@ hipError_t gated_go(const GatedArgs &r, u32 dtype, hipStream_t stream)
     switch (gated_choice(r, dtype)) {
     case GatedKernel::few: return launch_gated_few(r, dtype, stream);
     case GatedKernel::wide: return launch_gated_wide(r, stream);
+    case GatedKernel::narrow: return launch_gated_narrow(r, stream);
     default: return dtype == LMK_GS_F32 ? all_go<float>(r, stream) : all_go<__bf16>(r, stream);
     }
 }
@@ -171,6 +173,8 @@ lmk_gs_linear both(const lmk_gs_linear &l)
     b.n = 2 * l.n;
     return b;
 }
+// all gradients in one kernel; dy of packed rows stands for any that fits
+bool one_pass_fits(const GatedArgs &r, u32 dtype, u64 lddx) { return dtype == LMK_GS_F32 && gated_narrow_backward_fits(r, lddx); }
 u64 round_up(u64 bytes) { return (bytes + 255) / 256 * 256; }
 // elements between rows of both projections' gradients: whole vectors
 u64 grads_stride(const lmk_gs_linear &l) { return ((u64)2 * l.n + 7) / 8 * 8; }
@@ -188,12 +192,21 @@ GatedSpace gated_space(const lmk_gs_linear &l)
     const u32 least = gated_few_fit(r, false) || gated_few_fit(r, true) ? kGatedFewRows : kGatedTileRows;
     s.sums = l.dtype == LMK_GS_F32 ? 0 : round_up(((u64)l.rows / least + l.blocks + 1) * 2 * l.n * 4);
     s.linear = grouped_backward_bytes(both(l));
+    if (one_pass_fits(r, l.dtype, l.k)) {
+        const u64 sets = ((u64)l.rows / gated_narrow_backward_rows(r) + 1 + l.blocks) * ((u64)2 * l.n * l.k + 2 * l.n) * 4;
+        s.linear = sets > s.linear ? sets : s.linear;
+    }
     return s;
 }
 
 }  // namespace
 
-bool grouped_gated_fits(const lmk_gs_linear &l, const void *x, u64 ldx) { return gated_threads(gated_args(l, x, ldx, nullptr, 0), l.dtype) < kMostThreads; }
+bool grouped_gated_fits(const lmk_gs_linear &l, const void *x, u64 ldx, u64 ldy)
+{
+    GatedArgs r = gated_args(l, x, ldx, nullptr, 0);
+    r.ldo = ldy;
+    return gated_threads(r, l.dtype) < kMostThreads;
+}
 
 size_t grouped_gated_backward_bytes(const lmk_gs_linear &l)
 {
@@ -201,13 +214,17 @@ size_t grouped_gated_backward_bytes(const lmk_gs_linear &l)
     return (size_t)(s.grads + s.sums + s.linear);
 }
 
-bool grouped_gated_backward_fits(const lmk_gs_linear &l, const void *x, u64 ldx, const lmk_gs_gated_grads &out)
+bool grouped_gated_backward_fits(const lmk_gs_linear &l, u64 lddy, const void *x, u64 ldx, const lmk_gs_gated_grads &out)
 {
-    if (grads_stride(l) > 1u << 28 || !grouped_gated_fits(l, x, ldx)) return false;
     const bool own_db = l.dtype == LMK_GS_BF16 && out.db;
-    const GatedArgs r = gated_args(l, x, ldx, nullptr, 0);
+    GatedArgs r = gated_args(l, x, ldx, nullptr, 0);
+    r.dy = reinterpret_cast<const void *>(256);             // told from NULL: gradients are asked for
+    r.lddy = lddy;
+    // one run a workgroup there, of which there are some hundred and one a block
+    if (one_pass_fits(r, l.dtype, out.lddx) && join_threads(2 * l.n, l.k, l.blocks, l.rows / gated_narrow_backward_rows(r) + 1) < kMostThreads) return true;
     if (own_db && join_threads(2 * l.n, 0, l.blocks, l.rows / gated_set_rows(r, l.dtype) + 1) >= kMostThreads) return false;
     const lmk_gs_linear_grads grads = {out.dx, out.lddx, static_cast<float *>(out.dw), own_db ? nullptr : out.db};
+    if (gated_threads(r, l.dtype) >= kMostThreads) return false;
     // the gradients' place in the workspace is aligned: any pointer that is stands for it
     return grouped_backward_fits(both(l), reinterpret_cast<const void *>(256), grads_stride(l), x, ldx, nullptr, false, grads);
 }
@@ -228,6 +245,14 @@ hipError_t launch_grouped_gated_backward(const lmk_gs_linear &l, const void *dy,
     GatedArgs r = gated_args(l, x, ldx, bias, act);
     r.dy = dy;
     r.lddy = lddy;
+    char *linear_space = workspace + space.grads + space.sums;
+    if (one_pass_fits(r, l.dtype, out.lddx)) {
+        float *part = reinterpret_cast<float *>(linear_space), *dw = static_cast<float *>(out.dw);
+        const hipError_t e = launch_gated_narrow_backward(r, static_cast<float *>(out.dx), out.lddx, dw, out.db, part, stream);
+        if (e != hipSuccess || !(dw || out.db)) return e;
+        const u32 per = gated_narrow_backward_rows(r);
+        return launch_join(l.offsets, l.blocks, l.rows, per, part, 2 * l.n, l.k, dw, out.db, l.rows / per + 1, stream);
+    }
     r.out = workspace;
     r.ldo = grads_stride(l);
     if (own_db) {
@@ -242,7 +267,7 @@ hipError_t launch_grouped_gated_backward(const lmk_gs_linear &l, const void *dy,
     }
     if (e != hipSuccess || !(out.dx || out.dw || (out.db && !own_db))) return e;
     const lmk_gs_linear_grads grads = {out.dx, out.lddx, static_cast<float *>(out.dw), own_db ? nullptr : out.db};
-    return launch_grouped_backward(both(l), workspace, grads_stride(l), x, ldx, nullptr, false, grads, workspace + space.grads + space.sums, stream,
+    return launch_grouped_backward(both(l), workspace, grads_stride(l), x, ldx, nullptr, false, grads, linear_space, stream,
                                    l.dtype == LMK_GS_BF16);
 }
 

@@ -10,7 +10,7 @@
 // 300 000 rows in 24 blocks: 35 x 96 in 86 us, 32 x 70 with the gate in 57 us.  Bound by the float32 instructions (35 us for the
 // first at their rate), which wait for the LDS reads in front of them: the sums of 96 x 48 leave registers for two
 // wavefronts a SIMD.  About 13 us are a run's own costs: weights into LDS, the four wavefronts' sums joined.
-#include "grouped_narrow.h"
+#include "grouped_narrow_bwd.h"
 
 namespace lmk {
 
@@ -53,31 +53,6 @@ template <u32 N> struct CodePieces {
     }
 };
 
-constexpr u32 kFillers = 64;            // workgroups for dx of rows of no block
-
-// Steps of dx's product, four outputs each, in whole turns of four.  Those behind the last output have zeros on both sides: a
-// weight that is not finite, multiplied by a zero of dy, would be a NaN.
-__host__ __device__ constexpr u32 whole_steps(u32 n) { return (n + 15) / 16 * 4; }
-
-// floats between the outputs of the joined sums in LDS
-constexpr u32 sums_pitch(u32 ck) { return 16 * ck + 4; }
-constexpr u32 sums_floats(u32 cn, u32 ck) { return 16 * cn * sums_pitch(ck) + 16 * cn; }
-
-// LDS of the widest matrices of a shape: weights and the four wavefronts' tiles, then their sums in the same place
-constexpr u32 shape_lds(u32 cn, u32 ck)
-{
-    const u32 before = 4 * cn * ck * kWave + 4 * kTileRows * (pitch_of(16 * cn) + pitch_of(16 * ck)), sums = 4 * sums_floats(cn, ck);
-    return (before > sums ? before : sums) * 4;
-}
-// Workgroups of a compute unit (wavefronts of a SIMD), what the registers of the sums and LDS both leave: three up to twelve tiles
-// of sums, whose wavefronts take at most 168 registers, two up to 24.  LDS is given out in pieces of 1280 bytes; 64 x 48 and 96 x 32
-// have two workgroups for it, 80 x 64 and 96 x 64 one.
-constexpr u32 resident(u32 cn, u32 ck)
-{
-    const u32 registers = cn * ck <= 12 ? 3 : 2, lds = kLdsBytes / ((shape_lds(cn, ck) + kLdsPiece - 1) / kLdsPiece * kLdsPiece);
-    return registers < lds ? registers : lds;
-}
-
 // CN, CK: 16 outputs and 16 inputs each
 template <u32 CN, u32 CK, bool CODES>
 __global__ __launch_bounds__(256, resident(CN, CK)) void narrow_backward_kernel(const BackwardArgs r)
@@ -85,13 +60,7 @@ __global__ __launch_bounds__(256, resident(CN, CK)) void narrow_backward_kernel(
     extern __shared__ __align__(16) float narrow_lds[];
     const u32 wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     if (blockIdx.x >= r.runs) {
-        // rows in front of the first block and behind the last one
-        u32 front = r.offsets[0], back = r.offsets[r.blocks];
-        front = front < r.rows ? front : r.rows;
-        back = back < front ? front : back < r.rows ? back : r.rows;
-        const u32 count = front + (r.rows - back);
-        for (u32 i = blockIdx.x - r.runs; i < count && r.dx; i += kFillers)
-            for (u32 c = threadIdx.x; c < r.k; c += 256) r.dx[(u64)(i < front ? i : back + (i - front)) * r.lddx + c] = 0.0f;
+        fill_outside(r.offsets, r.blocks, r.rows, blockIdx.x - r.runs, r.dx, r.lddx, r.k);
         return;
     }
     const u32 pn = pitch_of(r.n), pk = pitch_of(r.k), kp = (r.k + 31) / 32 * 32, steps = (r.n + 3) / 4;
@@ -123,8 +92,7 @@ __global__ __launch_bounds__(256, resident(CN, CK)) void narrow_backward_kernel(
         if constexpr (CODES) tile_x.request(x + first * kp, scale + first * (kp / 32), r.x ? rows : 0u);
         else tile_x.request(x + first * r.ldx * 4, r.x ? rows : 0u);
     };
-    f32x4 dw[CK][CN] = {};
-    float db[CN] = {};
+    NarrowSums<CN, CK> sums = {};
     auto put = [&]() {
         tile_y.put(ly);
         tile_x.put(lx);
@@ -135,52 +103,10 @@ __global__ __launch_bounds__(256, resident(CN, CK)) void narrow_backward_kernel(
     for (u32 tile = wave; tile < tiles; tile += 4) {
         const u32 base = tile * kTileRows, left = height - base;
         wave_meets();
-        // sums over the tile's rows; columns that are not there hold what lies behind a row, and reach only results that are not kept
-        float fy[2][CN], fx[2][CK];
-        auto operands = [&](u32 s, u32 at) {
-#pragma unroll
-            for (u32 b = 0; b < CN; ++b) fy[at][b] = 16 * b + j < pn ? ly[(4 * s + q) * pn + 16 * b + j] : 0.0f;
-#pragma unroll
-            for (u32 a = 0; a < CK; ++a) fx[at][a] = 16 * a + j < pk ? lx[(4 * s + q) * pk + 16 * a + j] : 0.0f;
-        };
-        operands(0, 0);
-#pragma unroll
-        for (u32 s = 0; s < 4; ++s) {
-            if (s < 3) operands(s + 1, (s + 1) & 1);
-#pragma unroll
-            for (u32 b = 0; b < CN; ++b) db[b] += fy[s & 1][b];
-#pragma unroll
-            for (u32 a = 0; a < CK; ++a)
-#pragma unroll
-                for (u32 b = 0; b < CN; ++b) dw[a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[s & 1][a], fy[s & 1][b], dw[a][b], 0, 0, 0);
-        }
+        sums.add(ly, pn, lx, pk, j, q);
         f32x4 acc[CK] = {};
         if (r.dx) {
-            // two steps' operands are on their way from LDS while two are multiplied; behind the last one zeros.  Behind the last whole
-            // turn: what lies there in LDS, and is not multiplied
-            float v[2][2], w[2][2][CK];
-            auto fetch = [&](u32 s, u32 at) {
-#pragma unroll
-                for (u32 e = 0; e < 2; ++e) {
-                    const float y = ly[j * pn + 4 * (s + e) + q];
-                    v[at][e] = s + e < steps ? y : 0.0f;
-#pragma unroll
-                    for (u32 c = 0; c < CK; ++c) w[at][e][c] = lw[((s + e) * CK + c) * kWave + lane];
-                }
-            };
-            auto multiply = [&](u32 at) {
-#pragma unroll
-                for (u32 e = 0; e < 2; ++e)
-#pragma unroll
-                    for (u32 c = 0; c < CK; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[at][e][c], v[at][e], acc[c], 0, 0, 0);
-            };
-            fetch(0, 0);
-            for (u32 s = 0; s < steps; s += 4) {
-                fetch(s + 2, 1);
-                multiply(0);
-                fetch(s + 4, 0);
-                multiply(1);
-            }
+            narrow_dx(acc, ly, pn, lw, steps, lane, j, q);
             if (r.gate) {
 #pragma unroll
                 for (u32 c = 0; c < CK; ++c) {
@@ -196,48 +122,12 @@ __global__ __launch_bounds__(256, resident(CN, CK)) void narrow_backward_kernel(
         wave_meets();
         put();
         request(tile + 8);
-        if (r.dx && j < left) {
-            float *out = r.dx + (u64)(row0 + base) * r.lddx + j * (u32)r.lddx;
-#pragma unroll
-            for (u32 c = 0; c < CK; ++c) {
-                const u32 col = 16 * c + 4 * q;
-                if (col + 4 <= r.k) {
-                    store4(out + col, acc[c]);
-                } else {
-#pragma unroll
-                    for (u32 e = 0; e < 3; ++e)
-                        if (col + e < r.k) out[col + e] = acc[c][e];
-                }
-            }
-        }
+        if (r.dx && j < left) store_row(r.dx + (u64)(row0 + base) * r.lddx + j * (u32)r.lddx, acc, r.k, q);
     }
-    // ---- the four wavefronts' sums, [output][input] and then db each
-    constexpr u32 ps = sums_pitch(CK), part = sums_floats(CN, CK);
-    __syncthreads();
-    float *ls = narrow_lds + wave * part, *lb = ls + 16 * CN * ps;
-#pragma unroll
-    for (u32 b = 0; b < CN; ++b) {
-        db[b] += __shfl_xor(db[b], 16, kWave);
-        db[b] += __shfl_xor(db[b], 32, kWave);
-#pragma unroll
-        for (u32 a = 0; a < CK; ++a) *reinterpret_cast<f32x4 *>(ls + (16 * b + j) * ps + 16 * a + 4 * q) = dw[a][b];
-        if (q == 0) lb[16 * b + j] = db[b];
-    }
-    __syncthreads();
     const u32 size = r.n * r.k;
-    float *to_w = run.whole ? r.dw + (u64)run.block * size : r.part + (u64)run.partial() * (size + r.n);
-    float *to_b = run.whole ? r.db + (u64)run.block * r.n : r.part + (u64)run.partial() * (size + r.n) + size;
-    const auto joined = [&](u32 at) { return ((narrow_lds[at] + narrow_lds[part + at]) + narrow_lds[2 * part + at]) + narrow_lds[3 * part + at]; };
-    if (r.dw) {
-        const u32 width = r.in_major ? r.n : r.k;
-#pragma unroll 4
-        for (u32 i = threadIdx.x; i < size; i += 256) {
-            const u32 outer = i / width, inner = i - outer * width;
-            to_w[i] = joined(r.in_major ? inner * ps + outer : outer * ps + inner);
-        }
-    }
-    if (r.db)
-        for (u32 i = threadIdx.x; i < r.n; i += 256) to_b[i] = joined(16 * CN * ps + i);
+    float *set = r.part + (u64)run.partial() * (size + r.n);
+    sums.join(narrow_lds, wave, j, q, r.n, r.k, r.in_major != 0, r.dw ? run.whole ? r.dw + (u64)run.block * size : set : nullptr,
+              r.db ? run.whole ? r.db + (u64)run.block * r.n : set + size : nullptr);
 }
 
 template <u32 CN, u32 CK>

@@ -190,8 +190,8 @@ hipError_t launch_grouped_norm(const lmk_gs_norm &n, const void *x, u64 ldx, voi
 hipError_t launch_grouped_norm_backward(const lmk_gs_norm &n, const void *dy, u64 lddy, const void *x, u64 ldx,
                                         const lmk_gs_norm_grads &out, char *workspace, hipStream_t stream);
 // gated layers of blocks
-bool grouped_gated_fits(const lmk_gs_linear &l, const void *x, u64 ldx);
-bool grouped_gated_backward_fits(const lmk_gs_linear &l, const void *x, u64 ldx, const lmk_gs_gated_grads &out);
+bool grouped_gated_fits(const lmk_gs_linear &l, const void *x, u64 ldx, u64 ldy);
+bool grouped_gated_backward_fits(const lmk_gs_linear &l, u64 lddy, const void *x, u64 ldx, const lmk_gs_gated_grads &out);
 size_t grouped_gated_backward_bytes(const lmk_gs_linear &l);
 hipError_t launch_grouped_gated(const lmk_gs_linear &l, const void *x, u64 ldx, const float *bias, u32 act, void *y, u64 ldy, hipStream_t stream);
 hipError_t launch_grouped_gated_backward(const lmk_gs_linear &l, const void *dy, u64 lddy, const void *x, u64 ldx, const float *bias, u32 act,

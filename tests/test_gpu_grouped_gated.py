@@ -87,7 +87,7 @@ class Layer:
             got = got.transpose(1, 2) if q == "dw" and self.in_major else got
             _close(got, want[i], bound[i], "f32" if q == "db" else self.dtype, q)
         self.between(self.dx, self.k)
-        assert (self.ws[-256:] == 255).all()
+        assert (self.ws[-256:] == self.ws[-1]).all() and int(self.ws[-1]) in (1, 255)
 
 
 # sizes of the blocks, inputs, outputs: single values, tiles that are just full or just not, every kernel in both its alignments, the anchor
@@ -150,13 +150,21 @@ def test_large_tiles(sizes, k, n, in_major):
     assert all(torch.equal(a.nan_to_num(), getattr(t, q).nan_to_num()) for a, q in zip(first, ("dx", "dw", "db")))      # the same bits
 
 
-def test_many_rows_of_small_matrices():
-    for act in ("silu", "gelu"):
-        t = Layer([30_011, 0, 64, 20_000], 35, 32, "f32", True, seed=2, act=act)
+# the one kernel that takes all gradients of small matrices, in all its shapes
+@pytest.mark.parametrize("in_major", [False, True])
+@pytest.mark.parametrize("k,n", [(4, 4), (5, 6), (16, 16), (35, 32), (33, 15), (48, 33), (64, 48), (63, 47), (20, 48), (64, 7), (65, 33), (40, 49), (100, 60)])
+def test_many_rows_of_small_matrices(k, n, in_major):
+    for act, pad in (("silu", 0), ("gelu", 3)):
+        t = Layer([5011, 0, 64, 20_000, 1], k, n, "f32", in_major, pad=pad, front=2, behind=3, seed=2, act=act)
         t.forward()
         t.check_forward()
         t.backward()
         t.check_backward()
+        for which in (("dx",), ("dw",), ("db",)):
+            for q in ("dx", "dw", "db"):
+                getattr(t, q).fill_(7.0)
+            t.backward(which)
+            t.check_backward(which)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -146,157 +146,195 @@ template <u32 TP, u32 TQ, u32 WAVES> struct Scales4 {
     }
 };
 
+// A workgroup takes tiles one after the other.  The next one's first loads are on their way before this one's results leave, and the stores,
+// which take as long as several steps, are not waited for until the next tile's second pair has to be there (vector memory operations
+// complete in order: what was asked for before the last kStores stores has arrived once no more than those are left).
 template <class T, class S, u32 TP, u32 TQ, u32 WP>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear4Args r)
 {
     extern __shared__ __align__(16) char wide_lds[];
-    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, S::kResident * kUnits);
-    // four rows of tiles beside each other: what a die works on at once is four by eight of them, and shares most of its operands
-    const u32 band = tile / (4 * r.col_tiles), in = tile - band * 4 * r.col_tiles, row_tile = 4 * band + in % 4, col0 = in / 4 * TP;
-    const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
-    if (!run.found) return;
-    const u32 row0 = run.begin + run.local * TQ;
-    const u32 height = run.end - row0 < TQ ? run.end - row0 : TQ;
-    const u32 width = r.n - col0 < TP ? r.n - col0 : TP;
+    constexpr u32 kScales = (TP + TQ) * 16, kStores = S::kP * S::kQ / (sizeof(T) == 2 ? 2 : 1);
     const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     const u32 p0 = wave % WP * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
-    const bool inside = run.block != ~0u;
-    // the sums begin with the bias
-    f32x4 acc[S::kP][S::kQ];
-#pragma unroll
-    for (u32 i = 0; i < S::kP; ++i) {
-        f32x4 b = {};
-        if (r.bias && inside) {
-            const u32 c = p0 + 16 * i + 4 * (lane >> 4);
-            const float *from = r.bias + (u64)run.block * r.n + col0;
-#pragma unroll
-            for (u32 v = 0; v < 4; ++v) b[v] = from[c + v < width ? c + v : 0u];
+    const u32 row_bytes = code_bytes(r.k), scales = scale_bytes(r.k), steps = row_bytes / 64;
+    lds_char *lds = (lds_char *)wide_lds, *lp = lds, *lq = lds + 2 * S::kPartP, *ls = lds + S::kLds, *lb = ls + 2 * kScales;
+
+    // the tile: block ~0u for rows of no block
+    struct Tile {
+        u32 block, row0, height, col0, width;
+    };
+    // the next one from number `id` on that there is
+    const auto locate = [&](u32 &id, Tile &to) {
+        for (; id < r.tiles; id += gridDim.x) {
+            const u32 tile = tile_of_workgroup(id, r.tiles, S::kResident * kUnits);
+            // four rows of tiles beside each other: what a die works on at once is four by eight of them, and shares most of its operands
+            const u32 band = tile / (4 * r.col_tiles), in = tile - band * 4 * r.col_tiles, row_tile = 4 * band + in % 4;
+            const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
+            if (!run.found) continue;
+            to.block = uniform(run.block);
+            to.row0 = uniform(run.begin + run.local * TQ);
+            to.height = uniform(run.end - to.row0 < TQ ? run.end - to.row0 : TQ);
+            to.col0 = uniform(in / 4 * TP);
+            to.width = uniform(r.n - to.col0 < TP ? r.n - to.col0 : TP);
+            return true;
         }
-#pragma unroll
-        for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = b;
-    }
-    if (inside) {
-        lds_char *lds = (lds_char *)wide_lds, *lp = lds, *lq = lds + 2 * S::kPartP, *ls = lds + S::kLds;
-        constexpr u32 kScales = (TP + TQ) * 16;
-        const u32 row_bytes = code_bytes(r.k), scales = scale_bytes(r.k), steps = row_bytes / 64;
-        const u64 wrow = (u64)run.block * r.n + col0;
-        Along16<TP, S::kWaves> p;
-        Along16<TQ, S::kWaves> q;
-        Scales4<TP, TQ, S::kWaves> sc;
+        return false;
+    };
+    Along16<TP, S::kWaves> p;
+    Along16<TQ, S::kWaves> q;
+    Scales4<TP, TQ, S::kWaves> sc;
+    // `part` of the codes; the scales of steps 4 i and on are in half i % 2 of theirs
+    const auto fill = [&](u32 part, u32 pair) {
+        p.fill(lp + part * S::kPartP, wave);
+        q.fill(lq + part * S::kPartQ, wave);
+        if (pair % 2 == 0) sc.fill(ls + (pair / 2 & 1) * kScales, wave);
+    };
+    const auto begin = [&](const Tile &t) {
+        if (t.block == ~0u) return;
+        const u32 at = afresh(lane);
+        const u64 wrow = (u64)t.block * r.n + t.col0;
         const auto first_of = [](const char *of, u64 bytes) { return reinterpret_cast<const __bf16 *>(uniform64(reinterpret_cast<u64>(of) + bytes)); };
-        p.init(first_of(r.w, wrow * row_bytes), row_bytes / 2, width, row_bytes / 2, wave, lane);
-        q.init(first_of(r.x, (u64)row0 * row_bytes), row_bytes / 2, height, row_bytes / 2, wave, lane);
-        sc.init(r.ws + wrow * scales, width, r.xs + (u64)row0 * scales, height, scales, wave, lane, p0, q0);
-        i32x4 fp[S::kP], fq[2][S::kQ];
-        u32 sp[S::kP], sq[2][S::kQ];
-        // `part` of the codes; the scales of steps 4 i and on are in half i % 2 of theirs
-        auto fill = [&](u32 part, u32 pair) {
-            p.fill(lp + part * S::kPartP, wave);
-            q.fill(lq + part * S::kPartQ, wave);
-            if (pair % 2 == 0) sc.fill(ls + (pair / 2 & 1) * kScales, wave);
-        };
-        // step t of eight, of which two pairs have the codes' parts and four the halves of the scales in turns
-        auto read_p = [&](u32 i, u32 t) {
-            fp[i] = __builtin_bit_cast(i32x4, p.fragment(lp + (t / 2 & 1) * S::kPartP, t & 1, p0, i));
-            sp[i] = sc.of(ls + (t / 4 & 1) * kScales, sc.p_read, i, t & 3);
-        };
-        auto read_q = [&](u32 j, u32 t) {
-            fq[t & 1][j] = __builtin_bit_cast(i32x4, q.fragment(lq + (t / 2 & 1) * S::kPartQ, t & 1, q0, j));
-            sq[t & 1][j] = sc.of(ls + (t / 4 & 1) * kScales, sc.q_read, j, t & 3);
-        };
-        // multiplies step t and reads the fragments of the next: those of P take the place of what has been used
-        auto step = [&](u32 t) {
-#pragma unroll
-            for (u32 j = 0; j < S::kQ; ++j) read_q(j, t + 1);
-#pragma unroll
-            for (u32 i = 0; i < S::kP; ++i) {
-#pragma unroll
-                for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = product4(fp[i], sp[i], fq[t & 1][j], sq[t & 1][j], acc[i][j]);
-                read_p(i, t + 1);
-            }
-            asm volatile("" ::: "memory");              // the reads stay in this step
-        };
+        p.init(first_of(r.w, wrow * row_bytes), row_bytes / 2, t.width, row_bytes / 2, wave, at);
+        q.init(first_of(r.x, (u64)t.row0 * row_bytes), row_bytes / 2, t.height, row_bytes / 2, wave, at);
+        sc.init(r.ws + wrow * scales, t.width, r.xs + (u64)t.row0 * scales, t.height, scales, wave, at, p0, q0);
+        if (wave < TP / kWave) {
+            const u64 bias = r.bias ? reinterpret_cast<u64>(r.bias + wrow) : reinterpret_cast<u64>(r.offsets);
+            const __amdgpu_buffer_rsrc_t from = buffer_of(reinterpret_cast<const void *>(uniform64(bias)), r.bias ? uniform(t.width * 4) : 0u);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lb + wave * kWave * 4, 4, (int)((wave * kWave + at) * 4), 0, 0, 0);
+        }
         fill(0, 0);
         fill(1, 1);
-        wavefronts_meet<0x070>();
+    };
+
+    u32 id = blockIdx.x;
+    Tile tile;
+    if (!locate(id, tile)) return;
+    wavefronts_meet<0x070>();               // nothing but those loads is on its way, here as for every other tile
+    begin(tile);
+    bool counted = false;
+    for (;;) {
+        if (counted) wavefronts_meet<(kStores & 15) | (kStores >> 4) << 14 | 0x070>();
+        else wavefronts_meet<0x070>();
+        // the sums begin with the bias
+        f32x4 acc[S::kP][S::kQ];
+        const lds_char *own_bias = lb + (p0 + 4 * (afresh(lane) >> 4)) * 4;
 #pragma unroll
-        for (u32 i = 0; i < S::kP; ++i) read_p(i, 0);
+        for (u32 i = 0; i < S::kP; ++i) {
+            const f32x4 b = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(own_bias + 64 * i);
 #pragma unroll
-        for (u32 j = 0; j < S::kQ; ++j) read_q(j, 0);
-        for (u32 t0 = 0; t0 < steps; t0 += 8) {
+            for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = tile.block != ~0u ? b : f32x4{};
+        }
+        if (tile.block != ~0u) {
+            i32x4 fp[S::kP], fq[2][S::kQ];
+            u32 sp[S::kP], sq[2][S::kQ];
+            // step t of eight, of which two pairs have the codes' parts and four the halves of the scales in turns
+            auto read_p = [&](u32 i, u32 t) {
+                fp[i] = __builtin_bit_cast(i32x4, p.fragment(lp + (t / 2 & 1) * S::kPartP, t & 1, p0, i));
+                sp[i] = sc.of(ls + (t / 4 & 1) * kScales, sc.p_read, i, t & 3);
+            };
+            auto read_q = [&](u32 j, u32 t) {
+                fq[t & 1][j] = __builtin_bit_cast(i32x4, q.fragment(lq + (t / 2 & 1) * S::kPartQ, t & 1, q0, j));
+                sq[t & 1][j] = sc.of(ls + (t / 4 & 1) * kScales, sc.q_read, j, t & 3);
+            };
+            // multiplies step t and reads the fragments of the next: those of P take the place of what has been used
+            auto step = [&](u32 t) {
 #pragma unroll
-            for (u32 t = 0; t < 8; t += 2) {
-                if (t0 + t >= steps) break;
-                step(t);
-                if (t0 + t + 1 >= steps) break;
-                // the next pair has arrived, and this pair's fragments have left LDS
-                wavefronts_meet<0x070>();
-                fill(t / 2 & 1, t / 2 + 2);
-                step(t + 1);
+                for (u32 j = 0; j < S::kQ; ++j) read_q(j, t + 1);
+#pragma unroll
+                for (u32 i = 0; i < S::kP; ++i) {
+#pragma unroll
+                    for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = product4(fp[i], sp[i], fq[t & 1][j], sq[t & 1][j], acc[i][j]);
+                    read_p(i, t + 1);
+                }
+                asm volatile("" ::: "memory");              // the reads stay in this step
+            };
+#pragma unroll
+            for (u32 i = 0; i < S::kP; ++i) read_p(i, 0);
+#pragma unroll
+            for (u32 j = 0; j < S::kQ; ++j) read_q(j, 0);
+            for (u32 t0 = 0; t0 < steps; t0 += 8) {
+#pragma unroll
+                for (u32 t = 0; t < 8; t += 2) {
+                    if (t0 + t >= steps) break;
+                    step(t);
+                    if (t0 + t + 1 >= steps) break;
+                    // the next pair has arrived, and this pair's fragments have left LDS
+                    wavefronts_meet<0x070>();
+                    fill(t / 2 & 1, t / 2 + 2);
+                    step(t + 1);
+                }
             }
         }
-        // nothing may be on its way into LDS when the workgroup ends
-        __builtin_amdgcn_s_waitcnt(0x070);
-    }
-    if (r.relu) {
+        const Tile done = tile;
+        id += gridDim.x;
+        const bool more = locate(id, tile);
+        // nothing may be on its way into LDS when it is filled for the next tile, or when the workgroup ends
+        wavefronts_meet<0x070>();
+        if (more) begin(tile);
+        asm volatile("" ::: "memory");                      // the stores stay behind those loads
+        if (r.relu) {
 #pragma unroll
-        for (u32 i = 0; i < S::kP; ++i)
+            for (u32 i = 0; i < S::kP; ++i)
 #pragma unroll
-            for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = __builtin_elementwise_maximum(acc[i][j], f32x4{});          // NaN stays
-    }
-    T *out = static_cast<T *>(r.y) + (u64)row0 * r.ldy + col0;
-    // `all`: every result of the tile is there
-    const auto store = [&](auto all) {
-        const u32 group = lane >> 4;
+                for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = __builtin_elementwise_maximum(acc[i][j], f32x4{});          // NaN stays
+        }
+        T *out = static_cast<T *>(r.y) + (u64)done.row0 * r.ldy + done.col0;
+        // `all`: every result of the tile is there
+        const u32 at = afresh(lane), group = at >> 4;               // where its results go is not held through the product
+        const auto store = [&](auto all) {
 #pragma unroll
-        for (u32 j = 0; j < S::kQ; ++j) {
-            const u32 row = q0 + 16 * j + (lane & 15);
-            T *to = out + (u64)row * r.ldy;
+            for (u32 j = 0; j < S::kQ; ++j) {
+                const u32 row = q0 + 16 * j + (at & 15);
+                T *to = out + (u64)row * r.ldy;
 #pragma unroll
-            for (u32 i = 0; i < S::kP; i += 2) {
-                if constexpr (sizeof(T) == 2) {
-                    // two neighbouring results exchange lanes: eight consecutive values a lane
-                    const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i + 1][j][0], acc[i + 1][j][1]), false, false);
-                    const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][2], acc[i][j][3]), pack_bf16(acc[i + 1][j][2], acc[i + 1][j][3]), false, false);
-                    const u32x4 v = {a[0], b[0], a[1], b[1]};
-                    const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1);
-                    if (all || (row < height && c + 8 <= width)) {
-                        store_any(to + c, v);
-                    } else if (row < height) {
+                for (u32 i = 0; i < S::kP; i += 2) {
+                    if constexpr (sizeof(T) == 2) {
+                        // two neighbouring results exchange lanes: eight consecutive values a lane
+                        const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i + 1][j][0], acc[i + 1][j][1]), false, false);
+                        const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][2], acc[i][j][3]), pack_bf16(acc[i + 1][j][2], acc[i + 1][j][3]), false, false);
+                        const u32x4 v = {a[0], b[0], a[1], b[1]};
+                        const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1);
+                        if (all || (row < done.height && c + 8 <= done.width)) {
+                            store_any(to + c, v);
+                        } else if (row < done.height) {
 #pragma unroll
-                        for (u32 e = 0; e < 7; ++e)
-                            if (c + e < width) to[c + e] = __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2))));
-                    }
-                } else {
+                            for (u32 e = 0; e < 7; ++e)
+                                if (c + e < done.width) to[c + e] = __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2))));
+                        }
+                    } else {
 #pragma unroll
-                    for (u32 h = 0; h < 2; ++h) {
-                        const u32 c = p0 + 16 * (i + h) + 4 * group;
-                        if (all || (row < height && c + 4 <= width)) {
-                            store_any(to + c, acc[i + h][j]);
-                        } else if (row < height) {
+                        for (u32 h = 0; h < 2; ++h) {
+                            const u32 c = p0 + 16 * (i + h) + 4 * group;
+                            if (all || (row < done.height && c + 4 <= done.width)) {
+                                store_any(to + c, acc[i + h][j]);
+                            } else if (row < done.height) {
 #pragma unroll
-                            for (u32 v = 0; v < 3; ++v)
-                                if (c + v < width) to[c + v] = acc[i + h][j][v];
+                                for (u32 v = 0; v < 3; ++v)
+                                    if (c + v < done.width) to[c + v] = acc[i + h][j][v];
+                            }
                         }
                     }
                 }
             }
-        }
-    };
-    if (height == TQ && width == TP) store(std::true_type{});
-    else store(std::false_type{});
+        };
+        counted = done.height == TQ && done.width == TP;
+        if (counted) store(std::true_type{});
+        else store(std::false_type{});
+        if (!more) return;
+    }
 }
 
 template <class T, u32 TP, u32 TQ, u32 WP, u32 WQ> hipError_t wide_go(Linear4Args r, hipStream_t stream)
 {
     using S = Shape<TP, TQ, WP, WQ>;
-    constexpr u32 lds = S::kLds + 2 * (TP + TQ) * 16;
+    constexpr u32 lds = S::kLds + 2 * (TP + TQ) * 16 + TP * 4;
     r.col_tiles = (r.n + TP - 1) / TP;
     r.tiles = (u32)((max_runs(r.rows, r.blocks, TQ) + 3) / 4 * 4 * r.col_tiles);
     auto kernel = wide_rows4_kernel<T, S, TP, TQ, WP>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), lds, stream, r);
+    const u32 at_once = 8 * kUnits * S::kResident;
+    hipLaunchKernelGGL(kernel, dim3(r.tiles < at_once ? r.tiles : at_once), dim3(S::kThreads), lds, stream, r);
     return hipGetLastError();
 }
 // as in grouped_wide.hip

@@ -20,7 +20,8 @@ constexpr u32 kNowhere = 0x7ffffff0u;       // a byte offset behind every buffer
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, u32 bytes)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
+    // what the compiler does not see to be the same in all lanes costs a loop around every load
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(uniform64(reinterpret_cast<u64>(p))), 0, (int)uniform(bytes), 0x00020000);
 }
 
 // ---- an operand of `W` rows (columns) by kPair sum indices in LDS, 128 W bytes, filled by loads that go to LDS

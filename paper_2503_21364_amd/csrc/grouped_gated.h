@@ -23,6 +23,7 @@ struct GatedArgs {
     float *part;                // NULL, or sets of partial sums over rows of the gradients, 2 n each
     float *db;                  // where blocks of one set have theirs
     u32 tiles, col_tiles;
+    bool past;                  // `out` is more than the caches of the dies hold
 };
 
 // 1 / (1 + e^-a): the exponent's product is off by |a| 2^-24, which is e^-a's relative error

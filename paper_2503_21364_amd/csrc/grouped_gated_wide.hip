@@ -190,15 +190,22 @@ __device__ __forceinline__ u32x4 eight_of(const float (&lo)[4], const float (&hi
     const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(lo[2], lo[3]), pack_bf16(hi[2], hi[3]), false, false);
     return u32x4{a[0], b[0], a[1], b[1]};
 }
-// at most eight values at p, `count` of them there
-template <bool ANY> __device__ __forceinline__ void store_eight(__bf16 *p, u32x4 v, u32 count)
+// and back
+__device__ __forceinline__ void four_and_four(u32x4 v, u32x2 (&of)[2])
 {
-    if (!ANY || count >= 8) {
-        store_any(p, v);
+    const u32x2 a = __builtin_amdgcn_permlane16_swap(v[0], v[2], false, false), b = __builtin_amdgcn_permlane16_swap(v[1], v[3], false, false);
+    of[0] = u32x2{a[0], b[0]};
+    of[1] = u32x2{a[1], b[1]};
+}
+// at most eight values at p, `count` of them there
+template <bool ALL, bool PAST> __device__ __forceinline__ void store_eight(__bf16 *p, u32x4 v, u32 count)
+{
+    if (ALL || count >= 8) {
+        store_vector<PAST>(p, v);
         return;
     }
 #pragma unroll
-    for (u32 e = 0; e < 8; ++e)
+    for (u32 e = 0; e < 7; ++e)
         if (e < count) p[e] = __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2))));
 }
 // sum over the 16 lanes of a row of lanes
@@ -212,130 +219,214 @@ __device__ __forceinline__ float sixteen_sum(float v)
     return v;
 }
 
+// LDS behind the operands: the tile's bias, and sums over its rows by the wavefronts beside each other
+template <class S, u32 TP, u32 WP> constexpr u32 gated_lds() { return S::kLds + TP * 4 + S::kWaves / WP * TP * 4; }
+
+// A workgroup takes tiles one after the other; as in grouped_linear4.hip the next one's first loads are on their way before this one's results
+// leave, where operands go to LDS directly.
 template <class S, u32 TP, u32 TQ, u32 WP, bool ACROSS, bool ANY, bool BACKWARD>
 __global__ __launch_bounds__(S::kThreads, 2) void gated_wide_kernel(const GatedArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
-    constexpr u32 kOut = TP / 2;
-    const u32 tile = tile_of_workgroup(blockIdx.x, r.tiles, S::kResident * kUnits);
-    const u32 row_tile = tile / r.col_tiles, col0 = (tile - row_tile * r.col_tiles) * kOut;
-    const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
-    if (!run.found) return;
-    const u32 row0 = run.begin + run.local * TQ;
-    const u32 height = run.end - row0 < TQ ? run.end - row0 : TQ;
-    const u32 width = r.n - col0 < kOut ? r.n - col0 : kOut;
+    constexpr u32 kOut = TP / 2, kAcross = S::kWaves / WP, kPairs = S::kP / 4, kStores = kPairs * S::kQ * (BACKWARD ? 2 : 1);
     const u32 lane = threadIdx.x & (kWave - 1), wave = (u32)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWave));
     const u32 p0 = wave % WP * (S::kP * 16), q0 = wave / WP * (S::kQ * 16);
-    const bool inside = run.block != ~0u;
-    lds_char *lds = (lds_char *)wide_lds;
-    f32x4 acc[S::kP][S::kQ] = {};
-    if (inside) {
-        const u32 steps = (r.k + kStep - 1) / kStep;
-        const auto nothing = [](const bf16x8 (&)[S::kQ]) {};
-        const auto unseen = [](u32, const lds_char *) {};
-        typename std::conditional<ANY, AlongAny<TQ, S::kWaves>, Along16<TQ, S::kWaves>>::type q;
-        q.init(static_cast<const __bf16 *>(r.x) + (u64)row0 * r.ldx, r.ldx, height, r.k, wave, lane);
-        const __bf16 *w = static_cast<const __bf16 *>(r.w) + (u64)run.block * r.w_block;
-        if constexpr (ACROSS) {
-            typename std::conditional<ANY, BothAcrossAny<TP, S::kWaves>, BothAcross16<TP, S::kWaves>>::type p;
-            p.init(w + col0, r.n, r.ldw, width, r.k, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing, unseen);
-        } else {
-            typename std::conditional<ANY, BothAlongAny<TP, S::kWaves>, BothAlong16<TP, S::kWaves>>::type p;
-            p.init(w + (u64)col0 * r.ldw, (u64)r.n * r.ldw, r.ldw, width, r.k, wave, lane);
-            wide_product<S>(p, q, steps, lds, wave, p0, q0, acc, nothing, unseen);
+    const u32 steps = (r.k + kStep - 1) / kStep;
+    lds_char *lds = (lds_char *)wide_lds, *lb = lds + S::kLds;
+    float *sums = reinterpret_cast<float *>(wide_lds + S::kLds + TP * 4);          // [wavefront across the rows][projection][output]
+
+    // the tile: block ~0u for rows of no block
+    struct Tile {
+        u32 block, row0, height, begin, end, local, col0, width;
+    };
+    // the next one from number `id` on that there is
+    const auto locate = [&](u32 &id, Tile &to) {
+        for (; id < r.tiles; id += gridDim.x) {
+            const u32 tile = tile_of_workgroup(id, r.tiles, S::kResident * kUnits);
+            // four rows of tiles beside each other: what a die works on at once is four by eight of them, and shares most of its operands
+            const u32 band = tile / (4 * r.col_tiles), in = tile - band * 4 * r.col_tiles, row_tile = 4 * band + in % 4;
+            const RowRun run = find_run(r.offsets, r.blocks, r.rows, TQ, row_tile);
+            if (!run.found) continue;
+            to.block = uniform(run.block);
+            to.begin = uniform(run.begin);
+            to.end = uniform(run.end);
+            to.local = uniform(run.local);
+            to.row0 = uniform(run.begin + run.local * TQ);
+            to.height = uniform(run.end - to.row0 < TQ ? run.end - to.row0 : TQ);
+            to.col0 = uniform(in / 4 * kOut);
+            to.width = uniform(r.n - to.col0 < kOut ? r.n - to.col0 : kOut);
+            return true;
         }
-    }
-    // accumulators 2 m and 2 m + 1: outputs p0 / 2 + 16 m + 4 group and on, of the gate and of the other projection
-    const u32 group = lane >> 4;
-    __bf16 *out = static_cast<__bf16 *>(r.out) + (u64)row0 * r.ldo + col0;
-    const float *bias = r.bias && inside ? r.bias + (u64)run.block * 2 * r.n + col0 : nullptr;
-    float *sums = reinterpret_cast<float *>(wide_lds);          // BACKWARD: [wavefront across the rows][2][outputs]
-    if (BACKWARD && r.part) __syncthreads();                    // the product is out of LDS
-#pragma unroll
-    for (u32 m = 0; m < S::kP / 2; m += 2) {
-        f32x4 b[2][2] = {};                                     // [of m, m + 1][projection]
-        float sum[2][2][4] = {};
-        if (bias) {
-#pragma unroll
-            for (u32 h = 0; h < 2; ++h)
-#pragma unroll
-                for (u32 v = 0; v < 4; ++v) {
-                    const u32 o = p0 / 2 + 16 * (m + h) + 4 * group + v;
-                    b[h][0][v] = o < width ? bias[o] : 0.0f;
-                    b[h][1][v] = o < width ? bias[r.n + o] : 0.0f;
-                }
+        return false;
+    };
+    using Q = typename std::conditional<ANY, AlongAny<TQ, S::kWaves>, Along16<TQ, S::kWaves>>::type;
+    using P = typename std::conditional<ACROSS, typename std::conditional<ANY, BothAcrossAny<TP, S::kWaves>, BothAcross16<TP, S::kWaves>>::type,
+                                        typename std::conditional<ANY, BothAlongAny<TP, S::kWaves>, BothAlong16<TP, S::kWaves>>::type>::type;
+    P p;
+    Q q;
+    const auto begin = [&](const Tile &t) {
+        if (t.block == ~0u) return;
+        const u32 at = afresh(lane);
+        if (wave < TP / kWave) {
+            const u32 h = wave * kWave / kOut, o = wave * kWave % kOut;
+            const u64 from = r.bias ? reinterpret_cast<u64>(r.bias + (u64)t.block * 2 * r.n + h * r.n + t.col0) : reinterpret_cast<u64>(r.offsets);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_of(reinterpret_cast<const void *>(from), r.bias ? t.width * 4 : 0u), lb + wave * kWave * 4, 4,
+                                                     (int)((o + at) * 4), 0, 0, 0);
         }
-        const u32 o = p0 / 2 + 16 * (m + (group & 1)) + 8 * (group >> 1);           // after the exchange
+        q.init(static_cast<const __bf16 *>(r.x) + (u64)t.row0 * r.ldx, r.ldx, t.height, r.k, wave, at);
+        const __bf16 *w = static_cast<const __bf16 *>(r.w) + (u64)t.block * r.w_block;
+        if constexpr (ACROSS) p.init(w + t.col0, r.n, r.ldw, t.width, r.k, wave, at);
+        else p.init(w + (u64)t.col0 * r.ldw, (u64)r.n * r.ldw, r.ldw, t.width, r.k, wave, at);
 #pragma unroll
-        for (u32 j = 0; j < S::kQ; ++j) {
-            const u32 row = q0 + 16 * j + (lane & 15);
-            if constexpr (!BACKWARD) {
-                float y[2][4];
+        for (u32 part = 0; part < 2; ++part) {
+            p.fill(lds + part * S::kPartP, wave);
+            q.fill(lds + 2 * S::kPartP + part * S::kPartQ, wave);
+        }
+    };
+
+    u32 id = blockIdx.x;
+    Tile tile;
+    if (!locate(id, tile)) return;
+    wavefronts_meet<0x070>();               // nothing but those loads is on its way, here as for every other tile
+    begin(tile);
+    bool counted = false;
+    for (;;) {
+        if (counted) wavefronts_meet<(kStores & 15) | (kStores >> 4) << 14 | 0x070>();
+        else wavefronts_meet<0x070>();
+        // the sums begin with the bias; accumulators 2 m and 2 m + 1: outputs p0 / 2 + 16 m + 4 (lane / 16) and on, of the gate and of the other projection
+        f32x4 acc[S::kP][S::kQ];
+        const lds_char *own_bias = lb + (p0 / 2 + 4 * (afresh(lane) >> 4)) * 4;
 #pragma unroll
-                for (u32 h = 0; h < 2; ++h)
+        for (u32 i = 0; i < S::kP; ++i) {
+            const f32x4 b = *reinterpret_cast<const __attribute__((address_space(3))) f32x4 *>(own_bias + (i % 2 * kOut + i / 2 * 16) * 4);
 #pragma unroll
-                    for (u32 v = 0; v < 4; ++v)
-                        y[h][v] = gated(r.act, acc[2 * (m + h)][j][v] + b[h][0][v], acc[2 * (m + h) + 1][j][v] + b[h][1][v]);
-                u32x4 v = eight_of(y[0], y[1]);
-                if (!inside) v = u32x4{0, 0, 0, 0};
-                if (row < height && o < width) store_eight<ANY>(out + (u64)row * r.ldo + o, v, width - o);
-            } else {
-                float da[2][4], du[2][4];
+            for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = tile.block != ~0u ? b : f32x4{};
+        }
+        if (tile.block != ~0u)
+            wide_product<S, true>(p, q, steps, lds, wave, p0, q0, acc, [](const bf16x8 (&)[S::kQ]) {}, [](u32, const lds_char *) {});
+
+        const Tile done = tile;
+        const bool whole = done.height == TQ && done.width == kOut, inside = done.block != ~0u;
+        const u32 at = afresh(lane), group = at >> 4;               // where its results go is not held through the product
+        // outputs and row of a lane after the exchange of eight_of
+        const auto out_of = [&](u32 m) { return p0 / 2 + 16 * (m + (group & 1)) + 8 * (group >> 1); };
+        const auto row_of = [&](u32 j) { return q0 + 16 * j + (at & 15); };
+        // dy, eight values a lane as results leave, kAhead of them on their way: number i is of outputs 2 (i / kQ) and rows i % kQ
+        constexpr u32 kAhead = 3;
+        u32x4 up[kAhead];
+        const __bf16 *dy_tile = static_cast<const __bf16 *>(r.dy) + (u64)done.row0 * r.lddy + done.col0;
+        const auto fetch = [&](u32 i) {
+            if (!BACKWARD || i >= kPairs * S::kQ) return;
+            const u32 o = out_of(2 * (i / S::kQ)), row = row_of(i % S::kQ);
+            u32x4 v = {0, 0, 0, 0};
+            if (inside && row < done.height) {
+                const __bf16 *from = dy_tile + (u64)row * r.lddy + o;
+                if (o + 8 <= done.width) {
+                    v = load_any<u32x4>(from);
+                } else if (ANY) {
 #pragma unroll
-                for (u32 h = 0; h < 2; ++h) {
-                    const u32 at = p0 / 2 + 16 * (m + h) + 4 * group;
-                    const bool on = inside && row < height && at < width;
-                    f32x4 dy = {0.0f, 0.0f, 0.0f, 0.0f};
-                    const __bf16 *from = static_cast<const __bf16 *>(r.dy) + (u64)(row0 + row) * r.lddy + col0 + at;
-                    if (on && (!ANY || at + 4 <= width)) {
-                        dy = load4(from);
-                    } else if (ANY && on) {
+                    for (u32 e = 0; e < 7; ++e)
+                        if (o + e < done.width) v[e / 2] |= (u32)__builtin_bit_cast(unsigned short, from[e]) << (16 * (e % 2));
+                }
+            }
+            up[i % kAhead] = v;
+        };
 #pragma unroll
-                        for (u32 v = 0; v < 3; ++v)
-                            if (at + v < width) dy[v] = (float)from[v];
-                    }
+        for (u32 i = 0; i < kAhead; ++i) fetch(i);
+        id += gridDim.x;
+        const bool more = locate(id, tile);
+        // nothing may be on its way into LDS when it is filled for the next tile, or when the workgroup ends
+        wavefronts_meet<0x070>();
+        if (!ANY && more) begin(tile);
+        asm volatile("" ::: "memory");                              // the stores stay behind those loads
+        __bf16 *out = static_cast<__bf16 *>(r.out) + (u64)done.row0 * r.ldo + done.col0;
+        const auto finish = [&](auto act, auto all) {
+            constexpr bool kEight = !ANY || all, kPast = !BACKWARD && all;
 #pragma unroll
-                    for (u32 v = 0; v < 4; ++v) {
-                        gated_gradient(r.act, acc[2 * (m + h)][j][v] + b[h][0][v], acc[2 * (m + h) + 1][j][v] + b[h][1][v], dy[v], da[h][v], du[h][v]);
-                        const bool there = on && (!ANY || at + v < width);
-                        da[h][v] = there ? da[h][v] : 0.0f;
-                        du[h][v] = there ? du[h][v] : 0.0f;
-                        sum[h][0][v] += da[h][v];
-                        sum[h][1][v] += du[h][v];
+            for (u32 m = 0; m < 2 * kPairs; m += 2) {
+                float sum[2][2][4] = {};                            // [of m, m + 1][projection]
+                const u32 o = out_of(m);
+#pragma unroll
+                for (u32 j = 0; j < S::kQ; ++j) {
+                    const u32 row = row_of(j);
+                    __bf16 *to = out + (u64)row * r.ldo + o;
+                    const bool there = all || (row < done.height && o < done.width);
+                    if constexpr (!BACKWARD) {
+                        float y[2][4];
+#pragma unroll
+                        for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                            for (u32 v = 0; v < 4; ++v) y[h][v] = gated(act, acc[2 * (m + h)][j][v], acc[2 * (m + h) + 1][j][v]);
+                        const u32x4 v = eight_of(y[0], y[1]);
+                        if (there) store_eight<kEight, kPast>(to, v, done.width - o);
+                    } else {
+                        float da[2][4], du[2][4];
+                        u32x2 dy[2];
+                        four_and_four(up[(m / 2 * S::kQ + j) % kAhead], dy);
+                        fetch(m / 2 * S::kQ + j + kAhead);
+#pragma unroll
+                        for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                            for (u32 v = 0; v < 4; ++v) {
+                                const float g = __uint_as_float(v % 2 ? dy[h][v / 2] & 0xffff0000u : dy[h][v / 2] << 16);
+                                gated_gradient(act, acc[2 * (m + h)][j][v], acc[2 * (m + h) + 1][j][v], g, da[h][v], du[h][v]);
+                                // what is not there has a dy of 0, but may be multiplied by what is not finite
+                                const bool on = all || (row < done.height && p0 / 2 + 16 * (m + h) + 4 * group + v < done.width);
+                                da[h][v] = on ? da[h][v] : 0.0f;
+                                du[h][v] = on ? du[h][v] : 0.0f;
+                                sum[h][0][v] += da[h][v];
+                                sum[h][1][v] += du[h][v];
+                            }
+                        const u32x4 va = eight_of(da[0], da[1]), vu = eight_of(du[0], du[1]);
+                        if (there) {
+                            store_eight<kEight, kPast>(to, va, done.width - o);
+                            store_eight<kEight, kPast>(to + r.n, vu, done.width - o);
+                        }
                     }
                 }
-                const u32x4 va = eight_of(da[0], da[1]), vu = eight_of(du[0], du[1]);
-                if (row < height && o < width) {
-                    store_eight<ANY>(out + (u64)row * r.ldo + o, va, width - o);
-                    store_eight<ANY>(out + (u64)row * r.ldo + r.n + o, vu, width - o);
+                if (BACKWARD && r.part) {
+#pragma unroll
+                    for (u32 h = 0; h < 2; ++h)
+#pragma unroll
+                        for (u32 s = 0; s < 2; ++s)
+#pragma unroll
+                            for (u32 v = 0; v < 4; ++v) {
+                                const float over_rows = sixteen_sum(sum[h][s][v]);
+                                if ((at & 15) == 0) sums[(wave / WP * 2 + s) * kOut + p0 / 2 + 16 * (m + h) + 4 * group + v] = over_rows;
+                            }
+                }
+            }
+        };
+        // Tiles of which everything is there, and the others.  The gradients are read again at once, and not stored past the caches.
+        counted = !ANY && whole && inside && (BACKWARD || r.past);
+        const auto finish_act = [&](auto act) {
+            if (whole && (BACKWARD || r.past)) finish(act, std::true_type{});
+            else finish(act, std::false_type{});
+        };
+        // rows of no block get zeros: the activation of 0 is 0, and so is what a dy of 0 is multiplied by
+        if (inside && r.act == LMK_GS_SILU) finish_act(std::integral_constant<u32, LMK_GS_SILU>{});
+        else if (inside && r.act == LMK_GS_GELU) finish_act(std::integral_constant<u32, LMK_GS_GELU>{});
+        else finish_act(std::integral_constant<u32, LMK_GS_RELU>{});
+        if (BACKWARD && r.part) {
+            wavefronts_meet<0xC07F>();                              // LDS alone is waited for
+            if (inside) {
+                RowRun run;
+                run.block = done.block;
+                run.begin = done.begin;
+                run.end = done.end;
+                run.local = done.local;
+                for (u32 i = threadIdx.x; i < 2 * kOut; i += S::kThreads) {
+                    const u32 s = i / kOut, o = i % kOut;
+                    if (o >= done.width) continue;
+                    float over_rows = 0.0f;
+#pragma unroll
+                    for (u32 w = 0; w < kAcross; ++w) over_rows += sums[(w * 2 + s) * kOut + o];
+                    set_of(r, run, TQ)[s * r.n + done.col0 + o] = over_rows;
                 }
             }
         }
-        if (BACKWARD && r.part) {
-#pragma unroll
-            for (u32 h = 0; h < 2; ++h)
-#pragma unroll
-                for (u32 s = 0; s < 2; ++s)
-#pragma unroll
-                    for (u32 v = 0; v < 4; ++v) {
-                        const float all = sixteen_sum(sum[h][s][v]);
-                        if ((lane & 15) == 0) sums[(wave / WP * 2 + s) * kOut + p0 / 2 + 16 * (m + h) + 4 * group + v] = all;
-                    }
-        }
-    }
-    if (BACKWARD && r.part) {
-        __syncthreads();
-        if (!inside) return;
-        constexpr u32 kAcross = S::kWaves / WP;
-        for (u32 i = threadIdx.x; i < 2 * kOut; i += S::kThreads) {
-            const u32 s = i / kOut, o = i % kOut;
-            if (o >= width) continue;
-            float all = 0.0f;
-#pragma unroll
-            for (u32 q = 0; q < kAcross; ++q) all += sums[(q * 2 + s) * kOut + o];
-            set_of(r, run, TQ)[s * r.n + col0 + o] = all;
-        }
+        if (!more) return;
+        if (ANY) begin(tile);
     }
 }
 
@@ -357,12 +448,14 @@ template <u32 TP, u32 TQ, u32 WP, u32 WQ, bool ACROSS, bool ANY, bool BACKWARD>
 hipError_t wide_go(GatedArgs r, hipStream_t stream)
 {
     using S = Shape<TP, TQ, WP, WQ>;
+    constexpr u32 lds = gated_lds<S, TP, WP>(), at_once = 8 * kUnits * S::kResident;
+    r.past = past_caches((u64)r.rows * r.n * (BACKWARD ? 4 : 2));
     r.col_tiles = (r.n + TP / 2 - 1) / (TP / 2);
-    r.tiles = (u32)(max_runs(r.rows, r.blocks, TQ) * r.col_tiles);
+    r.tiles = (u32)((max_runs(r.rows, r.blocks, TQ) + 3) / 4 * 4 * r.col_tiles);
     auto kernel = gated_wide_kernel<S, TP, TQ, WP, ACROSS, ANY, BACKWARD>;
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), S::kLds, stream, r);
+    hipLaunchKernelGGL(kernel, dim3(r.tiles < at_once ? r.tiles : at_once), dim3(S::kThreads), lds, stream, r);
     return hipGetLastError();
 }
 template <bool ACROSS, bool BACKWARD>
@@ -387,7 +480,7 @@ u32 gated_wide_rows(const GatedArgs &r) { return large_tiles(r) ? 256 : 128; }
 u64 gated_wide_threads(const GatedArgs &r)
 {
     const u32 side = gated_wide_rows(r);
-    return max_runs(r.rows, r.blocks, side) * ((r.n + side / 2 - 1) / (side / 2)) * (side * 2);
+    return (max_runs(r.rows, r.blocks, side) + 3) * ((r.n + side / 2 - 1) / (side / 2)) * (side * 2);
 }
 
 hipError_t launch_gated_wide(const GatedArgs &r, hipStream_t stream)

@@ -23,6 +23,7 @@ struct Linear4Args {
     void *y;
     u64 ldy;
     u32 tiles, col_tiles;
+    bool past;                  // y is more than the caches of the dies hold
 };
 
 // acc += w x: rows of w along the accumulator's registers (four a lane), rows of x along its lanes.  Format 4: e2m1
@@ -279,47 +280,63 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear
                 for (u32 j = 0; j < S::kQ; ++j) acc[i][j] = __builtin_elementwise_maximum(acc[i][j], f32x4{});          // NaN stays
         }
         T *out = static_cast<T *>(r.y) + (u64)done.row0 * r.ldy + done.col0;
-        // `all`: every result of the tile is there
+        // `all`: every result of the tile is there; `past`: past the caches
         const u32 at = afresh(lane), group = at >> 4;               // where its results go is not held through the product
-        const auto store = [&](auto all) {
+        const auto store = [&](auto all, auto past) {
 #pragma unroll
             for (u32 j = 0; j < S::kQ; ++j) {
-                const u32 row = q0 + 16 * j + (at & 15);
-                T *to = out + (u64)row * r.ldy;
-#pragma unroll
-                for (u32 i = 0; i < S::kP; i += 2) {
-                    if constexpr (sizeof(T) == 2) {
-                        // two neighbouring results exchange lanes: eight consecutive values a lane
+                if constexpr (sizeof(T) == 2) {
+                    // Two neighbouring results exchange lanes: eight consecutive values a lane, 64 bytes a row; then two of those, lanes eight
+                    // rows apart: whole lines, of rows row % 8 and of the next eight.
+                    const auto eight = [&](u32 i) {
                         const u32x2 a = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i + 1][j][0], acc[i + 1][j][1]), false, false);
                         const u32x2 b = __builtin_amdgcn_permlane16_swap(pack_bf16(acc[i][j][2], acc[i][j][3]), pack_bf16(acc[i + 1][j][2], acc[i + 1][j][3]), false, false);
-                        const u32x4 v = {a[0], b[0], a[1], b[1]};
-                        const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1);
-                        if (all || (row < done.height && c + 8 <= done.width)) {
-                            store_any(to + c, v);
-                        } else if (row < done.height) {
+                        return u32x4{a[0], b[0], a[1], b[1]};
+                    };
 #pragma unroll
-                            for (u32 e = 0; e < 7; ++e)
-                                if (c + e < done.width) to[c + e] = __builtin_bit_cast(__bf16, (unsigned short)(v[e / 2] >> (16 * (e % 2))));
+                    for (u32 i = 0; i < S::kP; i += 4) {
+                        const u32x4 lo = eight(i), hi = eight(i + 2);
+                        u32x4 v[2];
+#pragma unroll
+                        for (u32 e = 0; e < 4; ++e) {
+                            v[0][e] = (u32)__builtin_amdgcn_update_dpp((int)lo[e], (int)hi[e], 0x128, 0xf, 0xc, false);         // row_ror:8
+                            v[1][e] = (u32)__builtin_amdgcn_update_dpp((int)hi[e], (int)lo[e], 0x128, 0xf, 0x3, false);
                         }
-                    } else {
+                        const u32 c = p0 + 16 * (i + (group & 1)) + 8 * (group >> 1) + (at & 8) * 4;
 #pragma unroll
                         for (u32 h = 0; h < 2; ++h) {
-                            const u32 c = p0 + 16 * (i + h) + 4 * group;
-                            if (all || (row < done.height && c + 4 <= done.width)) {
-                                store_any(to + c, acc[i + h][j]);
+                            const u32 row = q0 + 16 * j + (at & 7) + 8 * h;
+                            T *to = out + (u64)row * r.ldy;
+                            if (all || (row < done.height && c + 8 <= done.width)) {
+                                store_vector<past>(to + c, v[h]);
                             } else if (row < done.height) {
 #pragma unroll
-                                for (u32 v = 0; v < 3; ++v)
-                                    if (c + v < done.width) to[c + v] = acc[i + h][j][v];
+                                for (u32 e = 0; e < 7; ++e)
+                                    if (c + e < done.width) to[c + e] = __builtin_bit_cast(__bf16, (unsigned short)(v[h][e / 2] >> (16 * (e % 2))));
                             }
+                        }
+                    }
+                } else {
+                    const u32 row = q0 + 16 * j + (at & 15);
+                    T *to = out + (u64)row * r.ldy;
+#pragma unroll
+                    for (u32 i = 0; i < S::kP; ++i) {
+                        const u32 c = p0 + 16 * i + 4 * group;
+                        if (all || (row < done.height && c + 4 <= done.width)) {
+                            store_vector<past>(to + c, acc[i][j]);
+                        } else if (row < done.height) {
+#pragma unroll
+                            for (u32 v = 0; v < 3; ++v)
+                                if (c + v < done.width) to[c + v] = acc[i][j][v];
                         }
                     }
                 }
             }
         };
         counted = done.height == TQ && done.width == TP;
-        if (counted) store(std::true_type{});
-        else store(std::false_type{});
+        if (counted && r.past) store(std::true_type{}, std::true_type{});
+        else if (counted) store(std::true_type{}, std::false_type{});
+        else store(std::false_type{}, std::false_type{});
         if (!more) return;
     }
 }
@@ -328,6 +345,7 @@ template <class T, u32 TP, u32 TQ, u32 WP, u32 WQ> hipError_t wide_go(Linear4Arg
 {
     using S = Shape<TP, TQ, WP, WQ>;
     constexpr u32 lds = S::kLds + 2 * (TP + TQ) * 16 + TP * 4;
+    r.past = past_caches((u64)r.rows * r.n * sizeof(T));
     r.col_tiles = (r.n + TP - 1) / TP;
     r.tiles = (u32)((max_runs(r.rows, r.blocks, TQ) + 3) / 4 * 4 * r.col_tiles);
     auto kernel = wide_rows4_kernel<T, S, TP, TQ, WP>;

@@ -259,8 +259,8 @@ template <u32 WAIT> __device__ __forceinline__ void wavefronts_meet()
 // acc[i][j] += P Q over `steps`.  LDS holds two pairs of steps.  A step's fragments are read from LDS while the step in front of
 // it is multiplied; once the second step's are with all wavefronts, the pair's part is filled again, which has the
 // time of two steps to arrive.  One meeting of the wavefronts a pair.
-// `also` sees the fragments of Q, `look` a pair of steps of Q in LDS.
-template <class S, class P, class Q, class Also, class Look>
+// `also` sees the fragments of Q, `look` a pair of steps of Q in LDS.  STARTED: the first two pairs have been asked for, and the first is there.
+template <class S, bool STARTED = false, class P, class Q, class Also, class Look>
 __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *lds, u32 wave, u32 p0, u32 q0,
                                              f32x4 (&acc)[S::kP][S::kQ], Also &&also, Look &&look)
 {
@@ -286,9 +286,11 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
         also(fq[h]);
         asm volatile("" ::: "memory");              // the reads stay in this step
     };
-    fill(0);
-    fill(1);
-    wavefronts_meet<kDirect ? 0xF70 | 8 : 0x070>();                 // the second pair's eight loads may be on their way
+    if constexpr (!STARTED) {
+        fill(0);
+        fill(1);
+        wavefronts_meet<kDirect ? 0xF70 | 8 : 0x070>();             // the second pair's eight loads may be on their way
+    }
 #pragma unroll
     for (u32 i = 0; i < S::kP; ++i) fp[i] = p.fragment(lp, 0, p0, i);
 #pragma unroll
@@ -317,6 +319,19 @@ __device__ __forceinline__ u32 pack_bf16(float a, float b)
     typedef __attribute__((ext_vector_type(2))) float f32x2;
     typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
     return __builtin_bit_cast(u32, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+// Results of a launch that are more than the dies' caches hold together are stored past them: the operands stay there (y of 65 536 x 2048 from
+// operands in 4 bits: 215 us, so 198).  16 bytes at any address.
+inline bool past_caches(u64 bytes) { return bytes > 32u << 20; }
+template <bool PAST, class T, class V> __device__ __forceinline__ void store_vector(T *p, V v)
+{
+    if constexpr (PAST) {
+        typedef V any __attribute__((aligned(2)));
+        __builtin_nontemporal_store(v, reinterpret_cast<any *>(p));
+    } else {
+        store_any(p, v);
+    }
 }
 
 }  // namespace lmk

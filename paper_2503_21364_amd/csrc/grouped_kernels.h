@@ -91,6 +91,8 @@ template <class T, u32 V, bool WHOLE> __device__ __forceinline__ Run<T, V> load_
     Run<T, V> v = {};
     if constexpr (WHOLE) {
         if (s < sums) v = load_any<Run<T, V>>(p + s);
+    } else if (s + V <= sums) {
+        v = load_any<Run<T, V>>(p + s);
     } else {
 #pragma unroll
         for (u32 e = 0; e < V; ++e)

@@ -299,10 +299,10 @@ static RunPlan run_plan(const lmk_gs_linear &l)
 
 // How the partial sums are joined
 struct JoinShape {
-    bool many, parts;
+    bool many, parts, thin;
     u32 pieces;             // workgroups of a block
 };
-static JoinShape join_shape(u32 n, u32 k, u32 blocks, u32 slices)
+static JoinShape join_shape(u32 n, u32 k, u32 blocks, u32 slices, bool thin = false)
 {
     // few sums are many sets each, and latency; many are bytes (24 blocks of 96 x 35, 300 000 rows, gradients with
     // few as many and as few: 94 / 93 us; one block: 128 / 97; 4 blocks of 1024 x 1024, 1000 rows: 33 / 38)
@@ -311,27 +311,35 @@ static JoinShape join_shape(u32 n, u32 k, u32 blocks, u32 slices)
     j.many = stride * blocks >= 1u << 20;
     // few sets a block are not worth parts (7 blocks of 131 x 257, 71 sets: 7.5 us with them, 4.0 without)
     j.parts = !j.many && slices / blocks >= 16;
-    const u32 width = j.many ? 1024 : j.parts ? 32 : 256;
+    j.thin = thin && !j.many && slices / blocks >= 64;
+    const u32 width = j.many ? 1024 : j.thin ? 8 : j.parts ? 32 : 256;
     j.pieces = (u32)((stride + width - 1) / width);
     return j;
 }
 
+// `thin`: few sums, and hundreds of sets of them, are taken by 32 parts (11 491 rows of 426 in one block, 958 sets: 19.6 us in eight parts)
 template <class D>
 static hipError_t join_go(const u32 *offsets, u32 blocks, u32 rows, u32 per, bool by_blocks, const float *part, u32 n, u32 k, D *dw, float *db,
-                          u32 slices, hipStream_t stream)
+                          u32 slices, hipStream_t stream, bool thin = false)
 {
-    const JoinShape j = join_shape(n, k, blocks, slices);
+    const JoinShape j = join_shape(n, k, blocks, slices, thin);
+    if (j.thin) {
+        hipLaunchKernelGGL((join_kernel<D, 1, 8, 32>), dim3(j.pieces * blocks), dim3(kThreads), 0, stream, offsets, blocks, rows, per, by_blocks, part, n, k,
+                           dw, db, j.pieces);
+        return hipGetLastError();
+    }
     auto kernel = j.many ? join_kernel<D, 4, 4, 1> : j.parts ? join_kernel<D, 1, 4, 8> : join_kernel<D, 1, 8, 1>;
     hipLaunchKernelGGL(kernel, dim3(j.pieces * blocks), dim3(kThreads), 0, stream, offsets, blocks, rows, per, by_blocks, part, n, k, dw, db, j.pieces);
     return hipGetLastError();
 }
 
-u64 join_threads(u32 n, u32 k, u32 blocks, u32 slices) { return (u64)join_shape(n, k, blocks, slices).pieces * blocks * kThreads; }
+static u64 join_threads(const JoinShape &j, u32 blocks) { return (u64)j.pieces * blocks * kThreads; }
+u64 join_threads(u32 n, u32 k, u32 blocks, u32 slices) { return join_threads(join_shape(n, k, blocks, slices, true), blocks); }
 
 hipError_t launch_join(const u32 *offsets, u32 blocks, u32 rows, u32 per, const float *part, u32 n, u32 k, float *dw, float *db, u32 slices,
                        hipStream_t stream)
 {
-    return join_go(offsets, blocks, rows, per, true, part, n, k, dw, db, slices, stream);
+    return join_go(offsets, blocks, rows, per, true, part, n, k, dw, db, slices, stream, true);
 }
 
 // ---- what the calls hand to the kernels
@@ -411,7 +419,7 @@ bool grouped_backward_fits(const lmk_gs_linear &l, const void *dy, u64 lddy, con
 {
     const bool sums = out.dw || out.db;
     const RunPlan plan = sums ? run_plan(l) : RunPlan{};
-    if (sums && join_threads(l.n, l.k, l.blocks, plan.slices) >= kMostThreads) return false;
+    if (sums && join_threads(join_shape(l.n, l.k, l.blocks, plan.slices), l.blocks) >= kMostThreads) return false;
     // one pass takes a workgroup a run, of which there are at most some 1000 and one a block
     if (sums && one_pass(l) && narrow_backward_fits(one_pass_args(l, plan, dy, lddy, x, ldx, kept, gate, out, nullptr), kept != nullptr)) return true;
     if (out.dx && rows_threads(dx_args(l, dy, lddy, x, ldx, kept, gate, out), l.dtype, l.in_major == 0) >= kMostThreads) return false;

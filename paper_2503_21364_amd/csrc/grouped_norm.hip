@@ -85,38 +85,79 @@ template <u32 G, u32 N> struct RowSums {
     }
 };
 
-// Chunk c of this lane: columns (c G + lane) V and on
+// Four values (eight of bfloat16) moved down by d places, zeros behind them; eight and more: zeros
+__device__ __forceinline__ f32x4 moved(f32x4 v, u32 d)
+{
+    if (d == 0) return v;
+    return f32x4{d == 1 ? v[1] : d == 2 ? v[2] : d == 3 ? v[3] : 0.0f, d == 1 ? v[2] : d == 2 ? v[3] : 0.0f, d == 1 ? v[3] : 0.0f, 0.0f};
+}
+__device__ __forceinline__ bf16x8 moved(bf16x8 v, u32 d)
+{
+    typedef __attribute__((ext_vector_type(2))) u64 u64x2;
+    const u64x2 b = __builtin_bit_cast(u64x2, v);
+    u64 lo = b[0], hi = b[1];
+    if (d >= 8) {
+        lo = hi = 0;
+    } else if (d >= 4) {
+        lo = hi >> (16 * (d - 4));
+        hi = 0;
+    } else if (d > 0) {
+        lo = lo >> (16 * d) | hi << (64 - 16 * d);
+        hi >>= 16 * d;
+    }
+    return __builtin_bit_cast(bf16x8, u64x2{lo, hi});
+}
+
+// Chunk c of this lane: columns (c G + lane) V and on.  No load has a condition of its own, which would be waited for one after the other: what
+// would reach beyond the row is read as its last whole vector, and moved into place when it is used.
 template <class T, u32 G, u32 C> struct RowOf {
     static constexpr u32 V = kVec<T>;
-    // `whole`: the row is whole vectors
-    __device__ __forceinline__ static void load(Vec<T> (&v)[C], const T *p, u32 k, u32 lane, bool whole)
+    __device__ __forceinline__ static u32 column(u32 c, u32 lane) { return (c * G + lane) * V; }
+    // k >= V; rows of fewer are read value by value
+    __device__ __forceinline__ static void load(Vec<T> (&v)[C], const T *p, u32 k, u32 lane)
     {
 #pragma unroll
         for (u32 c = 0; c < C; ++c) {
-            const u32 at = (c * G + lane) * V;
-            if (whole) {
-                if (at < k) v[c] = load_any<Vec<T>>(p + at);
-                else v[c] = Vec<T>{};
+            const u32 at = column(c, lane);
+            if (k >= V) {
+                v[c] = load_any<Vec<T>>(p + (at + V <= k ? at : k - V));
             } else {
 #pragma unroll
                 for (u32 e = 0; e < V; ++e) v[c][e] = at + e < k ? p[at + e] : (T)0.0f;
             }
         }
     }
-    __device__ __forceinline__ static void store(T *p, const float (&v)[C][V], u32 k, u32 lane, bool whole)
+    // the values; zeros beyond the row
+    __device__ __forceinline__ static void use(float (&f)[C][V], const Vec<T> (&v)[C], u32 k, u32 lane)
     {
 #pragma unroll
         for (u32 c = 0; c < C; ++c) {
-            const u32 at = (c * G + lane) * V;
-            if (whole) {
-                Vec<T> o;
+            const u32 at = column(c, lane);
+            Vec<T> w = v[c];
+            if (k % V == 0) {
 #pragma unroll
-                for (u32 e = 0; e < V; ++e) o[e] = (T)v[c][e];
-                if (at < k) store_any(p + at, o);
+                for (u32 e = 0; e < V; ++e) f[c][e] = at < k ? to_f32(w[e]) : 0.0f;
+                continue;
+            }
+            if (k > V) w = moved(w, at + V <= k ? 0u : at - (k - V));
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) f[c][e] = to_f32(w[e]);
+        }
+    }
+    __device__ __forceinline__ static void store(T *p, const float (&v)[C][V], u32 k, u32 lane)
+    {
+#pragma unroll
+        for (u32 c = 0; c < C; ++c) {
+            const u32 at = column(c, lane);
+            Vec<T> o;
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) o[e] = (T)v[c][e];
+            if (at + V <= k) {
+                store_any(p + at, o);
             } else {
 #pragma unroll
                 for (u32 e = 0; e < V; ++e)
-                    if (at + e < k) p[at + e] = (T)v[c][e];
+                    if (at + e < k) p[at + e] = o[e];
             }
         }
     }
@@ -125,9 +166,17 @@ template <class T, u32 G, u32 C> struct RowOf {
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) {
-                const u32 at = (c * G + lane) * V + e;
-                v[c][e] = at >= k ? 0.0f : p ? p[at] : none;
+            for (u32 q = 0; q < V; q += 4) {
+                const u32 at = column(c, lane) + q;
+                f32x4 w = {none, none, none, none};
+                if (p && k >= 4) {
+                    w = moved(load_any<f32x4>(p + (at + 4 <= k ? at : k - 4)), at + 4 <= k ? 0u : at - (k - 4));
+                } else if (p) {
+#pragma unroll
+                    for (u32 e = 0; e < 4; ++e) w[e] = at + e < k ? p[at + e] : 0.0f;
+                }
+#pragma unroll
+                for (u32 e = 0; e < 4; ++e) v[c][q + e] = w[e];
             }
     }
 };
@@ -144,11 +193,11 @@ __global__ __launch_bounds__(threads_of(G)) void norm_kernel(const NormArgs r)
     if (!run.found) return;
     const u32 lane = threadIdx.x % G, begin = run.begin + run.local * r.per;
     const u32 end = run.end - begin < r.per ? run.end : begin + r.per;
-    const bool whole = r.k % V == 0, inside = run.block != ~0u;
+    const bool inside = run.block != ~0u;
     T *out = static_cast<T *>(r.out);
     if (!inside) {
         const float none[C][V] = {};
-        for (u32 row = begin + threadIdx.x / G; row < end; row += kAtOnce) Row::store(out + (u64)row * r.ldo, none, r.k, lane, whole);
+        for (u32 row = begin + threadIdx.x / G; row < end; row += kAtOnce) Row::store(out + (u64)row * r.ldo, none, r.k, lane);
         return;
     }
     const T *x = static_cast<const T *>(r.x);
@@ -165,18 +214,16 @@ __global__ __launch_bounds__(threads_of(G)) void norm_kernel(const NormArgs r)
         const u32 row = begin + t * kAtOnce + threadIdx.x / G;
         return row < end ? row : end - 1;
     };
-    Row::load(next, x + (u64)row_at(0) * r.ldx, r.k, lane, whole);
+    Row::load(next, x + (u64)row_at(0) * r.ldx, r.k, lane);
     for (u32 t = 0; t < turns; ++t) {
         float v[C][V];
         float sum[1] = {0.0f};
+        Row::use(v, next, r.k, lane);
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) {
-                v[c][e] = to_f32(next[c][e]);
-                sum[0] += v[c][e];
-            }
-        if (t + 1 < turns) Row::load(next, x + (u64)row_at(t + 1) * r.ldx, r.k, lane, whole);
+            for (u32 e = 0; e < V; ++e) sum[0] += v[c][e];
+        if (t + 1 < turns) Row::load(next, x + (u64)row_at(t + 1) * r.ldx, r.k, lane);
         RowSums<G, 1>::of(sum, meet, turn);
         const float mean = sum[0] / (float)r.k;
         sum[0] = 0.0f;
@@ -194,7 +241,7 @@ __global__ __launch_bounds__(threads_of(G)) void norm_kernel(const NormArgs r)
 #pragma unroll
             for (u32 e = 0; e < V; ++e) v[c][e] = v[c][e] * s * gain[c][e] + shift[c][e];
         const u32 row = begin + t * kAtOnce + threadIdx.x / G;
-        if (row < end) Row::store(out + (u64)row * r.ldo, v, r.k, lane, whole);
+        if (row < end) Row::store(out + (u64)row * r.ldo, v, r.k, lane);
     }
 }
 
@@ -210,12 +257,12 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
     if (!run.found) return;
     const u32 lane = threadIdx.x % G, begin = run.begin + run.local * r.per;
     const u32 end = run.end - begin < r.per ? run.end : begin + r.per;
-    const bool whole = r.k % V == 0, inside = run.block != ~0u;
+    const bool inside = run.block != ~0u;
     T *out = static_cast<T *>(r.out);
     if (!inside) {
         const float none[C][V] = {};
         if (out)
-            for (u32 row = begin + threadIdx.x / G; row < end; row += kAtOnce) Row::store(out + (u64)row * r.ldo, none, r.k, lane, whole);
+            for (u32 row = begin + threadIdx.x / G; row < end; row += kAtOnce) Row::store(out + (u64)row * r.ldo, none, r.k, lane);
         return;
     }
     const T *x = static_cast<const T *>(r.x), *dy = static_cast<const T *>(r.dy);
@@ -229,8 +276,8 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
     const auto request = [&](u32 t) {
         u32 row = begin + t * kAtOnce + threadIdx.x / G;
         row = row < end ? row : end - 1;
-        Row::load(next_x, x + (u64)row * r.ldx, r.k, lane, whole);
-        Row::load(next_dy, dy + (u64)row * r.lddy, r.k, lane, whole);
+        Row::load(next_x, x + (u64)row * r.ldx, r.k, lane);
+        Row::load(next_dy, dy + (u64)row * r.lddy, r.k, lane);
     };
     request(0);
     for (u32 t = 0; t < turns; ++t) {
@@ -238,14 +285,12 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
         const bool there = row < end;
         float h[C][V], d[C][V];
         float sum[1] = {0.0f};
+        Row::use(h, next_x, r.k, lane);
+        Row::use(d, next_dy, r.k, lane);
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) {
-                h[c][e] = to_f32(next_x[c][e]);
-                d[c][e] = to_f32(next_dy[c][e]);
-                sum[0] += h[c][e];
-            }
+            for (u32 e = 0; e < V; ++e) sum[0] += h[c][e];
         if (t + 1 < turns) request(t + 1);
         RowSums<G, 1>::of(sum, meet, turn);
         const float mean = sum[0] / (float)r.k;
@@ -276,7 +321,7 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
                 }
                 d[c][e] = s * (g * gain[c][e] - level - h[c][e] * along);
             }
-        if (there && out) Row::store(out + (u64)row * r.ldo, d, r.k, lane, whole);
+        if (there && out) Row::store(out + (u64)row * r.ldo, d, r.k, lane);
     }
     if constexpr (SUMS) {
         const bool alone = run.end - run.begin <= r.per;
@@ -415,14 +460,31 @@ NormShape norm_shape(u32 k, u32 dtype, bool backward)
     return {0, 0};
 }
 
-// rows of a run
-u32 norm_per(u32 rows, u32 k, u32 dtype, bool backward)
+// Rows of a run: whole turns of the rows that run beside each other.  Forward, eight workgroups a compute unit hide each other's loads.  Of the
+// gradients' runs as many as are held at once, and where that makes them short, fewer: a run's sums are written and read again (2 k floats), and
+// joined one after the other.  A turn of a wavefront's rows is two chains of exchanges, of a workgroup's rows two meetings.
+u32 norm_per(u32 rows, u32 blocks, u32 k, u32 dtype, bool backward)
 {
     const NormShape s = norm_shape(k, dtype, backward);
     const u32 at_once = s.g == 0 ? 1 : threads_of(s.g) / s.g;
-    // eight workgroups a compute unit, of whole turns
-    const u32 turns = (u32)(((u64)rows + 2048ull * at_once - 1) / (2048ull * at_once));
-    return (turns < 1 ? 1 : turns) * at_once;
+    const auto turns_of = [&](u32 workgroups) {
+        const u64 t = ((u64)rows + (u64)workgroups * at_once - 1) / ((u64)workgroups * at_once);
+        return (u32)(t < 1 ? 1 : t);
+    };
+    if (!backward || s.g == 0) return turns_of(2048) * at_once;
+    const u32 values = s.c * (dtype == LMK_GS_F32 ? 4 : 8), held = 256 * (s.g == 1024 ? 1 : values <= 8 ? 5 : 3);
+    const double turn_us = s.g <= 64 ? 0.5 : s.g == 256 ? 0.8 : 1.2, set_us = 16.0 * k / 4e6;
+    u32 best = 1;
+    double least = -1;
+    for (u32 turns = turns_of(held - (blocks < held / 2 ? blocks : held / 2)), i = 0; i < 8; ++i, turns *= 2) {
+        const double runs = (double)rows / ((double)turns * at_once) + 1;
+        const double us = turns * turn_us + runs * set_us + runs / blocks / 256 * 0.6;
+        if (least < 0 || us < least) {
+            least = us;
+            best = turns;
+        }
+    }
+    return best * at_once;
 }
 
 template <class T, bool BACKWARD, u32 G, u32 C>
@@ -480,12 +542,12 @@ NormArgs norm_args(const lmk_gs_norm &n, const void *x, u64 ldx, void *out, u64 
     r.gain = n.gain; r.shift = n.shift;
     r.offsets = n.offsets; r.blocks = n.blocks; r.rows = n.rows; r.k = n.k; r.eps = n.eps;
     r.out = out; r.ldo = ldo;
-    r.per = norm_per(n.rows, n.k, n.dtype, backward);
+    r.per = norm_per(n.rows, n.blocks, n.k, n.dtype, backward);
     return r;
 }
 
 // sets of partial sums
-u64 norm_sets(const lmk_gs_norm &n) { return (u64)n.rows / norm_per(n.rows, n.k, n.dtype, true) + n.blocks + 1; }
+u64 norm_sets(const lmk_gs_norm &n) { return (u64)n.rows / norm_per(n.rows, n.blocks, n.k, n.dtype, true) + n.blocks + 1; }
 size_t norm_sets_bytes(const lmk_gs_norm &n) { return (size_t)(norm_sets(n) * 2 * n.k * 4 + 255) / 256 * 256; }
 
 }  // namespace
@@ -493,7 +555,7 @@ size_t norm_sets_bytes(const lmk_gs_norm &n) { return (size_t)(norm_sets(n) * 2 
 bool grouped_norm_fits(const lmk_gs_norm &n, bool backward, bool sums)
 {
     const NormShape s = norm_shape(n.k, n.dtype, backward);
-    const u64 runs = max_runs(n.rows, n.blocks, norm_per(n.rows, n.k, n.dtype, backward));
+    const u64 runs = max_runs(n.rows, n.blocks, norm_per(n.rows, n.blocks, n.k, n.dtype, backward));
     if (s.g == 0 ? (u64)n.rows * kLong >= kMostThreads : runs * threads_of(s.g) >= kMostThreads) return false;
     if (s.g == 0 && sums && runs * ((n.k + 255) / 256) * 256 >= kMostThreads) return false;
     return !sums || join_threads(n.k, 1, n.blocks, (u32)(norm_sets(n) - n.blocks)) < kMostThreads;

@@ -129,3 +129,21 @@ def test_in_every_size_the_sets_of_partial_sums_fit_the_workspace():
         for k in (1, 96, 1024, 5000, 20_000, 65_536):
             for blocks in (1, 3, 300):
                 assert B.grouped_norm_backward_bytes(rows, blocks, k) >= (blocks + 1) * 2 * k * 4
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch):
+    class Somewhere:                    # a tensor on the second GPU, as far as the check looks
+        device = torch.device("cuda", 1)
+        get_device = lambda self: 1
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ValueError, match="current device"):
+        B._stream_on(Somewhere(), None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+
+    class Other:
+        device = torch.device("cuda", 0)
+        cuda_stream = 1
+
+    with pytest.raises(ValueError, match="stream"):
+        B._stream_on(Somewhere(), Other())

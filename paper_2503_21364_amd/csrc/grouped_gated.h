@@ -23,6 +23,7 @@ struct GatedArgs {
     float *part;                // NULL, or sets of partial sums over rows of the gradients, 2 n each
     float *db;                  // where blocks of one set have theirs
     u32 tiles, col_tiles;
+    bool out32;                 // gradients of few rows: in 32 bits whatever the type
     bool past;                  // `out` is more than the caches of the dies hold
 };
 
@@ -87,6 +88,9 @@ __device__ __forceinline__ float *set_of(const GatedArgs &r, const RowRun &run, 
 bool gated_few_fit(const GatedArgs &r, bool wide);
 u64 gated_few_threads(const GatedArgs &r);
 hipError_t launch_gated_few(const GatedArgs &r, u32 dtype, hipStream_t stream);
+// all gradients of few rows, those of both projections in 32 bits in between: `grads` [rows][2 n], rows ldg apart, whole vectors
+bool gated_few_backward_fits(u32 rows, u32 blocks, u32 n, u32 k, u32 dtype);
+hipError_t launch_gated_few_backward(GatedArgs r, u32 dtype, float *grads, u64 ldg, void *dx, u64 lddx, void *dw, float *db, hipStream_t stream);
 constexpr u32 kGatedFewRows = 16, kGatedTileRows = 64;
 
 // small matrices, float32: y; all gradients in one pass, the sets of partial sums as launch_join numbers them, in runs of `.._backward_rows`

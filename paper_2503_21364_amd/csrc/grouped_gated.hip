@@ -186,7 +186,8 @@ struct GatedSpace {
 GatedSpace gated_space(const lmk_gs_linear &l)
 {
     GatedSpace s;
-    s.grads = round_up(l.rows * grads_stride(l) * (l.dtype == LMK_GS_F32 ? 4 : 2));
+    const bool few = gated_few_backward_fits(l.rows, l.blocks, l.n, l.k, l.dtype);
+    s.grads = round_up(l.rows * grads_stride(l) * (l.dtype == LMK_GS_F32 || few ? 4 : 2));
     // the least rows of a set that any alignment gives
     const GatedArgs r = gated_args(l, nullptr, l.k, nullptr, 0);
     const u32 least = gated_few_fit(r, false) || gated_few_fit(r, true) ? kGatedFewRows : kGatedTileRows;
@@ -222,6 +223,7 @@ bool grouped_gated_backward_fits(const lmk_gs_linear &l, u64 lddy, const void *x
     r.lddy = lddy;
     // one run a workgroup there, of which there are some hundred and one a block
     if (one_pass_fits(r, l.dtype, out.lddx) && join_threads(2 * l.n, l.k, l.blocks, l.rows / gated_narrow_backward_rows(r) + 1) < kMostThreads) return true;
+    if (gated_few_backward_fits(l.rows, l.blocks, l.n, l.k, l.dtype)) return true;
     if (own_db && join_threads(2 * l.n, 0, l.blocks, l.rows / gated_set_rows(r, l.dtype) + 1) >= kMostThreads) return false;
     const lmk_gs_linear_grads grads = {out.dx, out.lddx, static_cast<float *>(out.dw), own_db ? nullptr : out.db};
     if (gated_threads(r, l.dtype) >= kMostThreads) return false;
@@ -253,6 +255,8 @@ hipError_t launch_grouped_gated_backward(const lmk_gs_linear &l, const void *dy,
         const u32 per = gated_narrow_backward_rows(r);
         return launch_join(l.offsets, l.blocks, l.rows, per, part, 2 * l.n, l.k, dw, out.db, l.rows / per + 1, stream);
     }
+    if (gated_few_backward_fits(l.rows, l.blocks, l.n, l.k, l.dtype))
+        return launch_gated_few_backward(r, l.dtype, reinterpret_cast<float *>(workspace), grads_stride(l), out.dx, out.lddx, out.dw, out.db, stream);
     r.out = workspace;
     r.ldo = grads_stride(l);
     if (own_db) {

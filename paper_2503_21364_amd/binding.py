@@ -525,27 +525,30 @@ def anchor_decode_culled(anchors: AnchorScene, index: AnchorIndex, cam: Camera, 
 
 # ---- perceptron layers whose weights belong to blocks of rows, and 8-bit checkpoints of their inputs
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+OFFSET_TYPES = torch.int32, torch.uint32
 
 
 def _dtype(t) -> int:
-    if t.dtype not in DTYPES:
+    code = DTYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"float32 or bfloat16 is expected, got {t.dtype}")
-    return DTYPES[t.dtype]
+    return code
 
 
 def _matrix(t, shape, like, name):
     """The row stride of a 2-d tensor of `shape` with whole rows, of the type and on the device of `like`."""
     if t.shape != shape:
         raise ValueError(f"{name} is {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype != like.dtype or t.device != like.device:
+    if t is not like and (t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name} has another type or device ({t.dtype}, {t.device})")
-    if shape[1] > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1:
         raise ValueError(f"{name}: the values of a row have to lie next to each other")
-    return max(t.stride(0), shape[1]) if shape[0] <= 1 else t.stride(0)
+    return max(ld, shape[1]) if shape[0] <= 1 else ld
 
 
 def _dense(t, shape, dtype, like, name):
-    if t is not None and (t.shape != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous()):
+    if t is not None and (t.shape != shape or t.dtype != dtype or t.get_device() != like.get_device() or not t.is_contiguous()):
         raise ValueError(f"{name} has to be a contiguous {dtype} tensor {tuple(shape)} on {like.device}")
 
 
@@ -577,17 +580,23 @@ class Checkpoint8:
         self.c = Checkpoint8C(_ptr(self.codes), _ptr(self.scale))
 
 
-def _layer(w, offsets, rows: int, in_major: bool) -> LinearC:
-    if w.dim() != 3 or offsets.dim() != 1 or offsets.numel() != w.shape[0] + 1:
+def _layer(w, offsets, rows: int, in_major: bool, projections: int = 1) -> LinearC:
+    """`projections`: how many of them the matrices hold; n is of one."""
+    shape, counts = w.shape, offsets.shape
+    if len(shape) != 3 or len(counts) != 1 or counts[0] != shape[0] + 1:
         raise ValueError("weights are [blocks][outputs][inputs] (in_major: [blocks][inputs][outputs]) and offsets [blocks + 1]")
-    if offsets.dtype not in (torch.int32, torch.uint32) or not offsets.is_contiguous() or offsets.device != w.device:
+    if offsets.dtype not in OFFSET_TYPES or not offsets.is_contiguous() or offsets.get_device() != w.get_device():
         raise ValueError("offsets have to be a contiguous 32-bit tensor on the weights' device")
-    if w.shape[2] > 1 and w.stride(2) != 1:
+    block, ldw, step = w.stride()
+    if step != 1 and shape[2] > 1:
         raise ValueError("the last axis of the weights has to be contiguous")
-    n, k = (w.shape[2], w.shape[1]) if in_major else (w.shape[1], w.shape[2])
-    _fit_u32(rows, w.shape[0], n, k)
-    ldw = w.stride(1) if w.shape[1] > 1 else max(w.stride(1), w.shape[2])
-    return LinearC(_ptr(w), _ptr(offsets), ldw, w.stride(0), w.shape[0], rows, n, k, _dtype(w), int(in_major))
+    n, k = (shape[2], shape[1]) if in_major else (shape[1], shape[2])
+    _fit_u32(rows, shape[0], n, k)
+    if n % projections:
+        raise ValueError("weights hold two projections: [blocks][2 outputs][inputs] (in_major: [blocks][inputs][2 outputs])")
+    if shape[1] <= 1:
+        ldw = max(ldw, shape[2])
+    return LinearC(w.data_ptr(), offsets.data_ptr(), ldw, block, shape[0], rows, n // projections, k, _dtype(w), int(in_major))
 
 
 def grouped_linear(x, w, offsets, out, bias=None, relu: bool = False, in_major: bool = False,
@@ -673,7 +682,7 @@ def checkpoint8_unpack(checkpoint: Checkpoint8, out, stream=None) -> None:
 # ---- layer norm of the rows of blocks
 def _stream_on(like, stream):
     """The handle of `stream` (None: the current one), which has to be of the tensors' device, and that the current one."""
-    device = torch.cuda.current_device()
+    device = torch._C._cuda_getDevice()                 # torch.cuda.current_device() without its look whether there is one: the tensors are there
     if like.get_device() != device:
         raise ValueError(f"the tensors are on {like.device}, the current device is cuda:{device}")
     if stream is None:
@@ -685,11 +694,12 @@ def _stream_on(like, stream):
 
 def _offsets(offsets, like) -> int:
     """The number of blocks."""
-    if offsets.dim() != 1 or offsets.numel() < 2 or offsets.dtype not in (torch.int32, torch.uint32) or not offsets.is_contiguous():
+    shape = offsets.shape
+    if len(shape) != 1 or shape[0] < 2 or offsets.dtype not in OFFSET_TYPES or not offsets.is_contiguous():
         raise ValueError("offsets have to be a contiguous 32-bit tensor [blocks + 1]")
-    if offsets.device != like.device:
+    if offsets.get_device() != like.get_device():
         raise ValueError(f"offsets are on {offsets.device}, the rows on {like.device}")
-    return offsets.numel() - 1
+    return shape[0] - 1
 
 
 def _workspace(t, like):
@@ -699,9 +709,11 @@ def _workspace(t, like):
 
 
 def _norm(x, offsets, gain, shift, eps: float) -> NormC:
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError("x is [rows][k]")
-    rows, k, blocks = x.shape[0], x.shape[1], _offsets(offsets, x)
+    rows, k = shape
+    blocks = _offsets(offsets, x)
     _fit_u32(rows, k, blocks)
     _dense(gain, (blocks, k), torch.float32, x, "gain")
     _dense(shift, (blocks, k), torch.float32, x, "shift")
@@ -758,11 +770,7 @@ def _gated(w, offsets, rows: int, in_major: bool, act: str) -> LinearC:
     """The layer with n of the outputs, of which its matrices have two each."""
     if act not in ACTS:
         raise ValueError(f"act is one of {tuple(ACTS)}, got {act!r}")
-    layer = _layer(w, offsets, rows, in_major)
-    if layer.n % 2:
-        raise ValueError("weights hold two projections: [blocks][2 outputs][inputs] (in_major: [blocks][inputs][2 outputs])")
-    layer.n //= 2
-    return layer
+    return _layer(w, offsets, rows, in_major, 2)
 
 
 def grouped_gated(x, w, offsets, out, bias=None, act: str = "silu", in_major: bool = False, stream=None) -> None:
@@ -771,9 +779,10 @@ def grouped_gated(x, w, offsets, out, bias=None, act: str = "silu", in_major: bo
     bg and then bu; x [rows][inputs], out [rows][outputs], float32 or bfloat16 as w; offsets int32 [blocks + 1] on the device; act: "silu",
     "gelu" or "relu"."""
     layer = _gated(w, offsets, x.shape[0], in_major, act)
-    ldx = _matrix(x, (layer.rows, layer.k), w, "x")
-    ldy = _matrix(out, (layer.rows, layer.n), w, "out")
-    _dense(bias, (layer.blocks, 2 * layer.n), torch.float32, w, "bias")
+    rows, n = layer.rows, layer.n
+    ldx = _matrix(x, (rows, layer.k), w, "x")
+    ldy = _matrix(out, (rows, n), w, "out")
+    _dense(bias, (layer.blocks, 2 * n), torch.float32, w, "bias")
     _on_gpu(w)
     rc = lib().lmk_gs_grouped_gated(C.byref(layer), _ptr(x), ldx, _ptr(bias), ACTS[act], _ptr(out), ldy, _stream_on(w, stream))
     if rc != OK:

@@ -136,10 +136,10 @@ def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch)
         device = torch.device("cuda", 1)
         get_device = lambda self: 1
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
     with pytest.raises(ValueError, match="current device"):
         B._stream_on(Somewhere(), None)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
 
     class Other:
         device = torch.device("cuda", 0)

@@ -266,7 +266,15 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
 {
     lds_char *lp = lds, *lq = lds + 2 * S::kPartP;
     constexpr bool kDirect = P::kDirect && Q::kDirect;
-    if constexpr (kDirect) static_assert(P::kLoads + Q::kLoads == 8, "the wait below counts eight loads a pair");
+    // the second pair's loads may be on their way
+    constexpr u32 kFirst = [] {
+        if constexpr (kDirect) {
+            static_assert(P::kLoads + Q::kLoads < 16, "four bits of a count");
+            return 0xF70u | (P::kLoads + Q::kLoads);
+        } else {
+            return 0x070u;
+        }
+    }();
     bf16x8 fp[S::kP], fq[2][S::kQ];
     auto fill = [&](u32 part) {
         p.fill(lp + part * S::kPartP, wave);
@@ -289,7 +297,7 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
     if constexpr (!STARTED) {
         fill(0);
         fill(1);
-        wavefronts_meet<kDirect ? 0xF70 | 8 : 0x070>();             // the second pair's eight loads may be on their way
+        wavefronts_meet<kFirst>();
     }
 #pragma unroll
     for (u32 i = 0; i < S::kP; ++i) fp[i] = p.fragment(lp, 0, p0, i);

@@ -337,17 +337,29 @@ bool rows_sixteen(const RowsArgs &r)
 // tiles a round is 256, and its costs come whole; of 128 x 128 it is 512, two workgroups a compute unit, with 0.7 of the time
 // for half of the results, and the two even out what a last round leaves.  8 ragged blocks of 1024 x 1024, large / small tiles: 4096 rows
 // 30 / 20 us, 16 384 56 / 48, 65 536 158 / 183; one of 512 x 512: 16 384 20 / 14, 32 768 23 / 31.
-bool large_tiles(const RowsArgs &r)
+// 256 columns x 192 rows, 0.82 of the time of 256 x 256 for three quarters of the results, where a last round of those would be nearly empty and
+// this leaves a tenth (dx of 16 384 rows of 4 ragged blocks, 8192 -> 2048: 128 x 128 593 us, 256 x 192 490; of even blocks 256 x 256 406).
+struct RowsTile {
+    u32 cols, rows;
+};
+RowsTile rows_tile(const RowsArgs &r, bool gate)
 {
-    const auto share = [&](u32 side) { return __builtin_ceilf((float)r.rows / side + 0.5f * (r.blocks - 1)) * ((r.cols + side - 1) / side); };
-    return __builtin_ceilf(share(256) / 256) < 0.7f * share(128) / 512;
+    const auto share = [&](u32 cols, u32 rows) { return __builtin_ceilf((float)r.rows / rows + 0.5f * (r.blocks - 1)) * ((r.cols + cols - 1) / cols); };
+    const float large = __builtin_ceilf(share(256, 256) / 256), small = 0.7f * share(128, 128) / 512;
+    const float between = 0.82f * __builtin_ceilf(share(256, 192) / 256);
+    if (!gate && between < 0.9f * (large < small ? large : small)) return RowsTile{256, 192};
+    return large < small ? RowsTile{256, 256} : RowsTile{128, 128};
 }
 
 template <bool ACROSS, u32 GATE>
 hipError_t wide_shape(const RowsArgs &r, hipStream_t stream)
 {
     if (!rows_sixteen(r)) return wide_go<128, 128, 2, 2, ACROSS, true, GATE>(r, stream);
-    if (large_tiles(r)) return wide_go<256, 256, 2, 4, ACROSS, false, GATE>(r, stream);
+    const u32 rows = rows_tile(r, GATE != 0).rows;
+    if (rows == 256) return wide_go<256, 256, 2, 4, ACROSS, false, GATE>(r, stream);
+    if constexpr (GATE == 0) {
+        if (rows == 192) return wide_go<256, 192, 4, 2, ACROSS, false, GATE>(r, stream);
+    }
     return wide_go<128, 128, 2, 2, ACROSS, false, GATE>(r, stream);
 }
 
@@ -381,8 +393,8 @@ bool wide_rows_fit(const RowsArgs &r)
 
 u64 wide_rows_threads(const RowsArgs &r)
 {
-    const u32 side = rows_sixteen(r) && large_tiles(r) ? 256 : 128;
-    return max_runs(r.rows, r.blocks, side) * ((r.cols + side - 1) / side) * (side * 2);
+    const RowsTile tile = rows_sixteen(r) ? rows_tile(r, r.gate || r.keep_codes) : RowsTile{128, 128};
+    return max_runs(r.rows, r.blocks, tile.rows) * ((r.cols + tile.cols - 1) / tile.cols) * (tile.cols * 2);
 }
 
 hipError_t launch_wide_rows(const RowsArgs &r, bool across, hipStream_t stream)

@@ -297,3 +297,23 @@ def test_rows_of_no_block_where_rows_are_few(dtype):
     xs[1][:3] = xs[1][15:] = 0
     want, mag = Q.forward(xs, data(w4), [3, 7, 7, 15], k)
     _close(y, want, (k + 3) * U * mag, dtype == "bf16", "y of 4 bits")
+
+
+def test_tiles_of_192_rows():
+    """A size whose tiles of 256 x 256 would leave a last round nearly empty: forward (n = 4096) and dx (k = 4096) of 8300 rows in ragged blocks."""
+    rows, offsets, many, few = 8300, [1, 3000, 3001, 8290], 4096, 72
+    g = torch.Generator().manual_seed(12)
+    off = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+    a = torch.randn(rows, few, generator=g).to(torch.bfloat16).to(DEV)
+    w = (torch.randn(3, many, few, generator=g) / 8).to(torch.bfloat16).to(DEV)
+    out = torch.full((rows, many), 7.0, dtype=torch.bfloat16, device=DEV)
+    want, mag = L.forward(_np(a), _np(w), offsets)
+    B.grouped_linear(a, w, off, out)
+    _close(out, want, (few + 2) * U * mag, True, "y")
+    # the same product as dx of a layer of 4096 inputs and 72 outputs
+    v = w.transpose(1, 2).contiguous()
+    ws = torch.empty(B.grouped_linear_backward_bytes(rows, 3, few, many, torch.bfloat16), dtype=torch.uint8, device=DEV)
+    first = out.clone()
+    B.grouped_linear_backward(a, v, off, ws, dx=out)
+    _close(out, want, (few + 2) * U * mag, True, "dx")
+    assert torch.equal(first, out)          # the same sums in the same order

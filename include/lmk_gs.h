@@ -496,8 +496,8 @@ typedef struct lmk_gs_gated_grads {
 int32_t lmk_gs_grouped_gated_backward_bytes(const lmk_gs_linear *layer, size_t *bytes);
 
 /* From dy [rows][n], the gradient of y, and the input x (a and u are computed again).  The gradients of a and u are rounded to dtype
- * before dx and dw are summed from them in 32 bits; db is summed from them before that.  Sums over a block's rows are taken in an
- * order that depends on the sizes and alignments only.  workspace: 256-byte aligned, always needed.  Outputs must not overlap inputs.  Errors as
+ * before dx and dw are summed from them in 32 bits (not where rows are few); db is summed from them before that.  Sums over a block's rows are
+ * taken in an order that depends on the sizes and alignments only.  workspace: 256-byte aligned, always needed.  Outputs must not overlap inputs.  Errors as
  * lmk_gs_grouped_gated; LMK_GS_ERR_CAPACITY: workspace too small. */
 int32_t lmk_gs_grouped_gated_backward(const lmk_gs_linear *layer, const void *dy, uint64_t lddy, const void *x, uint64_t ldx,
                                       const float *bias, uint32_t act, const lmk_gs_gated_grads *out, void *workspace,

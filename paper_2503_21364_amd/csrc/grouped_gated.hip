@@ -7,9 +7,10 @@
 // side by side, [rows][2 n], in the workspace; from there dx = [da du] W and dW = [da du]^T x are the grouped layers' own products.
 // In bfloat16 da and du are rounded there (the matrix instructions take nothing wider), so that a dW in 32 bits would hold that rounding
 // at twice the bytes: it has the weights' type.  The bias' gradient does not go through them: it is summed in 32 bits beside the
-// activation, before the rounding.
+// activation, before the rounding.  Few rows (grouped_gated_few.hip) and small float32 matrices (grouped_gated_narrow.hip) have da and du in 32 bits.
 //
-// Kernel here: v_mfma_f32_32x32x2_f32, tiles of 64 rows x 64 outputs of both projections, the rows' part of LDS being read for both.
+// Kernel here: v_mfma_f32_32x32x2_f32, tiles of 64 rows x 64 outputs of both projections, the rows' part of LDS being read for both.  Bound by
+// those instructions where k is large; 25 362 rows, 64 -> 576: 62 us, 60 of 154 TFLOP/s, a tile being two steps between a chain of loads and its stores.
 #include "grouped_gated.h"
 #include "grouped_tiles.h"
 
@@ -222,7 +223,7 @@ bool grouped_gated_backward_fits(const lmk_gs_linear &l, u64 lddy, const void *x
     r.dy = reinterpret_cast<const void *>(256);             // told from NULL: gradients are asked for
     r.lddy = lddy;
     // one run a workgroup there, of which there are some hundred and one a block
-    if (one_pass_fits(r, l.dtype, out.lddx) && join_threads(2 * l.n, l.k, l.blocks, l.rows / gated_narrow_backward_rows(r) + 1) < kMostThreads) return true;
+    if (one_pass_fits(r, l.dtype, out.lddx)) return join_threads(2 * l.n, l.k, l.blocks, l.rows / gated_narrow_backward_rows(r) + 1) < kMostThreads;
     if (gated_few_backward_fits(l.rows, l.blocks, l.n, l.k, l.dtype)) return true;
     if (own_db && join_threads(2 * l.n, 0, l.blocks, l.rows / gated_set_rows(r, l.dtype) + 1) >= kMostThreads) return false;
     const lmk_gs_linear_grads grads = {out.dx, out.lddx, static_cast<float *>(out.dw), own_db ? nullptr : out.db};

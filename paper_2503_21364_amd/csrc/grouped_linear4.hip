@@ -1,6 +1,10 @@
 // Layers whose weights belong to blocks of rows, both operands in 4 bits (lmk_gs_grouped_linear4): y = act(x w_g^T + b_g) on
 // v_mfma_scale_f32_16x16x128_f8f6f4.  A lane feeds 32 codes, 16 bytes, of one row and their scale byte; the products of codes and powers of two are
 // exact, sums are in 32 bits.
+//
+// 8192 x 8192 x 8192 262 us, 4.2 PFLOP/s; 65 536 rows of 2048 -> 2048 in 16 blocks 171 us of the same inputs (3.2) and 196 to 216 of others (268 MB
+// of results in bfloat16 alone take 52).  Bound by LDS and its loads: a step's fragments and scales take it as long as their products take the
+// matrix instructions, which reach 7 PFLOP/s by themselves.
 #include "block4.h"
 #include "grouped_wide.h"
 
@@ -114,6 +118,8 @@ template <class T, u32 NT> hipError_t few_go(Linear4Args r, hipStream_t stream)
     hipLaunchKernelGGL((few_rows4_kernel<T, NT>), dim3(r.tiles), dim3(512), 0, stream, r);
     return hipGetLastError();
 }
+// 64 outputs where that fills the compute units (128 rows, one block of 2048 -> 2048, 64 / 16: 7.0 / 9.5 us; 24 rows, 64 blocks of 1024 -> 2048 8.2 /
+// 11.3), 16 where not (one row, 8 blocks of 4096 -> 4096: 9.5 / 4.3)
 u32 few_columns(const Linear4Args &r) { return max_runs(r.rows, r.blocks, kRows) * ((r.n + 63) / 64) >= 320 ? 64 : 16; }
 
 // ---- tiles, as in grouped_wide.hip: a row's 256 codes are the 128 bytes that 64 bfloat16 are there, and come into LDS by the same loads, and a
@@ -355,12 +361,15 @@ template <class T, u32 TP, u32 TQ, u32 WP, u32 WQ> hipError_t wide_go(Linear4Arg
     hipLaunchKernelGGL(kernel, dim3(r.tiles < at_once ? r.tiles : at_once), dim3(S::kThreads), lds, stream, r);
     return hipGetLastError();
 }
-// as in grouped_wide.hip
+// As in grouped_wide.hip.  256 x 256 / 128 x 128, 8 blocks of 1024 -> 1024: 4096 rows 15.6 / 10.2 us, 16 384 18.9 / 21.3, 65 536 61 / 72;
+// 10 007 rows in 7 of 1000 -> 257 18.3 / 11.1; 8192 x 8192 x 8192 262 / 321.
 bool large_tiles(const Linear4Args &r)
 {
     const auto share = [&](u32 side) { return __builtin_ceilf((float)r.rows / side + 0.5f * (r.blocks - 1)) * ((r.n + side - 1) / side); };
     return __builtin_ceilf(share(256) / 256) < 0.7f * share(128) / 512;
 }
+// This kernel / tiles: one row, 8 blocks of 4096 -> 4096 4.3 / 12.9 us; 128 rows, one block of 2048 -> 2048 7.1 / 8.7, 8 of 1024 -> 1024 4.2 / 6.0;
+// 64 blocks of 1024 -> 2048, 24 rows 8.1 / 7.6
 bool few_fit(const Linear4Args &r)
 {
     const u64 row_tiles = r.rows < r.blocks ? r.rows : r.blocks;

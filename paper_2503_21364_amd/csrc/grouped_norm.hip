@@ -10,6 +10,10 @@
 // Bound by memory: a row is read once.  It stays in the registers of G lanes, C vectors of 16 bytes each, and what is summed
 // over it goes from lane to lane without LDS (G <= 64), or through LDS once a sum.  A workgroup has a run of rows of one block,
 // so that gain and shift are in registers, and so are its sums of dgain and dshift: x and dy are read once for all three gradients.
+//
+// The same inputs again and again: 65 536 rows of 1024 in 32 blocks, bfloat16, 52 us (5.2 TB/s), all gradients 91 (4.4 TB/s); 300 000 x 96 in 24,
+// float32, 38 (6.0 TB/s; 52 with other inputs every time); 4744 x 4033 in 7, bfloat16, 19, gradients 54: there are four rows a workgroup, and a
+// row's two meetings stand behind its loads; one row of 1024 3.0, a chain of latencies.
 #include "grouped_kernels.h"
 
 namespace lmk {
@@ -364,9 +368,20 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
 // ---- rows longer than a workgroup's registers: one row a workgroup of 1024, read again for every pass over it (from cache, mostly)
 constexpr u32 kLong = 1024;
 
+// The vectors of a row that this thread has: f(first column, vector that begins there or in front of it, first of its values that counts)
+template <class T, class F> __device__ __forceinline__ void each_vector(u32 first, u32 step, u32 k, F &&f)
+{
+    constexpr u32 V = kVec<T>;
+    for (u32 at = first * V; at < k; at += step * V) {
+        const u32 from = at + V <= k ? at : k - V;
+        f(from, at - from);
+    }
+}
+
 template <class T, bool BACKWARD>
 __global__ __launch_bounds__(kLong) void long_norm_kernel(const NormArgs r)
 {
+    constexpr u32 V = kVec<T>;
     __shared__ float meet[2 * 16 * 4];
     const RowRun run = find_run(r.offsets, r.blocks, r.rows, 1, blockIdx.x);          // runs of one row
     if (!run.found) return;
@@ -382,19 +397,30 @@ __global__ __launch_bounds__(kLong) void long_norm_kernel(const NormArgs r)
     const float share = 1.0f / (float)r.k;
     u32 turn = 0;
     float sum[1] = {0.0f};
-    for (u32 i = threadIdx.x; i < r.k; i += kLong) sum[0] += to_f32(x[i]);
+    each_vector<T>(threadIdx.x, kLong, r.k, [&](u32 from, u32 first) {
+        const Vec<T> v = load_any<Vec<T>>(x + from);
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) sum[0] += e >= first ? to_f32(v[e]) : 0.0f;
+    });
     RowSums<kLong, 1>::of(sum, meet, turn);
     const float mean = sum[0] / (float)r.k;
     float sums[3] = {0.0f, 0.0f, 0.0f};
-    for (u32 i = threadIdx.x; i < r.k; i += kLong) {
-        const float h = to_f32(x[i]) - mean;
-        sums[0] += h * h;
-        if (BACKWARD) {
-            const float w = to_f32(dy[i]) * (gain ? gain[i] : 1.0f);
-            sums[1] += w;
-            sums[2] += w * h;
+    each_vector<T>(threadIdx.x, kLong, r.k, [&](u32 from, u32 first) {
+        const Vec<T> v = load_any<Vec<T>>(x + from);
+        Vec<T> g = {};
+        if (BACKWARD) g = load_any<Vec<T>>(dy + from);
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) {
+            if (e < first) continue;
+            const float h = to_f32(v[e]) - mean;
+            sums[0] += h * h;
+            if (BACKWARD) {
+                const float w = to_f32(g[e]) * (gain ? gain[from + e] : 1.0f);
+                sums[1] += w;
+                sums[2] += w * h;
+            }
         }
-    }
+    });
     RowSums<kLong, 3>::of(sums, meet, turn);
     const float s = 1.0f / sqrtf(sums[0] * share + r.eps), level = sums[1] * share, along = sums[2] * share * s;
     if (BACKWARD && r.stats && threadIdx.x == 0) {
@@ -402,40 +428,75 @@ __global__ __launch_bounds__(kLong) void long_norm_kernel(const NormArgs r)
         r.stats[2 * (u64)row + 1] = s;
     }
     if (!out) return;
-    for (u32 i = threadIdx.x; i < r.k; i += kLong) {
-        const float h = (to_f32(x[i]) - mean) * s, w = gain ? gain[i] : 1.0f;
-        out[i] = BACKWARD ? (T)(s * (to_f32(dy[i]) * w - level - h * along)) : (T)(h * w + (shift ? shift[i] : 0.0f));
-    }
+    // out may be x or dy: what a vector holds in front of its first value may have its result already, and is not used
+    each_vector<T>(threadIdx.x, kLong, r.k, [&](u32 from, u32 first) {
+        const Vec<T> v = load_any<Vec<T>>(x + from);
+        Vec<T> g = {}, o;
+        if (BACKWARD) g = load_any<Vec<T>>(dy + from);
+#pragma unroll
+        for (u32 e = 0; e < V; ++e) {
+            const float h = (to_f32(v[e]) - mean) * s, w = gain ? gain[from + e] : 1.0f;
+            o[e] = BACKWARD ? (T)(s * (to_f32(g[e]) * w - level - h * along)) : (T)(h * w + (shift ? shift[from + e] : 0.0f));
+        }
+        if (first == 0) {
+            store_any(out + from, o);
+        } else {
+#pragma unroll
+            for (u32 e = 1; e < V; ++e)
+                if (e >= first) out[from + e] = o[e];
+        }
+    });
 }
 
-// dgain and dshift of such rows: a thread sums a column over a run of rows
+// dgain and dshift of such rows: a thread sums a vector of columns over a run of rows, four of them on their way
 template <class T>
 __global__ __launch_bounds__(256) void long_norm_sums_kernel(const NormArgs r)
 {
-    const u32 pieces = (r.k + 255) / 256, t = blockIdx.x / pieces;
+    constexpr u32 V = kVec<T>, kRows = 4;
+    const u32 pieces = (r.k + 256 * V - 1) / (256 * V), t = blockIdx.x / pieces;
     const RowRun run = find_run(r.offsets, r.blocks, r.rows, r.per, t);
     if (!run.found || run.block == ~0u) return;
-    const u32 at = (blockIdx.x - t * pieces) * 256 + threadIdx.x, begin = run.begin + run.local * r.per;
+    const u32 at = ((blockIdx.x - t * pieces) * 256 + threadIdx.x) * V, begin = run.begin + run.local * r.per;
     const u32 end = run.end - begin < r.per ? run.end : begin + r.per;
     if (at >= r.k) return;
-    float dgain = 0.0f, dshift = 0.0f;
-    for (u32 row = begin; row < end; ++row) {
-        const float g = to_f32(static_cast<const T *>(r.dy)[(u64)row * r.lddy + at]);
-        const float h = (to_f32(static_cast<const T *>(r.x)[(u64)row * r.ldx + at]) - r.stats[2 * (u64)row]) * r.stats[2 * (u64)row + 1];
-        dgain += g * h;
-        dshift += g;
+    const u32 from = at + V <= r.k ? at : r.k - V, first = at - from;
+    float dgain[V] = {}, dshift[V] = {};
+    for (u32 row0 = begin; row0 < end; row0 += kRows) {
+        Vec<T> x[kRows], dy[kRows];
+        float mean[kRows], s[kRows];
+#pragma unroll
+        for (u32 i = 0; i < kRows; ++i) {
+            const u64 row = row0 + i < end ? row0 + i : row0;
+            x[i] = load_any<Vec<T>>(static_cast<const T *>(r.x) + row * r.ldx + from);
+            dy[i] = load_any<Vec<T>>(static_cast<const T *>(r.dy) + row * r.lddy + from);
+            mean[i] = r.stats[2 * row];
+            s[i] = r.stats[2 * row + 1];
+        }
+#pragma unroll
+        for (u32 i = 0; i < kRows; ++i) {
+            if (row0 + i >= end) break;
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                const float g = to_f32(dy[i][e]);
+                dgain[e] += g * ((to_f32(x[i][e]) - mean[i]) * s[i]);
+                dshift[e] += g;
+            }
+        }
     }
     RowSlices all;
     all.init(r.offsets, r.blocks, r.rows, r.per);
-    if (run.end - run.begin <= r.per) {
-        if (r.dgain) r.dgain[(u64)run.block * r.k + at] = dgain;
-        if (r.dshift) r.dshift[(u64)run.block * r.k + at] = dshift;
-    } else {
-        float *set = r.part + (u64)(run.block + all.slice_of(run.begin) + run.local) * 2 * r.k;
-        set[at] = dgain;
-        set[r.k + at] = dshift;
+    const bool alone = run.end - run.begin <= r.per;
+    float *set = r.part + (u64)(run.block + all.slice_of(run.begin) + run.local) * 2 * r.k;
+    float *to_gain = alone ? r.dgain ? r.dgain + (u64)run.block * r.k : nullptr : set;
+    float *to_shift = alone ? r.dshift ? r.dshift + (u64)run.block * r.k : nullptr : set + r.k;
+#pragma unroll
+    for (u32 e = 0; e < V; ++e) {
+        if (e < first) continue;
+        if (to_gain) to_gain[from + e] = dgain[e];
+        if (to_shift) to_shift[from + e] = dshift[e];
     }
 }
+u32 long_pieces(u32 k, u32 dtype) { return (k + 256 * (dtype == LMK_GS_F32 ? 4 : 8) - 1) / (256 * (dtype == LMK_GS_F32 ? 4 : 8)); }
 
 // ---- launches
 
@@ -471,7 +532,13 @@ u32 norm_per(u32 rows, u32 blocks, u32 k, u32 dtype, bool backward)
         const u64 t = ((u64)rows + (u64)workgroups * at_once - 1) / ((u64)workgroups * at_once);
         return (u32)(t < 1 ? 1 : t);
     };
-    if (!backward || s.g == 0) return turns_of(2048) * at_once;
+    if (!backward) return turns_of(2048) * at_once;
+    // of rows longer than registers: the sums' workgroups fill the device four times, with 16 rows or more (all gradients of 4096 rows of 16 000 in
+    // bfloat16 527 us; 937 with runs of two rows, a column a thread)
+    if (s.g == 0) {
+        const u32 runs = 1024 / long_pieces(k, dtype), per = turns_of(runs < 1 ? 1 : runs);
+        return per < 16 ? 16 : per;
+    }
     const u32 values = s.c * (dtype == LMK_GS_F32 ? 4 : 8), held = 256 * (s.g == 1024 ? 1 : values <= 8 ? 5 : 3);
     const double turn_us = s.g <= 64 ? 0.5 : s.g == 256 ? 0.8 : 1.2, set_us = 16.0 * k / 4e6;
     u32 best = 1;
@@ -530,7 +597,7 @@ hipError_t norm_as(const NormArgs &r, hipStream_t stream)
     stats.out = nullptr;
     hipError_t e = rows_go(stats);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(long_norm_sums_kernel<T>, dim3((r.k + 255) / 256 * (u32)max_runs(r.rows, r.blocks, r.per)), dim3(256), 0, stream, r);
+    hipLaunchKernelGGL(long_norm_sums_kernel<T>, dim3(long_pieces(r.k, kF32 ? LMK_GS_F32 : LMK_GS_BF16) * (u32)max_runs(r.rows, r.blocks, r.per)), dim3(256), 0, stream, r);
     e = hipGetLastError();
     return e == hipSuccess && r.out ? rows_go(r) : e;
 }
@@ -557,7 +624,7 @@ bool grouped_norm_fits(const lmk_gs_norm &n, bool backward, bool sums)
     const NormShape s = norm_shape(n.k, n.dtype, backward);
     const u64 runs = max_runs(n.rows, n.blocks, norm_per(n.rows, n.blocks, n.k, n.dtype, backward));
     if (s.g == 0 ? (u64)n.rows * kLong >= kMostThreads : runs * threads_of(s.g) >= kMostThreads) return false;
-    if (s.g == 0 && sums && runs * ((n.k + 255) / 256) * 256 >= kMostThreads) return false;
+    if (s.g == 0 && sums && runs * long_pieces(n.k, n.dtype) * 256 >= kMostThreads) return false;
     return !sums || join_threads(n.k, 1, n.blocks, (u32)(norm_sets(n) - n.blocks)) < kMostThreads;
 }
 

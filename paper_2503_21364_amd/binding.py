@@ -834,13 +834,14 @@ class Block4:
         self.scale = torch.empty(shapes[1], dtype=torch.uint8, device=self.codes.device) if scale is None else scale
         _dense(self.codes, shapes[0], torch.uint8, self.codes, "codes")
         _dense(self.scale, shapes[1], torch.uint8, self.codes, "scale")
+        self.device = self.codes.get_device()
         self.c = Block4C(_ptr(self.codes), _ptr(self.scale))
 
 
 def block4_pack(x, form: Block4, stream=None) -> None:
     """lmk_gs_block4_pack: the 4-bit form of x [rows][k], float32 or bfloat16."""
     ldx = _matrix(x, (form.rows, form.k), x, "x")
-    if x.device != form.codes.device:
+    if x.get_device() != form.device:
         raise ValueError("x and the 4-bit form are on different devices")
     dtype = _dtype(x)
     _on_gpu(x)
@@ -852,7 +853,7 @@ def block4_pack(x, form: Block4, stream=None) -> None:
 def block4_unpack(form: Block4, out, stream=None) -> None:
     """lmk_gs_block4_unpack: the values the codes stand for (exact in bfloat16 too)."""
     ldx = _matrix(out, (form.rows, form.k), out, "out")
-    if out.device != form.codes.device:
+    if out.get_device() != form.device:
         raise ValueError("out and the 4-bit form are on different devices")
     dtype = _dtype(out)
     _on_gpu(out)
@@ -865,15 +866,15 @@ def grouped_linear4(x: Block4, w: Block4, offsets, out, bias=None, relu: bool = 
     """lmk_gs_grouped_linear4: out[r] = act(w[g] x[r] + bias[g]) for the rows offsets[g] .. offsets[g+1]-1 of every block g, x [rows][inputs]
     and w in 4 bits: w is the form of all blocks' matrices below each other, [blocks * outputs][inputs].  out [rows][outputs], float32 or
     bfloat16; offsets int32 [blocks + 1] on the device; bias float32 [blocks][outputs]."""
-    blocks = _offsets(offsets, out)
-    if out.dim() != 2 or w.rows != blocks * out.shape[1]:
+    blocks, shape = _offsets(offsets, out), out.shape
+    if len(shape) != 2 or w.rows != blocks * shape[1]:
         raise ValueError(f"out is [rows][outputs], and the weights' form has blocks * outputs rows, {w.rows} for {blocks} blocks")
-    n = out.shape[1]
+    n = shape[1]
     _fit_u32(blocks, n)
     ldy = _matrix(out, (x.rows, n), out, "out")
     if x.k != w.k:
         raise ValueError(f"x has {x.k} inputs, the weights {w.k}")
-    if x.codes.device != out.device or w.codes.device != out.device:
+    if x.device != w.device or w.device != out.get_device():
         raise ValueError("x, the weights and out are on different devices")
     _dense(bias, (blocks, n), torch.float32, out, "bias")
     layer = Linear4C(w.c, _ptr(offsets), blocks, x.rows, n, x.k, _dtype(out))

@@ -12,8 +12,8 @@
 // so that gain and shift are in registers, and so are its sums of dgain and dshift: x and dy are read once for all three gradients.
 //
 // The same inputs again and again: 65 536 rows of 1024 in 32 blocks, bfloat16, 52 us (5.2 TB/s), all gradients 91 (4.4 TB/s); 300 000 x 96 in 24,
-// float32, 38 (6.0 TB/s; 52 with other inputs every time); 4744 x 4033 in 7, bfloat16, 19, gradients 54: there are four rows a workgroup, and a
-// row's two meetings stand behind its loads; one row of 1024 3.0, a chain of latencies.
+// float32, 38 (6.0 TB/s; 52 with other inputs every time); 4744 x 4033 in 7, bfloat16, 20, gradients 45: there are four rows a workgroup, and a
+// row's two meetings stand behind its loads; one row of 1024 3.0, a chain of latencies.  Sums leave as vectors: 4 bytes a lane took 55.
 #include "grouped_kernels.h"
 
 namespace lmk {
@@ -341,9 +341,15 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
 #pragma unroll
                 for (u32 c = 0; c < C; ++c)
 #pragma unroll
-                    for (u32 e = 0; e < V; ++e) {
+                    for (u32 e = 0; e < V; e += 4) {
                         const u32 at = (c * G + lane) * V + e;
-                        if (at < r.k) to[q][at] = v[c][e];
+                        if (at + 4 <= r.k) {
+                            store_any(to[q] + at, f32x4{v[c][e], v[c][e + 1], v[c][e + 2], v[c][e + 3]});
+                        } else {
+#pragma unroll
+                            for (u32 i = 0; i < 3; ++i)
+                                if (at + i < r.k) to[q][at + i] = v[c][e + i];
+                        }
                     }
             } else {
                 // the rows that ran beside each other, added in their order
@@ -521,8 +527,9 @@ NormShape norm_shape(u32 k, u32 dtype, bool backward)
     return {0, 0};
 }
 
-// Rows of a run: whole turns of the rows that run beside each other.  Forward, eight workgroups a compute unit hide each other's loads.  Of the
-// gradients' runs as many as are held at once, and where that makes them short, fewer: a run's sums are written and read again (2 k floats), and
+// Rows of a run: whole turns of the rows that run beside each other.  Forward, eight workgroups a compute unit hide each other's loads (20 000 x 2000
+// in bfloat16, eight / four / two: 29 / 32 / 42 us); those of 1024 threads all run at once, two a compute unit or, of more than eight values a thread,
+// one (2889 x 4201 in bfloat16, eight / two / one: 25 / 21 / 24; 3000 x 12 000 48 / 37 / 33).  Of the gradients' runs as many as are held at once, and where that makes them short, fewer: a run's sums are written and read again (2 k floats), and
 // joined one after the other.  A turn of a wavefront's rows is two chains of exchanges, of a workgroup's rows two meetings.
 u32 norm_per(u32 rows, u32 blocks, u32 k, u32 dtype, bool backward)
 {
@@ -532,7 +539,7 @@ u32 norm_per(u32 rows, u32 blocks, u32 k, u32 dtype, bool backward)
         const u64 t = ((u64)rows + (u64)workgroups * at_once - 1) / ((u64)workgroups * at_once);
         return (u32)(t < 1 ? 1 : t);
     };
-    if (!backward) return turns_of(2048) * at_once;
+    if (!backward) return turns_of(s.g < 1024 ? 2048 : s.c * (dtype == LMK_GS_F32 ? 4 : 8) <= 8 ? 512 : 256) * at_once;
     // of rows longer than registers: the sums' workgroups fill the device four times, with 16 rows or more (all gradients of 4096 rows of 16 000 in
     // bfloat16 527 us; 937 with runs of two rows, a column a thread)
     if (s.g == 0) {

@@ -316,8 +316,9 @@ __global__ __launch_bounds__(S::kThreads, 2) void gated_wide_kernel(const GatedA
         // outputs and row of a lane after the exchange of eight_of
         const auto out_of = [&](u32 m) { return p0 / 2 + 16 * (m + (group & 1)) + 8 * (group >> 1); };
         const auto row_of = [&](u32 j) { return q0 + 16 * j + (at & 15); };
-        // dy, eight values a lane as results leave, kAhead of them on their way: number i is of outputs 2 (i / kQ) and rows i % kQ
-        constexpr u32 kAhead = 3;
+        // dy, eight values a lane as results leave, kAhead of them on their way: number i is of outputs 2 (i / kQ) and rows i % kQ.  More of them cost
+        // registers that the large tile has not (65 536 rows of 1024 -> 2048 in 32 blocks: three 764 us, one 717).
+        constexpr u32 kAhead = 1;
         u32x4 up[kAhead];
         const __bf16 *dy_tile = static_cast<const __bf16 *>(r.dy) + (u64)done.row0 * r.lddy + done.col0;
         const auto fetch = [&](u32 i) {

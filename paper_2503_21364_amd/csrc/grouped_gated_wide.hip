@@ -456,7 +456,7 @@ hipError_t wide_go(GatedArgs r, hipStream_t stream)
 {
     using S = Shape<TP, TQ, WP, WQ>;
     constexpr u32 lds = gated_lds<S, TP, WP>(), at_once = 8 * kUnits * S::kResident;
-    r.past = past_caches((u64)r.rows * r.n * (BACKWARD ? 4 : 2));
+    r.past = !BACKWARD && past_caches(r.out, r.ldo * 2, (u64)r.rows * r.n * 2);
     r.col_tiles = (r.n + TP / 2 - 1) / (TP / 2);
     r.tiles = (u32)((max_runs(r.rows, r.blocks, TQ) + 3) / 4 * 4 * r.col_tiles);
     auto kernel = gated_wide_kernel<S, TP, TQ, WP, ACROSS, ANY, BACKWARD>;

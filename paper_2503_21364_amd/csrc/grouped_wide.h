@@ -330,8 +330,13 @@ __device__ __forceinline__ u32 pack_bf16(float a, float b)
 }
 
 // Results of a launch that are more than the dies' caches hold together are stored past them: the operands stay there (y of 65 536 x 2048 from
-// operands in 4 bits: 215 us, so 198).  16 bytes at any address.
-inline bool past_caches(u64 bytes) { return bytes > 32u << 20; }
+// operands in 4 bits: 215 us, so 198).  Rows have to begin with whole lines: parts of one are not put together there (65 536 rows of 512 -> 1000 in
+// 4 bits: 61 us, through the caches 45).
+inline bool past_caches(const void *p, u64 row_bytes, u64 bytes)
+{
+    return bytes > 32u << 20 && row_bytes % 128 == 0 && reinterpret_cast<uintptr_t>(p) % 128 == 0;
+}
+// 16 bytes at any address
 template <bool PAST, class T, class V> __device__ __forceinline__ void store_vector(T *p, V v)
 {
     if constexpr (PAST) {

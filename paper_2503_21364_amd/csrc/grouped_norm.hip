@@ -187,6 +187,20 @@ template <class T, u32 G, u32 C> struct RowOf {
 
 constexpr u32 threads_of(u32 g) { return g > 256 ? g : 256; }
 
+// Rows on their way to a thread of the gradients: two in workgroups of 1024 in bfloat16, of which a compute unit has one (6000 x 8192: 87 us, one row
+// 97; in float32 the registers do not hold them)
+template <class T, u32 G> constexpr u32 kDeep = G == 1024 && sizeof(T) == 2 ? 2 : 1;
+// f(turn, turn % DEEP)
+template <u32 DEEP, class F> __device__ __forceinline__ void each_turn(u32 turns, F &&f)
+{
+    for (u32 t = 0; t < turns; t += DEEP) {
+        f(t, std::integral_constant<u32, 0>{});
+        if constexpr (DEEP == 2) {
+            if (t + 1 < turns) f(t + 1, std::integral_constant<u32, 1>{});
+        }
+    }
+}
+
 template <class T, u32 G, u32 C>
 __global__ __launch_bounds__(threads_of(G)) void norm_kernel(const NormArgs r)
 {
@@ -275,27 +289,28 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
     Row::weights(gain, r.gain ? r.gain + own : nullptr, r.k, lane, 1.0f);
     const float share = 1.0f / (float)r.k;
     u32 turn = 0;
-    Vec<T> next_x[C], next_dy[C];
+    Vec<T> next_x[kDeep<T, G>][C], next_dy[kDeep<T, G>][C];
     const u32 turns = (end - begin + kAtOnce - 1) / kAtOnce;
-    const auto request = [&](u32 t) {
+    const auto request = [&](u32 t, auto part) {
         u32 row = begin + t * kAtOnce + threadIdx.x / G;
         row = row < end ? row : end - 1;
-        Row::load(next_x, x + (u64)row * r.ldx, r.k, lane);
-        Row::load(next_dy, dy + (u64)row * r.lddy, r.k, lane);
+        Row::load(next_x[part], x + (u64)row * r.ldx, r.k, lane);
+        Row::load(next_dy[part], dy + (u64)row * r.lddy, r.k, lane);
     };
-    request(0);
-    for (u32 t = 0; t < turns; ++t) {
+#pragma unroll
+    for (u32 i = 0; i < kDeep<T, G>; ++i) request(i, i);
+    each_turn<kDeep<T, G>>(turns, [&](u32 t, auto part) {
         const u32 row = begin + t * kAtOnce + threadIdx.x / G;
         const bool there = row < end;
         float h[C][V], d[C][V];
         float sum[1] = {0.0f};
-        Row::use(h, next_x, r.k, lane);
-        Row::use(d, next_dy, r.k, lane);
+        Row::use(h, next_x[part], r.k, lane);
+        Row::use(d, next_dy[part], r.k, lane);
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
             for (u32 e = 0; e < V; ++e) sum[0] += h[c][e];
-        if (t + 1 < turns) request(t + 1);
+        if (t + kDeep<T, G> < turns) request(t + kDeep<T, G>, part);
         RowSums<G, 1>::of(sum, meet, turn);
         const float mean = sum[0] / (float)r.k;
         // squares, d, and d (x - m): the last two need no deviation yet
@@ -326,7 +341,7 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
                 d[c][e] = s * (g * gain[c][e] - level - h[c][e] * along);
             }
         if (there && out) Row::store(out + (u64)row * r.ldo, d, r.k, lane);
-    }
+    });
     if constexpr (SUMS) {
         const bool alone = run.end - run.begin <= r.per;
         RowSlices all;

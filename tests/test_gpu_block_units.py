@@ -317,3 +317,26 @@ def test_tiles_of_192_rows():
     B.grouped_linear_backward(a, v, off, ws, dx=out)
     _close(out, want, (few + 2) * U * mag, True, "dx")
     assert torch.equal(first, out)          # the same sums in the same order
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [4101, 8191, 8193, 16385, 20011])
+def test_norms_of_long_rows_in_place(k, dtype):
+    """Rows whose last vector begins in front of the one before it ends, results in the place of x and of dy, many rows a run."""
+    dt, half, rows, offsets = DT[dtype], dtype == "bf16", 600, [2, 2, 30, 597]
+    g = torch.Generator().manual_seed(k)
+    x0, dy0 = (torch.randn(rows, k, generator=g).to(dt).to(DEV) for _ in range(2))
+    gain, shift = torch.randn(3, k, generator=g).to(DEV), torch.randn(3, k, generator=g).to(DEV)
+    off = torch.tensor(offsets, dtype=torch.int32, device=DEV)
+    y = x0.clone()
+    B.grouped_norm(y, off, y, gain=gain, shift=shift)
+    _close(y, *N.forward(_np(x0), offsets, _np(gain), _np(shift)), half, "y")
+    want, bound = N.backward(_np(dy0), _np(x0), offsets, _np(gain))
+    ws = torch.empty(B.grouped_norm_backward_bytes(rows, 3, k, dt), dtype=torch.uint8, device=DEV)
+    for place in ("x", "dy"):
+        x, dy, dgain, dshift = x0.clone(), dy0.clone(), torch.full((3, k), 7.0, device=DEV), torch.full((3, k), 7.0, device=DEV)
+        dx = x if place == "x" else dy
+        B.grouped_norm_backward(dy, x, off, ws, gain=gain, dx=dx, dgain=dgain, dshift=dshift)
+        _close(dx, want[0], bound[0], half, "dx")
+        _close(dgain, want[1], bound[1], False, "dgain")
+        _close(dshift, want[2], bound[2], False, "dshift")

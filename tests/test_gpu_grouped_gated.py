@@ -278,3 +278,67 @@ def test_on_a_stream_and_in_a_graph(dtype, k, n, sizes):
         torch.cuda.synchronize()
         t.check_forward()
         t.check_backward()
+
+
+# ---- few rows: all gradients from those of both projections in 32 bits
+FEW = [([1], 1, 1), ([2], 3, 1), ([1], 2, 2), ([3, 0, 1], 3, 2), ([2, 1], 4, 2), ([0, 1, 0], 5, 2), ([1], 1, 300), ([1, 2], 300, 1), ([5, 0, 9, 16, 17], 65, 33),
+       ([1, 1], 259, 131), ([64], 66, 34), ([3] * 20, 129, 63), ([0] * 5 + [33], 600, 72), ([1] * 70, 12, 7), ([7, 12], 1030, 513), ([4] * 60, 257, 130),
+       ([0, 0, 300] + [0] * 30, 70, 66)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("in_major", [False, True])
+@pytest.mark.parametrize("sizes,k,n", FEW)
+def test_few_rows(sizes, k, n, in_major, dtype):
+    for pad, front, act in ((0, 0, "silu"), (3, 2, "gelu")):
+        t = Layer(sizes, k, n, dtype, in_major, pad=pad, front=front, behind=front, seed=k, act=act, wpad=pad)
+        t.forward()
+        t.check_forward()
+        t.backward()
+        t.check_backward()
+        first = [getattr(t, q).clone() for q in ("dx", "dw", "db")]
+        for which in (("dx",), ("dw",), ("db",), ("dx", "db"), ("dw", "db")):
+            for q in ("dx", "dw", "db"):
+                getattr(t, q).fill_(7.0)
+            t.ws.fill_(255)
+            t.backward(which)
+            t.check_backward(which)
+            for q, was in zip(("dx", "dw", "db"), first):
+                assert q not in which or torch.equal(getattr(t, q).nan_to_num(), was.nan_to_num())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("in_major", [False, True])
+def test_few_rows_that_are_not_finite_touch_no_other_and_no_other_block(in_major, dtype):
+    # widths that end inside the vectors: what is read twice, or behind the sums, must not be multiplied by what is not finite
+    t, clean = (Layer([5, 7, 0, 2], 67, 37, dtype, in_major, seed=6) for _ in range(2))
+    t.x[2] = float("nan")
+    t.dy[7, 36] = float("inf")
+    for q in (t, clean):
+        q.backward()
+    keep = torch.ones(t.rows, dtype=torch.bool, device=DEV)
+    keep[2] = keep[7] = False
+    assert torch.isnan(t.dx[2]).all() and not torch.isfinite(t.dx[7]).any() and torch.equal(t.dx[keep], clean.dx[keep])
+    assert torch.isnan(t.dw[0]).all() and torch.isnan(t.db[0]).all()
+    assert torch.equal(t.dw[2:], clean.dw[2:]) and torch.equal(t.db[2:], clean.db[2:])
+    dw, own = (q.dw[1].transpose(0, 1) if in_major else q.dw[1] for q in (t, clean))
+    touched = [36, 37 + 36]
+    rest = [o for o in range(2 * 37) if o not in touched]
+    assert torch.equal(dw[rest], own[rest]) and not torch.isfinite(dw[touched]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_rows_in_a_graph(dtype):
+    t = Layer([3, 0, 9, 1], 130, 70, dtype, seed=12)
+    t.backward()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        t.backward()
+    for i in range(3):
+        t.x.copy_(torch.randn(t.x.shape, generator=torch.Generator().manual_seed(i)))
+        for q in ("dx", "dw", "db", "ws"):
+            getattr(t, q).fill_(7 if q != "ws" else 1)
+        graph.replay()
+        torch.cuda.synchronize()
+        t.check_backward()

@@ -13,7 +13,8 @@
 //
 // The same inputs again and again: 65 536 rows of 1024 in 32 blocks, bfloat16, 52 us (5.2 TB/s), all gradients 91 (4.4 TB/s); 300 000 x 96 in 24,
 // float32, 38 (6.0 TB/s; 52 with other inputs every time); 4744 x 4033 in 7, bfloat16, 20, gradients 45: there are four rows a workgroup, and a
-// row's two meetings stand behind its loads; one row of 1024 3.0, a chain of latencies.  Sums leave as vectors: 4 bytes a lane took 55.
+// row's two meetings stand behind its loads; one row of 1024 3.0, a chain of latencies.  Sums leave as vectors: with 4 bytes a lane those gradients
+// took 55.
 #include "grouped_kernels.h"
 
 namespace lmk {
@@ -544,8 +545,9 @@ NormShape norm_shape(u32 k, u32 dtype, bool backward)
 
 // Rows of a run: whole turns of the rows that run beside each other.  Forward, eight workgroups a compute unit hide each other's loads (20 000 x 2000
 // in bfloat16, eight / four / two: 29 / 32 / 42 us); those of 1024 threads all run at once, two a compute unit or, of more than eight values a thread,
-// one (2889 x 4201 in bfloat16, eight / two / one: 25 / 21 / 24; 3000 x 12 000 48 / 37 / 33).  Of the gradients' runs as many as are held at once, and where that makes them short, fewer: a run's sums are written and read again (2 k floats), and
-// joined one after the other.  A turn of a wavefront's rows is two chains of exchanges, of a workgroup's rows two meetings.
+// one (2889 x 4201 in bfloat16, eight / two / one: 25 / 21 / 24; 3000 x 12 000 48 / 37 / 33).  Of the gradients' runs as many as are held at once,
+// and where that makes them short, fewer: a run's sums are written and read again (2 k floats), and joined one after the other.  A turn of a
+// wavefront's rows is two chains of exchanges, of a workgroup's rows two meetings.
 u32 norm_per(u32 rows, u32 blocks, u32 k, u32 dtype, bool backward)
 {
     const NormShape s = norm_shape(k, dtype, backward);
@@ -619,7 +621,8 @@ hipError_t norm_as(const NormArgs &r, hipStream_t stream)
     stats.out = nullptr;
     hipError_t e = rows_go(stats);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(long_norm_sums_kernel<T>, dim3(long_pieces(r.k, kF32 ? LMK_GS_F32 : LMK_GS_BF16) * (u32)max_runs(r.rows, r.blocks, r.per)), dim3(256), 0, stream, r);
+    const u32 pieces = long_pieces(r.k, kF32 ? LMK_GS_F32 : LMK_GS_BF16);
+    hipLaunchKernelGGL(long_norm_sums_kernel<T>, dim3(pieces * (u32)max_runs(r.rows, r.blocks, r.per)), dim3(256), 0, stream, r);
     e = hipGetLastError();
     return e == hipSuccess && r.out ? rows_go(r) : e;
 }

@@ -474,8 +474,8 @@ int32_t lmk_gs_grouped_norm_backward(const lmk_gs_norm *norm, const void *dy, ui
  * `layer` is a lmk_gs_linear whose matrices hold both projections, the gate's first: [2 n][k] with rows 0 .. n-1 of Wg and n .. 2n-1 of
  * Wu, or with in_major [k][2 n]; n is the outputs of y, 1 .. 32768, and ldw at least 2 n with in_major.  Sums and activation in 32 bits, one rounding to
  * dtype.  Rows of no block give zeros and enter no gradient. */
-#define LMK_GS_SILU 0u      /* a / (1 + e^-a); an a of -infinity gives NaN                              */
-#define LMK_GS_GELU 1u      /* a times the normal distribution at a; the same                           */
+#define LMK_GS_SILU 0u      /* a / (1 + e^-a), within (2 |a| + 8) 2^-24 of itself; an a of -infinity gives NaN */
+#define LMK_GS_GELU 1u      /* a times the normal distribution at a, within 13 2^-24 of itself as long as the latter is 2^-126 or more; the same */
 #define LMK_GS_RELU 2u      /* max(a, 0), a NaN stays one; the gradient of a is 0 where a <= 0           */
 
 /* bias: [blocks][2 n] float32, bg first, or NULL.  y must not overlap x or w.  Otherwise as lmk_gs_grouped_linear; another act is

@@ -4,8 +4,7 @@ Every result comes with a bound of what 32 bits may be off by (u = 2^-24):
   a and u, sums of k products: (k + 3) u times the sum of the magnitudes.
   The activation moves by at most 1.13 of what a moves (the steepest slope of the three), its slope by 0.8 of it.
   SiLU: e^-a as a power of two of a rounded product is off by (2 |a| + 2) u of itself, sum, reciprocal and product by 6 u more.
-  GELU: the normal distribution is off by 0.75e-7 (half of what its polynomial is published with) and 10 roundings, its density by
-  (a^2 + 4) u of itself, and |a|^3 times the density is below 0.5.
+  GELU: the normal distribution and its density are off by 12 u of themselves, each product or sum behind them by one more.
   ReLU: exact, but for the slope of an a that may as well be on the other side of 0.
 `half`: the roundings of both projections' gradients to bfloat16, 2^-8 of each, on their way into dx and dw."""
 from __future__ import annotations
@@ -34,7 +33,7 @@ def activation(a, act: str):
             p = 1 / (1 + np.exp(-a))
         return a * p, p * (1 + a * (1 - p)), size * p * (2 * size + 8) * U, (10 + 14 * size) * U
     p, d = normal(a), np.exp(-a * a / 2) / np.sqrt(2 * np.pi)
-    return a * p, p + a * d, size * (0.75e-7 + 10 * U), np.full_like(a, 0.75e-7 + 14 * U)
+    return a * p, p + a * d, size * p * 13 * U, (p + size * d) * 14 * U
 
 
 def _projections(x, w, bias, n: int):

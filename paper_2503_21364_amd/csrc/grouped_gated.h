@@ -32,17 +32,27 @@ __device__ __forceinline__ float logistic(float a)
 {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(a * -1.44269504f));
 }
-// The normal distribution at a, and its density.  Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), off by
-// 1.5e-7 at most for x >= 0; x = |a| / sqrt 2.
+// The normal distribution at a, and its density, each within 12 roundings of itself as long as it is 2^-126 or more; below that 0 for it.
+// erfc(x) e^(x^2) / 2 of x = |a| / sqrt 2 is t P(t), t = 1 / (1 + p x), P of degree 8 with the least largest relative deviation over x up to 9.6
+// (2.3e-8, by least squares with weights that grow where the deviation does).  -x^2 log2 e is taken in two parts: rounded once, the power of two of it
+// would be off by a^2 2^-24 of itself.  From |a| = 16 on both are as they are there.
 __device__ __forceinline__ float normal(float a, float &density)
 {
-    const float x = __builtin_fabsf(a) * 0.707106781f, e = __builtin_amdgcn_exp2f(a * a * -0.721347520f);
-    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
-    float s = 1.061405429f * t - 1.453152027f;
-    s = s * t + 1.421413741f;
-    s = s * t - 0.284496736f;
-    s = s * t + 0.254829592f;
-    const float tail = 0.5f * s * t * e;
+    const float x = __builtin_fminf(__builtin_fabsf(a), 16.0f), q = x * x, rest = __builtin_fmaf(x, x, -q);
+    constexpr float kHi = -0.72134752f, kLo = (float)(-0.72134752044448170368 - (double)kHi);          // -log2(e) / 2
+    const float y = q * kHi, low = __builtin_fmaf(rest, kHi, __builtin_fmaf(q, kLo, __builtin_fmaf(q, kHi, -y)));
+    float e = __builtin_amdgcn_exp2f(y);
+    e = __builtin_fmaf(e, low * 0.69314718f, e);
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.34648234f, x, 1.0f));
+    float s = __builtin_fmaf(-0.028645312f, t, 0.145065382f);
+    s = __builtin_fmaf(s, t, -0.266854078f);
+    s = __builtin_fmaf(s, t, 0.178982466f);
+    s = __builtin_fmaf(s, t, -0.0332354568f);
+    s = __builtin_fmaf(s, t, 0.109878853f);
+    s = __builtin_fmaf(s, t, 0.118032135f);
+    s = __builtin_fmaf(s, t, 0.138562888f);
+    s = __builtin_fmaf(s, t, 0.138213098f);
+    const float tail = s * t * e;
     density = e * 0.398942280f;
     return a < 0.0f ? tail : 1.0f - tail;
 }

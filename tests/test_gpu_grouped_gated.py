@@ -342,3 +342,28 @@ def test_few_rows_in_a_graph(dtype):
         graph.replay()
         torch.cuda.synchronize()
         t.check_backward()
+
+
+# rows, inputs and outputs of every kernel's own: few rows, small float32 matrices (both directions), the general one, bfloat16 tiles
+@pytest.mark.parametrize("dtype,rows,k,n", [("f32", 40, 16, 64), ("f32", 5000, 16, 48), ("f32", 5000, 16, 64), ("f32", 5000, 80, 80), ("bf16", 40, 16, 64),
+                                            ("bf16", 3000, 16, 64), ("bf16", 5000, 4, 64)])
+def test_gelu_keeps_its_digits_far_below_zero(dtype, rows, k, n):
+    # a from -0.4 to -12.8 by way of the bias, u = 1, both exact; the normal distribution goes down to 1e-37 there.  It and its density are off by 12
+    # roundings, a product with a, u or dy by one more each; a result in bfloat16 is rounded once more
+    t = Layer([rows], k, n, dtype, act="gelu", seed=21)
+    t.w.zero_()
+    t.dy.zero_()
+    t.dy[0] = 1.0                               # the bias' gradients are those of one row
+    t.b[0, :n] = -torch.linspace(0.4, 12.8, n).to(DEV)
+    t.b[0, n:] = 1.0
+    t.forward()
+    t.backward()
+    a, u24 = _np(t.b[0, :n]), 2.0 ** -24
+    p, d = G.normal(a), np.exp(-a * a / 2) / np.sqrt(2 * np.pi)
+    assert p.min() > 2.0 ** -125
+    y = _np(t.y)
+    assert (y == y[0]).all()
+    assert (np.abs(y[0] - a * p) <= np.abs(a * p) * (14 * u24 + (2.0 ** -8 if dtype == "bf16" else 0))).all()
+    db = _np(t.db[0])
+    assert (np.abs(db[n:] - a * p) <= np.abs(a * p) * 14 * u24).all()
+    assert (np.abs(db[:n] - (p + a * d)) <= (p + np.abs(a) * d) * 15 * u24).all()

@@ -433,8 +433,8 @@ int32_t lmk_gs_checkpoint8_unpack(const lmk_gs_checkpoint8 *kept, uint32_t rows,
 
 /* ---- Layer norm of the rows of blocks, each with gain and shift of its own, and its gradients.
  *   m = mean(x[r]), s = 1 / sqrt(mean((x[r] - m)^2) + eps), h = (x[r] - m) s, y[r] = gain[g] h + shift[g]
- * in 32 bits, one rounding to dtype.  Rows of no block give zeros and enter no gradient; a row that holds what is not finite gives
- * NaN and touches no other. */
+ * in 32 bits, one rounding to dtype.  Finite rows have finite m, s and h, however large their values are; in float32 the mean's rounding is taken out of
+ * x - m.  Rows of no block give zeros and enter no gradient; a row that holds what is not finite gives NaN and touches no other. */
 typedef struct lmk_gs_norm {
     const float *gain;        /* [blocks][k], or NULL: all 1                                    */
     const float *shift;       /* [blocks][k], or NULL: all 0; the gradients do not read it      */

@@ -5,7 +5,12 @@
 // Everything between the loads and the one rounding of y and dx is in 32 bits.  The squares are of x less the mean, not
 // mean(x^2) - m^2: rows far from zero keep their digits.
 //
-// The mean is a quotient: a row of one value gives its shift.
+// The mean is a quotient.  In float32 it is rounded, and so are the sums it is taken from: d = x - m is exact where x is far from zero, and what is
+// left of a mean in d is summed beside its squares and taken out of both, so that a row of any level has the digits of one of level zero, and a
+// row of one value gives its shift.  In bfloat16 sums of values that are alike are exact.
+//
+// Finite rows have finite statistics: sums are of 2^-16 of the values, of which there are no more than 2^16, d is of their halves, and where its
+// squares pass 2^128 all the same, of 2^-80.
 //
 // Bound by memory: a row is read once.  It stays in the registers of G lanes, C vectors of 16 bytes each, and what is summed
 // over it goes from lane to lane without LDS (G <= 64), or through LDS once a sum.  A workgroup has a run of rows of one block,
@@ -34,11 +39,31 @@ struct NormArgs {
     u64 ldo;
     float *dgain, *dshift;      // [blocks][k], either may be NULL
     float *part;                // sets of partial sums: k of dgain, then k of dshift
-    float *stats;               // rows longer than registers: mean and 1 / deviation of every row
+    f32x4 *stats;               // rows longer than registers: every row's scale, mean times it, off and rate
     u32 per;                    // rows of a run
 };
 
+// h = ((x scale - mean scale) - off) rate
+constexpr float kOfSum = 0x1p-16f, kHalf = 0.5f, kFar = 0x1p-80f;
+__device__ __forceinline__ float mean_of(float sum, u32 k) { return sum / ((float)k * kOfSum); }
+__device__ __forceinline__ bool held(float squares) { return squares < __builtin_inff(); }
+// Mean of the squares of d, less the square of d's mean, `off`.  Where that is all there is, a difference of roundings would be left: no
+// less than 2^-16 of it, beside which d - off is nothing.
+__device__ __forceinline__ float variance(float square, float off)
+{
+    return __builtin_fmaxf(__builtin_fmaf(-off, off, square), off * off * 0x1p-16f);
+}
+// 1 / deviation of d.  0: a row of one value, and nothing of eps is left at this scale; d is 0, too
+__device__ __forceinline__ float rate_of(float var, float eps, float scale)
+{
+    const float q = var + eps * scale * scale;
+    return q == 0.0f ? 0.0f : 1.0f / sqrtf(q);
+}
+// and of x
+__device__ __forceinline__ float rate_of_row(float rate, float eps, float scale) { return rate == 0.0f ? 1.0f / sqrtf(eps) : rate * scale; }
+
 template <class T> constexpr u32 kVec = 16 / sizeof(T);
+template <class T> constexpr bool kCentred = sizeof(T) == 4;           // off is taken
 template <class T> using Vec = T __attribute__((ext_vector_type(16 / sizeof(T))));
 
 // Sum over the G lanes of a row, the same bits in all of them: neighbours, pairs, quads and halves of 16 lanes, then rows of 16 and
@@ -82,9 +107,13 @@ template <u32 G, u32 N> struct RowSums {
             __syncthreads();
 #pragma unroll
             for (u32 i = 0; i < N; ++i) {
-                v[i] = 0.0f;
+                if constexpr (kWaves == 16) {           // a wavefront's a lane: sixteen reads would hold 64 registers
+                    v[i] = lanes_sum<16>(at[(threadIdx.x & 15) * 4 + i]);
+                } else {
+                    v[i] = 0.0f;
 #pragma unroll
-                for (u32 w = 0; w < kWaves; ++w) v[i] += at[w * 4 + i];
+                    for (u32 w = 0; w < kWaves; ++w) v[i] += at[w * 4 + i];
+                }
             }
         }
     }
@@ -188,8 +217,8 @@ template <class T, u32 G, u32 C> struct RowOf {
 
 constexpr u32 threads_of(u32 g) { return g > 256 ? g : 256; }
 
-// Rows on their way to a thread of the gradients: two in workgroups of 1024 in bfloat16, of which a compute unit has one (6000 x 8192: 87 us, one row
-// 97; in float32 the registers do not hold them)
+// Rows on their way to a thread of the gradients: two in workgroups of 1024 in bfloat16, of which a compute unit has one (6000 x 8192: 79 us, one row
+// 93; in float32 134 and 136)
 template <class T, u32 G> constexpr u32 kDeep = G == 1024 && sizeof(T) == 2 ? 2 : 1;
 // f(turn, turn % DEEP)
 template <u32 DEEP, class F> __device__ __forceinline__ void each_turn(u32 turns, F &&f)
@@ -241,32 +270,55 @@ __global__ __launch_bounds__(threads_of(G)) void norm_kernel(const NormArgs r)
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) sum[0] += v[c][e];
+            for (u32 e = 0; e < V; ++e) sum[0] = __builtin_fmaf(v[c][e], kOfSum, sum[0]);
         if (t + 1 < turns) Row::load(next, x + (u64)row_at(t + 1) * r.ldx, r.k, lane);
         RowSums<G, 1>::of(sum, meet, turn);
-        const float mean = sum[0] / (float)r.k;
-        sum[0] = 0.0f;
+        const float level = mean_of(sum[0], r.k) * kHalf;
+        constexpr u32 kSums = kCentred<T> ? 2 : 1;
+        float sums[kSums], scale = kHalf, off = 0.0f;
+        const auto square = [&] {
+#pragma unroll
+            for (u32 i = 0; i < kSums; ++i) sums[i] = 0.0f;
+#pragma unroll
+            for (u32 c = 0; c < C; ++c)
+#pragma unroll
+                for (u32 e = 0; e < V; ++e) {
+                    sums[0] += v[c][e] * v[c][e];
+                    if constexpr (kCentred<T>) sums[1] += v[c][e];
+                }
+            RowSums<G, kSums>::of(sums, meet, turn);
+            if constexpr (kCentred<T>) off = sums[1] * share;
+        };
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) {
-                v[c][e] -= mean;
-                if ((c * G + lane) * V + e < r.k) sum[0] += v[c][e] * v[c][e];
-            }
-        RowSums<G, 1>::of(sum, meet, turn);
-        const float s = 1.0f / sqrtf(sum[0] * share + r.eps);
+            for (u32 e = 0; e < V; ++e) v[c][e] = (c * G + lane) * V + e < r.k ? __builtin_fmaf(v[c][e], kHalf, -level) : 0.0f;
+        square();
+        if (!held(sums[0])) {                       // the same in all threads of the row
+#pragma unroll
+            for (u32 c = 0; c < C; ++c)
+#pragma unroll
+                for (u32 e = 0; e < V; ++e) v[c][e] *= kFar / kHalf;
+            scale = kFar;
+            square();
+        }
+        const float s = rate_of(variance(sums[0] * share, off), r.eps, scale);
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) v[c][e] = v[c][e] * s * gain[c][e] + shift[c][e];
+            for (u32 e = 0; e < V; ++e) v[c][e] = (v[c][e] - off) * s * gain[c][e] + shift[c][e];
         const u32 row = begin + t * kAtOnce + threadIdx.x / G;
         if (row < end) Row::store(out + (u64)row * r.ldo, v, r.k, lane);
     }
 }
 
+// Wavefronts of a SIMD that the registers have to leave: three where the compiler would end four registers above (65 536 rows of 1024 in float32, all
+// gradients: 171 us, of two 185)
+constexpr u32 norm_resident(u32 g, u32 c) { return g == 64 && c == 4 ? 3 : 1; }
+
 // SUMS: dgain and dshift, too
 template <class T, u32 G, u32 C, bool SUMS>
-__global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const NormArgs r)
+__global__ __launch_bounds__(threads_of(G), norm_resident(G, C)) void norm_backward_kernel(const NormArgs r)
 {
     using Row = RowOf<T, G, C>;
     constexpr u32 V = Row::V, kThreads = threads_of(G), kAtOnce = kThreads / G;
@@ -310,31 +362,50 @@ __global__ __launch_bounds__(threads_of(G)) void norm_backward_kernel(const Norm
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) sum[0] += h[c][e];
+            for (u32 e = 0; e < V; ++e) sum[0] = __builtin_fmaf(h[c][e], kOfSum, sum[0]);
         if (t + kDeep<T, G> < turns) request(t + kDeep<T, G>, part);
         RowSums<G, 1>::of(sum, meet, turn);
-        const float mean = sum[0] / (float)r.k;
+        const float mean = mean_of(sum[0], r.k) * kHalf;
         // squares, d, and d (x - m): the last two need no deviation yet
-        float sums[3] = {0.0f, 0.0f, 0.0f};
+        constexpr u32 kSums = kCentred<T> ? 4 : 3;
+        float sums[kSums], scale = kHalf, off = 0.0f;
+        const auto square = [&] {
+#pragma unroll
+            for (u32 i = 0; i < kSums; ++i) sums[i] = 0.0f;
+#pragma unroll
+            for (u32 c = 0; c < C; ++c)
+#pragma unroll
+                for (u32 e = 0; e < V; ++e) {
+                    const float w = d[c][e] * gain[c][e];
+                    sums[0] += h[c][e] * h[c][e];
+                    sums[1] += w;
+                    sums[2] += w * h[c][e];
+                    if constexpr (kCentred<T>) sums[3] += h[c][e];
+                }
+            RowSums<G, kSums>::of(sums, meet, turn);
+            if constexpr (kCentred<T>) off = sums[3] * share;
+        };
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
-            for (u32 e = 0; e < V; ++e) {
-                const bool on = (c * G + lane) * V + e < r.k;
-                h[c][e] = on ? h[c][e] - mean : 0.0f;
-                const float w = d[c][e] * gain[c][e];
-                sums[0] += h[c][e] * h[c][e];
-                sums[1] += w;
-                sums[2] += w * h[c][e];
-            }
-        RowSums<G, 3>::of(sums, meet, turn);
-        const float s = 1.0f / sqrtf(sums[0] * share + r.eps), level = sums[1] * share, along = sums[2] * share * s;
+            for (u32 e = 0; e < V; ++e) h[c][e] = (c * G + lane) * V + e < r.k ? __builtin_fmaf(h[c][e], kHalf, -mean) : 0.0f;
+        square();
+        if (!held(sums[0])) {                       // the same in all threads of the row
+#pragma unroll
+            for (u32 c = 0; c < C; ++c)
+#pragma unroll
+                for (u32 e = 0; e < V; ++e) h[c][e] *= kFar / kHalf;
+            scale = kFar;
+            square();
+        }
+        const float rate = rate_of(variance(sums[0] * share, off), r.eps, scale), s = rate_of_row(rate, r.eps, scale);
+        const float level = sums[1] * share, along = (sums[2] * share - off * level) * rate;
 #pragma unroll
         for (u32 c = 0; c < C; ++c)
 #pragma unroll
             for (u32 e = 0; e < V; ++e) {
                 const float g = d[c][e];
-                h[c][e] *= s;
+                h[c][e] = (h[c][e] - off) * rate;
                 if (SUMS && there) {
                     dgain[c][e] += g * h[c][e];
                     dshift[c][e] += g;
@@ -422,33 +493,41 @@ __global__ __launch_bounds__(kLong) void long_norm_kernel(const NormArgs r)
     each_vector<T>(threadIdx.x, kLong, r.k, [&](u32 from, u32 first) {
         const Vec<T> v = load_any<Vec<T>>(x + from);
 #pragma unroll
-        for (u32 e = 0; e < V; ++e) sum[0] += e >= first ? to_f32(v[e]) : 0.0f;
+        for (u32 e = 0; e < V; ++e) sum[0] = __builtin_fmaf(e >= first ? to_f32(v[e]) : 0.0f, kOfSum, sum[0]);
     });
     RowSums<kLong, 1>::of(sum, meet, turn);
-    const float mean = sum[0] / (float)r.k;
-    float sums[3] = {0.0f, 0.0f, 0.0f};
-    each_vector<T>(threadIdx.x, kLong, r.k, [&](u32 from, u32 first) {
-        const Vec<T> v = load_any<Vec<T>>(x + from);
-        Vec<T> g = {};
-        if (BACKWARD) g = load_any<Vec<T>>(dy + from);
+    const float mean = mean_of(sum[0], r.k);
+    float sums[4], scale = kHalf;
+    const auto square = [&] {
 #pragma unroll
-        for (u32 e = 0; e < V; ++e) {
-            if (e < first) continue;
-            const float h = to_f32(v[e]) - mean;
-            sums[0] += h * h;
-            if (BACKWARD) {
-                const float w = to_f32(g[e]) * (gain ? gain[from + e] : 1.0f);
-                sums[1] += w;
-                sums[2] += w * h;
+        for (u32 i = 0; i < 4; ++i) sums[i] = 0.0f;
+        each_vector<T>(threadIdx.x, kLong, r.k, [&](u32 from, u32 first) {
+            const Vec<T> v = load_any<Vec<T>>(x + from);
+            Vec<T> g = {};
+            if (BACKWARD) g = load_any<Vec<T>>(dy + from);
+#pragma unroll
+            for (u32 e = 0; e < V; ++e) {
+                if (e < first) continue;
+                const float h = __builtin_fmaf(to_f32(v[e]), scale, -(mean * scale));
+                sums[0] += h * h;
+                if (BACKWARD) {
+                    const float w = to_f32(g[e]) * (gain ? gain[from + e] : 1.0f);
+                    sums[1] += w;
+                    sums[2] += w * h;
+                }
+                if (kCentred<T>) sums[3] += h;
             }
-        }
-    });
-    RowSums<kLong, 3>::of(sums, meet, turn);
-    const float s = 1.0f / sqrtf(sums[0] * share + r.eps), level = sums[1] * share, along = sums[2] * share * s;
-    if (BACKWARD && r.stats && threadIdx.x == 0) {
-        r.stats[2 * (u64)row] = mean;
-        r.stats[2 * (u64)row + 1] = s;
+        });
+        RowSums<kLong, 4>::of(sums, meet, turn);
+    };
+    square();
+    if (!held(sums[0])) {                           // the same in all threads
+        scale = kFar;
+        square();
     }
+    const float off = sums[3] * share, rate = rate_of(variance(sums[0] * share, off), r.eps, scale), s = rate_of_row(rate, r.eps, scale);
+    const float level = sums[1] * share, along = (sums[2] * share - off * level) * rate;
+    if (BACKWARD && r.stats && threadIdx.x == 0) r.stats[row] = f32x4{scale, mean * scale, off, rate};
     if (!out) return;
     // out may be x or dy: what a vector holds in front of its first value may have its result already, and is not used
     each_vector<T>(threadIdx.x, kLong, r.k, [&](u32 from, u32 first) {
@@ -457,7 +536,7 @@ __global__ __launch_bounds__(kLong) void long_norm_kernel(const NormArgs r)
         if (BACKWARD) g = load_any<Vec<T>>(dy + from);
 #pragma unroll
         for (u32 e = 0; e < V; ++e) {
-            const float h = (to_f32(v[e]) - mean) * s, w = gain ? gain[from + e] : 1.0f;
+            const float h = (__builtin_fmaf(to_f32(v[e]), scale, -(mean * scale)) - off) * rate, w = gain ? gain[from + e] : 1.0f;
             o[e] = BACKWARD ? (T)(s * (to_f32(g[e]) * w - level - h * along)) : (T)(h * w + (shift ? shift[from + e] : 0.0f));
         }
         if (first == 0) {
@@ -485,14 +564,13 @@ __global__ __launch_bounds__(256) void long_norm_sums_kernel(const NormArgs r)
     float dgain[V] = {}, dshift[V] = {};
     for (u32 row0 = begin; row0 < end; row0 += kRows) {
         Vec<T> x[kRows], dy[kRows];
-        float mean[kRows], s[kRows];
+        f32x4 m[kRows];
 #pragma unroll
         for (u32 i = 0; i < kRows; ++i) {
             const u64 row = row0 + i < end ? row0 + i : row0;
             x[i] = load_any<Vec<T>>(static_cast<const T *>(r.x) + row * r.ldx + from);
             dy[i] = load_any<Vec<T>>(static_cast<const T *>(r.dy) + row * r.lddy + from);
-            mean[i] = r.stats[2 * row];
-            s[i] = r.stats[2 * row + 1];
+            m[i] = r.stats[row];
         }
 #pragma unroll
         for (u32 i = 0; i < kRows; ++i) {
@@ -500,7 +578,7 @@ __global__ __launch_bounds__(256) void long_norm_sums_kernel(const NormArgs r)
 #pragma unroll
             for (u32 e = 0; e < V; ++e) {
                 const float g = to_f32(dy[i][e]);
-                dgain[e] += g * ((to_f32(x[i][e]) - mean[i]) * s[i]);
+                dgain[e] += g * ((__builtin_fmaf(to_f32(x[i][e]), m[i][0], -m[i][1]) - m[i][2]) * m[i][3]);
                 dshift[e] += g;
             }
         }
@@ -558,7 +636,7 @@ u32 norm_per(u32 rows, u32 blocks, u32 k, u32 dtype, bool backward)
     };
     if (!backward) return turns_of(s.g < 1024 ? 2048 : s.c * (dtype == LMK_GS_F32 ? 4 : 8) <= 8 ? 512 : 256) * at_once;
     // of rows longer than registers: the sums' workgroups fill the device four times, with 16 rows or more (all gradients of 4096 rows of 16 000 in
-    // bfloat16 527 us; 937 with runs of two rows, a column a thread)
+    // bfloat16 466 us)
     if (s.g == 0) {
         const u32 runs = 1024 / long_pieces(k, dtype), per = turns_of(runs < 1 ? 1 : runs);
         return per < 16 ? 16 : per;
@@ -655,7 +733,7 @@ bool grouped_norm_fits(const lmk_gs_norm &n, bool backward, bool sums)
 
 size_t grouped_norm_backward_bytes(const lmk_gs_norm &n)
 {
-    return norm_sets_bytes(n) + (norm_shape(n.k, n.dtype, true).g == 0 ? (size_t)n.rows * 8 : 0);
+    return norm_sets_bytes(n) + (norm_shape(n.k, n.dtype, true).g == 0 ? (size_t)n.rows * sizeof(f32x4) : 0);
 }
 
 hipError_t launch_grouped_norm(const lmk_gs_norm &n, const void *x, u64 ldx, void *y, u64 ldy, hipStream_t stream)
@@ -672,7 +750,7 @@ hipError_t launch_grouped_norm_backward(const lmk_gs_norm &n, const void *dy, u6
     r.dgain = out.dgain; r.dshift = out.dshift;
     const bool sums = out.dgain || out.dshift;
     r.part = reinterpret_cast<float *>(workspace);
-    r.stats = sums ? reinterpret_cast<float *>(workspace + norm_sets_bytes(n)) : nullptr;
+    r.stats = sums ? reinterpret_cast<f32x4 *>(workspace + norm_sets_bytes(n)) : nullptr;
     if (n.rows > 0) {
         const hipError_t e = n.dtype == LMK_GS_F32 ? norm_as<float, true>(r, stream) : norm_as<__bf16, true>(r, stream);
         if (e != hipSuccess) return e;

@@ -11,6 +11,7 @@ pytestmark = pytest.mark.gpu
 
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 DEV = "cuda:0"
+U = 2.0 ** -24
 
 
 def _np(t):
@@ -220,3 +221,100 @@ def test_on_a_stream_and_in_a_graph(k):
         torch.cuda.synchronize()
         t.check_forward()
         t.check_backward()
+
+
+def _additions(k):
+    """On a value's way into a sum over a row: those of a thread, over a wavefront and over wavefronts."""
+    return min(k, max(16, (k + 1023) // 1024 + 3) + 6 + 4)
+
+
+# every arrangement of a row: over 8, 16, 64, 256 and 1024 lanes, and longer than registers
+FAR_WIDTHS = [1, 20, 96, 100, 500, 1000, 4000, 4100, 8190, 9000, 20_000]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", FAR_WIDTHS)
+def test_rows_of_one_value_give_their_shift(k, dtype):
+    # d = x - mean is the mean's error, (M + 2) u of the value at most; its own mean is off by (M + 2) u of it, the difference rounded once; 1 / deviation
+    # is 1 / sqrt(eps), or 2^8 / d, at most.  In bfloat16 sums of values that are alike are exact, and so is d
+    t = Case([6, 2], k, dtype, seed=31)
+    t.gain[1:].fill_(1.0)
+    t.shift[1:].fill_(0.0)
+    for i, v in enumerate((0.1, -1000.1, 1e6 + 0.5, 1e10, 3.3e38, -7.7e20, 0.0, 1e-30)):
+        t.x[i] = v
+    t.forward()
+    m, value = _additions(k) + 4, np.abs(_np(t.x[:, :1]))
+    h = 0.0 * value if dtype == "bf16" else np.minimum(m * m * U * U * value / 1e-5 ** 0.5, 2.0 ** 8 * m * U)
+    gain, shift = (_np(v)[[0] * 6 + [1] * 2] for v in (t.gain, t.shift))
+    assert (np.abs(_np(t.y) - shift) <= np.abs(gain) * h + (2 * U + (2.0 ** -8 if dtype == "bf16" else 0)) * (np.abs(shift) + np.abs(gain) * h)).all()
+    # the gradients: h is 0, 1 / deviation 1 / sqrt(eps), but for d's square: of the first two rows alone, whose d is small beside it
+    t.backward()
+    assert torch.isfinite(t.dx).all()
+    dy, dgain = _np(t.dy), _np(t.dgain)
+    assert (np.abs(dgain[0]) <= (np.abs(dy[:6]) * h[:6]).sum(0) * (1 + 20 * U)).all() and (np.abs(dgain[1]) <= (np.abs(dy[6:]) * h[6:]).sum(0) * (1 + 20 * U)).all()
+    d = dy[:2] * gain[:2]
+    want = (d - d.mean(1, keepdims=True)) / 1e-5 ** 0.5
+    near = (m * U * value[:2]) ** 2 * (2.0 ** -16 + 4 * m * U) / 1e-5 if dtype == "f32" else 0.0
+    off = np.abs(d).mean(1, keepdims=True)
+    tol = ((np.abs(d) + off) * (near + m * U + h[:2] ** 2) + off * h[:2] ** 2) / 1e-5 ** 0.5
+    assert (np.abs(_np(t.dx[:2]) - want) <= tol * 1.01 + (2.0 ** -8 * np.abs(want) if dtype == "bf16" else 0)).all()
+
+
+@pytest.mark.parametrize("k", FAR_WIDTHS[3:])
+def test_rows_far_from_zero_are_those_of_level_zero(k):
+    # level 2^20, spread 1, float32: d is exact, its mean `off` the mean's error, (M + 2) u 2^20 at most and itself off by (M + 2) u of what it is summed
+    # from; the mean of the squares is off by (M + 2) u of itself, which holds off^2, too
+    g = torch.Generator().manual_seed(32)
+    x = (2.0 ** 20 + torch.randn(40, k, generator=g)).to(DEV)
+    y, off = torch.empty_like(x), torch.tensor([0, 40], dtype=torch.int32, device=DEV)
+    B.grouped_norm(x, off, y)
+    want, _ = N.forward(_np(x), [0, 40])
+    m = _additions(k) + 4
+    e = m * U * 2.0 ** 20
+    tol = m * U * (1.2 + e) + np.abs(want) * (m * U * (1.2 + e * e) + 4 * U)
+    assert (np.abs(_np(y) - want) <= tol).all(), np.abs(_np(y) - want).max()
+    dy, dx, dgain = torch.randn(40, k, generator=g).to(DEV), torch.empty_like(x), torch.empty(1, k, device=DEV)
+    ws = torch.empty(B.grouped_norm_backward_bytes(40, 1, k), dtype=torch.uint8, device=DEV)
+    B.grouped_norm_backward(dy, x, off, ws, dx=dx, dgain=dgain)
+    d = _np(dy)
+    grads, _ = N.backward(d, _np(x), [0, 40])
+    assert (np.abs(_np(dgain)[0] - grads[1][0]) <= (np.abs(d) * tol).sum(0) + 42 * U * np.abs(d * want).sum(0)).all()
+    # s (dy - mean(dy) - h mean(dy h)): of the terms' magnitudes, 1.2 being more than 1 / deviation, the sum of w d has off times that of w beside it
+    size = np.abs(d) + np.abs(d).mean(1, keepdims=True) + np.abs(want) * np.abs(d * want).mean(1, keepdims=True)
+    along = (np.abs(d) * tol).mean(1, keepdims=True) + m * U * (np.abs(d * want).mean(1, keepdims=True) + 2.4 * e * np.abs(d).mean(1, keepdims=True))
+    spread = m * U * (1.2 + e * e) + 8 * U
+    assert (np.abs(_np(dx) - grads[0]) <= 1.2 * (size * (spread + m * U) + np.abs(want) * along + tol * np.abs(d * want).mean(1, keepdims=True))).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", FAR_WIDTHS[1:])
+def test_rows_of_large_values_keep_theirs(k, dtype):
+    # squares, sums and differences that pass 2^128, in blocks with ordinary rows
+    t = Case([9, 3], k, dtype, pad=3, seed=33)
+    sign = torch.where(torch.arange(k) % 2 == 0, 1.0, -1.0).to(DEV)
+    for i, v in ((1, 1e18), (2, 3e19), (4, 1e25), (5, 1e30), (7, 1e37)):
+        t.x[i] *= v
+    t.x[8] = 3.3e38 * sign
+    t.x[9] = 3.3e38
+    t.x[9, 0] = -3.3e38
+    t.x[10] = 2.0 ** 100 * (1 + 2.0 ** -7 * (torch.arange(k) % 3).to(DEV))
+    t.forward()
+    t.check_forward()
+    assert (t.y[8] != t.shift[0].to(t.y.dtype)).any() and torch.isfinite(t.y).all()
+    t.backward()
+    t.check_backward()
+    assert torch.isfinite(t.dx).all() and torch.isfinite(t.dgain).all()
+
+
+@pytest.mark.parametrize("k", [96, 1000, 20_000])
+def test_rows_of_large_values_in_place(k):
+    t = Case([5, 80], k, "f32", seed=34)
+    t.x[3] *= 1e30
+    t.x[70:] *= 1e22
+    x, dy = _np(t.x), _np(t.dy)
+    t.dx = t.dy
+    t.backward()
+    t.check_backward(inputs=(dy, x))
+    t.y = t.x
+    t.forward()
+    _close(t.y, *N.forward(x, t.offsets, _np(t.gain), _np(t.shift)), "f32", "y in the place of x")

@@ -348,6 +348,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void gated_wide_kernel(const GatedA
         __bf16 *out = static_cast<__bf16 *>(r.out) + (u64)done.row0 * r.ldo + done.col0;
         const auto finish = [&](auto act, auto all) {
             constexpr bool kEight = !ANY || all, kPast = !BACKWARD && all;
+            if constexpr (!ANY && all) stores_begin<kStores>();
 #pragma unroll
             for (u32 m = 0; m < 2 * kPairs; m += 2) {
                 float sum[2][2][4] = {};                            // [of m, m + 1][projection]
@@ -402,6 +403,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void gated_wide_kernel(const GatedA
                             }
                 }
             }
+            if constexpr (!ANY && all) stores_end();
         };
         // Tiles of which everything is there, and the others.  The gradients are read again at once, and not stored past the caches.  (A third form
         // of y's, for whole tiles that go through the caches, costs the others 3 %: 414 us, with it 423.)

@@ -289,6 +289,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear
         // `all`: every result of the tile is there; `past`: past the caches
         const u32 at = afresh(lane), group = at >> 4;               // where its results go is not held through the product
         const auto store = [&](auto all, auto past) {
+            if constexpr (all) stores_begin<kStores>();
 #pragma unroll
             for (u32 j = 0; j < S::kQ; ++j) {
                 if constexpr (sizeof(T) == 2) {
@@ -338,6 +339,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_rows4_kernel(const Linear
                     }
                 }
             }
+            if constexpr (all) stores_end();
         };
         counted = done.height == TQ && done.width == TP;
         if (sizeof(T) == 2 && counted && r.past) store(std::true_type{}, std::bool_constant<sizeof(T) == 2>{});

@@ -321,6 +321,11 @@ __device__ __forceinline__ void wide_product(P &p, Q &q, u32 steps, lds_char *ld
     __builtin_amdgcn_s_waitcnt(0x070);
 }
 
+// Around the stores of a whole tile, of which the next tile's first wait counts N behind its loads: a remark in the compiler's output, where a test
+// counts those that every lane reaches.  Fewer would end that wait before the loads are there.
+template <u32 N> __device__ __forceinline__ void stores_begin() { asm volatile("; %0 stores begin" : : "n"(N) : "memory"); }
+__device__ __forceinline__ void stores_end() { asm volatile("; stores end" : : : "memory"); }
+
 // one conversion instruction
 __device__ __forceinline__ u32 pack_bf16(float a, float b)
 {

@@ -129,3 +129,51 @@ def test_all_runs_of_a_product_of_small_matrices_are_held_at_once(narrow_rows, t
         least = {3: 4, 4: 37, 8: 65}[pieces]                              # sums of the kernel's smallest size
         assert r["Occupancy [waves/SIMD]"] >= min(4, _workgroups(_narrow_lds(16 * tiles, least))), (tiles, pieces, gate)
         assert r["VGPRs Spill"] == 0 and r["ScratchSize [bytes/lane]"] == 0
+
+
+# ---- the counted wait of kernels whose workgroups take tiles one after the other: no more than N accesses to memory may be left, where N stores stand
+# behind the loads that are waited for
+def stores_between_marks(assembly):
+    """(kernel, N, stores between the marks that no branch can pass by), of every place where a whole tile is stored."""
+    found, lines, kernel, i = [], assembly.splitlines(), None, 0
+    while i < len(lines):
+        label = re.match(r"(_Z\S+):", lines[i])
+        kernel = label.group(1) if label else kernel
+        mark = re.search(r"; (\d+) stores begin", lines[i])
+        i += 1
+        if not mark:
+            continue
+        count, past = 0, None                   # past: the label up to which a branch leads
+        while "stores end" not in lines[i]:
+            line = lines[i].split(";")[0].strip()
+            assert not line.startswith(("s_endpgm", "flat_", "s_branch", "s_setpc")) and "stores begin" not in lines[i], (kernel, line)
+            if line == f"{past}:":
+                past = None
+            elif line.startswith("s_cbranch"):
+                past = past or line.split()[-1]
+            elif past is None and line.startswith(("global_store_dwordx4", "buffer_store_dwordx4")):
+                count += 1
+            i += 1
+        assert past is None, (kernel, past)
+        found.append((kernel, int(mark.group(1)), count))
+    return found
+
+
+@pytest.mark.parametrize("unit,places", [("grouped_linear4.hip", 6), ("grouped_gated_wide.hip", 24)])
+def test_as_many_stores_as_the_next_tile_counts(unit, places, tmp_path):
+    # places: the tiles' sizes by the types, past the caches or not; by both layouts, both directions and three activations
+    out = str(tmp_path / "unit.s")
+    subprocess.run([hip_build.hipcc(), *hip_build.COMMON, *hip_build.UNITS[unit], "--cuda-device-only", "-S", os.path.join(hip_build.CSRC, unit), "-o", out],
+                   check=True, capture_output=True)
+    with open(out) as f:
+        found = stores_between_marks(f.read())
+    assert len(found) == places
+    assert all(count >= n for _, n, count in found), found
+
+
+def test_a_store_that_a_branch_passes_by_is_not_counted():
+    store = "\tglobal_store_dwordx4 v[0:1], v[2:5], off nt"
+    skipped = ["\ts_cbranch_execz .LBB0_2", store, ".LBB0_2:    ; %x"]
+    for lines, count in (([store, store], 2), ([store, *skipped, store], 2), (skipped, 0), (["\tglobal_load_dwordx4 v[0:3], v[4:5], off"], 0)):
+        text = "\n".join(["_ZN3lmk1kE:", "\t; 2 stores begin", *lines, "\t; stores end"])
+        assert stores_between_marks(text) == [("_ZN3lmk1kE", 2, count)]

@@ -528,11 +528,15 @@ DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 OFFSET_TYPES = torch.int32, torch.uint32
 
 
-def _dtype(t) -> int:
-    code = DTYPES.get(t.dtype)
+def _code(dtype) -> int:
+    code = DTYPES.get(dtype)
     if code is None:
-        raise ValueError(f"float32 or bfloat16 is expected, got {t.dtype}")
+        raise ValueError(f"float32 or bfloat16 is expected, got {dtype}")
     return code
+
+
+def _dtype(t) -> int:
+    return _code(t.dtype)
 
 
 def _matrix(t, shape, like, name):
@@ -622,7 +626,7 @@ def grouped_linear_backward_bytes(rows: int, blocks: int, n: int, k: int, dtype=
     """Workspace of grouped_linear_backward in bytes."""
     out = C.c_size_t(0)
     _fit_u32(rows, blocks, n, k)
-    layer = LinearC(256, 256, max(n, k), max(n, k) ** 2, blocks, rows, n, k, DTYPES[dtype], 0)
+    layer = LinearC(256, 256, max(n, k), max(n, k) ** 2, blocks, rows, n, k, _code(dtype), 0)
     rc = lib().lmk_gs_grouped_linear_backward_bytes(C.byref(layer), C.byref(out))
     if rc != OK:
         raise LmkGsError(rc, "lmk_gs_grouped_linear_backward_bytes")
@@ -736,7 +740,7 @@ def grouped_norm_backward_bytes(rows: int, blocks: int, k: int, dtype=torch.floa
     """Workspace of grouped_norm_backward in bytes."""
     out = C.c_size_t(0)
     _fit_u32(rows, blocks, k)
-    norm = NormC(None, None, 256, blocks, rows, k, DTYPES[dtype], 1.0)
+    norm = NormC(None, None, 256, blocks, rows, k, _code(dtype), 1.0)
     rc = lib().lmk_gs_grouped_norm_backward_bytes(C.byref(norm), C.byref(out))
     if rc != OK:
         raise LmkGsError(rc, "lmk_gs_grouped_norm_backward_bytes")
@@ -793,7 +797,7 @@ def grouped_gated_backward_bytes(rows: int, blocks: int, n: int, k: int, dtype=t
     """Workspace of grouped_gated_backward in bytes; n: outputs."""
     out = C.c_size_t(0)
     _fit_u32(rows, blocks, 2 * n, k)
-    layer = LinearC(256, 256, max(2 * n, k), max(2 * n, k) ** 2, blocks, rows, n, k, DTYPES[dtype], 0)
+    layer = LinearC(256, 256, max(2 * n, k), max(2 * n, k) ** 2, blocks, rows, n, k, _code(dtype), 0)
     rc = lib().lmk_gs_grouped_gated_backward_bytes(C.byref(layer), C.byref(out))
     if rc != OK:
         raise LmkGsError(rc, "lmk_gs_grouped_gated_backward_bytes")

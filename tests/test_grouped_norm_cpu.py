@@ -147,3 +147,12 @@ def test_tensors_of_another_device_than_the_current_one_are_refused(monkeypatch)
 
     with pytest.raises(ValueError, match="stream"):
         B._stream_on(Somewhere(), Other())
+
+
+@pytest.mark.parametrize("bytes_of", [lambda t: B.grouped_linear_backward_bytes(10, 2, 8, 8, t), lambda t: B.grouped_norm_backward_bytes(10, 2, 8, t),
+                                      lambda t: B.grouped_gated_backward_bytes(10, 2, 8, 8, t)])
+def test_a_workspace_of_another_type_is_refused_as_the_calls_refuse_it(bytes_of):
+    assert bytes_of(torch.float32) > 0 and bytes_of(torch.bfloat16) > 0
+    for dtype in (torch.float16, torch.float64, None):
+        with pytest.raises(ValueError, match="float32 or bfloat16"):
+            bytes_of(dtype)

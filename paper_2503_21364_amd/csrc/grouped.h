@@ -37,6 +37,33 @@ __device__ __forceinline__ void store4(__bf16 *p, f32x4 v)
     store_any(p, bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]});
 }
 
+// Values moved down by d places, zeros behind them; as many places as there are and more: zeros
+__device__ __forceinline__ f32x4 moved(f32x4 v, u32 d)
+{
+    if (d == 0) return v;
+    return f32x4{d == 1 ? v[1] : d == 2 ? v[2] : d == 3 ? v[3] : 0.0f, d == 1 ? v[2] : d == 2 ? v[3] : 0.0f, d == 1 ? v[3] : 0.0f, 0.0f};
+}
+__device__ __forceinline__ bf16x4 moved(bf16x4 v, u32 d)
+{
+    return __builtin_bit_cast(bf16x4, d < 4 ? __builtin_bit_cast(u64, v) >> (16 * d) : (u64)0);
+}
+__device__ __forceinline__ bf16x8 moved(bf16x8 v, u32 d)
+{
+    typedef __attribute__((ext_vector_type(2))) u64 u64x2;
+    const u64x2 b = __builtin_bit_cast(u64x2, v);
+    u64 lo = b[0], hi = b[1];
+    if (d >= 8) {
+        lo = hi = 0;
+    } else if (d >= 4) {
+        lo = hi >> (16 * (d - 4));
+        hi = 0;
+    } else if (d > 0) {
+        lo = lo >> (16 * d) | hi << (64 - 16 * d);
+        hi >>= 16 * d;
+    }
+    return __builtin_bit_cast(bf16x8, u64x2{lo, hi});
+}
+
 // The rows a workgroup works on: run `local` of `per` rows of the rows begin..end of a block.
 struct RowRun {
     u32 block, begin, end, local;            // block == ~0u: rows of no block

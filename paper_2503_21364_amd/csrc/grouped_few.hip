@@ -16,8 +16,8 @@ namespace {
 constexpr u32 kRows = 16;
 
 // GATE: 0 none, 1 values, 2 codes
-template <class T, u32 NT, bool ACROSS, bool WHOLE, u32 GATE>
-__global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const RowsArgs r)
+template <class T, u32 NT, bool ACROSS, Ends ENDS, u32 GATE>
+__global__ __launch_bounds__(512, ENDS == Ends::whole ? 6 : 4) void few_rows_kernel(const RowsArgs r)
 {
     constexpr u32 kWaves = 8, kC = NT / 16, V = ACROSS ? 4 : 16 / sizeof(T), kAhead = NT == 64 ? 2 : 4;
     __shared__ float part[kWaves][kRows][NT + 1];
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const Rows
     const u32 row0 = run.begin + run.local * kRows;
     const u32 height = run.end - row0 < kRows ? run.end - row0 : kRows;
     const u32 width = r.cols - col0 < NT ? r.cols - col0 : NT;
-    const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 15, q = lane >> 4;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), j = lane & 15, q = lane >> 4;
     const bool inside = run.block != ~0u;
     if (inside) {
         f32x4 acc[kC] = {};
@@ -39,23 +39,42 @@ __global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const Rows
         const u32 first = wave * per, last = first + per < all ? first + per : all;
         Run<T, V> fx[kAhead];
         Run<T, V> along[kAhead][kC];                    // weights: V sum indices of a column,
-        Run<T, kC> across[kAhead][V];                   // or kC columns of a sum index
+        Run<T, kC> across[kAhead][V];                   // or kC columns of a sum index: the last ones of the row where fewer are left
+        const u32 own = kC * j < width ? kC * j : 0u, left = r.cols - col0;
+        const int col = ENDS == Ends::any && own + kC > left ? (int)left - (int)kC : (int)own;
         for (u32 t0 = first; t0 < last; t0 += kAhead) {
 #pragma unroll
             for (u32 a = 0; a < kAhead; ++a) {
                 const u32 s = (t0 + a) * step + q * V;
                 const bool on = t0 + a < last;
-                fx[a] = load_run<T, V, WHOLE>(x, s, on ? r.sums : 0u);
-                if constexpr (ACROSS) {
+                if (ENDS == Ends::any && !on) break;            // the same in all lanes
+                const u32 sums = on ? r.sums : 0u;
+                fx[a] = load_run<T, V, ENDS>(x, s, sums);
+                if constexpr (ACROSS && ENDS == Ends::any) {
 #pragma unroll
-                    for (u32 e = 0; e < V; ++e)
-                        across[a][e] = load_run<T, kC, WHOLE>(w + (u64)(s + e) * r.ldw + col0, kC * j, on && s + e < r.sums ? width : 0u);
+                    for (u32 e = 0; e < V; ++e) across[a][e] = load_any<Run<T, kC>>(w + (u64)(s + e < sums ? s + e : sums - 1) * r.ldw + col0 + col);
+                } else if constexpr (ACROSS) {
+#pragma unroll
+                    for (u32 e = 0; e < V; ++e) across[a][e] = load_run<T, kC, ENDS>(w + (u64)(s + e) * r.ldw + col0, kC * j, s + e < sums ? width : 0u);
                 } else {
 #pragma unroll
                     for (u32 c = 0; c < kC; ++c) {
                         const u32 n = 16 * c + j;
-                        along[a][c] = load_run<T, V, WHOLE>(w + (u64)(col0 + (n < width ? n : 0)) * r.ldw, s, on ? r.sums : 0u);
+                        along[a][c] = load_run<T, V, ENDS>(w + (u64)(col0 + (n < width ? n : 0)) * r.ldw, s, sums);
                     }
+                }
+            }
+            if (ENDS == Ends::any && (t0 + kAhead > last || (t0 + kAhead) * step > r.sums)) {
+#pragma unroll
+                for (u32 a = 0; a < kAhead; ++a) {
+                    const u32 s = t0 + a < last ? (t0 + a) * step + q * V : r.sums;
+                    in_place<T, V>(fx[a], s, r.sums);
+#pragma unroll
+                    for (u32 c = 0; c < kC; ++c)
+                        if constexpr (!ACROSS) in_place<T, V>(along[a][c], s, r.sums);
+#pragma unroll
+                    for (u32 e = 0; e < V; ++e)
+                        if (ACROSS && s + e >= r.sums) across[a][e] = Run<T, kC>{};
                 }
             }
 #pragma unroll
@@ -70,7 +89,11 @@ __global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const Rows
 #pragma unroll
         for (u32 c = 0; c < kC; ++c)
 #pragma unroll
-            for (u32 v = 0; v < 4; ++v) part[wave][4 * q + v][ACROSS ? kC * j + c : 16 * c + j] = acc[c][v];
+            for (u32 v = 0; v < 4; ++v) {
+                // columns in front of the tile are another one's
+                const int at = !ACROSS ? (int)(16 * c + j) : ENDS == Ends::any ? col + (int)c : (int)(kC * j + c);
+                if (!ACROSS || ENDS != Ends::any || (at >= 0 && kC * j < width)) part[wave][4 * q + v][at] = acc[c][v];
+            }
     }
     __syncthreads();
     for (u32 i = threadIdx.x; i < kRows * NT; i += 512) {
@@ -90,12 +113,12 @@ __global__ __launch_bounds__(512, WHOLE ? 6 : 4) void few_rows_kernel(const Rows
     }
 }
 
-template <class T, u32 NT, bool ACROSS, bool WHOLE, u32 GATE>
+template <class T, u32 NT, bool ACROSS, Ends ENDS, u32 GATE>
 hipError_t few_go(RowsArgs r, hipStream_t stream)
 {
     r.col_tiles = (r.cols + NT - 1) / NT;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, kRows) * r.col_tiles);
-    hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, WHOLE, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
+    hipLaunchKernelGGL((few_rows_kernel<T, NT, ACROSS, ENDS, GATE>), dim3(r.tiles), dim3(512), 0, stream, r);
     return hipGetLastError();
 }
 // Columns of a workgroup.  64 make whole lines where columns are contiguous (8 blocks of 1024 x 1024 in bfloat16, 128 rows, 64 / 16
@@ -109,10 +132,16 @@ template <class T, bool ACROSS, u32 GATE>
 hipError_t few_width(const RowsArgs &r, hipStream_t stream)
 {
     constexpr u32 v = ACROSS ? 4 : 16 / sizeof(T);          // a run of x, and of the weights
-    const bool whole = r.sums % v == 0 && (!ACROSS || r.cols % v == 0);
-    if (few_columns(r, ACROSS) == 64)
-        return whole ? few_go<T, 64, ACROSS, true, GATE>(r, stream) : few_go<T, 64, ACROSS, false, GATE>(r, stream);
-    return whole ? few_go<T, 16, ACROSS, true, GATE>(r, stream) : few_go<T, 16, ACROSS, false, GATE>(r, stream);
+    const bool wide = few_columns(r, ACROSS) == 64;
+    const Ends sums = ends_of(r.sums, v), cols = ACROSS && wide ? ends_of(r.cols, 4) : Ends::whole;
+    // value by value where a row is a few vectors of four, and so many columns share a line (408 rows of 76 blocks -> 1715 in float32, 15 inputs: 10.8 us,
+    // by vectors 12.9; 47: 15.1 and 15.2; 61: 16.6 and 15.6; 200 rows of 20 in bfloat16, eight to a vector, 15 inputs: 8.5 and 7.8)
+    const bool single = sizeof(T) == 4 && !ACROSS && sums == Ends::any && r.sums < 48;
+    if (single || sums == Ends::early || cols == Ends::early)
+        return wide ? few_go<T, 64, ACROSS, Ends::early, GATE>(r, stream) : few_go<T, 16, ACROSS, Ends::early, GATE>(r, stream);
+    if (sums == Ends::any || cols == Ends::any)
+        return wide ? few_go<T, 64, ACROSS, Ends::any, GATE>(r, stream) : few_go<T, 16, ACROSS, Ends::any, GATE>(r, stream);
+    return wide ? few_go<T, 64, ACROSS, Ends::whole, GATE>(r, stream) : few_go<T, 16, ACROSS, Ends::whole, GATE>(r, stream);
 }
 template <class T>
 hipError_t few_as(const RowsArgs &r, bool across, hipStream_t stream)

@@ -13,7 +13,7 @@ namespace {
 constexpr u32 kRows = kGatedFewRows;
 
 // BACKWARD: the gradients of both projections instead of y
-template <class T, u32 NT, bool ACROSS, bool WHOLE, bool BACKWARD>
+template <class T, u32 NT, bool ACROSS, Ends ENDS, bool BACKWARD>
 __global__ __launch_bounds__(512, 4) void gated_few_kernel(const GatedArgs r)
 {
     constexpr u32 kWaves = 8, kC = NT / 16, V = ACROSS ? 4 : 16 / sizeof(T), kAhead = NT == 32 ? 2 : 4;
@@ -24,7 +24,7 @@ __global__ __launch_bounds__(512, 4) void gated_few_kernel(const GatedArgs r)
     const u32 row0 = run.begin + run.local * kRows;
     const u32 height = run.end - row0 < kRows ? run.end - row0 : kRows;
     const u32 width = r.n - col0 < NT ? r.n - col0 : NT;
-    const u32 lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, j = lane & 15, q = lane >> 4;
+    const u32 lane = threadIdx.x & (kWave - 1), wave = uniform(threadIdx.x / kWave), j = lane & 15, q = lane >> 4;
     const bool inside = run.block != ~0u;
     if (inside) {
         f32x4 acc[2][kC] = {};
@@ -36,25 +36,49 @@ __global__ __launch_bounds__(512, 4) void gated_few_kernel(const GatedArgs r)
         const u32 first = wave * per, last = first + per < all ? first + per : all;
         Run<T, V> fx[kAhead];
         Run<T, V> along[kAhead][2][kC];                 // weights: V sum indices of a column,
-        Run<T, kC> across[kAhead][2][V];                // or kC columns of a sum index
+        Run<T, kC> across[kAhead][2][V];                // or kC columns of a sum index: the last ones of the row where fewer are left
+        const u32 own = kC * j < width ? kC * j : 0u, left = r.n - col0;
+        const int col = ENDS == Ends::any && own + kC > left ? (int)left - (int)kC : (int)own;
         for (u32 t0 = first; t0 < last; t0 += kAhead) {
 #pragma unroll
             for (u32 a = 0; a < kAhead; ++a) {
                 const u32 s = (t0 + a) * step + q * V;
                 const bool on = t0 + a < last;
-                fx[a] = load_run<T, V, WHOLE>(x, s, on ? r.k : 0u);
+                if (ENDS == Ends::any && !on) break;            // the same in all lanes
+                const u32 sums = on ? r.k : 0u;
+                fx[a] = load_run<T, V, ENDS>(x, s, sums);
 #pragma unroll
                 for (u32 h = 0; h < 2; ++h) {
-                    if constexpr (ACROSS) {
+                    if constexpr (ACROSS && ENDS == Ends::any) {
 #pragma unroll
                         for (u32 e = 0; e < V; ++e)
-                            across[a][h][e] = load_run<T, kC, WHOLE>(w + (u64)(s + e) * r.ldw + h * r.n + col0, kC * j, on && s + e < r.k ? width : 0u);
+                            across[a][h][e] = load_any<Run<T, kC>>(w + (u64)(s + e < sums ? s + e : sums - 1) * r.ldw + h * r.n + col0 + col);
+                    } else if constexpr (ACROSS) {
+#pragma unroll
+                        for (u32 e = 0; e < V; ++e)
+                            across[a][h][e] = load_run<T, kC, ENDS>(w + (u64)(s + e) * r.ldw + h * r.n + col0, kC * j, s + e < sums ? width : 0u);
                     } else {
 #pragma unroll
                         for (u32 c = 0; c < kC; ++c) {
                             const u32 n = 16 * c + j;
-                            along[a][h][c] = load_run<T, V, WHOLE>(w + (u64)(h * r.n + col0 + (n < width ? n : 0)) * r.ldw, s, on ? r.k : 0u);
+                            along[a][h][c] = load_run<T, V, ENDS>(w + (u64)(h * r.n + col0 + (n < width ? n : 0)) * r.ldw, s, sums);
                         }
+                    }
+                }
+            }
+            if (ENDS == Ends::any && (t0 + kAhead > last || (t0 + kAhead) * step > r.k)) {
+#pragma unroll
+                for (u32 a = 0; a < kAhead; ++a) {
+                    const u32 s = t0 + a < last ? (t0 + a) * step + q * V : r.k;
+                    in_place<T, V>(fx[a], s, r.k);
+#pragma unroll
+                    for (u32 h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (u32 c = 0; c < kC; ++c)
+                            if constexpr (!ACROSS) in_place<T, V>(along[a][h][c], s, r.k);
+#pragma unroll
+                        for (u32 e = 0; e < V; ++e)
+                            if (ACROSS && s + e >= r.k) across[a][h][e] = Run<T, kC>{};
                     }
                 }
             }
@@ -75,7 +99,11 @@ __global__ __launch_bounds__(512, 4) void gated_few_kernel(const GatedArgs r)
 #pragma unroll
             for (u32 c = 0; c < kC; ++c)
 #pragma unroll
-                for (u32 v = 0; v < 4; ++v) part[wave][4 * q + v][h * NT + (ACROSS ? kC * j + c : 16 * c + j)] = acc[h][c][v];
+                for (u32 v = 0; v < 4; ++v) {
+                    // columns in front of the tile are another one's
+                    const int at = !ACROSS ? (int)(16 * c + j) : ENDS == Ends::any ? col + (int)c : (int)(kC * j + c);
+                    if (!ACROSS || ENDS != Ends::any || (at >= 0 && kC * j < width)) part[wave][4 * q + v][h * NT + at] = acc[h][c][v];
+                }
     }
     __syncthreads();
     const u32 row = threadIdx.x / NT, c = threadIdx.x % NT;
@@ -123,13 +151,13 @@ __global__ __launch_bounds__(512, 4) void gated_few_kernel(const GatedArgs r)
     }
 }
 
-template <class T, u32 NT, bool ACROSS, bool WHOLE>
+template <class T, u32 NT, bool ACROSS, Ends ENDS>
 hipError_t few_go(GatedArgs r, hipStream_t stream)
 {
     r.col_tiles = (r.n + NT - 1) / NT;
     r.tiles = (u32)(max_runs(r.rows, r.blocks, kRows) * r.col_tiles);
-    if (r.dy) hipLaunchKernelGGL((gated_few_kernel<T, NT, ACROSS, WHOLE, true>), dim3(r.tiles), dim3(512), 0, stream, r);
-    else hipLaunchKernelGGL((gated_few_kernel<T, NT, ACROSS, WHOLE, false>), dim3(r.tiles), dim3(512), 0, stream, r);
+    if (r.dy) hipLaunchKernelGGL((gated_few_kernel<T, NT, ACROSS, ENDS, true>), dim3(r.tiles), dim3(512), 0, stream, r);
+    else hipLaunchKernelGGL((gated_few_kernel<T, NT, ACROSS, ENDS, false>), dim3(r.tiles), dim3(512), 0, stream, r);
     return hipGetLastError();
 }
 // Outputs of a workgroup: 32 where that fills the compute units (512 rows, one block of 1024 -> 1024 in float32, 32 / 16 outputs: 46 / 54 us), 16
@@ -142,9 +170,13 @@ template <class T, bool ACROSS>
 hipError_t few_width(const GatedArgs &r, hipStream_t stream)
 {
     constexpr u32 v = ACROSS ? 4 : 16 / sizeof(T);          // a run of x, and of the weights
-    const bool whole = r.k % v == 0 && (!ACROSS || r.n % v == 0);
-    if (few_columns(r) == 32) return whole ? few_go<T, 32, ACROSS, true>(r, stream) : few_go<T, 32, ACROSS, false>(r, stream);
-    return whole ? few_go<T, 16, ACROSS, true>(r, stream) : few_go<T, 16, ACROSS, false>(r, stream);
+    const bool wide = few_columns(r) == 32;
+    const Ends sums = ends_of(r.k, v), cols = ACROSS && wide ? ends_of(r.n, 2) : Ends::whole;
+    const bool single = sizeof(T) == 4 && !ACROSS && sums == Ends::any && r.k < 48;         // as in grouped_few.hip
+    if (single || sums == Ends::early || cols == Ends::early)
+        return wide ? few_go<T, 32, ACROSS, Ends::early>(r, stream) : few_go<T, 16, ACROSS, Ends::early>(r, stream);
+    if (sums == Ends::any || cols == Ends::any) return wide ? few_go<T, 32, ACROSS, Ends::any>(r, stream) : few_go<T, 16, ACROSS, Ends::any>(r, stream);
+    return wide ? few_go<T, 32, ACROSS, Ends::whole>(r, stream) : few_go<T, 16, ACROSS, Ends::whole>(r, stream);
 }
 
 // ---- dx, dW and db of few rows from the gradients of both projections in 32 bits, [rows][2 n]: one launch, since what a launch costs is more than
@@ -175,7 +207,7 @@ struct FewGrads {
 template <bool FOUR> __device__ __forceinline__ u32 four_from(u32 i, u32 count) { return FOUR && i + 4 > count ? count - 4 : i; }
 template <bool FOUR, class T> __device__ __forceinline__ Run<T, 4> load_four(const T *p, u32 i, u32 count)
 {
-    return FOUR ? load_any<Run<T, 4>>(p + i) : load_run<T, 4, false>(p, i, count);
+    return FOUR ? load_any<Run<T, 4>>(p + i) : load_run<T, 4, Ends::early>(p, i, count);
 }
 
 template <class T, u32 NT, bool IN_MAJOR, bool FOUR>
@@ -218,7 +250,7 @@ __device__ __forceinline__ void few_dx(const FewGrads &r, float (&part)[8][kRows
                     for (u32 e = 0; e < V; ++e) {
                         const u32 o = at + e < r.n2 ? at + e : r.n2 - 1;
                         if constexpr (FOUR) across[a][e] = load_any<Run<T, kC>>(w + (u64)o * r.ldw + col);
-                        else across[a][e] = load_run<T, kC, false>(w + (u64)o * r.ldw, col, r.k);
+                        else across[a][e] = load_run<T, kC, Ends::early>(w + (u64)o * r.ldw, col, r.k);
                     }
                 }
             }

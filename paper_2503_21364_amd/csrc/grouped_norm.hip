@@ -119,29 +119,6 @@ template <u32 G, u32 N> struct RowSums {
     }
 };
 
-// Four values (eight of bfloat16) moved down by d places, zeros behind them; eight and more: zeros
-__device__ __forceinline__ f32x4 moved(f32x4 v, u32 d)
-{
-    if (d == 0) return v;
-    return f32x4{d == 1 ? v[1] : d == 2 ? v[2] : d == 3 ? v[3] : 0.0f, d == 1 ? v[2] : d == 2 ? v[3] : 0.0f, d == 1 ? v[3] : 0.0f, 0.0f};
-}
-__device__ __forceinline__ bf16x8 moved(bf16x8 v, u32 d)
-{
-    typedef __attribute__((ext_vector_type(2))) u64 u64x2;
-    const u64x2 b = __builtin_bit_cast(u64x2, v);
-    u64 lo = b[0], hi = b[1];
-    if (d >= 8) {
-        lo = hi = 0;
-    } else if (d >= 4) {
-        lo = hi >> (16 * (d - 4));
-        hi = 0;
-    } else if (d > 0) {
-        lo = lo >> (16 * d) | hi << (64 - 16 * d);
-        hi >>= 16 * d;
-    }
-    return __builtin_bit_cast(bf16x8, u64x2{lo, hi});
-}
-
 // Chunk c of this lane: columns (c G + lane) V and on.  No load has a condition of its own, which would be waited for one after the other: what
 // would reach beyond the row is read as its last whole vector, and moved into place when it is used.
 template <class T, u32 G, u32 C> struct RowOf {

@@ -443,3 +443,16 @@ def test_many_sets_of_few_sums(k, n):
     t.check_backward(which=("db",))
     t.backward(which=("dw",))
     t.check_backward(which=("dw",))
+
+
+# few rows: rows that end inside a vector, before the first one does, and in its last value; columns likewise, by tiles of 16 and of 64
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("in_major", [False, True])
+@pytest.mark.parametrize("sizes", [[1], [3, 0, 17], [2] * 70])
+def test_few_rows_however_their_vectors_end(sizes, in_major, dtype):
+    for k, n in ((1, 1), (2, 3), (3, 65), (5, 67), (7, 130), (9, 2), (15, 129), (17, 66), (31, 131), (47, 70), (49, 33), (66, 1), (127, 18), (130, 257), (515, 67)):
+        t = Layer(sizes, k, n, dtype, in_major, pad=3, front=1, behind=2, seed=k + n)
+        t.forward()
+        t.check_forward()
+        t.backward()
+        t.check_backward()

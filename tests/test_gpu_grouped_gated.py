@@ -367,3 +367,16 @@ def test_gelu_keeps_its_digits_far_below_zero(dtype, rows, k, n):
     db = _np(t.db[0])
     assert (np.abs(db[n:] - a * p) <= np.abs(a * p) * 14 * u24).all()
     assert (np.abs(db[:n] - (p + a * d)) <= (p + np.abs(a) * d) * 15 * u24).all()
+
+
+# rows that end inside a vector, before the first one does, and in its last value; outputs likewise, by tiles of 16 and of 32; NaN behind every row
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("in_major", [False, True])
+@pytest.mark.parametrize("sizes", [[1], [3, 0, 17], [2] * 170])
+def test_few_rows_however_their_vectors_end(sizes, in_major, dtype):
+    for k, n in ((1, 1), (2, 3), (3, 65), (5, 33), (7, 70), (9, 2), (15, 69), (17, 66), (31, 35), (47, 34), (49, 33), (66, 1), (127, 18), (130, 97), (515, 67)):
+        t = Layer(sizes, k, n, dtype, in_major, pad=3, front=1, behind=2, seed=k + n, wpad=5)
+        t.forward()
+        t.check_forward()
+        t.backward()
+        t.check_backward()

@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256, 4) void sums_kernel(const SumsArgs r)
                 const u32 row = wave / 2 * 32 + row_of(v, hi);
                 if (row >= height || col >= width) continue;
                 const u64 at = r.in_major ? (u64)(k0 + col) * r.n + n0 + row : (u64)(n0 + row) * r.k + k0 + col;
-                if (r.dw16 && run.whole) reinterpret_cast<__bf16 *>(r.dw)[(u64)run.block * size + at] = (__bf16)acc[v];
+                if (sizeof(T) == 2 && r.dw16 && run.whole) reinterpret_cast<__bf16 *>(r.dw)[(u64)run.block * size + at] = (__bf16)acc[v];
                 else dw[at] = acc[v];
             }
         }
@@ -175,8 +175,9 @@ __global__ __launch_bounds__(256) void join_kernel(const u32 *__restrict__ offse
     }
     for (u64 i = at; i < at + V && i < stride; ++i) {
         if (i < size ? !dw : !db) continue;
-        if (i < size) dw[(u64)block * size + i] = (D)sum(0.0f, i);
-        else db[(u64)block * n + (i - size)] = sum(0.0f, i);
+        const float s = sum(0.0f, i);
+        if (i < size) dw[(u64)block * size + i] = (D)s;
+        else db[(u64)block * n + (i - size)] = s;
     }
 }
 

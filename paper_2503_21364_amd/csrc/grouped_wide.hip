@@ -237,7 +237,8 @@ template <u32 W, u32 WAVES> struct Codes16 {
 
 // Tiles of dw over a slice of the rows: P = x (inputs), Q = dy (outputs).  db rides on the tiles of the first inputs: a
 // matrix instruction with ones in the place of x, the wavefronts along P taking turns.
-template <class S, u32 TP, u32 TQ, u32 WP, bool CODES, bool ANY>
+// DW16: dw in bfloat16.
+template <class S, u32 TP, u32 TQ, u32 WP, bool CODES, bool ANY, bool DW16>
 __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArgs r)
 {
     extern __shared__ __align__(16) char wide_lds[];
@@ -290,7 +291,7 @@ __global__ __launch_bounds__(S::kThreads, 2) void wide_sums_kernel(const SumsArg
             for (u32 i = 0; i < S::kP; ++i) {
                 const u32 k = k0 + p0 + 16 * i + 4 * (lane >> 4);
                 if (k >= r.k) continue;
-                if (r.dw16 && run.whole) {
+                if (DW16 && run.whole) {
                     __bf16 *dw16 = reinterpret_cast<__bf16 *>(r.dw) + (u64)run.block * size;
                     if (r.in_major || (ANY && k + 4 > r.k)) {
 #pragma unroll
@@ -375,7 +376,9 @@ hipError_t wide_sums_go(SumsArgs r, bool codes, hipStream_t stream)
     r.n_tiles = (r.n + TQ - 1) / TQ;
     r.k_tiles = (r.k + TP - 1) / TP;
     r.tiles = (u32)((u64)r.slices * r.n_tiles * r.k_tiles);
-    auto kernel = codes ? wide_sums_kernel<S, TP, TQ, WP, true, ANY> : wide_sums_kernel<S, TP, TQ, WP, false, ANY>;
+    // gated layers alone have dw in bfloat16, and no codes
+    auto kernel = codes ? wide_sums_kernel<S, TP, TQ, WP, true, ANY, false>
+                  : r.dw16 ? wide_sums_kernel<S, TP, TQ, WP, false, ANY, true> : wide_sums_kernel<S, TP, TQ, WP, false, ANY, false>;
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)S::kLds);
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(kernel, dim3(r.tiles), dim3(S::kThreads), S::kLds, stream, r);

@@ -339,16 +339,19 @@ bool rows_sixteen(const RowsArgs &r)
 // for half of the results, and the two even out what a last round leaves.  8 ragged blocks of 1024 x 1024, large / small tiles: 4096 rows
 // 30 / 20 us, 16 384 56 / 48, 65 536 158 / 183; one of 512 x 512: 16 384 20 / 14, 32 768 23 / 31.
 // 256 columns x 192 rows, 0.82 of the time of 256 x 256 for three quarters of the results, where a last round of those would be nearly empty and
-// this leaves a tenth (dx of 16 384 rows of 4 ragged blocks, 8192 -> 2048: 128 x 128 593 us, 256 x 192 490; of even blocks 256 x 256 406).
+// this leaves a tenth, ends of all ragged blocks counted (dx of 16 384 rows of 4 ragged blocks, 8192 -> 2048: 128 x 128 593 us, 256 x 192 487; of even
+// blocks 256 x 256 406).  48 drawn sizes of one to three rounds and 512 sums or more, up to 48 blocks: 0.88 of the others' time in the mean, 0.72 to
+// 1.01.  Of fewer sums (memory is most of them) or more rounds a fifth of the sizes took 2 to 11 % more.
 struct RowsTile {
     u32 cols, rows;
 };
 RowsTile rows_tile(const RowsArgs &r, bool gate)
 {
-    const auto share = [&](u32 cols, u32 rows) { return __builtin_ceilf((float)r.rows / rows + 0.5f * (r.blocks - 1)) * ((r.cols + cols - 1) / cols); };
-    const float large = __builtin_ceilf(share(256, 256) / 256), small = 0.7f * share(128, 128) / 512;
-    const float between = 0.82f * __builtin_ceilf(share(256, 192) / 256);
-    if (!gate && between < 0.9f * (large < small ? large : small)) return RowsTile{256, 192};
+    const auto share = [&](u32 cols, u32 rows, float ends) { return __builtin_ceilf((float)r.rows / rows + ends) * ((r.cols + cols - 1) / cols); };
+    const float some = 0.5f * (r.blocks - 1), all = r.blocks > 1 ? 0.5f * r.blocks : 0.0f;
+    const float large = __builtin_ceilf(share(256, 256, some) / 256), small = 0.7f * share(128, 128, some) / 512;
+    const float between = 0.82f * __builtin_ceilf(share(256, 192, all) / 256);
+    if (!gate && r.sums >= 512 && large <= 3 && between < 0.9f * (large < small ? large : small)) return RowsTile{256, 192};
     return large < small ? RowsTile{256, 256} : RowsTile{128, 128};
 }
 

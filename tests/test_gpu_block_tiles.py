@@ -162,3 +162,22 @@ def test_gradients_of_gated_layers_tile_after_tile(sizes, front, behind, n, k, p
             assert torch.equal(got, right), (g, (got != right).nonzero()[:4].tolist())
     if pad:
         assert (dx.as_strided((t.rows, pad), dx.stride(), k) == 7.0).all()
+
+
+@pytest.mark.parametrize("k", [512, 520, 1000])
+def test_layers_in_tiles_of_192_rows(k):
+    # a size whose tiles of 256 x 256 would leave a last round nearly empty, of 512 sums and more: forward, and the same product as dx
+    n, (off, offsets) = 4096, _offsets([2999, 1, 0, 5289], 1)
+    rows = off[-1] + 10
+    x, w = _whole((rows, k), 7, 1).to(torch.bfloat16), _whole((4, n, k), 8, 1).to(torch.bfloat16)
+    b = _whole((4, n), 9, 9)
+    y, dx = (torch.full((rows, n), 7.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    B.grouped_linear(x, w, offsets, y, bias=b, relu=True)
+    ws = torch.empty(B.grouped_linear_backward_bytes(rows, 4, k, n, torch.bfloat16), dtype=torch.uint8, device=DEV)
+    B.grouped_linear_backward(x, w.transpose(1, 2).contiguous(), offsets, ws, dx=dx)
+    want, plain = (torch.zeros((rows, n), dtype=torch.float64, device=DEV) for _ in range(2))
+    for g, s, e in _blocks(off):
+        plain[s:e] = x[s:e].double() @ w[g].double().t().contiguous()
+        want[s:e] = (plain[s:e] + b[g].double()).clamp(min=0)
+    assert torch.equal(y.double(), _rounded(want, "bf16"))
+    assert torch.equal(dx.double(), _rounded(plain, "bf16"))

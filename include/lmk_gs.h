@@ -487,7 +487,7 @@ int32_t lmk_gs_grouped_gated(const lmk_gs_linear *layer, const void *x, uint64_t
 typedef struct lmk_gs_gated_grads {
     void *dx;        /* [rows][k], rows lddx apart, dtype                                                       */
     uint64_t lddx;
-    void *dw;        /* laid out as w, dense ([blocks][2 n][k] or [blocks][k][2 n]), dtype, aligned to 4 bytes      */
+    void *dw;        /* laid out as w, dense ([blocks][2 n][k] or [blocks][k][2 n]), dtype (lmk_gs_linear_grads.dw is float32), aligned to 4 bytes */
     float *db;       /* [blocks][2 n]                                                                            */
 } lmk_gs_gated_grads;
 
@@ -496,14 +496,16 @@ typedef struct lmk_gs_gated_grads {
 int32_t lmk_gs_grouped_gated_backward_bytes(const lmk_gs_linear *layer, size_t *bytes);
 
 /* From dy [rows][n], the gradient of y, and the input x (a and u are computed again).  The gradients of a and u are rounded to dtype
- * before dx and dw are summed from them in 32 bits (not where rows are few); db is summed from them before that.  Sums over a block's rows are
+ * before dx and dw are summed from them in 32 bits (not where rows are few): in bfloat16 dx and dw are off by that rounding, 2^-8 of each term at most,
+ * beside their own; db is summed from them before that.  Sums over a block's rows are
  * taken in an order that depends on the sizes and alignments only.  workspace: 256-byte aligned, always needed.  Outputs must not overlap inputs.  Errors as
  * lmk_gs_grouped_gated; LMK_GS_ERR_CAPACITY: workspace too small. */
 int32_t lmk_gs_grouped_gated_backward(const lmk_gs_linear *layer, const void *dy, uint64_t lddy, const void *x, uint64_t ldx,
                                       const float *bias, uint32_t act, const lmk_gs_gated_grads *out, void *workspace,
                                       size_t workspace_bytes, void *stream);
 
-/* ---- Layers of blocks in 4 bits: weights that stay resident in a quarter of bfloat16's bytes, and inputs taken to 4 bits for the product.
+/* ---- Layers of blocks in 4 bits: weights that stay resident in 64 ceil(k / 128) + 16 ceil(k / 512) bytes a row (0.27 of bfloat16's where rows are long, 0.31
+ * at 128 inputs, more than bfloat16's below 40), and inputs taken to 4 bits for the product.
  *
  * The 4-bit form of a matrix of `rows` rows of k values: 32 consecutive values of a row share a power of two.  With A the
  * largest |x| of the 32: the step is 2^e, e the least exponent >= -126 for which A / 2^e < 7, but at most 125; the code of x is the nearest of 0, 1/2, 1,

@@ -5,8 +5,9 @@
 // The gradients keep nothing of the forward pass: a kernel takes both projections again and writes their gradients
 //     da = dy u act'(a),  du = dy act(a)
 // side by side, [rows][2 n], in the workspace; from there dx = [da du] W and dW = [da du]^T x are the grouped layers' own products.
-// In bfloat16 da and du are rounded there (the matrix instructions take nothing wider), so that a dW in 32 bits would hold that rounding
-// at twice the bytes: it has the weights' type.  The bias' gradient does not go through them: it is summed in 32 bits beside the
+// In bfloat16 da and du are rounded there: the matrix instructions take nothing wider, and two bfloat16 for each would be twice the products of dx
+// and dW (some 900 us more at 16 384 rows of 2048 -> 4096 in 4 blocks, now 1500).  It costs as much as the results' own rounding (2.3e-3 altogether, without
+// it 1.7e-3).  dW has the weights' type, half the bytes of 32 bits; who adds up many calls' adds in float32.  The bias' gradient does not go through them: it is summed in 32 bits beside the
 // activation, before the rounding.  Few rows (grouped_gated_few.hip) and small float32 matrices (grouped_gated_narrow.hip) have da and du in 32 bits.
 //
 // Kernel here: v_mfma_f32_32x32x2_f32, tiles of 64 rows x 64 outputs of both projections, the rows' part of LDS being read for both.  Bound by

@@ -2,8 +2,8 @@
 // gate and the next 16 of the other projection, in turns.  A lane then has both projections of the same four outputs in neighbouring
 // accumulators, and the activation, the product and their gradients need no exchange.
 //
-// Bound by the bfloat16 instructions and by LDS: y of 8192 rows of 8192 -> 4096 at 1446 TFLOP/s, of 16 384 rows of 2048 -> 4096 in 4 blocks at 1331;
-// 65 536 rows of 1024 -> 2048 in 32 blocks 499 us (1101): a block's weights are read by eight or nine tiles of rows only, and a tile has 32 steps
+// Bound by the bfloat16 instructions and by LDS: y of 8192 rows of 8192 -> 4096 at 1446 TFLOP/s, of 16 384 rows of 2048 -> 4096 in 4 even blocks at 1370 (SiLU; GELU 1260);
+// 65 536 rows of 1024 -> 2048 in 32 even blocks 491 us (1120), in ragged ones 510 to 546: a block's weights are read by eight or nine tiles of rows only, and a tile has 32 steps
 // between its first loads and its last stores.  The gradients of both projections of the second take 545 us: the activation's arithmetic and two
 // results for each of y's, with nothing of the products beside them.
 #include "grouped_gated.h"

@@ -2,8 +2,9 @@
 // v_mfma_scale_f32_16x16x128_f8f6f4.  A lane feeds 32 codes, 16 bytes, of one row and their scale byte; the products of codes and powers of two are
 // exact, sums are in 32 bits.
 //
-// 8192 x 8192 x 8192 262 us, 4.2 PFLOP/s; 65 536 rows of 2048 -> 2048 in 16 blocks 171 us of the same inputs (3.2) and 196 to 216 of others (268 MB
-// of results in bfloat16 alone take 52).  Bound by LDS and its loads: a step's fragments and scales take it as long as their products take the
+// 8192 x 8192 x 8192 258 us, 4.3 PFLOP/s; 65 536 rows of 2048 -> 2048 in 16 even blocks 171 us (3.2; 268 MB of results in bfloat16 alone take 52), in
+// ragged ones, whose last tiles are partly empty, 186 of the same inputs again and again, 188 to 195 behind their packing, 207 of others, 213 behind a
+// fill of 268 MB.  Bound by LDS and its loads: a step's fragments and scales take it as long as their products take the
 // matrix instructions, which reach 7 PFLOP/s by themselves.
 #include "block4.h"
 #include "grouped_wide.h"

@@ -16,8 +16,8 @@
 // over it goes from lane to lane without LDS (G <= 64), or through LDS once a sum.  A workgroup has a run of rows of one block,
 // so that gain and shift are in registers, and so are its sums of dgain and dshift: x and dy are read once for all three gradients.
 //
-// The same inputs again and again: 65 536 rows of 1024 in 32 blocks, bfloat16, 52 us (5.2 TB/s), all gradients 91 (4.4 TB/s); 300 000 x 96 in 24,
-// float32, 38 (6.0 TB/s; 52 with other inputs every time); 4744 x 4033 in 7, bfloat16, 20, gradients 45: there are four rows a workgroup, and a
+// The same inputs again and again: 65 536 rows of 1024 in 32 blocks, bfloat16, 49 us (5.4 TB/s), all gradients 91 (4.4 TB/s); 300 000 x 96 in 24,
+// float32, 38 (6.0 TB/s; 52 with other inputs every time); 4744 x 4033 in 7, bfloat16, 19, gradients 44: there are four rows a workgroup, and a
 // row's two meetings stand behind its loads; one row of 1024 3.0, a chain of latencies.  Sums leave as vectors: with 4 bytes a lane those gradients
 // took 55.
 #include "grouped_kernels.h"

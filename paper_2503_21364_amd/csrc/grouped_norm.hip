@@ -51,7 +51,8 @@ __device__ __forceinline__ bool held(float squares) { return squares < __builtin
 // less than 2^-16 of it, beside which d - off is nothing.
 __device__ __forceinline__ float variance(float square, float off)
 {
-    return __builtin_fmaxf(__builtin_fmaf(-off, off, square), off * off * 0x1p-16f);
+    const float var = __builtin_fmaf(-off, off, square), least = off * off * 0x1p-16f;
+    return var < least ? least : var;                       // NaN stays
 }
 // 1 / deviation of d.  0: a row of one value, and nothing of eps is left at this scale; d is 0, too
 __device__ __forceinline__ float rate_of(float var, float eps, float scale)

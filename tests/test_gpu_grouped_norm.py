@@ -318,3 +318,19 @@ def test_rows_of_large_values_in_place(k):
     t.y = t.x
     t.forward()
     _close(t.y, *N.forward(x, t.offsets, _np(t.gain), _np(t.shift)), "f32", "y in the place of x")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [9, 96, 1000, 5000, 20_000])
+@pytest.mark.parametrize("eps", [1e-5, 1e6])
+def test_rows_that_are_not_finite_are_nan_whatever_eps_is(eps, k, dtype):
+    # of an eps that is left at the scale of large rows, too, where it is all there is beside what is no number
+    t = Case([4, 2], k, dtype, seed=35)
+    t.x[1, k // 2] = float("inf")
+    t.x[2, 0] = float("-inf")
+    t.x[4, k - 1] = float("nan")
+    t.forward(eps=eps)
+    t.backward(eps=eps)
+    bad = torch.tensor([False, True, True, False, True, False], device=DEV)
+    for got in (t.y, t.dx):
+        assert torch.isnan(got[bad]).all() and torch.isfinite(got[~bad]).all()

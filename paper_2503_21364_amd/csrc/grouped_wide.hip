@@ -340,8 +340,8 @@ bool rows_sixteen(const RowsArgs &r)
 // 30 / 20 us, 16 384 56 / 48, 65 536 158 / 183; one of 512 x 512: 16 384 20 / 14, 32 768 23 / 31.
 // 256 columns x 192 rows, 0.82 of the time of 256 x 256 for three quarters of the results, where a last round of those would be nearly empty and
 // this leaves a tenth, ends of all ragged blocks counted (dx of 16 384 rows of 4 ragged blocks, 8192 -> 2048: 128 x 128 593 us, 256 x 192 487; of even
-// blocks 256 x 256 406).  48 drawn sizes of one to three rounds and 512 sums or more, up to 48 blocks: 0.88 of the others' time in the mean, 0.72 to
-// 1.01.  Of fewer sums (memory is most of them) or more rounds a fifth of the sizes took 2 to 11 % more.
+// blocks 256 x 256 406).  65 sizes of one to three rounds and 512 sums or more, up to 48 blocks: 0.88 of the others' time in the mean, 0.72 to
+// 1.01.  Of fewer sums (memory is most of them) or more rounds a quarter of 45 sizes took 2 to 11 % more.
 struct RowsTile {
     u32 cols, rows;
 };
